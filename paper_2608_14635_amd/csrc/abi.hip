@@ -19,6 +19,7 @@
 #include "kvr_verify.h"
 #include "kvr_reuse.h"
 #include "kvr_profile.h"
+#include "host.h"
 #include "launch.h"
 
 using namespace kvr;
@@ -44,7 +45,7 @@ kv_status ok() {
 
 }  // namespace
 
-// error reporting for the other host files of the library (ipc.hip)
+// error reporting for the other host files of the library
 namespace kvr_err {
 kv_status set(kv_status st, const char* fmt, ...) {
   char buf[512];
@@ -58,12 +59,7 @@ kv_status set(kv_status st, const char* fmt, ...) {
 kv_status clear() { return ok(); }
 }  // namespace kvr_err
 
-namespace {
-
-int64_t elem_bytes(int32_t dtype) { return dtype == KV_BF16 ? 2 : 4; }
-int64_t round_up(int64_t v, int64_t a) { return (v + a - 1) / a * a; }
-
-kv_status check_desc(const kv_model_desc* d) {
+kv_status kvr::check_desc(const kv_model_desc* d) {
   if (!d) return fail(KV_EINVAL, "null model description");
   if (d->num_layers <= 0 || d->hidden <= 0 || d->num_q_heads <= 0 || d->num_kv_heads <= 0 ||
       d->head_dim <= 0 || d->ffn_dim <= 0 || d->vocab <= 0)
@@ -94,6 +90,8 @@ kv_status check_desc(const kv_model_desc* d) {
   }
   return KV_OK;
 }
+
+namespace {
 
 bool same_desc(const kv_model_desc& a, const kv_model_desc& b) {
   return a.num_layers == b.num_layers && a.hidden == b.hidden && a.num_q_heads == b.num_q_heads &&
@@ -181,29 +179,6 @@ struct Wave {
 
 }  // namespace
 
-struct kv_arena {
-  void* base;
-  uint64_t bytes;
-  kv_model_desc desc;
-  int32_t block_size;
-  int64_t num_blocks;
-  int32_t device;
-  int* probe_flag;
-  // pinned host staging for metadata uploads; reused after its last copy completed
-  void* pinned = nullptr;
-  size_t pinned_bytes = 0;
-  hipEvent_t staged = nullptr;
-  bool staged_pending = false;
-  // optional per-kernel-class timing
-  bool profile = false;
-  std::vector<std::pair<int, std::pair<hipEvent_t, hipEvent_t>>> prof_pending;
-  std::vector<hipEvent_t> prof_pool;
-  double prof_ms[KV_PROF_CLASSES] = {};
-  int64_t prof_launches[KV_PROF_CLASSES] = {};
-  double prof_flops[KV_PROF_CLASSES] = {};
-  std::vector<double> pending_flops;
-};
-
 struct kv_plan {
   kv_arena* arena;
   char* ws;
@@ -219,30 +194,19 @@ namespace {
 std::mutex g_reg_mu;
 std::set<const void*> g_arenas, g_plans;
 
-bool live_arena(const kv_arena* a) {
-  std::lock_guard<std::mutex> g(g_reg_mu);
-  return a && g_arenas.count(a);
-}
 bool live_plan(const kv_plan* p) {
   std::lock_guard<std::mutex> g(g_reg_mu);
   return p && g_plans.count(p);
 }
 
-struct DeviceGuard {
-  int prev = -1;
-  bool changed = false;
-  hipError_t err = hipSuccess;
-  explicit DeviceGuard(int dev) {
-    err = hipGetDevice(&prev);
-    if (err == hipSuccess && prev != dev) {
-      err = hipSetDevice(dev);
-      changed = err == hipSuccess;
-    }
-  }
-  ~DeviceGuard() {
-    if (changed) (void)hipSetDevice(prev);
-  }
-};
+}  // namespace
+
+bool kvr::live_arena(const kv_arena* a) {
+  std::lock_guard<std::mutex> g(g_reg_mu);
+  return a && g_arenas.count(a);
+}
+
+namespace {
 
 // starts may be null (every request from position 0).  Rules for starts:
 // 0 <= start <= len, start a multiple of 8 unless equal to len.  Blocks:

@@ -12,14 +12,9 @@
 #include <mutex>
 #include <string>
 
+#include "host.h"
 #include "kvr.h"
 #include "kvr_ipc.h"
-
-// the calling thread's error message, shared with the rest of the library
-namespace kvr_err {
-kv_status set(kv_status st, const char* fmt, ...);
-kv_status clear();
-}  // namespace kvr_err
 
 namespace {
 

@@ -1,4 +1,4 @@
-// Kernel launch interface between the host planner (abi.cpp) and the device
+// Kernel launch interface between the host planner (abi.hip) and the device
 // code.  Plain structs of device pointers and sizes; no HIP types beyond
 // hipStream_t.
 #pragma once

@@ -1,5 +1,6 @@
 """Thin ctypes binding of libkvr.so (include/kvr.h, include/kvr_decode.h,
-include/kvr_ipc.h, include/kvr_verify.h, include/kvr_reuse.h, include/kvr_profile.h).
+include/kvr_ipc.h, include/kvr_verify.h, include/kvr_reuse.h, include/kvr_profile.h,
+include/kvr_tables.h).
 
 Argument marshalling only: every step of the rebuild runs in the library's
 HIP kernels.  Device buffers are passed as integer addresses (for example a
@@ -122,6 +123,9 @@ def lib() -> C.CDLL:
     L.kv_verify.argtypes = [vp, i32p, C.c_int32, i32p, C.c_int32, vp, vp, C.c_uint64, vp, vp, vp]
     L.kv_verify_noalloc.restype = C.c_int
     L.kv_verify_noalloc.argtypes = [vp, i32p, C.c_int32, i32p, C.c_int32, vp, vp, vp, vp]
+    L.kv_tables_grow.restype = C.c_int
+    L.kv_tables_grow.argtypes = [vp, vp, C.c_int32, C.c_int32, vp, C.c_int32, vp, C.c_int32, C.c_int64, vp, vp,
+                                 vp, vp, C.c_int32, vp]
     hp = C.POINTER(kv_ipc_handle)
     L.kv_ipc_export.restype = C.c_int
     L.kv_ipc_export.argtypes = [vp, C.c_uint64, hp]
@@ -360,6 +364,16 @@ def kv_verify_noalloc(arena: int, lens, tables, committed: int, intact: int, dig
                                    C.c_void_p(digests or None), C.c_void_p(intact)))
 
 
+def kv_tables_grow(held: int, lens: int, num_requests: int, block_size: int, free_blocks: int, num_free: int,
+                   tables: int, max_blocks: int, max_rows: int, row_offsets: int, slots: int, positions: int,
+                   counts: int, device: int = 0, stream: int = 0) -> None:
+    """Block tables grown and slots listed on the GPU; every array is a device address."""
+    _check(lib().kv_tables_grow(C.c_void_p(held or None), C.c_void_p(lens), num_requests, block_size,
+                                C.c_void_p(free_blocks), num_free, C.c_void_p(tables), max_blocks, max_rows,
+                                C.c_void_p(row_offsets), C.c_void_p(slots), C.c_void_p(positions or None),
+                                C.c_void_p(counts), device, C.c_void_p(stream)))
+
+
 def kv_ipc_export(ptr: int, nbytes: int) -> bytes:
     """Owner side: the handle of device memory [ptr, ptr+nbytes) as plain bytes."""
     h = kv_ipc_handle()
@@ -420,4 +434,4 @@ def exported_symbols() -> Iterable[str]:
             "kv_ipc_export", "kv_ipc_owner_alive", "kv_ipc_open", "kv_ipc_close",
             "kv_verify_workspace_bytes", "kv_block_digests", "kv_verify", "kv_verify_noalloc",
             "kv_rebuild_from_workspace_bytes", "kv_rebuild_from_check", "kv_rebuild_from",
-            "kv_rebuild_stage_from")
+            "kv_rebuild_stage_from", "kv_tables_grow")
