@@ -1,0 +1,89 @@
+/*
+ * kvr_packed.h -- K/V held in 4 bits: a packed arena beside the retained one.
+ *
+ * The replacement worker keeps K/V in a retained arena (kvr.h).  A packed arena
+ * holds the same rows in 17/64 of the bf16 bytes: interrupted or waiting requests
+ * are parked in it and brought back, and generation can attend (and resume) over
+ * it directly.  Same conventions as kvr.h (status codes, host/device pointers,
+ * void* streams, host-side validation before any device work, thread-compatible:
+ * calls on one packed arena must not overlap where one of them writes it).
+ *
+ * Values.  The head dim's elements are taken 32 at a time.  A group's scale is the
+ * least power of two 2^e, -120 <= e <= 125, with max|x| <= 6 * 2^e; each x is held
+ * as a sign and the nearest of {0, 0.5, 1, 1.5, 2, 3, 4, 6} to |x| / 2^e, ties to
+ * the even code (0, 1, 2, 4).  A group with a value that is not finite reads as NaN
+ * in all 32.
+ *
+ * Layout.  Per layer, block, kv head and tile of 16 slots one record of 17 d bytes:
+ *   record(l, b, h, t) = (((l*num_blocks + b)*nkv + h)*(block_size/16) + t) * 17 d
+ *   K values  at 0        [16 slots][d/2]
+ *   V values  at 8 d      [4][16][4][d/32]: slots 4i .. 4i+3, sixteenth of the dims, slot
+ *   K scales  at 16 d     [16 slots][d/32]
+ *   V scales  at 16.5 d   [4][d/32][4]: slots 4i .. 4i+3, group, slot
+ * A byte of values holds two of them, the even dim in the low four bits: 8 for the
+ * sign and 0 .. 7 for the magnitudes above.  A scale byte holds e + 127, 255 for NaN.
+ * (A record is what one wave of the attention reads in one go: a tile's K and V
+ * values are two contiguous loads of 16 bytes a lane at d = 128, each lane's bytes
+ * already those of its matrix operand.)
+ */
+#ifndef KVR_PACKED_H
+#define KVR_PACKED_H
+
+#include <stdint.h>
+
+#include "kvr.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+typedef struct kv_packed* kv_packed_t;
+
+/* Bytes of a packed arena; 0 for an invalid description (kvr.h's rules, and
+ * head_dim % 32 == 0), a block_size that is not a positive multiple of 16, or
+ * num_blocks <= 0. */
+uint64_t kv_packed_bytes(const kv_model_desc* desc, int32_t block_size, int64_t num_blocks);
+
+/* Bind a packed arena: `base` is device memory on `device`, on a boundary of 16
+ * bytes, of at least kv_packed_bytes bytes.  Checked like kv_arena_bind's, health
+ * probe included; never written.  *out receives the handle. */
+kv_status kv_packed_bind(void* base, uint64_t bytes, const kv_model_desc* desc,
+                         int32_t block_size, int64_t num_blocks, int32_t device,
+                         kv_packed_t* out);
+/* Drop a handle.  Never frees or writes `base`. */
+kv_status kv_packed_release(kv_packed_t packed);
+
+/* Store K/V rows of one layer.
+ *   k, v        device [rows][nkv][d] in the model dtype, rows k_stride / v_stride
+ *               elements apart (even ones in bf16)
+ *   slots       device int64 [rows]: row i goes to slot slots[i] = block *
+ *               block_size + position % block_size (as kv_tables_grow lists them);
+ *               rows whose slot lies outside the arena (-1, say) are passed over.
+ *               A slot listed more than once holds undefined values afterwards.
+ * Writes exactly the listed slots of the layer. */
+kv_status kv_packed_store(kv_packed_t packed, int32_t layer, const void* k, int64_t k_stride,
+                          const void* v, int64_t v_stride, const int64_t* slots, int64_t rows,
+                          void* stream);
+/* The way back: row i of k, v receives the values slot slots[i] holds, in the
+ * model dtype (exactly: every one of them is a bf16 number).  Rows whose slot lies
+ * outside the arena keep their bits. */
+kv_status kv_packed_load(kv_packed_t packed, int32_t layer, void* k, int64_t k_stride, void* v,
+                         int64_t v_stride, const int64_t* slots, int64_t rows, void* stream);
+
+/* Park: every layer's K/V of the retained arena's slots arena_slots[i] (device
+ * int64 [rows]) into the packed arena's slots packed_slots[i].  Restore: the way
+ * back.  The two arenas describe the same model on one device; block sizes and
+ * tables are their own.  Pairs with a slot outside its arena are passed over, a
+ * destination listed more than once holds undefined values afterwards.
+ *   KV_EINVAL  null arrays, rows < 0, a stride below nkv * d, a pointer not on its
+ *              boundary
+ *   KV_ESTATE  unknown handle, arenas of different models or devices */
+kv_status kv_packed_park(kv_arena_t arena, const int64_t* arena_slots, kv_packed_t packed,
+                         const int64_t* packed_slots, int64_t rows, void* stream);
+kv_status kv_packed_restore(kv_packed_t packed, const int64_t* packed_slots, kv_arena_t arena,
+                            const int64_t* arena_slots, int64_t rows, void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif

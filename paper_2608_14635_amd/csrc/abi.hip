@@ -189,6 +189,37 @@ struct kv_plan {
   bool has_prefix;   // some request starts past position 0
 };
 
+kv_status kvr::probe_memory(const void* base, int32_t device, int** out) {
+  const char* force = getenv("KVR_DEBUG_FAIL_PROBE");
+  if (force && force[0] == '1') return fail(KV_EDEVICE, "health probe failed (forced by KVR_DEBUG_FAIL_PROBE)");
+
+  DeviceGuard dg(device);
+  if (dg.err != hipSuccess) return fail(KV_EDEVICE, "cannot select device %d: %s", device, hipGetErrorString(dg.err));
+  hipPointerAttribute_t attr;
+  hipError_t e = hipPointerGetAttributes(&attr, base);
+  if (e != hipSuccess) {
+    (void)hipGetLastError();
+    return fail(KV_EDEVICE, "arena pointer not known to HIP: %s", hipGetErrorString(e));
+  }
+  if (attr.type != hipMemoryTypeDevice || attr.device != device)
+    return fail(KV_EDEVICE, "arena pointer is not device memory on device %d", device);
+  // health probe: a kernel round trip on the device (Sec. 4.2 step 2)
+  int* flag = nullptr;
+  if ((e = hipMalloc(&flag, sizeof(int))) != hipSuccess)
+    return fail(KV_EDEVICE, "probe allocation failed: %s", hipGetErrorString(e));
+  int host_flag = 0;
+  bool good = hipMemset(flag, 0, sizeof(int)) == hipSuccess && launch_probe(flag, nullptr) == 0 &&
+              hipMemcpy(&host_flag, flag, sizeof(int), hipMemcpyDeviceToHost) == hipSuccess &&
+              host_flag == 0x600D;
+  if (!good) {
+    (void)hipGetLastError();
+    (void)hipFree(flag);
+    return fail(KV_EDEVICE, "GPU health probe failed on device %d", device);
+  }
+  *out = flag;
+  return KV_OK;
+}
+
 namespace {
 
 std::mutex g_reg_mu;
@@ -473,32 +504,10 @@ kv_status kv_arena_bind(void* base, uint64_t bytes, const kv_model_desc* desc, i
   if (need > (unsigned __int128)bytes)
     return fail(KV_EINVAL, "arena of %llu bytes is smaller than its geometry needs",
                 (unsigned long long)bytes);
-  const char* force = getenv("KVR_DEBUG_FAIL_PROBE");
-  if (force && force[0] == '1') return fail(KV_EDEVICE, "health probe failed (forced by KVR_DEBUG_FAIL_PROBE)");
-
-  DeviceGuard dg(device);
-  if (dg.err != hipSuccess) return fail(KV_EDEVICE, "cannot select device %d: %s", device, hipGetErrorString(dg.err));
-  hipPointerAttribute_t attr;
-  hipError_t e = hipPointerGetAttributes(&attr, base);
-  if (e != hipSuccess) {
-    (void)hipGetLastError();
-    return fail(KV_EDEVICE, "arena pointer not known to HIP: %s", hipGetErrorString(e));
-  }
-  if (attr.type != hipMemoryTypeDevice || attr.device != device)
-    return fail(KV_EDEVICE, "arena pointer is not device memory on device %d", device);
-  // health probe: a kernel round trip on the device (Sec. 4.2 step 2)
   int* flag = nullptr;
-  if ((e = hipMalloc(&flag, sizeof(int))) != hipSuccess)
-    return fail(KV_EDEVICE, "probe allocation failed: %s", hipGetErrorString(e));
-  int host_flag = 0;
-  bool good = hipMemset(flag, 0, sizeof(int)) == hipSuccess && launch_probe(flag, nullptr) == 0 &&
-              hipMemcpy(&host_flag, flag, sizeof(int), hipMemcpyDeviceToHost) == hipSuccess &&
-              host_flag == 0x600D;
-  if (!good) {
-    (void)hipGetLastError();
-    (void)hipFree(flag);
-    return fail(KV_EDEVICE, "GPU health probe failed on device %d", device);
-  }
+  st = probe_memory(base, device, &flag);
+  if (st != KV_OK) return st;
+  DeviceGuard dg(device);
   kv_arena* a = new (std::nothrow) kv_arena();
   if (!a) {
     (void)hipFree(flag);

@@ -39,6 +39,15 @@ struct kv_arena {
   std::vector<double> pending_flops;
 };
 
+struct kv_packed {
+  void* base;
+  uint64_t bytes;
+  kv_model_desc desc;
+  int32_t block_size;
+  int64_t num_blocks;
+  int32_t device;
+};
+
 namespace kvr {
 
 inline int64_t elem_bytes(int32_t dtype) { return dtype == KV_BF16 ? 2 : 4; }
@@ -46,6 +55,11 @@ inline int64_t round_up(int64_t v, int64_t a) { return (v + a - 1) / a * a; }
 
 kv_status check_desc(const kv_model_desc* d);
 bool live_arena(const kv_arena* a);
+bool live_packed(const kv_packed* a);
+struct PackedLayer packed_layer(const kv_packed* a, int32_t layer);
+// The checks of a bind: `base` is device memory on `device`, and a kernel's round
+// trip there succeeds (Sec. 4.2 step 2).  *flag receives the 4 bytes it used.
+kv_status probe_memory(const void* base, int32_t device, int** flag);
 
 struct DeviceGuard {
   int prev = -1;

@@ -1,6 +1,6 @@
 """Thin ctypes binding of libkvr.so (include/kvr.h, include/kvr_decode.h,
 include/kvr_ipc.h, include/kvr_verify.h, include/kvr_reuse.h, include/kvr_profile.h,
-include/kvr_tables.h).
+include/kvr_tables.h, include/kvr_packed.h).
 
 Argument marshalling only: every step of the rebuild runs in the library's
 HIP kernels.  Device buffers are passed as integer addresses (for example a
@@ -126,6 +126,17 @@ def lib() -> C.CDLL:
     L.kv_tables_grow.restype = C.c_int
     L.kv_tables_grow.argtypes = [vp, vp, C.c_int32, C.c_int32, vp, C.c_int32, vp, C.c_int32, C.c_int64, vp, vp,
                                  vp, vp, C.c_int32, vp]
+    i64 = C.c_int64
+    L.kv_packed_bytes.restype = C.c_uint64
+    L.kv_packed_bytes.argtypes = [C.POINTER(kv_model_desc), C.c_int32, i64]
+    L.kv_packed_bind.restype = C.c_int
+    L.kv_packed_bind.argtypes = [vp, C.c_uint64, C.POINTER(kv_model_desc), C.c_int32, i64, C.c_int32, C.POINTER(vp)]
+    L.kv_packed_release.restype = C.c_int
+    L.kv_packed_release.argtypes = [vp]
+    L.kv_packed_store.restype = L.kv_packed_load.restype = C.c_int
+    L.kv_packed_store.argtypes = L.kv_packed_load.argtypes = [vp, C.c_int32, vp, i64, vp, i64, vp, i64, vp]
+    L.kv_packed_park.restype = L.kv_packed_restore.restype = C.c_int
+    L.kv_packed_park.argtypes = L.kv_packed_restore.argtypes = [vp, vp, vp, vp, i64, vp]
     hp = C.POINTER(kv_ipc_handle)
     L.kv_ipc_export.restype = C.c_int
     L.kv_ipc_export.argtypes = [vp, C.c_uint64, hp]
@@ -374,6 +385,52 @@ def kv_tables_grow(held: int, lens: int, num_requests: int, block_size: int, fre
                                 C.c_void_p(counts), device, C.c_void_p(stream)))
 
 
+def kv_packed_bytes(shape_or_desc, block_size: int, num_blocks: int) -> int:
+    d = shape_or_desc if isinstance(shape_or_desc, kv_model_desc) else make_desc(shape_or_desc)
+    return int(lib().kv_packed_bytes(C.byref(d), block_size, num_blocks))
+
+
+def kv_packed_bind(base: int, nbytes: int, shape_or_desc, block_size: int, num_blocks: int,
+                   device: int = 0) -> int:
+    d = shape_or_desc if isinstance(shape_or_desc, kv_model_desc) else make_desc(shape_or_desc)
+    h = C.c_void_p()
+    _check(lib().kv_packed_bind(C.c_void_p(base), nbytes, C.byref(d), block_size, num_blocks, device,
+                                C.byref(h)))
+    return h.value
+
+
+def kv_packed_release(packed: int) -> None:
+    _check(lib().kv_packed_release(C.c_void_p(packed)))
+
+
+def kv_packed_store(packed: int, layer: int, k: int, k_stride: int, v: int, v_stride: int, slots: int,
+                    rows: int, stream: int = 0) -> None:
+    """Rows of k, v (device addresses, strides in elements) into the packed arena's slots."""
+    _check(lib().kv_packed_store(C.c_void_p(packed), layer, C.c_void_p(k), k_stride, C.c_void_p(v), v_stride,
+                                 C.c_void_p(slots), rows, C.c_void_p(stream)))
+
+
+def kv_packed_load(packed: int, layer: int, k: int, k_stride: int, v: int, v_stride: int, slots: int,
+                   rows: int, stream: int = 0) -> None:
+    """The values of the packed arena's slots as rows of k, v."""
+    _check(lib().kv_packed_load(C.c_void_p(packed), layer, C.c_void_p(k), k_stride, C.c_void_p(v), v_stride,
+                                C.c_void_p(slots), rows, C.c_void_p(stream)))
+
+
+def kv_packed_park(arena: int, arena_slots: int, packed: int, packed_slots: int, rows: int,
+                   stream: int = 0) -> None:
+    """Every layer of the arena's slots into the packed arena's (device int64 arrays)."""
+    _check(lib().kv_packed_park(C.c_void_p(arena), C.c_void_p(arena_slots), C.c_void_p(packed),
+                                C.c_void_p(packed_slots), rows, C.c_void_p(stream)))
+
+
+def kv_packed_restore(packed: int, packed_slots: int, arena: int, arena_slots: int, rows: int,
+                      stream: int = 0) -> None:
+    """Every layer of the packed arena's slots back into the arena's."""
+    _check(lib().kv_packed_restore(C.c_void_p(packed), C.c_void_p(packed_slots), C.c_void_p(arena),
+                                   C.c_void_p(arena_slots), rows, C.c_void_p(stream)))
+
+
 def kv_ipc_export(ptr: int, nbytes: int) -> bytes:
     """Owner side: the handle of device memory [ptr, ptr+nbytes) as plain bytes."""
     h = kv_ipc_handle()
@@ -434,4 +491,5 @@ def exported_symbols() -> Iterable[str]:
             "kv_ipc_export", "kv_ipc_owner_alive", "kv_ipc_open", "kv_ipc_close",
             "kv_verify_workspace_bytes", "kv_block_digests", "kv_verify", "kv_verify_noalloc",
             "kv_rebuild_from_workspace_bytes", "kv_rebuild_from_check", "kv_rebuild_from",
-            "kv_rebuild_stage_from", "kv_tables_grow")
+            "kv_rebuild_stage_from", "kv_tables_grow", "kv_packed_bytes", "kv_packed_bind", "kv_packed_release",
+            "kv_packed_store", "kv_packed_load", "kv_packed_park", "kv_packed_restore")
