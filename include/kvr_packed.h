@@ -83,6 +83,47 @@ kv_status kv_packed_park(kv_arena_t arena, const int64_t* arena_slots, kv_packed
 kv_status kv_packed_restore(kv_packed_t packed, const int64_t* packed_slots, kv_arena_t arena,
                             const int64_t* arena_slots, int64_t rows, void* stream);
 
+/* Workspace bytes of kv_packed_attention for up to num_requests requests, `rows`
+ * query rows in all, at most max_query of one request, lengths up to max_len; 0 for
+ * an invalid description (kv_packed_bytes's, at most 16 q heads per kv head) or
+ * non-positive sizes. */
+uint64_t kv_packed_attention_workspace_bytes(const kv_model_desc* desc, int32_t num_requests,
+                                             int64_t rows, int32_t max_query, int64_t max_len);
+
+/* Attention of one layer over a packed arena: one new token of each request, or
+ * several (drafted tokens to be checked, a prompt's next piece).
+ *   q            device [rows][nq][d], model dtype, rows q_stride elements apart
+ *   q_offsets    device int32 [num_requests + 1]: request r's query rows are
+ *                q_offsets[r] .. q_offsets[r+1] - 1; NULL: row r is request r's only
+ *                one, rows == num_requests
+ *   lens         device int32 [num_requests]: positions of request r in the arena,
+ *                its query rows' own included (stored before the call); of m query
+ *                rows, row i is at position lens[r] - m + i
+ *   block_tables device int32 [num_requests][max_blocks_per_req]
+ *   max_query, max_len  host bounds of a request's query rows and length
+ *   out          device [rows][nq][d], model dtype, rows out_stride elements apart
+ *   workspace    device scratch, on a boundary of 16 bytes; calls in flight at once
+ *                need one each
+ * Row i attends positions 0 .. its own: out = sum_j p_j v_j, p the softmax of
+ * q . k_j / sqrt(d), q head h reading kv head h / (nq/nkv).  Scores, softmax and sums
+ * are fp32, the output is rounded once.  Positions in a block whose table entry is
+ * outside the arena, and those past max_blocks_per_req, are left out; a row that is
+ * left with no position is zero.  Nothing but a request's rows of out is written;
+ * q and out may be the same memory only as the same rows.  The arrays on the device are
+ * read when the call runs there, so a captured call follows their contents.
+ *   KV_EINVAL  null arrays, a layer outside the model, negative sizes, a stride below
+ *              nq * d, a pointer or stride not on its boundary (4 bytes), more than 16
+ *              q heads per kv head, rows != num_requests without q_offsets, max_query
+ *              or max_len < 1
+ *   KV_ENOMEM  workspace smaller than kv_packed_attention_workspace_bytes
+ *   KV_ESTATE  unknown handle */
+kv_status kv_packed_attention(kv_packed_t packed, int32_t layer, const void* q, int64_t q_stride,
+                              const int32_t* q_offsets, int64_t rows, const int32_t* lens,
+                              const int32_t* block_tables, int32_t num_requests,
+                              int32_t max_blocks_per_req, int32_t max_query, int64_t max_len,
+                              void* out, int64_t out_stride, void* workspace,
+                              uint64_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -40,4 +40,20 @@ struct PackedMoveParams {
 };
 void launch_packed_move(int dtype, int d, bool to_packed, const PackedMoveParams& p, hipStream_t s);
 
+// Attention over one layer of a packed arena.
+struct PackedAttnParams {
+  PackedLayer packed;
+  int64_t num_blocks;
+  const char* q;               // rows of queries, model dtype
+  char* out;
+  int64_t q_stride, out_stride;  // bytes
+  const int32_t* q_offsets;    // null: row r is request r's
+  int64_t rows;
+  const int32_t* lens;
+  const int32_t* tables;
+  int R, max_blocks;
+  int nq;
+};
+void launch_packed_attention(int dtype, int d, const PackedAttnParams& p, hipStream_t s);
+
 }  // namespace kvr

@@ -137,6 +137,11 @@ def lib() -> C.CDLL:
     L.kv_packed_store.argtypes = L.kv_packed_load.argtypes = [vp, C.c_int32, vp, i64, vp, i64, vp, i64, vp]
     L.kv_packed_park.restype = L.kv_packed_restore.restype = C.c_int
     L.kv_packed_park.argtypes = L.kv_packed_restore.argtypes = [vp, vp, vp, vp, i64, vp]
+    L.kv_packed_attention_workspace_bytes.restype = C.c_uint64
+    L.kv_packed_attention_workspace_bytes.argtypes = [C.POINTER(kv_model_desc), C.c_int32, i64, C.c_int32, i64]
+    L.kv_packed_attention.restype = C.c_int
+    L.kv_packed_attention.argtypes = [vp, C.c_int32, vp, i64, vp, i64, vp, vp, C.c_int32, C.c_int32, C.c_int32,
+                                      i64, vp, i64, vp, C.c_uint64, vp]
     hp = C.POINTER(kv_ipc_handle)
     L.kv_ipc_export.restype = C.c_int
     L.kv_ipc_export.argtypes = [vp, C.c_uint64, hp]
@@ -431,6 +436,22 @@ def kv_packed_restore(packed: int, packed_slots: int, arena: int, arena_slots: i
                                    C.c_void_p(arena_slots), rows, C.c_void_p(stream)))
 
 
+def kv_packed_attention_workspace_bytes(shape_or_desc, num_requests: int, rows: int, max_query: int,
+                                        max_len: int) -> int:
+    d = shape_or_desc if isinstance(shape_or_desc, kv_model_desc) else make_desc(shape_or_desc)
+    return int(lib().kv_packed_attention_workspace_bytes(C.byref(d), num_requests, rows, max_query, max_len))
+
+
+def kv_packed_attention(packed: int, layer: int, q: int, q_stride: int, q_offsets: int, rows: int, lens: int,
+                        tables: int, num_requests: int, max_blocks: int, max_query: int, max_len: int, out: int,
+                        out_stride: int, workspace: int, workspace_bytes: int, stream: int = 0) -> None:
+    """Attention of one layer over the packed arena; arrays are device addresses."""
+    _check(lib().kv_packed_attention(C.c_void_p(packed), layer, C.c_void_p(q), q_stride,
+                                     C.c_void_p(q_offsets or None), rows, C.c_void_p(lens), C.c_void_p(tables),
+                                     num_requests, max_blocks, max_query, max_len, C.c_void_p(out), out_stride,
+                                     C.c_void_p(workspace), workspace_bytes, C.c_void_p(stream)))
+
+
 def kv_ipc_export(ptr: int, nbytes: int) -> bytes:
     """Owner side: the handle of device memory [ptr, ptr+nbytes) as plain bytes."""
     h = kv_ipc_handle()
@@ -492,4 +513,5 @@ def exported_symbols() -> Iterable[str]:
             "kv_verify_workspace_bytes", "kv_block_digests", "kv_verify", "kv_verify_noalloc",
             "kv_rebuild_from_workspace_bytes", "kv_rebuild_from_check", "kv_rebuild_from",
             "kv_rebuild_stage_from", "kv_tables_grow", "kv_packed_bytes", "kv_packed_bind", "kv_packed_release",
-            "kv_packed_store", "kv_packed_load", "kv_packed_park", "kv_packed_restore")
+            "kv_packed_store", "kv_packed_load", "kv_packed_park", "kv_packed_restore",
+            "kv_packed_attention_workspace_bytes", "kv_packed_attention")

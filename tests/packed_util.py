@@ -43,7 +43,7 @@ def quantise(x):
 def values(codes, scales):
     """What codes [..., d] and scale bytes [..., d/32] stand for, 64 bits."""
     s = np.where(scales == 255, np.nan, np.exp2(scales.astype(np.float64) - 127))
-    v = VALUES[codes].reshape(*codes.shape[:-1], -1, 32) * s[..., None]
+    v = VALUES[codes].reshape(*scales.shape, 32) * s[..., None]
     return v.reshape(codes.shape)
 
 
