@@ -21,7 +21,7 @@ LIB = os.path.join(PKG, "libkvr.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 SOURCES = ["abi.hip", "misc.hip", "gemm_wide.hip", "gemm_tile.hip", "gemm_skinny.hip", "gemm_f32.hip", "attention.hip", "decode.hip", "ipc.hip", "verify.hip",
-           "tables.hip", "packed.hip", "packed_attn.hip"]
+           "tables.hip", "packed.hip", "packed_attn.hip", "logprob.hip"]
 # Device code is built without packed-fp32 instructions (the host pass warns
 # that it does not know the feature; that is expected).
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-I", INCLUDE, "-I", CSRC,

@@ -1,6 +1,6 @@
 """Thin ctypes binding of libkvr.so (include/kvr.h, include/kvr_decode.h,
 include/kvr_ipc.h, include/kvr_verify.h, include/kvr_reuse.h, include/kvr_profile.h,
-include/kvr_tables.h, include/kvr_packed.h).
+include/kvr_tables.h, include/kvr_packed.h, include/kvr_logprob.h).
 
 Argument marshalling only: every step of the rebuild runs in the library's
 HIP kernels.  Device buffers are passed as integer addresses (for example a
@@ -142,6 +142,11 @@ def lib() -> C.CDLL:
     L.kv_packed_attention.restype = C.c_int
     L.kv_packed_attention.argtypes = [vp, C.c_int32, vp, i64, vp, i64, vp, vp, C.c_int32, C.c_int32, C.c_int32,
                                       i64, vp, i64, vp, C.c_uint64, vp]
+    L.kv_logprobs_workspace_bytes.restype = C.c_uint64
+    L.kv_logprobs_workspace_bytes.argtypes = [i64, C.c_int32, C.c_int32]
+    L.kv_logprobs.restype = C.c_int
+    L.kv_logprobs.argtypes = [vp, C.c_int32, i64, C.c_int32, i64, C.c_float, vp, C.c_int32, vp, vp, vp, vp, vp,
+                              C.c_uint64, C.c_int32, vp]
     hp = C.POINTER(kv_ipc_handle)
     L.kv_ipc_export.restype = C.c_int
     L.kv_ipc_export.argtypes = [vp, C.c_uint64, hp]
@@ -452,6 +457,25 @@ def kv_packed_attention(packed: int, layer: int, q: int, q_stride: int, q_offset
                                      C.c_void_p(workspace), workspace_bytes, C.c_void_p(stream)))
 
 
+# likeliest tokens a call returns at most
+KV_LOGPROBS_MAX_TOP = 64
+
+
+def kv_logprobs_workspace_bytes(rows: int, vocab: int, top_n: int) -> int:
+    return int(lib().kv_logprobs_workspace_bytes(rows, vocab, top_n))
+
+
+def kv_logprobs(logits: int, dtype: int, rows: int, vocab: int, stride: int, scale: float, tokens: int, top_n: int,
+                logprobs: int, entropy: int, top_logprobs: int, top_tokens: int, workspace: int,
+                workspace_bytes: int, device: int = 0, stream: int = 0) -> None:
+    """Log probabilities of the rows' tokens, entropies and likeliest tokens; arrays
+    are device addresses (0: not wanted)."""
+    _check(lib().kv_logprobs(C.c_void_p(logits), dtype, rows, vocab, stride, scale, C.c_void_p(tokens or None),
+                             top_n, C.c_void_p(logprobs or None), C.c_void_p(entropy or None),
+                             C.c_void_p(top_logprobs or None), C.c_void_p(top_tokens or None),
+                             C.c_void_p(workspace), workspace_bytes, device, C.c_void_p(stream)))
+
+
 def kv_ipc_export(ptr: int, nbytes: int) -> bytes:
     """Owner side: the handle of device memory [ptr, ptr+nbytes) as plain bytes."""
     h = kv_ipc_handle()
@@ -514,4 +538,5 @@ def exported_symbols() -> Iterable[str]:
             "kv_rebuild_from_workspace_bytes", "kv_rebuild_from_check", "kv_rebuild_from",
             "kv_rebuild_stage_from", "kv_tables_grow", "kv_packed_bytes", "kv_packed_bind", "kv_packed_release",
             "kv_packed_store", "kv_packed_load", "kv_packed_park", "kv_packed_restore",
-            "kv_packed_attention_workspace_bytes", "kv_packed_attention")
+            "kv_packed_attention_workspace_bytes", "kv_packed_attention",
+            "kv_logprobs_workspace_bytes", "kv_logprobs")
