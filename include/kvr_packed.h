@@ -124,6 +124,22 @@ kv_status kv_packed_attention(kv_packed_t packed, int32_t layer, const void* q, 
                               void* out, int64_t out_stride, void* workspace,
                               uint64_t workspace_bytes, void* stream);
 
+/* Workspace bytes of kv_packed_decode_step for up to num_requests requests whose
+ * positions are all < max_position; 0 for an invalid description or sizes. */
+uint64_t kv_packed_decode_workspace_bytes(const kv_model_desc* desc, int32_t num_requests,
+                                          int64_t max_position);
+
+/* One greedy decode step over a packed arena: kv_decode_step (kvr_decode.h) with the
+ * context's K/V in a packed arena, the new position's K/V stored there in every layer
+ * before that layer's attention reads it.  Arguments, outputs and status codes are
+ * kv_decode_step's. */
+kv_status kv_packed_decode_step(const kv_weights* w, const void* final_norm, const void* lm_head,
+                                const int32_t* tokens, const int32_t* positions,
+                                int32_t num_requests, const int32_t* block_tables,
+                                int32_t max_blocks_per_req, kv_packed_t packed, void* workspace,
+                                uint64_t workspace_bytes, void* stream, int32_t* next_tokens,
+                                float* logits);
+
 #ifdef __cplusplus
 }
 #endif

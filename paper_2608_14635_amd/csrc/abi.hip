@@ -12,15 +12,18 @@
 #include <mutex>
 #include <set>
 #include <string>
+#include <type_traits>
 #include <vector>
 
 #include "kvr.h"
 #include "kvr_decode.h"
 #include "kvr_verify.h"
+#include "kvr_packed.h"
 #include "kvr_reuse.h"
 #include "kvr_profile.h"
 #include "host.h"
 #include "launch.h"
+#include "packed.h"
 
 using namespace kvr;
 
@@ -323,9 +326,12 @@ struct DecodeLayout {
   size_t rope = 0, x = 0, a = 0, q = 0, u = 0, hf = 0, part = 0, gpart = 0, amax = 0, logit = 0;
   size_t total = 0;
   int64_t gpart_elems = 0;
+  // over a packed arena: contexts with the new position, the new rows' slots, and
+  // the rows as the QKV product leaves them, at slots 0 .. R-1 of planes of R slots
+  size_t lens = 0, pslot = 0, knew = 0, vnew = 0;
 };
 
-DecodeLayout make_decode_layout(const kv_model_desc& d, int32_t R, int64_t max_position) {
+DecodeLayout make_decode_layout(const kv_model_desc& d, int32_t R, int64_t max_position, bool packed) {
   DecodeLayout L;
   L.R = R;
   L.max_position = max_position;
@@ -350,6 +356,10 @@ DecodeLayout make_decode_layout(const kv_model_desc& d, int32_t R, int64_t max_p
   L.rowidx = seg(4 * (size_t)R);
   L.slot = seg(8 * (size_t)R);
   L.first = seg(4 * (size_t)R);
+  if (packed) {
+    L.lens = seg(4 * (size_t)R);
+    L.pslot = seg(8 * (size_t)R);
+  }
   L.tables = seg(4 * (size_t)R * (size_t)max_position);
   L.meta_end = off;
   L.rope = seg((size_t)8 * R * (d.head_dim / 2));
@@ -358,7 +368,14 @@ DecodeLayout make_decode_layout(const kv_model_desc& d, int32_t R, int64_t max_p
   L.q = seg((size_t)e * R * d.num_q_heads * d.head_dim);
   L.u = seg((size_t)e * R * d.num_q_heads * d.head_dim);
   L.hf = seg((size_t)e * R * d.ffn_dim);
-  L.part = seg((size_t)4 * R * d.num_q_heads * L.splits * (d.head_dim + 2));
+  if (packed) {
+    const size_t plane = (size_t)e * R * d.num_kv_heads * d.head_dim;
+    L.knew = seg(plane);
+    L.vnew = seg(plane);
+    L.part = seg(kv_packed_attention_workspace_bytes(&d, R, R, 1, max_position));
+  } else {
+    L.part = seg((size_t)4 * R * d.num_q_heads * L.splits * (d.head_dim + 2));
+  }
   L.gpart = seg((size_t)4 * L.gpart_elems);
   L.amax = seg((size_t)8 * ARGMAX_CHUNKS * R);
   L.logit = seg((size_t)4 * d.vocab * L.npad);
@@ -1035,7 +1052,7 @@ kv_status kv_rebuild(const kv_weights* w, const int32_t* tokens, const int32_t* 
 uint64_t kv_decode_workspace_bytes(const kv_model_desc* desc, int32_t num_requests,
                                    int64_t max_position) {
   if (check_desc(desc) != KV_OK || num_requests <= 0 || max_position <= 0) return 0;
-  return make_decode_layout(*desc, num_requests, max_position).total;
+  return make_decode_layout(*desc, num_requests, max_position, false).total;
 }
 
 kv_status kv_decode_check(const kv_model_desc* desc, int32_t block_size, int64_t num_blocks,
@@ -1046,12 +1063,18 @@ kv_status kv_decode_check(const kv_model_desc* desc, int32_t block_size, int64_t
   return st == KV_OK ? ok() : st;
 }
 
-kv_status kv_decode_step(const kv_weights* w, const void* final_norm, const void* lm_head,
-                         const int32_t* tokens, const int32_t* positions, int32_t R,
-                         const int32_t* tables, int32_t max_blocks, kv_arena_t arena,
-                         void* workspace, uint64_t ws_bytes, void* stream, int32_t* next_tokens,
-                         float* logits) {
-  if (!live_arena(arena)) return fail(KV_ESTATE, "unknown or released arena handle");
+}  // extern "C"
+
+namespace {
+
+// One step over a retained arena or a packed one: the latter's new rows go through
+// two planes of the workspace, and its own store and attention stand in for the
+// epilogue's scatter and the decode attention.
+template <typename Arena>
+kv_status decode_step(const kv_weights* w, const void* final_norm, const void* lm_head, const int32_t* tokens,
+                      const int32_t* positions, int32_t R, const int32_t* tables, int32_t max_blocks, Arena* arena,
+                      void* workspace, uint64_t ws_bytes, void* stream, int32_t* next_tokens, float* logits) {
+  constexpr bool PACKED = std::is_same<Arena, kv_packed>::value;
   if (!w || !w->embed || !w->layers) return fail(KV_EINVAL, "null weights");
   const kv_model_desc& d = arena->desc;
   if (!same_desc(w->desc, d)) return fail(KV_ESTATE, "weights and arena describe different models");
@@ -1073,7 +1096,7 @@ kv_status kv_decode_step(const kv_weights* w, const void* final_norm, const void
       return fail(KV_EINVAL, "qkv_bias model without bq/bk/bv in layer %d", l);
   }
   if (!workspace) return fail(KV_EINVAL, "null workspace");
-  const DecodeLayout L = make_decode_layout(d, R, max_pos + 1);
+  const DecodeLayout L = make_decode_layout(d, R, max_pos + 1, PACKED);
   if (L.total > ws_bytes)
     return fail(KV_ENOMEM, "workspace of %llu bytes < %llu needed", (unsigned long long)ws_bytes,
                 (unsigned long long)L.total);
@@ -1113,6 +1136,8 @@ kv_status kv_decode_step(const kv_weights* w, const void* final_norm, const void
   // key ranges of the attention, numbered request by request
   const int chunk = decode_attn_chunk(d.dtype, B, positions, R, d.num_q_heads, d.num_kv_heads, d.head_dim, max_pos + 1);
   int items = 0;
+  int32_t* hlens = reinterpret_cast<int32_t*>(hb + L.lens);
+  int64_t* hpslot = reinterpret_cast<int64_t*>(hb + L.pslot);
   for (int32_t r = 0; r < R; ++r) {
     const int32_t p = positions[r];
     const int32_t* tab = tables + (int64_t)r * max_blocks;
@@ -1120,6 +1145,11 @@ kv_status kv_decode_step(const kv_weights* w, const void* final_norm, const void
     hpos[r] = p;
     hrow[r] = r;
     hslot[r] = (int64_t)tab[p / B] * B + p % B;
+    if (PACKED) {
+      hlens[r] = p + 1;
+      hpslot[r] = hslot[r];
+      hslot[r] = r;
+    }
     hfirst[r] = items;
     items += (int)(((int64_t)p + chunk) / chunk);
     for (int32_t b = 0; b < tab_ld; ++b) htab[(int64_t)r * tab_ld + b] = b <= p / B ? tab[b] : 0;
@@ -1182,8 +1212,8 @@ kv_status kv_decode_step(const kv_weights* w, const void* final_norm, const void
   launch_embed_norm(dt, w->embed, d_tok, w->layers[0].attn_norm, X, A, R, H, eps, s);
   for (int l = 0; l < d.num_layers; ++l) {
     const kv_layer_weights& lw = w->layers[l];
-    char* plane_k = abase + (int64_t)(2 * l) * plane * elem_bytes(dt);
-    char* plane_v = abase + (int64_t)(2 * l + 1) * plane * elem_bytes(dt);
+    char* plane_k = PACKED ? ws + L.knew : abase + (int64_t)(2 * l) * plane * elem_bytes(dt);
+    char* plane_v = PACKED ? ws + L.vnew : abase + (int64_t)(2 * l + 1) * plane * elem_bytes(dt);
     GemmParams g{};
     g.A = A;
     g.lda = H;
@@ -1217,24 +1247,30 @@ kv_status kv_decode_step(const kv_weights* w, const void* final_norm, const void
     g.epi.eps = eps;
     gemm(EPI_QKV, g, s);
 
-    DecodeAttnParams ap{};
-    ap.q = Q;
-    ap.plane_k = plane_k;
-    ap.plane_v = plane_v;
-    ap.tables = d_tab;
-    ap.max_blocks = tab_ld;
-    ap.block_size = B;
-    ap.pos = d_pos;
-    ap.first = d_first;
-    ap.nq = nq;
-    ap.nkv = nkv;
-    ap.d = hd;
-    ap.R = R;
-    ap.chunk = chunk;
-    ap.splits = (int)((max_pos + chunk) / chunk);
-    ap.part = part;
-    ap.out = U;
-    launch_decode_attention(dt, ap, items, s);
+    if constexpr (PACKED) {
+      packed_store_rows(arena, l, plane_k, plane_v, reinterpret_cast<const int64_t*>(ws + L.pslot), R, s);
+      packed_attention_step(arena, l, Q, reinterpret_cast<const int32_t*>(ws + L.lens), d_tab, R, tab_ld,
+                            max_pos + 1, U, part, s);
+    } else {
+      DecodeAttnParams ap{};
+      ap.q = Q;
+      ap.plane_k = plane_k;
+      ap.plane_v = plane_v;
+      ap.tables = d_tab;
+      ap.max_blocks = tab_ld;
+      ap.block_size = B;
+      ap.pos = d_pos;
+      ap.first = d_first;
+      ap.nq = nq;
+      ap.nkv = nkv;
+      ap.d = hd;
+      ap.R = R;
+      ap.chunk = chunk;
+      ap.splits = (int)((max_pos + chunk) / chunk);
+      ap.part = part;
+      ap.out = U;
+      launch_decode_attention(dt, ap, items, s);
+    }
 
     GemmParams go{};
     go.A = U;
@@ -1316,6 +1352,40 @@ kv_status kv_decode_step(const kv_weights* w, const void* final_norm, const void
   const hipError_t err = hipGetLastError();
   if (err != hipSuccess) return fail(KV_EDEVICE, "kernel launch failed: %s", hipGetErrorString(err));
   return ok();
+}
+
+}  // namespace
+
+extern "C" {
+
+kv_status kv_decode_step(const kv_weights* w, const void* final_norm, const void* lm_head,
+                         const int32_t* tokens, const int32_t* positions, int32_t R,
+                         const int32_t* tables, int32_t max_blocks, kv_arena_t arena,
+                         void* workspace, uint64_t ws_bytes, void* stream, int32_t* next_tokens,
+                         float* logits) {
+  if (!live_arena(arena)) return fail(KV_ESTATE, "unknown or released arena handle");
+  return decode_step(w, final_norm, lm_head, tokens, positions, R, tables, max_blocks, arena, workspace,
+                     ws_bytes, stream, next_tokens, logits);
+}
+
+uint64_t kv_packed_decode_workspace_bytes(const kv_model_desc* desc, int32_t num_requests,
+                                          int64_t max_position) {
+  if (num_requests <= 0 || max_position <= 0 ||
+      kv_packed_attention_workspace_bytes(desc, num_requests, num_requests, 1, max_position) == 0)
+    return 0;
+  return make_decode_layout(*desc, num_requests, max_position, true).total;
+}
+
+kv_status kv_packed_decode_step(const kv_weights* w, const void* final_norm, const void* lm_head,
+                                const int32_t* tokens, const int32_t* positions, int32_t R,
+                                const int32_t* tables, int32_t max_blocks, kv_packed_t packed,
+                                void* workspace, uint64_t ws_bytes, void* stream, int32_t* next_tokens,
+                                float* logits) {
+  if (!live_packed(packed)) return fail(KV_ESTATE, "unknown or released packed arena handle");
+  if (workspace && (uintptr_t)workspace % 16 != 0)
+    return fail(KV_EINVAL, "the workspace needs a boundary of 16 bytes");
+  return decode_step(w, final_norm, lm_head, tokens, positions, R, tables, max_blocks, packed, workspace,
+                     ws_bytes, stream, next_tokens, logits);
 }
 
 // ---------------------------------------------------------------------------

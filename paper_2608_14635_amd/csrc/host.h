@@ -46,6 +46,11 @@ struct kv_packed {
   int32_t block_size;
   int64_t num_blocks;
   int32_t device;
+  // staging as kv_arena's (kv_packed_decode_step)
+  void* pinned = nullptr;
+  size_t pinned_bytes = 0;
+  hipEvent_t staged = nullptr;
+  bool staged_pending = false;
 };
 
 namespace kvr {

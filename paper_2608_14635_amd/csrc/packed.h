@@ -3,6 +3,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+struct kv_packed;
+
 namespace kvr {
 
 constexpr int PK_TILE = 16;    // slots of a record
@@ -39,6 +41,14 @@ struct PackedMoveParams {
   int layers;
 };
 void launch_packed_move(int dtype, int d, bool to_packed, const PackedMoveParams& p, hipStream_t s);
+
+// What a decode step does with a packed arena: its new rows, dense [rows][nkv][d],
+// into their slots, and the attention of one query row a request.
+void packed_store_rows(const kv_packed* a, int32_t layer, const void* k, const void* v, const int64_t* slots,
+                       int64_t rows, hipStream_t s);
+void packed_attention_step(const kv_packed* a, int32_t layer, const void* q, const int32_t* lens,
+                           const int32_t* tables, int R, int max_blocks, int64_t max_len, void* out,
+                           void* workspace, hipStream_t s);
 
 // Attention over one layer of a packed arena.
 struct PackedAttnParams {

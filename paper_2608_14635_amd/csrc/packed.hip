@@ -254,6 +254,22 @@ kv_status move_rows(kv_packed* a, bool to_packed, int32_t layer, const void* k, 
   return launched();
 }
 
+}  // namespace
+
+void kvr::packed_store_rows(const kv_packed* a, int32_t layer, const void* k, const void* v, const int64_t* slots,
+                            int64_t rows, hipStream_t s) {
+  const kv_model_desc& d = a->desc;
+  PackedMoveParams p = move_params(a, layer, 1);
+  p.k = static_cast<char*>(const_cast<void*>(k));
+  p.v = static_cast<char*>(const_cast<void*>(v));
+  p.k_stride = p.v_stride = (int64_t)d.num_kv_heads * d.head_dim * elem_bytes(d.dtype);
+  p.plain_rows = p.rows = rows;
+  p.packed_slots = slots;
+  launch_packed_move(d.dtype, d.head_dim, true, p, s);
+}
+
+namespace {
+
 // every layer, between the two arenas
 kv_status move_all(bool to_packed, kv_arena* arena, const int64_t* arena_slots, kv_packed* packed,
                    const int64_t* packed_slots, int64_t rows, void* stream) {
@@ -326,6 +342,11 @@ kv_status kv_packed_bind(void* base, uint64_t bytes, const kv_model_desc* desc, 
   }
   try {
     std::unique_ptr<kv_packed> a(new kv_packed{base, bytes, *desc, block_size, num_blocks, device});
+    DeviceGuard dg(device);
+    if (hipEventCreateWithFlags(&a->staged, hipEventDisableTiming) != hipSuccess) {
+      (void)hipGetLastError();
+      return kvr_err::set(KV_EDEVICE, "event creation failed");
+    }
     std::lock_guard<std::mutex> g(g_mu);
     g_packed.insert(a.get());
     *out = a.release();
@@ -342,6 +363,10 @@ kv_status kv_packed_release(kv_packed_t packed) {
       return kvr_err::set(KV_ESTATE, "unknown or released packed arena handle");
     g_packed.erase(packed);
   }
+  DeviceGuard dg(packed->device);
+  if (packed->staged_pending) (void)hipEventSynchronize(packed->staged);
+  if (packed->pinned) (void)hipHostFree(packed->pinned);
+  (void)hipEventDestroy(packed->staged);
   delete packed;
   return kvr_err::clear();
 }

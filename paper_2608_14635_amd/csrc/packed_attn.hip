@@ -122,6 +122,39 @@ void launch_packed_attention(int dtype, int d, const PackedAttnParams& p, hipStr
 
 using namespace kvr;
 
+namespace {
+
+void run(const kv_packed* packed, int32_t layer, const void* q, int64_t q_stride, const int32_t* q_offsets,
+         int64_t rows, const int32_t* lens, const int32_t* tables, int R, int max_blocks, int32_t max_query,
+         int64_t max_len, void* out, int64_t out_stride, void* workspace, hipStream_t s) {
+  const kv_model_desc& d = packed->desc;
+  const int64_t e = elem_bytes(d.dtype);
+  PackedAttnParams p{};
+  p.packed = packed_layer(packed, layer);
+  p.num_blocks = packed->num_blocks;
+  p.q = static_cast<const char*>(q);
+  p.out = static_cast<char*>(out);
+  p.q_stride = q_stride * e;
+  p.out_stride = out_stride * e;
+  p.q_offsets = q_offsets;
+  p.rows = rows;
+  p.lens = lens;
+  p.tables = tables;
+  p.R = R;
+  p.max_blocks = max_blocks;
+  p.nq = d.num_q_heads;
+  launch_packed_attention(d.dtype, d.head_dim, p, s);
+}
+
+}  // namespace
+
+void kvr::packed_attention_step(const kv_packed* a, int32_t layer, const void* q, const int32_t* lens,
+                                const int32_t* tables, int R, int max_blocks, int64_t max_len, void* out,
+                                void* workspace, hipStream_t s) {
+  const int64_t row = (int64_t)a->desc.num_q_heads * a->desc.head_dim;
+  run(a, layer, q, row, nullptr, R, lens, tables, R, max_blocks, 1, max_len, out, row, workspace, s);
+}
+
 extern "C" {
 
 uint64_t kv_packed_attention_workspace_bytes(const kv_model_desc* desc, int32_t num_requests, int64_t rows,
@@ -162,21 +195,8 @@ kv_status kv_packed_attention(kv_packed_t packed, int32_t layer, const void* q, 
   DeviceGuard dg(packed->device);
   const kv_status st = device_ready(dg, packed->device);
   if (st != KV_OK) return st;
-  PackedAttnParams p{};
-  p.packed = packed_layer(packed, layer);
-  p.num_blocks = packed->num_blocks;
-  p.q = static_cast<const char*>(q);
-  p.out = static_cast<char*>(out);
-  p.q_stride = q_stride * e;
-  p.out_stride = out_stride * e;
-  p.q_offsets = q_offsets;
-  p.rows = rows;
-  p.lens = lens;
-  p.tables = tables;
-  p.R = R;
-  p.max_blocks = max_blocks;
-  p.nq = d.num_q_heads;
-  launch_packed_attention(d.dtype, d.head_dim, p, reinterpret_cast<hipStream_t>(stream));
+  run(packed, layer, q, q_stride, q_offsets, rows, lens, tables, R, max_blocks, max_query, max_len, out, out_stride,
+      workspace, reinterpret_cast<hipStream_t>(stream));
   return launched();
 }
 

@@ -147,6 +147,10 @@ def lib() -> C.CDLL:
     L.kv_logprobs.restype = C.c_int
     L.kv_logprobs.argtypes = [vp, C.c_int32, i64, C.c_int32, i64, C.c_float, vp, C.c_int32, vp, vp, vp, vp, vp,
                               C.c_uint64, C.c_int32, vp]
+    L.kv_packed_decode_workspace_bytes.restype = C.c_uint64
+    L.kv_packed_decode_workspace_bytes.argtypes = L.kv_decode_workspace_bytes.argtypes
+    L.kv_packed_decode_step.restype = C.c_int
+    L.kv_packed_decode_step.argtypes = L.kv_decode_step.argtypes
     hp = C.POINTER(kv_ipc_handle)
     L.kv_ipc_export.restype = C.c_int
     L.kv_ipc_export.argtypes = [vp, C.c_uint64, hp]
@@ -457,6 +461,23 @@ def kv_packed_attention(packed: int, layer: int, q: int, q_stride: int, q_offset
                                      C.c_void_p(workspace), workspace_bytes, C.c_void_p(stream)))
 
 
+def kv_packed_decode_workspace_bytes(shape_or_desc, num_requests: int, max_position: int) -> int:
+    d = shape_or_desc if isinstance(shape_or_desc, kv_model_desc) else make_desc(shape_or_desc)
+    return int(lib().kv_packed_decode_workspace_bytes(C.byref(d), num_requests, max_position))
+
+
+def kv_packed_decode_step(weights: Weights, final_norm: int, lm_head: int, tokens, positions, tables,
+                          packed: int, workspace: int, workspace_bytes: int, next_tokens: int,
+                          logits: int = 0, stream: int = 0) -> None:
+    """One greedy decode step over a packed arena; arguments as kv_decode_step's."""
+    tok, pos = _i32(tokens), _i32(positions)
+    tab, mb = _tables2d(tables, len(tok))
+    _check(lib().kv_packed_decode_step(C.byref(weights.c), C.c_void_p(final_norm), C.c_void_p(lm_head),
+                                       _ptr(tok), _ptr(pos), len(tok), _ptr(tab), mb, C.c_void_p(packed),
+                                       C.c_void_p(workspace), workspace_bytes, C.c_void_p(stream),
+                                       C.c_void_p(next_tokens), C.c_void_p(logits or None)))
+
+
 # likeliest tokens a call returns at most
 KV_LOGPROBS_MAX_TOP = 64
 
@@ -539,4 +560,5 @@ def exported_symbols() -> Iterable[str]:
             "kv_rebuild_stage_from", "kv_tables_grow", "kv_packed_bytes", "kv_packed_bind", "kv_packed_release",
             "kv_packed_store", "kv_packed_load", "kv_packed_park", "kv_packed_restore",
             "kv_packed_attention_workspace_bytes", "kv_packed_attention",
+            "kv_packed_decode_workspace_bytes", "kv_packed_decode_step",
             "kv_logprobs_workspace_bytes", "kv_logprobs")
