@@ -50,20 +50,4 @@ void packed_attention_step(const kv_packed* a, int32_t layer, const void* q, con
                            const int32_t* tables, int R, int max_blocks, int64_t max_len, void* out,
                            void* workspace, hipStream_t s);
 
-// Attention over one layer of a packed arena.
-struct PackedAttnParams {
-  PackedLayer packed;
-  int64_t num_blocks;
-  const char* q;               // rows of queries, model dtype
-  char* out;
-  int64_t q_stride, out_stride;  // bytes
-  const int32_t* q_offsets;    // null: row r is request r's
-  int64_t rows;
-  const int32_t* lens;
-  const int32_t* tables;
-  int R, max_blocks;
-  int nq;
-};
-void launch_packed_attention(int dtype, int d, const PackedAttnParams& p, hipStream_t s);
-
 }  // namespace kvr
