@@ -1,22 +1,30 @@
 // Attention over a packed arena (kvr_packed.h).
 //
 // The query rows of a request that share a kv head are columns: column i g + h is
-// query i of q head h of the group.  An item is one request's 16 NT columns of one kv
-// head; its work comes in units of 32 positions.  Every wave takes an equal stretch of
-// the units of all items, request after request, whatever the lengths (they are known
-// on the device alone), so that all waves end together; where a stretch ends inside an
-// item, the wave leaves the item's sums so far, and a second kernel merges them.
+// query i of q head h of the group.  An item is one request's next 16 NT columns of one
+// kv head; its work comes in units of 32 or 64 positions.  Every wave takes an equal
+// stretch of the units of all items, request after request, whatever the lengths (they
+// are known on the device alone), so that all waves end together.  Where a stretch
+// ends inside an item the wave leaves the item's sums so far; the four waves of a
+// workgroup, whose stretches follow each other, merge theirs, and a second kernel
+// merges what is left between workgroups.
 //
 // A unit in a wave's registers, lane (q, c) = (lane / 16, lane % 16):
 //   S^T = K Q^T on v_mfma_f32_16x16x32_bf16, 16 positions a tile: position c's dims
 //   q d/4 .. are the lane's K operand, d/8 bytes and one scale; the conversions to bf16
-//   are exact.  It gets the scores of positions 4q .. 4q+3 for column c.
+//   are exact.  The lane gets the scores of positions 4q .. 4q+3 for column c.
+//   Where at most 16 / COPIES columns are in use (4 copies of 4, 2 of 8), every copy of
+//   them takes the scores of another tile, with a softmax of its own: all 16 columns
+//   work, and a lane has 4 scores of 64 positions instead of 16, of which a quarter
+//   counts.  The copies are merged at the end of the stretch.
 //   Online softmax per column, exp2 domain, rescaled only where the maximum rose by
 //   more than 2^SLACK.
-//   O = P V: the lane's weights of two tiles are the A operand as they are, positions
-//   4q .. 4q+3 of both being its eight k's; V's layout gives the lane the dims
-//   c d/16 .. of the same positions, which it pairs into the B operands of d/16
-//   products.  Nothing passes through LDS.
+//   O = P V: the lane's weights of two tiles are the A operand as they are (0 where the
+//   tile is another copy's), positions 4q .. 4q+3 of both being its eight k's; V's
+//   layout gives the lane the dims c d/16 .. of the same positions, which it pairs into
+//   the B operands of d/16 products.  Nothing passes through LDS.
+// A tile's next bytes are loaded as soon as its registers are free, K after the scores
+// and V after the products.
 // Weights enter the product as a bf16 number and the bf16 rest (2^-17 of a weight lost),
 // in fp32 models as three (as do the queries): rounding them once would cost more than
 // the output's own rounding where few positions weigh, and the products are not what
@@ -33,23 +41,29 @@
 namespace kvr {
 namespace {
 
-constexpr int PA_UNIT = 32;        // positions of a unit
 constexpr int PA_NT = 256;         // four waves
 constexpr float SLACK = 8.0f;      // rescale slack, log2 units
-constexpr int PA_WAVES = 2048;     // waves of a call
+
+// Copies of the columns, and column tiles, that a kernel is built for.
+template <int NT_, int COPIES_>
+struct Shape {
+  static constexpr int NT = NT_, COPIES = COPIES_;
+  static constexpr int COLS = 16 * NT / COPIES;       // columns of an item
+  static constexpr int TILES = COPIES == 4 ? 4 : 2;   // tiles of a unit
+  static constexpr int UNIT = 16 * TILES;             // positions of a unit
+  static constexpr int OWN = COPIES == 1 ? TILES : 1; // tiles a column scores
+};
 
 template <typename T> struct Split;  // bf16 numbers that stand for a query, for a weight
 template <> struct Split<bf16_t> { static constexpr int Q = 1, P = 2; };
 template <> struct Split<float> { static constexpr int Q = 3, P = 3; };
 
-// What a wave leaves of an item it did not finish: the item, its units' end, and the
-// units of all items.
+// The item that a workgroup began and left open: its units' end, the units of all
+// items, and the wave that began it.
 struct OpenItem {
   int64_t end, total;
-  int request, tile;  // request -1: none
+  int request, tile, wave;  // request -1: none
 };
-
-__device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
 
 struct PackedAttnParams {
   PackedLayer packed;
@@ -64,10 +78,10 @@ struct PackedAttnParams {
   int R, max_blocks;
   int nq;
   int max_query;                 // rows of a request past it are left out: the sums have no room
-  int workers;                   // stretches per kv head
+  int workers;                   // stretches per kv head, a multiple of four
   int part_cols;                 // columns of a slot of sums
-  OpenItem* open;                // [workers]
-  float* part;                   // [nkv][workers][2][part_cols][D + 2]
+  OpenItem* open;                // [workers / 4]
+  float* part;                   // [nkv][workers][2][part_cols][D + 2]: an item begun before, one left open
 };
 
 // f(0), f(1), .. with the index a constant
@@ -83,7 +97,7 @@ struct Request {
   int row, m, len, want;  // first query row, rows, positions there are, position after the last query
   int tiles, steps;       // column tiles, units of each
 };
-template <int NT>
+template <int COLS, int UNIT>
 __device__ __forceinline__ Request get_request(const PackedAttnParams& p, int r) {
   Request q;
   q.row = r;
@@ -96,9 +110,15 @@ __device__ __forceinline__ Request get_request(const PackedAttnParams& p, int r)
   q.want = p.lens[r];
   q.len = (int)max((int64_t)0, min((int64_t)q.want, (int64_t)p.max_blocks * p.packed.block_size));
   const int g = p.nq / p.packed.nkv;
-  q.tiles = (int)(((int64_t)q.m * g + 16 * NT - 1) / (16 * NT));
-  q.steps = max(1, (q.len + PA_UNIT - 1) / PA_UNIT);
+  q.tiles = (int)(((int64_t)q.m * g + COLS - 1) / COLS);
+  q.steps = max(1, (int)(((int64_t)q.len + UNIT - 1) / UNIT));
   return q;
+}
+
+// The scale of byte i of a word.  The conversions read the exponent alone, whatever the
+// neighbouring bytes leave in the sign and the mantissa.
+__device__ __forceinline__ float scale_of(uint32_t word, int i) {
+  return __uint_as_float(i == 3 ? word >> 1 : word << (23 - 8 * i));
 }
 
 template <int BYTES>
@@ -123,22 +143,64 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
 }
 
-// A unit's bytes of a lane.
+// One position's values of a lane's V bytes, and its scale, to 0.
 template <int D>
-struct Unit {
-  static constexpr int W = D / 32;  // words of K, and of V, a tile
-  uint32_t k[2][W], v[2][W], ks[2], vs[2];
-  bool there[2];  // the tile's block is in the arena
+__device__ __forceinline__ void clear_v(uint32_t* v, uint32_t& vs, int j) {
+  constexpr int KB = D / 32;  // bytes of a position
+#pragma unroll
+  for (int y = 0; y < KB; ++y) v[(j * KB + y) / 4] &= ~(0xffu << ((j * KB + y) % 4 * 8));
+  vs &= ~(0xffu << (8 * j));
+}
+
+// What a wave's stretch holds of items that are not its own alone.
+struct Stretch {
+  int head, head_closed;          // it begins inside an item; the item ends in it
+  int tail;                       // it begins an item and leaves it open
+  int request[2], tile[2];        // those items
+  int64_t end;                    // the open item's units' end
 };
 
-template <typename T, int D, int NT>
-__global__ __launch_bounds__(PA_NT) void packed_attn_kernel(PackedAttnParams p) {
+// One column of an item, from n partials of D sums, maximum and sum: o (of dims 64 i +
+// lane), and where the columns end up.
+template <typename T, int D, typename SRC>
+__device__ __forceinline__ void merge_column(SRC src, int n, int lane, float* o, float& m, float& l) {
+  constexpr int ND = (D + 63) / 64;
+  m = -INFINITY;
+  for (int i = 0; i < n; ++i) m = fmaxf(m, src(i)[D]);
+  const float base = m == -INFINITY ? 0.0f : m;
+  l = 0.0f;
+#pragma unroll
+  for (int d = 0; d < ND; ++d) o[d] = 0.0f;
+#pragma unroll 4
+  for (int i = 0; i < n; ++i) {
+    const float* x = src(i);
+    const float f = __builtin_amdgcn_exp2f(x[D] - base);
+    l = fmaf(x[D + 1], f, l);
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+      if (d * 64 + lane < D) o[d] = fmaf(x[d * 64 + lane], f, o[d]);
+  }
+}
+
+// The output row of a column of request x's tile, at kv head kvh.
+template <typename T, int D, int COLS>
+__device__ __forceinline__ T* out_of(const PackedAttnParams& p, const Request& x, int tile, int col, int kvh) {
+  const int g = p.nq / p.packed.nkv, gc = tile * COLS + col;
+  return reinterpret_cast<T*>(p.out + (int64_t)(x.row + gc / g) * p.out_stride) + (int64_t)(kvh * g + gc % g) * D;
+}
+
+template <typename T, int D, typename S, int OCC>
+__global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParams p) {
+  constexpr int NT = S::NT, COPIES = S::COPIES, COLS = S::COLS, TILES = S::TILES, UNIT = S::UNIT, OWN = S::OWN;
   constexpr int W = D / 32, DT = D / 16;  // words a tile; dims a lane, P.V products
   constexpr int QP = Split<T>::Q, PP = Split<T>::P;
+  constexpr int NV = 4 * OWN;             // scores of a lane and column
   __shared__ int64_t s_pre[PA_NT + 1];
   __shared__ int64_t s_wave[PA_NT / 64];
-  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, c = lane & 15, q = lane >> 4;
+  __shared__ Stretch s_str[PA_NT / 64];
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), c = lane & 15, q = lane >> 4;
   const int nkv = p.packed.nkv, g = p.nq / nkv;
+  const int kvh = blockIdx.x % nkv, w = blockIdx.x / nkv * (PA_NT / 64) + wave;
 
   // ---- the units before each thread's requests ----
   const int per = (p.R + PA_NT - 1) / PA_NT;
@@ -146,7 +208,7 @@ __global__ __launch_bounds__(PA_NT) void packed_attn_kernel(PackedAttnParams p) 
   for (int i = 0; i < per; ++i) {
     const int r = t * per + i;
     if (r < p.R) {
-      const Request x = get_request<NT>(p, r);
+      const Request x = get_request<COLS, UNIT>(p, r);
       mine += (int64_t)x.tiles * x.steps;
     }
   }
@@ -157,6 +219,7 @@ __global__ __launch_bounds__(PA_NT) void packed_attn_kernel(PackedAttnParams p) 
     if (lane >= o) incl += u;
   }
   if (lane == 63) s_wave[wave] = incl;
+  if (lane == 0) s_str[wave] = Stretch{};
   __syncthreads();
   int64_t before = 0, total = 0;
 #pragma unroll
@@ -168,27 +231,22 @@ __global__ __launch_bounds__(PA_NT) void packed_attn_kernel(PackedAttnParams p) 
   if (t == 0) s_pre[0] = 0;
   __syncthreads();
 
-  const int id = __builtin_amdgcn_readfirstlane(blockIdx.x * (PA_NT / 64) + wave);
-  const int kvh = id % nkv, w = id / nkv;
-  if (w >= p.workers) return;
-  OpenItem* open = p.open + w;
-  if (kvh == 0 && lane == 0) *open = OpenItem{0, total, -1, 0};
   const int64_t workers = min((int64_t)p.workers, total);  // a unit each at least
-  if (w >= workers) return;
+  float* const slots = p.part + ((int64_t)kvh * p.workers + w) * 2 * p.part_cols * (D + 2);
+  if (w < workers) {
   const int64_t u0 = total * w / workers, u1 = total * (w + 1) / workers;
-
   int a = 0, b = PA_NT - 1;  // the last thread's requests that begin at or before u0
   while (a < b) {
     const int m = (a + b + 1) / 2;
     if (s_pre[m] <= u0) a = m;
     else b = m - 1;
   }
-  int r = a * per;
+  int r = __builtin_amdgcn_readfirstlane(a) * per;
   int64_t base = s_pre[a];
-  Request rq = get_request<NT>(p, r);
+  Request rq = get_request<COLS, UNIT>(p, r);
   while (base + (int64_t)rq.tiles * rq.steps <= u0) {
     base += (int64_t)rq.tiles * rq.steps;
-    rq = get_request<NT>(p, ++r);
+    rq = get_request<COLS, UNIT>(p, ++r);
   }
 
   const int B = p.packed.block_size, tpb = B / PK_TILE;
@@ -197,22 +255,23 @@ __global__ __launch_bounds__(PA_NT) void packed_attn_kernel(PackedAttnParams p) 
   const int64_t block_bytes = (int64_t)nkv * tpb * (17 * D);
   const int k_off = c * (D / 2) + q * (D / 8), v_off = 8 * D + q * (2 * D) + c * (D / 8);
   const int ks_off = 16 * D + c * (D / 32) + q * D / 128, vs_off = 16 * D + D / 2 + q * (D / 8) + c * D / 512 * 4;
+  const int copy = c / (16 / COPIES);  // whose tile the lane's column scores
 
   for (int64_t u = u0; u < u1;) {
     // ---- the stretch's part of one item ----
     const int tile = (int)((u - base) / rq.steps), first = (int)(u - base - (int64_t)tile * rq.steps);
     const int upto = (int)min((int64_t)rq.steps, first + (u1 - u));
-    const int cols = min(16 * NT, rq.m * g - tile * 16 * NT);  // of this tile
+    const int cols = min(COLS, rq.m * g - tile * COLS);  // of this tile
     // positions that every column sees, and that any does
-    const int i_lo = tile * 16 * NT / g, i_hi = (tile * 16 * NT + cols - 1) / g;
+    const int i_lo = tile * COLS / g, i_hi = (tile * COLS + cols - 1) / g;
     const int all = min(rq.len, rq.want - rq.m + i_lo + 1), some = min(rq.len, rq.want - rq.m + i_hi + 1);
-    const int stop = min(upto, (max(some, 0) + PA_UNIT - 1) / PA_UNIT);
+    const int stop = min(upto, (max(some, 0) + UNIT - 1) / UNIT);
 
     bf16x8 qf[NT][QP][W];
-    int limit[NT];  // positions column c of tile nt sees
+    int limit[NT];  // positions the lane's column sees
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      const int col = nt * 16 + c, gc = tile * 16 * NT + col, i = gc / g;
+      const int col = COPIES == 1 ? nt * 16 + c : c % (16 / COPIES), gc = tile * COLS + col, i = gc / g;
       limit[nt] = col < cols ? min(rq.len, rq.want - rq.m + i + 1) : some;
       const T* src = reinterpret_cast<const T*>(p.q + (int64_t)(rq.row + min(i, rq.m - 1)) * p.q_stride) +
                      (int64_t)(kvh * g + gc % g) * D + q * (D / 4);
@@ -244,87 +303,113 @@ __global__ __launch_bounds__(PA_NT) void packed_attn_kernel(PackedAttnParams p) 
       for (int j = 0; j < DT; ++j) o[nt][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
 
-    // 64 table entries at a time, one a lane
+    // records of a unit's tiles: 64 table entries at a time, one a lane
     const int32_t* table = p.tables + (int64_t)r * p.max_blocks;
     auto entries = [&](int b0) { return b0 + lane < p.max_blocks ? table[b0 + lane] : -1; };
-    int bi = first * 2 / tpb, ti = first * 2 % tpb;  // the next tile's block and place in it
+    int bi = first * TILES / tpb, ti = first * TILES % tpb;  // the next tile's block and place in it
     int window = bi, tab = entries(bi);
-    auto fetch = [&](Unit<D>& n) {
+    const char* rec[TILES];
+    auto locate = [&]() {  // bit x: tile x's block is in the arena
+      int there = 0;
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
+      for (int x = 0; x < TILES; ++x) {
         if (bi - window >= 64) {
           window = bi;
           tab = entries(bi);
         }
         const int e = __builtin_amdgcn_readlane(tab, bi - window);
-        n.there[x] = e >= 0 && e < p.num_blocks;
-        const char* rec = head + (n.there[x] ? e : 0) * block_bytes + ti * (17 * D);
-        load_words<D / 8>(rec + k_off, n.k[x]);
-        load_words<D / 8>(rec + v_off, n.v[x]);
-        n.ks[x] = (uint8_t)rec[ks_off];
-        n.vs[x] = *reinterpret_cast<const uint32_t*>(rec + vs_off);
+        const bool in = e >= 0 && e < p.num_blocks;
+        there |= (int)in << x;
+        rec[x] = head + (in ? e : 0) * block_bytes + ti * (17 * D);
         if (++ti == tpb) {
           ti = 0;
           ++bi;
         }
       }
+      return there;
     };
-
-    auto attend = [&](Unit<D>& n, int kt) {
-      const int j0 = kt * PA_UNIT + 4 * q;  // the lane's first position of tile 0
-      const bool whole = kt * PA_UNIT + PA_UNIT <= all && n.there[0] && n.there[1];
+    uint32_t kw[TILES][W], ks[TILES], vw[TILES][W], vs[TILES];
+    auto load_k = [&](int x) {
+      load_words<D / 8>(rec[x] + k_off, kw[x]);
+      ks[x] = (uint8_t)rec[x][ks_off];
+    };
+    auto load_v = [&](int x) {
+      load_words<D / 8>(rec[x] + v_off, vw[x]);
+      vs[x] = *reinterpret_cast<const uint32_t*>(rec[x] + vs_off);
+    };
+    int there = 0;
+    if (first < stop) {
+      there = locate();
+#pragma unroll
+      for (int x = 0; x < TILES; ++x) load_k(x);
+#pragma unroll
+      for (int x = 0; x < TILES; ++x) load_v(x);
+    }
+    for (int kt = first; kt < stop; ++kt) {
+      const bool more = kt + 1 < stop;
+      const int in = there;  // of this unit
+      if (more) there = locate();
+      const bool whole = (int64_t)(kt + 1) * UNIT <= all && in == (1 << TILES) - 1;
       // scores
-      f32x4 st[NT][2];
+      float sc[NT][NV];
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
+      for (int x = 0; x < TILES; ++x) {
+        f32x4 st[NT];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) st[nt][x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        const float ks = scale_of(n.ks[x]);
+        for (int nt = 0; nt < NT; ++nt) st[nt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        const float scale = scale_of(ks[x], 0);
 #pragma unroll
         for (int s = 0; s < W; ++s) {
           union { uint32_t w[4]; bf16x8 f; } kf;
-          kf.w[0] = pair_of<0>(n.k[x][s], ks);
-          kf.w[1] = pair_of<1>(n.k[x][s], ks);
-          kf.w[2] = pair_of<2>(n.k[x][s], ks);
-          kf.w[3] = pair_of<3>(n.k[x][s], ks);
+          kf.w[0] = pair_of<0>(kw[x][s], scale);
+          kf.w[1] = pair_of<1>(kw[x][s], scale);
+          kf.w[2] = pair_of<2>(kw[x][s], scale);
+          kf.w[3] = pair_of<3>(kw[x][s], scale);
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int part = 0; part < QP; ++part)
-              st[nt][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf.f, qf[nt][part][s], st[nt][x], 0, 0, 0);
+              st[nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf.f, qf[nt][part][s], st[nt], 0, 0, 0);
         }
+        if (more) load_k(x);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            if (COPIES == 1) sc[nt][4 * x + j] = st[nt][j];
+            else sc[nt][j] = x == 0 || copy == x ? st[nt][j] : sc[nt][j];
+          }
       }
+      // the lane's first position of the unit's first tile, and of its column's tile
+      const int p0 = kt * UNIT + 4 * q, c0 = p0 + (COPIES == 1 ? 0 : 16 * copy);
       bool nan_v = false;
       if (!whole) {
         // positions past a column's limit and in blocks that are not there leave its
         // softmax; V there may hold any bits, and 0 times them is not 0
 #pragma unroll
-        for (int x = 0; x < 2; ++x)
+        for (int i = 0; i < NV; ++i) {
+          const bool gone = !(in >> (COPIES == 1 ? i / 4 : copy) & 1);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+            if (gone || c0 + 16 * (i / 4) + i % 4 >= limit[nt]) sc[nt][i] = -INFINITY;
+        }
+#pragma unroll
+        for (int x = 0; x < TILES; ++x)
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const int pos = j0 + 16 * x + j;
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-              if (pos >= limit[nt] || !n.there[x]) st[nt][x][j] = -INFINITY;
-            if (pos >= some || !n.there[x]) {
-              constexpr int KB = D / 32;  // bytes of a position
-#pragma unroll
-              for (int y = 0; y < KB; ++y) n.v[x][(j * KB + y) / 4] &= ~(0xffu << ((j * KB + y) % 4 * 8));
-              n.vs[x] &= ~(0xffu << (8 * j));
-            }
-            nan_v |= (n.vs[x] >> (8 * j) & 0xff) == PK_NAN && pos >= all;
+            const int pos = p0 + 16 * x + j;
+            if (pos >= some || !(in >> x & 1)) clear_v<D>(vw[x], vs[x], j);
+            nan_v |= (vs[x] >> (8 * j) & 0xff) == PK_NAN && pos >= all;
           }
       }
       // weights
-      uint32_t pf[NT][PP][4];
+      uint32_t pw[NT][PP][NV / 2];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        float sc[8], mx = -INFINITY;
+        float mx = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          sc[i] = st[nt][i / 4][i % 4] * scale_log2;
-          mx = fmaxf(mx, sc[i]);
-        }
+        for (int i = 0; i < NV; ++i) mx = fmaxf(mx, sc[nt][i]);
+        mx *= scale_log2;
         mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
         mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
         if (__any(mx > m_run[nt] + SLACK)) {
@@ -341,124 +426,132 @@ __global__ __launch_bounds__(PA_NT) void packed_attn_kernel(PackedAttnParams p) 
         }
         // a column that has seen nothing yet: weights of 0
         const float m = m_run[nt] == -INFINITY ? 0.0f : m_run[nt];
+        float e[NV];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          sc[i] = __builtin_amdgcn_exp2f(sc[i] - m);
-          l_run[nt] += sc[i];
+        for (int i = 0; i < NV; ++i) {
+          e[i] = __builtin_amdgcn_exp2f(fmaf(sc[nt][i], scale_log2, -m));
+          l_run[nt] += e[i];
         }
 #pragma unroll
         for (int part = 0; part < PP; ++part)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            pf[nt][part][i] = pack_bf16(sc[2 * i], sc[2 * i + 1]);
-            sc[2 * i] -= __uint_as_float(pf[nt][part][i] << 16);
-            sc[2 * i + 1] -= __uint_as_float(pf[nt][part][i] & 0xffff0000u);
+          for (int i = 0; i < NV / 2; ++i) {
+            pw[nt][part][i] = pack_bf16(e[2 * i], e[2 * i + 1]);
+            e[2 * i] -= __uint_as_float(pw[nt][part][i] << 16);
+            e[2 * i + 1] -= __uint_as_float(pw[nt][part][i] & 0xffff0000u);
           }
       }
+      // a lane's words of its own tiles as the A operand of tiles 2y and 2y + 1
+      auto operand = [&](const uint32_t* own, int y) {
+        if constexpr (COPIES == 1) {
+          return __builtin_bit_cast(bf16x8, make_uint4(own[0], own[1], own[2], own[3]));
+        } else {
+          const bool lo = copy == 2 * y, hi = copy == 2 * y + 1;
+          return __builtin_bit_cast(bf16x8, make_uint4(lo ? own[0] : 0u, lo ? own[1] : 0u, hi ? own[0] : 0u,
+                                                       hi ? own[1] : 0u));
+        }
+      };
       if (!whole && __any(nan_v)) {
         // A NaN of V that some columns see and some do not: a product of ones counts,
         // for each column and dim, the NaN it sees; then V is 0 there.
-        uint32_t seen[NT][4], ind[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          uint32_t word = 0;
+        for (int y = 0; y < TILES / 2; ++y) {
+          uint32_t ind[4];
 #pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            const int k = 2 * i + y, x = k / 4, j = k % 4;
-            if ((n.vs[x] >> (8 * j) & 0xff) == PK_NAN) word |= 0x3f80u << (16 * y);
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t word = vs[2 * y + i / 2] >> (16 * (i % 2));  // scales of two positions
+            ind[i] = ((word & 0xff) == PK_NAN ? 0x3f80u : 0u) | ((word >> 8 & 0xff) == PK_NAN ? 0x3f800000u : 0u);
           }
-          ind[i] = word;
+          const bf16x8 nf = __builtin_bit_cast(bf16x8, make_uint4(ind[0], ind[1], ind[2], ind[3]));
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
-            seen[nt][i] = 0;
+            uint32_t seen[NV / 2];
 #pragma unroll
-            for (int y = 0; y < 2; ++y) {
-              const int k = 2 * i + y;
-              if (j0 + 16 * (k / 4) + k % 4 < limit[nt]) seen[nt][i] |= 0x3f80u << (16 * y);
+            for (int i = 0; i < NV / 2; ++i) {
+              const int pos = c0 + 16 * (i / 2) + 2 * (i % 2);
+              seen[i] = (pos < limit[nt] ? 0x3f80u : 0u) | (pos + 1 < limit[nt] ? 0x3f800000u : 0u);
             }
+            const f32x4 hits =
+                __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(seen, y), nf, f32x4{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              if (hits[j] > 0.0f)
+#pragma unroll
+                for (int d = 0; d < DT; ++d) o[nt][d][j] = __builtin_nanf("");
           }
         }
-        const bf16x8 nf = __builtin_bit_cast(bf16x8, make_uint4(ind[0], ind[1], ind[2], ind[3]));
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          const bf16x8 sf = __builtin_bit_cast(bf16x8, make_uint4(seen[nt][0], seen[nt][1], seen[nt][2], seen[nt][3]));
-          const f32x4 hits = __builtin_amdgcn_mfma_f32_16x16x32_bf16(sf, nf, f32x4{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
+        for (int x = 0; x < TILES; ++x)
 #pragma unroll
           for (int j = 0; j < 4; ++j)
-            if (hits[j] > 0.0f)
-#pragma unroll
-              for (int d = 0; d < DT; ++d) o[nt][d][j] = __builtin_nanf("");
-        }
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if ((n.vs[x] >> (8 * j) & 0xff) == PK_NAN) {
-              constexpr int KB = D / 32;
-#pragma unroll
-              for (int y = 0; y < KB; ++y) n.v[x][(j * KB + y) / 4] &= ~(0xffu << ((j * KB + y) % 4 * 8));
-              n.vs[x] &= ~(0xffu << (8 * j));
-            }
+            if ((vs[x] >> (8 * j) & 0xff) == PK_NAN) clear_v<D>(vw[x], vs[x], j);
       }
       // O += P V
-      float vs[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) vs[i] = scale_of(n.vs[i / 4] >> (8 * (i % 4)) & 0xff);
-      static_for<DT / 2>([&](auto S) {
-        constexpr int s = S;  // dims 2s and 2s + 1 of the lane
-        uint32_t pr[8];
-        static_for<8>([&](auto I) {
-          constexpr int i = I, byte = i % 4 * (D / 32) + s;
-          pr[i] = pair_of<byte % 4>(n.v[i / 4][byte / 4], vs[i]);
-        });
-        union { uint32_t w[4]; bf16x8 f; } lo, hi;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          lo.w[i] = __builtin_amdgcn_perm(pr[2 * i + 1], pr[2 * i], 0x05040100u);
-          hi.w[i] = __builtin_amdgcn_perm(pr[2 * i + 1], pr[2 * i], 0x07060302u);
-        }
+      for (int y = 0; y < TILES / 2; ++y) {
+        bf16x8 pf[NT][PP];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int part = 0; part < PP; ++part) {
-            const bf16x8 f = __builtin_bit_cast(bf16x8, make_uint4(pf[nt][part][0], pf[nt][part][1], pf[nt][part][2],
-                                                                   pf[nt][part][3]));
-            o[nt][2 * s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, lo.f, o[nt][2 * s], 0, 0, 0);
-            o[nt][2 * s + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, hi.f, o[nt][2 * s + 1], 0, 0, 0);
+          for (int part = 0; part < PP; ++part) pf[nt][part] = operand(pw[nt][part], y);
+        static_for<DT / 2>([&](auto DS) {
+          constexpr int s = DS;  // dims 2s and 2s + 1 of the lane
+          uint32_t pr[8];
+          static_for<8>([&](auto I) {
+            constexpr int i = I, byte = i % 4 * (D / 32) + s;
+            pr[i] = pair_of<byte % 4>(vw[2 * y + i / 4][byte / 4], scale_of(vs[2 * y + i / 4], i % 4));
+          });
+          union { uint32_t w[4]; bf16x8 f; } lo, hi;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            lo.w[i] = __builtin_amdgcn_perm(pr[2 * i + 1], pr[2 * i], 0x05040100u);
+            hi.w[i] = __builtin_amdgcn_perm(pr[2 * i + 1], pr[2 * i], 0x07060302u);
           }
-      });
-    };
-
-    Unit<D> now, next;
-    if (first < stop) fetch(now);
-    for (int kt = first; kt < stop; ++kt) {
-      if (kt + 1 < stop) fetch(next);
-      attend(now, kt);
-      now = next;
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int part = 0; part < PP; ++part) {
+              o[nt][2 * s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pf[nt][part], lo.f, o[nt][2 * s], 0, 0, 0);
+              o[nt][2 * s + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pf[nt][part], hi.f, o[nt][2 * s + 1], 0, 0, 0);
+            }
+        });
+        if (more) {
+          load_v(2 * y);
+          load_v(2 * y + 1);
+        }
+      }
     }
 
     // ---- the columns' outputs, or what there is of them ----
     const bool done = first == 0 && upto == rq.steps;
-    float* part = p.part + (((int64_t)kvh * p.workers + w) * 2 + (first > 0 ? 0 : 1)) * p.part_cols * (D + 2);
+    float* part = slots + (first > 0 ? 0 : 1) * p.part_cols * (D + 2);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       float l = l_run[nt] + __shfl_xor(l_run[nt], 16, 64);
       l += __shfl_xor(l, 32, 64);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const int col = nt * 16 + 4 * q + j;
-        const float lj = __shfl(l, 4 * q + j, 64), mj = __shfl(m_run[nt], 4 * q + j, 64);
-        if (col >= cols) continue;
+        // row 4q + j: column (4q + j) % (16 / COPIES) of copy (4q + j) / (16 / COPIES)
+        float lj = __shfl(l, 4 * q + j, 64), mj = __shfl(m_run[nt], 4 * q + j, 64);
         float x[DT];
 #pragma unroll
         for (int d = 0; d < DT; ++d) x[d] = o[nt][d][j];
-        if (done) {
-          const int gc = tile * 16 * NT + col;
-          T* dst = reinterpret_cast<T*>(p.out + (int64_t)(rq.row + gc / g) * p.out_stride) +
-                   (int64_t)(kvh * g + gc % g) * D + c * DT;
-          const float inv = lj == 0.0f ? 0.0f : 1.0f / lj;
 #pragma unroll
-          for (int d = 0; d < DT; ++d) Elem<T>::store(dst, d, lj == 0.0f ? 0.0f : x[d] * inv);
+        for (int step = 32; step > 32 / COPIES && COPIES > 1; step >>= 1) {  // the copies of a column
+          const float mo = __shfl_xor(mj, step, 64), m = fmaxf(mj, mo), mb = m == -INFINITY ? 0.0f : m;
+          const float f = __builtin_amdgcn_exp2f(mj - mb), fo = __builtin_amdgcn_exp2f(mo - mb);
+          lj = lj * f + __shfl_xor(lj, step, 64) * fo;
+#pragma unroll
+          for (int d = 0; d < DT; ++d) x[d] = x[d] * f + __shfl_xor(x[d], step, 64) * fo;
+          mj = m;
+        }
+        const int col = COPIES == 4 ? j : COPIES == 2 ? 4 * (q & 1) + j : nt * 16 + 4 * q + j;
+        if (col >= cols) continue;
+        if (COPIES == 4 ? q != j : COPIES == 2 ? q >= 2 : false) continue;  // one copy's lanes write
+        if (done) {
+          T* dst = out_of<T, D, COLS>(p, rq, tile, col, kvh) + c * DT;
+#pragma unroll
+          for (int d = 0; d < DT; ++d) Elem<T>::store(dst, d, lj == 0.0f ? 0.0f : x[d] / lj);
         } else {
           float* dst = part + col * (D + 2);
 #pragma unroll
@@ -470,95 +563,149 @@ __global__ __launch_bounds__(PA_NT) void packed_attn_kernel(PackedAttnParams p) 
         }
       }
     }
-    if (first == 0 && !done && kvh == 0 && lane == 0)
-      *open = OpenItem{base + (int64_t)(tile + 1) * rq.steps, total, r, tile};
+    if (!done && lane == 0) {
+      Stretch& me = s_str[wave];
+      const int which = first > 0 ? 0 : 1;
+      me.request[which] = r;
+      me.tile[which] = tile;
+      if (first > 0) {
+        me.head = 1;
+        me.head_closed = upto == rq.steps;
+      } else {
+        me.tail = 1;
+        me.end = base + (int64_t)(tile + 1) * rq.steps;
+      }
+    }
     u += upto - first;
     if (u < u1)
       while (base + (int64_t)rq.tiles * rq.steps <= u) {
         base += (int64_t)rq.tiles * rq.steps;
-        rq = get_request<NT>(p, ++r);
+        rq = get_request<COLS, UNIT>(p, ++r);
       }
   }
+  }
+
+  // ---- the workgroup's own merges: an item begun before it, and those its waves left
+  // open, each over the waves that went on with it ----
+  __syncthreads();
+  OpenItem open{0, total, -1, 0, 0};
+  for (int lead = -1; lead < PA_NT / 64; ++lead) {
+    const int at = max(lead, 0), which = lead < 0 ? 0 : 1;
+    if (!(lead < 0 ? s_str[0].head : s_str[at].tail)) continue;
+    int n = 1;
+    bool closed = lead < 0 && s_str[0].head_closed;
+    while (!closed && at + n < PA_NT / 64 && s_str[at + n].head) closed = s_str[at + n++].head_closed;
+    const int request = s_str[at].request[which], tile = s_str[at].tile[which];
+    if (lead >= 0 && !closed) open = OpenItem{s_str[at].end, total, request, tile, at};
+    if (n == 1) continue;
+    const Request x = get_request<COLS, UNIT>(p, request);
+    const int64_t pitch = (int64_t)2 * p.part_cols * (D + 2);
+    float* lead_slot = slots + (at - wave) * pitch + which * p.part_cols * (D + 2);
+    float* next = slots + (at + 1 - wave) * pitch;
+    for (int col = wave; col < min(COLS, x.m * g - tile * COLS); col += PA_NT / 64) {
+      constexpr int ND = (D + 63) / 64;
+      float acc[ND], m, l;
+      merge_column<T, D>([&](int i) { return (i == 0 ? lead_slot : next + (i - 1) * pitch) + col * (D + 2); }, n, lane,
+                         acc, m, l);
+      T* out = out_of<T, D, COLS>(p, x, tile, col, kvh);
+      float* dst = lead_slot + col * (D + 2);
+#pragma unroll
+      for (int d = 0; d < ND; ++d)
+        if (d * 64 + lane < D) {
+          if (lead >= 0 && closed) Elem<T>::store(out, d * 64 + lane, l == 0.0f ? 0.0f : acc[d] / l);
+          else dst[d * 64 + lane] = acc[d];
+        }
+      if (lane == 0 && !(lead >= 0 && closed)) {
+        dst[D] = m;
+        dst[D + 1] = l;
+      }
+    }
+  }
+  if (kvh == 0 && t == 0) p.open[blockIdx.x / nkv] = open;
 }
 
-// Workgroup (kv head, worker): the item that the worker began and left open, merged
-// over the workers that went on with it, in their order.  A wave takes every fourth
-// column, a lane D / 64 dims of it.
-template <typename T, int D, int NT>
+// Workgroup (kv head, workgroup of the first kernel): the item that it began and left
+// open, merged over the workgroups that went on with it, in their order.
+template <typename T, int D, typename S>
 __global__ __launch_bounds__(PA_NT) void packed_attn_merge_kernel(PackedAttnParams p) {
-  const int nkv = p.packed.nkv, g = p.nq / nkv, w = blockIdx.x / nkv, kvh = blockIdx.x % nkv;
-  const OpenItem it = p.open[w];
+  constexpr int COLS = S::COLS, ND = (D + 63) / 64, WG = PA_NT / 64;
+  const int nkv = p.packed.nkv, g = p.nq / nkv, wg = blockIdx.x / nkv, kvh = blockIdx.x % nkv;
+  const OpenItem it = p.open[wg];
   if (it.request < 0) return;
-  const Request rq = get_request<NT>(p, it.request);
-  const int cols = min(16 * NT, rq.m * g - it.tile * 16 * NT);
+  const Request rq = get_request<COLS, S::UNIT>(p, it.request);
+  const int cols = min(COLS, rq.m * g - it.tile * COLS);
   const int64_t workers = min((int64_t)p.workers, it.total);
-  int n = 1;  // with the workers after w whose stretches begin inside the item
-  while (w + n < workers && it.total * (w + n) / workers < it.end) ++n;
+  int n = 1;  // with the workgroups after it whose stretches begin inside the item
+  while ((int64_t)(wg + n) * WG < workers && it.total * ((wg + n) * WG) / workers < it.end) ++n;
   const int lane = threadIdx.x & 63;
   const int64_t pitch = (int64_t)2 * p.part_cols * (D + 2);
-  const float* first = p.part + ((int64_t)kvh * p.workers + w) * pitch;
-  for (int col = threadIdx.x >> 6; col < cols; col += PA_NT / 64) {
-    // worker w's second slot, the others' first
-    auto src = [&](int i) { return first + i * pitch + (i == 0 ? p.part_cols * (D + 2) : 0) + col * (D + 2); };
-    float m = -INFINITY;
-    for (int i = 0; i < n; ++i) m = fmaxf(m, src(i)[D]);
-    const float base = m == -INFINITY ? 0.0f : m;
-    float l = 0.0f, o[(D + 63) / 64] = {};
-    for (int i = 0; i < n; ++i) {
-      const float* x = src(i);
-      const float f = __builtin_amdgcn_exp2f(x[D] - base);
-      l = fmaf(x[D + 1], f, l);
+  const float* first = p.part + ((int64_t)kvh * p.workers + wg * WG) * pitch;
+  const float* lead = first + it.wave * pitch + p.part_cols * (D + 2);
+  for (int col = threadIdx.x >> 6; col < cols; col += WG) {
+    float acc[ND], m, l;
+    merge_column<T, D>([&](int i) { return (i == 0 ? lead : first + i * WG * pitch) + col * (D + 2); }, n, lane, acc, m,
+                       l);
+    T* out = out_of<T, D, COLS>(p, rq, it.tile, col, kvh);
 #pragma unroll
-      for (int d = 0; d < (D + 63) / 64; ++d)
-        if (d * 64 + lane < D) o[d] = fmaf(x[d * 64 + lane], f, o[d]);
-    }
-    const int gc = it.tile * 16 * NT + col;
-    T* dst = reinterpret_cast<T*>(p.out + (int64_t)(rq.row + gc / g) * p.out_stride) +
-             (int64_t)(kvh * g + gc % g) * D;
-#pragma unroll
-    for (int d = 0; d < (D + 63) / 64; ++d)
-      if (d * 64 + lane < D) Elem<T>::store(dst, d * 64 + lane, l == 0.0f ? 0.0f : o[d] / l);
+    for (int d = 0; d < ND; ++d)
+      if (d * 64 + lane < D) Elem<T>::store(out, d * 64 + lane, l == 0.0f ? 0.0f : acc[d] / l);
   }
 }
 
-// Column tiles of a wave: as many as the rows of one request fill.
-int column_tiles(int dtype, int g, int32_t max_query) {
+// Workgroups a CU holds by their registers.
+constexpr int occupancy_of(bool f32, int d, int nt) { return nt == 4 || (f32 && d == 128 && nt == 2) ? 1 : nt == 2 || (f32 && d == 128) ? 2 : 3; }
+
+// The kernel for a call's columns per request: as few column tiles as take them, and
+// where a tile's half or quarter does, as many copies.
+struct Plan {
+  int nt, copies, cols, unit, occupancy;
+};
+Plan plan_of(int dtype, int d, int g, int32_t max_query) {
   const int64_t cols = (int64_t)g * max_query;
-  return cols <= 16 ? 1 : cols <= 32 || dtype == KV_F32 ? 2 : 4;
+  const int copies = cols <= 4 ? 4 : cols <= 8 ? 2 : 1;
+  const int nt = cols <= 16 ? 1 : cols <= 32 || dtype == KV_F32 ? 2 : 4;
+  return Plan{nt, copies, 16 * nt / copies, copies == 4 ? 64 : 32,
+              occupancy_of(dtype == KV_F32, d, nt)};
 }
 
-// Stretches per kv head: PA_WAVES waves in all, but no more than units there can be.
-int workers_of(int nkv, int R, int64_t rows, int g, int nt, int64_t max_len) {
-  const int64_t items = R + rows * g / (16 * nt);
-  const int64_t units = items * ((max_len + PA_UNIT - 1) / PA_UNIT);
-  return (int)std::max<int64_t>(1, std::min<int64_t>((PA_WAVES + nkv - 1) / nkv, units));
+// Stretches per kv head: as many waves as the chip holds at once, but no more than
+// there can be units; whole workgroups.
+int workers_of(const Plan& pl, int nkv, int R, int64_t rows, int g, int64_t max_len) {
+  const int64_t items = R + rows * g / pl.cols;
+  const int64_t units = items * ((max_len + pl.unit - 1) / pl.unit);
+  const int64_t waves = 256 * 4 * (int64_t)pl.occupancy;
+  return (int)round_up(std::max<int64_t>(1, std::min<int64_t>((waves + nkv - 1) / nkv, units)), PA_NT / 64);
 }
 
-template <typename T, int D, int NT>
-void launch_nt(const PackedAttnParams& p, hipStream_t s) {
-  const int64_t waves = (int64_t)p.workers * p.packed.nkv;
-  hipLaunchKernelGGL((packed_attn_kernel<T, D, NT>), dim3((unsigned)((waves + 3) / 4)), dim3(PA_NT), 0, s, p);
-  hipLaunchKernelGGL((packed_attn_merge_kernel<T, D, NT>), dim3((unsigned)waves), dim3(PA_NT), 0, s, p);
+template <typename T, int D, typename S>
+void launch_shape(const PackedAttnParams& p, hipStream_t s) {
+  constexpr int OCC = occupancy_of(std::is_same<T, float>::value, D, S::NT);
+  const dim3 grid((unsigned)((int64_t)p.workers / (PA_NT / 64) * p.packed.nkv));
+  hipLaunchKernelGGL((packed_attn_kernel<T, D, S, OCC>), grid, dim3(PA_NT), 0, s, p);
+  hipLaunchKernelGGL((packed_attn_merge_kernel<T, D, S>), grid, dim3(PA_NT), 0, s, p);
 }
 template <typename T, int D>
-void launch(int nt, const PackedAttnParams& p, hipStream_t s) {
-  if (nt == 1) return launch_nt<T, D, 1>(p, s);
-  if (nt == 2) return launch_nt<T, D, 2>(p, s);
-  if constexpr (std::is_same<T, bf16_t>::value) launch_nt<T, D, 4>(p, s);
+void launch(const Plan& pl, const PackedAttnParams& p, hipStream_t s) {
+  if (pl.copies == 4) return launch_shape<T, D, Shape<1, 4>>(p, s);
+  if (pl.copies == 2) return launch_shape<T, D, Shape<1, 2>>(p, s);
+  if (pl.nt == 1) return launch_shape<T, D, Shape<1, 1>>(p, s);
+  if (pl.nt == 2) return launch_shape<T, D, Shape<2, 1>>(p, s);
+  if constexpr (std::is_same<T, bf16_t>::value) launch_shape<T, D, Shape<4, 1>>(p, s);
 }
 
-// The workspace: what workers left open, then their sums.
+// The workspace: what workgroups left open, then the waves' sums.
 struct AttnLayout {
-  int nt, workers, cols;
+  Plan plan;
+  int workers, cols;
   uint64_t part, total;
 };
 AttnLayout attn_layout(const kv_model_desc& d, int32_t R, int64_t rows, int32_t max_query, int64_t max_len) {
   AttnLayout L;
   const int g = d.num_q_heads / d.num_kv_heads;
-  L.nt = column_tiles(d.dtype, g, max_query);
-  L.workers = workers_of(d.num_kv_heads, R, rows, g, L.nt, max_len);
-  L.cols = (int)std::min<int64_t>(16 * L.nt, (int64_t)g * max_query);
-  L.part = (uint64_t)round_up((int64_t)L.workers * (int64_t)sizeof(OpenItem), 256);
+  L.plan = plan_of(d.dtype, d.head_dim, g, max_query);
+  L.workers = workers_of(L.plan, d.num_kv_heads, R, rows, g, max_len);
+  L.cols = (int)std::min<int64_t>(L.plan.cols, (int64_t)g * max_query);
+  L.part = (uint64_t)round_up((int64_t)L.workers / (PA_NT / 64) * (int64_t)sizeof(OpenItem), 256);
   L.total = L.part + (uint64_t)4 * d.num_kv_heads * L.workers * 2 * L.cols * (d.head_dim + 2);
   return L;
 }
@@ -595,10 +742,10 @@ void run(const kv_packed* packed, int32_t layer, const void* q, int64_t q_stride
   p.part_cols = L.cols;
   p.open = static_cast<OpenItem*>(workspace);
   p.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + L.part);
-  if (d.dtype == KV_BF16) launch<bf16_t, 128>(L.nt, p, s);
-  else if (d.head_dim == 128) launch<float, 128>(L.nt, p, s);
-  else if (d.head_dim == 64) launch<float, 64>(L.nt, p, s);
-  else launch<float, 32>(L.nt, p, s);
+  if (d.dtype == KV_BF16) launch<bf16_t, 128>(L.plan, p, s);
+  else if (d.head_dim == 128) launch<float, 128>(L.plan, p, s);
+  else if (d.head_dim == 64) launch<float, 64>(L.plan, p, s);
+  else launch<float, 32>(L.plan, p, s);
 }
 
 }  // namespace
