@@ -22,9 +22,11 @@
 //   O = P V: the lane's weights of two tiles are the A operand as they are (0 where the
 //   tile is another copy's), positions 4q .. 4q+3 of both being its eight k's; V's
 //   layout gives the lane the dims c d/16 .. of the same positions, which it pairs into
-//   the B operands of d/16 products.  Nothing passes through LDS.
-// A tile's next bytes are loaded as soon as its registers are free, K after the scores
-// and V after the products.
+//   the B operands of d/16 products.
+// Records reach a wave through a ring of its own in LDS, by direct-to-LDS loads: a
+// record is 17 d contiguous bytes, K's and V's lane by lane in the operands' order, so
+// the reads back are linear.  What bounds the kernel is the bytes in flight; the ring
+// keeps six or eight records a wave on their way without a register.
 // Weights enter the product as a bf16 number and the bf16 rest (2^-17 of a weight lost),
 // in fp32 models as three (as do the queries): rounding them once would cost more than
 // the output's own rounding where few positions weigh, and the products are not what
@@ -33,6 +35,7 @@
 #include <type_traits>
 
 #include "common.h"
+#include "dma.h"
 #include "host.h"
 #include "kvr_packed.h"
 #include "launch.h"
@@ -93,26 +96,38 @@ __device__ __forceinline__ void static_for(F&& f) {
   }
 }
 
+// Workgroups a CU holds by their registers, and the records of a wave's ring that
+// then fit its LDS.
+constexpr int occupancy_of(bool f32, int d, int nt, int copies) {
+  return nt == 4 || (f32 && d == 128 && nt == 2) ? 1 : nt == 2 || copies == 4 || (f32 && d == 128) ? 2 : 3;
+}
+constexpr int ring_of(int occupancy) { return occupancy == 3 ? 6 : 8; }
+
 struct Request {
   int row, m, len, want;  // first query row, rows, positions there are, position after the last query
   int tiles, steps;       // column tiles, units of each
 };
 template <int COLS, int UNIT>
-__device__ __forceinline__ Request get_request(const PackedAttnParams& p, int r) {
+__device__ __forceinline__ Request make_request(const PackedAttnParams& p, int row, int m, int want) {
   Request q;
-  q.row = r;
-  q.m = 1;
-  if (p.q_offsets) {
-    const int a = p.q_offsets[r], b = p.q_offsets[r + 1];
-    q.row = min(max(a, 0), (int)p.rows);
-    q.m = min(max(min(b, (int)p.rows) - q.row, 0), p.max_query);
-  }
-  q.want = p.lens[r];
-  q.len = (int)max((int64_t)0, min((int64_t)q.want, (int64_t)p.max_blocks * p.packed.block_size));
+  q.row = row;
+  q.m = m;
+  q.want = want;
+  q.len = (int)max((int64_t)0, min((int64_t)want, (int64_t)p.max_blocks * p.packed.block_size));
   const int g = p.nq / p.packed.nkv;
-  q.tiles = (int)(((int64_t)q.m * g + COLS - 1) / COLS);
+  q.tiles = (int)(((int64_t)m * g + COLS - 1) / COLS);
   q.steps = max(1, (int)(((int64_t)q.len + UNIT - 1) / UNIT));
   return q;
+}
+template <int COLS, int UNIT>
+__device__ __forceinline__ Request get_request(const PackedAttnParams& p, int r) {
+  int row = r, m = 1;
+  if (p.q_offsets) {
+    const int a = p.q_offsets[r], b = p.q_offsets[r + 1];
+    row = min(max(a, 0), (int)p.rows);
+    m = min(max(min(b, (int)p.rows) - row, 0), p.max_query);
+  }
+  return make_request<COLS, UNIT>(p, row, m, p.lens[r]);
 }
 
 // The scale of byte i of a word.  The conversions read the exponent alone, whatever the
@@ -195,7 +210,12 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
   constexpr int W = D / 32, DT = D / 16;  // words a tile; dims a lane, P.V products
   constexpr int QP = Split<T>::Q, PP = Split<T>::P;
   constexpr int NV = 4 * OWN;             // scores of a lane and column
-  __shared__ int64_t s_pre[PA_NT + 1];
+  constexpr int REC = 17 * D, RING = ring_of(OCC), LOADS = (16 * D + 1023) / 1024 + 1;
+  // the plan's arrays, then the waves' rings
+  __shared__ __attribute__((aligned(16))) char s_ring[PA_NT / 64][RING * REC];
+  static_assert(sizeof(s_ring) >= (PA_NT + 1) * 8 + PA_NT * 12, "the plan's arrays fit the rings");
+  int64_t* s_pre = reinterpret_cast<int64_t*>(&s_ring[0][0]);
+  int* s_req = reinterpret_cast<int*>(s_pre + PA_NT + 1);  // first row, rows, length of up to PA_NT requests
   __shared__ int64_t s_wave[PA_NT / 64];
   __shared__ Stretch s_str[PA_NT / 64];
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), c = lane & 15, q = lane >> 4;
@@ -210,6 +230,11 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
     if (r < p.R) {
       const Request x = get_request<COLS, UNIT>(p, r);
       mine += (int64_t)x.tiles * x.steps;
+      if (per == 1) {
+        s_req[3 * t] = x.row;
+        s_req[3 * t + 1] = x.m;
+        s_req[3 * t + 2] = x.want;
+      }
     }
   }
   int64_t incl = mine;
@@ -233,17 +258,29 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
 
   const int64_t workers = min((int64_t)p.workers, total);  // a unit each at least
   float* const slots = p.part + ((int64_t)kvh * p.workers + w) * 2 * p.part_cols * (D + 2);
+  int64_t u0 = 0, u1 = 0, base = 0;
+  int r = 0;
+  Request rq{};
   if (w < workers) {
-  const int64_t u0 = total * w / workers, u1 = total * (w + 1) / workers;
-  int a = 0, b = PA_NT - 1;  // the last thread's requests that begin at or before u0
-  while (a < b) {
-    const int m = (a + b + 1) / 2;
-    if (s_pre[m] <= u0) a = m;
-    else b = m - 1;
+    u0 = total * w / workers;
+    u1 = total * (w + 1) / workers;
+    int a = 0, b = PA_NT - 1;  // the last thread's requests that begin at or before u0
+    while (a < b) {
+      const int m = (a + b + 1) / 2;
+      if (s_pre[m] <= u0) a = m;
+      else b = m - 1;
+    }
+    r = __builtin_amdgcn_readfirstlane(a) * per;
+    base = s_pre[a];
+    if (per == 1)
+      rq = make_request<COLS, UNIT>(p, __builtin_amdgcn_readfirstlane(s_req[3 * a]),
+                                    __builtin_amdgcn_readfirstlane(s_req[3 * a + 1]),
+                                    __builtin_amdgcn_readfirstlane(s_req[3 * a + 2]));
+    else
+      rq = get_request<COLS, UNIT>(p, r);
   }
-  int r = __builtin_amdgcn_readfirstlane(a) * per;
-  int64_t base = s_pre[a];
-  Request rq = get_request<COLS, UNIT>(p, r);
+  __syncthreads();  // the rings are free
+  if (w < workers) {
   while (base + (int64_t)rq.tiles * rq.steps <= u0) {
     base += (int64_t)rq.tiles * rq.steps;
     rq = get_request<COLS, UNIT>(p, ++r);
@@ -253,6 +290,7 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
   const float scale_log2 = 1.4426950408889634f / sqrtf((float)D);
   const char* head = p.packed.base + (int64_t)kvh * tpb * (17 * D);
   const int64_t block_bytes = (int64_t)nkv * tpb * (17 * D);
+  char* const ring = s_ring[wave];
   const int k_off = c * (D / 2) + q * (D / 8), v_off = 8 * D + q * (2 * D) + c * (D / 8);
   const int ks_off = 16 * D + c * (D / 32) + q * D / 128, vs_off = 16 * D + D / 2 + q * (D / 8) + c * D / 512 * 4;
   const int copy = c / (16 / COPIES);  // whose tile the lane's column scores
@@ -267,29 +305,80 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
     const int all = min(rq.len, rq.want - rq.m + i_lo + 1), some = min(rq.len, rq.want - rq.m + i_hi + 1);
     const int stop = min(upto, (max(some, 0) + UNIT - 1) / UNIT);
 
-    bf16x8 qf[NT][QP][W];
+    // queries: loaded ahead of the records, used behind them
+    constexpr int QV = 8 * (int)sizeof(T) / 16;  // 16-byte pieces of eight dims
+    f32x4 qraw[NT][W][QV];
     int limit[NT];  // positions the lane's column sees
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      const int col = COPIES == 1 ? nt * 16 + c : c % (16 / COPIES), gc = tile * COLS + col, i = gc / g;
+      const int col = COPIES == 1 ? nt * 16 + c : c % (16 / COPIES), gc = tile * COLS + min(col, cols - 1), i = gc / g;
       limit[nt] = col < cols ? min(rq.len, rq.want - rq.m + i + 1) : some;
-      const T* src = reinterpret_cast<const T*>(p.q + (int64_t)(rq.row + min(i, rq.m - 1)) * p.q_stride) +
+      const T* src = reinterpret_cast<const T*>(p.q + (int64_t)(rq.row + i) * p.q_stride) +
                      (int64_t)(kvh * g + gc % g) * D + q * (D / 4);
 #pragma unroll
+      for (int s = 0; s < W; ++s)
+#pragma unroll
+        for (int e = 0; e < QV; ++e) qraw[nt][s][e] = reinterpret_cast<const f32x4_a4*>(src + 8 * s)[e];
+    }
+
+    // the ring: 64 table entries at a time, one a lane
+    const int32_t* table = p.tables + (int64_t)r * p.max_blocks;
+    auto entries = [&](int b0) {
+      int e = b0 + lane < p.max_blocks ? table[b0 + lane] : -1;
+      asm volatile("" : "+v"(e));  // waited for here, not at every use: that would wait for the ring's loads too
+      return e;
+    };
+    int next = first * TILES, bi = next / tpb, ti = next % tpb;  // the next record, its block and place in it
+    const int last = stop * TILES;
+    int window = bi, tab = entries(bi);
+    int put = 0, get = 0;   // bytes into the ring
+    uint32_t there = 0;     // bit n % 32: record n's block is in the arena
+    auto issue = [&]() {
+      if (bi - window >= 64) {
+        window = bi;
+        tab = entries(bi);
+      }
+      const int e = __builtin_amdgcn_readlane(tab, bi - window);
+      const bool in = e >= 0 && e < p.num_blocks;
+      there = (there & ~(1u << (next & 31))) | (uint32_t)in << (next & 31);
+      const char* rec = head + (in ? e : 0) * block_bytes + ti * REC;
+      constexpr int FULL = 16 * D / 1024;
+#pragma unroll
+      for (int i = 0; i < FULL; ++i) load_lds(rec, REC, ring + put + 1024 * i, lane * 16, 1024 * i);
+      if (FULL == 0 && lane < D) load_lds(rec, REC, ring + put, lane * 16, 0);
+      if (lane < D / 16) load_lds(rec, REC, ring + put + 16 * D, lane * 16, 16 * D);
+      put = put == (RING - 1) * REC ? 0 : put + REC;
+      ++next;
+      if (++ti == tpb) {
+        ti = 0;
+        ++bi;
+      }
+    };
+    for (int i = 0; i < RING && next < last; ++i) issue();
+
+    bf16x8 qf[NT][QP][W];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const bool used = (COPIES == 1 ? nt * 16 + c : c % (16 / COPIES)) < cols;
+#pragma unroll
       for (int s = 0; s < W; ++s) {
-        float x[8];
+        if constexpr (QP == 1) {
+          qf[nt][0][s] = used ? __builtin_bit_cast(bf16x8, qraw[nt][s][0]) : bf16x8{};
+        } else {
+          float x[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = col < cols ? Elem<T>::load(src, 8 * s + e) : 0.0f;
+          for (int e = 0; e < 8; ++e) x[e] = used ? qraw[nt][s][e / 4 % QV][e % 4] : 0.0f;
 #pragma unroll
-        for (int part = 0; part < QP; ++part) {
-          union { uint32_t w[4]; bf16x8 f; } f;
+          for (int part = 0; part < QP; ++part) {
+            union { uint32_t w[4]; bf16x8 f; } f;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            f.w[e] = pack_bf16(x[2 * e], x[2 * e + 1]);
-            x[2 * e] -= __uint_as_float(f.w[e] << 16);
-            x[2 * e + 1] -= __uint_as_float(f.w[e] & 0xffff0000u);
+            for (int e = 0; e < 4; ++e) {
+              f.w[e] = pack_bf16(x[2 * e], x[2 * e + 1]);
+              x[2 * e] -= __uint_as_float(f.w[e] << 16);
+              x[2 * e + 1] -= __uint_as_float(f.w[e] & 0xffff0000u);
+            }
+            qf[nt][part][s] = f.f;
           }
-          qf[nt][part][s] = f.f;
         }
       }
     }
@@ -303,52 +392,21 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
       for (int j = 0; j < DT; ++j) o[nt][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
 
-    // records of a unit's tiles: 64 table entries at a time, one a lane
-    const int32_t* table = p.tables + (int64_t)r * p.max_blocks;
-    auto entries = [&](int b0) { return b0 + lane < p.max_blocks ? table[b0 + lane] : -1; };
-    int bi = first * TILES / tpb, ti = first * TILES % tpb;  // the next tile's block and place in it
-    int window = bi, tab = entries(bi);
-    const char* rec[TILES];
-    auto locate = [&]() {  // bit x: tile x's block is in the arena
-      int there = 0;
+    for (int kt = first; kt < stop; ++kt) {
+      // this unit's records have landed; of those behind it, RING - TILES at most are on their way
+      const int behind = next - (kt + 1) * TILES;
+      if (behind >= RING - TILES) KVR_WAIT_VMCNT((RING - TILES) * LOADS);
+      else if (RING - TILES > TILES && behind >= RING - 2 * TILES) KVR_WAIT_VMCNT((RING - 2 * TILES) * LOADS);
+      else KVR_WAIT_VMCNT(0);
+      asm volatile("" ::: "memory");  // the reads below stay below
+      const uint32_t bits = there >> (kt * TILES & 31);
+      const int in = bits & ((1 << TILES) - 1);  // TILES divides 32: the unit's bits are neighbours
+      const char* rec[TILES];
 #pragma unroll
       for (int x = 0; x < TILES; ++x) {
-        if (bi - window >= 64) {
-          window = bi;
-          tab = entries(bi);
-        }
-        const int e = __builtin_amdgcn_readlane(tab, bi - window);
-        const bool in = e >= 0 && e < p.num_blocks;
-        there |= (int)in << x;
-        rec[x] = head + (in ? e : 0) * block_bytes + ti * (17 * D);
-        if (++ti == tpb) {
-          ti = 0;
-          ++bi;
-        }
+        rec[x] = ring + get;
+        get = get == (RING - 1) * REC ? 0 : get + REC;
       }
-      return there;
-    };
-    uint32_t kw[TILES][W], ks[TILES], vw[TILES][W], vs[TILES];
-    auto load_k = [&](int x) {
-      load_words<D / 8>(rec[x] + k_off, kw[x]);
-      ks[x] = (uint8_t)rec[x][ks_off];
-    };
-    auto load_v = [&](int x) {
-      load_words<D / 8>(rec[x] + v_off, vw[x]);
-      vs[x] = *reinterpret_cast<const uint32_t*>(rec[x] + vs_off);
-    };
-    int there = 0;
-    if (first < stop) {
-      there = locate();
-#pragma unroll
-      for (int x = 0; x < TILES; ++x) load_k(x);
-#pragma unroll
-      for (int x = 0; x < TILES; ++x) load_v(x);
-    }
-    for (int kt = first; kt < stop; ++kt) {
-      const bool more = kt + 1 < stop;
-      const int in = there;  // of this unit
-      if (more) there = locate();
       const bool whole = (int64_t)(kt + 1) * UNIT <= all && in == (1 << TILES) - 1;
       // scores
       float sc[NT][NV];
@@ -357,21 +415,22 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
         f32x4 st[NT];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) st[nt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        const float scale = scale_of(ks[x], 0);
+        uint32_t kw[W];
+        load_words<D / 8>(rec[x] + k_off, kw);
+        const float scale = scale_of((uint8_t)rec[x][ks_off], 0);
 #pragma unroll
         for (int s = 0; s < W; ++s) {
           union { uint32_t w[4]; bf16x8 f; } kf;
-          kf.w[0] = pair_of<0>(kw[x][s], scale);
-          kf.w[1] = pair_of<1>(kw[x][s], scale);
-          kf.w[2] = pair_of<2>(kw[x][s], scale);
-          kf.w[3] = pair_of<3>(kw[x][s], scale);
+          kf.w[0] = pair_of<0>(kw[s], scale);
+          kf.w[1] = pair_of<1>(kw[s], scale);
+          kf.w[2] = pair_of<2>(kw[s], scale);
+          kf.w[3] = pair_of<3>(kw[s], scale);
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int part = 0; part < QP; ++part)
               st[nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf.f, qf[nt][part][s], st[nt], 0, 0, 0);
         }
-        if (more) load_k(x);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -382,6 +441,12 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
       }
       // the lane's first position of the unit's first tile, and of its column's tile
       const int p0 = kt * UNIT + 4 * q, c0 = p0 + (COPIES == 1 ? 0 : 16 * copy);
+      uint32_t vw[TILES][W], vs[TILES];
+#pragma unroll
+      for (int x = 0; x < TILES; ++x) {
+        load_words<D / 8>(rec[x] + v_off, vw[x]);
+        vs[x] = *reinterpret_cast<const uint32_t*>(rec[x] + vs_off);
+      }
       bool nan_v = false;
       if (!whole) {
         // positions past a column's limit and in blocks that are not there leave its
@@ -515,11 +580,12 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
               o[nt][2 * s + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pf[nt][part], hi.f, o[nt][2 * s + 1], 0, 0, 0);
             }
         });
-        if (more) {
-          load_v(2 * y);
-          load_v(2 * y + 1);
-        }
       }
+      KVR_WAIT_LGKM0();  // the unit's records are in registers: the ring takes the next ones
+      asm volatile("" ::: "memory");
+#pragma unroll
+      for (int x = 0; x < TILES; ++x)
+        if (next < last) issue();
     }
 
     // ---- the columns' outputs, or what there is of them ----
@@ -652,9 +718,6 @@ __global__ __launch_bounds__(PA_NT) void packed_attn_merge_kernel(PackedAttnPara
   }
 }
 
-// Workgroups a CU holds by their registers.
-constexpr int occupancy_of(bool f32, int d, int nt) { return nt == 4 || (f32 && d == 128 && nt == 2) ? 1 : nt == 2 || (f32 && d == 128) ? 2 : 3; }
-
 // The kernel for a call's columns per request: as few column tiles as take them, and
 // where a tile's half or quarter does, as many copies.
 struct Plan {
@@ -665,7 +728,7 @@ Plan plan_of(int dtype, int d, int g, int32_t max_query) {
   const int copies = cols <= 4 ? 4 : cols <= 8 ? 2 : 1;
   const int nt = cols <= 16 ? 1 : cols <= 32 || dtype == KV_F32 ? 2 : 4;
   return Plan{nt, copies, 16 * nt / copies, copies == 4 ? 64 : 32,
-              occupancy_of(dtype == KV_F32, d, nt)};
+              occupancy_of(dtype == KV_F32, d, nt, copies)};
 }
 
 // Stretches per kv head: as many waves as the chip holds at once, but no more than
@@ -679,7 +742,7 @@ int workers_of(const Plan& pl, int nkv, int R, int64_t rows, int g, int64_t max_
 
 template <typename T, int D, typename S>
 void launch_shape(const PackedAttnParams& p, hipStream_t s) {
-  constexpr int OCC = occupancy_of(std::is_same<T, float>::value, D, S::NT);
+  constexpr int OCC = occupancy_of(std::is_same<T, float>::value, D, S::NT, S::COPIES);
   const dim3 grid((unsigned)((int64_t)p.workers / (PA_NT / 64) * p.packed.nkv));
   hipLaunchKernelGGL((packed_attn_kernel<T, D, S, OCC>), grid, dim3(PA_NT), 0, s, p);
   hipLaunchKernelGGL((packed_attn_merge_kernel<T, D, S>), grid, dim3(PA_NT), 0, s, p);
