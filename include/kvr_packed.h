@@ -111,7 +111,7 @@ uint64_t kv_packed_attention_workspace_bytes(const kv_model_desc* desc, int32_t 
  * left with no position is zero.  Nothing but a request's rows of out is written;
  * q and out may be the same memory only as the same rows.  The arrays on the device are
  * read when the call runs there, so a captured call follows their contents.
- *   KV_EINVAL  null arrays, a layer outside the model, negative sizes, a stride below
+ *   KV_EINVAL  null arrays, a layer outside the model, negative sizes, rows above 2^24, a stride below
  *              nq * d, a pointer or stride not on its boundary (4 bytes), more than 16
  *              q heads per kv head, rows != num_requests without q_offsets, max_query
  *              or max_len < 1

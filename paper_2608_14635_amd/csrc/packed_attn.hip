@@ -61,16 +61,16 @@ template <typename T> struct Split;  // bf16 numbers that stand for a query, for
 template <> struct Split<bf16_t> { static constexpr int Q = 1, P = 2; };
 template <> struct Split<float> { static constexpr int Q = 3, P = 3; };
 
-// The item that a workgroup began and left open: its units' end, the units of all
-// items, and the wave that began it.
+// The item that a workgroup began and left open, for the second kernel: its columns (0:
+// none), first query row and column tile, the wave that began it, and the workgroups
+// that hold sums of it.
 struct OpenItem {
-  int64_t end, total;
-  int request, tile, wave;  // request -1: none
+  int cols, row, tile, wave, groups;
 };
 
 struct PackedAttnParams {
   PackedLayer packed;
-  int64_t num_blocks;
+  uint32_t num_blocks;           // of the arena, or all that an entry can name
   const char* q;                 // rows of queries, model dtype
   char* out;
   int64_t q_stride, out_stride;  // bytes
@@ -79,7 +79,8 @@ struct PackedAttnParams {
   const int32_t* lens;
   const int32_t* tables;
   int R, max_blocks;
-  int nq;
+  int nq, g;                     // q heads, and those of a kv head
+  uint32_t g_inv;                // ceil(2^32 / g), 0 for g = 1: n / g of n < 2^28 is the product's high half
   int max_query;                 // rows of a request past it are left out: the sums have no room
   int workers;                   // stretches per kv head, a multiple of four
   int part_cols;                 // columns of a slot of sums
@@ -103,6 +104,37 @@ constexpr int occupancy_of(bool f32, int d, int nt, int copies) {
 }
 constexpr int ring_of(int occupancy) { return occupancy == 3 ? 6 : 8; }
 
+__device__ __forceinline__ int by_g(const PackedAttnParams& p, int n) {
+  return p.g_inv ? (int)__umulhi((uint32_t)n, p.g_inv) : n;
+}
+// a / b of whole numbers below 2^53 / b: a correctly rounded quotient never reaches the
+// next whole number
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) { return (int64_t)((double)a / (double)b); }
+// The maximum of the four lanes (q, c) of a c.
+__device__ __forceinline__ float max_over_q(float v) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+// a value that all lanes share, as a scalar
+__device__ __forceinline__ int64_t uniform(int64_t v) {
+  return (int64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)v) |
+         (int64_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32;
+}
+
+// Stretches: workers equal parts of all units, the first ones a unit longer.
+struct Stretches {
+  int workers;
+  int64_t size, longer;
+  __device__ __forceinline__ Stretches(int most, int64_t total) {
+    workers = (int)min((int64_t)most, total);  // a unit each at least
+    size = total ? quotient(total, workers) : 0;
+    longer = total - size * workers;
+  }
+  __device__ __forceinline__ int64_t begin(int w) const { return w * size + min((int64_t)w, longer); }
+};
+
 struct Request {
   int row, m, len, want;  // first query row, rows, positions there are, position after the last query
   int tiles, steps;       // column tiles, units of each
@@ -114,8 +146,7 @@ __device__ __forceinline__ Request make_request(const PackedAttnParams& p, int r
   q.m = m;
   q.want = want;
   q.len = (int)max((int64_t)0, min((int64_t)want, (int64_t)p.max_blocks * p.packed.block_size));
-  const int g = p.nq / p.packed.nkv;
-  q.tiles = (int)(((int64_t)m * g + COLS - 1) / COLS);
+  q.tiles = (int)(((int64_t)m * p.g + COLS - 1) / COLS);
   q.steps = max(1, (int)(((int64_t)q.len + UNIT - 1) / UNIT));
   return q;
 }
@@ -134,6 +165,12 @@ __device__ __forceinline__ Request get_request(const PackedAttnParams& p, int r)
 // neighbouring bytes leave in the sign and the mantissa.
 __device__ __forceinline__ float scale_of(uint32_t word, int i) {
   return __uint_as_float(i == 3 ? word >> 1 : word << (23 - 8 * i));
+}
+
+// Masks of a word's first n bytes, and of its bytes that are 255.
+__device__ __forceinline__ uint32_t first_bytes(int n) { return n >= 4 ? ~0u : n <= 0 ? 0u : (1u << 8 * n) - 1; }
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
+  return (((w & 0x7f7f7f7fu) + 0x01010101u) & w & 0x80808080u) >> 7;  // 1 in each
 }
 
 template <int BYTES>
@@ -158,50 +195,118 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
 }
 
-// One position's values of a lane's V bytes, and its scale, to 0.
-template <int D>
-__device__ __forceinline__ void clear_v(uint32_t* v, uint32_t& vs, int j) {
-  constexpr int KB = D / 32;  // bytes of a position
-#pragma unroll
-  for (int y = 0; y < KB; ++y) v[(j * KB + y) / 4] &= ~(0xffu << ((j * KB + y) % 4 * 8));
-  vs &= ~(0xffu << (8 * j));
-}
-
-// What a wave's stretch holds of items that are not its own alone.
+// What a wave's stretch holds of items that are not its own alone: of one begun before
+// it ([0]), of one it leaves open ([1]).
 struct Stretch {
-  int head, head_closed;          // it begins inside an item; the item ends in it
-  int tail;                       // it begins an item and leaves it open
-  int request[2], tile[2];        // those items
+  int cols[2];                    // columns, 0: no such item
+  int row[2], tile[2];
+  const float* sums[2];           // in the wave's ring or in the workspace
+  int head_closed;                // the item begun before ends in it
   int64_t end;                    // the open item's units' end
 };
 
-// One column of an item, from n partials of D sums, maximum and sum: o (of dims 64 i +
-// lane), and where the columns end up.
-template <typename T, int D, typename SRC>
-__device__ __forceinline__ void merge_column(SRC src, int n, int lane, float* o, float& m, float& l) {
-  constexpr int ND = (D + 63) / 64;
-  m = -INFINITY;
-  for (int i = 0; i < n; ++i) m = fmaxf(m, src(i)[D]);
-  const float base = m == -INFINITY ? 0.0f : m;
-  l = 0.0f;
+// One column from n partials of D sums, a maximum and a sum of weights, in their order:
+// the lane's dims DPL lane .. of the sums.
+template <int D>
+constexpr int DPL = D < 64 ? 1 : D / 64;  // dims of a lane
+template <int D>
+struct Column {
+  float m, l, o[DPL<D>];
+};
+template <int D, int CHUNK, typename SRC>  // CHUNK: partials whose loads are on their way together
+__device__ __forceinline__ Column<D> merge_column(SRC src, int n, int lane) {
+  const int at = lane * DPL<D> % D;
+  Column<D> x;
+  x.m = -INFINITY;
+  x.l = 0.0f;
 #pragma unroll
-  for (int d = 0; d < ND; ++d) o[d] = 0.0f;
-#pragma unroll 4
-  for (int i = 0; i < n; ++i) {
-    const float* x = src(i);
-    const float f = __builtin_amdgcn_exp2f(x[D] - base);
-    l = fmaf(x[D + 1], f, l);
+  for (int d = 0; d < DPL<D>; ++d) x.o[d] = 0.0f;
+#pragma unroll 1
+  for (int i0 = 0; i0 < n; i0 += CHUNK) {
+    const int mine = min(i0 + lane % CHUNK, n - 1);
+    float m = src(mine)[D], l = src(mine)[D + 1];
+    float o[CHUNK][DPL<D>];
 #pragma unroll
-    for (int d = 0; d < ND; ++d)
-      if (d * 64 + lane < D) o[d] = fmaf(x[d * 64 + lane], f, o[d]);
+    for (int i = 0; i < CHUNK; ++i)
+      if (i0 + i < n)
+#pragma unroll
+        for (int d = 0; d < DPL<D>; ++d) o[i][d] = src(i0 + i)[at + d];
+    if (i0 + lane % CHUNK >= n) {
+      m = -INFINITY;
+      l = 0.0f;
+    }
+    float top = fmaxf(x.m, m);
+#pragma unroll
+    for (int w = CHUNK / 2; w > 0; w >>= 1) top = fmaxf(top, __shfl_xor(top, w, 64));
+    const float base = top == -INFINITY ? 0.0f : top;
+    const float was = __builtin_amdgcn_exp2f(x.m - base), f = __builtin_amdgcn_exp2f(m - base);
+    l *= f;
+#pragma unroll
+    for (int w = CHUNK / 2; w > 0; w >>= 1) l += __shfl_xor(l, w, 64);
+    x.l = fmaf(x.l, was, l);
+    x.m = top;
+#pragma unroll
+    for (int d = 0; d < DPL<D>; ++d) x.o[d] *= was;
+#pragma unroll
+    for (int i = 0; i < CHUNK; ++i)
+      if (i0 + i < n) {
+        const float fi = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), i));
+#pragma unroll
+        for (int d = 0; d < DPL<D>; ++d) x.o[d] = fmaf(o[i][d], fi, x.o[d]);
+      }
   }
+  return x;
 }
 
-// The output row of a column of request x's tile, at kv head kvh.
+// The same of N partials at hand.
+template <int D, int N, typename SRC>
+__device__ __forceinline__ Column<D> merge_column(SRC src, int lane) {
+  const int at = lane * DPL<D> % D;
+  Column<D> x;
+  x.m = src(0)[D];
+#pragma unroll
+  for (int k = 1; k < N; ++k) x.m = fmaxf(x.m, src(k)[D]);
+  const float base = x.m == -INFINITY ? 0.0f : x.m;
+  x.l = 0.0f;
+#pragma unroll
+  for (int d = 0; d < DPL<D>; ++d) x.o[d] = 0.0f;
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    const float f = N == 1 ? 1.0f : __builtin_amdgcn_exp2f(src(k)[D] - base);
+    x.l = fmaf(src(k)[D + 1], f, x.l);
+#pragma unroll
+    for (int d = 0; d < DPL<D>; ++d) x.o[d] = fmaf(src(k)[at + d], f, x.o[d]);
+  }
+  return x;
+}
+
+// A merged column of a tile as its output row at kv head kvh, the tile's request's query
+// rows from `row` on, or as a partial.
 template <typename T, int D, int COLS>
-__device__ __forceinline__ T* out_of(const PackedAttnParams& p, const Request& x, int tile, int col, int kvh) {
-  const int g = p.nq / p.packed.nkv, gc = tile * COLS + col;
-  return reinterpret_cast<T*>(p.out + (int64_t)(x.row + gc / g) * p.out_stride) + (int64_t)(kvh * g + gc % g) * D;
+__device__ __forceinline__ void put_out(const PackedAttnParams& p, int row, int tile, int col, int kvh, int lane,
+                                        const Column<D>& v) {
+  if (lane * DPL<D> >= D) return;
+  const int gc = tile * COLS + col, i = by_g(p, gc);
+  T* dst = reinterpret_cast<T*>(p.out + (int64_t)(row + i) * p.out_stride) +
+           (int64_t)(kvh * p.g + gc - i * p.g) * D + lane * DPL<D>;
+  const float inv = v.l == 0.0f ? 0.0f : 1.0f / v.l;
+  if constexpr (DPL<D> == 2 && sizeof(T) == 2) {
+    *reinterpret_cast<uint32_t*>(dst) = v.l == 0.0f ? 0u : pack_bf16(v.o[0] * inv, v.o[1] * inv);
+  } else {
+#pragma unroll
+    for (int d = 0; d < DPL<D>; ++d) Elem<T>::store(dst, d, v.l == 0.0f ? 0.0f : v.o[d] * inv);
+  }
+}
+template <int D>
+__device__ __forceinline__ void put_part(float* dst, int lane, const Column<D>& v) {
+  if (lane * DPL<D> < D) {
+#pragma unroll
+    for (int d = 0; d < DPL<D>; ++d) dst[lane * DPL<D> + d] = v.o[d];
+  }
+  if (lane == 0) {
+    dst[D] = v.m;
+    dst[D + 1] = v.l;
+  }
 }
 
 template <typename T, int D, typename S, int OCC>
@@ -213,13 +318,16 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
   constexpr int REC = 17 * D, RING = ring_of(OCC), LOADS = (16 * D + 1023) / 1024 + 1;
   // the plan's arrays, then the waves' rings
   __shared__ __attribute__((aligned(16))) char s_ring[PA_NT / 64][RING * REC];
+  static_assert(RING % TILES == 0, "units do not wrap in the ring");
+  static_assert(RING * REC >= 64 * (D + 2), "16 rows fit the ring");
+  constexpr bool LOCAL = RING * REC >= NT * 64 * (D + 2);  // all columns' rows do
   static_assert(sizeof(s_ring) >= (PA_NT + 1) * 8 + PA_NT * 12, "the plan's arrays fit the rings");
   int64_t* s_pre = reinterpret_cast<int64_t*>(&s_ring[0][0]);
   int* s_req = reinterpret_cast<int*>(s_pre + PA_NT + 1);  // first row, rows, length of up to PA_NT requests
   __shared__ int64_t s_wave[PA_NT / 64];
   __shared__ Stretch s_str[PA_NT / 64];
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), c = lane & 15, q = lane >> 4;
-  const int nkv = p.packed.nkv, g = p.nq / nkv;
+  const int nkv = p.packed.nkv, g = p.g;
   const int kvh = blockIdx.x % nkv, w = blockIdx.x / nkv * (PA_NT / 64) + wave;
 
   // ---- the units before each thread's requests ----
@@ -256,22 +364,23 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
   if (t == 0) s_pre[0] = 0;
   __syncthreads();
 
-  const int64_t workers = min((int64_t)p.workers, total);  // a unit each at least
+  total = uniform(total);
+  const Stretches st(p.workers, total);
   float* const slots = p.part + ((int64_t)kvh * p.workers + w) * 2 * p.part_cols * (D + 2);
   int64_t u0 = 0, u1 = 0, base = 0;
   int r = 0;
   Request rq{};
-  if (w < workers) {
-    u0 = total * w / workers;
-    u1 = total * (w + 1) / workers;
+  if (w < st.workers) {
+    u0 = st.begin(w);
+    u1 = st.begin(w + 1);
     int a = 0, b = PA_NT - 1;  // the last thread's requests that begin at or before u0
     while (a < b) {
       const int m = (a + b + 1) / 2;
-      if (s_pre[m] <= u0) a = m;
+      if (uniform(s_pre[m]) <= u0) a = m;
       else b = m - 1;
     }
-    r = __builtin_amdgcn_readfirstlane(a) * per;
-    base = s_pre[a];
+    r = a * per;
+    base = uniform(s_pre[a]);
     if (per == 1)
       rq = make_request<COLS, UNIT>(p, __builtin_amdgcn_readfirstlane(s_req[3 * a]),
                                     __builtin_amdgcn_readfirstlane(s_req[3 * a + 1]),
@@ -280,7 +389,7 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
       rq = get_request<COLS, UNIT>(p, r);
   }
   __syncthreads();  // the rings are free
-  if (w < workers) {
+  if (w < st.workers) {
   while (base + (int64_t)rq.tiles * rq.steps <= u0) {
     base += (int64_t)rq.tiles * rq.steps;
     rq = get_request<COLS, UNIT>(p, ++r);
@@ -297,11 +406,11 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
 
   for (int64_t u = u0; u < u1;) {
     // ---- the stretch's part of one item ----
-    const int tile = (int)((u - base) / rq.steps), first = (int)(u - base - (int64_t)tile * rq.steps);
+    const int tile = (int)quotient(u - base, rq.steps), first = (int)(u - base - (int64_t)tile * rq.steps);
     const int upto = (int)min((int64_t)rq.steps, first + (u1 - u));
     const int cols = min(COLS, rq.m * g - tile * COLS);  // of this tile
     // positions that every column sees, and that any does
-    const int i_lo = tile * COLS / g, i_hi = (tile * COLS + cols - 1) / g;
+    const int i_lo = by_g(p, tile * COLS), i_hi = by_g(p, tile * COLS + cols - 1);
     const int all = min(rq.len, rq.want - rq.m + i_lo + 1), some = min(rq.len, rq.want - rq.m + i_hi + 1);
     const int stop = min(upto, (max(some, 0) + UNIT - 1) / UNIT);
 
@@ -311,10 +420,10 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
     int limit[NT];  // positions the lane's column sees
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      const int col = COPIES == 1 ? nt * 16 + c : c % (16 / COPIES), gc = tile * COLS + min(col, cols - 1), i = gc / g;
+      const int col = COPIES == 1 ? nt * 16 + c : c % (16 / COPIES), gc = tile * COLS + min(col, cols - 1), i = by_g(p, gc);
       limit[nt] = col < cols ? min(rq.len, rq.want - rq.m + i + 1) : some;
       const T* src = reinterpret_cast<const T*>(p.q + (int64_t)(rq.row + i) * p.q_stride) +
-                     (int64_t)(kvh * g + gc % g) * D + q * (D / 4);
+                     (int64_t)(kvh * g + gc - i * g) * D + q * (D / 4);
 #pragma unroll
       for (int s = 0; s < W; ++s)
 #pragma unroll
@@ -332,15 +441,15 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
     const int last = stop * TILES;
     int window = bi, tab = entries(bi);
     int put = 0, get = 0;   // bytes into the ring
-    uint32_t there = 0;     // bit n % 32: record n's block is in the arena
+    bool broken = false;    // a block is not in the arena
     auto issue = [&]() {
       if (bi - window >= 64) {
         window = bi;
         tab = entries(bi);
       }
       const int e = __builtin_amdgcn_readlane(tab, bi - window);
-      const bool in = e >= 0 && e < p.num_blocks;
-      there = (there & ~(1u << (next & 31))) | (uint32_t)in << (next & 31);
+      const bool in = (uint32_t)e < p.num_blocks;
+      broken |= !in;
       const char* rec = head + (in ? e : 0) * block_bytes + ti * REC;
       constexpr int FULL = 16 * D / 1024;
 #pragma unroll
@@ -354,6 +463,7 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
         ++bi;
       }
     };
+#pragma unroll 1
     for (int i = 0; i < RING && next < last; ++i) issue();
 
     bf16x8 qf[NT][QP][W];
@@ -399,58 +509,68 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
       else if (RING - TILES > TILES && behind >= RING - 2 * TILES) KVR_WAIT_VMCNT((RING - 2 * TILES) * LOADS);
       else KVR_WAIT_VMCNT(0);
       asm volatile("" ::: "memory");  // the reads below stay below
-      const uint32_t bits = there >> (kt * TILES & 31);
-      const int in = bits & ((1 << TILES) - 1);  // TILES divides 32: the unit's bits are neighbours
-      const char* rec[TILES];
-#pragma unroll
-      for (int x = 0; x < TILES; ++x) {
-        rec[x] = ring + get;
-        get = get == (RING - 1) * REC ? 0 : get + REC;
-      }
-      const bool whole = (int64_t)(kt + 1) * UNIT <= all && in == (1 << TILES) - 1;
+      // record x of the unit: TILES divides the ring into whole units
+      auto at = [&](int x) { return ring + get + x * REC; };
+      const bool whole = (int64_t)(kt + 1) * UNIT <= all && !broken;
       // scores
-      float sc[NT][NV];
+      uint32_t kw[TILES][W], ks[TILES];
 #pragma unroll
       for (int x = 0; x < TILES; ++x) {
-        f32x4 st[NT];
+        load_words<D / 8>(at(x) + k_off, kw[x]);
+        ks[x] = (uint8_t)at(x)[ks_off];
+      }
+      f32x4 st[NT][TILES];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) st[nt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        uint32_t kw[W];
-        load_words<D / 8>(rec[x] + k_off, kw);
-        const float scale = scale_of((uint8_t)rec[x][ks_off], 0);
+      for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int s = 0; s < W; ++s) {
+        for (int x = 0; x < TILES; ++x) st[nt][x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int s = 0; s < W; ++s)
+#pragma unroll
+        for (int x = 0; x < TILES; ++x) {
+          const float scale = scale_of(ks[x], 0);
           union { uint32_t w[4]; bf16x8 f; } kf;
-          kf.w[0] = pair_of<0>(kw[s], scale);
-          kf.w[1] = pair_of<1>(kw[s], scale);
-          kf.w[2] = pair_of<2>(kw[s], scale);
-          kf.w[3] = pair_of<3>(kw[s], scale);
+          kf.w[0] = pair_of<0>(kw[x][s], scale);
+          kf.w[1] = pair_of<1>(kw[x][s], scale);
+          kf.w[2] = pair_of<2>(kw[x][s], scale);
+          kf.w[3] = pair_of<3>(kw[x][s], scale);
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int part = 0; part < QP; ++part)
-              st[nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf.f, qf[nt][part][s], st[nt], 0, 0, 0);
+              st[nt][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf.f, qf[nt][part][s], st[nt][x], 0, 0, 0);
         }
+      float sc[NT][NV];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int x = 0; x < TILES; ++x)
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            if (COPIES == 1) sc[nt][4 * x + j] = st[nt][j];
-            else sc[nt][j] = x == 0 || copy == x ? st[nt][j] : sc[nt][j];
+            if (COPIES == 1) sc[nt][4 * x + j] = st[nt][x][j];
+            else sc[nt][j] = x == 0 || copy == x ? st[nt][x][j] : sc[nt][j];
           }
-      }
       // the lane's first position of the unit's first tile, and of its column's tile
       const int p0 = kt * UNIT + 4 * q, c0 = p0 + (COPIES == 1 ? 0 : 16 * copy);
       uint32_t vw[TILES][W], vs[TILES];
 #pragma unroll
       for (int x = 0; x < TILES; ++x) {
-        load_words<D / 8>(rec[x] + v_off, vw[x]);
-        vs[x] = *reinterpret_cast<const uint32_t*>(rec[x] + vs_off);
+        load_words<D / 8>(at(x) + v_off, vw[x]);
+        vs[x] = *reinterpret_cast<const uint32_t*>(at(x) + vs_off);
       }
       bool nan_v = false;
       if (!whole) {
         // positions past a column's limit and in blocks that are not there leave its
         // softmax; V there may hold any bits, and 0 times them is not 0
+        int in = (1 << TILES) - 1;  // the unit's tiles whose blocks are in the arena
+        if (broken) {
+          in = 0;
+#pragma unroll 1
+          for (int x = 0; x < TILES; ++x) {
+            const int b = (kt * TILES + x) / tpb;
+            in |= (int)(b < p.max_blocks && (uint32_t)table[b] < p.num_blocks) << x;
+          }
+        }
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
           const bool gone = !(in >> (COPIES == 1 ? i / 4 : copy) & 1);
@@ -458,14 +578,17 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
           for (int nt = 0; nt < NT; ++nt)
             if (gone || c0 + 16 * (i / 4) + i % 4 >= limit[nt]) sc[nt][i] = -INFINITY;
         }
+        uint32_t nan = 0;
 #pragma unroll
-        for (int x = 0; x < TILES; ++x)
+        for (int x = 0; x < TILES; ++x) {
+          const int n = in >> x & 1 ? some - (p0 + 16 * x) : 0;  // of the lane's four positions
+          constexpr int KB = D / 32;                             // bytes of one
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int pos = p0 + 16 * x + j;
-            if (pos >= some || !(in >> x & 1)) clear_v<D>(vw[x], vs[x], j);
-            nan_v |= (vs[x] >> (8 * j) & 0xff) == PK_NAN && pos >= all;
-          }
+          for (int i = 0; i < W; ++i) vw[x][i] &= first_bytes(min(n, 4) * KB - 4 * i);
+          vs[x] &= first_bytes(n);
+          nan |= nan_bytes(vs[x]) & ~first_bytes(all - (p0 + 16 * x));  // seen by some columns only
+        }
+        nan_v = nan != 0;
       }
       // weights
       uint32_t pw[NT][PP][NV / 2];
@@ -475,8 +598,7 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
 #pragma unroll
         for (int i = 0; i < NV; ++i) mx = fmaxf(mx, sc[nt][i]);
         mx *= scale_log2;
-        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        mx = max_over_q(mx);
         if (__any(mx > m_run[nt] + SLACK)) {
           const float m_new = fmaxf(m_run[nt], mx);
           const float alpha = m_new == m_run[nt] ? 1.0f : __builtin_amdgcn_exp2f(m_run[nt] - m_new);
@@ -524,8 +646,8 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
           uint32_t ind[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const uint32_t word = vs[2 * y + i / 2] >> (16 * (i % 2));  // scales of two positions
-            ind[i] = ((word & 0xff) == PK_NAN ? 0x3f80u : 0u) | ((word >> 8 & 0xff) == PK_NAN ? 0x3f800000u : 0u);
+            const uint32_t two = nan_bytes(vs[2 * y + i / 2]) >> (16 * (i % 2));  // of two positions
+            ind[i] = (two & 1) * 0x3f80u | (two >> 8 & 1) * 0x3f800000u;
           }
           const bf16x8 nf = __builtin_bit_cast(bf16x8, make_uint4(ind[0], ind[1], ind[2], ind[3]));
 #pragma unroll
@@ -539,17 +661,25 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
             const f32x4 hits =
                 __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(seen, y), nf, f32x4{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-              if (hits[j] > 0.0f)
+            for (int j = 0; j < 4; ++j) {
+              const float add = hits[j] > 0.0f ? __builtin_nanf("") : 0.0f;
 #pragma unroll
-                for (int d = 0; d < DT; ++d) o[nt][d][j] = __builtin_nanf("");
+              for (int d = 0; d < DT; ++d) o[nt][d][j] += add;
+            }
           }
         }
 #pragma unroll
-        for (int x = 0; x < TILES; ++x)
+        for (int x = 0; x < TILES; ++x) {
+          const uint32_t gone = nan_bytes(vs[x]) * 255u;
+          vs[x] &= ~gone;
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if ((vs[x] >> (8 * j) & 0xff) == PK_NAN) clear_v<D>(vw[x], vs[x], j);
+          for (int i = 0; i < W; ++i) {
+            uint32_t bytes = 0;  // of word i, those of positions that are gone
+#pragma unroll
+            for (int y = 0; y < 4; ++y) bytes |= (gone >> (8 * ((4 * i + y) / (D / 32))) & 255u) << (8 * y);
+            vw[x][i] &= ~bytes;
+          }
+        }
       }
       // O += P V
 #pragma unroll
@@ -583,64 +713,51 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
       }
       KVR_WAIT_LGKM0();  // the unit's records are in registers: the ring takes the next ones
       asm volatile("" ::: "memory");
-#pragma unroll
-      for (int x = 0; x < TILES; ++x)
-        if (next < last) issue();
+      get = get == (RING - TILES) * REC ? 0 : get + TILES * REC;
+#pragma unroll 1
+      for (int x = 0; x < TILES && next < last; ++x) issue();
     }
 
     // ---- the columns' outputs, or what there is of them ----
-    const bool done = first == 0 && upto == rq.steps;
-    float* part = slots + (first > 0 ? 0 : 1) * p.part_cols * (D + 2);
+    // 16 rows at a time through the ring, a row's dims over the lanes; the copies of a
+    // column are merged on the way.  What stays open goes to the workspace, or at the
+    // stretch's end, where the ring has no more to take, stays where it is.
+    const bool done = first == 0 && upto == rq.steps, stay = LOCAL && u + upto - first >= u1;
+    float* const rows = reinterpret_cast<float*>(ring);
+    float* const part = stay ? rows : slots + (first > 0 ? 0 : 1) * p.part_cols * (D + 2);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
+      float* const tr = rows + (LOCAL ? nt : 0) * 16 * (D + 2);
       float l = l_run[nt] + __shfl_xor(l_run[nt], 16, 64);
       l += __shfl_xor(l, 32, 64);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        // row 4q + j: column (4q + j) % (16 / COPIES) of copy (4q + j) / (16 / COPIES)
-        float lj = __shfl(l, 4 * q + j, 64), mj = __shfl(m_run[nt], 4 * q + j, 64);
-        float x[DT];
-#pragma unroll
-        for (int d = 0; d < DT; ++d) x[d] = o[nt][d][j];
-#pragma unroll
-        for (int step = 32; step > 32 / COPIES && COPIES > 1; step >>= 1) {  // the copies of a column
-          const float mo = __shfl_xor(mj, step, 64), m = fmaxf(mj, mo), mb = m == -INFINITY ? 0.0f : m;
-          const float f = __builtin_amdgcn_exp2f(mj - mb), fo = __builtin_amdgcn_exp2f(mo - mb);
-          lj = lj * f + __shfl_xor(lj, step, 64) * fo;
-#pragma unroll
-          for (int d = 0; d < DT; ++d) x[d] = x[d] * f + __shfl_xor(x[d], step, 64) * fo;
-          mj = m;
-        }
-        const int col = COPIES == 4 ? j : COPIES == 2 ? 4 * (q & 1) + j : nt * 16 + 4 * q + j;
-        if (col >= cols) continue;
-        if (COPIES == 4 ? q != j : COPIES == 2 ? q >= 2 : false) continue;  // one copy's lanes write
-        if (done) {
-          T* dst = out_of<T, D, COLS>(p, rq, tile, col, kvh) + c * DT;
-#pragma unroll
-          for (int d = 0; d < DT; ++d) Elem<T>::store(dst, d, lj == 0.0f ? 0.0f : x[d] / lj);
-        } else {
-          float* dst = part + col * (D + 2);
-#pragma unroll
-          for (int d = 0; d < DT; ++d) dst[c * DT + d] = x[d];
-          if (c == 0) {
-            dst[D] = mj;
-            dst[D + 1] = lj;
-          }
-        }
+      if (q == 0) {
+        tr[c * (D + 2) + D] = m_run[nt];
+        tr[c * (D + 2) + D + 1] = l;
       }
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int d = 0; d < DT; ++d) tr[(4 * q + j) * (D + 2) + c * DT + d] = o[nt][d][j];
+      asm volatile("" ::: "memory");
+#pragma unroll 1
+      for (int i = 0; i < min(16 / COPIES, cols - nt * 16); ++i) {
+        if (COPIES == 1 && stay && !done) break;  // the rows are the partials
+        const Column<D> v = merge_column<D, COPIES>([&](int k) { return tr + (k * (16 / COPIES) + i) * (D + 2); }, lane);
+        if (done) put_out<T, D, COLS>(p, rq.row, tile, nt * 16 + i, kvh, lane, v);
+        else put_part<D>(part + (nt * 16 + i) * (D + 2), lane, v);
+      }
+      KVR_WAIT_LGKM0();  // the rows have been read: the ring may be filled again
+      asm volatile("" ::: "memory");
     }
     if (!done && lane == 0) {
       Stretch& me = s_str[wave];
       const int which = first > 0 ? 0 : 1;
-      me.request[which] = r;
+      me.cols[which] = cols;
+      me.row[which] = rq.row;
       me.tile[which] = tile;
-      if (first > 0) {
-        me.head = 1;
-        me.head_closed = upto == rq.steps;
-      } else {
-        me.tail = 1;
-        me.end = base + (int64_t)(tile + 1) * rq.steps;
-      }
+      me.sums[which] = part;
+      if (first > 0) me.head_closed = upto == rq.steps;
+      else me.end = base + (int64_t)(tile + 1) * rq.steps;
     }
     u += upto - first;
     if (u < u1)
@@ -654,68 +771,54 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
   // ---- the workgroup's own merges: an item begun before it, and those its waves left
   // open, each over the waves that went on with it ----
   __syncthreads();
-  OpenItem open{0, total, -1, 0, 0};
+  OpenItem open{0, 0, 0, 0, 0};
+  const int64_t pitch = (int64_t)2 * p.part_cols * (D + 2);
+#pragma unroll 1
   for (int lead = -1; lead < PA_NT / 64; ++lead) {
     const int at = max(lead, 0), which = lead < 0 ? 0 : 1;
-    if (!(lead < 0 ? s_str[0].head : s_str[at].tail)) continue;
+    const int cols = s_str[at].cols[which];
+    if (cols == 0) continue;
     int n = 1;
     bool closed = lead < 0 && s_str[0].head_closed;
-    while (!closed && at + n < PA_NT / 64 && s_str[at + n].head) closed = s_str[at + n++].head_closed;
-    const int request = s_str[at].request[which], tile = s_str[at].tile[which];
-    if (lead >= 0 && !closed) open = OpenItem{s_str[at].end, total, request, tile, at};
-    if (n == 1) continue;
-    const Request x = get_request<COLS, UNIT>(p, request);
-    const int64_t pitch = (int64_t)2 * p.part_cols * (D + 2);
-    float* lead_slot = slots + (at - wave) * pitch + which * p.part_cols * (D + 2);
-    float* next = slots + (at + 1 - wave) * pitch;
-    for (int col = wave; col < min(COLS, x.m * g - tile * COLS); col += PA_NT / 64) {
-      constexpr int ND = (D + 63) / 64;
-      float acc[ND], m, l;
-      merge_column<T, D>([&](int i) { return (i == 0 ? lead_slot : next + (i - 1) * pitch) + col * (D + 2); }, n, lane,
-                         acc, m, l);
-      T* out = out_of<T, D, COLS>(p, x, tile, col, kvh);
-      float* dst = lead_slot + col * (D + 2);
-#pragma unroll
-      for (int d = 0; d < ND; ++d)
-        if (d * 64 + lane < D) {
-          if (lead >= 0 && closed) Elem<T>::store(out, d * 64 + lane, l == 0.0f ? 0.0f : acc[d] / l);
-          else dst[d * 64 + lane] = acc[d];
-        }
-      if (lane == 0 && !(lead >= 0 && closed)) {
-        dst[D] = m;
-        dst[D + 1] = l;
-      }
+    while (!closed && at + n < PA_NT / 64 && s_str[at + n].cols[0]) closed = s_str[at + n++].head_closed;
+    const int row = s_str[at].row[which], tile = s_str[at].tile[which];
+    closed &= lead >= 0;  // all of the item is here
+    if (lead >= 0 && !closed) {
+      const int wg = blockIdx.x / nkv;
+      int groups = 1;
+      while ((wg + groups) * (PA_NT / 64) < st.workers && st.begin((wg + groups) * (PA_NT / 64)) < s_str[at].end) ++groups;
+      open = OpenItem{cols, row, tile, at, groups};
+    }
+    float* slot = slots + (at - wave) * pitch + which * p.part_cols * (D + 2);
+    if (n == 1 && s_str[at].sums[which] == slot) continue;
+#pragma unroll 1
+    for (int col = wave; col < cols; col += PA_NT / 64) {
+      const Column<D> v = merge_column<D, PA_NT / 64>(
+          [&](int i) { return s_str[at + min(i, n - 1)].sums[i == 0 ? which : 0] + col * (D + 2); }, n, lane);
+      if (closed) put_out<T, D, COLS>(p, row, tile, col, kvh, lane, v);
+      else put_part<D>(slot + col * (D + 2), lane, v);
     }
   }
   if (kvh == 0 && t == 0) p.open[blockIdx.x / nkv] = open;
 }
 
 // Workgroup (kv head, workgroup of the first kernel): the item that it began and left
-// open, merged over the workgroups that went on with it, in their order.
+// open, merged over the workgroups that went on with it, in their order, a wave a
+// column.
 template <typename T, int D, typename S>
 __global__ __launch_bounds__(PA_NT) void packed_attn_merge_kernel(PackedAttnParams p) {
-  constexpr int COLS = S::COLS, ND = (D + 63) / 64, WG = PA_NT / 64;
-  const int nkv = p.packed.nkv, g = p.nq / nkv, wg = blockIdx.x / nkv, kvh = blockIdx.x % nkv;
+  constexpr int WG = PA_NT / 64;
+  const int nkv = p.packed.nkv, wg = blockIdx.x / nkv, kvh = blockIdx.x % nkv;
   const OpenItem it = p.open[wg];
-  if (it.request < 0) return;
-  const Request rq = get_request<COLS, S::UNIT>(p, it.request);
-  const int cols = min(COLS, rq.m * g - it.tile * COLS);
-  const int64_t workers = min((int64_t)p.workers, it.total);
-  int n = 1;  // with the workgroups after it whose stretches begin inside the item
-  while ((int64_t)(wg + n) * WG < workers && it.total * ((wg + n) * WG) / workers < it.end) ++n;
-  const int lane = threadIdx.x & 63;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t pitch = (int64_t)2 * p.part_cols * (D + 2);
   const float* first = p.part + ((int64_t)kvh * p.workers + wg * WG) * pitch;
   const float* lead = first + it.wave * pitch + p.part_cols * (D + 2);
-  for (int col = threadIdx.x >> 6; col < cols; col += WG) {
-    float acc[ND], m, l;
-    merge_column<T, D>([&](int i) { return (i == 0 ? lead : first + i * WG * pitch) + col * (D + 2); }, n, lane, acc, m,
-                       l);
-    T* out = out_of<T, D, COLS>(p, rq, it.tile, col, kvh);
-#pragma unroll
-    for (int d = 0; d < ND; ++d)
-      if (d * 64 + lane < D) Elem<T>::store(out, d * 64 + lane, l == 0.0f ? 0.0f : acc[d] / l);
-  }
+#pragma unroll 1
+  for (int col = wave; col < it.cols; col += WG)
+    put_out<T, D, S::COLS>(p, it.row, it.tile, col, kvh, lane,
+                           merge_column<D, 16>([&](int i) { return (i == 0 ? lead : first + i * WG * pitch) + col * (D + 2); },
+                                               it.groups, lane));
 }
 
 // The kernel for a call's columns per request: as few column tiles as take them, and
@@ -787,7 +890,7 @@ void run(const kv_packed* packed, int32_t layer, const void* q, int64_t q_stride
   const int64_t e = elem_bytes(d.dtype);
   PackedAttnParams p{};
   p.packed = packed_layer(packed, layer);
-  p.num_blocks = packed->num_blocks;
+  p.num_blocks = (uint32_t)std::min<int64_t>(packed->num_blocks, (int64_t)INT32_MAX + 1);
   p.q = static_cast<const char*>(q);
   p.out = static_cast<char*>(out);
   p.q_stride = q_stride * e;
@@ -799,6 +902,8 @@ void run(const kv_packed* packed, int32_t layer, const void* q, int64_t q_stride
   p.R = R;
   p.max_blocks = max_blocks;
   p.nq = d.num_q_heads;
+  p.g = d.num_q_heads / d.num_kv_heads;
+  p.g_inv = p.g == 1 ? 0 : (uint32_t)(((1ull << 32) + p.g - 1) / p.g);
   const AttnLayout L = attn_layout(d, R, rows, max_query, max_len);
   p.max_query = max_query;
   p.workers = L.workers;
@@ -840,8 +945,8 @@ kv_status kv_packed_attention(kv_packed_t packed, int32_t layer, const void* q, 
     return kvr_err::set(KV_EINVAL, "packed attention supports at most 16 q heads per kv head");
   if (layer < 0 || layer >= d.num_layers)
     return kvr_err::set(KV_EINVAL, "layer %d outside [0, %d)", layer, d.num_layers);
-  if (R < 0 || rows < 0 || rows > INT32_MAX || max_blocks < 0)
-    return kvr_err::set(KV_EINVAL, "num_requests, rows and max_blocks_per_req are 0 .. 2^31 - 1");
+  if (R < 0 || rows < 0 || rows > (1 << 24) || max_blocks < 0)
+    return kvr_err::set(KV_EINVAL, "num_requests and max_blocks_per_req are 0 .. 2^31 - 1, rows 0 .. 2^24");
   if (!q_offsets && rows != R) return kvr_err::set(KV_EINVAL, "without q_offsets rows must equal num_requests");
   if (R == 0 || rows == 0) return kvr_err::clear();
   if (max_query < 1 || max_len < 1) return kvr_err::set(KV_EINVAL, "max_query and max_len must be positive");
