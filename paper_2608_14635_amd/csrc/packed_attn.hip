@@ -2,7 +2,7 @@
 //
 // The query rows of a request that share a kv head are columns: column i g + h is
 // query i of q head h of the group.  An item is one request's next 16 NT columns of one
-// kv head; its work comes in units of 32 or 64 positions.  Every wave takes an equal
+// kv head; its work comes in units of 32 positions.  Every wave takes an equal
 // stretch of the units of all items, request after request, whatever the lengths (they
 // are known on the device alone), so that all waves end together.  Where a stretch
 // ends inside an item the wave leaves the item's sums so far; the four waves of a
@@ -13,10 +13,10 @@
 //   S^T = K Q^T on v_mfma_f32_16x16x32_bf16, 16 positions a tile: position c's dims
 //   q d/4 .. are the lane's K operand, d/8 bytes and one scale; the conversions to bf16
 //   are exact.  The lane gets the scores of positions 4q .. 4q+3 for column c.
-//   Where at most 16 / COPIES columns are in use (4 copies of 4, 2 of 8), every copy of
-//   them takes the scores of another tile, with a softmax of its own: all 16 columns
-//   work, and a lane has 4 scores of 64 positions instead of 16, of which a quarter
-//   counts.  The copies are merged at the end of the stretch.
+//   Where at most 8 columns are in use, the unit's two tiles are scored by a copy of
+//   them each, with a softmax of its own: all 16 columns work, and a lane has 4 scores
+//   of the unit instead of 8.  The copies are merged at the end of the stretch.  (Four
+//   copies of 4 columns over 64 positions took as long: the softmax is not the bound.)
 //   Online softmax per column, exp2 domain, rescaled only where the maximum rose by
 //   more than 2^SLACK.
 //   O = P V: the lane's weights of two tiles are the A operand as they are (0 where the
@@ -52,7 +52,7 @@ template <int NT_, int COPIES_>
 struct Shape {
   static constexpr int NT = NT_, COPIES = COPIES_;
   static constexpr int COLS = 16 * NT / COPIES;       // columns of an item
-  static constexpr int TILES = COPIES == 4 ? 4 : 2;   // tiles of a unit
+  static constexpr int TILES = 2;                     // tiles of a unit
   static constexpr int UNIT = 16 * TILES;             // positions of a unit
   static constexpr int OWN = COPIES == 1 ? TILES : 1; // tiles a column scores
 };
@@ -99,10 +99,10 @@ __device__ __forceinline__ void static_for(F&& f) {
 
 // Workgroups a CU holds by their registers, and the records of a wave's ring that
 // then fit its LDS.
-constexpr int occupancy_of(bool f32, int d, int nt, int copies) {
-  return nt == 4 || (f32 && d == 128 && nt == 2) ? 1 : nt == 2 || copies == 4 || (f32 && d == 128) ? 2 : 3;
+constexpr int occupancy_of(bool f32, int d, int nt) {
+  return nt == 4 || (f32 && d == 128 && nt == 2) ? 1 : nt == 2 || (f32 && d == 128) ? 2 : 3;
 }
-constexpr int ring_of(int occupancy) { return occupancy == 3 ? 6 : 8; }
+constexpr int ring_of(int occupancy) { return occupancy == 3 ? 4 : 8; }
 
 __device__ __forceinline__ int by_g(const PackedAttnParams& p, int n) {
   return p.g_inv ? (int)__umulhi((uint32_t)n, p.g_inv) : n;
@@ -133,6 +133,10 @@ struct Stretches {
     longer = total - size * workers;
   }
   __device__ __forceinline__ int64_t begin(int w) const { return w * size + min((int64_t)w, longer); }
+  __device__ __forceinline__ int holder(int64_t u) const {  // whose unit u is
+    const int64_t head = longer * (size + 1);
+    return (int)(u < head ? quotient(u, size + 1) : longer + quotient(u - head, size));
+  }
 };
 
 struct Request {
@@ -198,11 +202,11 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
 // What a wave's stretch holds of items that are not its own alone: of one begun before
 // it ([0]), of one it leaves open ([1]).
 struct Stretch {
-  int cols[2];                    // columns, 0: no such item
+  int cols[2];   // columns, 0: no such item
   int row[2], tile[2];
-  const float* sums[2];           // in the wave's ring or in the workspace
-  int head_closed;                // the item begun before ends in it
-  int64_t end;                    // the open item's units' end
+  int flags;     // 1: the item begun before ends in it; 2, 4: [0]'s, [1]'s sums are in the wave's ring
+  int pad;
+  int64_t end;   // the open item's units' end
 };
 
 // One column from n partials of D sums, a maximum and a sum of weights, in their order:
@@ -755,9 +759,8 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
       me.cols[which] = cols;
       me.row[which] = rq.row;
       me.tile[which] = tile;
-      me.sums[which] = part;
-      if (first > 0) me.head_closed = upto == rq.steps;
-      else me.end = base + (int64_t)(tile + 1) * rq.steps;
+      me.flags |= (stay ? 2 << which : 0) | (first > 0 && upto == rq.steps ? 1 : 0);
+      if (first == 0) me.end = base + (int64_t)(tile + 1) * rq.steps;
     }
     u += upto - first;
     if (u < u1)
@@ -771,42 +774,55 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
   // ---- the workgroup's own merges: an item begun before it, and those its waves left
   // open, each over the waves that went on with it ----
   __syncthreads();
+  constexpr int WAVES = PA_NT / 64;
+  const Stretch str = s_str[lane % WAVES];  // lane i: wave i's
+  const auto of_waves = [](bool v) { return (uint32_t)__ballot(v) & ((1u << WAVES) - 1); };
+  const uint32_t begun = of_waves(str.cols[0] != 0), left = of_waves(str.cols[1] != 0), ended = of_waves(str.flags & 1);
+  const uint32_t near[2] = {of_waves(str.flags & 2), of_waves(str.flags & 4)};  // sums in the rings
   OpenItem open{0, 0, 0, 0, 0};
   const int64_t pitch = (int64_t)2 * p.part_cols * (D + 2);
+  float* const slots0 = slots - wave * pitch;
 #pragma unroll 1
-  for (int lead = -1; lead < PA_NT / 64; ++lead) {
+  for (int lead = -1; lead < WAVES; ++lead) {
     const int at = max(lead, 0), which = lead < 0 ? 0 : 1;
-    const int cols = s_str[at].cols[which];
-    if (cols == 0) continue;
+    if (!((which ? left : begun) >> at & 1)) continue;
     int n = 1;
-    bool closed = lead < 0 && s_str[0].head_closed;
-    while (!closed && at + n < PA_NT / 64 && s_str[at + n].cols[0]) closed = s_str[at + n++].head_closed;
-    const int row = s_str[at].row[which], tile = s_str[at].tile[which];
+    bool closed = lead < 0 && (ended & 1);
+    while (!closed && at + n < WAVES && begun >> (at + n) & 1) closed = ended >> (at + n++) & 1;
+    const int cols = __builtin_amdgcn_readlane(str.cols[which], at), row = __builtin_amdgcn_readlane(str.row[which], at);
+    const int tile = __builtin_amdgcn_readlane(str.tile[which], at);
     closed &= lead >= 0;  // all of the item is here
-    if (lead >= 0 && !closed) {
-      const int wg = blockIdx.x / nkv;
-      int groups = 1;
-      while ((wg + groups) * (PA_NT / 64) < st.workers && st.begin((wg + groups) * (PA_NT / 64)) < s_str[at].end) ++groups;
-      open = OpenItem{cols, row, tile, at, groups};
-    }
-    float* slot = slots + (at - wave) * pitch + which * p.part_cols * (D + 2);
-    if (n == 1 && s_str[at].sums[which] == slot) continue;
+    float* slot = slots0 + at * pitch + which * p.part_cols * (D + 2);
+    if (lead >= 0 && !closed) open = OpenItem{cols, row, tile, at, 0};
+    if (n == 1 && !(near[which] >> at & 1)) continue;
 #pragma unroll 1
-    for (int col = wave; col < cols; col += PA_NT / 64) {
-      const Column<D> v = merge_column<D, PA_NT / 64>(
-          [&](int i) { return s_str[at + min(i, n - 1)].sums[i == 0 ? which : 0] + col * (D + 2); }, n, lane);
+    for (int col = wave; col < cols; col += WAVES) {
+      const Column<D> v = merge_column<D, WAVES>(
+          [&](int i) -> const float* {
+            const int j = at + i;
+            const float* far = i == 0 ? slot : slots0 + j * pitch;
+            const float* ring = reinterpret_cast<const float*>(&s_ring[0][0] + j * (RING * REC));
+            return ((i == 0 ? near[which] : near[0]) >> j & 1 ? ring : far) + col * (D + 2);
+          },
+          n, lane);
       if (closed) put_out<T, D, COLS>(p, row, tile, col, kvh, lane, v);
       else put_part<D>(slot + col * (D + 2), lane, v);
     }
   }
-  if (kvh == 0 && t == 0) p.open[blockIdx.x / nkv] = open;
+  if (kvh == 0 && t == 0) {
+    const int wg = blockIdx.x / nkv;
+    if (open.cols) open.groups = st.holder(s_str[open.wave].end - 1) / WAVES - wg + 1;
+    p.open[wg] = open;
+  }
 }
 
 // Workgroup (kv head, workgroup of the first kernel): the item that it began and left
 // open, merged over the workgroups that went on with it, in their order, a wave a
-// column.
+// column.  (Eight waves: four took 12 us where eight take 8, with 48 partials of 5
+// columns; sixteen cost calls of few more than they gave.)
+constexpr int PM_NT = 512;
 template <typename T, int D, typename S>
-__global__ __launch_bounds__(PA_NT) void packed_attn_merge_kernel(PackedAttnParams p) {
+__global__ __launch_bounds__(PM_NT) void packed_attn_merge_kernel(PackedAttnParams p) {
   constexpr int WG = PA_NT / 64;
   const int nkv = p.packed.nkv, wg = blockIdx.x / nkv, kvh = blockIdx.x % nkv;
   const OpenItem it = p.open[wg];
@@ -815,7 +831,7 @@ __global__ __launch_bounds__(PA_NT) void packed_attn_merge_kernel(PackedAttnPara
   const float* first = p.part + ((int64_t)kvh * p.workers + wg * WG) * pitch;
   const float* lead = first + it.wave * pitch + p.part_cols * (D + 2);
 #pragma unroll 1
-  for (int col = wave; col < it.cols; col += WG)
+  for (int col = wave; col < it.cols; col += PM_NT / 64)
     put_out<T, D, S::COLS>(p, it.row, it.tile, col, kvh, lane,
                            merge_column<D, 16>([&](int i) { return (i == 0 ? lead : first + i * WG * pitch) + col * (D + 2); },
                                                it.groups, lane));
@@ -828,10 +844,9 @@ struct Plan {
 };
 Plan plan_of(int dtype, int d, int g, int32_t max_query) {
   const int64_t cols = (int64_t)g * max_query;
-  const int copies = cols <= 4 ? 4 : cols <= 8 ? 2 : 1;
+  const int copies = cols <= 8 ? 2 : 1;
   const int nt = cols <= 16 ? 1 : cols <= 32 || dtype == KV_F32 ? 2 : 4;
-  return Plan{nt, copies, 16 * nt / copies, copies == 4 ? 64 : 32,
-              occupancy_of(dtype == KV_F32, d, nt, copies)};
+  return Plan{nt, copies, 16 * nt / copies, 32, occupancy_of(dtype == KV_F32, d, nt)};
 }
 
 // Stretches per kv head: as many waves as the chip holds at once, but no more than
@@ -845,14 +860,13 @@ int workers_of(const Plan& pl, int nkv, int R, int64_t rows, int g, int64_t max_
 
 template <typename T, int D, typename S>
 void launch_shape(const PackedAttnParams& p, hipStream_t s) {
-  constexpr int OCC = occupancy_of(std::is_same<T, float>::value, D, S::NT, S::COPIES);
+  constexpr int OCC = occupancy_of(std::is_same<T, float>::value, D, S::NT);
   const dim3 grid((unsigned)((int64_t)p.workers / (PA_NT / 64) * p.packed.nkv));
   hipLaunchKernelGGL((packed_attn_kernel<T, D, S, OCC>), grid, dim3(PA_NT), 0, s, p);
-  hipLaunchKernelGGL((packed_attn_merge_kernel<T, D, S>), grid, dim3(PA_NT), 0, s, p);
+  hipLaunchKernelGGL((packed_attn_merge_kernel<T, D, S>), grid, dim3(PM_NT), 0, s, p);
 }
 template <typename T, int D>
 void launch(const Plan& pl, const PackedAttnParams& p, hipStream_t s) {
-  if (pl.copies == 4) return launch_shape<T, D, Shape<1, 4>>(p, s);
   if (pl.copies == 2) return launch_shape<T, D, Shape<1, 2>>(p, s);
   if (pl.nt == 1) return launch_shape<T, D, Shape<1, 1>>(p, s);
   if (pl.nt == 2) return launch_shape<T, D, Shape<2, 1>>(p, s);
