@@ -1,21 +1,25 @@
 // Log probabilities of given tokens, entropy and likeliest tokens (kvr_logprob.h).
 //
-// With m the largest logit of a row, e_v = exp(scale (z_v - m)), l = sum e_v and
-// s = sum (z_v - m) e_v:
-//   log p_t = scale (z_t - m) - log l,   entropy = log l - scale s / l
-// (both terms of the entropy are of one sign, so nothing cancels).  A row is cut into
-// chunks; a workgroup reads its chunk once, into registers, takes the chunk's m, l and
+// In log2 units, t_v = c (z_v - m') with c = scale log2 e and m' next to the row's
+// largest logit m (C = c m rounded, t_v = fma(c, z_v, -C): the rounding of C is the same
+// factor in every term and cancels), e_v = 2^t_v, l = sum e_v and s = sum t_v e_v:
+//   log p_t = ln 2 (t_t - log2 l),   entropy = ln 2 (log2 l - s / l)
+// (both terms of the entropy are of one sign, so nothing cancels).  Where C would
+// overflow (masks of the dtype's lowest value alone in a row), t_v = (z_v - m) c.  A row is cut into
+// chunks; a workgroup reads its chunk once, into registers, takes the chunk's C, l and
 // s from there and, where asked, its top_n entries; a second kernel merges the
 // chunks of each row in a fixed order.
 //
 // Top entries.  (value, lower index first) is one 64-bit key, so that all keys of a
-// row differ and the order is total.  The top_n-th largest of the 256 threads' own
-// largest keys is a bound that at least top_n entries reach, and only entries of
-// top_n threads can: those are collected in LDS (a few more than top_n as a rule, at
-// most top_n * ITEMS) and ranked by counting.
+// row differ and the order is total.  A bound that at least top_n entries reach comes
+// from the threads' own largest values: one wave finds, bit by bit from the top, a
+// value that at least top_n and not many more threads reach; entries that reach
+// it lie in those threads alone, so they fit the list in LDS, where they are ranked
+// by counting.  (Ranking the threads' values by counting took 1.7 us a chunk.)  Where
+// equal values make too many threads, the bound is the top_n-th of the threads' keys.
 //
 // Bound by HBM where rows are many (4 or 2 bytes a logit against one exp and some
-// eight other operations), by latency where they are few.
+// six other operations), by latency where they are few.
 #include <algorithm>
 
 #include "common.h"
@@ -28,13 +32,14 @@ namespace {
 constexpr int LP_NT = 256;
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr int LP_MAX_VOCAB = 1 << 22;
-constexpr int LP_KEYS = 4096;  // collected keys: top_n * ITEMS, and top_n * chunks * top_n / 256, at most
+constexpr int LP_KEYS = 4096;  // collected keys: of at most KEYS / ITEMS threads' ITEMS entries
+constexpr float LN2 = 0.6931471805599453f;
 
 struct LogprobParams {
   const char* logits;
   int64_t stride;  // bytes
   int vocab, chunks, top;
-  float scale;
+  float scale, scale2;  // scale log2 e
   const int32_t* tokens;
   float* logprobs;
   float* entropy;
@@ -47,20 +52,27 @@ struct LogprobParams {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef u32x4 u32x4_a2 __attribute__((aligned(2)));
 
-// 16 bytes of logits as values, from any boundary of their elements
-__device__ __forceinline__ void get_vec(const float* p, float* v) {
-  const f32x4 a = *reinterpret_cast<const f32x4_a4*>(p);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = a[i];
-}
-__device__ __forceinline__ void get_vec(const bf16_t* p, float* v) {
-  const u32x4 u = *reinterpret_cast<const u32x4_a2*>(p);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    v[2 * i] = __uint_as_float(u[i] << 16);
-    v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+// 16 bytes of logits, on any boundary of their elements, and their values.
+template <typename T> struct Piece;
+template <> struct Piece<float> {
+  static constexpr int N = 4;
+  f32x4 w;
+  __device__ __forceinline__ void load(const float* p) { w = *reinterpret_cast<const f32x4_a4*>(p); }
+  __device__ __forceinline__ void set(int j, float v) { w[j] = v; }
+  __device__ __forceinline__ float value(int j) const { return w[j]; }
+};
+template <> struct Piece<bf16_t> {
+  static constexpr int N = 8;
+  u32x4 w;
+  __device__ __forceinline__ void load(const bf16_t* p) { w = *reinterpret_cast<const u32x4_a2*>(p); }
+  __device__ __forceinline__ void set(int j, float v) {  // of a bf16 number
+    const uint32_t b = __float_as_uint(v) >> 16;
+    w[j / 2] = j % 2 ? (w[j / 2] & 0xffffu) | b << 16 : (w[j / 2] & 0xffff0000u) | b;
   }
-}
+  __device__ __forceinline__ float value(int j) const {
+    return __uint_as_float(j % 2 ? w[j / 2] & 0xffff0000u : w[j / 2] << 16);
+  }
+};
 
 // Unsigned numbers that order as the values do; -0 as +0, NaN below all.
 __device__ __forceinline__ uint32_t order_bits(float z) {
@@ -84,183 +96,259 @@ __device__ __forceinline__ float wave_max(float v) {
 // Ranks by counting: how many of the n keys in LDS are larger.
 __device__ __forceinline__ int rank_of(uint64_t key, const uint64_t* keys, int n) {
   int r = 0;
+#pragma unroll 4
   for (int i = 0; i < n; ++i) r += keys[i] > key;
   return r;
 }
 
 struct TopScratch {
   uint64_t keys[LP_KEYS];
-  uint64_t own[LP_NT];
-  uint64_t bound;
+  uint32_t own[LP_NT];
+  uint32_t bound;  // of the order bits; 0xffffffff: too many equal values
   int count;
 };
 
-// The bound: the top-th largest of the threads' own largest keys.
-__device__ __forceinline__ uint64_t top_bound(uint64_t own, int top, TopScratch& s) {
-  const int t = threadIdx.x;
-  s.own[t] = own;
-  if (t == 0) s.count = 0;
-  __syncthreads();
-  if (rank_of(own, s.own, LP_NT) == top - 1) s.bound = own;
-  __syncthreads();
-  return s.bound;
+// Wave 0: a value that at least `top` and at most `most` of the threads' largest reach.
+__device__ __forceinline__ void find_bound(int top, int most, TopScratch& s) {
+  const int lane = threadIdx.x & 63;
+  uint32_t u[LP_NT / 64];
+#pragma unroll
+  for (int i = 0; i < LP_NT / 64; ++i) u[i] = s.own[i * 64 + lane];
+  auto reach = [&](uint32_t v) {
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < LP_NT / 64; ++i) n += __builtin_popcountll(__ballot(u[i] >= v));
+    return n;
+  };
+  uint32_t bound = 0;
+  int n = LP_NT;
+#pragma unroll 1
+  for (int b = 31; b >= 0 && n > most; --b) {
+    const uint32_t v = bound | 1u << b;
+    const int k = reach(v);
+    if (k >= top) {
+      bound = v;
+      n = k;
+    }
+  }
+  if (lane == 0) {
+    s.bound = n > most ? 0xffffffffu : bound;
+    s.count = 0;
+  }
 }
 __device__ __forceinline__ void collect(uint64_t key, TopScratch& s) {
   const int at = atomicAdd(&s.count, 1);  // any order: the ranks settle it
   if (at < LP_KEYS) s.keys[at] = key;
 }
+// The same with whole keys, all different: the top-th largest of the threads' own,
+// ranked by counting in the list's place.
+__device__ __forceinline__ uint64_t bound_of_keys(uint64_t own, int top, TopScratch& s) {
+  const int t = threadIdx.x;
+  s.keys[t] = own;
+  __syncthreads();
+  if (rank_of(own, s.keys, LP_NT) == top - 1) s.keys[LP_NT] = own;
+  __syncthreads();
+  const uint64_t bound = s.keys[LP_NT];
+  __syncthreads();
+  return bound;
+}
 
-template <typename T, int ITEMS>
+// C of a maximum: rounded, not contracted into what it enters.
+__device__ __forceinline__ float c_of(float m, float scale2) {
+#pragma clang fp contract(off)
+  return m == -INFINITY ? 0.0f : m * scale2;
+}
+// Whether a maximum m's C stands for it: no overflow in C, or in t of a value near it
+// (-infinity: C = 0, every t is -infinity).
+__device__ __forceinline__ bool plain(float m) { return fabsf(m) < 1e36f || m == -INFINITY; }
+
+// Sum over the workgroup, in every thread; red holds a value a wave.
+__device__ __forceinline__ float block_total(float v, float* red) {
+  v = wave_sum(v);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = 0.0f;
+#pragma unroll
+  for (int i = 0; i < LP_NT / 64; ++i) v += red[i];
+  return v;
+}
+__device__ __forceinline__ float block_most(float v, float* red) {
+  v = wave_max(v);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < LP_NT / 64; ++i) v = fmaxf(v, red[i]);
+  return v;
+}
+
+template <typename T, int ITEMS, bool TOP>
 __global__ __launch_bounds__(LP_NT) void logprob_chunk_kernel(LogprobParams p) {
-  constexpr int VEC = 16 / (int)sizeof(T), VECS = ITEMS / VEC;
+  constexpr int VEC = Piece<T>::N, VECS = ITEMS / VEC, STEP = LP_NT * VEC;
   __shared__ float s_red[3][LP_NT / 64];
-  __shared__ TopScratch s_top;
-  const int t = threadIdx.x, w = t >> 6, lane = t & 63;
+  const int t = threadIdx.x;
   const int c = blockIdx.x % p.chunks;
   const int64_t row = blockIdx.x / p.chunks;
   const T* z = reinterpret_cast<const T*>(p.logits + row * p.stride);
-  const int first = c * (LP_NT * ITEMS) + t * VEC;
-  float v[ITEMS];
+  const int begin = c * (LP_NT * ITEMS), first = begin + t * VEC;
+  Piece<T> v[VECS];
+  if (begin + LP_NT * ITEMS <= p.vocab) {
+#pragma unroll
+    for (int i = 0; i < VECS; ++i) v[i].load(z + (begin + i * STEP) + (uint32_t)(t * VEC));
+  } else {
+    // the row's end: a piece that crosses it is loaded from further left, what others
+    // hold of it masked
+#pragma unroll
+    for (int i = 0; i < VECS; ++i) {
+      const int at = first + i * STEP, from = min(at, p.vocab - VEC);
+      if (p.vocab >= VEC) {
+        v[i].load(z + from);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) v[i].set(j, from + j >= at ? v[i].value(j) : -INFINITY);
+      } else {
+        v[i] = Piece<T>{};
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) v[i].set(j, i == 0 && at + j < p.vocab ? Elem<T>::load(z, at + j) : -INFINITY);
+      }
+    }
+  }
+  float most[VECS], own = -INFINITY;
 #pragma unroll
   for (int i = 0; i < VECS; ++i) {
-    const int at = first + i * (LP_NT * VEC);
-    if (at + VEC <= p.vocab) {
-      get_vec(z + at, v + i * VEC);
-    } else {
+    most[i] = v[i].value(0);
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) v[i * VEC + j] = at + j < p.vocab ? Elem<T>::load(z, at + j) : -INFINITY;
-    }
+    for (int j = 1; j < VEC; ++j) most[i] = fmaxf(most[i], v[i].value(j));
+    own = fmaxf(own, most[i]);
   }
-  float m = -INFINITY;
-#pragma unroll
-  for (int i = 0; i < ITEMS; ++i) m = fmaxf(m, v[i]);
-  m = wave_max(m);
-  if (lane == 0) s_red[0][w] = m;
-  __syncthreads();
-  m = s_red[0][0];
-#pragma unroll
-  for (int i = 1; i < LP_NT / 64; ++i) m = fmaxf(m, s_red[0][i]);
   // nothing but -infinity (or NaN): sums of zeros (or NaN)
-  const float base = m == -INFINITY ? 0.0f : m, scale2 = p.scale * LOG2E;
+  const float m = block_most(own, s_red[0]);
   float l = 0.0f, s = 0.0f;
-#pragma unroll
-  for (int i = 0; i < ITEMS; ++i) {
-    const float x = v[i] - base, e = __builtin_amdgcn_exp2f(x * scale2);
+  auto add = [&](float x) {
+    const float e = __builtin_amdgcn_exp2f(x);
     l += e;
-    s += e == 0.0f ? 0.0f : x * e;
-  }
-  l = wave_sum(l);
-  s = wave_sum(s);
-  if (lane == 0) {
-    s_red[1][w] = l;
-    s_red[2][w] = s;
-  }
-  __syncthreads();
-  if (t == 0) {
-    l = s = 0.0f;
-    for (int i = 0; i < LP_NT / 64; ++i) {
-      l += s_red[1][i];
-      s += s_red[2][i];
-    }
-    p.stats[row * p.chunks + c] = make_float4(m, l, s, 0.0f);
-  }
-  if (p.top == 0) return;
-  // entries past the vocabulary order as NaN of higher indices: below all others
-  uint64_t own = 0;
+    s = fmaf(fmaxf(x, -1e30f), e, s);  // -infinity times 0; a NaN is in l
+  };
+  if (plain(m)) {
+    const float base = c_of(m, p.scale2);
 #pragma unroll
-  for (int i = 0; i < ITEMS; ++i) {
-    const int at = first + i / VEC * (LP_NT * VEC) + i % VEC;
-    const uint64_t k = make_key(at < p.vocab ? order_bits(v[i]) : 0u, at);
-    own = k > own ? k : own;
-  }
-  const uint64_t bound = top_bound(own, p.top, s_top);
-  if (own >= bound) {
+    for (int i = 0; i < VECS; ++i)
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i) {
-      const int at = first + i / VEC * (LP_NT * VEC) + i % VEC;
-      const uint64_t k = make_key(at < p.vocab ? order_bits(v[i]) : 0u, at);
-      if (k >= bound) collect(k, s_top);
-    }
+      for (int j = 0; j < VEC; ++j) add(fmaf(v[i].value(j), p.scale2, -base));
+  } else {
+#pragma unroll
+    for (int i = 0; i < VECS; ++i)
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) add((v[i].value(j) - m) * p.scale2);
   }
-  __syncthreads();
-  const int n = min(s_top.count, LP_KEYS);
-  uint64_t* out = p.keys + (row * p.chunks + c) * p.top;
-  for (int i = t; i < n; i += LP_NT) {
-    const int r = rank_of(s_top.keys[i], s_top.keys, n);
-    if (r < p.top) out[r] = s_top.keys[i];
+  l = block_total(l, s_red[1]);
+  s = block_total(s, s_red[2]);
+  if (t == 0) p.stats[row * p.chunks + c] = make_float4(m, l, s, 0.0f);
+  if constexpr (TOP) {
+    __shared__ TopScratch s_top;
+    s_top.own[t] = order_bits(own);
+    __syncthreads();
+    if (t < 64) find_bound(p.top, min(LP_KEYS / ITEMS, 2 * p.top + 8), s_top);
+    __syncthreads();
+    uint64_t bound = (uint64_t)s_top.bound << 32;
+    const auto key_at = [&](int at) {  // past the vocabulary: as NaN of higher indices, below all others
+      return make_key(at < p.vocab ? order_bits(Elem<T>::load(z, at)) : 0u, at);
+    };
+    if (s_top.bound == 0xffffffffu) {
+      uint64_t key = 0;
+#pragma unroll 1
+      for (int i = 0; i < ITEMS; ++i) key = max(key, key_at(first + i / VEC * STEP + i % VEC));
+      bound = bound_of_keys(key, p.top, s_top);
+    }
+    // pieces with an entry that may reach the bound are looked at again, one by one
+    uint32_t hit = 0;
+#pragma unroll
+    for (int i = 0; i < VECS; ++i) hit |= (order_bits(most[i]) >= (uint32_t)(bound >> 32) ? 1u : 0u) << i;
+#pragma unroll 1
+    while (hit) {
+      const int at = first + (__ffs(hit) - 1) * STEP;
+      hit &= hit - 1;
+#pragma unroll 1
+      for (int j = 0; j < VEC; ++j) {
+        const uint64_t k = key_at(at + j);
+        if (k >= bound) collect(k, s_top);
+      }
+    }
+    __syncthreads();
+    const int n = min(s_top.count, LP_KEYS);
+    uint64_t* out = p.keys + (row * p.chunks + c) * p.top;
+    for (int i = t; i < n; i += LP_NT) {
+      const int r = rank_of(s_top.keys[i], s_top.keys, n);
+      if (r < p.top) out[r] = s_top.keys[i];
+    }
   }
 }
 
-template <typename T>
+template <typename T, bool TOP>
 __global__ __launch_bounds__(LP_NT) void logprob_row_kernel(LogprobParams p) {
   __shared__ float s_red[3][LP_NT / 64];
-  __shared__ TopScratch s_top;
-  const int t = threadIdx.x, w = t >> 6, lane = t & 63;
+  const int t = threadIdx.x;
   const int64_t row = blockIdx.x;
   const float4* stats = p.stats + row * p.chunks;
+  int tok = -1;
+  float z = 0.0f;
+  if (t == 0 && p.logprobs) {
+    tok = p.tokens[row];
+    if (tok >= 0 && tok < p.vocab) z = Elem<T>::load(reinterpret_cast<const T*>(p.logits + row * p.stride), tok);
+  }
   float m = -INFINITY;
   for (int c = t; c < p.chunks; c += LP_NT) m = fmaxf(m, stats[c].x);
-  m = wave_max(m);
-  if (lane == 0) s_red[0][w] = m;
-  __syncthreads();
-  m = s_red[0][0];
-#pragma unroll
-  for (int i = 1; i < LP_NT / 64; ++i) m = fmaxf(m, s_red[0][i]);
-  const float scale2 = p.scale * LOG2E;
+  m = block_most(m, s_red[0]);
+  const bool by_c = plain(m);
+  const float base = by_c ? c_of(m, p.scale2) : 0.0f;
   float l = 0.0f, s = 0.0f;
   for (int c = t; c < p.chunks; c += LP_NT) {
-    // a chunk of -infinity alone adds l = s = 0 (or its NaN)
     const float4 q = stats[c];
-    const float x = q.x == -INFINITY ? 0.0f : q.x - m, e = __builtin_amdgcn_exp2f(x * scale2);
+    const float x = fmaxf(by_c ? (plain(q.x) ? c_of(q.x, p.scale2) - base : -INFINITY) : (q.x - m) * p.scale2, -1e30f);
+    const float e = __builtin_amdgcn_exp2f(x);
     l = fmaf(q.y, e, l);
-    s += e == 0.0f ? 0.0f * q.z : e * fmaf(x, q.y, q.z);
+    s += e * fmaf(x, q.y, q.z);
   }
-  l = wave_sum(l);
-  s = wave_sum(s);
-  if (lane == 0) {
-    s_red[1][w] = l;
-    s_red[2][w] = s;
-  }
-  __syncthreads();
-  l = s = 0.0f;
-#pragma unroll
-  for (int i = 0; i < LP_NT / 64; ++i) {
-    l += s_red[1][i];
-    s += s_red[2][i];
-  }
+  l = block_total(l, s_red[1]);
+  s = block_total(s, s_red[2]);
   const bool none = l == 0.0f;  // every logit -infinity
-  const float log_l = none ? 0.0f : logf(l);
-  auto logprob = [&](float z) { return none ? -INFINITY : (z - m) * p.scale - log_l; };
+  const float log_l = none ? 0.0f : log2f(l);
+  auto logprob = [&](float v) {
+    if (none) return -INFINITY;
+    if (!by_c) return (v - m) * p.scale - LN2 * log_l;
+    const float x = fmaf(v, p.scale2, -base);
+    return x == -INFINITY && l == l ? v * p.scale : LN2 * (x - log_l);  // a finite v far below all others
+  };
   if (t == 0) {
-    if (p.logprobs) {
-      const int tok = p.tokens[row];
-      float lp = tok < 0 ? 0.0f : l != l ? l : -INFINITY;
-      if (tok >= 0 && tok < p.vocab)
-        lp = logprob(Elem<T>::load(reinterpret_cast<const T*>(p.logits + row * p.stride), tok));
-      p.logprobs[row] = lp;
-    }
+    if (p.logprobs) p.logprobs[row] = tok < 0 ? 0.0f : tok < p.vocab ? logprob(z) : l != l ? l : -INFINITY;
     if (p.entropy) {
-      const float h = log_l - p.scale * s / l;
+      const float h = LN2 * (log_l - s / l);
       p.entropy[row] = none || h < 0.0f ? 0.0f : h;  // NaN stays
     }
   }
-  if (p.top == 0) return;
-  const uint64_t* keys = p.keys + row * p.chunks * p.top;
-  const int total = p.chunks * p.top;
-  uint64_t own = t;  // threads without a key: below all of them, and different
-  for (int i = t; i < total; i += LP_NT) own = max(own, keys[i]);
-  const uint64_t bound = top_bound(own, p.top, s_top);
-  if (own >= bound)
-    for (int i = t; i < total; i += LP_NT)
-      if (keys[i] >= bound) collect(keys[i], s_top);
-  __syncthreads();
-  const int n = min(s_top.count, LP_KEYS);
-  for (int i = t; i < n; i += LP_NT) {
-    const uint64_t k = s_top.keys[i];
-    const int r = rank_of(k, s_top.keys, n);
-    if (r < p.top) {
-      p.top_tokens[row * p.top + r] = (int32_t)key_index(k);
-      p.top_logprobs[row * p.top + r] = logprob(ordered_value((uint32_t)(k >> 32)));
+  if constexpr (TOP) {
+    __shared__ TopScratch s_top;
+    const uint64_t* keys = p.keys + row * p.chunks * p.top;
+    const int total = p.chunks * p.top;
+    uint64_t own = t;  // threads without a key: below all of them, and different
+    for (int i = t; i < total; i += LP_NT) own = max(own, keys[i]);
+    s_top.own[t] = (uint32_t)(own >> 32);
+    __syncthreads();
+    const int per = (total + LP_NT - 1) / LP_NT;  // keys of a thread: at most 64 (kv_logprobs_workspace_bytes)
+    if (t < 64) find_bound(p.top, min(LP_KEYS / per, 2 * p.top + 8), s_top);
+    __syncthreads();
+    uint64_t bound = (uint64_t)s_top.bound << 32;
+    if (s_top.bound == 0xffffffffu) bound = bound_of_keys(own, p.top, s_top);
+    if (own >= bound)
+      for (int i = t; i < total; i += LP_NT)
+        if (keys[i] >= bound) collect(keys[i], s_top);
+    __syncthreads();
+    const int n = min(s_top.count, LP_KEYS);
+    for (int i = t; i < n; i += LP_NT) {
+      const uint64_t k = s_top.keys[i];
+      const int r = rank_of(k, s_top.keys, n);
+      if (r < p.top) {
+        p.top_tokens[row * p.top + r] = (int32_t)key_index(k);
+        p.top_logprobs[row * p.top + r] = logprob(ordered_value((uint32_t)(k >> 32)));
+      }
     }
   }
 }
@@ -273,14 +361,14 @@ int items_of(int64_t rows, int vocab) {
 }
 int chunks_of(int items, int vocab) { return (vocab + LP_NT * items - 1) / (LP_NT * items); }
 
-template <typename T>
+template <typename T, bool TOP>
 void launch(const LogprobParams& p, int64_t rows, int items, hipStream_t s) {
   const dim3 grid((unsigned)(rows * p.chunks));
   if (items == 64)
-    hipLaunchKernelGGL((logprob_chunk_kernel<T, 64>), grid, dim3(LP_NT), 0, s, p);
+    hipLaunchKernelGGL((logprob_chunk_kernel<T, 64, TOP>), grid, dim3(LP_NT), 0, s, p);
   else
-    hipLaunchKernelGGL((logprob_chunk_kernel<T, 16>), grid, dim3(LP_NT), 0, s, p);
-  hipLaunchKernelGGL(logprob_row_kernel<T>, dim3((unsigned)rows), dim3(LP_NT), 0, s, p);
+    hipLaunchKernelGGL((logprob_chunk_kernel<T, 16, TOP>), grid, dim3(LP_NT), 0, s, p);
+  hipLaunchKernelGGL((logprob_row_kernel<T, TOP>), dim3((unsigned)rows), dim3(LP_NT), 0, s, p);
 }
 
 }  // namespace
@@ -333,6 +421,7 @@ kv_status kv_logprobs(const void* logits, int32_t dtype, int64_t rows, int32_t v
   p.chunks = chunks;
   p.top = top_n;
   p.scale = scale;
+  p.scale2 = scale * LOG2E;
   p.tokens = tokens;
   p.logprobs = logprobs;
   p.entropy = entropy;
@@ -341,8 +430,8 @@ kv_status kv_logprobs(const void* logits, int32_t dtype, int64_t rows, int32_t v
   p.stats = static_cast<float4*>(workspace);
   p.keys = reinterpret_cast<uint64_t*>(p.stats + rows * chunks);
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  if (dtype == KV_BF16) launch<bf16_t>(p, rows, items, s);
-  else launch<float>(p, rows, items, s);
+  if (dtype == KV_BF16) top_n ? launch<bf16_t, true>(p, rows, items, s) : launch<bf16_t, false>(p, rows, items, s);
+  else top_n ? launch<float, true>(p, rows, items, s) : launch<float, false>(p, rows, items, s);
   return launched();
 }
 
