@@ -31,8 +31,12 @@ namespace {
 
 constexpr int LP_NT = 256;
 constexpr float LOG2E = 1.4426950408889634f;
-constexpr int LP_MAX_VOCAB = 1 << 22;
-constexpr int LP_KEYS = 4096;  // collected keys: of at most KEYS / ITEMS threads' ITEMS entries
+// Entries of a thread.  A workgroup's piece in flight is 32 KB of fp32: 1024 rows of
+// 151936 in bf16 took 70 us with 64 entries, 64 with 16 and 55 with 32; one row takes
+// as long with 16 as with 32.
+constexpr int LP_ITEMS = 32;
+constexpr int LP_CHUNK = LP_NT * LP_ITEMS;
+constexpr int LP_MAX_VOCAB = 256 * LP_CHUNK;
 constexpr float LN2 = 0.6931471805599453f;
 
 struct LogprobParams {
@@ -101,15 +105,21 @@ __device__ __forceinline__ int rank_of(uint64_t key, const uint64_t* keys, int n
   return r;
 }
 
+// PER: entries of a thread at most.  At most 64 threads' are collected where the bound
+// comes from their values, and top_n <= 64 threads' where it is one of their keys.
+template <int PER>
 struct TopScratch {
-  uint64_t keys[LP_KEYS];
+  static constexpr int KEYS = 64 * PER;
+  uint64_t keys[KEYS];
   uint32_t own[LP_NT];
   uint32_t bound;  // of the order bits; 0xffffffff: too many equal values
   int count;
 };
 
 // Wave 0: a value that at least `top` and at most `most` of the threads' largest reach.
-__device__ __forceinline__ void find_bound(int top, int most, TopScratch& s) {
+template <typename S>
+__device__ __forceinline__ void find_bound(int top, S& s) {
+  const int most = min(64, 2 * top + 8);
   const int lane = threadIdx.x & 63;
   uint32_t u[LP_NT / 64];
 #pragma unroll
@@ -136,13 +146,16 @@ __device__ __forceinline__ void find_bound(int top, int most, TopScratch& s) {
     s.count = 0;
   }
 }
-__device__ __forceinline__ void collect(uint64_t key, TopScratch& s) {
+template <typename S>
+__device__ __forceinline__ void collect(uint64_t key, S& s) {
   const int at = atomicAdd(&s.count, 1);  // any order: the ranks settle it
-  if (at < LP_KEYS) s.keys[at] = key;
+  if (at < S::KEYS) s.keys[at] = key;
 }
 // The same with whole keys, all different: the top-th largest of the threads' own,
 // ranked by counting in the list's place.
-__device__ __forceinline__ uint64_t bound_of_keys(uint64_t own, int top, TopScratch& s) {
+template <typename S>
+__device__ __forceinline__ uint64_t bound_of_keys(uint64_t own, int top, S& s) {
+  static_assert(S::KEYS > LP_NT, "the threads' keys fit the list");
   const int t = threadIdx.x;
   s.keys[t] = own;
   __syncthreads();
@@ -162,14 +175,18 @@ __device__ __forceinline__ float c_of(float m, float scale2) {
 // (-infinity: C = 0, every t is -infinity).
 __device__ __forceinline__ bool plain(float m) { return fabsf(m) < 1e36f || m == -INFINITY; }
 
-// Sum over the workgroup, in every thread; red holds a value a wave.
-__device__ __forceinline__ float block_total(float v, float* red) {
-  v = wave_sum(v);
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+// Sums and maximum over the workgroup, in every thread; red holds a value a wave.
+__device__ __forceinline__ float2 block_total(float a, float b, float2* red) {
+  a = wave_sum(a);
+  b = wave_sum(b);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = make_float2(a, b);
   __syncthreads();
-  v = 0.0f;
+  float2 v = red[0];
 #pragma unroll
-  for (int i = 0; i < LP_NT / 64; ++i) v += red[i];
+  for (int i = 1; i < LP_NT / 64; ++i) {
+    v.x += red[i].x;
+    v.y += red[i].y;
+  }
   return v;
 }
 __device__ __forceinline__ float block_most(float v, float* red) {
@@ -181,17 +198,18 @@ __device__ __forceinline__ float block_most(float v, float* red) {
   return v;
 }
 
-template <typename T, int ITEMS, bool TOP>
+template <typename T, bool TOP>
 __global__ __launch_bounds__(LP_NT) void logprob_chunk_kernel(LogprobParams p) {
-  constexpr int VEC = Piece<T>::N, VECS = ITEMS / VEC, STEP = LP_NT * VEC;
-  __shared__ float s_red[3][LP_NT / 64];
+  constexpr int VEC = Piece<T>::N, VECS = LP_ITEMS / VEC, STEP = LP_NT * VEC;
+  __shared__ float s_most[LP_NT / 64];
+  __shared__ float2 s_sums[LP_NT / 64];
   const int t = threadIdx.x;
   const int c = blockIdx.x % p.chunks;
   const int64_t row = blockIdx.x / p.chunks;
   const T* z = reinterpret_cast<const T*>(p.logits + row * p.stride);
-  const int begin = c * (LP_NT * ITEMS), first = begin + t * VEC;
+  const int begin = c * LP_CHUNK, first = begin + t * VEC;
   Piece<T> v[VECS];
-  if (begin + LP_NT * ITEMS <= p.vocab) {
+  if (begin + LP_CHUNK <= p.vocab) {
 #pragma unroll
     for (int i = 0; i < VECS; ++i) v[i].load(z + (begin + i * STEP) + (uint32_t)(t * VEC));
   } else {
@@ -220,7 +238,7 @@ __global__ __launch_bounds__(LP_NT) void logprob_chunk_kernel(LogprobParams p) {
     own = fmaxf(own, most[i]);
   }
   // nothing but -infinity (or NaN): sums of zeros (or NaN)
-  const float m = block_most(own, s_red[0]);
+  const float m = block_most(own, s_most);
   float l = 0.0f, s = 0.0f;
   auto add = [&](float x) {
     const float e = __builtin_amdgcn_exp2f(x);
@@ -239,14 +257,13 @@ __global__ __launch_bounds__(LP_NT) void logprob_chunk_kernel(LogprobParams p) {
 #pragma unroll
       for (int j = 0; j < VEC; ++j) add((v[i].value(j) - m) * p.scale2);
   }
-  l = block_total(l, s_red[1]);
-  s = block_total(s, s_red[2]);
-  if (t == 0) p.stats[row * p.chunks + c] = make_float4(m, l, s, 0.0f);
+  const float2 sums = block_total(l, s, s_sums);
+  if (t == 0) p.stats[row * p.chunks + c] = make_float4(m, sums.x, sums.y, 0.0f);
   if constexpr (TOP) {
-    __shared__ TopScratch s_top;
+    __shared__ TopScratch<LP_ITEMS> s_top;
     s_top.own[t] = order_bits(own);
     __syncthreads();
-    if (t < 64) find_bound(p.top, min(LP_KEYS / ITEMS, 2 * p.top + 8), s_top);
+    if (t < 64) find_bound(p.top, s_top);
     __syncthreads();
     uint64_t bound = (uint64_t)s_top.bound << 32;
     const auto key_at = [&](int at) {  // past the vocabulary: as NaN of higher indices, below all others
@@ -255,10 +272,10 @@ __global__ __launch_bounds__(LP_NT) void logprob_chunk_kernel(LogprobParams p) {
     if (s_top.bound == 0xffffffffu) {
       uint64_t key = 0;
 #pragma unroll 1
-      for (int i = 0; i < ITEMS; ++i) key = max(key, key_at(first + i / VEC * STEP + i % VEC));
+      for (int i = 0; i < LP_ITEMS; ++i) key = max(key, key_at(first + i / VEC * STEP + i % VEC));
       bound = bound_of_keys(key, p.top, s_top);
     }
-    // pieces with an entry that may reach the bound are looked at again, one by one
+    // pieces with an entry that may reach the bound are read again
     uint32_t hit = 0;
 #pragma unroll
     for (int i = 0; i < VECS; ++i) hit |= (order_bits(most[i]) >= (uint32_t)(bound >> 32) ? 1u : 0u) << i;
@@ -266,14 +283,24 @@ __global__ __launch_bounds__(LP_NT) void logprob_chunk_kernel(LogprobParams p) {
     while (hit) {
       const int at = first + (__ffs(hit) - 1) * STEP;
       hit &= hit - 1;
+      if (at + VEC <= p.vocab) {
+        Piece<T> w;
+        w.load(z + at);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+          const uint64_t k = make_key(order_bits(w.value(j)), at + j);
+          if (k >= bound) collect(k, s_top);
+        }
+      } else {
 #pragma unroll 1
-      for (int j = 0; j < VEC; ++j) {
-        const uint64_t k = key_at(at + j);
-        if (k >= bound) collect(k, s_top);
+        for (int j = 0; j < VEC; ++j) {
+          const uint64_t k = key_at(at + j);
+          if (k >= bound) collect(k, s_top);
+        }
       }
     }
     __syncthreads();
-    const int n = min(s_top.count, LP_KEYS);
+    const int n = min(s_top.count, s_top.KEYS);
     uint64_t* out = p.keys + (row * p.chunks + c) * p.top;
     for (int i = t; i < n; i += LP_NT) {
       const int r = rank_of(s_top.keys[i], s_top.keys, n);
@@ -284,31 +311,36 @@ __global__ __launch_bounds__(LP_NT) void logprob_chunk_kernel(LogprobParams p) {
 
 template <typename T, bool TOP>
 __global__ __launch_bounds__(LP_NT) void logprob_row_kernel(LogprobParams p) {
-  __shared__ float s_red[3][LP_NT / 64];
-  const int t = threadIdx.x;
+  const int t = threadIdx.x, lane = t & 63;
   const int64_t row = blockIdx.x;
   const float4* stats = p.stats + row * p.chunks;
+  const uint64_t* keys = p.keys + row * p.chunks * p.top;
+  const int total = p.chunks * p.top;
+  uint64_t own = t;  // threads without a key: below all of them, and different
+  if (TOP)
+    for (int i = t; i < total; i += LP_NT) own = max(own, keys[i]);
   int tok = -1;
   float z = 0.0f;
   if (t == 0 && p.logprobs) {
     tok = p.tokens[row];
     if (tok >= 0 && tok < p.vocab) z = Elem<T>::load(reinterpret_cast<const T*>(p.logits + row * p.stride), tok);
   }
+  // every wave merges all chunks, in the same order
   float m = -INFINITY;
-  for (int c = t; c < p.chunks; c += LP_NT) m = fmaxf(m, stats[c].x);
-  m = block_most(m, s_red[0]);
+  for (int c = lane; c < p.chunks; c += 64) m = fmaxf(m, stats[c].x);
+  m = wave_max(m);
   const bool by_c = plain(m);
   const float base = by_c ? c_of(m, p.scale2) : 0.0f;
   float l = 0.0f, s = 0.0f;
-  for (int c = t; c < p.chunks; c += LP_NT) {
+  for (int c = lane; c < p.chunks; c += 64) {
     const float4 q = stats[c];
     const float x = fmaxf(by_c ? (plain(q.x) ? c_of(q.x, p.scale2) - base : -INFINITY) : (q.x - m) * p.scale2, -1e30f);
     const float e = __builtin_amdgcn_exp2f(x);
     l = fmaf(q.y, e, l);
     s += e * fmaf(x, q.y, q.z);
   }
-  l = block_total(l, s_red[1]);
-  s = block_total(s, s_red[2]);
+  l = wave_sum(l);
+  s = wave_sum(s);
   const bool none = l == 0.0f;  // every logit -infinity
   const float log_l = none ? 0.0f : log2f(l);
   auto logprob = [&](float v) {
@@ -325,15 +357,11 @@ __global__ __launch_bounds__(LP_NT) void logprob_row_kernel(LogprobParams p) {
     }
   }
   if constexpr (TOP) {
-    __shared__ TopScratch s_top;
-    const uint64_t* keys = p.keys + row * p.chunks * p.top;
-    const int total = p.chunks * p.top;
-    uint64_t own = t;  // threads without a key: below all of them, and different
-    for (int i = t; i < total; i += LP_NT) own = max(own, keys[i]);
+    // a thread holds ceil(256 * 64 / 256) keys at most
+    __shared__ TopScratch<64> s_top;
     s_top.own[t] = (uint32_t)(own >> 32);
     __syncthreads();
-    const int per = (total + LP_NT - 1) / LP_NT;  // keys of a thread: at most 64 (kv_logprobs_workspace_bytes)
-    if (t < 64) find_bound(p.top, min(LP_KEYS / per, 2 * p.top + 8), s_top);
+    if (t < 64) find_bound(p.top, s_top);
     __syncthreads();
     uint64_t bound = (uint64_t)s_top.bound << 32;
     if (s_top.bound == 0xffffffffu) bound = bound_of_keys(own, p.top, s_top);
@@ -341,7 +369,7 @@ __global__ __launch_bounds__(LP_NT) void logprob_row_kernel(LogprobParams p) {
       for (int i = t; i < total; i += LP_NT)
         if (keys[i] >= bound) collect(keys[i], s_top);
     __syncthreads();
-    const int n = min(s_top.count, LP_KEYS);
+    const int n = min(s_top.count, s_top.KEYS);
     for (int i = t; i < n; i += LP_NT) {
       const uint64_t k = s_top.keys[i];
       const int r = rank_of(k, s_top.keys, n);
@@ -353,21 +381,11 @@ __global__ __launch_bounds__(LP_NT) void logprob_row_kernel(LogprobParams p) {
   }
 }
 
-// Entries a thread takes: 64 where rows are many (a workgroup's 64 KB of fp32 in
-// flight), 16 where they would leave CUs idle.
-int items_of(int64_t rows, int vocab) {
-  const int64_t wide = (vocab + LP_NT * 64 - 1) / (LP_NT * 64);
-  return rows * wide >= 512 || vocab > LP_NT * 16 * 256 ? 64 : 16;
-}
-int chunks_of(int items, int vocab) { return (vocab + LP_NT * items - 1) / (LP_NT * items); }
+int chunks_of(int vocab) { return (vocab + LP_CHUNK - 1) / LP_CHUNK; }
 
 template <typename T, bool TOP>
-void launch(const LogprobParams& p, int64_t rows, int items, hipStream_t s) {
-  const dim3 grid((unsigned)(rows * p.chunks));
-  if (items == 64)
-    hipLaunchKernelGGL((logprob_chunk_kernel<T, 64, TOP>), grid, dim3(LP_NT), 0, s, p);
-  else
-    hipLaunchKernelGGL((logprob_chunk_kernel<T, 16, TOP>), grid, dim3(LP_NT), 0, s, p);
+void launch(const LogprobParams& p, int64_t rows, hipStream_t s) {
+  hipLaunchKernelGGL((logprob_chunk_kernel<T, TOP>), dim3((unsigned)(rows * p.chunks)), dim3(LP_NT), 0, s, p);
   hipLaunchKernelGGL((logprob_row_kernel<T, TOP>), dim3((unsigned)rows), dim3(LP_NT), 0, s, p);
 }
 
@@ -382,7 +400,7 @@ uint64_t kv_logprobs_workspace_bytes(int64_t rows, int32_t vocab, int32_t top_n)
   if (rows <= 0 || rows > (1 << 20) || vocab <= 0 || vocab > LP_MAX_VOCAB || top_n < 0 ||
       top_n > KV_LOGPROBS_MAX_TOP || top_n > vocab)
     return 0;
-  const int64_t chunks = chunks_of(items_of(rows, vocab), vocab);
+  const int64_t chunks = chunks_of(vocab);
   return (uint64_t)(rows * chunks * (16 + 8 * (int64_t)top_n));
 }
 
@@ -391,7 +409,7 @@ kv_status kv_logprobs(const void* logits, int32_t dtype, int64_t rows, int32_t v
                       int32_t* top_tokens, void* workspace, uint64_t ws_bytes, int32_t device, void* stream) {
   if (dtype != KV_F32 && dtype != KV_BF16) return kvr_err::set(KV_EINVAL, "unknown dtype %d", dtype);
   if (rows < 0 || rows > (1 << 20)) return kvr_err::set(KV_EINVAL, "rows must be 0 .. 2^20");
-  if (vocab < 1 || vocab > LP_MAX_VOCAB) return kvr_err::set(KV_EINVAL, "vocab must be 1 .. 2^22");
+  if (vocab < 1 || vocab > LP_MAX_VOCAB) return kvr_err::set(KV_EINVAL, "vocab must be 1 .. 2^21");
   if (stride < vocab) return kvr_err::set(KV_EINVAL, "the stride is below the vocabulary");
   if (!(scale > 0.0f) || !(scale < INFINITY)) return kvr_err::set(KV_EINVAL, "scale must be positive and finite");
   if (top_n < 0 || top_n > KV_LOGPROBS_MAX_TOP || top_n > vocab)
@@ -413,7 +431,7 @@ kv_status kv_logprobs(const void* logits, int32_t dtype, int64_t rows, int32_t v
   DeviceGuard dg(device);
   const kv_status st = device_ready(dg, device);
   if (st != KV_OK) return st;
-  const int items = items_of(rows, vocab), chunks = chunks_of(items, vocab);
+  const int chunks = chunks_of(vocab);
   LogprobParams p{};
   p.logits = static_cast<const char*>(logits);
   p.stride = stride * elem_bytes(dtype);
@@ -430,8 +448,8 @@ kv_status kv_logprobs(const void* logits, int32_t dtype, int64_t rows, int32_t v
   p.stats = static_cast<float4*>(workspace);
   p.keys = reinterpret_cast<uint64_t*>(p.stats + rows * chunks);
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  if (dtype == KV_BF16) top_n ? launch<bf16_t, true>(p, rows, items, s) : launch<bf16_t, false>(p, rows, items, s);
-  else top_n ? launch<float, true>(p, rows, items, s) : launch<float, false>(p, rows, items, s);
+  if (dtype == KV_BF16) top_n ? launch<bf16_t, true>(p, rows, s) : launch<bf16_t, false>(p, rows, s);
+  else top_n ? launch<float, true>(p, rows, s) : launch<float, false>(p, rows, s);
   return launched();
 }
 

@@ -109,8 +109,8 @@ def random_rows(R, V, dtype, seed, std=3.0):
 
 
 DT = {"f32": torch.float32, "bf16": torch.bfloat16}
-# one entry, fewer than a workgroup's threads, both sides of a chunk of 4096 and of 16384
-VOCABS = [1, 5, 63, 255, 1000, 4095, 4096, 4097, 16384, 16385, 40001]
+# one entry, fewer than a workgroup's threads, both sides of whole chunks of 8192
+VOCABS = [1, 5, 63, 255, 1000, 4097, 8191, 8192, 8193, 16385, 40001]
 
 
 @pytest.mark.gpu
@@ -238,14 +238,14 @@ def test_calls_on_two_streams_at_once():
 def test_workspace_bytes():
     assert kvr.kv_logprobs_workspace_bytes(16, 128256, 0) > 0
     assert kvr.kv_logprobs_workspace_bytes(16, 128256, 20) > kvr.kv_logprobs_workspace_bytes(16, 128256, 0)
-    for bad in ((0, 100, 0), (-1, 100, 0), (1 << 21, 100, 0), (1, 0, 0), (1, (1 << 22) + 1, 0), (1, 100, -1),
+    for bad in ((0, 100, 0), (-1, 100, 0), (1 << 21, 100, 0), (1, 0, 0), (1, (1 << 21) + 1, 0), (1, 100, -1),
                 (1, 100, 65), (1, 10, 11)):
         assert kvr.kv_logprobs_workspace_bytes(*bad) == 0
 
 
 @pytest.mark.parametrize("bad,status", [
     (dict(dtype=2), kvr.KV_EINVAL), (dict(rows=-1), kvr.KV_EINVAL), (dict(rows=(1 << 20) + 1), kvr.KV_EINVAL),
-    (dict(vocab=0), kvr.KV_EINVAL), (dict(vocab=(1 << 22) + 1, stride=1 << 23), kvr.KV_EINVAL),
+    (dict(vocab=0), kvr.KV_EINVAL), (dict(vocab=(1 << 21) + 1, stride=1 << 22), kvr.KV_EINVAL),
     (dict(stride=999), kvr.KV_EINVAL), (dict(scale=0.0), kvr.KV_EINVAL), (dict(scale=-1.0), kvr.KV_EINVAL),
     (dict(scale=float("inf")), kvr.KV_EINVAL), (dict(scale=float("nan")), kvr.KV_EINVAL),
     (dict(top_n=-1), kvr.KV_EINVAL), (dict(top_n=65), kvr.KV_EINVAL), (dict(vocab=3, top_n=4), kvr.KV_EINVAL),
