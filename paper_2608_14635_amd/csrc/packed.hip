@@ -6,10 +6,11 @@
 // lanes make a group and agree on its scale with two exchanges.  gfx950 converts
 // two values at a time with the scale's exponent applied, to the nearest code, ties
 // to even (v_cvt_scalef32_pk_fp4_f32 and its inverse), which is the definition.
-// A wave takes 16 consecutive rows of one kv head, K and V, so that rows in
-// consecutive slots fill whole records; the four waves of a workgroup take
-// neighbouring heads, so that together they read whole rows.  Bound by HBM: 2 bytes
-// in and 17/32 out a value in bf16.
+// A wave takes 4 consecutive rows of one kv head (8 or 16 of smaller heads) at a time,
+// K and V; rows in consecutive slots fill whole lines of a record.  The four waves of a
+// workgroup take neighbouring heads, so that together they read whole rows.  Bound by
+// HBM: 2 bytes in and 17/32 out a value in bf16 (65K tokens of 4 layers: 1.27 GB each
+// way at 4.2 TB/s in and 5.3 out; a plain copy reaches 4.8).
 #include <algorithm>
 #include <memory>
 #include <mutex>
@@ -28,23 +29,33 @@ namespace {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef u32x4 u32x4_a4 __attribute__((aligned(4)));  // 16 bytes on any 4-byte boundary
 
-// Eight values of a row as fp32, and back.
-__device__ __forceinline__ void get8(const char* p, float* v, bf16_t) {
-  const u32x4 u = *reinterpret_cast<const u32x4_a4*>(p);
+// Eight values of a row as they lie in memory, as fp32, and back from codes.
+template <typename T> struct Raw8;
+template <> struct Raw8<bf16_t> {
+  u32x4 u;
+  __device__ __forceinline__ void load(const char* p) { u = *reinterpret_cast<const u32x4_a4*>(p); }
+  __device__ __forceinline__ void values(float* v) const {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    v[2 * i] = __uint_as_float(u[i] << 16);
-    v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = __uint_as_float(u[i] << 16);
+      v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+    }
   }
-}
-__device__ __forceinline__ void get8(const char* p, float* v, float) {
-  const f32x4 a = reinterpret_cast<const f32x4_a4*>(p)[0], b = reinterpret_cast<const f32x4_a4*>(p)[1];
+};
+template <> struct Raw8<float> {
+  f32x4 a, b;
+  __device__ __forceinline__ void load(const char* p) {
+    a = reinterpret_cast<const f32x4_a4*>(p)[0];
+    b = reinterpret_cast<const f32x4_a4*>(p)[1];
+  }
+  __device__ __forceinline__ void values(float* v) const {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    v[i] = a[i];
-    v[4 + i] = b[i];
+    for (int i = 0; i < 4; ++i) {
+      v[i] = a[i];
+      v[4 + i] = b[i];
+    }
   }
-}
+};
 __device__ __forceinline__ void put8(char* p, uint32_t codes, float scale, bf16_t) {
   u32x4 u;
   u[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0));
@@ -120,13 +131,15 @@ __device__ __forceinline__ uint32_t v_get(const char* rec, int c, int u) {
   return word;
 }
 
-template <typename T, int D, bool TO_PACKED>
+// N: times that a wave takes as many rows as fit it; all loads are on their way before
+// the first is used.
+template <typename T, int D, bool TO_PACKED, int N>
 __global__ __launch_bounds__(256) void packed_move_kernel(PackedMoveParams p) {
-  constexpr int LANES = D / 8;          // lanes of a row
-  constexpr int STEP = 64 / LANES;      // rows of a wave at a time
+  constexpr int LANES = D / 8;                        // lanes of a row
+  constexpr int STEP = 64 / LANES;                    // rows of a wave at a time
   const int lane = threadIdx.x & 63, u = lane % LANES;
   const int nkv = p.packed.nkv;
-  const int64_t chunks = (p.rows + 15) / 16, items = chunks * nkv * p.layers;
+  const int64_t chunks = (p.rows + N * STEP - 1) / (N * STEP), items = chunks * nkv * p.layers;
   for (int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); item < items;
        item += (int64_t)gridDim.x * 4) {
     const int h = (int)(item % nkv);
@@ -134,49 +147,90 @@ __global__ __launch_bounds__(256) void packed_move_kernel(PackedMoveParams p) {
     const int l = (int)(item / nkv / chunks);
     PackedLayer pl = p.packed;
     pl.base += l * p.packed_layer;
-    const int64_t first = c * 16 + lane / LANES;
+    const int64_t first = c * (N * STEP) + lane / LANES;
+    // a row that does not count is one that does not exist: slot -1.  The four lanes of
+    // a group share a row, so they agree.
+    int64_t slot[N], from[N];
 #pragma unroll
-    for (int i = 0; i < 16 / STEP; ++i) {
+    for (int i = 0; i < N; ++i) {
       const int64_t row = first + i * STEP;
-      // the four lanes of a group share a row, so the exchanges below see all of it
-      if (row >= p.rows) continue;
-      const int64_t slot = p.packed_slots[row], from = p.plain_slots ? p.plain_slots[row] : row;
-      if (slot < 0 || slot >= pl.slots || from < 0 || from >= p.plain_rows) continue;
-      char* rec = packed_record(pl, slot, h, D);
-      const int s = (int)(slot % PK_TILE);
+      slot[i] = row < p.rows ? p.packed_slots[row] : -1;
+      from[i] = row < p.rows && p.plain_slots ? p.plain_slots[row] : row;
+    }
+    char *rec[N], *k[N], *v[N];
+    int s[N];
+    bool in[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      in[i] = slot[i] >= 0 && slot[i] < pl.slots && from[i] >= 0 && from[i] < p.plain_rows;
+      rec[i] = packed_record(pl, in[i] ? slot[i] : 0, h, D);
+      s[i] = (int)(slot[i] & (PK_TILE - 1));
       const int64_t in_row = ((int64_t)h * D + 8 * u) * sizeof(T);
-      char* k = p.k + l * p.plain_layer + from * p.k_stride + in_row;
-      char* v = p.v + l * p.plain_layer + from * p.v_stride + in_row;
-      if constexpr (TO_PACKED) {
-        float x[8], y[8];
-        get8(k, x, T{});
-        get8(v, y, T{});
-        uint32_t kb, vb;
-        const uint32_t kw = encode8(x, kb), vw = encode8(y, vb);
-        *reinterpret_cast<uint32_t*>(rec + k_word<D>(s, u)) = kw;
-        v_put<D>(rec, s, u, vw);
-        if (u % 4 == 0) {
-          rec[k_scale<D>(s, u / 4)] = (char)kb;
-          rec[v_scale<D>(s, u / 4)] = (char)vb;
+      k[i] = p.k + l * p.plain_layer + from[i] * p.k_stride + in_row;
+      v[i] = p.v + l * p.plain_layer + from[i] * p.v_stride + in_row;
+    }
+    if constexpr (TO_PACKED) {
+      Raw8<T> kr[N], vr[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (in[i]) {
+          kr[i].load(k[i]);
+          vr[i].load(v[i]);
         }
-      } else {
-        const uint32_t kw = *reinterpret_cast<const uint32_t*>(rec + k_word<D>(s, u)), vw = v_get<D>(rec, s, u);
-        const uint32_t kb = (uint8_t)rec[k_scale<D>(s, u / 4)], vb = (uint8_t)rec[v_scale<D>(s, u / 4)];
-        put8(k, kw, __uint_as_float(kb << 23), T{});
-        put8(v, vw, __uint_as_float(vb << 23), T{});
-      }
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (in[i]) {
+          float x[8], y[8];
+          kr[i].values(x);
+          vr[i].values(y);
+          uint32_t kb, vb;
+          const uint32_t kw = encode8(x, kb), vw = encode8(y, vb);
+          *reinterpret_cast<uint32_t*>(rec[i] + k_word<D>(s[i], u)) = kw;
+          v_put<D>(rec[i], s[i], u, vw);
+          if (u % 4 == 0) {
+            rec[i][k_scale<D>(s[i], u / 4)] = (char)kb;
+            rec[i][v_scale<D>(s[i], u / 4)] = (char)vb;
+          }
+        }
+    } else {
+      uint32_t kw[N], vw[N], kb[N], vb[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (in[i]) {
+          kw[i] = *reinterpret_cast<const uint32_t*>(rec[i] + k_word<D>(s[i], u));
+          vw[i] = v_get<D>(rec[i], s[i], u);
+          kb[i] = (uint8_t)rec[i][k_scale<D>(s[i], u / 4)];
+          vb[i] = (uint8_t)rec[i][v_scale<D>(s[i], u / 4)];
+        }
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (in[i]) {
+          put8(k[i], kw[i], __uint_as_float(kb[i] << 23), T{});
+          put8(v[i], vw[i], __uint_as_float(vb[i] << 23), T{});
+        }
     }
   }
 }
 
+// 65K tokens of 4 layers (8 kv heads of 128, bf16) took 325 + 270 us to pack and to load
+// with one time, 304 + 237 with two, 308 + 240 with four; 171 tokens of 28 layers (2 kv
+// heads) 4.1 + 3.9 with one, 4.3 + 4.0 with two, 5.5 + 4.6 with four: once where that
+// leaves the chip's 8192 waves unfilled.
 template <typename T, int D>
 void launch_move(bool to_packed, const PackedMoveParams& p, hipStream_t s) {
-  const int64_t items = (p.rows + 15) / 16 * p.packed.nkv * p.layers;
+  constexpr int STEP = 64 / (D / 8);
+  const int64_t once = (p.rows + STEP - 1) / STEP * p.packed.nkv * p.layers;
+  const bool twice = once > 2 * 8192;
+  const int64_t items = twice ? (p.rows + 2 * STEP - 1) / (2 * STEP) * p.packed.nkv * p.layers : once;
   const dim3 grid((unsigned)std::min<int64_t>((items + 3) / 4, 1 << 16));
-  if (to_packed)
-    hipLaunchKernelGGL((packed_move_kernel<T, D, true>), grid, dim3(256), 0, s, p);
+  if (to_packed && twice)
+    hipLaunchKernelGGL((packed_move_kernel<T, D, true, 2>), grid, dim3(256), 0, s, p);
+  else if (to_packed)
+    hipLaunchKernelGGL((packed_move_kernel<T, D, true, 1>), grid, dim3(256), 0, s, p);
+  else if (twice)
+    hipLaunchKernelGGL((packed_move_kernel<T, D, false, 2>), grid, dim3(256), 0, s, p);
   else
-    hipLaunchKernelGGL((packed_move_kernel<T, D, false>), grid, dim3(256), 0, s, p);
+    hipLaunchKernelGGL((packed_move_kernel<T, D, false, 1>), grid, dim3(256), 0, s, p);
 }
 
 }  // namespace

@@ -10,8 +10,11 @@
 //
 // One launch: every workgroup sums over all requests itself, 512 a step, and
 // works off its window of rows against each step's requests while they are in
-// LDS; no workgroup waits for another.  The writes of the rows (12 bytes each) bound
-// long calls, the launch and one scan step short ones.
+// LDS; no workgroup waits for another.  Short calls are the launch and one scan step (64
+// requests: 4.4 us); of long ones the rows' writes are half (333 requests, 2.7 million
+// positions: 33 MB in 14.9 us), the rest each workgroup's way through scan, search and
+// free list.  (A workgroup that worked off two or four windows for each scan took 19 and
+// 28 us.)
 #include <algorithm>
 
 #include "host.h"
@@ -27,7 +30,7 @@ constexpr int TG_WIN = TG_NT * TG_PER;
 struct GrowParams {
   const int32_t* held;
   const int32_t* lens;
-  int R, B;
+  int R, B, shift;  // shift: log2 B, or -1
   const int32_t* free_blocks;
   int num_free;
   int32_t* tables;
@@ -42,26 +45,30 @@ struct GrowParams {
 // Two sums in one word: rows in the low half, blocks in the high one.  Both stay
 // below 2^32 for calls as documented; whatever they hold, every index made from
 // them is checked before its use.
-__device__ __forceinline__ uint64_t wave_scan(uint64_t v, int lane) {
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const uint64_t u = __shfl_up(v, o, 64);
-    if (lane >= o) v += u;
-  }
+__device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
+  // within rows of 16 lanes, then their last lanes' sums into the rows behind
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);   // row_shr:1
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);   // row_shr:2
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);   // row_shr:4
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);   // row_shr:8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // row_bcast:15 into rows 1 and 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);  // row_bcast:31 into rows 2 and 3
   return v;
 }
 
 __global__ __launch_bounds__(TG_NT) void tables_grow_kernel(GrowParams p) {
   __shared__ uint32_t s_row[TG_NT], s_at[TG_NT];
-  __shared__ int s_held[TG_NT], s_n[TG_NT];
+  __shared__ int s_held[TG_NT], s_have[TG_NT], s_n[TG_NT];
   __shared__ uint64_t s_wave[TG_NT / 64];
   __shared__ int s_unplaced;
   const int t = threadIdx.x, lane = t & 63, w = t >> 6;
   const uint32_t B = (uint32_t)p.B;
+  // n / B: a shift where B is a power of two (a division by a number known only here is some twenty instructions)
+  const auto blocks_of = [&](uint32_t n) { return p.shift >= 0 ? n >> p.shift : n / B; };
   int unplaced = 0;
   if (t == 0) s_unplaced = 0;
   for (int64_t win = blockIdx.x;; win += gridDim.x) {
-    const int64_t row0 = win * TG_WIN + t * TG_PER;
+    const int64_t row0 = win * TG_WIN + t * TG_PER;  // the thread's first row
     int64_t slot[TG_PER];
     int pos[TG_PER];
 #pragma unroll
@@ -75,12 +82,12 @@ __global__ __launch_bounds__(TG_NT) void tables_grow_kernel(GrowParams p) {
         held = p.held ? max(p.held[r], 0) : 0;
         const int len = max(p.lens[r], held);
         n = len - held;
-        have = ((uint32_t)held + B - 1) / B;
-        want = min(((uint32_t)len + B - 1) / B, (uint32_t)p.max_blocks);
+        have = blocks_of((uint32_t)held + B - 1);
+        want = min(blocks_of((uint32_t)len + B - 1), (uint32_t)p.max_blocks);
         need = want > have ? want - have : 0;
       }
       const uint64_t own = (uint64_t)need << 32 | (uint32_t)n;
-      const uint64_t incl = wave_scan(own, lane);
+      const uint64_t incl = (uint64_t)wave_scan(need) << 32 | wave_scan((uint32_t)n);
       if (lane == 63) s_wave[w] = incl;
       __syncthreads();
       uint64_t before = base;
@@ -94,6 +101,7 @@ __global__ __launch_bounds__(TG_NT) void tables_grow_kernel(GrowParams p) {
       s_row[t] = row;
       s_at[t] = at;
       s_held[t] = held;
+      s_have[t] = (int)have;
       s_n[t] = n;
       if (blockIdx.x == 0 && win == 0 && r < p.R) {
         p.row_offsets[r] = (int32_t)row;
@@ -124,44 +132,69 @@ __global__ __launch_bounds__(TG_NT) void tables_grow_kernel(GrowParams p) {
           if (s_row[m] <= first) a = m;
           else b = m - 1;
         }
-        int known = -1, entry = -1;  // the entry of position known * B ..
+        int64_t end = 0;  // behind the request's last row
+        int q = 0, j = 0, off = 0, entry = -1;  // a row's position: offset `off` of table entry j, whose block this is
+        auto look = [&]() {
+          int32_t* cell = p.tables + (int64_t)(r0 + a) * p.max_blocks + j;
+          const int fresh = j - s_have[a];  // an entry of the call's own
+          entry = -1;
+          if ((uint32_t)j >= (uint32_t)p.max_blocks) return;
+          if (fresh < 0) {
+            entry = *cell;
+          } else {
+            const uint32_t f = s_at[a] + fresh;
+            if (f < (uint32_t)p.num_free) entry = p.free_blocks[f];
+            if (off == 0) *cell = entry;
+          }
+        };
+        auto enter = [&](int64_t i) {
+          end = (int64_t)s_row[a] + s_n[a];
+          q = s_held[a] + (int)(i - s_row[a]);
+          j = blocks_of(q);
+          off = q - j * p.B;
+          look();
+        };
+        bool in = false;
 #pragma unroll
         for (int u = 0; u < TG_PER; ++u) {
           const int64_t i = row0 + u;
           if (i < first || i >= hi) continue;
-          while (a + 1 < count && s_row[a + 1] <= i) {
-            ++a;
-            known = -1;
-          }
-          const int h = s_held[a], q = h + (int)(i - s_row[a]);
-          const int j = (uint32_t)q / B, have_a = ((uint32_t)h + B - 1) / B;
-          int32_t* cell = p.tables + (int64_t)(r0 + a) * p.max_blocks + j;
-          if (j != known) {
-            known = j;
-            entry = -1;
-            if (j < p.max_blocks) {
-              if (j < have_a) {
-                entry = *cell;
-              } else {
-                const uint32_t f = s_at[a] + (j - have_a);
-                if (f < (uint32_t)p.num_free) entry = p.free_blocks[f];
-              }
+          if (!in) {
+            enter(i);
+            in = true;
+          } else if (i >= end) {
+            do a = min(a + 1, count - 1);
+            while (a < count - 1 && s_n[a] == 0);  // i < hi: a request further on holds it
+            enter(i);
+          } else {
+            ++q;
+            if (++off == p.B) {
+              off = 0;
+              ++j;
+              look();
             }
           }
-          if ((uint32_t)q == (uint32_t)j * B && j >= have_a && j < p.max_blocks) *cell = entry;
           pos[u] = q;
-          slot[u] = entry >= 0 ? (int64_t)entry * B + (q - j * (int)B) : -1;
+          slot[u] = entry >= 0 ? (int64_t)entry * p.B + off : -1;
         }
       }
       __syncthreads();
     }
     const int64_t total = (uint32_t)base;
+    if (row0 + TG_PER <= p.max_rows) {
+      typedef int64_t pair __attribute__((ext_vector_type(2), aligned(8)));
+      typedef int quad __attribute__((ext_vector_type(4), aligned(4)));
+      reinterpret_cast<pair*>(p.slots + row0)[0] = pair{slot[0], slot[1]};
+      reinterpret_cast<pair*>(p.slots + row0)[1] = pair{slot[2], slot[3]};
+      if (p.positions) *reinterpret_cast<quad*>(p.positions + row0) = quad{pos[0], pos[1], pos[2], pos[3]};
+    } else {
 #pragma unroll
-    for (int u = 0; u < TG_PER; ++u)
-      if (row0 + u < p.max_rows) {
-        p.slots[row0 + u] = slot[u];
-        if (p.positions) p.positions[row0 + u] = pos[u];
-      }
+      for (int u = 0; u < TG_PER; ++u)
+        if (row0 + u < p.max_rows) {
+          p.slots[row0 + u] = slot[u];
+          if (p.positions) p.positions[row0 + u] = pos[u];
+        }
+    }
     if (blockIdx.x == 0 && win == 0) {
       if (unplaced) atomicAdd(&s_unplaced, unplaced);
       __syncthreads();
@@ -203,10 +236,10 @@ extern "C" kv_status kv_tables_grow(const int32_t* held, const int32_t* lens, in
   DeviceGuard dg(device);
   const kv_status st = device_ready(dg, device);
   if (st != KV_OK) return st;
-  const GrowParams p{held, lens, R, B, free_blocks, num_free, tables, max_blocks, max_rows, row_offsets,
+  const GrowParams p{held, lens, R, B, (B & (B - 1)) == 0 ? __builtin_ctz(B) : -1, free_blocks, num_free, tables, max_blocks, max_rows, row_offsets,
                      slots, positions, counts};
-  // a workgroup a window, up to four to a CU; further windows are walked
-  const int grid = (int)std::max<int64_t>(1, std::min<int64_t>((max_rows + TG_WIN - 1) / TG_WIN, 1024));
+  // a workgroup a window, up to 2^25 rows; further windows are walked
+  const int grid = (int)std::max<int64_t>(1, std::min<int64_t>((max_rows + TG_WIN - 1) / TG_WIN, 1 << 14));
   hipLaunchKernelGGL(tables_grow_kernel, dim3(grid), dim3(TG_NT), 0, reinterpret_cast<hipStream_t>(stream), p);
   return launched();
 }
