@@ -227,37 +227,31 @@ __device__ __forceinline__ Column<D> merge_column(SRC src, int n, int lane) {
   for (int d = 0; d < DPL<D>; ++d) x.o[d] = 0.0f;
 #pragma unroll 1
   for (int i0 = 0; i0 < n; i0 += CHUNK) {
-    const int mine = min(i0 + lane % CHUNK, n - 1);
-    float m = src(mine)[D], l = src(mine)[D + 1];
+    float2 ml[CHUNK];
     float o[CHUNK][DPL<D>];
 #pragma unroll
-    for (int i = 0; i < CHUNK; ++i)
-      if (i0 + i < n)
+    for (int i = 0; i < CHUNK; ++i) {  // past the last: the last again, not counted below
+      const float* part = src(min(i0 + i, n - 1));
+      ml[i] = *reinterpret_cast<const float2*>(part + D);
 #pragma unroll
-        for (int d = 0; d < DPL<D>; ++d) o[i][d] = src(i0 + i)[at + d];
-    if (i0 + lane % CHUNK >= n) {
-      m = -INFINITY;
-      l = 0.0f;
+      for (int d = 0; d < DPL<D>; ++d) o[i][d] = part[at + d];
     }
-    float top = fmaxf(x.m, m);
+    float top = x.m;
 #pragma unroll
-    for (int w = CHUNK / 2; w > 0; w >>= 1) top = fmaxf(top, __shfl_xor(top, w, 64));
+    for (int i = 0; i < CHUNK; ++i) top = fmaxf(top, ml[i].x);
     const float base = top == -INFINITY ? 0.0f : top;
-    const float was = __builtin_amdgcn_exp2f(x.m - base), f = __builtin_amdgcn_exp2f(m - base);
-    l *= f;
-#pragma unroll
-    for (int w = CHUNK / 2; w > 0; w >>= 1) l += __shfl_xor(l, w, 64);
-    x.l = fmaf(x.l, was, l);
+    const float was = __builtin_amdgcn_exp2f(x.m - base);
     x.m = top;
+    x.l *= was;
 #pragma unroll
     for (int d = 0; d < DPL<D>; ++d) x.o[d] *= was;
 #pragma unroll
-    for (int i = 0; i < CHUNK; ++i)
-      if (i0 + i < n) {
-        const float fi = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), i));
+    for (int i = 0; i < CHUNK; ++i) {
+      const float f = i0 + i < n ? __builtin_amdgcn_exp2f(ml[i].x - base) : 0.0f;
+      x.l = fmaf(ml[i].y, f, x.l);
 #pragma unroll
-        for (int d = 0; d < DPL<D>; ++d) x.o[d] = fmaf(o[i][d], fi, x.o[d]);
-      }
+      for (int d = 0; d < DPL<D>; ++d) x.o[d] = fmaf(o[i][d], f, x.o[d]);
+    }
   }
   return x;
 }
@@ -743,9 +737,9 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
 #pragma unroll
         for (int d = 0; d < DT; ++d) tr[(4 * q + j) * (D + 2) + c * DT + d] = o[nt][d][j];
       asm volatile("" ::: "memory");
-#pragma unroll 1
-      for (int i = 0; i < min(16 / COPIES, cols - nt * 16); ++i) {
-        if (COPIES == 1 && stay && !done) break;  // the rows are the partials
+      const int used = COPIES == 1 && stay && !done ? 0 : min(16 / COPIES, cols - nt * 16);  // 0: the rows are the partials
+#pragma unroll 2
+      for (int i = 0; i < used; ++i) {
         const Column<D> v = merge_column<D, COPIES>([&](int k) { return tr + (k * (16 / COPIES) + i) * (D + 2); }, lane);
         if (done) put_out<T, D, COLS>(p, rq.row, tile, nt * 16 + i, kvh, lane, v);
         else put_part<D>(part + (nt * 16 + i) * (D + 2), lane, v);
@@ -795,7 +789,7 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
     float* slot = slots0 + at * pitch + which * p.part_cols * (D + 2);
     if (lead >= 0 && !closed) open = OpenItem{cols, row, tile, at, 0};
     if (n == 1 && !(near[which] >> at & 1)) continue;
-#pragma unroll 1
+#pragma unroll 2
     for (int col = wave; col < cols; col += WAVES) {
       const Column<D> v = merge_column<D, WAVES>(
           [&](int i) -> const float* {
@@ -830,11 +824,16 @@ __global__ __launch_bounds__(PM_NT) void packed_attn_merge_kernel(PackedAttnPara
   const int64_t pitch = (int64_t)2 * p.part_cols * (D + 2);
   const float* first = p.part + ((int64_t)kvh * p.workers + wg * WG) * pitch;
   const float* lead = first + it.wave * pitch + p.part_cols * (D + 2);
+  auto merge = [&](auto chunk) {
 #pragma unroll 1
-  for (int col = wave; col < it.cols; col += PM_NT / 64)
-    put_out<T, D, S::COLS>(p, it.row, it.tile, col, kvh, lane,
-                           merge_column<D, 16>([&](int i) { return (i == 0 ? lead : first + i * WG * pitch) + col * (D + 2); },
-                                               it.groups, lane));
+    for (int col = wave; col < it.cols; col += PM_NT / 64)
+      put_out<T, D, S::COLS>(
+          p, it.row, it.tile, col, kvh, lane,
+          merge_column<D, chunk>([&](int i) { return (i == 0 ? lead : first + i * WG * pitch) + col * (D + 2); },
+                                 it.groups, lane));
+  };
+  if (it.groups <= 4) merge(std::integral_constant<int, 4>{});
+  else merge(std::integral_constant<int, 8>{});
 }
 
 // The kernel for a call's columns per request: as few column tiles as take them, and
