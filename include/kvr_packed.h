@@ -100,21 +100,24 @@ uint64_t kv_packed_attention_workspace_bytes(const kv_model_desc* desc, int32_t 
  *                its query rows' own included (stored before the call); of m query
  *                rows, row i is at position lens[r] - m + i
  *   block_tables device int32 [num_requests][max_blocks_per_req]
- *   max_query, max_len  host bounds of a request's query rows and length
+ *   max_query, max_len  host bounds of a request's query rows and length: rows and
+ *                positions past them are left out.  The workspace and the work of a call
+ *                are sized by them; (num_requests + rows * nq/nkv / 8) * max_len / 32
+ *                below 2^31 always goes
  *   out          device [rows][nq][d], model dtype, rows out_stride elements apart
  *   workspace    device scratch, on a boundary of 16 bytes; calls in flight at once
  *                need one each
  * Row i attends positions 0 .. its own: out = sum_j p_j v_j, p the softmax of
  * q . k_j / sqrt(d), q head h reading kv head h / (nq/nkv).  Scores, softmax and sums
  * are fp32, the output is rounded once.  Positions in a block whose table entry is
- * outside the arena, and those past max_blocks_per_req, are left out; a row that is
+ * outside the arena, and those past max_len or max_blocks_per_req, are left out; a row that is
  * left with no position is zero.  Nothing but a request's rows of out is written;
  * q and out may be the same memory only as the same rows.  The arrays on the device are
  * read when the call runs there, so a captured call follows their contents.
  *   KV_EINVAL  null arrays, a layer outside the model, negative sizes, rows above 2^24, a stride below
  *              nq * d, a pointer or stride not on its boundary (4 bytes), more than 16
  *              q heads per kv head, rows != num_requests without q_offsets, max_query
- *              or max_len < 1
+ *              or max_len < 1, more work than 2^31 units
  *   KV_ENOMEM  workspace smaller than kv_packed_attention_workspace_bytes
  *   KV_ESTATE  unknown handle */
 kv_status kv_packed_attention(kv_packed_t packed, int32_t layer, const void* q, int64_t q_stride,

@@ -82,6 +82,7 @@ struct PackedAttnParams {
   int nq, g;                     // q heads, and those of a kv head
   uint32_t g_inv;                // ceil(2^32 / g), 0 for g = 1: n / g of n < 2^28 is the product's high half
   int max_query;                 // rows of a request past it are left out: the sums have no room
+  int most_len;                  // positions of a request: max_len, or what its table holds
   int workers;                   // stretches per kv head, a multiple of four
   int part_cols;                 // columns of a slot of sums
   OpenItem* open;                // [workers / 4]
@@ -107,9 +108,20 @@ constexpr int ring_of(int occupancy) { return occupancy == 3 ? 4 : 8; }
 __device__ __forceinline__ int by_g(const PackedAttnParams& p, int n) {
   return p.g_inv ? (int)__umulhi((uint32_t)n, p.g_inv) : n;
 }
-// a / b of whole numbers below 2^53 / b: a correctly rounded quotient never reaches the
-// next whole number
-__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) { return (int64_t)((double)a / (double)b); }
+// Inclusive sums over the wave's lanes: within rows of 16, then the rows' last into those
+// behind.
+__device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);   // row_shr:1
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);   // row_shr:2
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);   // row_shr:4
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);   // row_shr:8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // row_bcast:15 into rows 1 and 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);  // row_bcast:31 into rows 2 and 3
+  return v;
+}
+// a / b of whole numbers: a correctly rounded quotient of such small ones never reaches
+// the next whole number
+__device__ __forceinline__ uint32_t quotient(uint32_t a, uint32_t b) { return (uint32_t)((double)a / (double)b); }
 // The maximum of the four lanes (q, c) of a c.
 __device__ __forceinline__ float max_over_q(float v) {
   const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -117,31 +129,25 @@ __device__ __forceinline__ float max_over_q(float v) {
   const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
-// a value that all lanes share, as a scalar
-__device__ __forceinline__ int64_t uniform(int64_t v) {
-  return (int64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)v) |
-         (int64_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32;
-}
-
 // Stretches: workers equal parts of all units, the first ones a unit longer.
 struct Stretches {
-  int workers;
-  int64_t size, longer;
-  __device__ __forceinline__ Stretches(int most, int64_t total) {
-    workers = (int)min((int64_t)most, total);  // a unit each at least
+  uint32_t workers, size, longer;
+  __device__ __forceinline__ Stretches(uint32_t most, uint32_t total) {
+    workers = min(most, total);  // a unit each at least
     size = total ? quotient(total, workers) : 0;
     longer = total - size * workers;
   }
-  __device__ __forceinline__ int64_t begin(int w) const { return w * size + min((int64_t)w, longer); }
-  __device__ __forceinline__ int holder(int64_t u) const {  // whose unit u is
-    const int64_t head = longer * (size + 1);
-    return (int)(u < head ? quotient(u, size + 1) : longer + quotient(u - head, size));
+  __device__ __forceinline__ uint32_t begin(uint32_t w) const { return w * size + min(w, longer); }
+  __device__ __forceinline__ uint32_t holder(uint32_t u) const {  // whose unit u is
+    const uint32_t head = longer * (size + 1);
+    return u < head ? quotient(u, size + 1) : longer + quotient(u - head, size);
   }
 };
 
 struct Request {
   int row, m, len, want;  // first query row, rows, positions there are, position after the last query
   int tiles, steps;       // column tiles, units of each
+  __device__ __forceinline__ uint32_t units() const { return (uint32_t)tiles * (uint32_t)steps; }
 };
 template <int COLS, int UNIT>
 __device__ __forceinline__ Request make_request(const PackedAttnParams& p, int row, int m, int want) {
@@ -149,7 +155,7 @@ __device__ __forceinline__ Request make_request(const PackedAttnParams& p, int r
   q.row = row;
   q.m = m;
   q.want = want;
-  q.len = (int)max((int64_t)0, min((int64_t)want, (int64_t)p.max_blocks * p.packed.block_size));
+  q.len = max(0, min(want, p.most_len));
   q.tiles = (int)(((int64_t)m * p.g + COLS - 1) / COLS);
   q.steps = max(1, (int)(((int64_t)q.len + UNIT - 1) / UNIT));
   return q;
@@ -205,8 +211,7 @@ struct Stretch {
   int cols[2];   // columns, 0: no such item
   int row[2], tile[2];
   int flags;     // 1: the item begun before ends in it; 2, 4: [0]'s, [1]'s sums are in the wave's ring
-  int pad;
-  int64_t end;   // the open item's units' end
+  uint32_t end;  // the open item's units' end
 };
 
 // One column from n partials of D sums, a maximum and a sum of weights, in their order:
@@ -230,12 +235,12 @@ __device__ __forceinline__ Column<D> merge_column(SRC src, int n, int lane) {
     float2 ml[CHUNK];
     float o[CHUNK][DPL<D>];
 #pragma unroll
-    for (int i = 0; i < CHUNK; ++i) {  // past the last: the last again, not counted below
-      const float* part = src(min(i0 + i, n - 1));
-      ml[i] = *reinterpret_cast<const float2*>(part + D);
+    for (int i = 0; i < CHUNK; ++i)  // past the last: the last again, not counted below
+      src(min(i0 + i, n - 1), [&](const auto* part) {
+        ml[i] = make_float2(part[D], part[D + 1]);
 #pragma unroll
-      for (int d = 0; d < DPL<D>; ++d) o[i][d] = part[at + d];
-    }
+        for (int d = 0; d < DPL<D>; ++d) o[i][d] = part[at + d];
+      });
     float top = x.m;
 #pragma unroll
     for (int i = 0; i < CHUNK; ++i) top = fmaxf(top, ml[i].x);
@@ -314,82 +319,66 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
   constexpr int QP = Split<T>::Q, PP = Split<T>::P;
   constexpr int NV = 4 * OWN;             // scores of a lane and column
   constexpr int REC = 17 * D, RING = ring_of(OCC), LOADS = (16 * D + 1023) / 1024 + 1;
-  // the plan's arrays, then the waves' rings
   __shared__ __attribute__((aligned(16))) char s_ring[PA_NT / 64][RING * REC];
   static_assert(RING % TILES == 0, "units do not wrap in the ring");
   static_assert(RING * REC >= 64 * (D + 2), "16 rows fit the ring");
   constexpr bool LOCAL = RING * REC >= NT * 64 * (D + 2);  // all columns' rows do
-  static_assert(sizeof(s_ring) >= (PA_NT + 1) * 8 + PA_NT * 12, "the plan's arrays fit the rings");
-  int64_t* s_pre = reinterpret_cast<int64_t*>(&s_ring[0][0]);
-  int* s_req = reinterpret_cast<int*>(s_pre + PA_NT + 1);  // first row, rows, length of up to PA_NT requests
-  __shared__ int64_t s_wave[PA_NT / 64];
-  __shared__ Stretch s_str[PA_NT / 64];
+  constexpr int WAVES = PA_NT / 64;
+  __shared__ uint32_t s_wave[WAVES];
+  __shared__ Stretch s_str[WAVES];
+  __shared__ int s_begin[WAVES][5];  // where a wave's stretch begins: request, its first unit, row, rows, length
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), c = lane & 15, q = lane >> 4;
   const int nkv = p.packed.nkv, g = p.g;
-  const int kvh = blockIdx.x % nkv, w = blockIdx.x / nkv * (PA_NT / 64) + wave;
+  const int kvh = blockIdx.x % nkv, w = blockIdx.x / nkv * WAVES + wave;
 
   // ---- the units before each thread's requests ----
   const int per = (p.R + PA_NT - 1) / PA_NT;
-  int64_t mine = 0;
-  for (int i = 0; i < per; ++i) {
-    const int r = t * per + i;
-    if (r < p.R) {
-      const Request x = get_request<COLS, UNIT>(p, r);
-      mine += (int64_t)x.tiles * x.steps;
-      if (per == 1) {
-        s_req[3 * t] = x.row;
-        s_req[3 * t + 1] = x.m;
-        s_req[3 * t + 2] = x.want;
-      }
+  uint32_t mine = 0;
+  Request rq{};
+  for (int i = 0; i < per; ++i)
+    if (t * per + i < p.R) {
+      rq = get_request<COLS, UNIT>(p, t * per + i);
+      mine += rq.units();
     }
+  uint32_t pre = wave_scan(mine);
+  if (lane == 63) s_wave[wave] = pre;
+  if (lane == 0) {
+    s_str[wave] = Stretch{};
+    s_begin[wave][0] = -1;
   }
-  int64_t incl = mine;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int64_t u = __shfl_up(incl, o, 64);
-    if (lane >= o) incl += u;
-  }
-  if (lane == 63) s_wave[wave] = incl;
-  if (lane == 0) s_str[wave] = Stretch{};
   __syncthreads();
-  int64_t before = 0, total = 0;
+  uint32_t total = 0;
+  pre -= mine;
 #pragma unroll
-  for (int i = 0; i < PA_NT / 64; ++i) {
-    if (i < wave) before += s_wave[i];
+  for (int i = 0; i < WAVES; ++i) {
+    if (i < wave) pre += s_wave[i];
     total += s_wave[i];
   }
-  s_pre[t + 1] = before + incl;
-  if (t == 0) s_pre[0] = 0;
+  total = __builtin_amdgcn_readfirstlane(total);
+  const Stretches st(p.workers, total);
+  // the thread whose requests hold a wave's first unit says so
+#pragma unroll
+  for (int i = 0; i < WAVES; ++i) {
+    const uint32_t v = blockIdx.x / nkv * WAVES + i, first = st.begin(v);
+    if (v < st.workers && first >= pre && first - pre < mine) {
+      s_begin[i][0] = t * per;
+      s_begin[i][1] = (int)pre;
+      s_begin[i][2] = rq.row;
+      s_begin[i][3] = rq.m;
+      s_begin[i][4] = rq.want;
+    }
+  }
   __syncthreads();
 
-  total = uniform(total);
-  const Stretches st(p.workers, total);
   float* const slots = p.part + ((int64_t)kvh * p.workers + w) * 2 * p.part_cols * (D + 2);
-  int64_t u0 = 0, u1 = 0, base = 0;
-  int r = 0;
-  Request rq{};
-  if (w < st.workers) {
-    u0 = st.begin(w);
-    u1 = st.begin(w + 1);
-    int a = 0, b = PA_NT - 1;  // the last thread's requests that begin at or before u0
-    while (a < b) {
-      const int m = (a + b + 1) / 2;
-      if (uniform(s_pre[m]) <= u0) a = m;
-      else b = m - 1;
-    }
-    r = a * per;
-    base = uniform(s_pre[a]);
-    if (per == 1)
-      rq = make_request<COLS, UNIT>(p, __builtin_amdgcn_readfirstlane(s_req[3 * a]),
-                                    __builtin_amdgcn_readfirstlane(s_req[3 * a + 1]),
-                                    __builtin_amdgcn_readfirstlane(s_req[3 * a + 2]));
-    else
-      rq = get_request<COLS, UNIT>(p, r);
-  }
-  __syncthreads();  // the rings are free
-  if (w < st.workers) {
-  while (base + (int64_t)rq.tiles * rq.steps <= u0) {
-    base += (int64_t)rq.tiles * rq.steps;
+  const auto begin_of = [&](int i) { return __builtin_amdgcn_readfirstlane(s_begin[wave][i]); };
+  int r = begin_of(0);
+  if (r >= 0) {
+  const uint32_t u0 = st.begin(w), u1 = st.begin(w + 1);
+  uint32_t base = begin_of(1);
+  rq = per == 1 ? make_request<COLS, UNIT>(p, begin_of(2), begin_of(3), begin_of(4)) : get_request<COLS, UNIT>(p, r);
+  while (u0 - base >= rq.units() && r + 1 < p.R) {
+    base += rq.units();
     rq = get_request<COLS, UNIT>(p, ++r);
   }
 
@@ -402,17 +391,21 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
   const int ks_off = 16 * D + c * (D / 32) + q * D / 128, vs_off = 16 * D + D / 2 + q * (D / 8) + c * D / 512 * 4;
   const int copy = c / (16 / COPIES);  // whose tile the lane's column scores
 
-  for (int64_t u = u0; u < u1;) {
+  for (uint32_t u = u0; u < u1;) {
     // ---- the stretch's part of one item ----
-    const int tile = (int)quotient(u - base, rq.steps), first = (int)(u - base - (int64_t)tile * rq.steps);
-    const int upto = (int)min((int64_t)rq.steps, first + (u1 - u));
+    const int tile = (int)quotient(u - base, rq.steps), first = (int)(u - base) - tile * rq.steps;
+    const int upto = (int)min((uint32_t)rq.steps, first + (u1 - u));
     const int cols = min(COLS, rq.m * g - tile * COLS);  // of this tile
+    if (cols <= 0) break;  // offsets that overlap so far that the units passed 2^32
     // positions that every column sees, and that any does
     const int i_lo = by_g(p, tile * COLS), i_hi = by_g(p, tile * COLS + cols - 1);
     const int all = min(rq.len, rq.want - rq.m + i_lo + 1), some = min(rq.len, rq.want - rq.m + i_hi + 1);
     const int stop = min(upto, (max(some, 0) + UNIT - 1) / UNIT);
 
-    // queries: loaded ahead of the records, used behind them
+    // 64 table entries, one a lane, and the queries: on their way ahead of the records
+    const int32_t* table = p.tables + (int64_t)r * p.max_blocks;
+    int next = first * TILES, bi = next / tpb, ti = next - bi * tpb;  // the next record, its block and place in it
+    int window = bi, tab = bi + lane < p.max_blocks ? table[bi + lane] : -1;
     constexpr int QV = 8 * (int)sizeof(T) / 16;  // 16-byte pieces of eight dims
     f32x4 qraw[NT][W][QV];
     int limit[NT];  // positions the lane's column sees
@@ -428,16 +421,15 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
         for (int e = 0; e < QV; ++e) qraw[nt][s][e] = reinterpret_cast<const f32x4_a4*>(src + 8 * s)[e];
     }
 
-    // the ring: 64 table entries at a time, one a lane
-    const int32_t* table = p.tables + (int64_t)r * p.max_blocks;
+    // the ring.  Entries are waited for where they are loaded, not at every use: that
+    // would wait for the ring's loads too.
+    asm volatile("" : "+v"(tab));
     auto entries = [&](int b0) {
       int e = b0 + lane < p.max_blocks ? table[b0 + lane] : -1;
-      asm volatile("" : "+v"(e));  // waited for here, not at every use: that would wait for the ring's loads too
+      asm volatile("" : "+v"(e));
       return e;
     };
-    int next = first * TILES, bi = next / tpb, ti = next % tpb;  // the next record, its block and place in it
     const int last = stop * TILES;
-    int window = bi, tab = entries(bi);
     int put = 0, get = 0;   // bytes into the ring
     bool broken = false;    // a block is not in the arena
     auto issue = [&]() {
@@ -754,12 +746,12 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
       me.row[which] = rq.row;
       me.tile[which] = tile;
       me.flags |= (stay ? 2 << which : 0) | (first > 0 && upto == rq.steps ? 1 : 0);
-      if (first == 0) me.end = base + (int64_t)(tile + 1) * rq.steps;
+      if (first == 0) me.end = base + (uint32_t)(tile + 1) * rq.steps;
     }
     u += upto - first;
     if (u < u1)
-      while (base + (int64_t)rq.tiles * rq.steps <= u) {
-        base += (int64_t)rq.tiles * rq.steps;
+      while (u - base >= rq.units() && r + 1 < p.R) {
+        base += rq.units();
         rq = get_request<COLS, UNIT>(p, ++r);
       }
   }
@@ -768,7 +760,6 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
   // ---- the workgroup's own merges: an item begun before it, and those its waves left
   // open, each over the waves that went on with it ----
   __syncthreads();
-  constexpr int WAVES = PA_NT / 64;
   const Stretch str = s_str[lane % WAVES];  // lane i: wave i's
   const auto of_waves = [](bool v) { return (uint32_t)__ballot(v) & ((1u << WAVES) - 1); };
   const uint32_t begun = of_waves(str.cols[0] != 0), left = of_waves(str.cols[1] != 0), ended = of_waves(str.flags & 1);
@@ -789,14 +780,17 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
     float* slot = slots0 + at * pitch + which * p.part_cols * (D + 2);
     if (lead >= 0 && !closed) open = OpenItem{cols, row, tile, at, 0};
     if (n == 1 && !(near[which] >> at & 1)) continue;
-#pragma unroll 2
+    // A wave's sums are in its ring or, where its stretch went on behind them, in the
+    // workspace: a branch for each, not loads that may be from either memory.
+#pragma unroll 1
     for (int col = wave; col < cols; col += WAVES) {
       const Column<D> v = merge_column<D, WAVES>(
-          [&](int i) -> const float* {
+          [&](int i, auto load) {
             const int j = at + i;
-            const float* far = i == 0 ? slot : slots0 + j * pitch;
-            const float* ring = reinterpret_cast<const float*>(&s_ring[0][0] + j * (RING * REC));
-            return ((i == 0 ? near[which] : near[0]) >> j & 1 ? ring : far) + col * (D + 2);
+            if ((i == 0 ? near[which] : near[0]) >> j & 1)
+              load(reinterpret_cast<const float*>(&s_ring[0][0] + j * (RING * REC)) + col * (D + 2));
+            else
+              load((i == 0 ? slot : slots0 + j * pitch) + col * (D + 2));
           },
           n, lane);
       if (closed) put_out<T, D, COLS>(p, row, tile, col, kvh, lane, v);
@@ -805,7 +799,7 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
   }
   if (kvh == 0 && t == 0) {
     const int wg = blockIdx.x / nkv;
-    if (open.cols) open.groups = st.holder(s_str[open.wave].end - 1) / WAVES - wg + 1;
+    if (open.cols) open.groups = min((int)st.holder(s_str[open.wave].end - 1), p.workers - 1) / WAVES - wg + 1;
     p.open[wg] = open;
   }
 }
@@ -829,8 +823,8 @@ __global__ __launch_bounds__(PM_NT) void packed_attn_merge_kernel(PackedAttnPara
     for (int col = wave; col < it.cols; col += PM_NT / 64)
       put_out<T, D, S::COLS>(
           p, it.row, it.tile, col, kvh, lane,
-          merge_column<D, chunk>([&](int i) { return (i == 0 ? lead : first + i * WG * pitch) + col * (D + 2); },
-                                 it.groups, lane));
+          merge_column<D, chunk>(
+              [&](int i, auto load) { load((i == 0 ? lead : first + i * WG * pitch) + col * (D + 2)); }, it.groups, lane));
   };
   if (it.groups <= 4) merge(std::integral_constant<int, 4>{});
   else merge(std::integral_constant<int, 8>{});
@@ -848,11 +842,15 @@ Plan plan_of(int dtype, int d, int g, int32_t max_query) {
   return Plan{nt, copies, 16 * nt / copies, 32, occupancy_of(dtype == KV_F32, d, nt)};
 }
 
+// Units of one kv head at most.
+int64_t units_of(const Plan& pl, int R, int64_t rows, int g, int64_t max_len) {
+  return (R + rows * g / pl.cols) * ((max_len + pl.unit - 1) / pl.unit);
+}
+
 // Stretches per kv head: as many waves as the chip holds at once, but no more than
 // there can be units; whole workgroups.
 int workers_of(const Plan& pl, int nkv, int R, int64_t rows, int g, int64_t max_len) {
-  const int64_t items = R + rows * g / pl.cols;
-  const int64_t units = items * ((max_len + pl.unit - 1) / pl.unit);
+  const int64_t units = units_of(pl, R, rows, g, max_len);
   const int64_t waves = 256 * 4 * (int64_t)pl.occupancy;
   return (int)round_up(std::max<int64_t>(1, std::min<int64_t>((waves + nkv - 1) / nkv, units)), PA_NT / 64);
 }
@@ -919,6 +917,7 @@ void run(const kv_packed* packed, int32_t layer, const void* q, int64_t q_stride
   p.g_inv = p.g == 1 ? 0 : (uint32_t)(((1ull << 32) + p.g - 1) / p.g);
   const AttnLayout L = attn_layout(d, R, rows, max_query, max_len);
   p.max_query = max_query;
+  p.most_len = (int)std::min<int64_t>({max_len, (int64_t)max_blocks * packed->block_size, INT32_MAX - 64});
   p.workers = L.workers;
   p.part_cols = L.cols;
   p.open = static_cast<OpenItem*>(workspace);
@@ -971,6 +970,10 @@ kv_status kv_packed_attention(kv_packed_t packed, int32_t layer, const void* q, 
     return kvr_err::set(KV_EINVAL, "the arrays and the strides need boundaries of 4 bytes");
   if (!workspace || (uintptr_t)workspace % 16 != 0)
     return kvr_err::set(KV_EINVAL, "null workspace, or one not on a boundary of 16 bytes");
+  const Plan plan = plan_of(d.dtype, d.head_dim, d.num_q_heads / d.num_kv_heads, max_query);
+  if (max_len > INT32_MAX ||
+      units_of(plan, R, rows, d.num_q_heads / d.num_kv_heads, max_len) > INT32_MAX)
+    return kvr_err::set(KV_EINVAL, "max_len or the work of one call above 2^31: split the query rows");
   const uint64_t need = kv_packed_attention_workspace_bytes(&d, R, rows, max_query, max_len);
   if (need > ws_bytes)
     return kvr_err::set(KV_ENOMEM, "workspace of %llu bytes < %llu needed", (unsigned long long)ws_bytes,

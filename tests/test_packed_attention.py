@@ -107,7 +107,7 @@ class Batch:
         half = torch.finfo(P.torch_dtype(s)).eps / 2
         for r, n in enumerate(self.lens):
             m = self.counts[r]
-            j = np.arange(max(0, min(n, self.tables.shape[1] * B)))
+            j = np.arange(max(0, min(n, self.tables.shape[1] * B, self.max_len)))
             blk = self.tables[r, j // B].astype(np.int64)
             there = (blk >= 0) & (blk < self.blocks)
             slots = (blk * B + j % B)[there]
@@ -353,7 +353,7 @@ def test_attention_refusals():
     for bad in (dict(layer=-1), dict(layer=2), dict(q=0), dict(out=0), dict(lens=0), dict(tables=0), dict(rows=-1),
                 dict(rows=1 << 31), dict(num_requests=-1), dict(max_blocks=-1), dict(max_query=0), dict(max_len=0),
                 dict(q_stride=w - 2), dict(out_stride=w - 2), dict(q_stride=w + 1), dict(q=0x1002), dict(lens=0x3001),
-                dict(q_offsets=0, rows=3), dict(workspace=0), dict(workspace=0x10008)):
+                dict(q_offsets=0, rows=3), dict(max_len=1 << 31), dict(rows=1 << 24, max_len=1 << 26), dict(workspace=0), dict(workspace=0x10008)):
         with pytest.raises(kvr.KvError) as e:
             kvr.kv_packed_attention(**{**ok, **bad})
         assert e.value.status == kvr.KV_EINVAL, bad
