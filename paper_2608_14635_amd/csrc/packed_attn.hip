@@ -214,33 +214,34 @@ struct Stretch {
   uint32_t end;  // the open item's units' end
 };
 
-// One column from n partials of D sums, a maximum and a sum of weights, in their order:
-// the lane's dims DPL lane .. of the sums.
+// Columns are merged 256 / D at a time: a lane has four dims of one of them.  A partial
+// is D sums, a maximum and a sum of weights; n of them go in their order.
 template <int D>
-constexpr int DPL = D < 64 ? 1 : D / 64;  // dims of a lane
+constexpr int LANES = D / 4;
 template <int D>
+constexpr int AT_ONCE = 64 / LANES<D>;
 struct Column {
-  float m, l, o[DPL<D>];
+  float m, l, o[4];
 };
+template <int D>
+__device__ __forceinline__ int dim_of(int lane) { return lane % LANES<D> * 4; }
+template <typename P>
+__device__ __forceinline__ void load_part(const P* part, int D, int dim, float2& ml, float* o) {
+  // rows of D + 2 floats: 8-byte aligned
+  ml = *reinterpret_cast<const float2*>(part + D);
+  const float2 a = *reinterpret_cast<const float2*>(part + dim), b = *reinterpret_cast<const float2*>(part + dim + 2);
+  o[0] = a.x; o[1] = a.y; o[2] = b.x; o[3] = b.y;
+}
 template <int D, int CHUNK, typename SRC>  // CHUNK: partials whose loads are on their way together
-__device__ __forceinline__ Column<D> merge_column(SRC src, int n, int lane) {
-  const int at = lane * DPL<D> % D;
-  Column<D> x;
-  x.m = -INFINITY;
-  x.l = 0.0f;
-#pragma unroll
-  for (int d = 0; d < DPL<D>; ++d) x.o[d] = 0.0f;
+__device__ __forceinline__ Column merge_column(SRC src, int n, int lane) {
+  Column x{-INFINITY, 0.0f, {0.0f, 0.0f, 0.0f, 0.0f}};
 #pragma unroll 1
   for (int i0 = 0; i0 < n; i0 += CHUNK) {
     float2 ml[CHUNK];
-    float o[CHUNK][DPL<D>];
+    float o[CHUNK][4];
 #pragma unroll
     for (int i = 0; i < CHUNK; ++i)  // past the last: the last again, not counted below
-      src(min(i0 + i, n - 1), [&](const auto* part) {
-        ml[i] = make_float2(part[D], part[D + 1]);
-#pragma unroll
-        for (int d = 0; d < DPL<D>; ++d) o[i][d] = part[at + d];
-      });
+      src(min(i0 + i, n - 1), [&](const auto* part) { load_part(part, D, dim_of<D>(lane), ml[i], o[i]); });
     float top = x.m;
 #pragma unroll
     for (int i = 0; i < CHUNK; ++i) top = fmaxf(top, ml[i].x);
@@ -249,36 +250,14 @@ __device__ __forceinline__ Column<D> merge_column(SRC src, int n, int lane) {
     x.m = top;
     x.l *= was;
 #pragma unroll
-    for (int d = 0; d < DPL<D>; ++d) x.o[d] *= was;
+    for (int d = 0; d < 4; ++d) x.o[d] *= was;
 #pragma unroll
     for (int i = 0; i < CHUNK; ++i) {
       const float f = i0 + i < n ? __builtin_amdgcn_exp2f(ml[i].x - base) : 0.0f;
       x.l = fmaf(ml[i].y, f, x.l);
 #pragma unroll
-      for (int d = 0; d < DPL<D>; ++d) x.o[d] = fmaf(o[i][d], f, x.o[d]);
+      for (int d = 0; d < 4; ++d) x.o[d] = fmaf(o[i][d], f, x.o[d]);
     }
-  }
-  return x;
-}
-
-// The same of N partials at hand.
-template <int D, int N, typename SRC>
-__device__ __forceinline__ Column<D> merge_column(SRC src, int lane) {
-  const int at = lane * DPL<D> % D;
-  Column<D> x;
-  x.m = src(0)[D];
-#pragma unroll
-  for (int k = 1; k < N; ++k) x.m = fmaxf(x.m, src(k)[D]);
-  const float base = x.m == -INFINITY ? 0.0f : x.m;
-  x.l = 0.0f;
-#pragma unroll
-  for (int d = 0; d < DPL<D>; ++d) x.o[d] = 0.0f;
-#pragma unroll
-  for (int k = 0; k < N; ++k) {
-    const float f = N == 1 ? 1.0f : __builtin_amdgcn_exp2f(src(k)[D] - base);
-    x.l = fmaf(src(k)[D + 1], f, x.l);
-#pragma unroll
-    for (int d = 0; d < DPL<D>; ++d) x.o[d] = fmaf(src(k)[at + d], f, x.o[d]);
   }
   return x;
 }
@@ -287,29 +266,26 @@ __device__ __forceinline__ Column<D> merge_column(SRC src, int lane) {
 // rows from `row` on, or as a partial.
 template <typename T, int D, int COLS>
 __device__ __forceinline__ void put_out(const PackedAttnParams& p, int row, int tile, int col, int kvh, int lane,
-                                        const Column<D>& v) {
-  if (lane * DPL<D> >= D) return;
+                                        const Column& v) {
   const int gc = tile * COLS + col, i = by_g(p, gc);
   T* dst = reinterpret_cast<T*>(p.out + (int64_t)(row + i) * p.out_stride) +
-           (int64_t)(kvh * p.g + gc - i * p.g) * D + lane * DPL<D>;
+           (int64_t)(kvh * p.g + gc - i * p.g) * D + dim_of<D>(lane);
   const float inv = v.l == 0.0f ? 0.0f : 1.0f / v.l;
-  if constexpr (DPL<D> == 2 && sizeof(T) == 2) {
-    *reinterpret_cast<uint32_t*>(dst) = v.l == 0.0f ? 0u : pack_bf16(v.o[0] * inv, v.o[1] * inv);
-  } else {
+  float x[4];
 #pragma unroll
-    for (int d = 0; d < DPL<D>; ++d) Elem<T>::store(dst, d, v.l == 0.0f ? 0.0f : v.o[d] * inv);
+  for (int d = 0; d < 4; ++d) x[d] = v.l == 0.0f ? 0.0f : v.o[d] * inv;
+  if constexpr (sizeof(T) == 2) {
+    typedef uint32_t u32x2_a4 __attribute__((ext_vector_type(2), aligned(4)));
+    *reinterpret_cast<u32x2_a4*>(dst) = u32x2_a4{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+  } else {
+    *reinterpret_cast<f32x4_a4*>(dst) = f32x4{x[0], x[1], x[2], x[3]};
   }
 }
 template <int D>
-__device__ __forceinline__ void put_part(float* dst, int lane, const Column<D>& v) {
-  if (lane * DPL<D> < D) {
-#pragma unroll
-    for (int d = 0; d < DPL<D>; ++d) dst[lane * DPL<D> + d] = v.o[d];
-  }
-  if (lane == 0) {
-    dst[D] = v.m;
-    dst[D + 1] = v.l;
-  }
+__device__ __forceinline__ void put_part(float* dst, int lane, const Column& v) {
+  reinterpret_cast<float2*>(dst + dim_of<D>(lane))[0] = make_float2(v.o[0], v.o[1]);
+  reinterpret_cast<float2*>(dst + dim_of<D>(lane))[1] = make_float2(v.o[2], v.o[3]);
+  if (dim_of<D>(lane) == 0) *reinterpret_cast<float2*>(dst + D) = make_float2(v.m, v.l);
 }
 
 template <typename T, int D, typename S, int OCC>
@@ -730,9 +706,12 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
         for (int d = 0; d < DT; ++d) tr[(4 * q + j) * (D + 2) + c * DT + d] = o[nt][d][j];
       asm volatile("" ::: "memory");
       const int used = COPIES == 1 && stay && !done ? 0 : min(16 / COPIES, cols - nt * 16);  // 0: the rows are the partials
-#pragma unroll 2
-      for (int i = 0; i < used; ++i) {
-        const Column<D> v = merge_column<D, COPIES>([&](int k) { return tr + (k * (16 / COPIES) + i) * (D + 2); }, lane);
+#pragma unroll 1
+      for (int i0 = 0; i0 < used; i0 += AT_ONCE<D>) {
+        const int i = i0 + lane / LANES<D>;
+        if (i >= used) continue;
+        const Column v = merge_column<D, COPIES>(
+            [&](int k, auto load) { load(tr + (k * (16 / COPIES) + i) * (D + 2)); }, COPIES, lane);
         if (done) put_out<T, D, COLS>(p, rq.row, tile, nt * 16 + i, kvh, lane, v);
         else put_part<D>(part + (nt * 16 + i) * (D + 2), lane, v);
       }
@@ -783,8 +762,10 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
     // A wave's sums are in its ring or, where its stretch went on behind them, in the
     // workspace: a branch for each, not loads that may be from either memory.
 #pragma unroll 1
-    for (int col = wave; col < cols; col += WAVES) {
-      const Column<D> v = merge_column<D, WAVES>(
+    for (int c0 = wave * AT_ONCE<D>; c0 < cols; c0 += WAVES * AT_ONCE<D>) {
+      const int col = c0 + lane / LANES<D>;
+      if (col >= cols) continue;
+      const Column v = merge_column<D, WAVES>(
           [&](int i, auto load) {
             const int j = at + i;
             if ((i == 0 ? near[which] : near[0]) >> j & 1)
@@ -805,10 +786,10 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
 }
 
 // Workgroup (kv head, workgroup of the first kernel): the item that it began and left
-// open, merged over the workgroups that went on with it, in their order, a wave a
-// column.  (Eight waves: four took 12 us where eight take 8, with 48 partials of 5
-// columns; sixteen cost calls of few more than they gave.)
-constexpr int PM_NT = 512;
+// open, merged over the workgroups that went on with it, in their order.  Its time is its
+// loads' way from other chiplets' caches: 3 us with few partials, 8.5 with 48 of 5
+// columns at 16 loads together (9.8 at 8).
+constexpr int PM_NT = 256;
 template <typename T, int D, typename S>
 __global__ __launch_bounds__(PM_NT) void packed_attn_merge_kernel(PackedAttnParams p) {
   constexpr int WG = PA_NT / 64;
@@ -820,14 +801,17 @@ __global__ __launch_bounds__(PM_NT) void packed_attn_merge_kernel(PackedAttnPara
   const float* lead = first + it.wave * pitch + p.part_cols * (D + 2);
   auto merge = [&](auto chunk) {
 #pragma unroll 1
-    for (int col = wave; col < it.cols; col += PM_NT / 64)
+    for (int c0 = wave * AT_ONCE<D>; c0 < it.cols; c0 += PM_NT / 64 * AT_ONCE<D>) {
+      const int col = c0 + lane / LANES<D>;
+      if (col >= it.cols) continue;
       put_out<T, D, S::COLS>(
           p, it.row, it.tile, col, kvh, lane,
           merge_column<D, chunk>(
               [&](int i, auto load) { load((i == 0 ? lead : first + i * WG * pitch) + col * (D + 2)); }, it.groups, lane));
+    }
   };
   if (it.groups <= 4) merge(std::integral_constant<int, 4>{});
-  else merge(std::integral_constant<int, 8>{});
+  else merge(std::integral_constant<int, 16>{});
 }
 
 // The kernel for a call's columns per request: as few column tiles as take them, and
