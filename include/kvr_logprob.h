@@ -24,7 +24,7 @@ extern "C" {
  * 1 .. 2^21, top_n 0 .. KV_LOGPROBS_MAX_TOP and at most vocab). */
 uint64_t kv_logprobs_workspace_bytes(int64_t rows, int32_t vocab, int32_t top_n);
 
-/* With x_v = scale * z_v of a row's logits z (scale > 0, the inverse temperature):
+/* With x_v = scale * z_v of a row's logits z (0 < scale <= 2^127, the inverse temperature):
  *   logprobs[i]     = x_t - log sum_v e^(x_v), t = tokens[i]
  *   entropy[i]      = - sum_v p_v log p_v, p = softmax(x); terms with p_v = 0 are 0
  *   top_tokens[i][] the top_n tokens of largest z_v in falling order, the lower
@@ -46,7 +46,7 @@ uint64_t kv_logprobs_workspace_bytes(int64_t rows, int32_t vocab, int32_t top_n)
  * makes its log probabilities and entropy NaN; its likeliest tokens rank NaN below
  * every number.  Sums are fp32; results do not depend on timing.
  *   KV_EINVAL  null arrays, rows or vocab out of range, stride < vocab, an unknown dtype, a
- *              scale that is not positive and finite, top_n out of range, a pointer not
+ *              scale that is not positive or above 2^127, top_n out of range, a pointer not
  *              on its boundary
  *   KV_ENOMEM  workspace smaller than kv_logprobs_workspace_bytes
  *   KV_EDEVICE device not selectable, or a device error */

@@ -1,11 +1,13 @@
 // Log probabilities of given tokens, entropy and likeliest tokens (kvr_logprob.h).
 //
-// In log2 units, t_v = c (z_v - m') with c = scale log2 e and m' next to the row's
-// largest logit m (C = c m rounded, t_v = fma(c, z_v, -C): the rounding of C is the same
-// factor in every term and cancels), e_v = 2^t_v, l = sum e_v and s = sum t_v e_v:
-//   log p_t = ln 2 (t_t - log2 l),   entropy = ln 2 (log2 l - s / l)
-// (both terms of the entropy are of one sign, so nothing cancels).  Where C would
-// overflow (masks of the dtype's lowest value alone in a row), t_v = (z_v - m) c.  A row is cut into
+// In log2 units, t_v = c (z_v - m) with c = scale log2 e and m the row's largest logit,
+// e_v = 2^t_v, l = sum e_v and s = sum t_v e_v:
+//   log p_t = scale (z_t - m) - ln 2 log2 l,   entropy = ln 2 (log2 l - s / l)
+// (both terms of each are of one sign, so nothing cancels).  Over a chunk of the row t_v is
+// one operation, fma(c, z_v, -C) with C = c m rounded (m the chunk's): the rounding of C
+// shifts all t alike, and is taken out where chunks meet.  Where C is so large that its
+// rounding would count, t_v = (z_v - m) c.  (That everywhere: 61 us for the prompt below,
+// not 55.)  A row is cut into
 // chunks; a workgroup reads its chunk once, into registers, takes the chunk's C, l and
 // s from there and, where asked, its top_n entries; a second kernel merges the
 // chunks of each row in a fixed order.
@@ -166,14 +168,16 @@ __device__ __forceinline__ uint64_t bound_of_keys(uint64_t own, int top, S& s) {
   return bound;
 }
 
+// What logits are taken relative to: -infinity stands for no logit above it, and
+// differences with it would be NaN.
+__device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.0f : m; }
 // C of a maximum: rounded, not contracted into what it enters.
 __device__ __forceinline__ float c_of(float m, float scale2) {
 #pragma clang fp contract(off)
-  return m == -INFINITY ? 0.0f : m * scale2;
+  return m * scale2;
 }
-// Whether a maximum m's C stands for it: no overflow in C, or in t of a value near it
-// (-infinity: C = 0, every t is -infinity).
-__device__ __forceinline__ bool plain(float m) { return fabsf(m) < 1e36f || m == -INFINITY; }
+// Whether C stands for c m up to 2^-5.
+__device__ __forceinline__ bool by_c(float c) { return fabsf(c) < 0x1p20f; }
 
 // Sums and maximum over the workgroup, in every thread; red holds a value a wave.
 __device__ __forceinline__ float2 block_total(float a, float b, float2* red) {
@@ -240,22 +244,22 @@ __global__ __launch_bounds__(LP_NT) void logprob_chunk_kernel(LogprobParams p) {
   // nothing but -infinity (or NaN): sums of zeros (or NaN)
   const float m = block_most(own, s_most);
   float l = 0.0f, s = 0.0f;
+  const float base = base_of(m), cm = c_of(base, p.scale2);
   auto add = [&](float x) {
     const float e = __builtin_amdgcn_exp2f(x);
     l += e;
     s = fmaf(fmaxf(x, -1e30f), e, s);  // -infinity times 0; a NaN is in l
   };
-  if (plain(m)) {
-    const float base = c_of(m, p.scale2);
+  if (by_c(cm)) {
 #pragma unroll
     for (int i = 0; i < VECS; ++i)
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) add(fmaf(v[i].value(j), p.scale2, -base));
+      for (int j = 0; j < VEC; ++j) add(fmaf(v[i].value(j), p.scale2, -cm));
   } else {
 #pragma unroll
     for (int i = 0; i < VECS; ++i)
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) add((v[i].value(j) - m) * p.scale2);
+      for (int j = 0; j < VEC; ++j) add((v[i].value(j) - base) * p.scale2);
   }
   const float2 sums = block_total(l, s, s_sums);
   if (t == 0) p.stats[row * p.chunks + c] = make_float4(m, sums.x, sums.y, 0.0f);
@@ -329,12 +333,13 @@ __global__ __launch_bounds__(LP_NT) void logprob_row_kernel(LogprobParams p) {
   float m = -INFINITY;
   for (int c = lane; c < p.chunks; c += 64) m = fmaxf(m, stats[c].x);
   m = wave_max(m);
-  const bool by_c = plain(m);
-  const float base = by_c ? c_of(m, p.scale2) : 0.0f;
+  const float base = base_of(m);
   float l = 0.0f, s = 0.0f;
   for (int c = lane; c < p.chunks; c += 64) {
     const float4 q = stats[c];
-    const float x = fmaxf(by_c ? (plain(q.x) ? c_of(q.x, p.scale2) - base : -INFINITY) : (q.x - m) * p.scale2, -1e30f);
+    // the chunk's t to the row's: by its largest logit, and without the rounding of its C
+    const float cm = c_of(base_of(q.x), p.scale2), off = by_c(cm) ? fmaf(base_of(q.x), p.scale2, -cm) : 0.0f;
+    const float x = fmaxf(fmaf(q.x - base, p.scale2, -off), -1e30f);
     const float e = __builtin_amdgcn_exp2f(x);
     l = fmaf(q.y, e, l);
     s += e * fmaf(x, q.y, q.z);
@@ -343,12 +348,7 @@ __global__ __launch_bounds__(LP_NT) void logprob_row_kernel(LogprobParams p) {
   s = wave_sum(s);
   const bool none = l == 0.0f;  // every logit -infinity
   const float log_l = none ? 0.0f : log2f(l);
-  auto logprob = [&](float v) {
-    if (none) return -INFINITY;
-    if (!by_c) return (v - m) * p.scale - LN2 * log_l;
-    const float x = fmaf(v, p.scale2, -base);
-    return x == -INFINITY && l == l ? v * p.scale : LN2 * (x - log_l);  // a finite v far below all others
-  };
+  auto logprob = [&](float v) { return none ? -INFINITY : (v - base) * p.scale - LN2 * log_l; };
   if (t == 0) {
     if (p.logprobs) p.logprobs[row] = tok < 0 ? 0.0f : tok < p.vocab ? logprob(z) : l != l ? l : -INFINITY;
     if (p.entropy) {
@@ -411,7 +411,7 @@ kv_status kv_logprobs(const void* logits, int32_t dtype, int64_t rows, int32_t v
   if (rows < 0 || rows > (1 << 20)) return kvr_err::set(KV_EINVAL, "rows must be 0 .. 2^20");
   if (vocab < 1 || vocab > LP_MAX_VOCAB) return kvr_err::set(KV_EINVAL, "vocab must be 1 .. 2^21");
   if (stride < vocab) return kvr_err::set(KV_EINVAL, "the stride is below the vocabulary");
-  if (!(scale > 0.0f) || !(scale < INFINITY)) return kvr_err::set(KV_EINVAL, "scale must be positive and finite");
+  if (!(scale > 0.0f) || !(scale <= 0x1p127f)) return kvr_err::set(KV_EINVAL, "scale must be positive and at most 2^127");
   if (top_n < 0 || top_n > KV_LOGPROBS_MAX_TOP || top_n > vocab)
     return kvr_err::set(KV_EINVAL, "top_n must be 0 .. %d and at most the vocabulary", KV_LOGPROBS_MAX_TOP);
   if (rows == 0) return kvr_err::clear();

@@ -184,6 +184,26 @@ def test_special_rows(V, top, dt):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dt", list(DT))
+def test_logits_of_any_size(dt):
+    """Where scale log2 e times the largest logit has steps above 1, or no fp32 value."""
+    V = 20000
+    base = torch.randn(V, generator=torch.Generator().manual_seed(4)) * 3
+    i = torch.arange(V)
+    for size in (1e8, 1e10, 1e20, 1e37):
+        rows = torch.stack([torch.full((V,), -size), torch.full((V,), size), base * size,
+                            torch.where(i < V // 2, -size, -1.25 * size), torch.where(i == 5, size, base),
+                            torch.where(i % 2 == 0, base, torch.tensor(-size))]).to(DT[dt])
+        for scale in (1.0, 2.0 / size, 2.0 ** (20 if size < 1e30 else 0)):
+            c = Call(rows, scale, [5, 7, 9, V - 1, 5, 6], 4)
+            c.run()
+            c.check()
+    c = Call((base * 2.0 ** -100).to(DT[dt])[None], 2.0 ** 100, [3], 4)
+    c.run()
+    c.check()
+
+
+@pytest.mark.gpu
 def test_outputs_not_wanted():
     z, tok = random_rows(4, 5000, torch.float32, 3)
     for want, top in (((True, False), 0), ((False, True), 0), ((False, False), 4), ((True, False), 2)):
@@ -247,7 +267,7 @@ def test_workspace_bytes():
     (dict(dtype=2), kvr.KV_EINVAL), (dict(rows=-1), kvr.KV_EINVAL), (dict(rows=(1 << 20) + 1), kvr.KV_EINVAL),
     (dict(vocab=0), kvr.KV_EINVAL), (dict(vocab=(1 << 21) + 1, stride=1 << 22), kvr.KV_EINVAL),
     (dict(stride=999), kvr.KV_EINVAL), (dict(scale=0.0), kvr.KV_EINVAL), (dict(scale=-1.0), kvr.KV_EINVAL),
-    (dict(scale=float("inf")), kvr.KV_EINVAL), (dict(scale=float("nan")), kvr.KV_EINVAL),
+    (dict(scale=float("inf")), kvr.KV_EINVAL), (dict(scale=2.0 ** 127 * 1.5), kvr.KV_EINVAL), (dict(scale=float("nan")), kvr.KV_EINVAL),
     (dict(top_n=-1), kvr.KV_EINVAL), (dict(top_n=65), kvr.KV_EINVAL), (dict(vocab=3, top_n=4), kvr.KV_EINVAL),
     (dict(logits=0), kvr.KV_EINVAL), (dict(tokens=0), kvr.KV_EINVAL), (dict(top_tokens=0), kvr.KV_EINVAL),
     (dict(top_logprobs=0), kvr.KV_EINVAL), (dict(logits=0x1002), kvr.KV_EINVAL), (dict(tokens=0x2001), kvr.KV_EINVAL),
