@@ -75,8 +75,9 @@ kv_status kv_packed_load(kv_packed_t packed, int32_t layer, void* k, int64_t k_s
  * back.  The two arenas describe the same model on one device; block sizes and
  * tables are their own.  Pairs with a slot outside its arena are passed over, a
  * destination listed more than once holds undefined values afterwards.
- *   KV_EINVAL  null arrays, rows < 0, a stride below nkv * d, a pointer not on its
- *              boundary
+ * For these four:
+ *   KV_EINVAL  null arrays, rows outside 0 .. 2^31 - 1, a layer outside the model, a
+ *              stride below nkv * d, a pointer or stride not on its boundary
  *   KV_ESTATE  unknown handle, arenas of different models or devices */
 kv_status kv_packed_park(kv_arena_t arena, const int64_t* arena_slots, kv_packed_t packed,
                          const int64_t* packed_slots, int64_t rows, void* stream);
@@ -86,7 +87,7 @@ kv_status kv_packed_restore(kv_packed_t packed, const int64_t* packed_slots, kv_
 /* Workspace bytes of kv_packed_attention for up to num_requests requests, `rows`
  * query rows in all, at most max_query of one request, lengths up to max_len; 0 for
  * an invalid description (kv_packed_bytes's, at most 16 q heads per kv head) or
- * non-positive sizes. */
+ * sizes that no call takes (requests and rows are 1 .. 2^24, max_len below 2^31). */
 uint64_t kv_packed_attention_workspace_bytes(const kv_model_desc* desc, int32_t num_requests,
                                              int64_t rows, int32_t max_query, int64_t max_len);
 
@@ -100,24 +101,28 @@ uint64_t kv_packed_attention_workspace_bytes(const kv_model_desc* desc, int32_t 
  *                its query rows' own included (stored before the call); of m query
  *                rows, row i is at position lens[r] - m + i
  *   block_tables device int32 [num_requests][max_blocks_per_req]
- *   max_query, max_len  host bounds of a request's query rows and length: rows and
- *                positions past them are left out.  The workspace and the work of a call
- *                are sized by them; (num_requests + rows * nq/nkv / 8) * max_len / 32
- *                below 2^31 always goes
+ *   max_query, max_len  host bounds of a request's query rows and length: its rows and
+ *                positions past them are left out (row i stays at lens[r] - m + i).
+ *                The workspace and the work of a call are sized by them;
+ *                (num_requests + rows * nq/nkv / 8) * max_len / 32 below 2^31 always
+ *                goes
  *   out          device [rows][nq][d], model dtype, rows out_stride elements apart
  *   workspace    device scratch, on a boundary of 16 bytes; calls in flight at once
  *                need one each
  * Row i attends positions 0 .. its own: out = sum_j p_j v_j, p the softmax of
  * q . k_j / sqrt(d), q head h reading kv head h / (nq/nkv).  Scores, softmax and sums
  * are fp32, the output is rounded once.  Positions in a block whose table entry is
- * outside the arena, and those past max_len or max_blocks_per_req, are left out; a row that is
- * left with no position is zero.  Nothing but a request's rows of out is written;
- * q and out may be the same memory only as the same rows.  The arrays on the device are
- * read when the call runs there, so a captured call follows their contents.
- *   KV_EINVAL  null arrays, a layer outside the model, negative sizes, rows above 2^24, a stride below
- *              nq * d, a pointer or stride not on its boundary (4 bytes), more than 16
- *              q heads per kv head, rows != num_requests without q_offsets, max_query
- *              or max_len < 1, more work than 2^31 units
+ * outside the arena, and those past max_len or max_blocks_per_req, are left out; a row
+ * that is left with no position, or with none whose score is above -infinity, is zero.
+ * Requests may share blocks, not query rows: q_offsets does not decrease.  Nothing but
+ * the requests' rows of out is written; q and out may be the same memory only as the
+ * same rows.  The arrays on the device are read when the call runs there, so a captured
+ * call follows their contents.
+ *   KV_EINVAL  null arrays, a layer outside the model, negative sizes, rows or
+ *              num_requests above 2^24, a stride below nq * d, a pointer or stride not
+ *              on its boundary (4 bytes), more than 16 q heads per kv head, rows !=
+ *              num_requests without q_offsets, max_query or max_len < 1, more work
+ *              than 2^31 units
  *   KV_ENOMEM  workspace smaller than kv_packed_attention_workspace_bytes
  *   KV_ESTATE  unknown handle */
 kv_status kv_packed_attention(kv_packed_t packed, int32_t layer, const void* q, int64_t q_stride,

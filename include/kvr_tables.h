@@ -47,8 +47,8 @@ extern "C" {
  *                  it lacked, rows, rows without a slot
  * No host synchronisation, no workspace; the same call again writes the same.
  *   KV_EINVAL  null arrays, num_requests, num_free, max_blocks_per_req or
- *              max_rows < 0, block_size <= 0, an array not on its elements'
- *              boundary
+ *              max_rows < 0, num_requests above 2^30, block_size <= 0, an array not
+ *              on its elements' boundary
  *   KV_EDEVICE device not selectable, or a device error */
 kv_status kv_tables_grow(const int32_t* held, const int32_t* lens, int32_t num_requests,
                          int32_t block_size, const int32_t* free_blocks, int32_t num_free,

@@ -285,7 +285,7 @@ kv_status move_rows(kv_packed* a, bool to_packed, int32_t layer, const void* k, 
   const int64_t e = elem_bytes(d.dtype), row = (int64_t)d.num_kv_heads * d.head_dim;
   if (layer < 0 || layer >= d.num_layers)
     return kvr_err::set(KV_EINVAL, "layer %d outside [0, %d)", layer, d.num_layers);
-  if (rows < 0) return kvr_err::set(KV_EINVAL, "rows < 0");
+  if (rows < 0 || rows > INT32_MAX) return kvr_err::set(KV_EINVAL, "rows must be 0 .. 2^31 - 1");
   if (rows == 0) return kvr_err::clear();
   if (!k || !v || !slots) return kvr_err::set(KV_EINVAL, "null k, v or slots");
   if (k_stride < row || v_stride < row)
@@ -334,7 +334,7 @@ kv_status move_all(bool to_packed, kv_arena* arena, const int64_t* arena_slots, 
       d.dtype != b.dtype)
     return kvr_err::set(KV_ESTATE, "the arenas describe different models");
   if (arena->device != packed->device) return kvr_err::set(KV_ESTATE, "the arenas are on different devices");
-  if (rows < 0) return kvr_err::set(KV_EINVAL, "rows < 0");
+  if (rows < 0 || rows > INT32_MAX) return kvr_err::set(KV_EINVAL, "rows must be 0 .. 2^31 - 1");
   if (rows == 0) return kvr_err::clear();
   if (!arena_slots || !packed_slots) return kvr_err::set(KV_EINVAL, "null slots");
   if (((uintptr_t)arena_slots | (uintptr_t)packed_slots) % 8 != 0)

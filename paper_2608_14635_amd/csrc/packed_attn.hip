@@ -25,12 +25,25 @@
 //   the B operands of d/16 products.
 // Records reach a wave through a ring of its own in LDS, by direct-to-LDS loads: a
 // record is 17 d contiguous bytes, K's and V's lane by lane in the operands' order, so
-// the reads back are linear.  What bounds the kernel is the bytes in flight; the ring
-// keeps six or eight records a wave on their way without a register.
+// the reads back are linear, and records are on their way without a register.
 // Weights enter the product as a bf16 number and the bf16 rest (2^-17 of a weight lost),
 // in fp32 models as three (as do the queries): rounding them once would cost more than
 // the output's own rounding where few positions weigh, and the products are not what
 // bounds the kernel.
+//
+// What bounds it, on 16 requests of 2048 - 16384 positions (8 kv heads of 128, 4 q heads
+// each, 124 MB of records), one query row each: 34 us (21 at a plain read's 6 TB/s).
+// Without the products and the softmax the loads take 31 us, without the loads the rest
+// takes 28; 9 us pass before the first record is there and after the last (the plan,
+// three loads that follow each other, the merges).  Two requests of 150 - 200 thousand
+// positions: 80 us (5 TB/s).  One to five query rows of 40 requests of 300 - 4000
+// positions (5 q heads a kv head, COLS 32): 41 us, the instructions of the softmax and
+// of the conversions.
+//   Workgroups a CU and records a ring: three and four.  Three and six took 36.4 us (a
+// little over half of the LDS left for the third), two and eight 38.6, four and four
+// 39.6 (registers spill).  Column tiles of 32 need two a CU: three took 60 us against 45.
+//   As many waves as run at once: one and a half times as many took 39 us, twice as
+// many 41; the stretches are equal, so more of them only merge more.
 #include <algorithm>
 #include <type_traits>
 
@@ -46,6 +59,7 @@ namespace {
 
 constexpr int PA_NT = 256;         // four waves
 constexpr float SLACK = 8.0f;      // rescale slack, log2 units
+constexpr int MOST_ROWS = 1 << 24; // query rows and requests of a call
 
 // Copies of the columns, and column tiles, that a kernel is built for.
 template <int NT_, int COPIES_>
@@ -79,7 +93,7 @@ struct PackedAttnParams {
   const int32_t* lens;
   const int32_t* tables;
   int R, max_blocks;
-  int nq, g;                     // q heads, and those of a kv head
+  int g;                         // q heads of a kv head
   uint32_t g_inv;                // ceil(2^32 / g), 0 for g = 1: n / g of n < 2^28 is the product's high half
   int max_query;                 // rows of a request past it are left out: the sums have no room
   int most_len;                  // positions of a request: max_len, or what its table holds
@@ -145,7 +159,7 @@ struct Stretches {
 };
 
 struct Request {
-  int row, m, len, want;  // first query row, rows, positions there are, position after the last query
+  int row, m, len, want;  // first query row, rows, positions there are, position after the last of these rows
   int tiles, steps;       // column tiles, units of each
   __device__ __forceinline__ uint32_t units() const { return (uint32_t)tiles * (uint32_t)steps; }
 };
@@ -162,13 +176,15 @@ __device__ __forceinline__ Request make_request(const PackedAttnParams& p, int r
 }
 template <int COLS, int UNIT>
 __device__ __forceinline__ Request get_request(const PackedAttnParams& p, int r) {
-  int row = r, m = 1;
+  int row = r, m = 1, want = p.lens[r];
   if (p.q_offsets) {
     const int a = p.q_offsets[r], b = p.q_offsets[r + 1];
     row = min(max(a, 0), (int)p.rows);
-    m = min(max(min(b, (int)p.rows) - row, 0), p.max_query);
+    const int all = max(min(b, (int)p.rows) - row, 0);
+    m = min(all, p.max_query);
+    want = max(want, 0) - (all - m);  // the rows left out are the last ones
   }
-  return make_request<COLS, UNIT>(p, row, m, p.lens[r]);
+  return make_request<COLS, UNIT>(p, row, m, want);
 }
 
 // The scale of byte i of a word.  The conversions read the exponent alone, whatever the
@@ -350,390 +366,393 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
   const auto begin_of = [&](int i) { return __builtin_amdgcn_readfirstlane(s_begin[wave][i]); };
   int r = begin_of(0);
   if (r >= 0) {
-  const uint32_t u0 = st.begin(w), u1 = st.begin(w + 1);
-  uint32_t base = begin_of(1);
-  rq = per == 1 ? make_request<COLS, UNIT>(p, begin_of(2), begin_of(3), begin_of(4)) : get_request<COLS, UNIT>(p, r);
-  while (u0 - base >= rq.units() && r + 1 < p.R) {
-    base += rq.units();
-    rq = get_request<COLS, UNIT>(p, ++r);
-  }
-
-  const int B = p.packed.block_size, tpb = B / PK_TILE;
-  const float scale_log2 = 1.4426950408889634f / sqrtf((float)D);
-  const char* head = p.packed.base + (int64_t)kvh * tpb * (17 * D);
-  const int64_t block_bytes = (int64_t)nkv * tpb * (17 * D);
-  char* const ring = s_ring[wave];
-  const int k_off = c * (D / 2) + q * (D / 8), v_off = 8 * D + q * (2 * D) + c * (D / 8);
-  const int ks_off = 16 * D + c * (D / 32) + q * D / 128, vs_off = 16 * D + D / 2 + q * (D / 8) + c * D / 512 * 4;
-  const int copy = c / (16 / COPIES);  // whose tile the lane's column scores
-
-  for (uint32_t u = u0; u < u1;) {
-    // ---- the stretch's part of one item ----
-    const int tile = (int)quotient(u - base, rq.steps), first = (int)(u - base) - tile * rq.steps;
-    const int upto = (int)min((uint32_t)rq.steps, first + (u1 - u));
-    const int cols = min(COLS, rq.m * g - tile * COLS);  // of this tile
-    if (cols <= 0) break;  // offsets that overlap so far that the units passed 2^32
-    // positions that every column sees, and that any does
-    const int i_lo = by_g(p, tile * COLS), i_hi = by_g(p, tile * COLS + cols - 1);
-    const int all = min(rq.len, rq.want - rq.m + i_lo + 1), some = min(rq.len, rq.want - rq.m + i_hi + 1);
-    const int stop = min(upto, (max(some, 0) + UNIT - 1) / UNIT);
-
-    // 64 table entries, one a lane, and the queries: on their way ahead of the records
-    const int32_t* table = p.tables + (int64_t)r * p.max_blocks;
-    int next = first * TILES, bi = next / tpb, ti = next - bi * tpb;  // the next record, its block and place in it
-    int window = bi, tab = bi + lane < p.max_blocks ? table[bi + lane] : -1;
-    constexpr int QV = 8 * (int)sizeof(T) / 16;  // 16-byte pieces of eight dims
-    f32x4 qraw[NT][W][QV];
-    int limit[NT];  // positions the lane's column sees
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      const int col = COPIES == 1 ? nt * 16 + c : c % (16 / COPIES), gc = tile * COLS + min(col, cols - 1), i = by_g(p, gc);
-      limit[nt] = col < cols ? min(rq.len, rq.want - rq.m + i + 1) : some;
-      const T* src = reinterpret_cast<const T*>(p.q + (int64_t)(rq.row + i) * p.q_stride) +
-                     (int64_t)(kvh * g + gc - i * g) * D + q * (D / 4);
-#pragma unroll
-      for (int s = 0; s < W; ++s)
-#pragma unroll
-        for (int e = 0; e < QV; ++e) qraw[nt][s][e] = reinterpret_cast<const f32x4_a4*>(src + 8 * s)[e];
+    const uint32_t u0 = st.begin(w), u1 = st.begin(w + 1);
+    uint32_t base = begin_of(1);
+    rq = per == 1 ? make_request<COLS, UNIT>(p, begin_of(2), begin_of(3), begin_of(4)) : get_request<COLS, UNIT>(p, r);
+    while (u0 - base >= rq.units() && r + 1 < p.R) {
+      base += rq.units();
+      rq = get_request<COLS, UNIT>(p, ++r);
     }
 
-    // the ring.  Entries are waited for where they are loaded, not at every use: that
-    // would wait for the ring's loads too.
-    asm volatile("" : "+v"(tab));
-    auto entries = [&](int b0) {
-      int e = b0 + lane < p.max_blocks ? table[b0 + lane] : -1;
-      asm volatile("" : "+v"(e));
-      return e;
-    };
-    const int last = stop * TILES;
-    int put = 0, get = 0;   // bytes into the ring
-    bool broken = false;    // a block is not in the arena
-    auto issue = [&]() {
-      if (bi - window >= 64) {
-        window = bi;
-        tab = entries(bi);
-      }
-      const int e = __builtin_amdgcn_readlane(tab, bi - window);
-      const bool in = (uint32_t)e < p.num_blocks;
-      broken |= !in;
-      const char* rec = head + (in ? e : 0) * block_bytes + ti * REC;
-      constexpr int FULL = 16 * D / 1024;
-#pragma unroll
-      for (int i = 0; i < FULL; ++i) load_lds(rec, REC, ring + put + 1024 * i, lane * 16, 1024 * i);
-      if (FULL == 0 && lane < D) load_lds(rec, REC, ring + put, lane * 16, 0);
-      if (lane < D / 16) load_lds(rec, REC, ring + put + 16 * D, lane * 16, 16 * D);
-      put = put == (RING - 1) * REC ? 0 : put + REC;
-      ++next;
-      if (++ti == tpb) {
-        ti = 0;
-        ++bi;
-      }
-    };
-#pragma unroll 1
-    for (int i = 0; i < RING && next < last; ++i) issue();
+    const int B = p.packed.block_size, tpb = B / PK_TILE;
+    const float scale_log2 = 1.4426950408889634f / sqrtf((float)D);
+    const char* head = p.packed.base + (int64_t)kvh * tpb * (17 * D);
+    const int64_t block_bytes = (int64_t)nkv * tpb * (17 * D);
+    char* const ring = s_ring[wave];
+    const int k_off = c * (D / 2) + q * (D / 8), v_off = 8 * D + q * (2 * D) + c * (D / 8);
+    const int ks_off = 16 * D + c * (D / 32) + q * D / 128, vs_off = 16 * D + D / 2 + q * (D / 8) + c * D / 512 * 4;
+    const int copy = c / (16 / COPIES);  // whose tile the lane's column scores
 
-    bf16x8 qf[NT][QP][W];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      const bool used = (COPIES == 1 ? nt * 16 + c : c % (16 / COPIES)) < cols;
-#pragma unroll
-      for (int s = 0; s < W; ++s) {
-        if constexpr (QP == 1) {
-          qf[nt][0][s] = used ? __builtin_bit_cast(bf16x8, qraw[nt][s][0]) : bf16x8{};
-        } else {
-          float x[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] = used ? qraw[nt][s][e / 4 % QV][e % 4] : 0.0f;
-#pragma unroll
-          for (int part = 0; part < QP; ++part) {
-            union { uint32_t w[4]; bf16x8 f; } f;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              f.w[e] = pack_bf16(x[2 * e], x[2 * e + 1]);
-              x[2 * e] -= __uint_as_float(f.w[e] << 16);
-              x[2 * e + 1] -= __uint_as_float(f.w[e] & 0xffff0000u);
-            }
-            qf[nt][part][s] = f.f;
-          }
-        }
-      }
-    }
-    float m_run[NT], l_run[NT];
-    f32x4 o[NT][DT];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      m_run[nt] = -INFINITY;
-      l_run[nt] = 0.0f;
-#pragma unroll
-      for (int j = 0; j < DT; ++j) o[nt][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    }
+    for (uint32_t u = u0; u < u1;) {
+      // ---- the stretch's part of one item ----
+      const int tile = (int)quotient(u - base, rq.steps), first = (int)(u - base) - tile * rq.steps;
+      const int upto = (int)min((uint32_t)rq.steps, first + (u1 - u));
+      const int cols = min(COLS, rq.m * g - tile * COLS);  // of this tile
+      if (cols <= 0) break;  // offsets that overlap so far that the units passed 2^32
+      // positions that every column sees, and that any does
+      const int i_lo = by_g(p, tile * COLS), i_hi = by_g(p, tile * COLS + cols - 1);
+      const int all = min(rq.len, rq.want - rq.m + i_lo + 1), some = min(rq.len, rq.want - rq.m + i_hi + 1);
+      const int stop = min(upto, (max(some, 0) + UNIT - 1) / UNIT);
 
-    for (int kt = first; kt < stop; ++kt) {
-      // this unit's records have landed; of those behind it, RING - TILES at most are on their way
-      const int behind = next - (kt + 1) * TILES;
-      if (behind >= RING - TILES) KVR_WAIT_VMCNT((RING - TILES) * LOADS);
-      else if (RING - TILES > TILES && behind >= RING - 2 * TILES) KVR_WAIT_VMCNT((RING - 2 * TILES) * LOADS);
-      else KVR_WAIT_VMCNT(0);
-      asm volatile("" ::: "memory");  // the reads below stay below
-      // record x of the unit: TILES divides the ring into whole units
-      auto at = [&](int x) { return ring + get + x * REC; };
-      const bool whole = (int64_t)(kt + 1) * UNIT <= all && !broken;
-      // scores
-      uint32_t kw[TILES][W], ks[TILES];
-#pragma unroll
-      for (int x = 0; x < TILES; ++x) {
-        load_words<D / 8>(at(x) + k_off, kw[x]);
-        ks[x] = (uint8_t)at(x)[ks_off];
-      }
-      f32x4 st[NT][TILES];
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int x = 0; x < TILES; ++x) st[nt][x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-      for (int s = 0; s < W; ++s)
-#pragma unroll
-        for (int x = 0; x < TILES; ++x) {
-          const float scale = scale_of(ks[x], 0);
-          union { uint32_t w[4]; bf16x8 f; } kf;
-          kf.w[0] = pair_of<0>(kw[x][s], scale);
-          kf.w[1] = pair_of<1>(kw[x][s], scale);
-          kf.w[2] = pair_of<2>(kw[x][s], scale);
-          kf.w[3] = pair_of<3>(kw[x][s], scale);
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int part = 0; part < QP; ++part)
-              st[nt][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf.f, qf[nt][part][s], st[nt][x], 0, 0, 0);
-        }
-      float sc[NT][NV];
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int x = 0; x < TILES; ++x)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            if (COPIES == 1) sc[nt][4 * x + j] = st[nt][x][j];
-            else sc[nt][j] = x == 0 || copy == x ? st[nt][x][j] : sc[nt][j];
-          }
-      // the lane's first position of the unit's first tile, and of its column's tile
-      const int p0 = kt * UNIT + 4 * q, c0 = p0 + (COPIES == 1 ? 0 : 16 * copy);
-      uint32_t vw[TILES][W], vs[TILES];
-#pragma unroll
-      for (int x = 0; x < TILES; ++x) {
-        load_words<D / 8>(at(x) + v_off, vw[x]);
-        vs[x] = *reinterpret_cast<const uint32_t*>(at(x) + vs_off);
-      }
-      bool nan_v = false;
-      if (!whole) {
-        // positions past a column's limit and in blocks that are not there leave its
-        // softmax; V there may hold any bits, and 0 times them is not 0
-        int in = (1 << TILES) - 1;  // the unit's tiles whose blocks are in the arena
-        if (broken) {
-          in = 0;
-#pragma unroll 1
-          for (int x = 0; x < TILES; ++x) {
-            const int b = (kt * TILES + x) / tpb;
-            in |= (int)(b < p.max_blocks && (uint32_t)table[b] < p.num_blocks) << x;
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-          const bool gone = !(in >> (COPIES == 1 ? i / 4 : copy) & 1);
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-            if (gone || c0 + 16 * (i / 4) + i % 4 >= limit[nt]) sc[nt][i] = -INFINITY;
-        }
-        uint32_t nan = 0;
-#pragma unroll
-        for (int x = 0; x < TILES; ++x) {
-          const int n = in >> x & 1 ? some - (p0 + 16 * x) : 0;  // of the lane's four positions
-          constexpr int KB = D / 32;                             // bytes of one
-#pragma unroll
-          for (int i = 0; i < W; ++i) vw[x][i] &= first_bytes(min(n, 4) * KB - 4 * i);
-          vs[x] &= first_bytes(n);
-          nan |= nan_bytes(vs[x]) & ~first_bytes(all - (p0 + 16 * x));  // seen by some columns only
-        }
-        nan_v = nan != 0;
-      }
-      // weights
-      uint32_t pw[NT][PP][NV / 2];
+      // 64 table entries, one a lane, and the queries: on their way ahead of the records
+      const int32_t* table = p.tables + (int64_t)r * p.max_blocks;
+      int next = first * TILES, bi = next / tpb, ti = next - bi * tpb;  // the next record, its block and place in it
+      int window = bi, tab = bi + lane < p.max_blocks ? table[bi + lane] : -1;
+      constexpr int QV = 8 * (int)sizeof(T) / 16;  // 16-byte pieces of eight dims
+      f32x4 qraw[NT][W][QV];
+      int limit[NT];  // positions the lane's column sees
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        float mx = -INFINITY;
+        const int col = COPIES == 1 ? nt * 16 + c : c % (16 / COPIES);
+        const int gc = tile * COLS + min(col, cols - 1), i = by_g(p, gc);
+        limit[nt] = col < cols ? min(rq.len, rq.want - rq.m + i + 1) : some;
+        const T* src = reinterpret_cast<const T*>(p.q + (int64_t)(rq.row + i) * p.q_stride) +
+                       (int64_t)(kvh * g + gc - i * g) * D + q * (D / 4);
 #pragma unroll
-        for (int i = 0; i < NV; ++i) mx = fmaxf(mx, sc[nt][i]);
-        mx *= scale_log2;
-        mx = max_over_q(mx);
-        if (__any(mx > m_run[nt] + SLACK)) {
-          const float m_new = fmaxf(m_run[nt], mx);
-          const float alpha = m_new == m_run[nt] ? 1.0f : __builtin_amdgcn_exp2f(m_run[nt] - m_new);
-          l_run[nt] *= alpha;
-          m_run[nt] = m_new;
+        for (int s = 0; s < W; ++s)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float f = __shfl(alpha, 4 * q + j, 64);  // column 4q + j's
-#pragma unroll
-            for (int d = 0; d < DT; ++d) o[nt][d][j] *= f;
-          }
-        }
-        // a column that has seen nothing yet: weights of 0
-        const float m = m_run[nt] == -INFINITY ? 0.0f : m_run[nt];
-        float e[NV];
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-          e[i] = __builtin_amdgcn_exp2f(fmaf(sc[nt][i], scale_log2, -m));
-          l_run[nt] += e[i];
-        }
-#pragma unroll
-        for (int part = 0; part < PP; ++part)
-#pragma unroll
-          for (int i = 0; i < NV / 2; ++i) {
-            pw[nt][part][i] = pack_bf16(e[2 * i], e[2 * i + 1]);
-            e[2 * i] -= __uint_as_float(pw[nt][part][i] << 16);
-            e[2 * i + 1] -= __uint_as_float(pw[nt][part][i] & 0xffff0000u);
-          }
+          for (int e = 0; e < QV; ++e) qraw[nt][s][e] = reinterpret_cast<const f32x4_a4*>(src + 8 * s)[e];
       }
-      // a lane's words of its own tiles as the A operand of tiles 2y and 2y + 1
-      auto operand = [&](const uint32_t* own, int y) {
-        if constexpr (COPIES == 1) {
-          return __builtin_bit_cast(bf16x8, make_uint4(own[0], own[1], own[2], own[3]));
-        } else {
-          const bool lo = copy == 2 * y, hi = copy == 2 * y + 1;
-          return __builtin_bit_cast(bf16x8, make_uint4(lo ? own[0] : 0u, lo ? own[1] : 0u, hi ? own[0] : 0u,
-                                                       hi ? own[1] : 0u));
+
+      // the ring.  Entries are waited for where they are loaded, not at every use: that
+      // would wait for the ring's loads too.
+      asm volatile("" : "+v"(tab));
+      auto entries = [&](int b0) {
+        int e = b0 + lane < p.max_blocks ? table[b0 + lane] : -1;
+        asm volatile("" : "+v"(e));
+        return e;
+      };
+      const int last = stop * TILES;
+      int put = 0, get = 0;   // bytes into the ring
+      bool broken = false;    // a block is not in the arena
+      auto issue = [&]() {
+        if (bi - window >= 64) {
+          window = bi;
+          tab = entries(bi);
+        }
+        const int e = __builtin_amdgcn_readlane(tab, bi - window);
+        const bool in = (uint32_t)e < p.num_blocks;
+        broken |= !in;
+        const char* rec = head + (in ? e : 0) * block_bytes + ti * REC;
+        constexpr int FULL = 16 * D / 1024;
+#pragma unroll
+        for (int i = 0; i < FULL; ++i) load_lds(rec, REC, ring + put + 1024 * i, lane * 16, 1024 * i);
+        if (FULL == 0 && lane < D) load_lds(rec, REC, ring + put, lane * 16, 0);
+        if (lane < D / 16) load_lds(rec, REC, ring + put + 16 * D, lane * 16, 16 * D);
+        put = put == (RING - 1) * REC ? 0 : put + REC;
+        ++next;
+        if (++ti == tpb) {
+          ti = 0;
+          ++bi;
         }
       };
-      if (!whole && __any(nan_v)) {
-        // A NaN of V that some columns see and some do not: a product of ones counts,
-        // for each column and dim, the NaN it sees; then V is 0 there.
+#pragma unroll 1
+      for (int i = 0; i < RING && next < last; ++i) issue();
+
+      bf16x8 qf[NT][QP][W];
 #pragma unroll
-        for (int y = 0; y < TILES / 2; ++y) {
-          uint32_t ind[4];
+      for (int nt = 0; nt < NT; ++nt) {
+        const bool used = (COPIES == 1 ? nt * 16 + c : c % (16 / COPIES)) < cols;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint32_t two = nan_bytes(vs[2 * y + i / 2]) >> (16 * (i % 2));  // of two positions
-            ind[i] = (two & 1) * 0x3f80u | (two >> 8 & 1) * 0x3f800000u;
-          }
-          const bf16x8 nf = __builtin_bit_cast(bf16x8, make_uint4(ind[0], ind[1], ind[2], ind[3]));
+        for (int s = 0; s < W; ++s) {
+          if constexpr (QP == 1) {
+            qf[nt][0][s] = used ? __builtin_bit_cast(bf16x8, qraw[nt][s][0]) : bf16x8{};
+          } else {
+            float x[8];
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            uint32_t seen[NV / 2];
+            for (int e = 0; e < 8; ++e) x[e] = used ? qraw[nt][s][e / 4 % QV][e % 4] : 0.0f;
 #pragma unroll
-            for (int i = 0; i < NV / 2; ++i) {
-              const int pos = c0 + 16 * (i / 2) + 2 * (i % 2);
-              seen[i] = (pos < limit[nt] ? 0x3f80u : 0u) | (pos + 1 < limit[nt] ? 0x3f800000u : 0u);
+            for (int part = 0; part < QP; ++part) {
+              union { uint32_t w[4]; bf16x8 f; } f;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                f.w[e] = pack_bf16(x[2 * e], x[2 * e + 1]);
+                x[2 * e] -= __uint_as_float(f.w[e] << 16);
+                x[2 * e + 1] -= __uint_as_float(f.w[e] & 0xffff0000u);
+              }
+              qf[nt][part][s] = f.f;
             }
-            const f32x4 hits =
-                __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(seen, y), nf, f32x4{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const float add = hits[j] > 0.0f ? __builtin_nanf("") : 0.0f;
-#pragma unroll
-              for (int d = 0; d < DT; ++d) o[nt][d][j] += add;
-            }
-          }
-        }
-#pragma unroll
-        for (int x = 0; x < TILES; ++x) {
-          const uint32_t gone = nan_bytes(vs[x]) * 255u;
-          vs[x] &= ~gone;
-#pragma unroll
-          for (int i = 0; i < W; ++i) {
-            uint32_t bytes = 0;  // of word i, those of positions that are gone
-#pragma unroll
-            for (int y = 0; y < 4; ++y) bytes |= (gone >> (8 * ((4 * i + y) / (D / 32))) & 255u) << (8 * y);
-            vw[x][i] &= ~bytes;
           }
         }
       }
-      // O += P V
+      float m_run[NT], l_run[NT];
+      f32x4 o[NT][DT];
 #pragma unroll
-      for (int y = 0; y < TILES / 2; ++y) {
-        bf16x8 pf[NT][PP];
+      for (int nt = 0; nt < NT; ++nt) {
+        m_run[nt] = -INFINITY;
+        l_run[nt] = 0.0f;
+#pragma unroll
+        for (int j = 0; j < DT; ++j) o[nt][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      }
+
+      for (int kt = first; kt < stop; ++kt) {
+        // this unit's records have landed; of those behind it, RING - TILES at most are on their way
+        const int behind = next - (kt + 1) * TILES;
+        if (behind >= RING - TILES) KVR_WAIT_VMCNT((RING - TILES) * LOADS);
+        else if (RING - TILES > TILES && behind >= RING - 2 * TILES) KVR_WAIT_VMCNT((RING - 2 * TILES) * LOADS);
+        else KVR_WAIT_VMCNT(0);
+        asm volatile("" ::: "memory");  // the reads below stay below
+        // record x of the unit: TILES divides the ring into whole units
+        auto at = [&](int x) { return ring + get + x * REC; };
+        const bool whole = (int64_t)(kt + 1) * UNIT <= all && !broken;
+        // scores
+        uint32_t kw[TILES][W], ks[TILES];
+#pragma unroll
+        for (int x = 0; x < TILES; ++x) {
+          load_words<D / 8>(at(x) + k_off, kw[x]);
+          ks[x] = (uint8_t)at(x)[ks_off];
+        }
+        f32x4 st[NT][TILES];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int part = 0; part < PP; ++part) pf[nt][part] = operand(pw[nt][part], y);
-        static_for<DT / 2>([&](auto DS) {
-          constexpr int s = DS;  // dims 2s and 2s + 1 of the lane
-          uint32_t pr[8];
-          static_for<8>([&](auto I) {
-            constexpr int i = I, byte = i % 4 * (D / 32) + s;
-            pr[i] = pair_of<byte % 4>(vw[2 * y + i / 4][byte / 4], scale_of(vs[2 * y + i / 4], i % 4));
-          });
-          union { uint32_t w[4]; bf16x8 f; } lo, hi;
+          for (int x = 0; x < TILES; ++x) st[nt][x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            lo.w[i] = __builtin_amdgcn_perm(pr[2 * i + 1], pr[2 * i], 0x05040100u);
-            hi.w[i] = __builtin_amdgcn_perm(pr[2 * i + 1], pr[2 * i], 0x07060302u);
+        for (int s = 0; s < W; ++s)
+#pragma unroll
+          for (int x = 0; x < TILES; ++x) {
+            const float scale = scale_of(ks[x], 0);
+            union { uint32_t w[4]; bf16x8 f; } kf;
+            kf.w[0] = pair_of<0>(kw[x][s], scale);
+            kf.w[1] = pair_of<1>(kw[x][s], scale);
+            kf.w[2] = pair_of<2>(kw[x][s], scale);
+            kf.w[3] = pair_of<3>(kw[x][s], scale);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int part = 0; part < QP; ++part)
+                st[nt][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf.f, qf[nt][part][s], st[nt][x], 0, 0, 0);
           }
+        float sc[NT][NV];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int x = 0; x < TILES; ++x)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              if (COPIES == 1) sc[nt][4 * x + j] = st[nt][x][j];
+              else sc[nt][j] = x == 0 || copy == x ? st[nt][x][j] : sc[nt][j];
+            }
+        // the lane's first position of the unit's first tile, and of its column's tile
+        const int p0 = kt * UNIT + 4 * q, c0 = p0 + (COPIES == 1 ? 0 : 16 * copy);
+        uint32_t vw[TILES][W], vs[TILES];
+#pragma unroll
+        for (int x = 0; x < TILES; ++x) {
+          load_words<D / 8>(at(x) + v_off, vw[x]);
+          vs[x] = *reinterpret_cast<const uint32_t*>(at(x) + vs_off);
+        }
+        bool nan_v = false;
+        if (!whole) {
+          // positions past a column's limit and in blocks that are not there leave its
+          // softmax; V there may hold any bits, and 0 times them is not 0
+          int in = (1 << TILES) - 1;  // the unit's tiles whose blocks are in the arena
+          if (broken) {
+            in = 0;
+#pragma unroll 1
+            for (int x = 0; x < TILES; ++x) {
+              const int b = (kt * TILES + x) / tpb;
+              in |= (int)(b < p.max_blocks && (uint32_t)table[b] < p.num_blocks) << x;
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < NV; ++i) {
+            const bool gone = !(in >> (COPIES == 1 ? i / 4 : copy) & 1);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+              if (gone || c0 + 16 * (i / 4) + i % 4 >= limit[nt]) sc[nt][i] = -INFINITY;
+          }
+          uint32_t nan = 0;
+#pragma unroll
+          for (int x = 0; x < TILES; ++x) {
+            const int n = in >> x & 1 ? some - (p0 + 16 * x) : 0;  // of the lane's four positions
+            constexpr int KB = D / 32;                             // bytes of one
+#pragma unroll
+            for (int i = 0; i < W; ++i) vw[x][i] &= first_bytes(min(n, 4) * KB - 4 * i);
+            vs[x] &= first_bytes(n);
+            nan |= nan_bytes(vs[x]) & ~first_bytes(all - (p0 + 16 * x));  // seen by some columns only
+          }
+          nan_v = nan != 0;
+        }
+        // weights
+        uint32_t pw[NT][PP][NV / 2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          float mx = -INFINITY;
+#pragma unroll
+          for (int i = 0; i < NV; ++i) mx = fmaxf(mx, sc[nt][i]);
+          mx *= scale_log2;
+          mx = max_over_q(mx);
+          if (__any(mx > m_run[nt] + SLACK)) {
+            const float m_new = fmaxf(m_run[nt], mx);
+            const float alpha = m_new == m_run[nt] ? 1.0f : __builtin_amdgcn_exp2f(m_run[nt] - m_new);
+            l_run[nt] *= alpha;
+            m_run[nt] = m_new;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float f = __shfl(alpha, 4 * q + j, 64);  // column 4q + j's
+#pragma unroll
+              for (int d = 0; d < DT; ++d) o[nt][d][j] *= f;
+            }
+          }
+          // a column that has seen nothing yet: weights of 0
+          const float m = m_run[nt] == -INFINITY ? 0.0f : m_run[nt];
+          float e[NV];
+#pragma unroll
+          for (int i = 0; i < NV; ++i) {
+            e[i] = __builtin_amdgcn_exp2f(fmaf(sc[nt][i], scale_log2, -m));
+            l_run[nt] += e[i];
+          }
+#pragma unroll
+          for (int part = 0; part < PP; ++part)
+#pragma unroll
+            for (int i = 0; i < NV / 2; ++i) {
+              pw[nt][part][i] = pack_bf16(e[2 * i], e[2 * i + 1]);
+              e[2 * i] -= __uint_as_float(pw[nt][part][i] << 16);
+              e[2 * i + 1] -= __uint_as_float(pw[nt][part][i] & 0xffff0000u);
+            }
+        }
+        // a lane's words of its own tiles as the A operand of tiles 2y and 2y + 1
+        auto operand = [&](const uint32_t* own, int y) {
+          if constexpr (COPIES == 1) {
+            return __builtin_bit_cast(bf16x8, make_uint4(own[0], own[1], own[2], own[3]));
+          } else {
+            const bool lo = copy == 2 * y, hi = copy == 2 * y + 1;
+            return __builtin_bit_cast(bf16x8, make_uint4(lo ? own[0] : 0u, lo ? own[1] : 0u, hi ? own[0] : 0u,
+                                                         hi ? own[1] : 0u));
+          }
+        };
+        if (!whole && __any(nan_v)) {
+          // A NaN of V that some columns see and some do not: a product of ones counts,
+          // for each column and dim, the NaN it sees; then V is 0 there.
+#pragma unroll
+          for (int y = 0; y < TILES / 2; ++y) {
+            uint32_t ind[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const uint32_t two = nan_bytes(vs[2 * y + i / 2]) >> (16 * (i % 2));  // of two positions
+              ind[i] = (two & 1) * 0x3f80u | (two >> 8 & 1) * 0x3f800000u;
+            }
+            const bf16x8 nf = __builtin_bit_cast(bf16x8, make_uint4(ind[0], ind[1], ind[2], ind[3]));
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              uint32_t seen[NV / 2];
+#pragma unroll
+              for (int i = 0; i < NV / 2; ++i) {
+                const int pos = c0 + 16 * (i / 2) + 2 * (i % 2);
+                seen[i] = (pos < limit[nt] ? 0x3f80u : 0u) | (pos + 1 < limit[nt] ? 0x3f800000u : 0u);
+              }
+              const f32x4 hits =
+                  __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(seen, y), nf, f32x4{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const float add = hits[j] > 0.0f ? __builtin_nanf("") : 0.0f;
+#pragma unroll
+                for (int d = 0; d < DT; ++d) o[nt][d][j] += add;
+              }
+            }
+          }
+#pragma unroll
+          for (int x = 0; x < TILES; ++x) {
+            const uint32_t gone = nan_bytes(vs[x]) * 255u;
+            vs[x] &= ~gone;
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+              uint32_t bytes = 0;  // of word i, those of positions that are gone
+#pragma unroll
+              for (int y = 0; y < 4; ++y) bytes |= (gone >> (8 * ((4 * i + y) / (D / 32))) & 255u) << (8 * y);
+              vw[x][i] &= ~bytes;
+            }
+          }
+        }
+        // O += P V
+#pragma unroll
+        for (int y = 0; y < TILES / 2; ++y) {
+          bf16x8 pf[NT][PP];
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int part = 0; part < PP; ++part) {
-              o[nt][2 * s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pf[nt][part], lo.f, o[nt][2 * s], 0, 0, 0);
-              o[nt][2 * s + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pf[nt][part], hi.f, o[nt][2 * s + 1], 0, 0, 0);
+            for (int part = 0; part < PP; ++part) pf[nt][part] = operand(pw[nt][part], y);
+          static_for<DT / 2>([&](auto DS) {
+            constexpr int s = DS;  // dims 2s and 2s + 1 of the lane
+            uint32_t pr[8];
+            static_for<8>([&](auto I) {
+              constexpr int i = I, byte = i % 4 * (D / 32) + s;
+              pr[i] = pair_of<byte % 4>(vw[2 * y + i / 4][byte / 4], scale_of(vs[2 * y + i / 4], i % 4));
+            });
+            union { uint32_t w[4]; bf16x8 f; } lo, hi;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              lo.w[i] = __builtin_amdgcn_perm(pr[2 * i + 1], pr[2 * i], 0x05040100u);
+              hi.w[i] = __builtin_amdgcn_perm(pr[2 * i + 1], pr[2 * i], 0x07060302u);
             }
-        });
-      }
-      KVR_WAIT_LGKM0();  // the unit's records are in registers: the ring takes the next ones
-      asm volatile("" ::: "memory");
-      get = get == (RING - TILES) * REC ? 0 : get + TILES * REC;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int part = 0; part < PP; ++part) {
+                o[nt][2 * s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pf[nt][part], lo.f, o[nt][2 * s], 0, 0, 0);
+                o[nt][2 * s + 1] =
+                    __builtin_amdgcn_mfma_f32_16x16x32_bf16(pf[nt][part], hi.f, o[nt][2 * s + 1], 0, 0, 0);
+              }
+          });
+        }
+        KVR_WAIT_LGKM0();  // the unit's records are in registers: the ring takes the next ones
+        asm volatile("" ::: "memory");
+        get = get == (RING - TILES) * REC ? 0 : get + TILES * REC;
 #pragma unroll 1
-      for (int x = 0; x < TILES && next < last; ++x) issue();
-    }
+        for (int x = 0; x < TILES && next < last; ++x) issue();
+      }
 
-    // ---- the columns' outputs, or what there is of them ----
-    // 16 rows at a time through the ring, a row's dims over the lanes; the copies of a
-    // column are merged on the way.  What stays open goes to the workspace, or at the
-    // stretch's end, where the ring has no more to take, stays where it is.
-    const bool done = first == 0 && upto == rq.steps, stay = LOCAL && u + upto - first >= u1;
-    float* const rows = reinterpret_cast<float*>(ring);
-    float* const part = stay ? rows : slots + (first > 0 ? 0 : 1) * p.part_cols * (D + 2);
+      // ---- the columns' outputs, or what there is of them ----
+      // 16 rows at a time through the ring, a row's dims over the lanes; the copies of a
+      // column are merged on the way.  What stays open goes to the workspace, or at the
+      // stretch's end, where the ring has no more to take, stays where it is.
+      const bool done = first == 0 && upto == rq.steps, stay = LOCAL && u + upto - first >= u1;
+      float* const rows = reinterpret_cast<float*>(ring);
+      float* const part = stay ? rows : slots + (first > 0 ? 0 : 1) * p.part_cols * (D + 2);
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      float* const tr = rows + (LOCAL ? nt : 0) * 16 * (D + 2);
-      float l = l_run[nt] + __shfl_xor(l_run[nt], 16, 64);
-      l += __shfl_xor(l, 32, 64);
-      if (q == 0) {
-        tr[c * (D + 2) + D] = m_run[nt];
-        tr[c * (D + 2) + D + 1] = l;
-      }
+      for (int nt = 0; nt < NT; ++nt) {
+        float* const tr = rows + (LOCAL ? nt : 0) * 16 * (D + 2);
+        float l = l_run[nt] + __shfl_xor(l_run[nt], 16, 64);
+        l += __shfl_xor(l, 32, 64);
+        if (q == 0) {
+          tr[c * (D + 2) + D] = m_run[nt];
+          tr[c * (D + 2) + D + 1] = l;
+        }
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < 4; ++j)
 #pragma unroll
-        for (int d = 0; d < DT; ++d) tr[(4 * q + j) * (D + 2) + c * DT + d] = o[nt][d][j];
-      asm volatile("" ::: "memory");
-      const int used = COPIES == 1 && stay && !done ? 0 : min(16 / COPIES, cols - nt * 16);  // 0: the rows are the partials
+          for (int d = 0; d < DT; ++d) tr[(4 * q + j) * (D + 2) + c * DT + d] = o[nt][d][j];
+        asm volatile("" ::: "memory");
+        // 0: the rows are the partials
+        const int used = COPIES == 1 && stay && !done ? 0 : min(16 / COPIES, cols - nt * 16);
 #pragma unroll 1
-      for (int i0 = 0; i0 < used; i0 += AT_ONCE<D>) {
-        const int i = i0 + lane / LANES<D>;
-        if (i >= used) continue;
-        const Column v = merge_column<D, COPIES>(
-            [&](int k, auto load) { load(tr + (k * (16 / COPIES) + i) * (D + 2)); }, COPIES, lane);
-        if (done) put_out<T, D, COLS>(p, rq.row, tile, nt * 16 + i, kvh, lane, v);
-        else put_part<D>(part + (nt * 16 + i) * (D + 2), lane, v);
+        for (int i0 = 0; i0 < used; i0 += AT_ONCE<D>) {
+          const int i = i0 + lane / LANES<D>;
+          if (i >= used) continue;
+          const Column v = merge_column<D, COPIES>(
+              [&](int k, auto load) { load(tr + (k * (16 / COPIES) + i) * (D + 2)); }, COPIES, lane);
+          if (done) put_out<T, D, COLS>(p, rq.row, tile, nt * 16 + i, kvh, lane, v);
+          else put_part<D>(part + (nt * 16 + i) * (D + 2), lane, v);
+        }
+        KVR_WAIT_LGKM0();  // the rows have been read: the ring may be filled again
+        asm volatile("" ::: "memory");
       }
-      KVR_WAIT_LGKM0();  // the rows have been read: the ring may be filled again
-      asm volatile("" ::: "memory");
-    }
-    if (!done && lane == 0) {
-      Stretch& me = s_str[wave];
-      const int which = first > 0 ? 0 : 1;
-      me.cols[which] = cols;
-      me.row[which] = rq.row;
-      me.tile[which] = tile;
-      me.flags |= (stay ? 2 << which : 0) | (first > 0 && upto == rq.steps ? 1 : 0);
-      if (first == 0) me.end = base + (uint32_t)(tile + 1) * rq.steps;
-    }
-    u += upto - first;
-    if (u < u1)
-      while (u - base >= rq.units() && r + 1 < p.R) {
-        base += rq.units();
-        rq = get_request<COLS, UNIT>(p, ++r);
+      if (!done && lane == 0) {
+        Stretch& me = s_str[wave];
+        const int which = first > 0 ? 0 : 1;
+        me.cols[which] = cols;
+        me.row[which] = rq.row;
+        me.tile[which] = tile;
+        me.flags |= (stay ? 2 << which : 0) | (first > 0 && upto == rq.steps ? 1 : 0);
+        if (first == 0) me.end = base + (uint32_t)(tile + 1) * rq.steps;
       }
-  }
+      u += upto - first;
+      if (u < u1)
+        while (u - base >= rq.units() && r + 1 < p.R) {
+          base += rq.units();
+          rq = get_request<COLS, UNIT>(p, ++r);
+        }
+    }
   }
 
   // ---- the workgroup's own merges: an item begun before it, and those its waves left
@@ -753,8 +772,8 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
     int n = 1;
     bool closed = lead < 0 && (ended & 1);
     while (!closed && at + n < WAVES && begun >> (at + n) & 1) closed = ended >> (at + n++) & 1;
-    const int cols = __builtin_amdgcn_readlane(str.cols[which], at), row = __builtin_amdgcn_readlane(str.row[which], at);
-    const int tile = __builtin_amdgcn_readlane(str.tile[which], at);
+    const int cols = __builtin_amdgcn_readlane(str.cols[which], at);
+    const int row = __builtin_amdgcn_readlane(str.row[which], at), tile = __builtin_amdgcn_readlane(str.tile[which], at);
     closed &= lead >= 0;  // all of the item is here
     float* slot = slots0 + at * pitch + which * p.part_cols * (D + 2);
     if (lead >= 0 && !closed) open = OpenItem{cols, row, tile, at, 0};
@@ -807,7 +826,8 @@ __global__ __launch_bounds__(PM_NT) void packed_attn_merge_kernel(PackedAttnPara
       put_out<T, D, S::COLS>(
           p, it.row, it.tile, col, kvh, lane,
           merge_column<D, chunk>(
-              [&](int i, auto load) { load((i == 0 ? lead : first + i * WG * pitch) + col * (D + 2)); }, it.groups, lane));
+              [&](int i, auto load) { load((i == 0 ? lead : first + i * WG * pitch) + col * (D + 2)); }, it.groups,
+              lane));
     }
   };
   if (it.groups <= 4) merge(std::integral_constant<int, 4>{});
@@ -896,7 +916,6 @@ void run(const kv_packed* packed, int32_t layer, const void* q, int64_t q_stride
   p.tables = tables;
   p.R = R;
   p.max_blocks = max_blocks;
-  p.nq = d.num_q_heads;
   p.g = d.num_q_heads / d.num_kv_heads;
   p.g_inv = p.g == 1 ? 0 : (uint32_t)(((1ull << 32) + p.g - 1) / p.g);
   const AttnLayout L = attn_layout(d, R, rows, max_query, max_len);
@@ -926,7 +945,9 @@ extern "C" {
 uint64_t kv_packed_attention_workspace_bytes(const kv_model_desc* desc, int32_t num_requests, int64_t rows,
                                              int32_t max_query, int64_t max_len) {
   if (kv_packed_bytes(desc, PK_TILE, 1) == 0 || desc->num_q_heads / desc->num_kv_heads > 16) return 0;
-  if (num_requests <= 0 || rows <= 0 || max_query <= 0 || max_len <= 0) return 0;
+  if (num_requests <= 0 || num_requests > MOST_ROWS || rows <= 0 || rows > MOST_ROWS || max_query <= 0 ||
+      max_len <= 0 || max_len > INT32_MAX)
+    return 0;
   return attn_layout(*desc, num_requests, rows, max_query, max_len).total;
 }
 
@@ -941,12 +962,13 @@ kv_status kv_packed_attention(kv_packed_t packed, int32_t layer, const void* q, 
     return kvr_err::set(KV_EINVAL, "packed attention supports at most 16 q heads per kv head");
   if (layer < 0 || layer >= d.num_layers)
     return kvr_err::set(KV_EINVAL, "layer %d outside [0, %d)", layer, d.num_layers);
-  if (R < 0 || rows < 0 || rows > (1 << 24) || max_blocks < 0)
-    return kvr_err::set(KV_EINVAL, "num_requests and max_blocks_per_req are 0 .. 2^31 - 1, rows 0 .. 2^24");
+  if (R < 0 || R > MOST_ROWS || rows < 0 || rows > MOST_ROWS || max_blocks < 0)
+    return kvr_err::set(KV_EINVAL, "num_requests and rows are 0 .. 2^24, max_blocks_per_req is not negative");
   if (!q_offsets && rows != R) return kvr_err::set(KV_EINVAL, "without q_offsets rows must equal num_requests");
   if (R == 0 || rows == 0) return kvr_err::clear();
   if (max_query < 1 || max_len < 1) return kvr_err::set(KV_EINVAL, "max_query and max_len must be positive");
-  if (!q || !out || !lens || (max_blocks > 0 && !tables)) return kvr_err::set(KV_EINVAL, "null q, out, lens or block_tables");
+  if (!q || !out || !lens || (max_blocks > 0 && !tables))
+    return kvr_err::set(KV_EINVAL, "null q, out, lens or block_tables");
   if (q_stride < row || out_stride < row)
     return kvr_err::set(KV_EINVAL, "a stride is below the row's %lld elements", (long long)row);
   if (((uintptr_t)q | (uintptr_t)out | (uintptr_t)(q_stride * e) | (uintptr_t)(out_stride * e) | (uintptr_t)q_offsets |

@@ -63,7 +63,8 @@ __global__ __launch_bounds__(TG_NT) void tables_grow_kernel(GrowParams p) {
   __shared__ int s_unplaced;
   const int t = threadIdx.x, lane = t & 63, w = t >> 6;
   const uint32_t B = (uint32_t)p.B;
-  // n / B: a shift where B is a power of two (a division by a number known only here is some twenty instructions)
+  // n / B: a shift where B is a power of two (a division by a number known only here is
+  // some twenty instructions)
   const auto blocks_of = [&](uint32_t n) { return p.shift >= 0 ? n >> p.shift : n / B; };
   int unplaced = 0;
   if (t == 0) s_unplaced = 0;
@@ -221,8 +222,8 @@ extern "C" kv_status kv_tables_grow(const int32_t* held, const int32_t* lens, in
                                     int32_t max_blocks, int64_t max_rows, int32_t* row_offsets,
                                     int64_t* slots, int32_t* positions, int32_t* counts, int32_t device,
                                     void* stream) {
-  if (R < 0 || num_free < 0 || max_blocks < 0 || max_rows < 0 || max_rows > INT32_MAX)
-    return kvr_err::set(KV_EINVAL, "num_requests, num_free, max_blocks_per_req and max_rows are 0 .. 2^31 - 1");
+  if (R < 0 || R > 1 << 30 || num_free < 0 || max_blocks < 0 || max_rows < 0 || max_rows > INT32_MAX)
+    return kvr_err::set(KV_EINVAL, "num_requests is 0 .. 2^30; num_free, max_blocks_per_req and max_rows 0 .. 2^31 - 1");
   if (B <= 0) return kvr_err::set(KV_EINVAL, "block_size must be positive");
   if (!row_offsets || !counts) return kvr_err::set(KV_EINVAL, "null row_offsets or counts");
   if (R > 0 && !lens) return kvr_err::set(KV_EINVAL, "null lens");
@@ -236,8 +237,9 @@ extern "C" kv_status kv_tables_grow(const int32_t* held, const int32_t* lens, in
   DeviceGuard dg(device);
   const kv_status st = device_ready(dg, device);
   if (st != KV_OK) return st;
-  const GrowParams p{held, lens, R, B, (B & (B - 1)) == 0 ? __builtin_ctz(B) : -1, free_blocks, num_free, tables, max_blocks, max_rows, row_offsets,
-                     slots, positions, counts};
+  const int shift = (B & (B - 1)) == 0 ? __builtin_ctz(B) : -1;
+  const GrowParams p{held,   lens,       R,        B,           shift, free_blocks, num_free,
+                     tables, max_blocks, max_rows, row_offsets, slots, positions,   counts};
   // a workgroup a window, up to 2^25 rows; further windows are walked
   const int grid = (int)std::max<int64_t>(1, std::min<int64_t>((max_rows + TG_WIN - 1) / TG_WIN, 1 << 14));
   hipLaunchKernelGGL(tables_grow_kernel, dim3(grid), dim3(TG_NT), 0, reinterpret_cast<hipStream_t>(stream), p);

@@ -225,7 +225,7 @@ def test_packed_refusals_on_live_handles():
     a = P.PackedArena(shape, 16, 4)
     w = shape.num_kv_heads * 128
     ok = dict(packed=a.handle, layer=0, k=0x1000, k_stride=w, v=0x2000, v_stride=w, slots=0x3000, rows=2)
-    for bad in (dict(layer=-1), dict(layer=2), dict(rows=-1), dict(k=0), dict(v=0), dict(slots=0),
+    for bad in (dict(layer=-1), dict(layer=2), dict(rows=-1), dict(rows=1 << 31), dict(k=0), dict(v=0), dict(slots=0),
                 dict(k_stride=w - 2), dict(v_stride=w - 2), dict(k_stride=w + 1), dict(k=0x1002), dict(slots=0x3004)):
         for call in (kvr.kv_packed_store, kvr.kv_packed_load):
             assert status(call, **{**ok, **bad}) == kvr.KV_EINVAL
@@ -233,7 +233,7 @@ def test_packed_refusals_on_live_handles():
     arena = bound_arena(shape, wl)
     other = bound_arena(W.TINY_BF16, W.small_workload(W.TINY_BF16, [5], seed=1))
     assert status(kvr.kv_packed_park, other.handle, 0x1000, a.handle, 0x2000, 1) == kvr.KV_ESTATE
-    for args in ((0, 0x2000, 1), (0x1000, 0, 1), (0x1000, 0x2000, -1), (0x1004, 0x2000, 1)):
+    for args in ((0, 0x2000, 1), (0x1000, 0, 1), (0x1000, 0x2000, -1), (0x1000, 0x2000, 1 << 31), (0x1004, 0x2000, 1)):
         s, p, n = args
         assert status(kvr.kv_packed_park, arena.handle, s, a.handle, p, n) == kvr.KV_EINVAL
         assert status(kvr.kv_packed_restore, a.handle, p, arena.handle, s, n) == kvr.KV_EINVAL

@@ -112,7 +112,7 @@ class Batch:
             there = (blk >= 0) & (blk < self.blocks)
             slots = (blk * B + j % B)[there]
             k, v = P.values(kc[slots], ks[slots]), P.values(vc[slots], vs[slots])
-            for i in range(m):
+            for i in range(min(m, self.max_query)):
                 row = self.off[r] + i
                 seen = j[there] <= n - m + i
                 if not seen.any():
@@ -312,6 +312,60 @@ def test_graphs_follow_the_lengths_and_share_a_workspace():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("name,g", [("bf16", 2), ("bf16", 5), ("f32_64", 16)])
+def test_more_rows_than_max_query(name, g):
+    """Rows past max_query are left out; those before them keep their positions."""
+    counts = [5, 9, 2, 7]
+    b = Batch(heads(name, g), [40, 9, 70, 4], counts, seed=12)
+    b.bind(max_query=4)
+    b.run()
+    torch.cuda.synchronize()
+    want, tol = b.reference()
+    got = b.out[:, :b.q.shape[1]].float().cpu().numpy().astype(np.float64).reshape(want.shape)
+    for r, m in enumerate(counts):
+        rows = slice(b.off[r], b.off[r] + min(m, 4))
+        assert (np.abs(got[rows] - want[rows]) <= tol[rows]).all(), r
+        assert (got[rows.stop:b.off[r] + m] == KEPT).all(), r
+    b.release()
+
+
+@pytest.mark.gpu
+def test_requests_that_share_blocks():
+    """A common prefix: two requests' tables name the same blocks, one block twice in a
+    third's."""
+    b = Batch(heads("bf16", 4), [100, 90, 64], [2, 3, 1], seed=13)
+    b.tables[1, :5] = b.tables[0, :5]
+    b.tables[2, 3] = b.tables[2, 0]
+    b.bind()
+    b.run()
+    torch.cuda.synchronize()
+    b.check()
+    b.release()
+
+
+@pytest.mark.gpu
+def test_attention_on_two_streams_at_once():
+    """Calls in flight together over one arena, a workspace each."""
+    b = Batch(heads("bf16", 4), [3000, 1, 700, 257], seed=14)
+    b.run()
+    torch.cuda.synchronize()
+    b.check()
+    want, outs = b.out.clone(), []
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    ws = [torch.full_like(b.ws, 255) for _ in streams]
+    torch.cuda.synchronize()
+    for _ in range(8):
+        for s, w in zip(streams, ws):
+            with torch.cuda.stream(s):
+                b.out = torch.full_like(want, KEPT)
+                b.run(w, s.cuda_stream)
+                outs.append(b.out)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want) for o in outs)
+    b.release()
+
+
+@pytest.mark.gpu
 def test_output_over_the_queries():
     """out may be q itself."""
     b = Batch(heads("bf16", 5), [70, 500, 3], [4, 2, 1], seed=11)
@@ -331,7 +385,8 @@ def test_output_over_the_queries():
 def test_workspace_bytes():
     s = W.LLAMA8B
     assert kvr.kv_packed_attention_workspace_bytes(s, 4, 4, 1, 1000) > 0
-    for bad in ((0, 4, 1, 10), (4, 0, 1, 10), (4, 4, 0, 10), (4, 4, 1, 0)):
+    for bad in ((0, 4, 1, 10), (4, 0, 1, 10), (4, 4, 0, 10), (4, 4, 1, 0), ((1 << 24) + 1, 4, 1, 10),
+                (4, (1 << 24) + 1, 1, 10), (4, 1 << 62, 1 << 30, 10), (4, 4, 1, 1 << 31), (4, 4, 1, 1 << 62)):
         assert kvr.kv_packed_attention_workspace_bytes(s, *bad) == 0
     wide = dataclasses.replace(s, num_q_heads=8 * 17)
     assert kvr.kv_packed_attention_workspace_bytes(wide, 4, 4, 1, 1000) == 0
@@ -351,7 +406,7 @@ def test_attention_refusals():
               tables=0x4000, num_requests=2, max_blocks=4, max_query=1, max_len=64, out=0x5000, out_stride=w,
               workspace=0x10000, workspace_bytes=b.ws_bytes)
     for bad in (dict(layer=-1), dict(layer=2), dict(q=0), dict(out=0), dict(lens=0), dict(tables=0), dict(rows=-1),
-                dict(rows=1 << 31), dict(num_requests=-1), dict(max_blocks=-1), dict(max_query=0), dict(max_len=0),
+                dict(rows=1 << 31), dict(num_requests=-1), dict(num_requests=(1 << 24) + 1), dict(max_blocks=-1), dict(max_query=0), dict(max_len=0),
                 dict(q_stride=w - 2), dict(out_stride=w - 2), dict(q_stride=w + 1), dict(q=0x1002), dict(lens=0x3001),
                 dict(q_offsets=0, rows=3), dict(max_len=1 << 31), dict(rows=1 << 24, max_len=1 << 26), dict(workspace=0), dict(workspace=0x10008)):
         with pytest.raises(kvr.KvError) as e:

@@ -181,7 +181,7 @@ def call_with(**kw):
 
 
 @pytest.mark.parametrize("bad", [
-    dict(num_requests=-1), dict(num_free=-1), dict(max_blocks=-1), dict(max_rows=-1), dict(max_rows=1 << 31),
+    dict(num_requests=-1), dict(num_requests=(1 << 30) + 1), dict(num_free=-1), dict(max_blocks=-1), dict(max_rows=-1), dict(max_rows=1 << 31),
     dict(block_size=0), dict(lens=0), dict(tables=0), dict(free_blocks=0), dict(slots=0), dict(row_offsets=0),
     dict(counts=0), dict(lens=0x2002), dict(slots=0x6004), dict(tables=0x4001)])
 def test_tables_grow_refusals(bad):
