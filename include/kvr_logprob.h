@@ -21,7 +21,8 @@ extern "C" {
 #define KV_LOGPROBS_MAX_TOP 64
 
 /* Workspace bytes of kv_logprobs; 0 for sizes it does not take (rows 1 .. 2^20, vocab
- * 1 .. 2^21, top_n 0 .. KV_LOGPROBS_MAX_TOP and at most vocab). */
+ * 1 .. 2^21, rows * ceil(vocab / 8192) below 2^24, top_n 0 .. KV_LOGPROBS_MAX_TOP and at
+ * most vocab). */
 uint64_t kv_logprobs_workspace_bytes(int64_t rows, int32_t vocab, int32_t top_n);
 
 /* With x_v = scale * z_v of a row's logits z (0 < scale <= 2^127, the inverse temperature):

@@ -39,6 +39,7 @@ constexpr float LOG2E = 1.4426950408889634f;
 constexpr int LP_ITEMS = 32;
 constexpr int LP_CHUNK = LP_NT * LP_ITEMS;
 constexpr int LP_MAX_VOCAB = 256 * LP_CHUNK;
+constexpr int64_t LP_MOST_CHUNKS = (1 << 24) - 1;  // of a call: a grid holds 2^32 - 1 threads
 constexpr float LN2 = 0.6931471805599453f;
 
 struct LogprobParams {
@@ -401,6 +402,7 @@ uint64_t kv_logprobs_workspace_bytes(int64_t rows, int32_t vocab, int32_t top_n)
       top_n > KV_LOGPROBS_MAX_TOP || top_n > vocab)
     return 0;
   const int64_t chunks = chunks_of(vocab);
+  if (rows * chunks > LP_MOST_CHUNKS) return 0;
   return (uint64_t)(rows * chunks * (16 + 8 * (int64_t)top_n));
 }
 
@@ -410,6 +412,8 @@ kv_status kv_logprobs(const void* logits, int32_t dtype, int64_t rows, int32_t v
   if (dtype != KV_F32 && dtype != KV_BF16) return kvr_err::set(KV_EINVAL, "unknown dtype %d", dtype);
   if (rows < 0 || rows > (1 << 20)) return kvr_err::set(KV_EINVAL, "rows must be 0 .. 2^20");
   if (vocab < 1 || vocab > LP_MAX_VOCAB) return kvr_err::set(KV_EINVAL, "vocab must be 1 .. 2^21");
+  if (rows * chunks_of(vocab) > LP_MOST_CHUNKS)
+    return kvr_err::set(KV_EINVAL, "rows * vocab of one call above 2^37: split the rows");
   if (stride < vocab) return kvr_err::set(KV_EINVAL, "the stride is below the vocabulary");
   if (!(scale > 0.0f) || !(scale <= 0x1p127f)) return kvr_err::set(KV_EINVAL, "scale must be positive and at most 2^127");
   if (top_n < 0 || top_n > KV_LOGPROBS_MAX_TOP || top_n > vocab)

@@ -257,15 +257,17 @@ def test_calls_on_two_streams_at_once():
 # ---- sizes and refusals (no device access) -------------------------------------
 def test_workspace_bytes():
     assert kvr.kv_logprobs_workspace_bytes(16, 128256, 0) > 0
+    assert kvr.kv_logprobs_workspace_bytes((1 << 20) - 1, 131072, 0) > 0
     assert kvr.kv_logprobs_workspace_bytes(16, 128256, 20) > kvr.kv_logprobs_workspace_bytes(16, 128256, 0)
     for bad in ((0, 100, 0), (-1, 100, 0), (1 << 21, 100, 0), (1, 0, 0), (1, (1 << 21) + 1, 0), (1, 100, -1),
-                (1, 100, 65), (1, 10, 11)):
+                (1, 100, 65), (1, 10, 11), (1 << 20, 131073, 0), (1 << 16, 1 << 21, 0)):
         assert kvr.kv_logprobs_workspace_bytes(*bad) == 0
 
 
 @pytest.mark.parametrize("bad,status", [
     (dict(dtype=2), kvr.KV_EINVAL), (dict(rows=-1), kvr.KV_EINVAL), (dict(rows=(1 << 20) + 1), kvr.KV_EINVAL),
-    (dict(vocab=0), kvr.KV_EINVAL), (dict(vocab=(1 << 21) + 1, stride=1 << 22), kvr.KV_EINVAL),
+    (dict(vocab=0), kvr.KV_EINVAL), (dict(rows=1 << 20, vocab=131073, stride=131073), kvr.KV_EINVAL),
+    (dict(vocab=(1 << 21) + 1, stride=1 << 22), kvr.KV_EINVAL),
     (dict(stride=999), kvr.KV_EINVAL), (dict(scale=0.0), kvr.KV_EINVAL), (dict(scale=-1.0), kvr.KV_EINVAL),
     (dict(scale=float("inf")), kvr.KV_EINVAL), (dict(scale=2.0 ** 127 * 1.5), kvr.KV_EINVAL), (dict(scale=float("nan")), kvr.KV_EINVAL),
     (dict(top_n=-1), kvr.KV_EINVAL), (dict(top_n=65), kvr.KV_EINVAL), (dict(vocab=3, top_n=4), kvr.KV_EINVAL),
