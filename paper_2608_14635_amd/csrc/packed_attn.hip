@@ -100,7 +100,7 @@ struct PackedAttnParams {
   int workers;                   // stretches per kv head, a multiple of four
   int part_cols;                 // columns of a slot of sums
   OpenItem* open;                // [workers / 4]
-  float* part;                   // [nkv][workers][2][part_cols][D + 2]: an item begun before, one left open
+  float* part;                   // [nkv][workers][2][part_cols][ROW]: an item begun before, one left open
 };
 
 // f(0), f(1), .. with the index a constant
@@ -230,6 +230,12 @@ struct Stretch {
   uint32_t end;  // the open item's units' end
 };
 
+// Floats of a partial's row: on boundaries of 16 bytes, of 8 where 16 rows have to fit a
+// ring of the smallest heads.
+constexpr int row_of(int d) { return d == 32 ? d + 2 : d + 4; }
+template <int D>
+constexpr int ROW = row_of(D);
+
 // Columns are merged 256 / D at a time: a lane has four dims of one of them.  A partial
 // is D sums, a maximum and a sum of weights; n of them go in their order.
 template <int D>
@@ -241,12 +247,25 @@ struct Column {
 };
 template <int D>
 __device__ __forceinline__ int dim_of(int lane) { return lane % LANES<D> * 4; }
-template <typename P>
-__device__ __forceinline__ void load_part(const P* part, int D, int dim, float2& ml, float* o) {
-  // rows of D + 2 floats: 8-byte aligned
+template <int D>
+__device__ __forceinline__ void load_part(const float* part, int dim, float2& ml, float* o) {
   ml = *reinterpret_cast<const float2*>(part + D);
-  const float2 a = *reinterpret_cast<const float2*>(part + dim), b = *reinterpret_cast<const float2*>(part + dim + 2);
-  o[0] = a.x; o[1] = a.y; o[2] = b.x; o[3] = b.y;
+  if constexpr (ROW<D> % 4 == 0) {
+    const float4 a = *reinterpret_cast<const float4*>(part + dim);
+    o[0] = a.x; o[1] = a.y; o[2] = a.z; o[3] = a.w;
+  } else {
+    const float2 a = *reinterpret_cast<const float2*>(part + dim), b = *reinterpret_cast<const float2*>(part + dim + 2);
+    o[0] = a.x; o[1] = a.y; o[2] = b.x; o[3] = b.y;
+  }
+}
+template <int D>
+__device__ __forceinline__ void store_part(float* part, int dim, const float* o) {
+  if constexpr (ROW<D> % 4 == 0) {
+    *reinterpret_cast<float4*>(part + dim) = make_float4(o[0], o[1], o[2], o[3]);
+  } else {
+    reinterpret_cast<float2*>(part + dim)[0] = make_float2(o[0], o[1]);
+    reinterpret_cast<float2*>(part + dim)[1] = make_float2(o[2], o[3]);
+  }
 }
 template <int D, int CHUNK, typename SRC>  // CHUNK: partials whose loads are on their way together
 __device__ __forceinline__ Column merge_column(SRC src, int n, int lane) {
@@ -257,7 +276,7 @@ __device__ __forceinline__ Column merge_column(SRC src, int n, int lane) {
     float o[CHUNK][4];
 #pragma unroll
     for (int i = 0; i < CHUNK; ++i)  // past the last: the last again, not counted below
-      src(min(i0 + i, n - 1), [&](const auto* part) { load_part(part, D, dim_of<D>(lane), ml[i], o[i]); });
+      src(min(i0 + i, n - 1), [&](const float* part) { load_part<D>(part, dim_of<D>(lane), ml[i], o[i]); });
     float top = x.m;
 #pragma unroll
     for (int i = 0; i < CHUNK; ++i) top = fmaxf(top, ml[i].x);
@@ -299,8 +318,7 @@ __device__ __forceinline__ void put_out(const PackedAttnParams& p, int row, int 
 }
 template <int D>
 __device__ __forceinline__ void put_part(float* dst, int lane, const Column& v) {
-  reinterpret_cast<float2*>(dst + dim_of<D>(lane))[0] = make_float2(v.o[0], v.o[1]);
-  reinterpret_cast<float2*>(dst + dim_of<D>(lane))[1] = make_float2(v.o[2], v.o[3]);
+  store_part<D>(dst, dim_of<D>(lane), v.o);
   if (dim_of<D>(lane) == 0) *reinterpret_cast<float2*>(dst + D) = make_float2(v.m, v.l);
 }
 
@@ -313,8 +331,8 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
   constexpr int REC = 17 * D, RING = ring_of(OCC), LOADS = (16 * D + 1023) / 1024 + 1;
   __shared__ __attribute__((aligned(16))) char s_ring[PA_NT / 64][RING * REC];
   static_assert(RING % TILES == 0, "units do not wrap in the ring");
-  static_assert(RING * REC >= 64 * (D + 2), "16 rows fit the ring");
-  constexpr bool LOCAL = RING * REC >= NT * 64 * (D + 2);  // all columns' rows do
+  static_assert(RING * REC >= 64 * ROW<D>, "16 rows fit the ring");
+  constexpr bool LOCAL = RING * REC >= NT * 64 * ROW<D>;  // all columns' rows do
   constexpr int WAVES = PA_NT / 64;
   __shared__ uint32_t s_wave[WAVES];
   __shared__ Stretch s_str[WAVES];
@@ -362,7 +380,7 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
   }
   __syncthreads();
 
-  float* const slots = p.part + ((int64_t)kvh * p.workers + w) * 2 * p.part_cols * (D + 2);
+  float* const slots = p.part + ((int64_t)kvh * p.workers + w) * 2 * p.part_cols * ROW<D>;
   const auto begin_of = [&](int i) { return __builtin_amdgcn_readfirstlane(s_begin[wave][i]); };
   int r = begin_of(0);
   if (r >= 0) {
@@ -708,21 +726,30 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
       // stretch's end, where the ring has no more to take, stays where it is.
       const bool done = first == 0 && upto == rq.steps, stay = LOCAL && u + upto - first >= u1;
       float* const rows = reinterpret_cast<float*>(ring);
-      float* const part = stay ? rows : slots + (first > 0 ? 0 : 1) * p.part_cols * (D + 2);
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        float* const tr = rows + (LOCAL ? nt : 0) * 16 * (D + 2);
+      float* const part = stay ? rows : slots + (first > 0 ? 0 : 1) * p.part_cols * ROW<D>;
+      const auto put_rows = [&](int nt, float* tr) {
         float l = l_run[nt] + __shfl_xor(l_run[nt], 16, 64);
         l += __shfl_xor(l, 32, 64);
         if (q == 0) {
-          tr[c * (D + 2) + D] = m_run[nt];
-          tr[c * (D + 2) + D + 1] = l;
+          *reinterpret_cast<float2*>(tr + c * ROW<D> + D) = make_float2(m_run[nt], l);
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < 4; ++j) {
+          float* const row = tr + (4 * q + j) * ROW<D>;
+          if constexpr (DT % 4 == 0) {
 #pragma unroll
-          for (int d = 0; d < DT; ++d) tr[(4 * q + j) * (D + 2) + c * DT + d] = o[nt][d][j];
+            for (int d = 0; d < DT; d += 4) {
+              const float x[4] = {o[nt][d][j], o[nt][d + 1][j], o[nt][d + 2][j], o[nt][d + 3][j]};
+              store_part<D>(row, c * DT + d, x);
+            }
+          } else {
+#pragma unroll
+            for (int d = 0; d < DT; ++d) row[c * DT + d] = o[nt][d][j];
+          }
+        }
         asm volatile("" ::: "memory");
+      };
+      const auto take_rows = [&](int nt, const float* tr) {
         // 0: the rows are the partials
         const int used = COPIES == 1 && stay && !done ? 0 : min(16 / COPIES, cols - nt * 16);
 #pragma unroll 1
@@ -730,12 +757,24 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
           const int i = i0 + lane / LANES<D>;
           if (i >= used) continue;
           const Column v = merge_column<D, COPIES>(
-              [&](int k, auto load) { load(tr + (k * (16 / COPIES) + i) * (D + 2)); }, COPIES, lane);
+              [&](int k, auto load) { load(tr + (k * (16 / COPIES) + i) * ROW<D>); }, COPIES, lane);
           if (done) put_out<T, D, COLS>(p, rq.row, tile, nt * 16 + i, kvh, lane, v);
-          else put_part<D>(part + (nt * 16 + i) * (D + 2), lane, v);
+          else put_part<D>(part + (nt * 16 + i) * ROW<D>, lane, v);
         }
         KVR_WAIT_LGKM0();  // the rows have been read: the ring may be filled again
         asm volatile("" ::: "memory");
+      };
+      if constexpr (LOCAL) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) put_rows(nt, rows + nt * 16 * ROW<D>);
+#pragma unroll 1
+        for (int nt = 0; nt < NT; ++nt) take_rows(nt, rows + nt * 16 * ROW<D>);
+      } else {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          put_rows(nt, rows);
+          take_rows(nt, rows);
+        }
       }
       if (!done && lane == 0) {
         Stretch& me = s_str[wave];
@@ -763,8 +802,9 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
   const uint32_t begun = of_waves(str.cols[0] != 0), left = of_waves(str.cols[1] != 0), ended = of_waves(str.flags & 1);
   const uint32_t near[2] = {of_waves(str.flags & 2), of_waves(str.flags & 4)};  // sums in the rings
   OpenItem open{0, 0, 0, 0, 0};
-  const int64_t pitch = (int64_t)2 * p.part_cols * (D + 2);
+  const int64_t pitch = (int64_t)2 * p.part_cols * ROW<D>;
   float* const slots0 = slots - wave * pitch;
+  int turn = wave;  // the wave's place among those that take the next columns
 #pragma unroll 1
   for (int lead = -1; lead < WAVES; ++lead) {
     const int at = max(lead, 0), which = lead < 0 ? 0 : 1;
@@ -775,27 +815,28 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
     const int cols = __builtin_amdgcn_readlane(str.cols[which], at);
     const int row = __builtin_amdgcn_readlane(str.row[which], at), tile = __builtin_amdgcn_readlane(str.tile[which], at);
     closed &= lead >= 0;  // all of the item is here
-    float* slot = slots0 + at * pitch + which * p.part_cols * (D + 2);
+    float* slot = slots0 + at * pitch + which * p.part_cols * ROW<D>;
     if (lead >= 0 && !closed) open = OpenItem{cols, row, tile, at, 0};
     if (n == 1 && !(near[which] >> at & 1)) continue;
     // A wave's sums are in its ring or, where its stretch went on behind them, in the
     // workspace: a branch for each, not loads that may be from either memory.
 #pragma unroll 1
-    for (int c0 = wave * AT_ONCE<D>; c0 < cols; c0 += WAVES * AT_ONCE<D>) {
+    for (int c0 = turn * AT_ONCE<D>; c0 < cols; c0 += WAVES * AT_ONCE<D>) {
       const int col = c0 + lane / LANES<D>;
       if (col >= cols) continue;
       const Column v = merge_column<D, WAVES>(
           [&](int i, auto load) {
             const int j = at + i;
             if ((i == 0 ? near[which] : near[0]) >> j & 1)
-              load(reinterpret_cast<const float*>(&s_ring[0][0] + j * (RING * REC)) + col * (D + 2));
+              load(reinterpret_cast<const float*>(&s_ring[0][0] + j * (RING * REC)) + col * ROW<D>);
             else
-              load((i == 0 ? slot : slots0 + j * pitch) + col * (D + 2));
+              load((i == 0 ? slot : slots0 + j * pitch) + col * ROW<D>);
           },
           n, lane);
       if (closed) put_out<T, D, COLS>(p, row, tile, col, kvh, lane, v);
-      else put_part<D>(slot + col * (D + 2), lane, v);
+      else put_part<D>(slot + col * ROW<D>, lane, v);
     }
+    turn = (turn - (cols + AT_ONCE<D> - 1) / AT_ONCE<D>) & (WAVES - 1);
   }
   if (kvh == 0 && t == 0) {
     const int wg = blockIdx.x / nkv;
@@ -815,9 +856,9 @@ __global__ __launch_bounds__(PM_NT) void packed_attn_merge_kernel(PackedAttnPara
   const int nkv = p.packed.nkv, wg = blockIdx.x / nkv, kvh = blockIdx.x % nkv;
   const OpenItem it = p.open[wg];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t pitch = (int64_t)2 * p.part_cols * (D + 2);
+  const int64_t pitch = (int64_t)2 * p.part_cols * ROW<D>;
   const float* first = p.part + ((int64_t)kvh * p.workers + wg * WG) * pitch;
-  const float* lead = first + it.wave * pitch + p.part_cols * (D + 2);
+  const float* lead = first + it.wave * pitch + p.part_cols * ROW<D>;
   auto merge = [&](auto chunk) {
 #pragma unroll 1
     for (int c0 = wave * AT_ONCE<D>; c0 < it.cols; c0 += PM_NT / 64 * AT_ONCE<D>) {
@@ -826,7 +867,7 @@ __global__ __launch_bounds__(PM_NT) void packed_attn_merge_kernel(PackedAttnPara
       put_out<T, D, S::COLS>(
           p, it.row, it.tile, col, kvh, lane,
           merge_column<D, chunk>(
-              [&](int i, auto load) { load((i == 0 ? lead : first + i * WG * pitch) + col * (D + 2)); }, it.groups,
+              [&](int i, auto load) { load((i == 0 ? lead : first + i * WG * pitch) + col * ROW<D>); }, it.groups,
               lane));
     }
   };
@@ -887,7 +928,7 @@ AttnLayout attn_layout(const kv_model_desc& d, int32_t R, int64_t rows, int32_t 
   L.workers = workers_of(L.plan, d.num_kv_heads, R, rows, g, max_len);
   L.cols = (int)std::min<int64_t>(L.plan.cols, (int64_t)g * max_query);
   L.part = (uint64_t)round_up((int64_t)L.workers / (PA_NT / 64) * (int64_t)sizeof(OpenItem), 256);
-  L.total = L.part + (uint64_t)4 * d.num_kv_heads * L.workers * 2 * L.cols * (d.head_dim + 2);
+  L.total = L.part + (uint64_t)4 * d.num_kv_heads * L.workers * 2 * L.cols * row_of(d.head_dim);
   return L;
 }
 
