@@ -97,6 +97,7 @@ struct PackedAttnParams {
   uint32_t g_inv;                // ceil(2^32 / g), 0 for g = 1: n / g of n < 2^28 is the product's high half
   int max_query;                 // rows of a request past it are left out: the sums have no room
   int most_len;                  // positions of a request: max_len, or what its table holds
+  int start;                     // units that an item's start counts as
   int workers;                   // stretches per kv head, a multiple of four
   int part_cols;                 // columns of a slot of sums
   OpenItem* open;                // [workers / 4]
@@ -161,7 +162,8 @@ struct Stretches {
 struct Request {
   int row, m, len, want;  // first query row, rows, positions there are, position after the last of these rows
   int tiles, steps;       // column tiles, units of each
-  __device__ __forceinline__ uint32_t units() const { return (uint32_t)tiles * (uint32_t)steps; }
+  uint32_t item;          // what an item counts: its units and its start
+  __device__ __forceinline__ uint32_t units() const { return (uint32_t)tiles * item; }
 };
 template <int COLS, int UNIT>
 __device__ __forceinline__ Request make_request(const PackedAttnParams& p, int row, int m, int want) {
@@ -172,6 +174,7 @@ __device__ __forceinline__ Request make_request(const PackedAttnParams& p, int r
   q.len = max(0, min(want, p.most_len));
   q.tiles = (int)(((int64_t)m * p.g + COLS - 1) / COLS);
   q.steps = max(1, (int)(((int64_t)q.len + UNIT - 1) / UNIT));
+  q.item = (uint32_t)(q.steps + p.start);
   return q;
 }
 template <int COLS, int UNIT>
@@ -387,10 +390,6 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
     const uint32_t u0 = st.begin(w), u1 = st.begin(w + 1);
     uint32_t base = begin_of(1);
     rq = per == 1 ? make_request<COLS, UNIT>(p, begin_of(2), begin_of(3), begin_of(4)) : get_request<COLS, UNIT>(p, r);
-    while (u0 - base >= rq.units() && r + 1 < p.R) {
-      base += rq.units();
-      rq = get_request<COLS, UNIT>(p, ++r);
-    }
 
     const int B = p.packed.block_size, tpb = B / PK_TILE;
     const float scale_log2 = 1.4426950408889634f / sqrtf((float)D);
@@ -403,8 +402,15 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
 
     for (uint32_t u = u0; u < u1;) {
       // ---- the stretch's part of one item ----
-      const int tile = (int)quotient(u - base, rq.steps), first = (int)(u - base) - tile * rq.steps;
-      const int upto = (int)min((uint32_t)rq.steps, first + (u1 - u));
+      while (u - base >= rq.units() && r + 1 < p.R) {
+        base += rq.units();
+        rq = get_request<COLS, UNIT>(p, ++r);
+      }
+      const int tile = (int)quotient(u - base, rq.item);
+      const uint32_t from = u - base - (uint32_t)tile * rq.item, to = min(rq.item, from + (u1 - u));
+      const int first = max((int)from - p.start, 0), upto = (int)to - p.start;
+      u += to - from;
+      if (upto <= 0) continue;  // of the start alone
       const int cols = min(COLS, rq.m * g - tile * COLS);  // of this tile
       if (cols <= 0) break;  // offsets that overlap so far that the units passed 2^32
       // positions that every column sees, and that any does
@@ -724,7 +730,7 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
       // 16 rows at a time through the ring, a row's dims over the lanes; the copies of a
       // column are merged on the way.  What stays open goes to the workspace, or at the
       // stretch's end, where the ring has no more to take, stays where it is.
-      const bool done = first == 0 && upto == rq.steps, stay = LOCAL && u + upto - first >= u1;
+      const bool done = first == 0 && upto == rq.steps, stay = LOCAL && u >= u1;
       float* const rows = reinterpret_cast<float*>(ring);
       float* const part = stay ? rows : slots + (first > 0 ? 0 : 1) * p.part_cols * ROW<D>;
       const auto put_rows = [&](int nt, float* tr) {
@@ -783,14 +789,8 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
         me.row[which] = rq.row;
         me.tile[which] = tile;
         me.flags |= (stay ? 2 << which : 0) | (first > 0 && upto == rq.steps ? 1 : 0);
-        if (first == 0) me.end = base + (uint32_t)(tile + 1) * rq.steps;
+        if (first == 0) me.end = base + (uint32_t)(tile + 1) * rq.item;
       }
-      u += upto - first;
-      if (u < u1)
-        while (u - base >= rq.units() && r + 1 < p.R) {
-          base += rq.units();
-          rq = get_request<COLS, UNIT>(p, ++r);
-        }
     }
   }
 
@@ -878,26 +878,34 @@ __global__ __launch_bounds__(PM_NT) void packed_attn_merge_kernel(PackedAttnPara
 // The kernel for a call's columns per request: as few column tiles as take them, and
 // where a tile's half or quarter does, as many copies.
 struct Plan {
-  int nt, copies, cols, unit, occupancy;
+  int nt, copies, cols, unit, occupancy, start;
 };
 Plan plan_of(int dtype, int d, int g, int32_t max_query) {
   const int64_t cols = (int64_t)g * max_query;
   const int copies = cols <= 8 ? 2 : 1;
   const int nt = cols <= 16 ? 1 : cols <= 32 || dtype == KV_F32 ? 2 : 4;
-  return Plan{nt, copies, 16 * nt / copies, 32, occupancy_of(dtype == KV_F32, d, nt)};
+  return Plan{nt, copies, 16 * nt / copies, 32, occupancy_of(dtype == KV_F32, d, nt), nt == 1 ? 4 : 2};
 }
 
-// Units of one kv head at most.
-int64_t units_of(const Plan& pl, int R, int64_t rows, int g, int64_t max_len) {
-  return (R + rows * g / pl.cols) * ((max_len + pl.unit - 1) / pl.unit);
+// Units of one kv head at most, `start` more for each item.
+int64_t units_of(const Plan& pl, int R, int64_t rows, int g, int64_t max_len, int start) {
+  return (R + rows * g / pl.cols) * ((max_len + pl.unit - 1) / pl.unit + start);
 }
 
-// Stretches per kv head: as many waves as the chip holds at once, but no more than
-// there can be units; whole workgroups.
-int workers_of(const Plan& pl, int nkv, int R, int64_t rows, int g, int64_t max_len) {
-  const int64_t units = units_of(pl, R, rows, g, max_len);
-  const int64_t waves = 256 * 4 * (int64_t)pl.occupancy;
-  return (int)round_up(std::max<int64_t>(1, std::min<int64_t>((waves + nkv - 1) / nkv, units)), PA_NT / 64);
+// Stretches per kv head, whole workgroups: a unit each where the chip holds as many waves
+// at once, else those waves.  Then an item's start counts as `start` units more: a wave
+// whose stretch goes on with another item ends the one and waits for the other's table,
+// queries and first records, some 4 us, and the waves should end together.  One column
+// tile: four, 30.8 us on 16 requests and 19.9 on 64 (33.2 and 22.3 with none, 31.0 and
+// 21.0 with two); several, whose units take longer: two, 35.5 us on 40 requests of one to
+// five rows and 69 on 8 of 64 (41.0 and 78 with none, 36.1 and 71 with four).
+struct Stretching {
+  int workers, start;
+};
+Stretching stretches_of(const Plan& pl, int nkv, int R, int64_t rows, int g, int64_t max_len) {
+  const int64_t units = units_of(pl, R, rows, g, max_len, 0), waves = (256 * 4 * pl.occupancy + nkv - 1) / nkv;
+  if (units <= waves) return {(int)round_up(std::max<int64_t>(1, units), PA_NT / 64), 0};
+  return {(int)round_up(waves, PA_NT / 64), pl.start};
 }
 
 template <typename T, int D, typename S>
@@ -918,17 +926,19 @@ void launch(const Plan& pl, const PackedAttnParams& p, hipStream_t s) {
 // The workspace: what workgroups left open, then the waves' sums.
 struct AttnLayout {
   Plan plan;
-  int workers, cols;
+  Stretching stretches;
+  int cols;
   uint64_t part, total;
 };
 AttnLayout attn_layout(const kv_model_desc& d, int32_t R, int64_t rows, int32_t max_query, int64_t max_len) {
   AttnLayout L;
   const int g = d.num_q_heads / d.num_kv_heads;
   L.plan = plan_of(d.dtype, d.head_dim, g, max_query);
-  L.workers = workers_of(L.plan, d.num_kv_heads, R, rows, g, max_len);
+  L.stretches = stretches_of(L.plan, d.num_kv_heads, R, rows, g, max_len);
+  const int64_t workers = L.stretches.workers;
   L.cols = (int)std::min<int64_t>(L.plan.cols, (int64_t)g * max_query);
-  L.part = (uint64_t)round_up((int64_t)L.workers / (PA_NT / 64) * (int64_t)sizeof(OpenItem), 256);
-  L.total = L.part + (uint64_t)4 * d.num_kv_heads * L.workers * 2 * L.cols * row_of(d.head_dim);
+  L.part = (uint64_t)round_up(workers / (PA_NT / 64) * (int64_t)sizeof(OpenItem), 256);
+  L.total = L.part + (uint64_t)4 * d.num_kv_heads * workers * 2 * L.cols * row_of(d.head_dim);
   return L;
 }
 
@@ -962,7 +972,8 @@ void run(const kv_packed* packed, int32_t layer, const void* q, int64_t q_stride
   const AttnLayout L = attn_layout(d, R, rows, max_query, max_len);
   p.max_query = max_query;
   p.most_len = (int)std::min<int64_t>({max_len, (int64_t)max_blocks * packed->block_size, INT32_MAX - 64});
-  p.workers = L.workers;
+  p.start = L.stretches.start;
+  p.workers = L.stretches.workers;
   p.part_cols = L.cols;
   p.open = static_cast<OpenItem*>(workspace);
   p.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + L.part);
@@ -1019,7 +1030,7 @@ kv_status kv_packed_attention(kv_packed_t packed, int32_t layer, const void* q, 
     return kvr_err::set(KV_EINVAL, "null workspace, or one not on a boundary of 16 bytes");
   const Plan plan = plan_of(d.dtype, d.head_dim, d.num_q_heads / d.num_kv_heads, max_query);
   if (max_len > INT32_MAX ||
-      units_of(plan, R, rows, d.num_q_heads / d.num_kv_heads, max_len) > INT32_MAX)
+      units_of(plan, R, rows, d.num_q_heads / d.num_kv_heads, max_len, plan.start) > INT32_MAX)
     return kvr_err::set(KV_EINVAL, "max_len or the work of one call above 2^31: split the query rows");
   const uint64_t need = kv_packed_attention_workspace_bytes(&d, R, rows, max_query, max_len);
   if (need > ws_bytes)
