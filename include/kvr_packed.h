@@ -104,7 +104,7 @@ uint64_t kv_packed_attention_workspace_bytes(const kv_model_desc* desc, int32_t 
  *   max_query, max_len  host bounds of a request's query rows and length: its rows and
  *                positions past them are left out (row i stays at lens[r] - m + i).
  *                The workspace and the work of a call are sized by them;
- *                (num_requests + rows * nq/nkv / 8) * (max_len / 32 + 4) below 2^31
+ *                (num_requests + rows * nq/nkv / 16) * (max_len / 32 + 5) below 2^31
  *                always goes
  *   out          device [rows][nq][d], model dtype, rows out_stride elements apart
  *   workspace    device scratch, on a boundary of 16 bytes; calls in flight at once

@@ -13,16 +13,13 @@
 //   S^T = K Q^T on v_mfma_f32_16x16x32_bf16, 16 positions a tile: position c's dims
 //   q d/4 .. are the lane's K operand, d/8 bytes and one scale; the conversions to bf16
 //   are exact.  The lane gets the scores of positions 4q .. 4q+3 for column c.
-//   Where at most 8 columns are in use, the unit's two tiles are scored by a copy of
-//   them each, with a softmax of its own: all 16 columns work, and a lane has 4 scores
-//   of the unit instead of 8.  The copies are merged at the end of the stretch.  (Four
-//   copies of 4 columns over 64 positions took as long: the softmax is not the bound.)
 //   Online softmax per column, exp2 domain, rescaled only where the maximum rose by
 //   more than 2^SLACK.
-//   O = P V: the lane's weights of two tiles are the A operand as they are (0 where the
-//   tile is another copy's), positions 4q .. 4q+3 of both being its eight k's; V's
-//   layout gives the lane the dims c d/16 .. of the same positions, which it pairs into
-//   the B operands of d/16 products.
+//   O = P V: the lane's weights of the unit's two tiles are the A operand as they are,
+//   positions 4q .. 4q+3 of both being its eight k's; V's layout gives the lane the dims
+//   c d/16 .. of the same positions, which it pairs into the B operands of d/16 products.
+//   (Up to 8 columns, a softmax a tile in the two halves of the 16, merged at the end,
+//   spares half the exponentials and took as long: 30.2 us against 29.5 below.)
 // Records reach a wave through a ring of its own in LDS, by direct-to-LDS loads: a
 // record is 17 d contiguous bytes, K's and V's lane by lane in the operands' order, so
 // the reads back are linear, and records are on their way without a register.
@@ -61,15 +58,8 @@ constexpr int PA_NT = 256;         // four waves
 constexpr float SLACK = 8.0f;      // rescale slack, log2 units
 constexpr int MOST_ROWS = 1 << 24; // query rows and requests of a call
 
-// Copies of the columns, and column tiles, that a kernel is built for.
-template <int NT_, int COPIES_>
-struct Shape {
-  static constexpr int NT = NT_, COPIES = COPIES_;
-  static constexpr int COLS = 16 * NT / COPIES;       // columns of an item
-  static constexpr int TILES = 2;                     // tiles of a unit
-  static constexpr int UNIT = 16 * TILES;             // positions of a unit
-  static constexpr int OWN = COPIES == 1 ? TILES : 1; // tiles a column scores
-};
+constexpr int TILES = 2;           // tiles of a unit
+constexpr int UNIT = 16 * TILES;   // positions of a unit
 
 template <typename T> struct Split;  // bf16 numbers that stand for a query, for a weight
 template <> struct Split<bf16_t> { static constexpr int Q = 1, P = 2; };
@@ -184,7 +174,7 @@ struct Request {
   uint32_t item;          // what an item counts: its units and its start
   __device__ __forceinline__ uint32_t units() const { return (uint32_t)tiles * item; }
 };
-template <int COLS, int UNIT>
+template <int COLS>
 __device__ __forceinline__ Request make_request(const PackedAttnParams& p, int row, int m, int want) {
   Request q;
   q.row = row;
@@ -196,7 +186,7 @@ __device__ __forceinline__ Request make_request(const PackedAttnParams& p, int r
   q.item = (uint32_t)(q.steps + p.start);
   return q;
 }
-template <int COLS, int UNIT>
+template <int COLS>
 __device__ __forceinline__ Request get_request(const PackedAttnParams& p, int r) {
   int row = r, m = 1, want = p.lens[r];
   if (p.q_offsets) {
@@ -206,7 +196,7 @@ __device__ __forceinline__ Request get_request(const PackedAttnParams& p, int r)
     m = min(all, p.max_query);
     want = max(want, 0) - (all - m);  // the rows left out are the last ones
   }
-  return make_request<COLS, UNIT>(p, row, m, want);
+  return make_request<COLS>(p, row, m, want);
 }
 
 // The scale of byte i of a word.  The conversions read the exponent alone, whatever the
@@ -344,12 +334,12 @@ __device__ __forceinline__ void put_part(float* dst, int lane, const Column& v) 
   if (dim_of<D>(lane) == 0) *reinterpret_cast<float2*>(dst + D) = make_float2(v.m, v.l);
 }
 
-template <typename T, int D, typename S, int OCC>
+template <typename T, int D, int NT, int OCC>
 __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParams p) {
-  constexpr int NT = S::NT, COPIES = S::COPIES, COLS = S::COLS, TILES = S::TILES, UNIT = S::UNIT, OWN = S::OWN;
+  constexpr int COLS = 16 * NT;           // columns of an item
   constexpr int W = D / 32, DT = D / 16;  // words a tile; dims a lane, P.V products
   constexpr int QP = Split<T>::Q, PP = Split<T>::P;
-  constexpr int NV = 4 * OWN;             // scores of a lane and column
+  constexpr int NV = 4 * TILES;           // scores of a lane and column
   constexpr int REC = 17 * D, RING = ring_of(OCC), LOADS = (16 * D + 1023) / 1024 + 1;
   __shared__ __attribute__((aligned(16))) char s_ring[PA_NT / 64][RING * REC];
   static_assert(RING % TILES == 0, "units do not wrap in the ring");
@@ -369,7 +359,7 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
   Request rq{};
   for (int i = 0; i < per; ++i)
     if (t * per + i < p.R) {
-      rq = get_request<COLS, UNIT>(p, t * per + i);
+      rq = get_request<COLS>(p, t * per + i);
       mine += rq.units();
     }
   uint32_t pre = wave_scan(mine);
@@ -408,7 +398,7 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
   if (r >= 0) {
     const uint32_t u0 = st.begin(w), u1 = st.begin(w + 1);
     uint32_t base = begin_of(1);
-    rq = per == 1 ? make_request<COLS, UNIT>(p, begin_of(2), begin_of(3), begin_of(4)) : get_request<COLS, UNIT>(p, r);
+    rq = per == 1 ? make_request<COLS>(p, begin_of(2), begin_of(3), begin_of(4)) : get_request<COLS>(p, r);
 
     const int B = p.packed.block_size, tpb = B / PK_TILE;
     const float scale_log2 = 1.4426950408889634f / sqrtf((float)D);
@@ -417,13 +407,12 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
     char* const ring = s_ring[wave];
     const int k_off = c * (D / 2) + q * (D / 8), v_off = 8 * D + q * (2 * D) + c * (D / 8);
     const int ks_off = 16 * D + c * (D / 32) + q * D / 128, vs_off = 16 * D + D / 2 + q * (D / 8) + c * D / 512 * 4;
-    const int copy = c / (16 / COPIES);  // whose tile the lane's column scores
 
     for (uint32_t u = u0; u < u1;) {
       // ---- the stretch's part of one item ----
       while (u - base >= rq.units() && r + 1 < p.R) {
         base += rq.units();
-        rq = get_request<COLS, UNIT>(p, ++r);
+        rq = get_request<COLS>(p, ++r);
       }
       const int tile = (int)quotient(u - base, rq.item);
       const uint32_t from = u - base - (uint32_t)tile * rq.item, to = min(rq.item, from + (u1 - u));
@@ -446,8 +435,7 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
       int limit[NT];  // positions the lane's column sees
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        const int col = COPIES == 1 ? nt * 16 + c : c % (16 / COPIES);
-        const int gc = tile * COLS + min(col, cols - 1), i = by_g(p, gc);
+        const int col = nt * 16 + c, gc = tile * COLS + min(col, cols - 1), i = by_g(p, gc);
         limit[nt] = col < cols ? min(rq.len, rq.want - rq.m + i + 1) : some;
         const T* src = reinterpret_cast<const T*>(p.q + (int64_t)(rq.row + i) * p.q_stride) +
                        (int64_t)(kvh * g + gc - i * g) * D + q * (D / 4);
@@ -495,7 +483,7 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
       bf16x8 qf[NT][QP][W];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        const bool used = (COPIES == 1 ? nt * 16 + c : c % (16 / COPIES)) < cols;
+        const bool used = nt * 16 + c < cols;
 #pragma unroll
         for (int s = 0; s < W; ++s) {
           if constexpr (QP == 1) {
@@ -570,14 +558,8 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int x = 0; x < TILES; ++x)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              if (COPIES == 1) sc[nt][4 * x + j] = st[nt][x][j];
-              else sc[nt][j] = x == 0 || copy == x ? st[nt][x][j] : sc[nt][j];
-            }
-        // the lane's first position of the unit's first tile, and of its column's tile
-        const int p0 = kt * UNIT + 4 * q, c0 = p0 + (COPIES == 1 ? 0 : 16 * copy);
+          for (int i = 0; i < NV; ++i) sc[nt][i] = st[nt][i / 4][i % 4];
+        const int p0 = kt * UNIT + 4 * q;  // the lane's first position of the unit's first tile
         uint32_t vw[TILES][W], vs[TILES];
 #pragma unroll
         for (int x = 0; x < TILES; ++x) {
@@ -599,10 +581,10 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
           }
 #pragma unroll
           for (int i = 0; i < NV; ++i) {
-            const bool gone = !(in >> (COPIES == 1 ? i / 4 : copy) & 1);
+            const bool gone = !(in >> (i / 4) & 1);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
-              if (gone || c0 + 16 * (i / 4) + i % 4 >= limit[nt]) sc[nt][i] = -INFINITY;
+              if (gone || p0 + 16 * (i / 4) + i % 4 >= limit[nt]) sc[nt][i] = -INFINITY;
           }
           uint32_t nan = 0;
 #pragma unroll
@@ -617,7 +599,7 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
           nan_v = nan != 0;
         }
         // weights
-        uint32_t pw[NT][PP][NV / 2];
+        uint32_t pw[NT][PP][4];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           float mx = -INFINITY;
@@ -648,50 +630,37 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
 #pragma unroll
           for (int part = 0; part < PP; ++part)
 #pragma unroll
-            for (int i = 0; i < NV / 2; ++i) {
+            for (int i = 0; i < 4; ++i) {
               pw[nt][part][i] = pack_bf16(e[2 * i], e[2 * i + 1]);
               e[2 * i] -= __uint_as_float(pw[nt][part][i] << 16);
               e[2 * i + 1] -= __uint_as_float(pw[nt][part][i] & 0xffff0000u);
             }
         }
-        // a lane's words of its own tiles as the A operand of tiles 2y and 2y + 1
-        auto operand = [&](const uint32_t* own, int y) {
-          if constexpr (COPIES == 1) {
-            return __builtin_bit_cast(bf16x8, make_uint4(own[0], own[1], own[2], own[3]));
-          } else {
-            const bool lo = copy == 2 * y, hi = copy == 2 * y + 1;
-            return __builtin_bit_cast(bf16x8, make_uint4(lo ? own[0] : 0u, lo ? own[1] : 0u, hi ? own[0] : 0u,
-                                                         hi ? own[1] : 0u));
-          }
-        };
         if (!whole && __any(nan_v)) {
           // A NaN of V that some columns see and some do not: a product of ones counts,
           // for each column and dim, the NaN it sees; then V is 0 there.
+          uint32_t ind[4];
 #pragma unroll
-          for (int y = 0; y < TILES / 2; ++y) {
-            uint32_t ind[4];
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t two = nan_bytes(vs[i / 2]) >> (16 * (i % 2));  // of two positions
+            ind[i] = (two & 1) * 0x3f80u | (two >> 8 & 1) * 0x3f800000u;
+          }
+          const bf16x8 nf = __builtin_bit_cast(bf16x8, make_uint4(ind[0], ind[1], ind[2], ind[3]));
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            uint32_t seen[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              const uint32_t two = nan_bytes(vs[2 * y + i / 2]) >> (16 * (i % 2));  // of two positions
-              ind[i] = (two & 1) * 0x3f80u | (two >> 8 & 1) * 0x3f800000u;
+              const int pos = p0 + 16 * (i / 2) + 2 * (i % 2);
+              seen[i] = (pos < limit[nt] ? 0x3f80u : 0u) | (pos + 1 < limit[nt] ? 0x3f800000u : 0u);
             }
-            const bf16x8 nf = __builtin_bit_cast(bf16x8, make_uint4(ind[0], ind[1], ind[2], ind[3]));
+            const bf16x8 sf = __builtin_bit_cast(bf16x8, make_uint4(seen[0], seen[1], seen[2], seen[3]));
+            const f32x4 hits = __builtin_amdgcn_mfma_f32_16x16x32_bf16(sf, nf, f32x4{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-              uint32_t seen[NV / 2];
+            for (int j = 0; j < 4; ++j) {
+              const float add = hits[j] > 0.0f ? __builtin_nanf("") : 0.0f;
 #pragma unroll
-              for (int i = 0; i < NV / 2; ++i) {
-                const int pos = c0 + 16 * (i / 2) + 2 * (i % 2);
-                seen[i] = (pos < limit[nt] ? 0x3f80u : 0u) | (pos + 1 < limit[nt] ? 0x3f800000u : 0u);
-              }
-              const f32x4 hits =
-                  __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(seen, y), nf, f32x4{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                const float add = hits[j] > 0.0f ? __builtin_nanf("") : 0.0f;
-#pragma unroll
-                for (int d = 0; d < DT; ++d) o[nt][d][j] += add;
-              }
+              for (int d = 0; d < DT; ++d) o[nt][d][j] += add;
             }
           }
 #pragma unroll
@@ -708,36 +677,34 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
           }
         }
         // O += P V
+        bf16x8 pf[NT][PP];
 #pragma unroll
-        for (int y = 0; y < TILES / 2; ++y) {
-          bf16x8 pf[NT][PP];
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int part = 0; part < PP; ++part)
+            pf[nt][part] = __builtin_bit_cast(
+                bf16x8, make_uint4(pw[nt][part][0], pw[nt][part][1], pw[nt][part][2], pw[nt][part][3]));
+        static_for<DT / 2>([&](auto DS) {
+          constexpr int s = DS;  // dims 2s and 2s + 1 of the lane
+          uint32_t pr[8];
+          static_for<8>([&](auto I) {
+            constexpr int i = I, byte = i % 4 * (D / 32) + s;
+            pr[i] = pair_of<byte % 4>(vw[i / 4][byte / 4], scale_of(vs[i / 4], i % 4));
+          });
+          union { uint32_t w[4]; bf16x8 f; } lo, hi;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            lo.w[i] = __builtin_amdgcn_perm(pr[2 * i + 1], pr[2 * i], 0x05040100u);
+            hi.w[i] = __builtin_amdgcn_perm(pr[2 * i + 1], pr[2 * i], 0x07060302u);
+          }
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int part = 0; part < PP; ++part) pf[nt][part] = operand(pw[nt][part], y);
-          static_for<DT / 2>([&](auto DS) {
-            constexpr int s = DS;  // dims 2s and 2s + 1 of the lane
-            uint32_t pr[8];
-            static_for<8>([&](auto I) {
-              constexpr int i = I, byte = i % 4 * (D / 32) + s;
-              pr[i] = pair_of<byte % 4>(vw[2 * y + i / 4][byte / 4], scale_of(vs[2 * y + i / 4], i % 4));
-            });
-            union { uint32_t w[4]; bf16x8 f; } lo, hi;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              lo.w[i] = __builtin_amdgcn_perm(pr[2 * i + 1], pr[2 * i], 0x05040100u);
-              hi.w[i] = __builtin_amdgcn_perm(pr[2 * i + 1], pr[2 * i], 0x07060302u);
+            for (int part = 0; part < PP; ++part) {
+              o[nt][2 * s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pf[nt][part], lo.f, o[nt][2 * s], 0, 0, 0);
+              o[nt][2 * s + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pf[nt][part], hi.f, o[nt][2 * s + 1], 0, 0, 0);
             }
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-              for (int part = 0; part < PP; ++part) {
-                o[nt][2 * s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pf[nt][part], lo.f, o[nt][2 * s], 0, 0, 0);
-                o[nt][2 * s + 1] =
-                    __builtin_amdgcn_mfma_f32_16x16x32_bf16(pf[nt][part], hi.f, o[nt][2 * s + 1], 0, 0, 0);
-              }
-          });
-        }
+        });
         KVR_WAIT_LGKM0();  // the unit's records are in registers: the ring takes the next ones
         asm volatile("" ::: "memory");
         get = get == (RING - TILES) * REC ? 0 : get + TILES * REC;
@@ -746,9 +713,9 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
       }
 
       // ---- the columns' outputs, or what there is of them ----
-      // 16 rows at a time through the ring, a row's dims over the lanes; the copies of a
-      // column are merged on the way.  What stays open goes to the workspace, or at the
-      // stretch's end, where the ring has no more to take, stays where it is.
+      // 16 rows at a time through the ring, a row's dims over the lanes.  What stays open
+      // goes to the workspace, or at the stretch's end, where the ring has no more to take,
+      // stays where it is.
       const bool done = first == 0 && upto == rq.steps, stay = LOCAL && u >= u1;
       float* const rows = reinterpret_cast<float*>(ring);
       float* const part = stay ? rows : slots + (first > 0 ? 0 : 1) * p.part_cols * ROW<D>;
@@ -775,14 +742,16 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
         asm volatile("" ::: "memory");
       };
       const auto take_rows = [&](int nt, const float* tr) {
-        // 0: the rows are the partials
-        const int used = COPIES == 1 && stay && !done ? 0 : min(16 / COPIES, cols - nt * 16);
+        const int used = stay && !done ? 0 : min(16, cols - nt * 16);  // 0: the rows are the partials
 #pragma unroll 1
         for (int i0 = 0; i0 < used; i0 += AT_ONCE<D>) {
           const int i = i0 + lane / LANES<D>;
           if (i >= used) continue;
-          const Column v = merge_column<D, COPIES>(
-              [&](int k, auto load) { load(tr + (k * (16 / COPIES) + i) * ROW<D>); }, COPIES, lane);
+          Column v;
+          float2 ml;
+          load_part<D>(tr + i * ROW<D>, dim_of<D>(lane), ml, v.o);
+          v.m = ml.x;
+          v.l = ml.y;
           if (done) put_out<T, D, COLS>(p, rq.row, tile, nt * 16 + i, kvh, lane, v);
           else put_part<D>(part + (nt * 16 + i) * ROW<D>, lane, v);
         }
@@ -832,7 +801,8 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
     bool closed = lead < 0 && (ended & 1);
     while (!closed && at + n < WAVES && begun >> (at + n) & 1) closed = ended >> (at + n++) & 1;
     const int cols = __builtin_amdgcn_readlane(str.cols[which], at);
-    const int row = __builtin_amdgcn_readlane(str.row[which], at), tile = __builtin_amdgcn_readlane(str.tile[which], at);
+    const int row = __builtin_amdgcn_readlane(str.row[which], at);
+    const int tile = __builtin_amdgcn_readlane(str.tile[which], at);
     closed &= lead >= 0;  // all of the item is here
     float* slot = slots0 + at * pitch + which * p.part_cols * ROW<D>;
     if (lead >= 0 && !closed) open = OpenItem{cols, row, tile, at, 0};
@@ -869,7 +839,7 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
 // loads' way from other chiplets' caches: 3 us with few partials, 8.5 with 48 of 5
 // columns at 16 loads together (9.8 at 8).
 constexpr int PM_NT = 256;
-template <typename T, int D, typename S>
+template <typename T, int D, int NT>
 __global__ __launch_bounds__(PM_NT) void packed_attn_merge_kernel(PackedAttnParams p) {
   constexpr int WG = PA_NT / 64;
   const int nkv = p.packed.nkv, wg = blockIdx.x / nkv, kvh = blockIdx.x % nkv;
@@ -883,7 +853,7 @@ __global__ __launch_bounds__(PM_NT) void packed_attn_merge_kernel(PackedAttnPara
     for (int c0 = wave * AT_ONCE<D>; c0 < it.cols; c0 += PM_NT / 64 * AT_ONCE<D>) {
       const int col = c0 + lane / LANES<D>;
       if (col >= it.cols) continue;
-      put_out<T, D, S::COLS>(
+      put_out<T, D, 16 * NT>(
           p, it.row, it.tile, col, kvh, lane,
           merge_column<D, chunk>(
               [&](int i, auto load) { load((i == 0 ? lead : first + i * WG * pitch) + col * ROW<D>); }, it.groups,
@@ -894,21 +864,21 @@ __global__ __launch_bounds__(PM_NT) void packed_attn_merge_kernel(PackedAttnPara
   else merge(std::integral_constant<int, 16>{});
 }
 
-// The kernel for a call's columns per request: as few column tiles as take them, and
-// where a tile's half or quarter does, as many copies.
+// The kernel for a call's columns per request: as few column tiles as take them, at most
+// four (two in fp32 models, whose queries and weights are three numbers each); a request
+// with more has several items, which read its records again.
 struct Plan {
-  int nt, copies, cols, unit, occupancy, start;
+  int nt, cols, occupancy, start;
 };
 Plan plan_of(int dtype, int d, int g, int32_t max_query) {
   const int64_t cols = (int64_t)g * max_query;
-  const int copies = cols <= 8 ? 2 : 1;
   const int nt = cols <= 16 ? 1 : cols <= 32 || dtype == KV_F32 ? 2 : 4;
-  return Plan{nt, copies, 16 * nt / copies, 32, occupancy_of(dtype == KV_F32, d, nt), nt == 1 ? 4 : 2};
+  return Plan{nt, 16 * nt, occupancy_of(dtype == KV_F32, d, nt), nt == 1 ? 4 : 2};
 }
 
 // Units of one kv head at most, `start` more for each item.
 int64_t units_of(const Plan& pl, int R, int64_t rows, int g, int64_t max_len, int start) {
-  return (R + rows * g / pl.cols) * ((max_len + pl.unit - 1) / pl.unit + start);
+  return (R + rows * g / pl.cols) * ((max_len + UNIT - 1) / UNIT + start);
 }
 
 // Stretches per kv head, whole workgroups: a unit each where the chip holds as many waves
@@ -927,19 +897,18 @@ Stretching stretches_of(const Plan& pl, int nkv, int R, int64_t rows, int g, int
   return {(int)round_up(waves, PA_NT / 64), pl.start};
 }
 
-template <typename T, int D, typename S>
-void launch_shape(const PackedAttnParams& p, hipStream_t s) {
-  constexpr int OCC = occupancy_of(std::is_same<T, float>::value, D, S::NT);
+template <typename T, int D, int NT>
+void launch_tiles(const PackedAttnParams& p, hipStream_t s) {
+  constexpr int OCC = occupancy_of(std::is_same<T, float>::value, D, NT);
   const dim3 grid((unsigned)((int64_t)p.workers / (PA_NT / 64) * p.packed.nkv));
-  hipLaunchKernelGGL((packed_attn_kernel<T, D, S, OCC>), grid, dim3(PA_NT), 0, s, p);
-  hipLaunchKernelGGL((packed_attn_merge_kernel<T, D, S>), grid, dim3(PM_NT), 0, s, p);
+  hipLaunchKernelGGL((packed_attn_kernel<T, D, NT, OCC>), grid, dim3(PA_NT), 0, s, p);
+  hipLaunchKernelGGL((packed_attn_merge_kernel<T, D, NT>), grid, dim3(PM_NT), 0, s, p);
 }
 template <typename T, int D>
 void launch(const Plan& pl, const PackedAttnParams& p, hipStream_t s) {
-  if (pl.copies == 2) return launch_shape<T, D, Shape<1, 2>>(p, s);
-  if (pl.nt == 1) return launch_shape<T, D, Shape<1, 1>>(p, s);
-  if (pl.nt == 2) return launch_shape<T, D, Shape<2, 1>>(p, s);
-  if constexpr (std::is_same<T, bf16_t>::value) launch_shape<T, D, Shape<4, 1>>(p, s);
+  if (pl.nt == 1) return launch_tiles<T, D, 1>(p, s);
+  if (pl.nt == 2) return launch_tiles<T, D, 2>(p, s);
+  if constexpr (std::is_same<T, bf16_t>::value) launch_tiles<T, D, 4>(p, s);
 }
 
 // The workspace: what workgroups left open, then the waves' sums.
