@@ -6,11 +6,10 @@
 // (both terms of each are of one sign, so nothing cancels).  Over a chunk of the row t_v is
 // one operation, fma(c, z_v, -C) with C = c m rounded (m the chunk's): the rounding of C
 // shifts all t alike, and is taken out where chunks meet.  Where C is so large that its
-// rounding would count, t_v = (z_v - m) c.  (That everywhere: 61 us for the prompt below,
-// not 55.)  A row is cut into
-// chunks; a workgroup reads its chunk once, into registers, takes the chunk's C, l and
-// s from there and, where asked, its top_n entries; a second kernel merges the
-// chunks of each row in a fixed order.
+// rounding would count, t_v = (z_v - m) c.  (That everywhere: 61 us for 1024 rows of 151936
+// in bf16, not 55.)  A row is cut into chunks; a workgroup reads its chunk once, into
+// registers, takes the chunk's m, l and s from there and, where asked, its top_n entries;
+// a second kernel merges the chunks of each row in a fixed order.
 //
 // Top entries.  (value, lower index first) is one 64-bit key, so that all keys of a
 // row differ and the order is total.  A bound that at least top_n entries reach comes
@@ -20,8 +19,11 @@
 // by counting.  (Ranking the threads' values by counting took 1.7 us a chunk.)  Where
 // equal values make too many threads, the bound is the top_n-th of the threads' keys.
 //
-// Bound by HBM where rows are many (4 or 2 bytes a logit against one exp and some
-// six other operations), by latency where they are few.
+// What bounds it.  Many rows: HBM, one exp and some six other operations for 4 or 2 bytes:
+// 1024 rows of 151936 in bf16 55 us, 311 MB at 5.7 TB/s, and 4.8 the second kernel.  64 rows
+// of 128256 in fp32 with the 20 likeliest, 13 + 5.3 us: all chunks are in flight at once, so
+// their phases follow each other: 3.5 us (the last 6.4) until a chunk is there, 1.1 for m, l
+// and s, 1.3 for the bound, 2 for the entries.  One row: latency, 6 + 4 us.
 #include <algorithm>
 
 #include "common.h"

@@ -28,19 +28,19 @@
 // the output's own rounding where few positions weigh, and the products are not what
 // bounds the kernel.
 //
-// What bounds it, on 16 requests of 2048 - 16384 positions (8 kv heads of 128, 4 q heads
-// each, 124 MB of records), one query row each: 34 us (21 at a plain read's 6 TB/s).
-// Without the products and the softmax the loads take 31 us, without the loads the rest
-// takes 28; 9 us pass before the first record is there and after the last (the plan,
-// three loads that follow each other, the merges).  Two requests of 150 - 200 thousand
-// positions: 80 us (5 TB/s).  One to five query rows of 40 requests of 300 - 4000
-// positions (5 q heads a kv head, COLS 32): 41 us, the instructions of the softmax and
-// of the conversions.
-//   Workgroups a CU and records a ring: three and four.  Three and six took 36.4 us (a
-// little over half of the LDS left for the third), two and eight 38.6, four and four
-// 39.6 (registers spill).  Column tiles of 32 need two a CU: three took 60 us against 45.
-//   As many waves as run at once: one and a half times as many took 39 us, twice as
-// many 41; the stretches are equal, so more of them only merge more.
+// What bounds it: the records' way from HBM and what a call costs once.  16 requests of
+// 2048 - 16384 positions (8 kv heads of 128, 4 q heads each, 124 MB of records), one query
+// row each: 29.7 us; without the products and the softmax 28.0, without the loads 21.1.
+// 1.1 us of them are the plan, 4 the way to the first record (three loads that follow each
+// other, while other waves' records keep the memory busy), 2 the merges.  Two requests of
+// 150 - 200 thousand positions (403 MB): 78 us, without products and softmax the same.
+// One to five query rows of 40 requests of 300 - 4000 positions (5 q heads a kv head,
+// COLS 32, 88 MB): 35 us, 33 without products and softmax, 29 without loads.
+//   Workgroups a CU and records a ring: three and four.  Three and six took 31.2 us, two
+// and eight 33.7, four and four 31.1 (the long ones 79, 85 and 81).  Two column tiles need
+// the registers of two a CU: with three, registers spill, 56 us against 35.
+//   As many waves as run at once: half as many more took 38 us, twice as many 37; the
+// stretches are equal, so more of them only merge more.
 #include <algorithm>
 #include <type_traits>
 
@@ -836,8 +836,8 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
 
 // Workgroup (kv head, workgroup of the first kernel): the item that it began and left
 // open, merged over the workgroups that went on with it, in their order.  Its time is its
-// loads' way from other chiplets' caches: 3 us with few partials, 8.5 with 48 of 5
-// columns at 16 loads together (9.8 at 8).
+// loads' way from other chiplets' caches: 3 us with few partials, 7.8 with 48 of 5
+// columns at 16 loads together (8.5 at 8).
 constexpr int PM_NT = 256;
 template <typename T, int D, int NT>
 __global__ __launch_bounds__(PM_NT) void packed_attn_merge_kernel(PackedAttnParams p) {

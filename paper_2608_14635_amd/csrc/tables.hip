@@ -14,7 +14,7 @@
 // requests: 4.4 us); of long ones the rows' writes are half (333 requests, 2.7 million
 // positions: 33 MB in 14.9 us), the rest each workgroup's way through scan, search and
 // free list.  (A workgroup that worked off two or four windows for each scan took 19 and
-// 28 us.)
+// 28 us; eight rows a thread 16.7, 256 threads 15.5, 1024 18.5.)
 #include <algorithm>
 
 #include "host.h"
