@@ -25,6 +25,7 @@
 // their phases follow each other: 3.5 us (the last 6.4) until a chunk is there, 1.1 for m, l
 // and s, 1.3 for the bound, 2 for the entries.  One row: latency, 6 + 4 us.
 #include <algorithm>
+#include <type_traits>
 
 #include "common.h"
 #include "host.h"
@@ -96,10 +97,27 @@ __device__ __forceinline__ uint64_t make_key(uint32_t order, uint32_t index) {
 }
 __device__ __forceinline__ uint32_t key_index(uint64_t k) { return 0xffffffffu - (uint32_t)k; }
 
-__device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
-  return v;
+// f over the wave's lanes, in every lane: neighbours, pairs, fours and eights of a row of
+// 16 by lane moves within it, then the rows.
+template <typename F>
+__device__ __forceinline__ float over_wave(float v, F f) {
+  const auto moved = [&](auto ctrl) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(ctrl)::value, 0xf, 0xf, true));
+  };
+  v = f(v, moved(std::integral_constant<int, 0xb1>{}));   // quad_perm 1 0 3 2
+  v = f(v, moved(std::integral_constant<int, 0x4e>{}));   // quad_perm 2 3 0 1
+  v = f(v, moved(std::integral_constant<int, 0x141>{}));  // row_half_mirror
+  v = f(v, moved(std::integral_constant<int, 0x140>{}));  // row_mirror
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = f(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return f(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float max_over_wave(float v) {
+  return over_wave(v, [](float a, float b) { return fmaxf(a, b); });
+}
+__device__ __forceinline__ float sum_over_wave(float v) {
+  return over_wave(v, [](float a, float b) { return a + b; });
 }
 
 // Ranks by counting: how many of the n keys in LDS are larger.
@@ -121,9 +139,11 @@ struct TopScratch {
   int count;
 };
 
-// Wave 0: a value that at least `top` and at most `most` of the threads' largest reach.
+// One wave: a value that at least `top` and at most `most` of the threads' largest reach.
+// First the longest run of the leading bits of `upper` (no smaller than any of them) that
+// enough of them reach, then bit by bit.
 template <typename S>
-__device__ __forceinline__ void find_bound(int top, S& s) {
+__device__ __forceinline__ void find_bound(int top, uint32_t upper, S& s) {
   const int most = min(64, 2 * top + 8);
   const int lane = threadIdx.x & 63;
   uint32_t u[LP_NT / 64];
@@ -136,9 +156,23 @@ __device__ __forceinline__ void find_bound(int top, S& s) {
     return n;
   };
   uint32_t bound = 0;
-  int n = LP_NT;
+  int n = LP_NT, free = 32;  // the lowest bits of the bound that are 0
 #pragma unroll 1
-  for (int b = 31; b >= 0 && n > most; --b) {
+  for (int low = 0; low < free;) {
+    const int mid = (low + free) / 2;
+    const uint32_t v = upper & ~0u << mid;
+    const int k = reach(v);
+    if (k >= top) {
+      bound = v;
+      n = k;
+      free = mid;
+    } else {
+      low = mid + 1;
+    }
+  }
+  // upper's next bit is 1, and with it too few reach
+#pragma unroll 1
+  for (int b = free - 2; b >= 0 && n > most; --b) {
     const uint32_t v = bound | 1u << b;
     const int k = reach(v);
     if (k >= top) {
@@ -184,8 +218,8 @@ __device__ __forceinline__ bool by_c(float c) { return fabsf(c) < 0x1p20f; }
 
 // Sums and maximum over the workgroup, in every thread; red holds a value a wave.
 __device__ __forceinline__ float2 block_total(float a, float b, float2* red) {
-  a = wave_sum(a);
-  b = wave_sum(b);
+  a = sum_over_wave(a);
+  b = sum_over_wave(b);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = make_float2(a, b);
   __syncthreads();
   float2 v = red[0];
@@ -197,7 +231,7 @@ __device__ __forceinline__ float2 block_total(float a, float b, float2* red) {
   return v;
 }
 __device__ __forceinline__ float block_most(float v, float* red) {
-  v = wave_max(v);
+  v = max_over_wave(v);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
   __syncthreads();
 #pragma unroll
@@ -245,7 +279,12 @@ __global__ __launch_bounds__(LP_NT) void logprob_chunk_kernel(LogprobParams p) {
     own = fmaxf(own, most[i]);
   }
   // nothing but -infinity (or NaN): sums of zeros (or NaN)
+  __shared__ typename std::conditional<TOP, TopScratch<LP_ITEMS>, int>::type s_top;
+  if constexpr (TOP) s_top.own[t] = order_bits(own);
   const float m = block_most(own, s_most);
+  // a wave finds the bound first (of the workgroups of a CU, which come 256 apart, not the same one)
+  if constexpr (TOP)
+    if (t / 64 == (blockIdx.x >> 8) % (LP_NT / 64)) find_bound(p.top, order_bits(m), s_top);
   float l = 0.0f, s = 0.0f;
   const float base = base_of(m), cm = c_of(base, p.scale2);
   auto add = [&](float x) {
@@ -267,11 +306,6 @@ __global__ __launch_bounds__(LP_NT) void logprob_chunk_kernel(LogprobParams p) {
   const float2 sums = block_total(l, s, s_sums);
   if (t == 0) p.stats[row * p.chunks + c] = make_float4(m, sums.x, sums.y, 0.0f);
   if constexpr (TOP) {
-    __shared__ TopScratch<LP_ITEMS> s_top;
-    s_top.own[t] = order_bits(own);
-    __syncthreads();
-    if (t < 64) find_bound(p.top, s_top);
-    __syncthreads();
     uint64_t bound = (uint64_t)s_top.bound << 32;
     const auto key_at = [&](int at) {  // past the vocabulary: as NaN of higher indices, below all others
       return make_key(at < p.vocab ? order_bits(Elem<T>::load(z, at)) : 0u, at);
@@ -335,7 +369,7 @@ __global__ __launch_bounds__(LP_NT) void logprob_row_kernel(LogprobParams p) {
   // every wave merges all chunks, in the same order
   float m = -INFINITY;
   for (int c = lane; c < p.chunks; c += 64) m = fmaxf(m, stats[c].x);
-  m = wave_max(m);
+  m = max_over_wave(m);
   const float base = base_of(m);
   float l = 0.0f, s = 0.0f;
   for (int c = lane; c < p.chunks; c += 64) {
@@ -347,8 +381,8 @@ __global__ __launch_bounds__(LP_NT) void logprob_row_kernel(LogprobParams p) {
     l = fmaf(q.y, e, l);
     s += e * fmaf(x, q.y, q.z);
   }
-  l = wave_sum(l);
-  s = wave_sum(s);
+  l = sum_over_wave(l);
+  s = sum_over_wave(s);
   const bool none = l == 0.0f;  // every logit -infinity
   const float log_l = none ? 0.0f : log2f(l);
   auto logprob = [&](float v) { return none ? -INFINITY : (v - base) * p.scale - LN2 * log_l; };
@@ -364,7 +398,7 @@ __global__ __launch_bounds__(LP_NT) void logprob_row_kernel(LogprobParams p) {
     __shared__ TopScratch<64> s_top;
     s_top.own[t] = (uint32_t)(own >> 32);
     __syncthreads();
-    if (t < 64) find_bound(p.top, s_top);
+    if (t < 64) find_bound(p.top, order_bits(m), s_top);
     __syncthreads();
     uint64_t bound = (uint64_t)s_top.bound << 32;
     if (s_top.bound == 0xffffffffu) bound = bound_of_keys(own, p.top, s_top);
