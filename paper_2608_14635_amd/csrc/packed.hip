@@ -85,8 +85,8 @@ __device__ __forceinline__ uint32_t encode8(const float* v, uint32_t& byte) {
   uint32_t most = 0;  // of |x|'s bits: they order as the values do, infinities and NaN above all
 #pragma unroll
   for (int i = 0; i < 8; ++i) most = max(most, __float_as_uint(v[i]) & 0x7fffffffu);
-  most = max(most, (uint32_t)__shfl_xor((int)most, 1, 64));
-  most = max(most, (uint32_t)__shfl_xor((int)most, 2, 64));
+  most = max(most, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)most, 0xb1, 0xf, 0xf, true));  // quad_perm 1 0 3 2
+  most = max(most, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)most, 0x4e, 0xf, 0xf, true));  // quad_perm 2 3 0 1
   byte = scale_byte(most);
   const float s = __uint_as_float(byte << 23);
   uint32_t c = 0;

@@ -127,12 +127,18 @@ __device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
 // a / b of whole numbers: a correctly rounded quotient of such small ones never reaches
 // the next whole number
 __device__ __forceinline__ uint32_t quotient(uint32_t a, uint32_t b) { return (uint32_t)((double)a / (double)b); }
-// The maximum of the four lanes (q, c) of a c.
+// The maximum, the sum over the four lanes (q, c) of a c.
 __device__ __forceinline__ float max_over_q(float v) {
   const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
   const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float sum_over_q(float v) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 // Stretches: all units in workers parts, equal but for LATER units: the waves of a CU's
 // second workgroup take that many fewer than those of its first, its third's twice as
@@ -720,8 +726,7 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
       float* const rows = reinterpret_cast<float*>(ring);
       float* const part = stay ? rows : slots + (first > 0 ? 0 : 1) * p.part_cols * ROW<D>;
       const auto put_rows = [&](int nt, float* tr) {
-        float l = l_run[nt] + __shfl_xor(l_run[nt], 16, 64);
-        l += __shfl_xor(l, 32, 64);
+        const float l = sum_over_q(l_run[nt]);
         if (q == 0) {
           *reinterpret_cast<float2*>(tr + c * ROW<D> + D) = make_float2(m_run[nt], l);
         }
