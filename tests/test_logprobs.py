@@ -204,6 +204,34 @@ def test_logits_of_any_size(dt):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dt", list(DT))
+def test_the_largest_vocabulary(dt):
+    V = 1 << 21
+    g = torch.Generator().manual_seed(9)
+    z = torch.stack([torch.randn(V, generator=g) * 3, torch.randint(0, 5, (V,), generator=g).float(), torch.zeros(V)])
+    c = Call(z.to(DT[dt]), 1.0, [V - 1, 0, V // 2], 64)
+    c.run()
+    c.check()
+
+
+@pytest.mark.gpu
+def test_more_rows_than_a_short_grid():
+    R, V = (1 << 17) + 3, 37
+    z, tok = random_rows(R, V, torch.float32, 10)
+    c = Call(z, 1.0, tok)
+    c.run()
+    x = z.double() - z.double().amax(1, keepdim=True)
+    lse = x.exp().sum(1).log()
+    p = (x - lse[:, None]).exp()
+    X = (p * x.abs()).sum(1)
+    xt = x.gather(1, torch.as_tensor(tok)[:, None])[:, 0]
+    base = (400 + 2 * X) * U + 4 * U * lse
+    near(c.lp[:R].cpu().numpy(), (xt - lse).numpy(), (base + 3 * U * xt.abs()).numpy())
+    near(c.ent[:R].cpu().numpy(), (lse + X).numpy(), ((800 + 4 * X) * U * (1 + X) + 4 * U * (lse + X)).numpy())
+    assert (c.lp[R:] == KEPT).all()
+
+
+@pytest.mark.gpu
 def test_outputs_not_wanted():
     z, tok = random_rows(4, 5000, torch.float32, 3)
     for want, top in (((True, False), 0), ((False, True), 0), ((False, False), 4), ((True, False), 2)):
@@ -262,6 +290,12 @@ def test_workspace_bytes():
     for bad in ((0, 100, 0), (-1, 100, 0), (1 << 21, 100, 0), (1, 0, 0), (1, (1 << 21) + 1, 0), (1, 100, -1),
                 (1, 100, 65), (1, 10, 11), (1 << 20, 131073, 0), (1 << 16, 1 << 21, 0)):
         assert kvr.kv_logprobs_workspace_bytes(*bad) == 0
+
+
+def test_a_device_that_is_not_there():
+    with pytest.raises(kvr.KvError) as e:
+        kvr.kv_logprobs(0x1000, kvr.KV_F32, 4, 1000, 1000, 1.0, 0x2000, 0, 0x3000, 0, 0, 0, 0x10000, 1 << 20, device=4096)
+    assert e.value.status == kvr.KV_EDEVICE and e.value.message
 
 
 @pytest.mark.parametrize("bad,status", [

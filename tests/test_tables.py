@@ -188,3 +188,9 @@ def test_tables_grow_refusals(bad):
     with pytest.raises(kvr.KvError) as e:
         call_with(**bad)
     assert e.value.status == kvr.KV_EINVAL and e.value.message
+
+
+def test_tables_grow_on_a_device_that_is_not_there():
+    with pytest.raises(kvr.KvError) as e:
+        call_with(device=4096)
+    assert e.value.status == kvr.KV_EDEVICE and e.value.message
