@@ -88,6 +88,7 @@ struct PackedAttnParams {
   int max_query;                 // rows of a request past it are left out: the sums have no room
   int most_len;                  // positions of a request: max_len, or what its table holds
   int start;                     // units that an item's start counts as
+  int whole;                     // units of a stretch where a workgroup has an item to itself, else 0
   int workers;                   // stretches per kv head, a multiple of four
   int part_cols;                 // columns of a slot of sums
   OpenItem* open;                // [workers / 4]
@@ -151,9 +152,15 @@ template <int OCC>
 struct Stretches {
   // the first `longer` ones are a unit longer; turn: waves of the CUs' first workgroups
   uint32_t workers, size, longer, turn, later;
-  __device__ __forceinline__ Stretches(uint32_t most, uint32_t total) {
-    workers = min(most, total);  // a unit each at least
+  __device__ __forceinline__ Stretches(uint32_t most, uint32_t total, uint32_t whole) {
     turn = most / OCC;
+    if (whole) {
+      workers = most;
+      size = whole;
+      longer = later = 0;
+      return;
+    }
+    workers = min(most, total);  // a unit each at least
     later = OCC > 1 && total / (2 * LATER) >= most ? LATER : 0;
     total += less(workers);
     size = total ? quotient(total, workers) : 0;
@@ -189,7 +196,7 @@ __device__ __forceinline__ Request make_request(const PackedAttnParams& p, int r
   q.len = max(0, min(want, p.most_len));
   q.tiles = (int)(((int64_t)m * p.g + COLS - 1) / COLS);
   q.steps = max(1, (int)(((int64_t)q.len + UNIT - 1) / UNIT));
-  q.item = (uint32_t)(q.steps + p.start);
+  q.item = (uint32_t)(p.whole ? p.whole * (PA_NT / 64) : q.steps + p.start);
   return q;
 }
 template <int COLS>
@@ -383,7 +390,7 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
     total += s_wave[i];
   }
   total = __builtin_amdgcn_readfirstlane(total);
-  const Stretches<OCC> st(p.workers, total);
+  const Stretches<OCC> st(p.workers, total, p.whole);
   // the thread whose requests hold a wave's first unit says so
 #pragma unroll
   for (int i = 0; i < WAVES; ++i) {
@@ -422,7 +429,7 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
       }
       const int tile = (int)quotient(u - base, rq.item);
       const uint32_t from = u - base - (uint32_t)tile * rq.item, to = min(rq.item, from + (u1 - u));
-      const int first = max((int)from - p.start, 0), upto = (int)to - p.start;
+      const int start = (int)rq.item - rq.steps, first = max((int)from - start, 0), upto = (int)to - start;
       u += to - from;
       if (upto <= 0) continue;  // of the start alone
       const int cols = min(COLS, rq.m * g - tile * COLS);  // of this tile
@@ -875,31 +882,47 @@ __global__ __launch_bounds__(PM_NT) void packed_attn_merge_kernel(PackedAttnPara
 struct Plan {
   int nt, cols, occupancy, start;
 };
-Plan plan_of(int dtype, int d, int g, int32_t max_query) {
-  const int64_t cols = (int64_t)g * max_query;
+Plan plan_of(int dtype, int d, int g, int64_t max_query) {
+  const int64_t cols = g * max_query;
   const int nt = cols <= 16 ? 1 : cols <= 32 || dtype == KV_F32 ? 2 : 4;
   return Plan{nt, 16 * nt, occupancy_of(dtype == KV_F32, d, nt), nt == 1 ? 4 : 2};
 }
 
-// Units of one kv head at most, `start` more for each item.
-int64_t units_of(const Plan& pl, int R, int64_t rows, int g, int64_t max_len, int start) {
-  return (R + rows * g / pl.cols) * ((max_len + UNIT - 1) / UNIT + start);
-}
-
-// Stretches per kv head, whole workgroups: a unit each where the chip holds as many waves
-// at once, else those waves.  Then an item's start counts as `start` units more: a wave
-// whose stretch goes on with another item ends the one and waits for the other's table,
-// queries and first records, some 4 us, and the waves should end together.  One column
-// tile: four, 30.8 us on 16 requests and 19.9 on 64 (33.2 and 22.3 with none, 31.0 and
-// 21.0 with two); several, whose units take longer: two, 35.5 us on 40 requests of one to
-// five rows and 69 on 8 of 64 (41.0 and 78 with none, 36.1 and 71 with four).
-struct Stretching {
-  int workers, start;
+// Items of one kv head, and their units, at most: of a call's R requests with `rows` query
+// rows in all, max_query of one, and max_len positions.
+struct Sizes {
+  int R, g;
+  int64_t rows, max_query, max_len;
+  int64_t items(int cols) const {
+    return std::min(R + rows * g / cols, R * ((max_query * g + cols - 1) / cols));
+  }
+  int64_t steps() const { return (max_len + UNIT - 1) / UNIT; }
 };
-Stretching stretches_of(const Plan& pl, int nkv, int R, int64_t rows, int g, int64_t max_len) {
-  const int64_t units = units_of(pl, R, rows, g, max_len, 0), waves = (256 * 4 * pl.occupancy + nkv - 1) / nkv;
-  if (units <= waves) return {(int)round_up(std::max<int64_t>(1, units), PA_NT / 64), 0};
-  return {(int)round_up(waves, PA_NT / 64), pl.start};
+
+// Stretches per kv head, whole workgroups.
+//   A workgroup to an item, its four waves equal parts of it, where the chip holds all of
+// them at once and a part is at most WHOLE units: nothing is left to merge between
+// workgroups, and the second kernel is not launched.  A call on 90 requests of up to 250
+// positions took 11.1 us so and 15.0 the other way, 16 of up to 500 9.7 and 11.6; parts of
+// eight, 16 of up to 1000, 14.9 and 13.2.
+//   Else a unit each where the chip holds as many waves at once, else those waves.  Then an
+// item's start counts as `start` units more: a wave whose stretch goes on with another item
+// ends the one and waits for the other's table, queries and first records, some 4 us, and
+// the waves should end together.  One column tile: four, 30.8 us on 16 requests and 19.9 on
+// 64 (33.2 and 22.3 with none, 31.0 and 21.0 with two); several, whose units take longer:
+// two, 35.5 us on 40 requests of one to five rows and 69 on 8 of 64 (41.0 and 78 with none,
+// 36.1 and 71 with four).
+constexpr int64_t WHOLE = 4;
+struct Stretching {
+  int workers, start, whole;
+};
+int64_t most_waves(const Plan& pl, int nkv) { return (256 * 4 * pl.occupancy + nkv - 1) / nkv; }
+Stretching stretches_of(const Plan& pl, int nkv, const Sizes& z) {
+  const int64_t items = z.items(pl.cols), units = items * z.steps(), waves = most_waves(pl, nkv);
+  const int64_t part = (z.steps() + 3) / 4;
+  if (part <= WHOLE && 4 * items <= waves) return {(int)(4 * items), 0, (int)part};
+  if (units <= waves) return {(int)round_up(units, PA_NT / 64), 0, 0};
+  return {(int)round_up(waves, PA_NT / 64), pl.start, 0};
 }
 
 template <typename T, int D, int NT>
@@ -907,7 +930,7 @@ void launch_tiles(const PackedAttnParams& p, hipStream_t s) {
   constexpr int OCC = occupancy_of(std::is_same<T, float>::value, D, NT);
   const dim3 grid((unsigned)((int64_t)p.workers / (PA_NT / 64) * p.packed.nkv));
   hipLaunchKernelGGL((packed_attn_kernel<T, D, NT, OCC>), grid, dim3(PA_NT), 0, s, p);
-  hipLaunchKernelGGL((packed_attn_merge_kernel<T, D, NT>), grid, dim3(PM_NT), 0, s, p);
+  if (!p.whole) hipLaunchKernelGGL((packed_attn_merge_kernel<T, D, NT>), grid, dim3(PM_NT), 0, s, p);
 }
 template <typename T, int D>
 void launch(const Plan& pl, const PackedAttnParams& p, hipStream_t s) {
@@ -916,22 +939,24 @@ void launch(const Plan& pl, const PackedAttnParams& p, hipStream_t s) {
   if constexpr (std::is_same<T, bf16_t>::value) launch_tiles<T, D, 4>(p, s);
 }
 
-// The workspace: what workgroups left open, then the waves' sums.
+// The workspace: what workgroups left open, then the waves' sums.  It is as large as any
+// call of no larger sizes needs, whichever kernel that one takes.
 struct AttnLayout {
-  Plan plan;
-  Stretching stretches;
-  int cols;
   uint64_t part, total;
 };
-AttnLayout attn_layout(const kv_model_desc& d, int32_t R, int64_t rows, int32_t max_query, int64_t max_len) {
+AttnLayout attn_layout(const kv_model_desc& d, const Sizes& z) {
+  int64_t workers = 0, columns = 0;
+  const Plan own = plan_of(d.dtype, d.head_dim, z.g, z.max_query);
+  for (int nt = 1; nt <= own.nt; nt *= 2) {
+    const Plan pl = plan_of(d.dtype, d.head_dim, 1, 16 * nt);
+    const int64_t units = z.items(pl.cols) * std::max<int64_t>(4, z.steps());
+    const int64_t w = round_up(std::min(most_waves(pl, d.num_kv_heads), units), PA_NT / 64);
+    workers = std::max(workers, w);
+    columns = std::max(columns, w * std::min<int64_t>(pl.cols, z.g * z.max_query));
+  }
   AttnLayout L;
-  const int g = d.num_q_heads / d.num_kv_heads;
-  L.plan = plan_of(d.dtype, d.head_dim, g, max_query);
-  L.stretches = stretches_of(L.plan, d.num_kv_heads, R, rows, g, max_len);
-  const int64_t workers = L.stretches.workers;
-  L.cols = (int)std::min<int64_t>(L.plan.cols, (int64_t)g * max_query);
   L.part = (uint64_t)round_up(workers / (PA_NT / 64) * (int64_t)sizeof(OpenItem), 256);
-  L.total = L.part + (uint64_t)4 * d.num_kv_heads * workers * 2 * L.cols * row_of(d.head_dim);
+  L.total = L.part + (uint64_t)(4 * d.num_kv_heads * 2 * columns * row_of(d.head_dim));
   return L;
 }
 
@@ -962,18 +987,21 @@ void run(const kv_packed* packed, int32_t layer, const void* q, int64_t q_stride
   p.max_blocks = max_blocks;
   p.g = d.num_q_heads / d.num_kv_heads;
   p.g_inv = p.g == 1 ? 0 : (uint32_t)(((1ull << 32) + p.g - 1) / p.g);
-  const AttnLayout L = attn_layout(d, R, rows, max_query, max_len);
+  const Sizes z{R, p.g, rows, max_query, max_len};
+  const Plan plan = plan_of(d.dtype, d.head_dim, p.g, max_query);
+  const Stretching st = stretches_of(plan, d.num_kv_heads, z);
   p.max_query = max_query;
   p.most_len = (int)std::min<int64_t>({max_len, (int64_t)max_blocks * packed->block_size, INT32_MAX - 64});
-  p.start = L.stretches.start;
-  p.workers = L.stretches.workers;
-  p.part_cols = L.cols;
+  p.start = st.start;
+  p.whole = st.whole;
+  p.workers = st.workers;
+  p.part_cols = (int)std::min<int64_t>(plan.cols, (int64_t)p.g * max_query);
   p.open = static_cast<OpenItem*>(workspace);
-  p.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + L.part);
-  if (d.dtype == KV_BF16) launch<bf16_t, 128>(L.plan, p, s);
-  else if (d.head_dim == 128) launch<float, 128>(L.plan, p, s);
-  else if (d.head_dim == 64) launch<float, 64>(L.plan, p, s);
-  else launch<float, 32>(L.plan, p, s);
+  p.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + attn_layout(d, z).part);
+  if (d.dtype == KV_BF16) launch<bf16_t, 128>(plan, p, s);
+  else if (d.head_dim == 128) launch<float, 128>(plan, p, s);
+  else if (d.head_dim == 64) launch<float, 64>(plan, p, s);
+  else launch<float, 32>(plan, p, s);
 }
 
 }  // namespace
@@ -993,7 +1021,7 @@ uint64_t kv_packed_attention_workspace_bytes(const kv_model_desc* desc, int32_t 
   if (num_requests <= 0 || num_requests > MOST_ROWS || rows <= 0 || rows > MOST_ROWS || max_query <= 0 ||
       max_len <= 0 || max_len > INT32_MAX)
     return 0;
-  return attn_layout(*desc, num_requests, rows, max_query, max_len).total;
+  return attn_layout(*desc, {num_requests, desc->num_q_heads / desc->num_kv_heads, rows, max_query, max_len}).total;
 }
 
 kv_status kv_packed_attention(kv_packed_t packed, int32_t layer, const void* q, int64_t q_stride,
@@ -1022,8 +1050,8 @@ kv_status kv_packed_attention(kv_packed_t packed, int32_t layer, const void* q, 
   if (!workspace || (uintptr_t)workspace % 16 != 0)
     return kvr_err::set(KV_EINVAL, "null workspace, or one not on a boundary of 16 bytes");
   const Plan plan = plan_of(d.dtype, d.head_dim, d.num_q_heads / d.num_kv_heads, max_query);
-  if (max_len > INT32_MAX ||
-      units_of(plan, R, rows, d.num_q_heads / d.num_kv_heads, max_len, plan.start) > INT32_MAX)
+  const Sizes z{R, d.num_q_heads / d.num_kv_heads, rows, max_query, max_len};
+  if (max_len > INT32_MAX || (R + rows * z.g / plan.cols) * (z.steps() + plan.start) > INT32_MAX)
     return kvr_err::set(KV_EINVAL, "max_len or the work of one call above 2^31: split the query rows");
   const uint64_t need = kv_packed_attention_workspace_bytes(&d, R, rows, max_query, max_len);
   if (need > ws_bytes)

@@ -392,6 +392,17 @@ def test_workspace_bytes():
     assert kvr.kv_packed_attention_workspace_bytes(wide, 4, 4, 1, 1000) == 0
 
 
+@pytest.mark.parametrize("name,g", [("bf16", 1), ("bf16", 4), ("bf16", 16), ("f32_32", 3), ("f32_128", 4)])
+def test_workspaces_take_every_smaller_call(name, g):
+    s, rng = heads(name, g), np.random.default_rng(5)
+    sizes = lambda: [int(2 ** rng.uniform(0, e)) for e in (9, 12, 7, 16)]  # noqa: E731
+    for _ in range(3000):
+        big = sizes()
+        small = [int(rng.integers(1, n + 1)) if rng.random() < 0.7 else n for n in big]
+        a, b = (kvr.kv_packed_attention_workspace_bytes(s, *x) for x in (small, big))
+        assert 0 < a <= b, (small, big)
+
+
 def test_attention_of_an_unknown_arena_is_refused():
     with pytest.raises(kvr.KvError) as e:
         kvr.kv_packed_attention(0x1234, 0, 0x1000, 4096, 0, 1, 0x2000, 0x3000, 1, 1, 1, 16, 0x4000, 4096, 0x10000, 1 << 20)
