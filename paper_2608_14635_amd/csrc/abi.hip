@@ -383,6 +383,15 @@ DecodeLayout make_decode_layout(const kv_model_desc& d, int32_t R, int64_t max_p
   return L;
 }
 
+// What any step of up to R requests needs: the split products take fewer K ranges of more
+// rows, from steps of 16 rows (up to 64) and of 256 on (one range from 65536 on).
+uint64_t decode_bytes(const kv_model_desc& d, int32_t R, int64_t max_position, bool packed) {
+  uint64_t most = make_decode_layout(d, R, max_position, packed).total;
+  for (int32_t r = 16; r < R && r <= 65536; r = r < 64 ? r + 16 : r == 64 ? 256 : r + 256)
+    most = std::max<uint64_t>(most, make_decode_layout(d, r, max_position, packed).total);
+  return most;
+}
+
 kv_status check_decode(const kv_model_desc* desc, int32_t B, int64_t NB, const int32_t* tokens,
                        const int32_t* positions, int32_t R, const int32_t* tables,
                        int32_t max_blocks, int64_t* max_pos_out) {
@@ -1052,7 +1061,7 @@ kv_status kv_rebuild(const kv_weights* w, const int32_t* tokens, const int32_t* 
 uint64_t kv_decode_workspace_bytes(const kv_model_desc* desc, int32_t num_requests,
                                    int64_t max_position) {
   if (check_desc(desc) != KV_OK || num_requests <= 0 || max_position <= 0) return 0;
-  return make_decode_layout(*desc, num_requests, max_position, false).total;
+  return decode_bytes(*desc, num_requests, max_position, false);
 }
 
 kv_status kv_decode_check(const kv_model_desc* desc, int32_t block_size, int64_t num_blocks,
@@ -1373,7 +1382,7 @@ uint64_t kv_packed_decode_workspace_bytes(const kv_model_desc* desc, int32_t num
   if (num_requests <= 0 || max_position <= 0 ||
       kv_packed_attention_workspace_bytes(desc, num_requests, num_requests, 1, max_position) == 0)
     return 0;
-  return make_decode_layout(*desc, num_requests, max_position, true).total;
+  return decode_bytes(*desc, num_requests, max_position, true);
 }
 
 kv_status kv_packed_decode_step(const kv_weights* w, const void* final_norm, const void* lm_head,

@@ -278,6 +278,16 @@ def test_a_captured_serving_step():
     b.arena.release()
 
 
+@pytest.mark.parametrize("name", ["tiny_f32", "qwen3_8b_2l", "g16_bf16"])
+def test_packed_decode_workspaces_take_every_smaller_step(name):
+    shape, rng = CASES[name][0], np.random.default_rng(6)
+    for _ in range(1000):
+        R, n = (int(2 ** rng.uniform(0, e)) for e in (8, 17))
+        r, m = int(rng.integers(1, R + 1)), int(rng.integers(1, n + 1))
+        for size in (kvr.kv_packed_decode_workspace_bytes, kvr.kv_decode_workspace_bytes):
+            assert 0 < size(shape, r, m) <= size(shape, R, n)
+
+
 def test_packed_decode_sizes_and_refusals():
     s = W.LLAMA8B
     a = kvr.kv_packed_decode_workspace_bytes(s, 4, 1000)
