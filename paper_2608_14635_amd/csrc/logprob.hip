@@ -20,10 +20,10 @@
 // equal values make too many threads, the bound is the top_n-th of the threads' keys.
 //
 // What bounds it.  Many rows: HBM, one exp and some six other operations for 4 or 2 bytes:
-// 1024 rows of 151936 in bf16 55 us, 311 MB at 5.7 TB/s, and 4.8 the second kernel.  64 rows
-// of 128256 in fp32 with the 20 likeliest, 13 + 5.3 us: all chunks are in flight at once, so
-// their phases follow each other: 3.5 us (the last 6.4) until a chunk is there, 1.1 for m, l
-// and s, 1.3 for the bound, 2 for the entries.  One row: latency, 6 + 4 us.
+// 1024 rows of 151936 in bf16 52 - 54 us, 311 MB at up to 6 TB/s, and 4.8 the second kernel.
+// 64 rows of 128256 in fp32 with the 20 likeliest, 12.5 + 4.8 us: all chunks are in flight at
+// once, so their phases follow each other: 3.5 us (the last 6.4) until a chunk is there, then
+// m, l and s, the bound beside them, the entries.  One row: latency, 5.2 + 3.5 us.
 #include <algorithm>
 #include <type_traits>
 
@@ -239,14 +239,66 @@ __device__ __forceinline__ float block_most(float v, float* red) {
   return v;
 }
 
-template <typename T, bool TOP>
+// A chunk's largest logit and sums, added to those of its row, whose t is relative to
+// `base`: by the two logits, and without the rounding of the chunk's C.
+__device__ __forceinline__ void add_chunk(float m, float chunk_l, float chunk_s, float base, float scale2, float& l,
+                                          float& s) {
+  const float cm = c_of(base_of(m), scale2), off = by_c(cm) ? fmaf(base_of(m), scale2, -cm) : 0.0f;
+  const float x = fmaxf(fmaf(m - base, scale2, -off), -1e30f);
+  const float e = __builtin_amdgcn_exp2f(x);
+  l = fmaf(chunk_l, e, l);
+  s += e * fmaf(x, chunk_l, chunk_s);
+}
+
+// A row's token and its logit, then the results from the row's sums.
+template <typename T>
+struct Row {
+  int64_t row;
+  int tok = -1;
+  float z = 0.0f;
+  float base, log_l, s_l;
+  bool none;  // every logit -infinity
+  __device__ __forceinline__ explicit Row(int64_t r) : row(r) {}
+  __device__ __forceinline__ void load(const LogprobParams& p) {
+    if (!p.logprobs) return;
+    tok = p.tokens[row];
+    if (tok >= 0 && tok < p.vocab) z = Elem<T>::load(reinterpret_cast<const T*>(p.logits + row * p.stride), tok);
+  }
+  __device__ __forceinline__ void sums(float m, float l, float s) {
+    base = base_of(m);
+    none = l == 0.0f;
+    log_l = none ? 0.0f : log2f(l);
+    s_l = s / l;
+  }
+  __device__ __forceinline__ float logprob(const LogprobParams& p, float v) const {
+    return none ? -INFINITY : (v - base) * p.scale - LN2 * log_l;
+  }
+  __device__ __forceinline__ void put(const LogprobParams& p) const {
+    if (p.logprobs)
+      p.logprobs[row] = tok < 0 ? 0.0f : tok < p.vocab ? logprob(p, z) : log_l != log_l ? log_l : -INFINITY;
+    if (p.entropy) {
+      const float h = LN2 * (log_l - s_l);
+      p.entropy[row] = none || h < 0.0f ? 0.0f : h;  // NaN stays
+    }
+  }
+  __device__ __forceinline__ void put_top(const LogprobParams& p, int rank, uint64_t key) const {
+    p.top_tokens[row * p.top + rank] = (int32_t)key_index(key);
+    p.top_logprobs[row * p.top + rank] = logprob(p, ordered_value((uint32_t)(key >> 32)));
+  }
+};
+
+// ONE: rows of one chunk, whose results it writes itself (a call on 64 rows of 5000 with the
+// 20 likeliest 6.9 us; 10.8 with the second kernel).
+template <typename T, bool TOP, bool ONE>
 __global__ __launch_bounds__(LP_NT) void logprob_chunk_kernel(LogprobParams p) {
   constexpr int VEC = Piece<T>::N, VECS = LP_ITEMS / VEC, STEP = LP_NT * VEC;
   __shared__ float s_most[LP_NT / 64];
   __shared__ float2 s_sums[LP_NT / 64];
   const int t = threadIdx.x;
-  const int c = blockIdx.x % p.chunks;
-  const int64_t row = blockIdx.x / p.chunks;
+  const int c = ONE ? 0 : blockIdx.x % p.chunks;
+  const int64_t row = ONE ? blockIdx.x : blockIdx.x / p.chunks;
+  Row<T> result(row);
+  if (ONE && t == 0) result.load(p);
   const T* z = reinterpret_cast<const T*>(p.logits + row * p.stride);
   const int begin = c * LP_CHUNK, first = begin + t * VEC;
   Piece<T> v[VECS];
@@ -304,7 +356,14 @@ __global__ __launch_bounds__(LP_NT) void logprob_chunk_kernel(LogprobParams p) {
       for (int j = 0; j < VEC; ++j) add((v[i].value(j) - base) * p.scale2);
   }
   const float2 sums = block_total(l, s, s_sums);
-  if (t == 0) p.stats[row * p.chunks + c] = make_float4(m, sums.x, sums.y, 0.0f);
+  if constexpr (ONE) {
+    l = s = 0.0f;
+    add_chunk(m, sums.x, sums.y, base, p.scale2, l, s);
+    result.sums(m, l, s);
+    if (t == 0) result.put(p);
+  } else {
+    if (t == 0) p.stats[row * p.chunks + c] = make_float4(m, sums.x, sums.y, 0.0f);
+  }
   if constexpr (TOP) {
     uint64_t bound = (uint64_t)s_top.bound << 32;
     const auto key_at = [&](int at) {  // past the vocabulary: as NaN of higher indices, below all others
@@ -344,8 +403,11 @@ __global__ __launch_bounds__(LP_NT) void logprob_chunk_kernel(LogprobParams p) {
     const int n = min(s_top.count, s_top.KEYS);
     uint64_t* out = p.keys + (row * p.chunks + c) * p.top;
     for (int i = t; i < n; i += LP_NT) {
-      const int r = rank_of(s_top.keys[i], s_top.keys, n);
-      if (r < p.top) out[r] = s_top.keys[i];
+      const uint64_t k = s_top.keys[i];
+      const int r = rank_of(k, s_top.keys, n);
+      if (r >= p.top) continue;
+      if (ONE) result.put_top(p, r, k);
+      else out[r] = k;
     }
   }
 }
@@ -360,39 +422,19 @@ __global__ __launch_bounds__(LP_NT) void logprob_row_kernel(LogprobParams p) {
   uint64_t own = t;  // threads without a key: below all of them, and different
   if (TOP)
     for (int i = t; i < total; i += LP_NT) own = max(own, keys[i]);
-  int tok = -1;
-  float z = 0.0f;
-  if (t == 0 && p.logprobs) {
-    tok = p.tokens[row];
-    if (tok >= 0 && tok < p.vocab) z = Elem<T>::load(reinterpret_cast<const T*>(p.logits + row * p.stride), tok);
-  }
+  Row<T> result(row);
+  if (t == 0) result.load(p);
   // every wave merges all chunks, in the same order
   float m = -INFINITY;
   for (int c = lane; c < p.chunks; c += 64) m = fmaxf(m, stats[c].x);
   m = max_over_wave(m);
-  const float base = base_of(m);
   float l = 0.0f, s = 0.0f;
   for (int c = lane; c < p.chunks; c += 64) {
     const float4 q = stats[c];
-    // the chunk's t to the row's: by its largest logit, and without the rounding of its C
-    const float cm = c_of(base_of(q.x), p.scale2), off = by_c(cm) ? fmaf(base_of(q.x), p.scale2, -cm) : 0.0f;
-    const float x = fmaxf(fmaf(q.x - base, p.scale2, -off), -1e30f);
-    const float e = __builtin_amdgcn_exp2f(x);
-    l = fmaf(q.y, e, l);
-    s += e * fmaf(x, q.y, q.z);
+    add_chunk(q.x, q.y, q.z, base_of(m), p.scale2, l, s);
   }
-  l = sum_over_wave(l);
-  s = sum_over_wave(s);
-  const bool none = l == 0.0f;  // every logit -infinity
-  const float log_l = none ? 0.0f : log2f(l);
-  auto logprob = [&](float v) { return none ? -INFINITY : (v - base) * p.scale - LN2 * log_l; };
-  if (t == 0) {
-    if (p.logprobs) p.logprobs[row] = tok < 0 ? 0.0f : tok < p.vocab ? logprob(z) : l != l ? l : -INFINITY;
-    if (p.entropy) {
-      const float h = LN2 * (log_l - s / l);
-      p.entropy[row] = none || h < 0.0f ? 0.0f : h;  // NaN stays
-    }
-  }
+  result.sums(m, sum_over_wave(l), sum_over_wave(s));
+  if (t == 0) result.put(p);
   if constexpr (TOP) {
     // a thread holds ceil(256 * 64 / 256) keys at most
     __shared__ TopScratch<64> s_top;
@@ -410,10 +452,7 @@ __global__ __launch_bounds__(LP_NT) void logprob_row_kernel(LogprobParams p) {
     for (int i = t; i < n; i += LP_NT) {
       const uint64_t k = s_top.keys[i];
       const int r = rank_of(k, s_top.keys, n);
-      if (r < p.top) {
-        p.top_tokens[row * p.top + r] = (int32_t)key_index(k);
-        p.top_logprobs[row * p.top + r] = logprob(ordered_value((uint32_t)(k >> 32)));
-      }
+      if (r < p.top) result.put_top(p, r, k);
     }
   }
 }
@@ -422,7 +461,12 @@ int chunks_of(int vocab) { return (vocab + LP_CHUNK - 1) / LP_CHUNK; }
 
 template <typename T, bool TOP>
 void launch(const LogprobParams& p, int64_t rows, hipStream_t s) {
-  hipLaunchKernelGGL((logprob_chunk_kernel<T, TOP>), dim3((unsigned)(rows * p.chunks)), dim3(LP_NT), 0, s, p);
+  const dim3 grid((unsigned)(rows * p.chunks));
+  if (p.chunks == 1) {
+    hipLaunchKernelGGL((logprob_chunk_kernel<T, TOP, true>), grid, dim3(LP_NT), 0, s, p);
+    return;
+  }
+  hipLaunchKernelGGL((logprob_chunk_kernel<T, TOP, false>), grid, dim3(LP_NT), 0, s, p);
   hipLaunchKernelGGL((logprob_row_kernel<T, TOP>), dim3((unsigned)rows), dim3(LP_NT), 0, s, p);
 }
 
