@@ -427,13 +427,14 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
         base += rq.units();
         rq = get_request<COLS>(p, ++r);
       }
-      const int tile = (int)quotient(u - base, rq.item);
-      const uint32_t from = u - base - (uint32_t)tile * rq.item, to = min(rq.item, from + (u1 - u));
+      const uint32_t item = quotient(u - base, rq.item);
+      if (item >= (uint32_t)rq.tiles) break;  // offsets that overlap so far that the units passed 2^32
+      const int tile = (int)item;
+      const uint32_t from = u - base - item * rq.item, to = min(rq.item, from + (u1 - u));
       const int start = (int)rq.item - rq.steps, first = max((int)from - start, 0), upto = (int)to - start;
       u += to - from;
       if (upto <= 0) continue;  // of the start alone
       const int cols = min(COLS, rq.m * g - tile * COLS);  // of this tile
-      if (cols <= 0) break;  // offsets that overlap so far that the units passed 2^32
       // positions that every column sees, and that any does
       const int i_lo = by_g(p, tile * COLS), i_hi = by_g(p, tile * COLS + cols - 1);
       const int all = min(rq.len, rq.want - rq.m + i_lo + 1), some = min(rq.len, rq.want - rq.m + i_hi + 1);
