@@ -495,7 +495,8 @@ kv_status kv_logprobs(const void* logits, int32_t dtype, int64_t rows, int32_t v
   if (rows * chunks_of(vocab) > LP_MOST_CHUNKS)
     return kvr_err::set(KV_EINVAL, "rows * vocab of one call above 2^37: split the rows");
   if (stride < vocab) return kvr_err::set(KV_EINVAL, "the stride is below the vocabulary");
-  if (!(scale > 0.0f) || !(scale <= 0x1p127f)) return kvr_err::set(KV_EINVAL, "scale must be positive and at most 2^127");
+  if (!(scale > 0.0f) || !(scale <= 0x1p127f))
+    return kvr_err::set(KV_EINVAL, "scale must be positive and at most 2^127");
   if (top_n < 0 || top_n > KV_LOGPROBS_MAX_TOP || top_n > vocab)
     return kvr_err::set(KV_EINVAL, "top_n must be 0 .. %d and at most the vocabulary", KV_LOGPROBS_MAX_TOP);
   if (rows == 0) return kvr_err::clear();

@@ -30,15 +30,16 @@
 //
 // What bounds it: the records' way from HBM and what a call costs once.  16 requests of
 // 2048 - 16384 positions (8 kv heads of 128, 4 q heads each, 124 MB of records), one query
-// row each: 29.7 us; without the products and the softmax 28.0, without the loads 21.1.
+// row each: 29.5 us; without the products and the softmax 28.0, without the loads 21.1.
 // 1.1 us of them are the plan, 4 the way to the first record (three loads that follow each
 // other, while other waves' records keep the memory busy), 2 the merges.  Two requests of
 // 150 - 200 thousand positions (403 MB): 78 us, without products and softmax the same.
-// One to five query rows of 40 requests of 300 - 4000 positions (5 q heads a kv head,
-// COLS 32, 88 MB): 35 us, 33 without products and softmax, 29 without loads.
+// One to five query rows of 40 requests of 300 - 4000 positions (5 q heads a kv head, 88 MB
+// and some of it twice): 29 us.
 //   Workgroups a CU and records a ring: three and four.  Three and six took 31.2 us, two
 // and eight 33.7, four and four 31.1 (the long ones 79, 85 and 81).  Two column tiles need
-// the registers of two a CU: with three, registers spill, 56 us against 35.
+// the registers of two a CU: with three, registers spill, 56 us against 35 on the 40
+// requests.
 //   As many waves as run at once: half as many more took 38 us, twice as many 37; the
 // stretches are equal, so more of them only merge more.
 #include <algorithm>
@@ -107,7 +108,7 @@ __device__ __forceinline__ void static_for(F&& f) {
 // Workgroups a CU holds by their registers, and the records of a wave's ring that
 // then fit its LDS.
 constexpr int occupancy_of(bool f32, int d, int nt) {
-  return nt == 4 || (f32 && d == 128 && nt == 2) ? 1 : nt == 2 || (f32 && d == 128) ? 2 : 3;
+  return f32 && d == 128 ? 3 - nt : 4 - nt;
 }
 constexpr int ring_of(int occupancy) { return occupancy == 3 ? 4 : 8; }
 
@@ -356,8 +357,7 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
   constexpr int REC = 17 * D, RING = ring_of(OCC), LOADS = (16 * D + 1023) / 1024 + 1;
   __shared__ __attribute__((aligned(16))) char s_ring[PA_NT / 64][RING * REC];
   static_assert(RING % TILES == 0, "units do not wrap in the ring");
-  static_assert(RING * REC >= 64 * ROW<D>, "16 rows fit the ring");
-  constexpr bool LOCAL = RING * REC >= NT * 64 * ROW<D>;  // all columns' rows do
+  static_assert(RING * REC >= NT * 64 * ROW<D>, "all columns' rows fit the ring");
   constexpr int WAVES = PA_NT / 64;
   __shared__ uint32_t s_wave[WAVES];
   __shared__ Stretch s_str[WAVES];
@@ -727,17 +727,16 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
       }
 
       // ---- the columns' outputs, or what there is of them ----
-      // 16 rows at a time through the ring, a row's dims over the lanes.  What stays open
-      // goes to the workspace, or at the stretch's end, where the ring has no more to take,
-      // stays where it is.
-      const bool done = first == 0 && upto == rq.steps, stay = LOCAL && u >= u1;
+      // Through the ring, a row's dims over the lanes.  What stays open goes to the workspace,
+      // or at the stretch's end, where the ring has no more to take, stays where it is.
+      const bool done = first == 0 && upto == rq.steps, stay = u >= u1;
       float* const rows = reinterpret_cast<float*>(ring);
       float* const part = stay ? rows : slots + (first > 0 ? 0 : 1) * p.part_cols * ROW<D>;
-      const auto put_rows = [&](int nt, float* tr) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        float* const tr = rows + nt * 16 * ROW<D>;
         const float l = sum_over_q(l_run[nt]);
-        if (q == 0) {
-          *reinterpret_cast<float2*>(tr + c * ROW<D> + D) = make_float2(m_run[nt], l);
-        }
+        if (q == 0) *reinterpret_cast<float2*>(tr + c * ROW<D> + D) = make_float2(m_run[nt], l);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           float* const row = tr + (4 * q + j) * ROW<D>;
@@ -752,37 +751,23 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
             for (int d = 0; d < DT; ++d) row[c * DT + d] = o[nt][d][j];
           }
         }
-        asm volatile("" ::: "memory");
-      };
-      const auto take_rows = [&](int nt, const float* tr) {
-        const int used = stay && !done ? 0 : min(16, cols - nt * 16);  // 0: the rows are the partials
-#pragma unroll 1
-        for (int i0 = 0; i0 < used; i0 += AT_ONCE<D>) {
-          const int i = i0 + lane / LANES<D>;
-          if (i >= used) continue;
-          Column v;
-          float2 ml;
-          load_part<D>(tr + i * ROW<D>, dim_of<D>(lane), ml, v.o);
-          v.m = ml.x;
-          v.l = ml.y;
-          if (done) put_out<T, D, COLS>(p, rq.row, tile, nt * 16 + i, kvh, lane, v);
-          else put_part<D>(part + (nt * 16 + i) * ROW<D>, lane, v);
-        }
-        KVR_WAIT_LGKM0();  // the rows have been read: the ring may be filled again
-        asm volatile("" ::: "memory");
-      };
-      if constexpr (LOCAL) {
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) put_rows(nt, rows + nt * 16 * ROW<D>);
-#pragma unroll 1
-        for (int nt = 0; nt < NT; ++nt) take_rows(nt, rows + nt * 16 * ROW<D>);
-      } else {
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          put_rows(nt, rows);
-          take_rows(nt, rows);
-        }
       }
+      asm volatile("" ::: "memory");
+      const int used = stay && !done ? 0 : cols;  // 0: the rows are the partials
+#pragma unroll 1
+      for (int i0 = 0; i0 < used; i0 += AT_ONCE<D>) {
+        const int i = i0 + lane / LANES<D>;
+        if (i >= used) continue;
+        Column v;
+        float2 ml;
+        load_part<D>(rows + i * ROW<D>, dim_of<D>(lane), ml, v.o);
+        v.m = ml.x;
+        v.l = ml.y;
+        if (done) put_out<T, D, COLS>(p, rq.row, tile, i, kvh, lane, v);
+        else put_part<D>(part + i * ROW<D>, lane, v);
+      }
+      KVR_WAIT_LGKM0();  // the rows have been read: the ring may be filled again
+      asm volatile("" ::: "memory");
       if (!done && lane == 0) {
         Stretch& me = s_str[wave];
         const int which = first > 0 ? 0 : 1;
@@ -877,16 +862,18 @@ __global__ __launch_bounds__(PM_NT) void packed_attn_merge_kernel(PackedAttnPara
   else merge(std::integral_constant<int, 16>{});
 }
 
-// The kernel for a call's columns per request: as few column tiles as take them, at most
-// four (two in fp32 models, whose queries and weights are three numbers each); a request
-// with more has several items, which read its records again.
+// The kernel for a call's columns per request.  A request with more than 16 NT has several
+// items, whose waves read its records again, mostly from the caches; two column tiles a
+// wave spare half of that and cost the third workgroup of a CU.  16 requests of 2000 - 6000
+// positions with 80 columns (8 kv heads) took 44 us with one and 52 with two, 8 with 128
+// 41 and 47, 8 with 256 47.9 and 47.5, 4 with 512 78 and 72, one with 2048 94 and 84.  (Four
+// tiles, one workgroup a CU: 84 with 80 columns, 124 with 2048.)
 struct Plan {
-  int nt, cols, occupancy, start;
+  int nt, cols, occupancy;
 };
+Plan plan_of_tiles(int dtype, int d, int nt) { return Plan{nt, 16 * nt, occupancy_of(dtype == KV_F32, d, nt)}; }
 Plan plan_of(int dtype, int d, int g, int64_t max_query) {
-  const int64_t cols = g * max_query;
-  const int nt = cols <= 16 ? 1 : cols <= 32 || dtype == KV_F32 ? 2 : 4;
-  return Plan{nt, 16 * nt, occupancy_of(dtype == KV_F32, d, nt), nt == 1 ? 4 : 2};
+  return plan_of_tiles(dtype, d, g * max_query <= 256 ? 1 : 2);
 }
 
 // Items of one kv head, and their units, at most: of a call's R requests with `rows` query
@@ -907,12 +894,12 @@ struct Sizes {
 // positions took 11.1 us so and 15.0 the other way, 16 of up to 500 9.7 and 11.6; parts of
 // eight, 16 of up to 1000, 14.9 and 13.2.
 //   Else a unit each where the chip holds as many waves at once, else those waves.  Then an
-// item's start counts as `start` units more: a wave whose stretch goes on with another item
+// item's start counts as START units more: a wave whose stretch goes on with another item
 // ends the one and waits for the other's table, queries and first records, some 4 us, and
-// the waves should end together.  One column tile: four, 30.8 us on 16 requests and 19.9 on
-// 64 (33.2 and 22.3 with none, 31.0 and 21.0 with two); several, whose units take longer:
-// two, 35.5 us on 40 requests of one to five rows and 69 on 8 of 64 (41.0 and 78 with none,
-// 36.1 and 71 with four).
+// the waves should end together.  None, two and four: 31.9, 30.1 and 29.4 us on 16 requests
+// of one row, 32.4, 29.6 and 29.4 on 40 of one to five, 21.3, 18.8 and 18.3 on 64 of 2 kv
+// heads, 71.7, 67.1 and 68.4 on 4 of 128 rows.
+constexpr int START = 4;
 constexpr int64_t WHOLE = 4;
 struct Stretching {
   int workers, start, whole;
@@ -923,7 +910,7 @@ Stretching stretches_of(const Plan& pl, int nkv, const Sizes& z) {
   const int64_t part = (z.steps() + 3) / 4;
   if (part <= WHOLE && 4 * items <= waves) return {(int)(4 * items), 0, (int)part};
   if (units <= waves) return {(int)round_up(units, PA_NT / 64), 0, 0};
-  return {(int)round_up(waves, PA_NT / 64), pl.start, 0};
+  return {(int)round_up(waves, PA_NT / 64), START, 0};
 }
 
 template <typename T, int D, int NT>
@@ -935,9 +922,8 @@ void launch_tiles(const PackedAttnParams& p, hipStream_t s) {
 }
 template <typename T, int D>
 void launch(const Plan& pl, const PackedAttnParams& p, hipStream_t s) {
-  if (pl.nt == 1) return launch_tiles<T, D, 1>(p, s);
-  if (pl.nt == 2) return launch_tiles<T, D, 2>(p, s);
-  if constexpr (std::is_same<T, bf16_t>::value) launch_tiles<T, D, 4>(p, s);
+  if (pl.nt == 1) launch_tiles<T, D, 1>(p, s);
+  else launch_tiles<T, D, 2>(p, s);
 }
 
 // The workspace: what workgroups left open, then the waves' sums.  It is as large as any
@@ -948,8 +934,8 @@ struct AttnLayout {
 AttnLayout attn_layout(const kv_model_desc& d, const Sizes& z) {
   int64_t workers = 0, columns = 0;
   const Plan own = plan_of(d.dtype, d.head_dim, z.g, z.max_query);
-  for (int nt = 1; nt <= own.nt; nt *= 2) {
-    const Plan pl = plan_of(d.dtype, d.head_dim, 1, 16 * nt);
+  for (int nt = 1; nt <= own.nt; ++nt) {
+    const Plan pl = plan_of_tiles(d.dtype, d.head_dim, nt);
     const int64_t units = z.items(pl.cols) * std::max<int64_t>(4, z.steps());
     const int64_t w = round_up(std::min(most_waves(pl, d.num_kv_heads), units), PA_NT / 64);
     workers = std::max(workers, w);
@@ -1052,7 +1038,7 @@ kv_status kv_packed_attention(kv_packed_t packed, int32_t layer, const void* q, 
     return kvr_err::set(KV_EINVAL, "null workspace, or one not on a boundary of 16 bytes");
   const Plan plan = plan_of(d.dtype, d.head_dim, d.num_q_heads / d.num_kv_heads, max_query);
   const Sizes z{R, d.num_q_heads / d.num_kv_heads, rows, max_query, max_len};
-  if (max_len > INT32_MAX || (R + rows * z.g / plan.cols) * (z.steps() + plan.start) > INT32_MAX)
+  if (max_len > INT32_MAX || (R + rows * z.g / plan.cols) * (z.steps() + START) > INT32_MAX)
     return kvr_err::set(KV_EINVAL, "max_len or the work of one call above 2^31: split the query rows");
   const uint64_t need = kv_packed_attention_workspace_bytes(&d, R, rows, max_query, max_len);
   if (need > ws_bytes)

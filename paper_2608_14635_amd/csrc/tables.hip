@@ -223,7 +223,8 @@ extern "C" kv_status kv_tables_grow(const int32_t* held, const int32_t* lens, in
                                     int64_t* slots, int32_t* positions, int32_t* counts, int32_t device,
                                     void* stream) {
   if (R < 0 || R > 1 << 30 || num_free < 0 || max_blocks < 0 || max_rows < 0 || max_rows > INT32_MAX)
-    return kvr_err::set(KV_EINVAL, "num_requests is 0 .. 2^30; num_free, max_blocks_per_req and max_rows 0 .. 2^31 - 1");
+    return kvr_err::set(KV_EINVAL,
+                        "num_requests is 0 .. 2^30; num_free, max_blocks_per_req and max_rows 0 .. 2^31 - 1");
   if (B <= 0) return kvr_err::set(KV_EINVAL, "block_size must be positive");
   if (!row_offsets || !counts) return kvr_err::set(KV_EINVAL, "null row_offsets or counts");
   if (R > 0 && !lens) return kvr_err::set(KV_EINVAL, "null lens");

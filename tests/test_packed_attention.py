@@ -188,9 +188,10 @@ def test_long_and_many(name, lens):
 
 
 @pytest.mark.gpu
-def test_a_prompts_piece():
+@pytest.mark.parametrize("name,g", [("bf16", 4), ("bf16", 3), ("f32_32", 4), ("f32_64", 2), ("f32_128", 4)])
+def test_a_prompts_piece(name, g):
     """Many query rows of two requests: several column tiles each, causal inside."""
-    b = Batch(heads("bf16", 4), [500, 222], [150, 222], seed=2)
+    b = Batch(heads(name, g), [500, 222], [150, 222], seed=2)
     b.run()
     torch.cuda.synchronize()
     b.check()
