@@ -14,10 +14,10 @@
 // Top entries.  (value, lower index first) is one 64-bit key, so that all keys of a
 // row differ and the order is total.  A bound that at least top_n entries reach comes
 // from the threads' own largest values: one wave finds, bit by bit from the top, a
-// value that at least top_n and not many more threads reach; entries that reach
-// it lie in those threads alone, so they fit the list in LDS, where they are ranked
-// by counting.  (Ranking the threads' values by counting took 1.7 us a chunk.)  Where
-// equal values make too many threads, the bound is the top_n-th of the threads' keys.
+// value that at least top_n and not many more threads reach; the entries that reach
+// it are listed in LDS and ranked by counting.  (Ranking the threads' values by counting
+// took 1.7 us a chunk.)  Where equal values make too many of them, the bound is the
+// top_n-th of the threads' keys.
 //
 // What bounds it.  Many rows: HBM, one exp and some six other operations for 4 or 2 bytes:
 // 1024 rows of 151936 in bf16 52 - 54 us, 311 MB at up to 6 TB/s, and 4.8 the second kernel.
@@ -128,21 +128,23 @@ __device__ __forceinline__ int rank_of(uint64_t key, const uint64_t* keys, int n
   return r;
 }
 
-// PER: entries of a thread at most.  At most 64 threads' are collected where the bound
-// comes from their values, and top_n <= 64 threads' where it is one of their keys.
+// PER: entries of a thread at most.  With a bound that is one of the threads' keys, the
+// top_n <= 64 threads that reach it have no more entries than the list takes; with one
+// that comes from their values, lists above LP_LIST are given up for that.
+constexpr int LP_LIST = 512;
 template <int PER>
 struct TopScratch {
   static constexpr int KEYS = 64 * PER;
   uint64_t keys[KEYS];
   uint32_t own[LP_NT];
-  uint32_t bound;  // of the order bits; 0xffffffff: too many equal values
+  uint32_t bound;  // of the order bits; 0xffffffff: too many threads reach it
   int count;
 };
 
-// One wave: a value that at least `top` and at most `most` of the threads' largest reach.
-// First the longest run of the leading bits of `upper` (no smaller than any of them) that
-// enough of them reach, then bit by bit.
-template <typename S>
+// One wave: a value that at least `top` and, equal values apart, not many more of the
+// threads' largest reach.  First the longest run of the leading bits of `upper` (no smaller
+// than any of them) that enough of them reach, then bit by bit of those that T has.
+template <typename T, typename S>
 __device__ __forceinline__ void find_bound(int top, uint32_t upper, S& s) {
   const int most = min(64, 2 * top + 8);
   const int lane = threadIdx.x & 63;
@@ -172,7 +174,7 @@ __device__ __forceinline__ void find_bound(int top, uint32_t upper, S& s) {
   }
   // upper's next bit is 1, and with it too few reach
 #pragma unroll 1
-  for (int b = free - 2; b >= 0 && n > most; --b) {
+  for (int b = free - 2; b >= 32 - 8 * (int)sizeof(T) && n > most; --b) {
     const uint32_t v = bound | 1u << b;
     const int k = reach(v);
     if (k >= top) {
@@ -181,7 +183,7 @@ __device__ __forceinline__ void find_bound(int top, uint32_t upper, S& s) {
     }
   }
   if (lane == 0) {
-    s.bound = n > most ? 0xffffffffu : bound;
+    s.bound = n > 160 ? 0xffffffffu : bound;
     s.count = 0;
   }
 }
@@ -196,7 +198,9 @@ template <typename S>
 __device__ __forceinline__ uint64_t bound_of_keys(uint64_t own, int top, S& s) {
   static_assert(S::KEYS > LP_NT, "the threads' keys fit the list");
   const int t = threadIdx.x;
+  __syncthreads();  // the list and its count have been read
   s.keys[t] = own;
+  if (t == 0) s.count = 0;
   __syncthreads();
   if (rank_of(own, s.keys, LP_NT) == top - 1) s.keys[LP_NT] = own;
   __syncthreads();
@@ -336,7 +340,7 @@ __global__ __launch_bounds__(LP_NT) void logprob_chunk_kernel(LogprobParams p) {
   const float m = block_most(own, s_most);
   // a wave finds the bound first (of the workgroups of a CU, which come 256 apart, not the same one)
   if constexpr (TOP)
-    if (t / 64 == (blockIdx.x >> 8) % (LP_NT / 64)) find_bound(p.top, order_bits(m), s_top);
+    if (t / 64 == (blockIdx.x >> 8) % (LP_NT / 64)) find_bound<T>(p.top, order_bits(m), s_top);
   float l = 0.0f, s = 0.0f;
   const float base = base_of(m), cm = c_of(base, p.scale2);
   auto add = [&](float x) {
@@ -369,37 +373,41 @@ __global__ __launch_bounds__(LP_NT) void logprob_chunk_kernel(LogprobParams p) {
     const auto key_at = [&](int at) {  // past the vocabulary: as NaN of higher indices, below all others
       return make_key(at < p.vocab ? order_bits(Elem<T>::load(z, at)) : 0u, at);
     };
-    if (s_top.bound == 0xffffffffu) {
-      uint64_t key = 0;
 #pragma unroll 1
-      for (int i = 0; i < LP_ITEMS; ++i) key = max(key, key_at(first + i / VEC * STEP + i % VEC));
-      bound = bound_of_keys(key, p.top, s_top);
-    }
-    // pieces with an entry that may reach the bound are read again
-    uint32_t hit = 0;
+    for (bool by_key = s_top.bound == 0xffffffffu;; by_key = true) {
+      if (by_key) {
+        uint64_t key = 0;
+#pragma unroll 8
+        for (int i = 0; i < LP_ITEMS; ++i) key = max(key, key_at(first + i / VEC * STEP + i % VEC));
+        bound = bound_of_keys(key, p.top, s_top);
+      }
+      // pieces with an entry that may reach the bound are read again
+      uint32_t hit = 0;
 #pragma unroll
-    for (int i = 0; i < VECS; ++i) hit |= (order_bits(most[i]) >= (uint32_t)(bound >> 32) ? 1u : 0u) << i;
+      for (int i = 0; i < VECS; ++i) hit |= (order_bits(most[i]) >= (uint32_t)(bound >> 32) ? 1u : 0u) << i;
 #pragma unroll 1
-    while (hit) {
-      const int at = first + (__ffs(hit) - 1) * STEP;
-      hit &= hit - 1;
-      if (at + VEC <= p.vocab) {
-        Piece<T> w;
-        w.load(z + at);
+      while (hit) {
+        const int at = first + (__ffs(hit) - 1) * STEP;
+        hit &= hit - 1;
+        if (at + VEC <= p.vocab) {
+          Piece<T> w;
+          w.load(z + at);
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-          const uint64_t k = make_key(order_bits(w.value(j)), at + j);
-          if (k >= bound) collect(k, s_top);
-        }
-      } else {
+          for (int j = 0; j < VEC; ++j) {
+            const uint64_t k = make_key(order_bits(w.value(j)), at + j);
+            if (k >= bound) collect(k, s_top);
+          }
+        } else {
 #pragma unroll 1
-        for (int j = 0; j < VEC; ++j) {
-          const uint64_t k = key_at(at + j);
-          if (k >= bound) collect(k, s_top);
+          for (int j = 0; j < VEC; ++j) {
+            const uint64_t k = key_at(at + j);
+            if (k >= bound) collect(k, s_top);
+          }
         }
       }
+      __syncthreads();
+      if (by_key || s_top.count <= LP_LIST) break;
     }
-    __syncthreads();
     const int n = min(s_top.count, s_top.KEYS);
     uint64_t* out = p.keys + (row * p.chunks + c) * p.top;
     for (int i = t; i < n; i += LP_NT) {
@@ -440,14 +448,18 @@ __global__ __launch_bounds__(LP_NT) void logprob_row_kernel(LogprobParams p) {
     __shared__ TopScratch<64> s_top;
     s_top.own[t] = (uint32_t)(own >> 32);
     __syncthreads();
-    if (t < 64) find_bound(p.top, order_bits(m), s_top);
+    if (t < 64) find_bound<T>(p.top, order_bits(m), s_top);
     __syncthreads();
     uint64_t bound = (uint64_t)s_top.bound << 32;
-    if (s_top.bound == 0xffffffffu) bound = bound_of_keys(own, p.top, s_top);
-    if (own >= bound)
-      for (int i = t; i < total; i += LP_NT)
-        if (keys[i] >= bound) collect(keys[i], s_top);
-    __syncthreads();
+#pragma unroll 1
+    for (bool by_key = s_top.bound == 0xffffffffu;; by_key = true) {
+      if (by_key) bound = bound_of_keys(own, p.top, s_top);
+      if (own >= bound)
+        for (int i = t; i < total; i += LP_NT)
+          if (keys[i] >= bound) collect(keys[i], s_top);
+      __syncthreads();
+      if (by_key || s_top.count <= LP_LIST) break;
+    }
     const int n = min(s_top.count, s_top.KEYS);
     for (int i = t; i < n; i += LP_NT) {
       const uint64_t k = s_top.keys[i];

@@ -215,6 +215,22 @@ def test_the_largest_vocabulary(dt):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dt", list(DT))
+def test_equal_values_that_fill_the_list(dt):
+    """Many equal entries of few threads, and of few ranks of many chunks: lists of a bound
+    on the threads' values that are given up."""
+    V = 64 * 8192
+    i = torch.arange(V)
+    low = -1 - torch.rand(V, generator=torch.Generator().manual_seed(11))
+    per = 4 if dt == "f32" else 8  # consecutive entries of a thread
+    rows = [torch.where(i % (256 * per) // per < 100, 2.0, low), torch.where(i % 8192 < 24, 2.0, low),
+            torch.where(i % 8192 % (8 * per) < per, (i // 8192 % 2).float(), low)]
+    c = Call(torch.stack(rows).to(DT[dt]), 1.0, [0, 5, V - 1], 64)
+    c.run()
+    c.check()
+
+
+@pytest.mark.gpu
 def test_more_rows_than_a_short_grid():
     R, V = (1 << 17) + 3, 37
     z, tok = random_rows(R, V, torch.float32, 10)
