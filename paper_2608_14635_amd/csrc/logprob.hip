@@ -123,7 +123,7 @@ __device__ __forceinline__ float sum_over_wave(float v) {
 // Ranks by counting: how many of the n keys in LDS are larger.
 __device__ __forceinline__ int rank_of(uint64_t key, const uint64_t* keys, int n) {
   int r = 0;
-#pragma unroll 4
+#pragma unroll 8
   for (int i = 0; i < n; ++i) r += keys[i] > key;
   return r;
 }
@@ -141,12 +141,11 @@ struct TopScratch {
   int count;
 };
 
-// One wave: a value that at least `top` and, equal values apart, not many more of the
-// threads' largest reach.  First the longest run of the leading bits of `upper` (no smaller
+// One wave: a value that at least `least` and, equal values apart, at most `most` of the
+// threads' values reach.  First the longest run of the leading bits of `upper` (no smaller
 // than any of them) that enough of them reach, then bit by bit of those that T has.
 template <typename T, typename S>
-__device__ __forceinline__ void find_bound(int top, uint32_t upper, S& s) {
-  const int most = min(64, 2 * top + 8);
+__device__ __forceinline__ void find_bound(int least, int most, uint32_t upper, S& s) {
   const int lane = threadIdx.x & 63;
   uint32_t u[LP_NT / 64];
 #pragma unroll
@@ -164,7 +163,7 @@ __device__ __forceinline__ void find_bound(int top, uint32_t upper, S& s) {
     const int mid = (low + free) / 2;
     const uint32_t v = upper & ~0u << mid;
     const int k = reach(v);
-    if (k >= top) {
+    if (k >= least) {
       bound = v;
       n = k;
       free = mid;
@@ -177,7 +176,7 @@ __device__ __forceinline__ void find_bound(int top, uint32_t upper, S& s) {
   for (int b = free - 2; b >= 32 - 8 * (int)sizeof(T) && n > most; --b) {
     const uint32_t v = bound | 1u << b;
     const int k = reach(v);
-    if (k >= top) {
+    if (k >= least) {
       bound = v;
       n = k;
     }
@@ -187,6 +186,7 @@ __device__ __forceinline__ void find_bound(int top, uint32_t upper, S& s) {
     s.count = 0;
   }
 }
+__device__ __forceinline__ int most_threads(int top) { return min(64, 2 * top + 8); }
 template <typename S>
 __device__ __forceinline__ void collect(uint64_t key, S& s) {
   const int at = atomicAdd(&s.count, 1);  // any order: the ranks settle it
@@ -340,7 +340,7 @@ __global__ __launch_bounds__(LP_NT) void logprob_chunk_kernel(LogprobParams p) {
   const float m = block_most(own, s_most);
   // a wave finds the bound first (of the workgroups of a CU, which come 256 apart, not the same one)
   if constexpr (TOP)
-    if (t / 64 == (blockIdx.x >> 8) % (LP_NT / 64)) find_bound<T>(p.top, order_bits(m), s_top);
+    if (t / 64 == (blockIdx.x >> 8) % (LP_NT / 64)) find_bound<T>(p.top, most_threads(p.top), order_bits(m), s_top);
   float l = 0.0f, s = 0.0f;
   const float base = base_of(m), cm = c_of(base, p.scale2);
   auto add = [&](float x) {
@@ -427,9 +427,15 @@ __global__ __launch_bounds__(LP_NT) void logprob_row_kernel(LogprobParams p) {
   const float4* stats = p.stats + row * p.chunks;
   const uint64_t* keys = p.keys + row * p.chunks * p.top;
   const int total = p.chunks * p.top;
-  uint64_t own = t;  // threads without a key: below all of them, and different
+  // `each` keys of falling order a thread: its largest, and its least where it has as many
+  const int each = (total + LP_NT - 1) / LP_NT;
+  uint64_t own = t, least = ~0ull;  // threads without a key: below all of them, and different
   if (TOP)
-    for (int i = t; i < total; i += LP_NT) own = max(own, keys[i]);
+    for (int i = t * each; i < (t + 1) * each; ++i) {
+      const uint64_t k = i < total ? keys[i] : 0;
+      own = max(own, k);
+      least = min(least, k);
+    }
   Row<T> result(row);
   if (t == 0) result.load(p);
   // every wave merges all chunks, in the same order
@@ -446,16 +452,18 @@ __global__ __launch_bounds__(LP_NT) void logprob_row_kernel(LogprobParams p) {
   if constexpr (TOP) {
     // a thread holds ceil(256 * 64 / 256) keys at most
     __shared__ TopScratch<64> s_top;
-    s_top.own[t] = (uint32_t)(own >> 32);
+    // a bound that top_n keys reach because enough threads' least ones do
+    s_top.own[t] = (uint32_t)(least >> 32);
     __syncthreads();
-    if (t < 64) find_bound<T>(p.top, order_bits(m), s_top);
+    const int threads = (p.top + each - 1) / each;
+    if (t < 64) find_bound<T>(threads, each == 1 ? most_threads(p.top) : threads + 8, order_bits(m), s_top);
     __syncthreads();
     uint64_t bound = (uint64_t)s_top.bound << 32;
 #pragma unroll 1
     for (bool by_key = s_top.bound == 0xffffffffu;; by_key = true) {
       if (by_key) bound = bound_of_keys(own, p.top, s_top);
       if (own >= bound)
-        for (int i = t; i < total; i += LP_NT)
+        for (int i = t * each; i < min((t + 1) * each, total); ++i)
           if (keys[i] >= bound) collect(keys[i], s_top);
       __syncthreads();
       if (by_key || s_top.count <= LP_LIST) break;
