@@ -834,9 +834,9 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
 
 // Workgroup (kv head, workgroup of the first kernel): the item that it began and left
 // open, merged over the workgroups that went on with it, in their order.  Its time is its
-// loads' way from other chiplets' caches: 3 us with few partials, 7.8 with 48 of 5
-// columns at 16 loads together (8.5 at 8), 4.8 with five to eight of 16 columns at 8 (6.2
-// at 16).
+// loads' way from other chiplets' caches: 3 us with few partials, 7.0 with 48 of 5
+// columns at 32 loads together (7.8 at 16, 8.5 at 8), 4.8 with five to eight of 16 columns
+// at 8 (6.2 at 16).
 constexpr int PM_NT = 256;
 template <typename T, int D, int NT>
 __global__ __launch_bounds__(PM_NT) void packed_attn_merge_kernel(PackedAttnParams p) {
@@ -861,7 +861,8 @@ __global__ __launch_bounds__(PM_NT) void packed_attn_merge_kernel(PackedAttnPara
   };
   if (it.groups <= 4) merge(std::integral_constant<int, 4>{});
   else if (it.groups <= 8) merge(std::integral_constant<int, 8>{});
-  else merge(std::integral_constant<int, 16>{});
+  else if (it.groups <= 16) merge(std::integral_constant<int, 16>{});
+  else merge(std::integral_constant<int, 32>{});
 }
 
 // The kernel for a call's columns per request.  A request with more than 16 NT has several
