@@ -478,7 +478,7 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
         const int e = __builtin_amdgcn_readlane(tab, bi - window);
         const bool in = (uint32_t)e < p.num_blocks;
         broken |= !in;
-        const char* rec = head + (in ? e : 0) * block_bytes + ti * REC;
+        const char* rec = head + (in ? e : 0) * block_bytes + (int64_t)ti * REC;
         constexpr int FULL = 16 * D / 1024;
 #pragma unroll
         for (int i = 0; i < FULL; ++i) load_lds(rec, REC, ring + put + 1024 * i, lane * 16, 1024 * i);

@@ -1,0 +1,89 @@
+"""Attention over a packed arena (kv_packed_attention, include/kvr_packed.h) at the ends
+of its range: blocks and lengths past 32-bit offsets, values and queries next to the
+largest numbers, and sums in which every position counts by itself."""
+import dataclasses
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from paper_2608_14635_amd import harness as Hn  # noqa: E402
+from paper_2608_14635_amd import kvr  # noqa: E402
+
+import packed_util as P  # noqa: E402
+
+U = 2.0 ** -24
+ONE_HEAD = dataclasses.replace(P.F32[128], num_layers=1, num_q_heads=4, num_kv_heads=1)
+
+
+def dev(a, dtype=torch.int32):
+    return torch.tensor(np.asarray(a), dtype=dtype, device="cuda")
+
+
+class Zeros:
+    """A packed arena of zeros (K and V 0 in every slot), with chosen rows stored."""
+
+    def __init__(self, shape, B, blocks):
+        self.shape, self.B, self.blocks = shape, B, blocks
+        n = kvr.kv_packed_bytes(shape, B, blocks)
+        self.raw = torch.zeros(n, dtype=torch.uint8, device="cuda")
+        self.handle = kvr.kv_packed_bind(self.raw.data_ptr(), n, shape, B, blocks)
+
+    def store(self, slots, k, v):
+        """k, v [n, nkv, d], values that the arena holds exactly."""
+        dt, w = P.torch_dtype(self.shape), self.shape.num_kv_heads * self.shape.head_dim
+        kd, vd = (torch.tensor(np.asarray(x).reshape(-1, w), dtype=torch.float32).to(dt).cuda() for x in (k, v))
+        sl = dev(slots, torch.int64)
+        kvr.kv_packed_store(self.handle, 0, kd.data_ptr(), w, vd.data_ptr(), w, sl.data_ptr(), len(sl), Hn.stream_ptr())
+        torch.cuda.synchronize()
+
+    def attend(self, q, lens, tables, counts=None, max_len=None):
+        """q [rows, nq, d] -> out [rows, nq, d] in 64 bits; counts: query rows of each request."""
+        s, lens, tables = self.shape, np.asarray(lens), np.asarray(tables, np.int32)
+        counts = np.ones(len(lens), int) if counts is None else np.asarray(counts)
+        w = s.num_q_heads * s.head_dim
+        qd = torch.tensor(np.asarray(q).reshape(-1, w), dtype=torch.float32).to(P.torch_dtype(s)).cuda()
+        out = torch.full_like(qd, 7.0)
+        off, ln, tab = dev(np.concatenate([[0], np.cumsum(counts)])), dev(lens), dev(tables)
+        m, n = int(counts.max()), int(max_len or lens.max())
+        size = kvr.kv_packed_attention_workspace_bytes(s, len(lens), len(qd), m, n)
+        ws = torch.full((size,), 255, dtype=torch.uint8, device="cuda")
+        kvr.kv_packed_attention(self.handle, 0, qd.data_ptr(), w, off.data_ptr(), len(qd), ln.data_ptr(), tab.data_ptr(),
+                                len(lens), tables.shape[1], m, n, out.data_ptr(), w, ws.data_ptr(), size, Hn.stream_ptr())
+        torch.cuda.synchronize()
+        return out.double().cpu().numpy().reshape(-1, s.num_q_heads, s.head_dim)
+
+    def release(self):
+        kvr.kv_packed_release(self.handle)
+
+
+def marks(n, d, seed=0):
+    """Values [n, 1, d] that the arena holds exactly, different in every row."""
+    rng = np.random.default_rng(seed)
+    v = rng.choice(P.VALUES, size=(n, 1, d))
+    v[..., ::32] = 6.0  # each group's scale is 1
+    return v
+
+
+@pytest.mark.gpu
+def test_records_past_two_gib_of_one_block():
+    """A block of 15.8 million slots: its last records lie more than 2^31 bytes behind its
+    first.  K is 0 but for a few positions, each of which outweighs all before it
+    by e^60 and more: what a request sees is the V of the last of them."""
+    d, B = 128, 15_800_000
+    border = 16 * ((1 << 31) // (17 * d) + 1)  # the first slot of a record that starts past 2^31
+    at = [100, border - 1, border, border + 13, B - 1]
+    a = Zeros(ONE_HEAD, B, 1)
+    k = np.zeros((len(at), 1, d))
+    for i in range(len(at)):
+        k[i, 0, :i + 1] = 6.0
+    v = marks(len(at), d)
+    a.store(at, k, v)
+    q = np.zeros((1, 4, d))
+    q[..., :len(at)] = 128.0  # scores 128 * 6 * (i + 1) / sqrt(128): 68 apart
+    lens = [p + 1 for p in at]
+    out = a.attend(np.repeat(q, len(at), 0), lens, np.zeros((len(at), 1)))
+    # the rest weighs at most 1.6e7 e^-67 of V's 6; the quotient and the weight's parts round by a few u
+    assert np.abs(out - v).max() <= 6 * 8 * U
+    a.release()
