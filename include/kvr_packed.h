@@ -140,7 +140,8 @@ uint64_t kv_packed_decode_workspace_bytes(const kv_model_desc* desc, int32_t num
 /* One greedy decode step over a packed arena: kv_decode_step (kvr_decode.h) with the
  * context's K/V in a packed arena, the new position's K/V stored there in every layer
  * before that layer's attention reads it.  Arguments, outputs and status codes are
- * kv_decode_step's. */
+ * kv_decode_step's; besides, KV_EINVAL where kv_packed_attention would not take the step's
+ * attention: above 2^24 requests, a position of 2^31 - 1, or more work than 2^31 units. */
 kv_status kv_packed_decode_step(const kv_weights* w, const void* final_norm, const void* lm_head,
                                 const int32_t* tokens, const int32_t* positions,
                                 int32_t num_requests, const int32_t* block_tables,

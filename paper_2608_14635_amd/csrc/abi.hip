@@ -1105,6 +1105,9 @@ kv_status decode_step(const kv_weights* w, const void* final_norm, const void* l
       return fail(KV_EINVAL, "qkv_bias model without bq/bk/bv in layer %d", l);
   }
   if (!workspace) return fail(KV_EINVAL, "null workspace");
+  if (PACKED && !packed_attention_takes(d, R, R, 1, max_pos + 1))
+    return fail(KV_EINVAL, "%d requests up to position %lld are more than a step over a packed arena takes", R,
+                (long long)max_pos);
   const DecodeLayout L = make_decode_layout(d, R, max_pos + 1, PACKED);
   if (L.total > ws_bytes)
     return fail(KV_ENOMEM, "workspace of %llu bytes < %llu needed", (unsigned long long)ws_bytes,

@@ -3,6 +3,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "kvr.h"
+
 struct kv_packed;
 
 namespace kvr {
@@ -41,6 +43,10 @@ struct PackedMoveParams {
   int layers;
 };
 void launch_packed_move(int dtype, int d, bool to_packed, const PackedMoveParams& p, hipStream_t s);
+
+// Whether the attention takes a call of R requests, `rows` query rows in all, at most
+// max_query of one, and lengths up to max_len (all positive): their numbers and the work.
+bool packed_attention_takes(const kv_model_desc& d, int64_t R, int64_t rows, int64_t max_query, int64_t max_len);
 
 // What a decode step does with a packed arena: its new rows, dense [rows][nkv][d],
 // into their slots, and the attention of one query row a request.

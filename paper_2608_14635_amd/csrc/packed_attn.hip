@@ -996,6 +996,14 @@ void run(const kv_packed* packed, int32_t layer, const void* q, int64_t q_stride
 
 }  // namespace
 
+bool kvr::packed_attention_takes(const kv_model_desc& d, int64_t R, int64_t rows, int64_t max_query, int64_t max_len) {
+  if (R > MOST_ROWS || rows > MOST_ROWS || max_len > INT32_MAX) return false;
+  const int g = d.num_q_heads / d.num_kv_heads;
+  const Plan plan = plan_of(d.dtype, d.head_dim, g, max_query);
+  const Sizes z{(int)R, g, rows, max_query, max_len};
+  return (R + rows * g / plan.cols) * (z.steps() + START) <= INT32_MAX;
+}
+
 void kvr::packed_attention_step(const kv_packed* a, int32_t layer, const void* q, const int32_t* lens,
                                 const int32_t* tables, int R, int max_blocks, int64_t max_len, void* out,
                                 void* workspace, hipStream_t s) {
@@ -1039,9 +1047,7 @@ kv_status kv_packed_attention(kv_packed_t packed, int32_t layer, const void* q, 
     return kvr_err::set(KV_EINVAL, "the arrays and the strides need boundaries of 4 bytes");
   if (!workspace || (uintptr_t)workspace % 16 != 0)
     return kvr_err::set(KV_EINVAL, "null workspace, or one not on a boundary of 16 bytes");
-  const Plan plan = plan_of(d.dtype, d.head_dim, d.num_q_heads / d.num_kv_heads, max_query);
-  const Sizes z{R, d.num_q_heads / d.num_kv_heads, rows, max_query, max_len};
-  if (max_len > INT32_MAX || (R + rows * z.g / plan.cols) * (z.steps() + START) > INT32_MAX)
+  if (!packed_attention_takes(d, R, rows, max_query, max_len))
     return kvr_err::set(KV_EINVAL, "max_len or the work of one call above 2^31: split the query rows");
   const uint64_t need = kv_packed_attention_workspace_bytes(&d, R, rows, max_query, max_len);
   if (need > ws_bytes)
