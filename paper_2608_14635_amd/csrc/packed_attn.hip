@@ -202,13 +202,13 @@ __device__ __forceinline__ Request make_request(const PackedAttnParams& p, int r
 }
 template <int COLS>
 __device__ __forceinline__ Request get_request(const PackedAttnParams& p, int r) {
-  int row = r, m = 1, want = p.lens[r];
+  int row = r, m = 1, want = max(p.lens[r], 0);
   if (p.q_offsets) {
     const int a = p.q_offsets[r], b = p.q_offsets[r + 1];
     row = min(max(a, 0), (int)p.rows);
     const int all = max(min(b, (int)p.rows) - row, 0);
     m = min(all, p.max_query);
-    want = max(want, 0) - (all - m);  // the rows left out are the last ones
+    want -= all - m;  // the rows left out are the last ones
   }
   return make_request<COLS>(p, row, m, want);
 }
@@ -438,7 +438,7 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
       // positions that every column sees, and that any does
       const int i_lo = by_g(p, tile * COLS), i_hi = by_g(p, tile * COLS + cols - 1);
       const int all = min(rq.len, rq.want - rq.m + i_lo + 1), some = min(rq.len, rq.want - rq.m + i_hi + 1);
-      const int stop = min(upto, (max(some, 0) + UNIT - 1) / UNIT);
+      const int stop = min(upto, (int)(((uint32_t)max(some, 0) + UNIT - 1) / UNIT));
 
       // 64 table entries, one a lane, and the queries: on their way ahead of the records
       const int32_t* table = p.tables + (int64_t)r * p.max_blocks;
@@ -981,7 +981,7 @@ void run(const kv_packed* packed, int32_t layer, const void* q, int64_t q_stride
   const Plan plan = plan_of(d.dtype, d.head_dim, p.g, max_query);
   const Stretching st = stretches_of(plan, d.num_kv_heads, z);
   p.max_query = max_query;
-  p.most_len = (int)std::min<int64_t>({max_len, (int64_t)max_blocks * packed->block_size, INT32_MAX - 64});
+  p.most_len = (int)std::min<int64_t>({max_len, (int64_t)max_blocks * packed->block_size, INT32_MAX});
   p.start = st.start;
   p.whole = st.whole;
   p.workers = st.workers;

@@ -87,3 +87,32 @@ def test_records_past_two_gib_of_one_block():
     # the rest weighs at most 1.6e7 e^-67 of V's 6; the quotient and the weight's parts round by a few u
     assert np.abs(out - v).max() <= 6 * 8 * U
     a.release()
+
+
+@pytest.mark.gpu
+def test_lengths_up_to_the_largest_number():
+    """Contexts whose last positions are next to 2^31, over one block listed many times;
+    the last of several query rows see them, as do requests some positions shorter."""
+    d, B = 128, 1 << 16
+    top, wide = (1 << 31) - 1, (1 << 31) // B
+    a = Zeros(ONE_HEAD, B, 2)
+    last = [B - 71, B - 41, B - 4, B - 3, B - 2]  # of block 1: positions 2^31 - 71 .. 2^31 - 2
+    k = np.zeros((len(last), 1, d))
+    for i in range(len(last)):
+        k[i, 0, :i + 1] = 6.0
+    v = marks(len(last), d, seed=1)
+    a.store([B + x for x in last], k, v)
+    q = np.zeros((5, 4, d))
+    q[..., :len(last)] = 128.0
+    table = np.zeros((3, wide))
+    table[:, -1] = 1
+    # rows at positions 2^31 - 71, 2^31 - 41, and the last three
+    out = a.attend(q, [top - 69, top - 39, top], table, counts=[1, 1, 3])
+    # 2^31 positions of weight e^-67 at most, V 0 there: 1.7e-20
+    assert np.abs(out - v).max() <= 6 * 8 * U
+    # a length beyond them, and a max_len below: its positions are left out
+    out = a.attend(q[:1], [top], table[:1], max_len=top - 39)
+    assert np.abs(out - v[1]).max() <= 6 * 8 * U
+    out = a.attend(q[:2], [-5, -(1 << 31)], table[:2], max_len=40)
+    assert (out == 0).all()
+    a.release()
