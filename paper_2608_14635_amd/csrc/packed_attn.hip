@@ -202,13 +202,13 @@ __device__ __forceinline__ Request make_request(const PackedAttnParams& p, int r
 }
 template <int COLS>
 __device__ __forceinline__ Request get_request(const PackedAttnParams& p, int r) {
-  int row = r, m = 1, want = max(p.lens[r], 0);
+  int row = r, m = 1, want = p.lens[r];
   if (p.q_offsets) {
     const int a = p.q_offsets[r], b = p.q_offsets[r + 1];
     row = min(max(a, 0), (int)p.rows);
     const int all = max(min(b, (int)p.rows) - row, 0);
     m = min(all, p.max_query);
-    want -= all - m;  // the rows left out are the last ones
+    want = max(want, 0) - (all - m);  // the rows left out are the last ones
   }
   return make_request<COLS>(p, row, m, want);
 }
