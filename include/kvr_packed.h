@@ -111,9 +111,11 @@ uint64_t kv_packed_attention_workspace_bytes(const kv_model_desc* desc, int32_t 
  *                need one each
  * Row i attends positions 0 .. its own: out = sum_j p_j v_j, p the softmax of
  * q . k_j / sqrt(d), q head h reading kv head h / (nq/nkv).  Scores, softmax and sums
- * are fp32, the output is rounded once.  Positions in a block whose table entry is
- * outside the arena, and those past max_len or max_blocks_per_req, are left out; a row
- * that is left with no position, or with none whose score is above -infinity, is zero.
+ * are fp32, the output is rounded once; values next to the largest number do not overflow
+ * on the way (below 2^-86 they may count as 0 beside values of 2^65 and more).  Positions
+ * in a block whose table entry is outside the arena, and those past max_len or
+ * max_blocks_per_req, are left out; a row that is left with no position, or with none whose
+ * score is above -infinity, is zero.
  * Requests may share blocks, not query rows: q_offsets does not decrease.  Nothing but
  * the requests' rows of out is written; q and out may be the same memory only as the
  * same rows.  The arrays on the device are read when the call runs there, so a captured

@@ -18,6 +18,12 @@
 //   O = P V: the lane's weights of the unit's two tiles are the A operand as they are,
 //   positions 4q .. 4q+3 of both being its eight k's; V's layout gives the lane the dims
 //   c d/16 .. of the same positions, which it pairs into the B operands of d/16 products.
+//   A weight may be 2^SLACK and 2^31 of them add up, so the sums of large V could pass the
+//   largest fp32 number where their quotient, which lies between the V's, does not.  From
+//   the first unit with a scale of 2^65 or more on, a wave takes an item's maxima LIFT too high
+//   and so all weights and their sum that much smaller: 2^31 2^SLACK 2^-LIFT 1.5 2^127 is below
+//   2^127, 2^31 2^SLACK 6 2^64 without it.  (Exponents are then rounded to 2^-19 and V below
+//   2^-86 may be lost.  Scores of 2^30 have no room for LIFT.)
 //   (Up to 8 columns, a softmax a tile in the two halves of the 16, merged at the end,
 //   spares half the exponentials and took as long: 30.2 us against 29.5 below.)
 // Records reach a wave through a ring of its own in LDS, by direct-to-LDS loads: a
@@ -57,6 +63,7 @@ namespace {
 
 constexpr int PA_NT = 256;         // four waves
 constexpr float SLACK = 8.0f;      // rescale slack, log2 units
+constexpr float LIFT = 40.0f;      // of maxima over large values, log2 units
 constexpr int MOST_ROWS = 1 << 24; // query rows and requests of a call
 
 constexpr int TILES = 2;           // tiles of a unit
@@ -522,6 +529,8 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
       }
       float m_run[NT], l_run[NT];
       f32x4 o[NT][DT];
+      float lift = 0.0f;             // LIFT from the first large scale on
+      uint32_t watch = 0x80808080u;  // and then 0
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         m_run[nt] = -INFINITY;
@@ -529,6 +538,19 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
 #pragma unroll
         for (int j = 0; j < DT; ++j) o[nt][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
       }
+
+      // sums relative to other maxima
+      auto rescale = [&](int nt, float m_new) {
+        const float alpha = m_new == m_run[nt] ? 1.0f : __builtin_amdgcn_exp2f(m_run[nt] - m_new);
+        l_run[nt] *= alpha;
+        m_run[nt] = m_new;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float f = __shfl(alpha, 4 * q + j, 64);  // column 4q + j's
+#pragma unroll
+          for (int d = 0; d < DT; ++d) o[nt][d][j] *= f;
+        }
+      };
 
       for (int kt = first; kt < stop; ++kt) {
         // this unit's records have landed; of those behind it, RING - TILES at most are on their way
@@ -612,6 +634,16 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
           }
           nan_v = nan != 0;
         }
+        // scales of 2^65 and more: their bytes start with two ones
+        uint32_t large = 0;
+#pragma unroll
+        for (int x = 0; x < TILES; ++x) large |= vs[x] & vs[x] << 1;
+        if (__any(large & watch)) {
+          lift = LIFT;
+          watch = 0;
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) rescale(nt, m_run[nt] + LIFT);
+        }
         // weights
         uint32_t pw[NT][PP][4];
 #pragma unroll
@@ -619,20 +651,9 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
           float mx = -INFINITY;
 #pragma unroll
           for (int i = 0; i < NV; ++i) mx = fmaxf(mx, sc[nt][i]);
-          mx *= scale_log2;
+          mx = fmaf(mx, scale_log2, lift);
           mx = max_over_q(mx);
-          if (__any(mx > m_run[nt] + SLACK)) {
-            const float m_new = fmaxf(m_run[nt], mx);
-            const float alpha = m_new == m_run[nt] ? 1.0f : __builtin_amdgcn_exp2f(m_run[nt] - m_new);
-            l_run[nt] *= alpha;
-            m_run[nt] = m_new;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const float f = __shfl(alpha, 4 * q + j, 64);  // column 4q + j's
-#pragma unroll
-              for (int d = 0; d < DT; ++d) o[nt][d][j] *= f;
-            }
-          }
+          if (__any(mx > m_run[nt] + SLACK)) rescale(nt, fmaxf(m_run[nt], mx));
           // a column that has seen nothing yet: weights of 0
           const float m = m_run[nt] == -INFINITY ? 0.0f : m_run[nt];
           float e[NV];

@@ -10,8 +10,10 @@ torch = pytest.importorskip("torch")
 
 from paper_2608_14635_amd import harness as Hn  # noqa: E402
 from paper_2608_14635_amd import kvr  # noqa: E402
+from paper_2608_14635_amd import workloads as W  # noqa: E402
 
 import packed_util as P  # noqa: E402
+import test_packed_attention as TA  # noqa: E402
 
 U = 2.0 ** -24
 ONE_HEAD = dataclasses.replace(P.F32[128], num_layers=1, num_q_heads=4, num_kv_heads=1)
@@ -116,3 +118,102 @@ def test_lengths_up_to_the_largest_number():
     out = a.attend(q[:2], [-5, -(1 << 31)], table[:2], max_len=40)
     assert (out == 0).all()
     a.release()
+
+
+class ByDim(TA.Batch):
+    """A batch whose K and V the test chooses, and whose tolerance goes by each dim's own
+    values: an output element is sum p_j v_j of its dim, so the errors of the weights
+    (test_packed_attention.py lists them) count times the largest |v_j| there.  Where V comes
+    near the largest number an exponential's argument may be some 40 more and rounded to 2^-19, in
+    the weights and where sums meet: 4 ln 2 2^-19 relative."""
+
+    def put(self, k, v):
+        dt, w = P.torch_dtype(self.shape), self.shape.num_kv_heads * self.shape.head_dim
+        k, v = (torch.tensor(x, dtype=torch.float64).to(dt).cuda().view(-1, w) for x in (k, v))
+        self.store(k, v, np.concatenate(self.slots))
+
+    def reference(self):
+        s, g = self.shape, self.shape.num_q_heads // self.shape.num_kv_heads
+        d = s.head_dim
+        kc, vc, ks, vs = (a[self.layer] for a in self.arena.parts())
+        q = self.q.float().cpu().numpy().astype(np.float64).reshape(self.rows, -1, g, d)
+        out, tol = np.zeros(q.shape), np.zeros(q.shape)
+        split = 2.0 ** -17 if s.dtype == W.BF16 else U
+        half = torch.finfo(P.torch_dtype(s)).eps / 2
+        for r, n in enumerate(self.lens):
+            sl = self.slots[r]
+            k, v = (P.values(c[sl], x[sl]).swapaxes(0, 1) for c, x in ((kc, ks), (vc, vs)))  # [nkv, n, d]
+            for i in range(self.counts[r]):
+                row, seen = self.off[r] + i, n - self.counts[r] + i + 1
+                if seen < 1:
+                    continue
+                x = q[row] @ k[:, :seen].swapaxes(1, 2) / np.sqrt(d)                        # [nkv, g, seen]
+                a = (np.abs(q[row]) @ np.abs(k[:, :seen]).swapaxes(1, 2)).max(-1) / np.sqrt(d)
+                p = np.exp(x - x.max(-1, keepdims=True))
+                p /= p.sum(-1, keepdims=True)
+                out[row] = p @ v[:, :seen]
+                rel = (2 * (d + 8) * a + 8 + 4 * a + 2 * (seen + 16)) * U + split
+                rel += 2.8 * 2.0 ** -19 * (np.abs(v).max() >= 2.0 ** 65)
+                tol[row] = rel[..., None] * np.abs(v[:, :seen]).max(1)[:, None] + half * np.abs(out[row])
+        return out.reshape(self.rows, -1, d), tol.reshape(self.rows, -1, d) + 2.0 ** -120
+
+
+HUGE = 6 * 2.0 ** 125  # the largest value a packed arena holds
+
+
+def large_values(kind, b, rng):
+    """V [n, nkv, d] over all requests' positions: all of them large; the first half of each
+    request's ordinary and the second large; one position's in one group; and all tiny."""
+    n, nkv, d = int(b.lens.sum()), b.shape.num_kv_heads, b.shape.head_dim
+    v = rng.choice(P.VALUES, size=(n, nkv, d))
+    o = np.concatenate([[0], np.cumsum(b.lens)])
+    if kind == "all":
+        return v * 2.0 ** 125
+    if kind == "tiny":
+        return v * 2.0 ** -100
+    for r, m in enumerate(b.lens):
+        if kind == "late":
+            v[o[r] + m // 2:o[r + 1]] *= 2.0 ** 125
+        elif m:
+            v[o[r] + m // 3, :, 32 * (r % (d // 32)):][..., :32] = HUGE * rng.choice([-1, 1])
+    return v
+
+
+# one request whose sums come together from a few workgroups up to (two kv heads alone) more
+# than the second kernel loads at a time
+TOGETHER = {"bf16": ([1 + 32 * 4 * n for n in (3, 7, 15, 31)], 8), "bf16_2": ([32 * 4 * 90], 2),
+            "f32_32": ([1 + 32 * 4 * n for n in (3, 7, 15, 31)], 8), "f32_64": ([32 * 4 * n + 9 for n in (4, 13, 30)], 4),
+            "f32_128": ([32 * 4 * n + 9 for n in (4, 13, 30)], 2), "f32_128_1": ([32 * 4 * 70 + 5], 1)}
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["all", "late"])
+@pytest.mark.parametrize("case", list(TOGETHER))
+def test_large_values_from_many_workgroups(case, kind):
+    lens, nkv = TOGETHER[case]
+    name = case if case in P.SHAPES else case.rsplit("_", 1)[0]
+    shape = dataclasses.replace(TA.heads(name), num_kv_heads=nkv, num_q_heads=3 * nkv if nkv > 1 else 4)
+    for n in lens:
+        b = ByDim(shape, [n], [2], seed=n)
+        rng = np.random.default_rng(n)
+        b.put(rng.normal(size=(n, nkv, shape.head_dim)), large_values(kind, b, rng))
+        b.run()
+        torch.cuda.synchronize()
+        b.check()
+        b.release()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["all", "late", "one", "tiny"])
+@pytest.mark.parametrize("name,g", [("bf16", 4), ("f32_32", 3), ("f32_64", 8), ("f32_128", 4)])
+@pytest.mark.parametrize("lens,counts", [([3000, 1, 700, 257, 33, 0], None), ([90, 40, 300], [1, 9, 70])])
+def test_values_next_to_the_largest(name, g, kind, lens, counts):
+    """V up to 1.5 * 2^127: outputs lie between the values, whatever their sums are."""
+    b = ByDim(TA.heads(name, g), lens, counts, seed=len(lens))
+    rng = np.random.default_rng(len(kind))
+    k = rng.normal(size=(int(b.lens.sum()), b.shape.num_kv_heads, b.shape.head_dim))
+    b.put(k * np.linspace(0.3, 1.5, len(k))[:, None, None], large_values(kind, b, rng))
+    b.run()
+    torch.cuda.synchronize()
+    b.check()
+    b.release()
