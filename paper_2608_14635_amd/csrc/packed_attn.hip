@@ -254,6 +254,10 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
 }
 
+// The nearest number to a query's that does not round to an infinite bf16 one (of an infinite
+// query it leaves an infinite rest).
+__device__ __forceinline__ float near_bf16(float v) { return __builtin_amdgcn_fmed3f(v, -0x1.fep127f, 0x1.fep127f); }
+
 // What a wave's stretch holds of items that are not its own alone: of one begun before
 // it ([0]), of one it leaves open ([1]).
 struct Stretch {
@@ -518,7 +522,7 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
               union { uint32_t w[4]; bf16x8 f; } f;
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
-                f.w[e] = pack_bf16(x[2 * e], x[2 * e + 1]);
+                f.w[e] = part ? pack_bf16(x[2 * e], x[2 * e + 1]) : pack_bf16(near_bf16(x[2 * e]), near_bf16(x[2 * e + 1]));
                 x[2 * e] -= __uint_as_float(f.w[e] << 16);
                 x[2 * e + 1] -= __uint_as_float(f.w[e] & 0xffff0000u);
               }

@@ -217,3 +217,30 @@ def test_values_next_to_the_largest(name, g, kind, lens, counts):
     torch.cuda.synchronize()
     b.check()
     b.release()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name,g", [("f32_32", 3), ("f32_64", 8), ("f32_128", 4), ("bf16", 4)])
+def test_queries_next_to_the_largest(name, g):
+    """Queries up to the largest number of their type, above the largest bf16 one in fp32,
+    against K whose products with them are ordinary; infinite and NaN ones beside them."""
+    b = ByDim(TA.heads(name, g), [300, 70, 33, 40, 50], [2, 5, 1, 1, 1], seed=3)
+    n, nkv, d = int(b.lens.sum()), b.shape.num_kv_heads, b.shape.head_dim
+    rng = np.random.default_rng(4)
+    k = np.zeros((n, nkv, d))
+    k[..., :32] = rng.choice(P.VALUES, size=(n, nkv, 32)) * 2.0 ** -120
+    b.put(k, rng.choice(P.VALUES, size=(n, nkv, d)))
+    most = torch.finfo(b.q.dtype).max
+    q = torch.tensor(rng.choice([-1, -0.999, -0.99609375, 0.998, 1, 0.5], size=(b.rows, b.q.shape[1])))
+    q = torch.where(torch.arange(b.q.shape[1]) % d % 32 < 5, q * most, q * 2.0 ** 100).to(b.q.dtype)
+    q[8, 0] = float("inf")
+    q[9, 2] = float("nan")
+    b.q.copy_(q)
+    b.run()
+    torch.cuda.synchronize()
+    with np.errstate(invalid="ignore"):
+        want, tol = b.reference()
+    got = b.out[:, :b.q.shape[1]].double().cpu().numpy().reshape(want.shape)
+    assert (np.abs(got[:8] - want[:8]) <= tol[:8]).all()
+    assert np.isnan(got[8:, 0]).all() and np.isfinite(got[8:, 1:]).all()
+    b.release()
