@@ -243,12 +243,18 @@ __device__ __forceinline__ float block_most(float v, float* red) {
   return v;
 }
 
+// scale (a - b) - off.  A difference that passes the largest number is taken of the halves.
+__device__ __forceinline__ float scaled_difference(float a, float b, float scale, float off) {
+  const float d = a - b;
+  return fabsf(d) < INFINITY ? fmaf(d, scale, -off) : fmaf(2.0f, (0.5f * a - 0.5f * b) * scale, -off);
+}
+
 // A chunk's largest logit and sums, added to those of its row, whose t is relative to
 // `base`: by the two logits, and without the rounding of the chunk's C.
 __device__ __forceinline__ void add_chunk(float m, float chunk_l, float chunk_s, float base, float scale2, float& l,
                                           float& s) {
   const float cm = c_of(base_of(m), scale2), off = by_c(cm) ? fmaf(base_of(m), scale2, -cm) : 0.0f;
-  const float x = fmaxf(fmaf(m - base, scale2, -off), -1e30f);
+  const float x = fmaxf(scaled_difference(m, base, scale2, off), -1e30f);
   const float e = __builtin_amdgcn_exp2f(x);
   l = fmaf(chunk_l, e, l);
   s += e * fmaf(x, chunk_l, chunk_s);
@@ -275,7 +281,7 @@ struct Row {
     s_l = s / l;
   }
   __device__ __forceinline__ float logprob(const LogprobParams& p, float v) const {
-    return none ? -INFINITY : (v - base) * p.scale - LN2 * log_l;
+    return none ? -INFINITY : scaled_difference(v, base, p.scale, LN2 * log_l);
   }
   __device__ __forceinline__ void put(const LogprobParams& p) const {
     if (p.logprobs)
