@@ -28,7 +28,9 @@ extern "C" {
  *                  already (NULL: none); a negative one counts as 0
  *   lens           device int32 [num_requests]; a request with len <= held
  *                  grows nothing.  The sum of the new positions stays below 2^31
- *   free_blocks    device int32 [num_free] block ids, handed out as they are
+ *   free_blocks    device int32 [num_free] block ids, handed out as they are.  A
+ *                  negative one counts as a block: it is written to its table entry,
+ *                  whose rows get slot -1 without being among counts[3]
  *   block_tables   device int32 [num_requests][max_blocks_per_req], in and out:
  *                  the needed entries are written (-1 where the free list has
  *                  ended), all others keep their bits
@@ -44,7 +46,8 @@ extern "C" {
  *   positions      optional device int32 [max_rows] (NULL = none), written: per
  *                  row its position, -1 behind the last row
  *   counts         device int32 [4], written: blocks taken from the list, blocks
- *                  it lacked, rows, rows without a slot
+ *                  it lacked, rows, rows without a slot (for lack of a block, of
+ *                  room in the table, or in a negative entry held before)
  * No host synchronisation, no workspace; the same call again writes the same.
  *   KV_EINVAL  null arrays, num_requests, num_free, max_blocks_per_req or
  *              max_rows < 0, num_requests above 2^30, block_size <= 0, an array not

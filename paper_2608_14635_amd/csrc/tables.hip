@@ -107,7 +107,8 @@ __global__ __launch_bounds__(TG_NT) void tables_grow_kernel(GrowParams p) {
       if (blockIdx.x == 0 && win == 0 && r < p.R) {
         p.row_offsets[r] = (int32_t)row;
         // rows without a slot: an old last block that is none, then the positions
-        // from the first entry the list or the table has no room for
+        // from the first entry the list or the table has no room for.  (The list's
+        // ids are not looked at: this workgroup would read all that are handed out.)
         const uint32_t len = (uint32_t)held + n;
         uint32_t from = held;  // first position of the new entries
         if (n > 0 && have * B > (uint32_t)held) {
