@@ -244,3 +244,64 @@ def test_queries_next_to_the_largest(name, g):
     assert (np.abs(got[:8] - want[:8]) <= tol[:8]).all()
     assert np.isnan(got[8:, 0]).all() and np.isfinite(got[8:, 1:]).all()
     b.release()
+
+
+def equal_weights(b, codes):
+    """Queries of 0 weigh all positions alike: with V = 1 in one dim a position (codes: of each
+    request, [nkv, n] dims, -1 for none) an output is the share of positions of that
+    dim.  Counts and sums are whole numbers, exact in fp32; the quotient takes two roundings and
+    the output's own."""
+    nkv, d = b.shape.num_kv_heads, b.shape.head_dim
+    g, dt = b.shape.num_q_heads // nkv, P.torch_dtype(b.shape)
+    tol = torch.finfo(dt).eps / 2 + 4 * U
+    for r, code in enumerate(codes):
+        n = code.shape[1]
+        if n == 0:
+            continue
+        v = torch.zeros(n, nkv, d + 1, dtype=dt, device="cuda").scatter_(2, torch.where(code < 0, d, code).t()[..., None], 1.0)[..., :d]
+        k = torch.randn(n, nkv * d, device="cuda").to(dt)
+        b.store(k, v.reshape(n, -1).contiguous(), b.slots[r])
+    b.q.zero_()
+    b.out.fill_(TA.KEPT)
+    b.run()
+    torch.cuda.synchronize()
+    out = b.out[:, :b.q.shape[1]].double().view(b.rows, nkv, g, d)
+    for r, code in enumerate(codes):
+        for i in range(b.counts[r]):
+            seen = code.shape[1] - b.counts[r] + i + 1
+            if seen < 1:
+                assert (out[b.off[r] + i] == 0).all()
+                continue
+            count = torch.stack([torch.bincount(c[c >= 0], minlength=d) for c in code[:, :seen]]).double()
+            want = (count / seen)[:, None].expand(nkv, g, d)
+            assert ((out[b.off[r] + i] - want).abs() <= tol * want).all(), (r, i)
+    return tol
+
+
+EVERY = {"bf16": (8, 4, [70001], [1]), "bf16_2": (2, 4, [70001, 5], [3, 1]), "bf16_ragged": (8, 4, [9000, 1, 4097, 20000, 0], [1, 1, 4, 1, 1]),
+         "f32_32": (8, 2, [20011], [1]), "f32_64": (4, 1, [5000, 3], [2, 1]), "f32_128": (1, 4, [40000, 333], [1, 70]),
+         "bf16_many": (8, 4, [1 + (37 * i) % 90 for i in range(520)], [1] * 520)}
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("case", list(EVERY))
+def test_every_position_counts_once(case):
+    """In every kv head, first by units of 32 positions, each in one dim of its own choice, then
+    position by position, a window of each request in each kv head, in turn."""
+    nkv, g, lens, counts = EVERY[case]
+    name = case if case in P.SHAPES else "bf16"
+    b = TA.Batch(dataclasses.replace(TA.heads(name), num_kv_heads=nkv, num_q_heads=g * nkv), lens, counts, seed=nkv)
+    d = b.shape.head_dim
+    pos = [torch.arange(n, device="cuda").expand(nkv, n) for n in lens]
+    head = torch.arange(nkv, device="cuda")[:, None]
+    tol = equal_weights(b, [(p // 32 * (2 * head + 3) + 7 * head) % d for p in pos])
+    # a unit that were left out, the shortest and the fullest dim's: beyond the tolerance
+    for n in lens:
+        most = 32 * -(-n // (32 * d))
+        assert n < 64 or 32 / most - 32 / n > 4 * tol
+    parts = max(nkv, -(-max(lens) // (d * 64)))  # windows in which a position shows beside its dim's others
+    for turn in range(parts):
+        # window (turn + head) mod parts of each request
+        equal_weights(b, [torch.where(p * parts // max(n, 1) == (turn + head) % parts, p % d, -1) for p, n in zip(pos, lens)])
+    assert 1 / 65 > 2 * tol
+    b.release()
