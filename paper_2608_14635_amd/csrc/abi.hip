@@ -9,6 +9,7 @@
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
+#include <exception>
 #include <mutex>
 #include <set>
 #include <string>
@@ -242,6 +243,22 @@ bool kvr::live_arena(const kv_arena* a) {
 
 namespace {
 
+// The request that writes each block (-1: none), up to the highest one written: an arena's
+// number of blocks is the caller's word, and need not fit host memory.
+struct Writers {
+  std::vector<int32_t> of;
+  int32_t operator[](int32_t blk) const { return (size_t)blk < of.size() ? of[blk] : -1; }
+  bool set(int32_t blk, int32_t r) {
+    try {
+      if ((size_t)blk >= of.size()) of.resize((size_t)blk + 1, -1);
+    } catch (const std::exception&) {
+      return false;
+    }
+    of[blk] = r;
+    return true;
+  }
+};
+
 // starts may be null (every request from position 0).  Rules for starts:
 // 0 <= start <= len, start a multiple of 8 unless equal to len.  Blocks:
 // a block holding a position >= start of its request is written and may be
@@ -282,8 +299,7 @@ kv_status check_request(const kv_model_desc* desc, int32_t B, int64_t NB, const 
     if (tokens[i] < 0 || tokens[i] >= desc->vocab)
       return fail(KV_ERANGE, "token %d at index %lld outside [0, %d)", tokens[i], (long long)i,
                   desc->vocab);
-  // writer of each block (-1: none)
-  std::vector<int32_t> writer((size_t)NB, -1);
+  Writers writer;
   for (int32_t r = 0; r < R; ++r) {
     const int64_t nb = ((int64_t)lens[r] + B - 1) / B;
     const int64_t s0 = starts ? starts[r] : 0;
@@ -294,7 +310,7 @@ kv_status check_request(const kv_model_desc* desc, int32_t B, int64_t NB, const 
                     blk, (long long)NB);
       if ((b + 1) * B > s0 && s0 < lens[r]) {  // holds a position >= start: written
         if (writer[blk] >= 0) return fail(KV_EALIAS, "block %d listed twice", blk);
-        writer[blk] = r;
+        if (!writer.set(blk, r)) return fail(KV_ENOMEM, "host allocation failed");
       }
     }
   }
@@ -425,12 +441,12 @@ kv_status check_decode(const kv_model_desc* desc, int32_t B, int64_t NB, const i
         return fail(KV_ERANGE, "block_tables[%d][%d] = %d outside [0, %lld)", r, b, blk,
                     (long long)NB);
     }
-  std::vector<int32_t> writer((size_t)NB, -1);
+  Writers writer;
   for (int32_t r = 0; r < R; ++r) {
     const int32_t blk = tables[(int64_t)r * max_blocks + positions[r] / B];
     if (writer[blk] >= 0)
       return fail(KV_EALIAS, "block %d holds the new positions of requests %d and %d", blk, writer[blk], r);
-    writer[blk] = r;
+    if (!writer.set(blk, r)) return fail(KV_ENOMEM, "host allocation failed");
   }
   for (int32_t r = 0; r < R; ++r)
     for (int32_t b = 0; b <= positions[r] / B; ++b) {
