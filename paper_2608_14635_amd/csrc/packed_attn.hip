@@ -36,12 +36,12 @@
 //
 // What bounds it: the records' way from HBM and what a call costs once.  16 requests of
 // 2048 - 16384 positions (8 kv heads of 128, 4 q heads each, 124 MB of records), one query
-// row each: 29.5 us; without the products and the softmax 28.0, without the loads 21.1.
-// 1.1 us of them are the plan, 4 the way to the first record (three loads that follow each
-// other, while other waves' records keep the memory busy), 2 the merges.  Two requests of
-// 150 - 200 thousand positions (403 MB): 78 us, without products and softmax the same.
-// One to five query rows of 40 requests of 300 - 4000 positions (5 q heads a kv head, 88 MB
-// and some of it twice): 29 us.
+// row each: 29.7 us.  1.8 of them are the plan (2.8 with 1100 requests, 9.7 with 4000, which
+// every workgroup reads), 4.6 the way to the first record (three loads that follow each other,
+// while other waves' records keep the memory busy), 2 - 3 the merges.  Two requests of
+// 150 - 200 thousand positions (403 MB): 78 us, of which the records' way at a large read's
+// rate is 67.  One to five query rows of 40 requests of 300 - 4000 positions (5 q heads a kv
+// head, 88 MB, 34 of them twice): 29.6 us, 106 MB past the L2 caches.
 //   Workgroups a CU and records a ring: three and four.  Three and six took 31.2 us, two
 // and eight 33.7, four and four 31.1 (the long ones 79, 85 and 81).  Two column tiles need
 // the registers of two a CU: with three, registers spill, 56 us against 35 on the 40
@@ -859,9 +859,11 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
 
 // Workgroup (kv head, workgroup of the first kernel): the item that it began and left
 // open, merged over the workgroups that went on with it, in their order.  Its time is its
-// loads' way from other chiplets' caches: 3 us with few partials, 7.0 with 48 of 5
-// columns at 32 loads together (7.8 at 16, 8.5 at 8), 4.8 with five to eight of 16 columns
-// at 8 (6.2 at 16).
+// loads' way from other chiplets' caches: 3 us with few partials, 6.8 with 48 of 5 columns.
+// The loads on their way together are the least of four numbers that holds the partials:
+// those past the last are loaded for nothing, and every round waits once.  At 32 always, 16
+// requests of 16 columns (five to eight partials each) take 12.3 us, not 4.9, 8 of 256 columns
+// 17.6, not 5.4; at 16 and more 6.9 and 10.2; at 8 and less the 48 partials 8.3.
 constexpr int PM_NT = 256;
 template <typename T, int D, int NT>
 __global__ __launch_bounds__(PM_NT) void packed_attn_merge_kernel(PackedAttnParams p) {
@@ -891,7 +893,7 @@ __global__ __launch_bounds__(PM_NT) void packed_attn_merge_kernel(PackedAttnPara
 }
 
 // The kernel for a call's columns per request.  A request with more than 16 NT has several
-// items, whose waves read its records again, mostly from the caches; two column tiles a
+// items, whose waves read its records again, about half of them from the L2 caches; two column tiles a
 // wave spare half of that and cost the third workgroup of a CU.  16 requests of 2000 - 6000
 // positions with 80 columns (8 kv heads) took 44 us with one and 52 with two, 8 with 128
 // 41 and 47, 8 with 256 47.9 and 47.5, 4 with 512 78 and 72, one with 2048 94 and 84.  (Four
