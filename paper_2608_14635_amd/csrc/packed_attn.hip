@@ -861,9 +861,9 @@ __global__ __launch_bounds__(PA_NT, OCC) void packed_attn_kernel(PackedAttnParam
 // open, merged over the workgroups that went on with it, in their order.  Its time is its
 // loads' way from other chiplets' caches: 3 us with few partials, 6.8 with 48 of 5 columns.
 // The loads on their way together are the least of four numbers that holds the partials:
-// those past the last are loaded for nothing, and every round waits once.  At 32 always, 16
-// requests of 16 columns (five to eight partials each) take 12.3 us, not 4.9, 8 of 256 columns
-// 17.6, not 5.4; at 16 and more 6.9 and 10.2; at 8 and less the 48 partials 8.3.
+// those past the last are loaded for nothing, and every round waits once.  At 32 always, 40
+// requests of 4 - 25 columns take 12.3 us, not 4.9, 8 of up to 256 columns 17.6, not 5.4; at 16
+// and more 6.9 and 10.2; at 8 and less the 48 partials 8.3.
 constexpr int PM_NT = 256;
 template <typename T, int D, int NT>
 __global__ __launch_bounds__(PM_NT) void packed_attn_merge_kernel(PackedAttnParams p) {
