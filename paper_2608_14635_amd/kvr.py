@@ -1,6 +1,6 @@
 """Thin ctypes binding of libkvr.so (include/kvr.h, include/kvr_decode.h,
 include/kvr_ipc.h, include/kvr_verify.h, include/kvr_reuse.h, include/kvr_profile.h,
-include/kvr_tables.h, include/kvr_packed.h, include/kvr_logprob.h).
+include/kvr_tables.h, include/kvr_packed.h, include/kvr_logprob.h, include/kvr_append.h).
 
 Argument marshalling only: every step of the rebuild runs in the library's
 HIP kernels.  Device buffers are passed as integer addresses (for example a
@@ -147,6 +147,9 @@ def lib() -> C.CDLL:
     L.kv_logprobs.restype = C.c_int
     L.kv_logprobs.argtypes = [vp, C.c_int32, i64, C.c_int32, i64, C.c_float, vp, C.c_int32, vp, vp, vp, vp, vp,
                               C.c_uint64, C.c_int32, vp]
+    L.kv_append.restype = C.c_int
+    L.kv_append.argtypes = [vp, C.c_int32, C.POINTER(kv_layer_weights), vp, i64, vp, i64, vp, i64, vp, vp, i64, vp,
+                            i64, vp]
     L.kv_packed_decode_workspace_bytes.restype = C.c_uint64
     L.kv_packed_decode_workspace_bytes.argtypes = L.kv_decode_workspace_bytes.argtypes
     L.kv_packed_decode_step.restype = C.c_int
@@ -399,6 +402,18 @@ def kv_tables_grow(held: int, lens: int, num_requests: int, block_size: int, fre
                                 C.c_void_p(counts), device, C.c_void_p(stream)))
 
 
+def kv_append(arena: int, layer: int, layer_weights: Optional[Dict[str, int]], q: int, q_stride: int, k: int,
+              k_stride: int, v: int, v_stride: int, positions: int, slots: int, rows: int, q_out: int,
+              q_out_stride: int, stream: int = 0) -> None:
+    """Rows of a layer's q, k, v products rotated, K and V into the arena's slots; arrays are
+    device addresses (q and q_out 0: k and v alone).  layer_weights: the layer's biases and
+    head norms by name, where the model has them."""
+    w = kv_layer_weights(**(layer_weights or {}))
+    _check(lib().kv_append(C.c_void_p(arena), layer, C.byref(w) if layer_weights else None, C.c_void_p(q or None),
+                           q_stride, C.c_void_p(k), k_stride, C.c_void_p(v), v_stride, C.c_void_p(positions),
+                           C.c_void_p(slots), rows, C.c_void_p(q_out or None), q_out_stride, C.c_void_p(stream)))
+
+
 def kv_packed_bytes(shape_or_desc, block_size: int, num_blocks: int) -> int:
     d = shape_or_desc if isinstance(shape_or_desc, kv_model_desc) else make_desc(shape_or_desc)
     return int(lib().kv_packed_bytes(C.byref(d), block_size, num_blocks))
@@ -561,4 +576,4 @@ def exported_symbols() -> Iterable[str]:
             "kv_packed_store", "kv_packed_load", "kv_packed_park", "kv_packed_restore",
             "kv_packed_attention_workspace_bytes", "kv_packed_attention",
             "kv_packed_decode_workspace_bytes", "kv_packed_decode_step",
-            "kv_logprobs_workspace_bytes", "kv_logprobs")
+            "kv_logprobs_workspace_bytes", "kv_logprobs", "kv_append")
