@@ -30,12 +30,12 @@
 #include "common.h"
 #include "host.h"
 #include "kvr_logprob.h"
+#include "logits.h"
 
 namespace kvr {
 namespace {
 
 constexpr int LP_NT = 256;
-constexpr float LOG2E = 1.4426950408889634f;
 // Entries of a thread.  A workgroup's piece in flight is 32 KB of fp32: 1024 rows of
 // 151936 in bf16 took 70 us with 64 entries, 64 with 16 and 55 with 32; one row takes
 // as long with 16 as with 32.
@@ -43,7 +43,6 @@ constexpr int LP_ITEMS = 32;
 constexpr int LP_CHUNK = LP_NT * LP_ITEMS;
 constexpr int LP_MAX_VOCAB = 256 * LP_CHUNK;
 constexpr int64_t LP_MOST_CHUNKS = (1 << 24) - 1;  // of a call: a grid holds 2^32 - 1 threads
-constexpr float LN2 = 0.6931471805599453f;
 
 struct LogprobParams {
   const char* logits;
@@ -59,31 +58,6 @@ struct LogprobParams {
   uint64_t* keys;  // [rows][chunks][top]
 };
 
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef u32x4 u32x4_a2 __attribute__((aligned(2)));
-
-// 16 bytes of logits, on any boundary of their elements, and their values.
-template <typename T> struct Piece;
-template <> struct Piece<float> {
-  static constexpr int N = 4;
-  f32x4 w;
-  __device__ __forceinline__ void load(const float* p) { w = *reinterpret_cast<const f32x4_a4*>(p); }
-  __device__ __forceinline__ void set(int j, float v) { w[j] = v; }
-  __device__ __forceinline__ float value(int j) const { return w[j]; }
-};
-template <> struct Piece<bf16_t> {
-  static constexpr int N = 8;
-  u32x4 w;
-  __device__ __forceinline__ void load(const bf16_t* p) { w = *reinterpret_cast<const u32x4_a2*>(p); }
-  __device__ __forceinline__ void set(int j, float v) {  // of a bf16 number
-    const uint32_t b = __float_as_uint(v) >> 16;
-    w[j / 2] = j % 2 ? (w[j / 2] & 0xffffu) | b << 16 : (w[j / 2] & 0xffff0000u) | b;
-  }
-  __device__ __forceinline__ float value(int j) const {
-    return __uint_as_float(j % 2 ? w[j / 2] & 0xffff0000u : w[j / 2] << 16);
-  }
-};
-
 // Unsigned numbers that order as the values do; -0 as +0, NaN below all.
 __device__ __forceinline__ uint32_t order_bits(float z) {
   const uint32_t b = __float_as_uint(z + 0.0f);
@@ -96,29 +70,6 @@ __device__ __forceinline__ uint64_t make_key(uint32_t order, uint32_t index) {
   return (uint64_t)order << 32 | (0xffffffffu - index);
 }
 __device__ __forceinline__ uint32_t key_index(uint64_t k) { return 0xffffffffu - (uint32_t)k; }
-
-// f over the wave's lanes, in every lane: neighbours, pairs, fours and eights of a row of
-// 16 by lane moves within it, then the rows.
-template <typename F>
-__device__ __forceinline__ float over_wave(float v, F f) {
-  const auto moved = [&](auto ctrl) {
-    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(ctrl)::value, 0xf, 0xf, true));
-  };
-  v = f(v, moved(std::integral_constant<int, 0xb1>{}));   // quad_perm 1 0 3 2
-  v = f(v, moved(std::integral_constant<int, 0x4e>{}));   // quad_perm 2 3 0 1
-  v = f(v, moved(std::integral_constant<int, 0x141>{}));  // row_half_mirror
-  v = f(v, moved(std::integral_constant<int, 0x140>{}));  // row_mirror
-  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  v = f(__uint_as_float(a[0]), __uint_as_float(a[1]));
-  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return f(__uint_as_float(b[0]), __uint_as_float(b[1]));
-}
-__device__ __forceinline__ float max_over_wave(float v) {
-  return over_wave(v, [](float a, float b) { return fmaxf(a, b); });
-}
-__device__ __forceinline__ float sum_over_wave(float v) {
-  return over_wave(v, [](float a, float b) { return a + b; });
-}
 
 // Ranks by counting: how many of the n keys in LDS are larger.
 __device__ __forceinline__ int rank_of(uint64_t key, const uint64_t* keys, int n) {
@@ -214,17 +165,6 @@ __device__ __forceinline__ uint64_t bound_of_keys(uint64_t own, int top, S& s) {
   return bound;
 }
 
-// What logits are taken relative to: -infinity stands for no logit above it, and
-// differences with it would be NaN.
-__device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.0f : m; }
-// C of a maximum: rounded, not contracted into what it enters.
-__device__ __forceinline__ float c_of(float m, float scale2) {
-#pragma clang fp contract(off)
-  return m * scale2;
-}
-// Whether C stands for c m up to 2^-5.
-__device__ __forceinline__ bool by_c(float c) { return fabsf(c) < 0x1p20f; }
-
 // Sums and maximum over the workgroup, in every thread; red holds a value a wave.
 __device__ __forceinline__ float2 block_total(float a, float b, float2* red) {
   a = sum_over_wave(a);
@@ -246,23 +186,6 @@ __device__ __forceinline__ float block_most(float v, float* red) {
 #pragma unroll
   for (int i = 0; i < LP_NT / 64; ++i) v = fmaxf(v, red[i]);
   return v;
-}
-
-// scale (a - b) - off.  A difference that passes the largest number is taken of the halves.
-__device__ __forceinline__ float scaled_difference(float a, float b, float scale, float off) {
-  const float d = a - b;
-  return fabsf(d) < INFINITY ? fmaf(d, scale, -off) : fmaf(2.0f, (0.5f * a - 0.5f * b) * scale, -off);
-}
-
-// A chunk's largest logit and sums, added to those of its row, whose t is relative to
-// `base`: by the two logits, and without the rounding of the chunk's C.
-__device__ __forceinline__ void add_chunk(float m, float chunk_l, float chunk_s, float base, float scale2, float& l,
-                                          float& s) {
-  const float cm = c_of(base_of(m), scale2), off = by_c(cm) ? fmaf(base_of(m), scale2, -cm) : 0.0f;
-  const float x = fmaxf(scaled_difference(m, base, scale2, off), -1e30f);
-  const float e = __builtin_amdgcn_exp2f(x);
-  l = fmaf(chunk_l, e, l);
-  s += e * fmaf(x, chunk_l, chunk_s);
 }
 
 // A row's token and its logit, then the results from the row's sums.

@@ -1,6 +1,7 @@
 """Thin ctypes binding of libkvr.so (include/kvr.h, include/kvr_decode.h,
 include/kvr_ipc.h, include/kvr_verify.h, include/kvr_reuse.h, include/kvr_profile.h,
-include/kvr_tables.h, include/kvr_packed.h, include/kvr_logprob.h, include/kvr_append.h).
+include/kvr_tables.h, include/kvr_packed.h, include/kvr_logprob.h, include/kvr_append.h,
+include/kvr_policy.h).
 
 Argument marshalling only: every step of the rebuild runs in the library's
 HIP kernels.  Device buffers are passed as integer addresses (for example a
@@ -147,6 +148,11 @@ def lib() -> C.CDLL:
     L.kv_logprobs.restype = C.c_int
     L.kv_logprobs.argtypes = [vp, C.c_int32, i64, C.c_int32, i64, C.c_float, vp, C.c_int32, vp, vp, vp, vp, vp,
                               C.c_uint64, C.c_int32, vp]
+    L.kv_policy_loss_workspace_bytes.restype = C.c_uint64
+    L.kv_policy_loss_workspace_bytes.argtypes = [i64, C.c_int32]
+    L.kv_policy_loss.restype = C.c_int
+    L.kv_policy_loss.argtypes = [vp, C.c_int32, i64, C.c_int32, i64, C.c_float, vp, vp, vp, vp, vp, C.c_float, C.c_float,
+                                 C.c_float, vp, vp, vp, vp, vp, i64, vp, C.c_uint64, C.c_int32, vp]
     L.kv_append.restype = C.c_int
     L.kv_append.argtypes = [vp, C.c_int32, C.POINTER(kv_layer_weights), vp, i64, vp, i64, vp, i64, vp, vp, i64, vp,
                             i64, vp]
@@ -512,6 +518,23 @@ def kv_logprobs(logits: int, dtype: int, rows: int, vocab: int, stride: int, sca
                              C.c_void_p(workspace), workspace_bytes, device, C.c_void_p(stream)))
 
 
+def kv_policy_loss_workspace_bytes(rows: int, vocab: int) -> int:
+    return int(lib().kv_policy_loss_workspace_bytes(rows, vocab))
+
+
+def kv_policy_loss(logits: int, dtype: int, rows: int, vocab: int, stride: int, scale: float, tokens: int,
+                   old_logprobs: int, ref_logprobs: int, advantages: int, weights: int, clip_low: float,
+                   clip_high: float, kl_coef: float, total: int, losses: int, logprobs: int, kls: int, grad: int,
+                   grad_stride: int, workspace: int, workspace_bytes: int, device: int = 0, stream: int = 0) -> None:
+    """The clipped policy loss of the rows' tokens and the gradient of their logits; arrays
+    are device addresses (0: not given, or not wanted)."""
+    p = lambda a: C.c_void_p(a or None)  # noqa: E731
+    _check(lib().kv_policy_loss(p(logits), dtype, rows, vocab, stride, scale, p(tokens), p(old_logprobs),
+                                p(ref_logprobs), p(advantages), p(weights), clip_low, clip_high, kl_coef, p(total),
+                                p(losses), p(logprobs), p(kls), p(grad), grad_stride, p(workspace), workspace_bytes,
+                                device, p(stream)))
+
+
 def kv_ipc_export(ptr: int, nbytes: int) -> bytes:
     """Owner side: the handle of device memory [ptr, ptr+nbytes) as plain bytes."""
     h = kv_ipc_handle()
@@ -576,4 +599,5 @@ def exported_symbols() -> Iterable[str]:
             "kv_packed_store", "kv_packed_load", "kv_packed_park", "kv_packed_restore",
             "kv_packed_attention_workspace_bytes", "kv_packed_attention",
             "kv_packed_decode_workspace_bytes", "kv_packed_decode_step",
-            "kv_logprobs_workspace_bytes", "kv_logprobs", "kv_append")
+            "kv_logprobs_workspace_bytes", "kv_logprobs", "kv_append",
+            "kv_policy_loss_workspace_bytes", "kv_policy_loss")
