@@ -1,7 +1,7 @@
 """Thin ctypes binding of libkvr.so (include/kvr.h, include/kvr_decode.h,
 include/kvr_ipc.h, include/kvr_verify.h, include/kvr_reuse.h, include/kvr_profile.h,
 include/kvr_tables.h, include/kvr_packed.h, include/kvr_logprob.h, include/kvr_append.h,
-include/kvr_policy.h).
+include/kvr_attention.h, include/kvr_policy.h).
 
 Argument marshalling only: every step of the rebuild runs in the library's
 HIP kernels.  Device buffers are passed as integer addresses (for example a
@@ -153,6 +153,11 @@ def lib() -> C.CDLL:
     L.kv_policy_loss.restype = C.c_int
     L.kv_policy_loss.argtypes = [vp, C.c_int32, i64, C.c_int32, i64, C.c_float, vp, vp, vp, vp, vp, C.c_float, C.c_float,
                                  C.c_float, vp, vp, vp, vp, vp, i64, vp, C.c_uint64, C.c_int32, vp]
+    L.kv_group_attention_workspace_bytes.restype = C.c_uint64
+    L.kv_group_attention_workspace_bytes.argtypes = [C.POINTER(kv_model_desc), C.c_int32, i64, C.c_int32, C.c_int32, i64]
+    L.kv_group_attention.restype = C.c_int
+    L.kv_group_attention.argtypes = [vp, C.c_int32, vp, i64, vp, i64, vp, vp, C.c_int32, C.c_int32, vp, vp, C.c_int32,
+                                     C.c_int32, i64, vp, i64, vp, C.c_uint64, vp]
     L.kv_append.restype = C.c_int
     L.kv_append.argtypes = [vp, C.c_int32, C.POINTER(kv_layer_weights), vp, i64, vp, i64, vp, i64, vp, vp, i64, vp,
                             i64, vp]
@@ -420,6 +425,25 @@ def kv_append(arena: int, layer: int, layer_weights: Optional[Dict[str, int]], q
                            C.c_void_p(slots), rows, C.c_void_p(q_out or None), q_out_stride, C.c_void_p(stream)))
 
 
+def kv_group_attention_workspace_bytes(shape_or_desc, num_requests: int, rows: int, num_groups: int, max_query: int,
+                                       max_len: int) -> int:
+    d = shape_or_desc if isinstance(shape_or_desc, kv_model_desc) else make_desc(shape_or_desc)
+    return int(lib().kv_group_attention_workspace_bytes(C.byref(d), num_requests, rows, num_groups, max_query, max_len))
+
+
+def kv_group_attention(arena: int, layer: int, q: int, q_stride: int, q_offsets: int, rows: int, lens: int, tables: int,
+                       num_requests: int, max_blocks: int, group_offsets: int, prefix_lens: int, num_groups: int,
+                       max_query: int, max_len: int, out: int, out_stride: int, workspace: int, workspace_bytes: int,
+                       stream: int = 0) -> None:
+    """Attention of one layer over the arena, a group's shared prefix read once; arrays are
+    device addresses."""
+    _check(lib().kv_group_attention(C.c_void_p(arena), layer, C.c_void_p(q), q_stride, C.c_void_p(q_offsets or None),
+                                    rows, C.c_void_p(lens), C.c_void_p(tables), num_requests, max_blocks,
+                                    C.c_void_p(group_offsets or None), C.c_void_p(prefix_lens or None), num_groups,
+                                    max_query, max_len, C.c_void_p(out), out_stride, C.c_void_p(workspace),
+                                    workspace_bytes, C.c_void_p(stream)))
+
+
 def kv_packed_bytes(shape_or_desc, block_size: int, num_blocks: int) -> int:
     d = shape_or_desc if isinstance(shape_or_desc, kv_model_desc) else make_desc(shape_or_desc)
     return int(lib().kv_packed_bytes(C.byref(d), block_size, num_blocks))
@@ -600,4 +624,5 @@ def exported_symbols() -> Iterable[str]:
             "kv_packed_attention_workspace_bytes", "kv_packed_attention",
             "kv_packed_decode_workspace_bytes", "kv_packed_decode_step",
             "kv_logprobs_workspace_bytes", "kv_logprobs", "kv_append",
-            "kv_policy_loss_workspace_bytes", "kv_policy_loss")
+            "kv_policy_loss_workspace_bytes", "kv_policy_loss",
+            "kv_group_attention_workspace_bytes", "kv_group_attention")
