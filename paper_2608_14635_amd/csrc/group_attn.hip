@@ -31,6 +31,7 @@
 #include <type_traits>
 
 #include "common.h"
+#include "dma.h"
 #include "host.h"
 #include "kvr_attention.h"
 
@@ -47,15 +48,11 @@ constexpr int KNOWN = 512;                   // groups whose offsets are kept in
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef u32x4 u32x4_a4 __attribute__((aligned(4)));
 
-template <typename T> struct Unit;
-template <> struct Unit<bf16_t> { static constexpr int POS = 32; };
-template <> struct Unit<float> { static constexpr int POS = 16; };
-
 // What the second kernel has to know of an entity: where its items' units begin, what each
 // counts, its first item among its kind, its first query row and its columns, its request's group.
 struct Entity {
   uint32_t base, item;
-  int first, row, cols, group, pad[2];
+  int first, row, cols, group, lo, pad;
 };
 struct Plan {
   uint32_t size, longer, workers, pad[5];
@@ -213,6 +210,12 @@ __device__ __forceinline__ Shape shape_of(const GroupAttnParams& p, const Groups
   return finish_shape<COLS, POS>(p, s);
 }
 
+// The same in every lane, and known to be.
+__device__ __forceinline__ Shape uniform(Shape s) {
+  const auto u = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+  return Shape{u(s.row), u(s.cols), u(s.lo), u(s.hi), u(s.table), u(s.group), u(s.tiles), (uint32_t)u((int)s.item)};
+}
+
 // Positions that a query row of a prefix's columns sees.
 __device__ __forceinline__ int limit_in_group(const GroupAttnParams& p, const Groups& groups, int e, int row) {
   if (!p.q_offsets) return p.lens[row];
@@ -256,162 +259,142 @@ __device__ __forceinline__ void store_out(T* dst, const float* v) {
 // dims q d/4 .., V's c d/16 ...
 template <typename T, int D> struct Regs;
 template <int D> struct Regs<bf16_t, D> {
-  static constexpr int TILES = 2, NK = D / 32, NV = 4 * TILES;
+  static constexpr int POS = 32, TILES = 2, NK = D / 32, NS = 4 * TILES;
+  typedef u32x4 Word;
   u32x4 k[TILES][NK];
-  u32x4 v[NV];
+  u32x4 v[NS];
+  __device__ __forceinline__ void load_k(int t, const char* row, int q) {
+#pragma unroll
+    for (int kk = 0; kk < NK; ++kk) k[t][kk] = *reinterpret_cast<const u32x4_a4*>(row + kk * 64 + q * 16);
+  }
+  __device__ __forceinline__ void load_v(int i, const char* row, int c) {
+    v[i] = *reinterpret_cast<const u32x4_a4*>(row + c * 16);
+  }
+  __device__ __forceinline__ void put_v(int i, char* row, int c) const { *reinterpret_cast<u32x4*>(row + c * 16) = v[i]; }
+  __device__ __forceinline__ void keep_v(int i, bool ok) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[i][e] = ok ? v[i][e] : 0u;
+  }
+  // whether a value is not finite; such values as zero
+  __device__ __forceinline__ bool odd() const {
+    bool y = false;
+#pragma unroll
+    for (int i = 0; i < NS; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y |= (v[i][e] & 0x7f80u) == 0x7f80u || (v[i][e] & 0x7f800000u) == 0x7f800000u;
+    return y;
+  }
+  __device__ __forceinline__ void without_odd() {
+#pragma unroll
+    for (int i = 0; i < NS; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if ((v[i][e] & 0x7f80u) == 0x7f80u) v[i][e] &= 0xffff0000u;
+        if ((v[i][e] & 0x7f800000u) == 0x7f800000u) v[i][e] &= 0xffffu;
+      }
+  }
 };
 template <int D> struct Regs<float, D> {
-  static constexpr int TILES = 1, NK = D / 16, NV = 4;
+  static constexpr int POS = 16, TILES = 1, NK = D / 16, NS = 4;
   static constexpr int VW = D / 16;  // floats of a position
+  typedef f32x4 Word;
   f32x4 k[TILES][NK];
-  float v[NV][VW];
+  float v[NS][VW];
+  __device__ __forceinline__ void load_k(int t, const char* row, int q) {
+#pragma unroll
+    for (int kk = 0; kk < NK; ++kk) k[t][kk] = *reinterpret_cast<const f32x4_a4*>(row + (q * (D / 4) + kk * 4) * 4);
+  }
+  __device__ __forceinline__ void load_v(int i, const char* row, int c) {
+#pragma unroll
+    for (int j = 0; j < VW; ++j) v[i][j] = reinterpret_cast<const float*>(row)[c * VW + j];
+  }
+  __device__ __forceinline__ void put_v(int i, char* row, int c) const {
+#pragma unroll
+    for (int j = 0; j < VW; ++j) reinterpret_cast<float*>(row)[c * VW + j] = v[i][j];
+  }
+  __device__ __forceinline__ void keep_v(int i, bool ok) {
+#pragma unroll
+    for (int j = 0; j < VW; ++j) v[i][j] = ok ? v[i][j] : 0.0f;
+  }
+  __device__ __forceinline__ bool odd() const {
+    bool y = false;
+#pragma unroll
+    for (int i = 0; i < NS; ++i)
+#pragma unroll
+      for (int j = 0; j < VW; ++j) y |= !(fabsf(v[i][j]) < INFINITY);
+    return y;
+  }
+  __device__ __forceinline__ void without_odd() {
+#pragma unroll
+    for (int i = 0; i < NS; ++i)
+#pragma unroll
+      for (int j = 0; j < VW; ++j) v[i][j] = fabsf(v[i][j]) < INFINITY ? v[i][j] : 0.0f;
+  }
 };
 
-// A part of an item: its unit range of a wave, and the columns.
+// Position of a lane's i-th score within its unit.
+__device__ __forceinline__ int at_of(int i, int q) { return (i / 4) * 16 + 4 * q + i % 4; }
+
+// A part of an item: its first column and their number, the units of a wave.
+struct Span {
+  int entity, tile, cols, first, upto, kvh;
+};
+
+// NT tiles of 16 columns in a wave's registers.
 template <typename T, int D, int NT>
-struct Part {
+struct Columns {
   using R = Regs<T, D>;
-  static constexpr int POS = Unit<T>::POS, TILES = R::TILES, NS = 4 * TILES, JN = D / 16;
-  f32x4 o[NT][JN];        // [j][r]: dim q d/4 + r d/16 + j of column c
-  float top[NT], l[NT];   // what weights are relative to; the lane's own weights' sum
-};
+  static constexpr int POS = R::POS, TILES = R::TILES, NS = R::NS, JN = D / 16;
+  typename R::Word q[NT][R::NK];
+  int limit[NT];         // positions that column c sees
+  int all;               // that every column does
+  f32x4 o[NT][JN];       // [j][r]: dim q d/4 + r d/16 + j of column c
+  float top[NT], l[NT];  // what weights are relative to; the lane's own weights' sum
 
-// The arena slots of a stretch of positions, 64 blocks' table entries in a wave's lanes.
-struct Table {
-  const int32_t* entries;
-  int max_blocks;
-  int first;   // block of lane 0's entry
-  int mine;
-  __device__ __forceinline__ void load(int block, int lane) {
-    first = block;
-    mine = (uint32_t)(block + lane) < (uint32_t)max_blocks ? entries[block + lane] : -1;
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      top[nt] = -INFINITY;
+      l[nt] = 0.0f;
+#pragma unroll
+      for (int j = 0; j < JN; ++j) o[nt][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
   }
-};
 
-template <typename T, int D, int NT>
-__device__ void attend_part(const GroupAttnParams& p, const Groups& groups, const Shape& s, int entity, int tile,
-                            int cols_tile, int first, int upto, int kvh, Part<T, D, NT>& x) {
-  using R = Regs<T, D>;
-  constexpr int POS = Unit<T>::POS, TILES = R::TILES, NS = 4 * TILES, JN = D / 16;
-  const int lane = threadIdx.x & 63, c = lane & 15, q = lane >> 4;
-  const float scale_log2 = 1.4426950408889634f / sqrtf((float)D);
+  // Queries and limits of columns x.tile + skip ..
+  __device__ __forceinline__ void load(const GroupAttnParams& p, const Groups& groups, const Shape& s, const Span& x,
+                                       int skip) {
+    const int lane = threadIdx.x & 63, c = lane & 15, qq = lane >> 4;
+    all = s.hi;
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    x.top[nt] = -INFINITY;
-    x.l[nt] = 0.0f;
-#pragma unroll
-    for (int j = 0; j < JN; ++j) x.o[nt][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  }
-  if (first >= upto) return;
-  // ---- queries, and the positions that each column sees ----
-  typename std::conditional<sizeof(T) == 2, u32x4, f32x4>::type qr[NT][R::NK];
-  int limit[NT], all = s.hi, some = 0;
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    const int cc = tile + nt * 16 + c, i = by_g(p, min(cc, s.cols - 1));
-    const bool there = nt * 16 + c < cols_tile;
-    const char* src = p.q + (int64_t)(s.row + i) * p.q_stride + (int64_t)(kvh * p.g + min(cc, s.cols - 1) - i * p.g) * D * sizeof(T);
-#pragma unroll
-    for (int kk = 0; kk < R::NK; ++kk) {
-      if constexpr (sizeof(T) == 2) {
-        qr[nt][kk] = there ? (u32x4)*reinterpret_cast<const u32x4_a4*>(src + kk * 64 + q * 16) : u32x4{0, 0, 0, 0};
-      } else {
-        qr[nt][kk] = there ? (f32x4)*reinterpret_cast<const f32x4_a4*>(src + (q * (D / 4) + kk * 4) * 4)
-                           : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-      }
-    }
-    int lim;
-    if (entity < p.G) {
-      lim = limit_in_group(p, groups, entity, s.row + i);
-    } else {
-      const Rows y = rows_of(p, s.table);
-      lim = max(p.lens[s.table], 0) - y.all + i + 1;
-    }
-    limit[nt] = clamp_to(lim, 0, s.hi);
-    all = there ? min(all, limit[nt]) : all;
-    some = there ? max(some, limit[nt]) : some;
-  }
-#pragma unroll
-  for (int o = 1; o < 16; o *= 2) {
-    all = min(all, __shfl_xor(all, o, 64));
-    some = max(some, __shfl_xor(some, o, 64));
-  }
-  all = __builtin_amdgcn_readfirstlane(all);
-  some = __builtin_amdgcn_readfirstlane(some);
-  upto = min(upto, (int)(((int64_t)max(some - s.lo, 0) + POS - 1) / POS));
-  if (first >= upto) return;
-
-  // ---- addresses ----
-  const int B = p.block_size;
-  const int pos0 = s.lo + first * POS;
-  int blk = pos0 / B, off = pos0 - blk * B;  // of the unit to be loaded next
-  Table table{p.tables + (int64_t)s.table * p.max_blocks, p.max_blocks, 0, 0};
-  table.load(blk, lane);
-  const char* head_k = p.plane_k + (int64_t)kvh * D * sizeof(T);
-  const char* head_v = p.plane_v + (int64_t)kvh * D * sizeof(T);
-  R u;
-  uint32_t valid = 0;  // bit i: position i of the lane's own NS is there
-  bool whole = true;   // every position of the unit is
-  int next = pos0;
-  // the unit's slots: lane x mod POS has position x's, -1: not there
-  const auto slots_of_unit = [&]() {
-    const int at = off + lane % POS;
-    int n;
-    if (p.block_inv) {
-      n = (int)((uint32_t)at * p.block_inv >> 16);
-    } else {
-      n = at >= B ? 1 : 0;
-    }
-    // the unit's last block
-    const int last = p.block_inv ? (int)((uint32_t)(off + POS - 1) * p.block_inv >> 16) : off + POS - 1 >= B ? 1 : 0;
-    if (blk + last - table.first >= 64) table.load(blk, lane);
-    const int entry = __shfl(table.mine, blk + n - table.first, 64);
-    const int slot = (uint32_t)entry < p.num_blocks && (uint32_t)(next + lane % POS) < (uint32_t)some ? entry * B + (at - n * B) : -1;
-    next += POS;
-    off += POS;
-    const int step = p.block_inv ? (int)((uint32_t)off * p.block_inv >> 16) : off >= B ? 1 : 0;
-    blk += step;
-    off -= step * B;
-    return slot;
-  };
-  const auto load_k = [&](int slot) {
-#pragma unroll
-    for (int t = 0; t < TILES; ++t) {
-      const int mine = max(__shfl(slot, t * 16 + c, 64), 0);
-      const char* src = head_k + mine * p.row_bytes;
+    for (int nt = 0; nt < NT; ++nt) {
+      const int in = skip + nt * 16 + c, cc = min(x.tile + in, s.cols - 1), i = by_g(p, cc);
+      const bool there = in < x.cols;
+      const char* src = p.q + (int64_t)(s.row + i) * p.q_stride + (int64_t)(x.kvh * p.g + cc - i * p.g) * D * sizeof(T);
 #pragma unroll
       for (int kk = 0; kk < R::NK; ++kk) {
-        if constexpr (sizeof(T) == 2) u.k[t][kk] = *reinterpret_cast<const u32x4_a4*>(src + kk * 64 + q * 16);
-        else u.k[t][kk] = *reinterpret_cast<const f32x4_a4*>(src + (q * (D / 4) + kk * 4) * 4);
+        if constexpr (sizeof(T) == 2)
+          q[nt][kk] = there ? (u32x4)*reinterpret_cast<const u32x4_a4*>(src + kk * 64 + qq * 16) : u32x4{0, 0, 0, 0};
+        else
+          q[nt][kk] = there ? (f32x4)*reinterpret_cast<const f32x4_a4*>(src + (qq * (D / 4) + kk * 4) * 4)
+                            : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
       }
-    }
-  };
-  const auto load_v = [&](int slot) {
-    valid = 0;
-#pragma unroll
-    for (int i = 0; i < NS; ++i) {
-      const int mine = __shfl(slot, (i / 4) * 16 + 4 * q + i % 4, 64);
-      valid |= (mine >= 0 ? 1u : 0u) << i;
-      const char* src = head_v + max(mine, 0) * p.row_bytes;
-      if constexpr (sizeof(T) == 2) {
-        u.v[i] = *reinterpret_cast<const u32x4_a4*>(src + c * 16);
+      int lim;
+      if (x.entity < p.G) {
+        lim = limit_in_group(p, groups, x.entity, s.row + i);
       } else {
-#pragma unroll
-        for (int j = 0; j < R::VW; ++j) u.v[i][j] = reinterpret_cast<const float*>(src)[c * R::VW + j];
+        const Rows y = rows_of(p, s.table);
+        lim = max(p.lens[s.table], 0) - y.all + i + 1;
       }
+      limit[nt] = clamp_to(lim, 0, s.hi);
+      all = there ? min(all, limit[nt]) : all;
     }
-    whole = __all(valid == (1u << NS) - 1);
-  };
-  int slot = slots_of_unit();
-  load_k(slot);
-  load_v(slot);
-#pragma unroll 1
-  for (int unit = first; unit < upto; ++unit) {
-    const int pos = s.lo + unit * POS;
-    const bool more = unit + 1 < upto;
-    const bool edge = !whole || (uint32_t)(pos + POS) > (uint32_t)all;
-    // ---- scores ----
-    f32x4 sc[NT][TILES];
+#pragma unroll
+    for (int o = 1; o < 16; o *= 2) all = min(all, __shfl_xor(all, o, 64));
+    all = __builtin_amdgcn_readfirstlane(all);
+  }
+
+  __device__ __forceinline__ void scores(const R& u, f32x4 (&sc)[NT][TILES]) const {
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -421,140 +404,99 @@ __device__ void attend_part(const GroupAttnParams& p, const Groups& groups, cons
 #pragma unroll
           for (int kk = 0; kk < R::NK; ++kk)
             a = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u.k[t][kk]),
-                                                        __builtin_bit_cast(bf16x8, qr[nt][kk]), a, 0, 0, 0);
+                                                        __builtin_bit_cast(bf16x8, q[nt][kk]), a, 0, 0, 0);
         } else {
 #pragma unroll
           for (int kk = 0; kk < R::NK; ++kk)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) a = __builtin_amdgcn_mfma_f32_16x16x4f32(u.k[t][kk][e], qr[nt][kk][e], a, 0, 0, 0);
+            for (int e = 0; e < 4; ++e) a = __builtin_amdgcn_mfma_f32_16x16x4f32(u.k[t][kk][e], q[nt][kk][e], a, 0, 0, 0);
         }
         sc[nt][t] = a;
       }
-    if (more) {
-      slot = slots_of_unit();
-      load_k(slot);
-    }
-    uint32_t seen[NT];
-    if (edge) {
+  }
+
+  // Scores of positions from `pos` on that are not there (`there`: a bit each), or that a column
+  // does not see.
+  __device__ __forceinline__ void mask(f32x4 (&sc)[NT][TILES], int pos, uint32_t there) const {
+    const int qq = (threadIdx.x & 63) >> 4;
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        seen[nt] = 0;
+    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int i = 0; i < NS; ++i) {
-          const bool ok = (valid >> i & 1) && (uint32_t)(pos + (i / 4) * 16 + 4 * q + i % 4) < (uint32_t)limit[nt];
-          seen[nt] |= (ok ? 1u : 0u) << i;
-          sc[nt][i / 4][i % 4] = ok ? sc[nt][i / 4][i % 4] : -INFINITY;
-        }
-      }
-    }
-    // ---- weights ----
-    float w[NT][NS];
+      for (int i = 0; i < NS; ++i)
+        if (!(there >> at_of(i, qq) & 1) || (uint32_t)(pos + at_of(i, qq)) >= (uint32_t)limit[nt])
+          sc[nt][i / 4][i % 4] = -INFINITY;
+  }
+
+  // Scores become weights.
+  __device__ __forceinline__ void weigh(f32x4 (&sc)[NT][TILES]) {
+    const float scale_log2 = 1.4426950408889634f / sqrtf((float)D);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       float most = sc[nt][0][0];
 #pragma unroll
       for (int i = 1; i < NS; ++i) most = fmaxf(most, sc[nt][i / 4][i % 4]);
-      most = max_over_q(most) * scale_log2;
       constexpr float lift = sizeof(T) == 2 ? LIFT : 0.0f;
-      const float rise = most + lift;
-      if (__any(rise > x.top[nt] + SLACK)) {
-        const float now = rise > x.top[nt] + SLACK ? rise : x.top[nt];
-        const float f = x.top[nt] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(x.top[nt] - now);
-        const float keep = now == x.top[nt] ? 1.0f : f;
-        x.top[nt] = now;
-        x.l[nt] *= keep;
+      const float rise = max_over_q(most) * scale_log2 + lift;
+      if (__any(rise > top[nt] + SLACK)) {
+        const float now = rise > top[nt] + SLACK ? rise : top[nt];
+        const float f = now == top[nt] ? 1.0f : __builtin_amdgcn_exp2f(top[nt] - now);
+        top[nt] = now;
+        l[nt] *= f;
 #pragma unroll
-        for (int j = 0; j < JN; ++j) x.o[nt][j] *= keep;
+        for (int j = 0; j < JN; ++j) o[nt][j] *= f;
       }
-      const float base = x.top[nt] == -INFINITY ? 0.0f : x.top[nt];
+      const float base = top[nt] == -INFINITY ? 0.0f : top[nt];
 #pragma unroll
       for (int i = 0; i < NS; ++i) {
         float e = __builtin_amdgcn_exp2f(fmaf(sc[nt][i / 4][i % 4], scale_log2, -base));
         if constexpr (sizeof(T) == 4) e *= 0x1p-40f;
-        w[nt][i] = e;
-        x.l[nt] += e;
+        sc[nt][i / 4][i % 4] = e;
+        l[nt] += e;
       }
     }
-    // ---- sums of values ----
-    if (edge) {
-      // what no column sees becomes zero, whatever lies there; values that are not finite at
-      // positions that only some columns see are taken out and counted for those that do
-      bool odd = false;
+  }
+
+  // Values at positions that are not there become zero, whatever they are.  Values that are not
+  // finite, at positions that only some columns see: NaN in those, and taken out.  rows: LDS for
+  // the unit's values, or where they lie.
+  __device__ __forceinline__ void mask_values(R& u, int pos, uint32_t there, char* rows, bool in_rows) {
+    const int lane = threadIdx.x & 63, c = lane & 15, qq = lane >> 4;
 #pragma unroll
-      for (int i = 0; i < NS; ++i) {
-        const bool ok = valid >> i & 1;
-        if constexpr (sizeof(T) == 2) {
+    for (int i = 0; i < NS; ++i) u.keep_v(i, there >> at_of(i, qq) & 1);
+    if (!__any(u.odd())) return;
+    constexpr int BYTES = D * sizeof(T);
+    if (!in_rows) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const uint32_t y = ok ? u.v[i][e] : 0u;
-            u.v[i][e] = y;
-            odd |= (y & 0x7f80u) == 0x7f80u || (y & 0x7f800000u) == 0x7f800000u;
-          }
-        } else {
-#pragma unroll
-          for (int j = 0; j < R::VW; ++j) {
-            const float y = ok ? u.v[i][j] : 0.0f;
-            u.v[i][j] = y;
-            odd |= !(fabsf(y) < INFINITY);
-          }
-        }
-      }
-      if (__any(odd)) {
+      for (int i = 0; i < NS; ++i) u.put_v(i, rows + at_of(i, qq) * BYTES, c);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
 #pragma unroll 1
-        for (int nt = 0; nt < NT; ++nt) {
+    for (int at = 0; at < POS; ++at) {
+      if (!(there >> at & 1)) continue;
+      const T* mine = reinterpret_cast<const T*>(rows + at * BYTES) + qq * (D / 4);
 #pragma unroll
-          for (int j = 0; j < JN; ++j) {
-            f32x4 n = {0.0f, 0.0f, 0.0f, 0.0f};
+      for (int r = 0; r < 4; ++r)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              // products of ones, four positions of a tile at a time
+        for (int j = 0; j < JN; ++j) {
+          const float y = Elem<T>::load(mine, r * JN + j);
+          if (!(fabsf(y) < INFINITY)) {
 #pragma unroll
-              for (int t = 0; t < TILES; ++t) {
-                bool bad;
-                if constexpr (sizeof(T) == 2) {
-                  const uint32_t y = j % 2 ? u.v[t * 4 + i][j / 2] >> 16 : u.v[t * 4 + i][j / 2] & 0xffffu;
-                  bad = (y & 0x7f80u) == 0x7f80u;
-                } else {
-                  bad = !(fabsf(u.v[t * 4 + i][j]) < INFINITY);
-                }
-                uint32_t sn = 0;
-#pragma unroll
-                for (int k = 0; k < NT; ++k) sn = k == nt ? seen[k] : sn;
-                const float b = sn >> (t * 4 + i) & 1 ? 1.0f : 0.0f;
-                n = __builtin_amdgcn_mfma_f32_16x16x4f32(bad ? 1.0f : 0.0f, b, n, 0, 0, 0);
-              }
-            }
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-#pragma unroll
-              for (int k = 0; k < NT; ++k)
-                if (k == nt) x.o[k][j][r] = n[r] > 0.0f ? NAN : x.o[k][j][r];
+            for (int nt = 0; nt < NT; ++nt)
+              if ((uint32_t)(pos + at) < (uint32_t)limit[nt]) o[nt][j][r] = NAN;
           }
         }
-#pragma unroll
-        for (int i = 0; i < NS; ++i) {
-          if constexpr (sizeof(T) == 2) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              uint32_t y = u.v[i][e];
-              if ((y & 0x7f80u) == 0x7f80u) y &= 0xffff0000u;
-              if ((y & 0x7f800000u) == 0x7f800000u) y &= 0xffffu;
-              u.v[i][e] = y;
-            }
-          } else {
-#pragma unroll
-            for (int j = 0; j < R::VW; ++j) u.v[i][j] = fabsf(u.v[i][j]) < INFINITY ? u.v[i][j] : 0.0f;
-          }
-        }
-      }
     }
+    u.without_odd();
+  }
+
+  __device__ __forceinline__ void sums(const R& u, const f32x4 (&w)[NT][TILES]) {
     if constexpr (sizeof(T) == 2) {
       u32x4 hi[NT], lo[NT];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float a = w[nt][2 * i], b = w[nt][2 * i + 1];
+          const float a = w[nt][i / 2][2 * i % 4], b = w[nt][i / 2][2 * i % 4 + 1];
           const uint32_t h = pack_bf16(a, b);
           hi[nt][i] = h;
           lo[nt][i] = pack_bf16(a - __uint_as_float(h << 16), b - __uint_as_float(h & 0xffff0000u));
@@ -567,10 +509,11 @@ __device__ void attend_part(const GroupAttnParams& p, const Groups& groups, cons
           a[i] = __builtin_amdgcn_perm(u.v[2 * i + 1][j / 2], u.v[2 * i][j / 2], j % 2 ? 0x07060302u : 0x05040100u);
         const bf16x8 av = __builtin_bit_cast(bf16x8, a);
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          x.o[nt][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, __builtin_bit_cast(bf16x8, hi[nt]), x.o[nt][j], 0, 0, 0);
-          x.o[nt][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, __builtin_bit_cast(bf16x8, lo[nt]), x.o[nt][j], 0, 0, 0);
-        }
+        for (int nt = 0; nt < NT; ++nt)
+          o[nt][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, __builtin_bit_cast(bf16x8, hi[nt]), o[nt][j], 0, 0, 0);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+          o[nt][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, __builtin_bit_cast(bf16x8, lo[nt]), o[nt][j], 0, 0, 0);
       }
     } else {
 #pragma unroll
@@ -579,11 +522,69 @@ __device__ void attend_part(const GroupAttnParams& p, const Groups& groups, cons
         for (int j = 0; j < JN; ++j)
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
-            x.o[nt][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(u.v[i][j], w[nt][i], x.o[nt][j], 0, 0, 0);
+            o[nt][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(u.v[i][j], w[nt][i / 4][i % 4], o[nt][j], 0, 0, 0);
     }
-    if (more) load_v(slot);
   }
+};
+
+// The arena's slots of positions lo + unit POS .., unit after unit: 64 blocks' table entries in a
+// wave's lanes.
+template <int POS>
+struct Slots {
+  const int32_t* entries;
+  int first, mine;      // block of lane 0's entry; the lane's own
+  int blk, off, next;   // of the next unit's first position
+  int end;
+  __device__ __forceinline__ Slots(const GroupAttnParams& p, const Shape& s, int pos, int end_)
+      : entries(p.tables + (int64_t)s.table * p.max_blocks), blk(pos / p.block_size), off(pos - blk * p.block_size),
+        next(pos), end(end_) {
+    fill(p);
+  }
+  __device__ __forceinline__ void fill(const GroupAttnParams& p) {
+    const int b = blk + (threadIdx.x & 63);
+    first = blk;
+    mine = (uint32_t)b < (uint32_t)p.max_blocks ? entries[b] : -1;
+  }
+  // blocks to the right of `blk` that position off + n of it lies in
+  __device__ __forceinline__ int blocks(const GroupAttnParams& p, int n) const {
+    const uint32_t x = (uint32_t)(off + n);
+    return p.block_inv ? (int)(x * p.block_inv >> 16) : x >= (uint32_t)p.block_size ? 1 : 0;
+  }
+  // The next unit's: lane x has position x mod POS's, any slot where it is not there; bits of
+  // those that are.
+  __device__ __forceinline__ int take(const GroupAttnParams& p, uint32_t& there) {
+    const int x = threadIdx.x & (POS - 1), n = blocks(p, x);
+    if (blk + blocks(p, POS - 1) - first >= 64) fill(p);
+    const int entry = __shfl(mine, blk + n - first, 64);
+    const bool ok = (uint32_t)entry < p.num_blocks && (uint32_t)(next + x) < (uint32_t)end;
+    const int slot = ok ? entry * p.block_size + (off + x - n * p.block_size) : 0;
+    there = (uint32_t)(__ballot(ok) & ((1ull << POS) - 1));
+    const int step = blocks(p, POS);
+    next += POS;
+    blk += step;
+    off += POS - step * p.block_size;
+    return slot;
+  }
+};
+
+constexpr int ring_rows(int d) { return 2 * 32 * d * 2; }  // bytes of a unit's K and V in bf16
+
+// Sums of the waves, a tile of 16 columns at a time; a wave's part is room for a unit's values too.
+template <int D>
+struct Scratch {
+  union {
+    float o[WAVES][16][ROW<D>];
+    char ring[2][ring_rows(D)];  // two units' K and V (bf16)
+  };
+};
+
+// The last position, and one more, that a part's columns see.
+__device__ __forceinline__ int end_of(const GroupAttnParams& p, const Shape& s, const Span& x) {
+  if (x.entity < p.G) return s.hi;
+  const Rows y = rows_of(p, s.table);
+  return clamp_to(max(p.lens[s.table], 0) - y.all + by_g(p, x.tile + x.cols - 1) + 1, 0, s.hi);
 }
+__device__ __forceinline__ int units_to(int n, int pos) { return (int)(((int64_t)max(n, 0) + pos - 1) / pos); }
 
 // An output row's quotient.
 template <int N>
@@ -599,84 +600,224 @@ __device__ __forceinline__ T* out_of(const GroupAttnParams& p, int row, int col,
   return reinterpret_cast<T*>(p.out + (int64_t)(row + i) * p.out_stride) + (int64_t)(kvh * p.g + col - i * p.g) * d + dim;
 }
 
-template <int D>
-struct MergeScratch {
-  float o[WAVES][16][ROW<D>];
-};
-
-// A part of an item of NT tiles of 16 columns: the waves' shares, merged, to `dst` ([column][ROW])
-// or, where that is null, to the output rows.
+// A part of an item of up to 16 NT columns, its units shared out to the waves: their sums,
+// merged, to `dst` ([column][ROW]) or, where that is null, to the output rows.
 template <typename T, int D, int NT>
-__device__ void run_part(const GroupAttnParams& p, const Groups& groups, const Shape& s, int entity, int tile,
-                         int cols_tile, int first, int upto, int kvh, float* dst, MergeScratch<D>& scratch) {
-  constexpr int JN = D / 16;
+__device__ __forceinline__ void run_split(const GroupAttnParams& p, const Groups& groups, const Shape& s, const Span& x,
+                                          float* dst, Scratch<D>& scratch) {
+  using R = Regs<T, D>;
+  constexpr int JN = D / 16, POS = R::POS, TILES = R::TILES, NS = R::NS;
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), c = lane & 15, q = lane >> 4;
-  const int n = upto - first;
-  Part<T, D, NT> x;
-  attend_part<T, D, NT>(p, groups, s, entity, tile, cols_tile, first + (int)((int64_t)n * wave / WAVES),
-                        first + (int)((int64_t)n * (wave + 1) / WAVES), kvh, x);
+  Columns<T, D, NT> cl;
+  cl.clear();
+  const int end = end_of(p, s, x), n = min(x.upto, units_to(end - s.lo, POS)) - x.first;
+  const int first = x.first + (int)((int64_t)max(n, 0) * wave / WAVES);
+  const int upto = x.first + (int)((int64_t)max(n, 0) * (wave + 1) / WAVES);
+  if (first < upto) {
+    cl.load(p, groups, s, x, 0);
+    const char* head_k = p.plane_k + (int64_t)x.kvh * D * sizeof(T);
+    const char* head_v = p.plane_v + (int64_t)x.kvh * D * sizeof(T);
+    Slots<POS> slots(p, s, s.lo + first * POS, end);
+    R u;
+    uint32_t there, coming;
+    int slot = slots.take(p, there);
+    const auto load_k = [&]() {
+#pragma unroll
+      for (int i = 0; i < TILES; ++i) u.load_k(i, head_k + __shfl(slot, i * 16 + c, 64) * p.row_bytes, q);
+    };
+    const auto load_v = [&]() {
+#pragma unroll
+      for (int i = 0; i < NS; ++i) u.load_v(i, head_v + __shfl(slot, at_of(i, q), 64) * p.row_bytes, c);
+    };
+    load_k();
+    load_v();
+#pragma unroll 1
+    for (int unit = first; unit < upto; ++unit) {
+      const int pos = s.lo + unit * POS;
+      const bool more = unit + 1 < upto;
+      const bool edge = there != (uint32_t)((1ull << POS) - 1) || (uint32_t)(pos + POS) > (uint32_t)cl.all;
+      f32x4 w[NT][TILES];
+      cl.scores(u, w);
+      if (more) {
+        slot = slots.take(p, coming);
+        load_k();
+      }
+      if (edge) cl.mask(w, pos, there);
+      cl.weigh(w);
+      if (edge) cl.mask_values(u, pos, there, reinterpret_cast<char*>(scratch.o[wave]), false);
+      cl.sums(u, w);
+      if (more) load_v();
+      there = coming;
+    }
+  }
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
-    if (nt * 16 < cols_tile) {
-      float* mine = scratch.o[wave][c];
-      const float l = sum_over_q(x.l[nt]);
+    if (nt * 16 >= x.cols) break;
+    float* mine = scratch.o[wave][c];
+    const float l = sum_over_q(cl.l[nt]);
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int j = 0; j < JN; ++j) mine[q * (D / 4) + r * JN + j] = cl.o[nt][j][r];
+    if (q == 0) {
+      mine[D] = cl.top[nt];
+      mine[D + 1] = l;
+    }
+    __syncthreads();
+    const int col = t / 16, dim = t % 16 * JN;
+    if (nt * 16 + col < x.cols) {
+      float top = -INFINITY, sum = 0.0f, v[JN];
+#pragma unroll
+      for (int i = 0; i < WAVES; ++i) top = fmaxf(top, scratch.o[i][col][D]);
+      const float base = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+      for (int j = 0; j < JN; ++j) v[j] = 0.0f;
+#pragma unroll
+      for (int i = 0; i < WAVES; ++i) {
+        const float f = __builtin_amdgcn_exp2f(scratch.o[i][col][D] - base);
+        sum = fmaf(scratch.o[i][col][D + 1], f, sum);
+#pragma unroll
+        for (int j = 0; j < JN; ++j) v[j] = fmaf(scratch.o[i][col][dim + j], f, v[j]);
+      }
+      if (dst) {
+        float* to = dst + (int64_t)(nt * 16 + col) * ROW<D>;
+#pragma unroll
+        for (int j = 0; j < JN; ++j) to[dim + j] = v[j];
+        if (dim == 0) {
+          to[D] = top;
+          to[D + 1] = sum;
+        }
+      } else {
+        divide<JN>(v, sum);
+        store_out<T, JN>(out_of<T>(p, s.row, x.tile + nt * 16 + col, x.kvh, D, dim), v);
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// The workgroup's waves meet; what they wrote to LDS is there, loads stay on their way.
+__device__ __forceinline__ void meet() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+  KVR_WAIT_LGKM0();
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("" ::: "memory");
+}
+
+// A part of an item of up to 64 NT columns of a bf16 model, its columns shared out to the waves:
+// units come to them through LDS.  A wave brings eight positions of a unit, in registers
+// while the unit before is worked off.  K's 16-byte words of row r lie at word ^ r mod 16, so that
+// the 16 rows that are read at once lie on different banks; V's rows are read whole.
+template <int D, int NT>
+__device__ __forceinline__ void run_shared(const GroupAttnParams& p, const Groups& groups, const Shape& s, const Span& x,
+                                           float* dst, Scratch<D>& scratch) {
+  using R = Regs<bf16_t, D>;
+  constexpr int JN = D / 16, POS = R::POS, TILES = R::TILES, NS = R::NS, ROWB = D * 2;
+  static_assert(ROWB == 256, "sixteen words a row");
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), c = lane & 15, q = lane >> 4;
+  Columns<bf16_t, D, NT> cl;
+  cl.clear();
+  const int skip = wave * 16 * NT;  // of the part's columns
+  const int end = end_of(p, s, x), upto = min(x.upto, units_to(end - s.lo, POS));
+  if (x.first < upto) {
+    cl.load(p, groups, s, x, skip);
+    const char* head_k = p.plane_k + (int64_t)x.kvh * ROWB;
+    const char* head_v = p.plane_v + (int64_t)x.kvh * ROWB;
+    Slots<POS> slots(p, s, s.lo + x.first * POS, end);
+    u32x4 bring[4];
+    uint32_t there, coming, after = 0;
+    const auto fetch = [&](uint32_t& bits) {
+      const int slot = slots.take(p, bits);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int64_t at = __shfl(slot, wave * 8 + i * 4 + q, 64) * p.row_bytes + c * 16;
+        bring[i] = *reinterpret_cast<const u32x4_a4*>(head_k + at);
+        bring[2 + i] = *reinterpret_cast<const u32x4_a4*>(head_v + at);
+      }
+    };
+    const auto put = [&](char* ring) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int row = wave * 8 + i * 4 + q;
+        *reinterpret_cast<u32x4*>(ring + row * ROWB + ((c ^ (row & 15)) * 16)) = bring[i];
+        *reinterpret_cast<u32x4*>(ring + POS * ROWB + row * ROWB + c * 16) = bring[2 + i];
+      }
+    };
+    fetch(there);
+    put(scratch.ring[0]);
+    if (x.first + 1 < upto) fetch(coming);
+    meet();
+#pragma unroll 1
+    for (int unit = x.first; unit < upto; ++unit) {
+      char* ring = scratch.ring[(unit - x.first) & 1];
+      const int pos = s.lo + unit * POS;
+      const bool edge = there != 0xffffffffu || (uint32_t)(pos + POS) > (uint32_t)cl.all;
+      const bool busy = skip < x.cols;
+      f32x4 w[NT][TILES];
+      R u;
+      if (busy) {
+#pragma unroll
+        for (int i = 0; i < TILES; ++i)
+#pragma unroll
+          for (int kk = 0; kk < R::NK; ++kk)
+            u.k[i][kk] = *reinterpret_cast<const u32x4*>(ring + (i * 16 + c) * ROWB + (((kk * 4 + q) ^ c) * 16));
+        cl.scores(u, w);
+        if (edge) cl.mask(w, pos, there);
+        cl.weigh(w);
+      }
+      // the next unit to the other half, the one after it on its way
+      if (unit + 1 < upto) put(scratch.ring[(unit - x.first + 1) & 1]);
+      if (unit + 2 < upto) fetch(after);
+      if (busy) {
+#pragma unroll
+        for (int i = 0; i < NS; ++i) u.v[i] = *reinterpret_cast<const u32x4*>(ring + POS * ROWB + at_of(i, q) * ROWB + c * 16);
+        if (edge) cl.mask_values(u, pos, there, ring + POS * ROWB, true);
+        cl.sums(u, w);
+      }
+      there = coming;
+      coming = after;
+      meet();
+    }
+  }
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int in = skip + nt * 16 + c;
+    float l = sum_over_q(cl.l[nt]);
+    if (in < x.cols) {
+      float v[D / 4];
 #pragma unroll
       for (int r = 0; r < 4; ++r)
 #pragma unroll
-        for (int j = 0; j < JN; ++j) mine[q * (D / 4) + r * JN + j] = x.o[nt][j][r];
-      if (q == 0) {
-        mine[D] = x.top[nt];
-        mine[D + 1] = l;
-      }
-      __syncthreads();
-      const int col = t / 16, dim = t % 16 * JN;
-      if (nt * 16 + col < cols_tile) {
-        float top = -INFINITY, sum = 0.0f, v[JN];
+        for (int j = 0; j < JN; ++j) v[r * JN + j] = cl.o[nt][j][r];
+      if (dst) {
+        float* to = dst + (int64_t)in * ROW<D>;
 #pragma unroll
-        for (int i = 0; i < WAVES; ++i) top = fmaxf(top, scratch.o[i][col][D]);
-        const float base = top == -INFINITY ? 0.0f : top;
-#pragma unroll
-        for (int j = 0; j < JN; ++j) v[j] = 0.0f;
-#pragma unroll
-        for (int i = 0; i < WAVES; ++i) {
-          const float f = __builtin_amdgcn_exp2f(scratch.o[i][col][D] - base);
-          sum = fmaf(scratch.o[i][col][D + 1], f, sum);
-#pragma unroll
-          for (int j = 0; j < JN; ++j) v[j] = fmaf(scratch.o[i][col][dim + j], f, v[j]);
+        for (int i = 0; i < D / 4; i += 4)
+          *reinterpret_cast<f32x4*>(to + q * (D / 4) + i) = f32x4{v[i], v[i + 1], v[i + 2], v[i + 3]};
+        if (q == 0) {
+          to[D] = cl.top[nt];
+          to[D + 1] = l;
         }
-        if (dst) {
-          float* to = dst + (int64_t)(nt * 16 + col) * ROW<D>;
-#pragma unroll
-          for (int j = 0; j < JN; ++j) to[dim + j] = v[j];
-          if (dim == 0) {
-            to[D] = top;
-            to[D + 1] = sum;
-          }
-        } else {
-          divide<JN>(v, sum);
-          T* to = out_of<T>(p, s.row, tile + nt * 16 + col, kvh, D, dim);
-          if constexpr (sizeof(T) == 2) {
-            store_out<T, JN>(to, v);
-          } else {
-#pragma unroll
-            for (int j = 0; j < JN; ++j) to[j] = v[j];
-          }
-        }
+      } else {
+        divide<D / 4>(v, l);
+        store_out<bf16_t, D / 4>(out_of<bf16_t>(p, s.row, x.tile + in, x.kvh, D, q * (D / 4)), v);
       }
-      __syncthreads();
     }
   }
 }
 
-constexpr int occupancy_of(int nt) { return nt == 4 ? 1 : 2; }
+// Workgroups of a CU by their registers.
+constexpr int occupancy_of(int cols) { return 2; }
 
-template <typename T, int D, int NT>
-__global__ __launch_bounds__(GA_NT, occupancy_of(NT)) void group_attn_kernel(GroupAttnParams p) {
-  constexpr int COLS = 16 * NT, POS = Unit<T>::POS;
+template <typename T, int D, int COLS>
+__global__ __launch_bounds__(GA_NT, occupancy_of(COLS)) void group_attn_kernel(GroupAttnParams p) {
+  constexpr int POS = Regs<T, D>::POS;
   __shared__ int32_t s_groups[KNOWN];
   __shared__ uint32_t s_sum[3][WAVES];
   __shared__ int s_begin[4];  // the stretch's first entity, units, prefixes' and other items before it
-  __shared__ MergeScratch<D> s_merge;
+  __shared__ __attribute__((aligned(16))) Scratch<D> scratch;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
   const int kvh = blockIdx.x % p.nkv, w = blockIdx.x / p.nkv;
   const Groups groups{s_groups};
@@ -732,7 +873,7 @@ __global__ __launch_bounds__(GA_NT, occupancy_of(NT)) void group_attn_kernel(Gro
       const int e = t * per + i;
       if (e < E) {
         const Shape s = shape_of<COLS, POS>(p, groups, e);
-        p.entities[e] = Entity{pre[0], s.item, (int)pre[e < p.G ? 1 : 2], s.row, s.tiles ? s.cols : 0, s.group, {s.lo, 0}};
+        p.entities[e] = Entity{pre[0], s.item, (int)pre[e < p.G ? 1 : 2], s.row, s.tiles ? s.cols : 0, s.group, s.lo, 0};
         pre[0] += s.units();
         pre[e < p.G ? 1 : 2] += s.tiles;
       }
@@ -743,12 +884,12 @@ __global__ __launch_bounds__(GA_NT, occupancy_of(NT)) void group_attn_kernel(Gro
   if (e < 0) return;
   uint32_t base = __builtin_amdgcn_readfirstlane(s_begin[1]);
   int items[2] = {__builtin_amdgcn_readfirstlane(s_begin[2]), __builtin_amdgcn_readfirstlane(s_begin[3])};
-  Shape s = shape_of<COLS, POS>(p, groups, e);
+  Shape s = uniform(shape_of<COLS, POS>(p, groups, e));
   for (uint32_t u = u0; u < u1;) {
     while (u - base >= s.units() && e + 1 < E) {
       base += s.units();
       items[e < p.G ? 0 : 1] += s.tiles;
-      s = shape_of<COLS, POS>(p, groups, ++e);
+      s = uniform(shape_of<COLS, POS>(p, groups, ++e));
     }
     const uint32_t tile = quotient(u - base, s.item);
     if (tile >= (uint32_t)s.tiles) break;  // offsets that overlap so far that the units passed 2^32
@@ -756,7 +897,7 @@ __global__ __launch_bounds__(GA_NT, occupancy_of(NT)) void group_attn_kernel(Gro
     u += to - from;
     const int first = max((int)from - START, 0), upto = (int)to - START;
     if (upto <= 0) continue;  // of the start alone
-    const int kind = e < p.G ? 0 : 1, cols = min(COLS, s.cols - (int)tile * COLS);
+    const int kind = e < p.G ? 0 : 1;
     // a request's item that is all here, with no prefix before it, goes straight out
     float* dst = nullptr;
     if (kind == 0 || s.lo > 0 || from > START || to < s.item) {
@@ -764,17 +905,22 @@ __global__ __launch_bounds__(GA_NT, occupancy_of(NT)) void group_attn_kernel(Gro
       if (slot >= p.slots[kind]) break;  // offsets that overlap: more items than rows make
       dst = p.part[kind] + (kvh * p.slots[kind] + slot) * p.part_cols[kind] * ROW<D>;
     }
-    const int at = (int)tile * COLS;
-    if (NT == 1 || cols <= 16) run_part<T, D, 1>(p, groups, s, e, at, cols, first, upto, kvh, dst, s_merge);
-    else if (NT == 2 || cols <= 32) run_part<T, D, 2>(p, groups, s, e, at, cols, first, upto, kvh, dst, s_merge);
-    else run_part<T, D, NT == 4 ? 4 : 2>(p, groups, s, e, at, cols, first, upto, kvh, dst, s_merge);
+    const Span x{e, (int)tile * COLS, min(COLS, s.cols - (int)tile * COLS), first, upto, kvh};
+    if (COLS == 16 || x.cols <= 16) {
+      run_split<T, D, 1>(p, groups, s, x, dst, scratch);
+    } else if (COLS == 32 || x.cols <= 32) {
+      if constexpr (COLS >= 32) run_split<T, D, 2>(p, groups, s, x, dst, scratch);
+    } else if constexpr (COLS >= 64) {
+      if (COLS == 64 || x.cols <= 64) run_shared<D, 1>(p, groups, s, x, dst, scratch);
+      else if constexpr (COLS == 128) run_shared<D, 2>(p, groups, s, x, dst, scratch);
+    }
   }
 }
 
 // Columns whose sums lie in several places: D / 4 lanes a column.
-template <typename T, int D, int NT>
+template <typename T, int D, int COLS>
 __global__ __launch_bounds__(GA_NT) void group_merge_kernel(GroupAttnParams p) {
-  constexpr int COLS = 16 * NT, LANES = D / 4, AT_ONCE = GA_NT / LANES, CHUNK = 8;
+  constexpr int LANES = D / 4, AT_ONCE = GA_NT / LANES, CHUNK = 8;
   const Stretches st(*p.plan);
   const int64_t all = (int64_t)p.R * p.nkv;
   for (int64_t b = blockIdx.x; b < all; b += gridDim.x) {
@@ -802,7 +948,7 @@ __global__ __launch_bounds__(GA_NT) void group_merge_kernel(GroupAttnParams p) {
         n[k] = z - a + 1;
         src[k] = p.part[k] + ((kvh * p.slots[k] + slot) * p.part_cols[k] + (at[k] - tile * COLS)) * ROW<D>;
       }
-      if (n[1] == 1 && own.pad[0] == 0) continue;  // written by the first kernel
+      if (n[1] == 1 && own.lo == 0) continue;  // written by the first kernel
       float top = -INFINITY, l = 0.0f, o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
       const int total = n[0] + n[1];
       for (int i0 = 0; i0 < total; i0 += CHUNK) {
@@ -846,12 +992,14 @@ struct Sizes {
   int g;
 };
 
-// Column tiles of an item: as many as the average of what shares it fills.
-int tiles_of(const Sizes& z) {
-  const int64_t cols = z.G > 0 ? (z.rows * z.g + z.G - 1) / z.G : z.g * z.max_query;
-  return cols > 32 ? 4 : cols > 16 ? 2 : 1;
+// Columns of an item: the fewest that the average of what shares it fills.  More than 32 go
+// through LDS, which takes bf16 and rows on boundaries of 16 bytes.
+int cols_of(const kv_model_desc& d, const Sizes& z, bool aligned) {
+  const int64_t cols = z.G > 0 ? (z.rows * z.g + z.G - 1) / z.G : z.g * std::min(z.max_query, z.rows);
+  if (d.dtype != KV_BF16 || !aligned) return cols > 16 ? 32 : 16;
+  return cols > 64 ? 128 : cols > 32 ? 64 : cols > 16 ? 32 : 16;
 }
-int most_workers(int nkv, int nt) { return std::max(1, CUS * occupancy_of(nt) / nkv); }
+int most_workers(int nkv, int cols) { return std::max(1, CUS * occupancy_of(cols) / nkv); }
 
 // The workspace: the plan, the entities, the sums of prefixes and those of requests.  Their
 // numbers grow with every size of a call, whichever kernel it takes.
@@ -860,17 +1008,17 @@ struct GroupLayout {
   int part_cols[2];   // for the call's own kernel
   int64_t slots[2];
 };
-GroupLayout layout_of(const kv_model_desc& d, const Sizes& z, int nt) {
-  const int64_t columns = z.rows * z.g, row = d.head_dim + 4, most = most_workers(d.num_kv_heads, 1);
-  const int64_t entity[2] = {z.G, z.R}, widest[2] = {std::min<int64_t>(64, columns), std::min<int64_t>(64, z.g * std::min(z.max_query, z.rows))};
+GroupLayout layout_of(const kv_model_desc& d, const Sizes& z, int cols) {
+  const int64_t columns = z.rows * z.g, row = d.head_dim + 4, most = most_workers(d.num_kv_heads, 16);
+  const int64_t entity[2] = {z.G, z.R}, widest[2] = {std::min<int64_t>(128, columns), std::min<int64_t>(128, z.g * std::min(z.max_query, z.rows))};
   GroupLayout L;
   L.entities = 256;
   L.part[0] = L.entities + (uint64_t)round_up((z.G + z.R) * (int64_t)sizeof(Entity), 256);
   for (int k = 0; k < 2; ++k) {
     const int64_t floats = k == 0 && z.G == 0 ? 0 : d.num_kv_heads * (columns + (entity[k] + most) * widest[k]) * row;
     (k == 0 ? L.part[1] : L.total) = L.part[k] + (uint64_t)round_up(4 * floats, 256);
-    L.part_cols[k] = (int)std::min<int64_t>(16 * nt, widest[k]);
-    L.slots[k] = floats ? columns / (16 * nt) + entity[k] + most_workers(d.num_kv_heads, nt) : 0;
+    L.part_cols[k] = (int)std::min<int64_t>(cols, widest[k]);
+    L.slots[k] = floats ? columns / cols + entity[k] + most_workers(d.num_kv_heads, cols) : 0;
   }
   return L;
 }
@@ -880,17 +1028,20 @@ bool takes(const Sizes& z) {
   return (z.R + z.G + z.rows * z.g / 8) * (z.max_len / 16 + 16) <= INT32_MAX;
 }
 
-template <typename T, int D, int NT>
-void launch_tiles(const GroupAttnParams& p, hipStream_t s) {
-  hipLaunchKernelGGL((group_attn_kernel<T, D, NT>), dim3((unsigned)(p.workers * p.nkv)), dim3(GA_NT), 0, s, p);
+template <typename T, int D, int COLS>
+void launch_cols(const GroupAttnParams& p, hipStream_t s) {
+  hipLaunchKernelGGL((group_attn_kernel<T, D, COLS>), dim3((unsigned)(p.workers * p.nkv)), dim3(GA_NT), 0, s, p);
   const int64_t blocks = std::min<int64_t>((int64_t)p.R * p.nkv, 1 << 20);
-  hipLaunchKernelGGL((group_merge_kernel<T, D, NT>), dim3((unsigned)blocks), dim3(GA_NT), 0, s, p);
+  hipLaunchKernelGGL((group_merge_kernel<T, D, COLS>), dim3((unsigned)blocks), dim3(GA_NT), 0, s, p);
 }
 template <typename T, int D>
-void launch(int nt, const GroupAttnParams& p, hipStream_t s) {
-  if (nt == 1) launch_tiles<T, D, 1>(p, s);
-  else if (nt == 2) launch_tiles<T, D, 2>(p, s);
-  else launch_tiles<T, D, 4>(p, s);
+void launch(int cols, const GroupAttnParams& p, hipStream_t s) {
+  if (cols == 16) launch_cols<T, D, 16>(p, s);
+  else if (cols == 32) launch_cols<T, D, 32>(p, s);
+  else if constexpr (sizeof(T) == 2) {
+    if (cols == 64) launch_cols<T, D, 64>(p, s);
+    else launch_cols<T, D, 128>(p, s);
+  }
 }
 
 bool head_sizes(const kv_model_desc& d) { return d.head_dim % 32 == 0 && d.num_q_heads / d.num_kv_heads <= 16; }
@@ -908,7 +1059,7 @@ uint64_t kv_group_attention_workspace_bytes(const kv_model_desc* desc, int32_t n
   if (num_requests <= 0 || num_requests > MOST_ROWS || rows <= 0 || rows > MOST_ROWS || num_groups < 0 ||
       num_groups > MOST_ROWS || max_query <= 0 || max_len <= 0 || max_len > INT32_MAX)
     return 0;
-  return layout_of(*desc, {num_requests, rows, num_groups, max_query, max_len, desc->num_q_heads / desc->num_kv_heads}, 1)
+  return layout_of(*desc, {num_requests, rows, num_groups, max_query, max_len, desc->num_q_heads / desc->num_kv_heads}, 16)
       .total;
 }
 
@@ -946,8 +1097,8 @@ kv_status kv_group_attention(kv_arena_t arena, int32_t layer, const void* q, int
   const int g = d.num_q_heads / d.num_kv_heads;
   const Sizes z{R, rows, num_groups, max_query, max_len, g};
   if (!takes(z)) return kvr_err::set(KV_EINVAL, "max_len or the work of one call above 2^31: split the query rows");
-  const int nt = tiles_of(z);
-  const GroupLayout L = layout_of(d, z, nt);
+  const int cols = cols_of(d, z, (uintptr_t)arena->base % 16 == 0);
+  const GroupLayout L = layout_of(d, z, cols);
   if (L.total > ws_bytes)
     return kvr_err::set(KV_ENOMEM, "workspace of %llu bytes < %llu needed", (unsigned long long)ws_bytes,
                         (unsigned long long)L.total);
@@ -980,7 +1131,7 @@ kv_status kv_group_attention(kv_arena_t arena, int32_t layer, const void* q, int
   p.g_inv = g == 1 ? 0 : (uint32_t)(((1ull << 32) + g - 1) / g);
   p.max_query = max_query;
   p.most_len = (int)std::min<int64_t>({max_len, (int64_t)max_blocks * arena->block_size, INT32_MAX});
-  p.workers = most_workers(d.num_kv_heads, nt);
+  p.workers = most_workers(d.num_kv_heads, cols);
   char* ws = static_cast<char*>(workspace);
   p.plan = reinterpret_cast<Plan*>(ws);
   p.entities = reinterpret_cast<Entity*>(ws + L.entities);
@@ -990,10 +1141,10 @@ kv_status kv_group_attention(kv_arena_t arena, int32_t layer, const void* q, int
     p.slots[k] = L.slots[k];
   }
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  if (d.dtype == KV_BF16) launch<bf16_t, 128>(nt, p, s);
-  else if (d.head_dim == 128) launch<float, 128>(nt, p, s);
-  else if (d.head_dim == 64) launch<float, 64>(nt, p, s);
-  else launch<float, 32>(nt, p, s);
+  if (d.dtype == KV_BF16) launch<bf16_t, 128>(cols, p, s);
+  else if (d.head_dim == 128) launch<float, 128>(cols, p, s);
+  else if (d.head_dim == 64) launch<float, 64>(cols, p, s);
+  else launch<float, 32>(cols, p, s);
   return launched();
 }
 
