@@ -51,7 +51,7 @@ uint64_t kv_group_attention_workspace_bytes(const kv_model_desc* desc, int32_t n
  *   max_query, max_len  host bounds of a request's query rows and length: its rows and
  *                positions past them are left out (row i stays at lens[r] - m + i).
  *                The workspace and the work of a call are sized by them;
- *                (num_requests + num_groups + rows * nq/nkv / 8) * (max_len / 16 + 16)
+ *                (num_requests + num_groups + rows * nq/nkv / 8) * (max_len / 8 + 16)
  *                below 2^31 always goes
  *   out          device [rows][nq][d], model dtype, rows out_stride elements apart
  *   workspace    device scratch, on a boundary of 16 bytes; calls in flight at once

@@ -41,18 +41,18 @@ namespace {
 constexpr int GA_NT = 256, WAVES = GA_NT / 64;
 constexpr float SLACK = 8.0f, LIFT = 40.0f;  // log2 units
 constexpr int MOST_ROWS = 1 << 24;           // query rows, requests and groups of a call
-constexpr int START = 4;                     // units that an item's start counts as
+constexpr int START = 8;                     // what an item's start costs
 constexpr int CUS = 256;
 constexpr int KNOWN = 512;                   // groups whose offsets are kept in LDS
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef u32x4 u32x4_a4 __attribute__((aligned(4)));
 
-// What the second kernel has to know of an entity: where its items' units begin, what each
-// counts, its first item among its kind, its first query row and its columns, its request's group.
+// What the second kernel has to know of an entity: where its items begin, what each
+// costs, its first item among its kind, its first query row and its columns, its request's group.
 struct Entity {
   uint32_t base, item;
-  int first, row, cols, group, lo, pad;
+  int first, row, cols, group, lo, cost;
 };
 struct Plan {
   uint32_t size, longer, workers, pad[5];
@@ -120,17 +120,25 @@ __device__ __forceinline__ float sum_over_q(float v) {
   return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
-// All units in `workers` stretches, the first `longer` of them a unit longer.
+// What a unit of an item of so many columns costs.
+constexpr int MOST_COST = 4;
+__host__ __device__ constexpr int cost_of(int cols, int most_cols) {
+  return most_cols <= 32 || cols <= 16 ? 2 : cols <= 64 ? 3 : MOST_COST;
+}
+
+// All costs in `workers` stretches, the first `longer` of them one longer.  A unit is the
+// worker's that has the first of its cost; none has less than a unit's, so that of an item that
+// several hold each one between the first and the last holds a unit.
 struct Stretches {
   uint32_t size, longer, workers;
   __device__ __forceinline__ Stretches(uint32_t most, uint32_t total) {
-    workers = min(most, total);
-    size = total ? quotient(total, workers) : 0;
+    workers = max(1u, min(most, total / MOST_COST));
+    size = quotient(total, workers);
     longer = total - size * workers;
   }
   __device__ __forceinline__ explicit Stretches(const Plan& p) : size(p.size), longer(p.longer), workers(p.workers) {}
   __device__ __forceinline__ uint32_t begin(uint32_t w) const { return w * size + min(w, longer); }
-  __device__ __forceinline__ int holder(uint32_t u) const {  // whose unit u is
+  __device__ __forceinline__ int holder(uint32_t u) const {  // whose u is
     const uint32_t head = longer * (size + 1);
     return (int)(u < head ? quotient(u, size + 1) : longer + quotient(u - head, size));
   }
@@ -151,12 +159,15 @@ __device__ __forceinline__ Rows rows_of(const GroupAttnParams& p, int r) {
   return x;
 }
 
-// An entity: columns that see positions lo .. hi - 1 through a table.
+// An entity: columns that see positions lo .. hi - 1 through a table.  Units begin at multiples
+// of their positions, the first with the one that lo lies in.
 struct Shape {
   int row, cols, lo, hi, table, group;
   int tiles;      // of columns; 0: nothing to do
-  uint32_t item;  // what an item counts: its units and its start
-  __device__ __forceinline__ uint32_t units() const { return (uint32_t)tiles * item; }
+  int units;      // of an item
+  int cost;       // of a unit
+  uint32_t item;  // what an item costs: its start and its units
+  __device__ __forceinline__ uint32_t all() const { return (uint32_t)tiles * item; }
 };
 
 // Group offsets, of the first KNOWN groups in LDS.
@@ -181,9 +192,10 @@ struct Groups {
 
 template <int COLS, int POS>
 __device__ __forceinline__ Shape finish_shape(const GroupAttnParams& p, Shape s) {
-  const int n = s.hi - s.lo;
-  s.tiles = n > 0 ? (int)(((int64_t)s.cols + COLS - 1) / COLS) : 0;
-  s.item = (uint32_t)(((int64_t)max(n, 0) + POS - 1) / POS) + START;
+  s.tiles = s.hi > s.lo ? (int)(((int64_t)s.cols + COLS - 1) / COLS) : 0;
+  s.units = s.hi > s.lo ? (s.hi - 1) / POS - s.lo / POS + 1 : 0;
+  s.cost = cost_of(min(s.cols, COLS), COLS);
+  s.item = (uint32_t)(START + s.units * s.cost);
   return s;
 }
 template <int COLS, int POS>
@@ -213,7 +225,7 @@ __device__ __forceinline__ Shape shape_of(const GroupAttnParams& p, const Groups
 // The same in every lane, and known to be.
 __device__ __forceinline__ Shape uniform(Shape s) {
   const auto u = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
-  return Shape{u(s.row), u(s.cols), u(s.lo), u(s.hi), u(s.table), u(s.group), u(s.tiles), (uint32_t)u((int)s.item)};
+  return Shape{u(s.row), u(s.cols), u(s.lo), u(s.hi), u(s.table), u(s.group), u(s.tiles), u(s.units), u(s.cost), (uint32_t)u((int)s.item)};
 }
 
 // Positions that a query row of a prefix's columns sees.
@@ -527,38 +539,47 @@ struct Columns {
   }
 };
 
-// The arena's slots of positions lo + unit POS .., unit after unit: 64 blocks' table entries in a
-// wave's lanes.
+// The arena's slots of positions pos .., unit after unit: 128 blocks' table entries in a wave's
+// lanes, the second 64 on their way while the first are used.
 template <int POS>
 struct Slots {
   const int32_t* entries;
-  int first, mine;      // block of lane 0's entry; the lane's own
-  int blk, off, next;   // of the next unit's first position
-  int end;
-  __device__ __forceinline__ Slots(const GroupAttnParams& p, const Shape& s, int pos, int end_)
+  int first, mine, more;  // block of lane 0's entry; the lane's own, and the one 64 further
+  int blk, off, next;     // of the next unit's first position
+  int lo, hi;
+  __device__ __forceinline__ Slots(const GroupAttnParams& p, const Shape& s, int pos, int end)
       : entries(p.tables + (int64_t)s.table * p.max_blocks), blk(pos / p.block_size), off(pos - blk * p.block_size),
-        next(pos), end(end_) {
-    fill(p);
-  }
-  __device__ __forceinline__ void fill(const GroupAttnParams& p) {
-    const int b = blk + (threadIdx.x & 63);
+        next(pos), lo(s.lo), hi(end) {
     first = blk;
-    mine = (uint32_t)b < (uint32_t)p.max_blocks ? entries[b] : -1;
+    mine = entry(p, first);
+    more = entry(p, first + 64);
+  }
+  __device__ __forceinline__ int entry(const GroupAttnParams& p, int block) const {
+    const uint32_t b = (uint32_t)block + (threadIdx.x & 63);
+    return b < (uint32_t)p.max_blocks ? entries[b] : -1;
   }
   // blocks to the right of `blk` that position off + n of it lies in
   __device__ __forceinline__ int blocks(const GroupAttnParams& p, int n) const {
     const uint32_t x = (uint32_t)(off + n);
     return p.block_inv ? (int)(x * p.block_inv >> 16) : x >= (uint32_t)p.block_size ? 1 : 0;
   }
-  // The next unit's: lane x has position x mod POS's, any slot where it is not there; bits of
-  // those that are.
+  // The next unit's: lane x has position x mod POS's, slot 0 where the table names none; bits of
+  // those positions that are there.
   __device__ __forceinline__ int take(const GroupAttnParams& p, uint32_t& there) {
-    const int x = threadIdx.x & (POS - 1), n = blocks(p, x);
-    if (blk + blocks(p, POS - 1) - first >= 64) fill(p);
-    const int entry = __shfl(mine, blk + n - first, 64);
-    const bool ok = (uint32_t)entry < p.num_blocks && (uint32_t)(next + x) < (uint32_t)end;
-    const int slot = ok ? entry * p.block_size + (off + x - n * p.block_size) : 0;
-    there = (uint32_t)(__ballot(ok) & ((1ull << POS) - 1));
+    if (blk - first >= 64) {
+      first += 64;
+      mine = more;
+      more = entry(p, first + 64);
+    }
+    const int x = threadIdx.x & (POS - 1), n = blocks(p, x), at = blk + n - first;
+    int named = __shfl(mine, at & 63, 64);
+    if (blk + blocks(p, POS - 1) - first >= 64) {
+      const int right = __shfl(more, at & 63, 64);
+      named = at >= 64 ? right : named;
+    }
+    const bool ok = (uint32_t)named < p.num_blocks;
+    const int slot = ok ? named * p.block_size + (off + x - n * p.block_size) : 0;
+    there = (uint32_t)(__ballot(ok && (uint32_t)(next + x) < (uint32_t)hi && next + x >= lo) & ((1ull << POS) - 1));
     const int step = blocks(p, POS);
     next += POS;
     blk += step;
@@ -567,14 +588,14 @@ struct Slots {
   }
 };
 
-constexpr int ring_rows(int d) { return 2 * 32 * d * 2; }  // bytes of a unit's K and V in bf16
-
-// Sums of the waves, a tile of 16 columns at a time; a wave's part is room for a unit's values too.
-template <int D>
+// Sums of the waves, a tile of 16 columns at a time (a wave's part is room for a unit's values
+// too), and units of bf16 K and V on their way and in use.
+constexpr int RING = 4, UNIT_BYTES = 2 * 32 * 256;
+template <int D, bool SHARED>
 struct Scratch {
   union {
     float o[WAVES][16][ROW<D>];
-    char ring[2][ring_rows(D)];  // two units' K and V (bf16)
+    char ring[SHARED ? RING : 1][SHARED ? UNIT_BYTES : 16];
   };
 };
 
@@ -584,7 +605,10 @@ __device__ __forceinline__ int end_of(const GroupAttnParams& p, const Shape& s, 
   const Rows y = rows_of(p, s.table);
   return clamp_to(max(p.lens[s.table], 0) - y.all + by_g(p, x.tile + x.cols - 1) + 1, 0, s.hi);
 }
-__device__ __forceinline__ int units_to(int n, int pos) { return (int)(((int64_t)max(n, 0) + pos - 1) / pos); }
+// Units of an entity up to a position that its columns see.
+__device__ __forceinline__ int units_to(const Shape& s, int end, int pos) {
+  return end > s.lo ? (end - 1) / pos - s.lo / pos + 1 : 0;
+}
 
 // An output row's quotient.
 template <int N>
@@ -602,22 +626,22 @@ __device__ __forceinline__ T* out_of(const GroupAttnParams& p, int row, int col,
 
 // A part of an item of up to 16 NT columns, its units shared out to the waves: their sums,
 // merged, to `dst` ([column][ROW]) or, where that is null, to the output rows.
-template <typename T, int D, int NT>
+template <typename T, int D, int NT, typename S>
 __device__ __forceinline__ void run_split(const GroupAttnParams& p, const Groups& groups, const Shape& s, const Span& x,
-                                          float* dst, Scratch<D>& scratch) {
+                                          float* dst, S& scratch) {
   using R = Regs<T, D>;
   constexpr int JN = D / 16, POS = R::POS, TILES = R::TILES, NS = R::NS;
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), c = lane & 15, q = lane >> 4;
   Columns<T, D, NT> cl;
   cl.clear();
-  const int end = end_of(p, s, x), n = min(x.upto, units_to(end - s.lo, POS)) - x.first;
+  const int end = end_of(p, s, x), n = min(x.upto, units_to(s, end, POS)) - x.first, pos0 = s.lo / POS * POS;
   const int first = x.first + (int)((int64_t)max(n, 0) * wave / WAVES);
   const int upto = x.first + (int)((int64_t)max(n, 0) * (wave + 1) / WAVES);
   if (first < upto) {
     cl.load(p, groups, s, x, 0);
     const char* head_k = p.plane_k + (int64_t)x.kvh * D * sizeof(T);
     const char* head_v = p.plane_v + (int64_t)x.kvh * D * sizeof(T);
-    Slots<POS> slots(p, s, s.lo + first * POS, end);
+    Slots<POS> slots(p, s, pos0 + first * POS, end);
     R u;
     uint32_t there, coming;
     int slot = slots.take(p, there);
@@ -633,7 +657,7 @@ __device__ __forceinline__ void run_split(const GroupAttnParams& p, const Groups
     load_v();
 #pragma unroll 1
     for (int unit = first; unit < upto; ++unit) {
-      const int pos = s.lo + unit * POS;
+      const int pos = pos0 + unit * POS;
       const bool more = unit + 1 < upto;
       const bool edge = there != (uint32_t)((1ull << POS) - 1) || (uint32_t)(pos + POS) > (uint32_t)cl.all;
       f32x4 w[NT][TILES];
@@ -696,90 +720,86 @@ __device__ __forceinline__ void run_split(const GroupAttnParams& p, const Groups
   }
 }
 
-// The workgroup's waves meet; what they wrote to LDS is there, loads stay on their way.
-__device__ __forceinline__ void meet() {
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_sched_barrier(0);
-  KVR_WAIT_LGKM0();
-  __builtin_amdgcn_s_barrier();
-  __builtin_amdgcn_sched_barrier(0);
-  asm volatile("" ::: "memory");
-}
-
 // A part of an item of up to 64 NT columns of a bf16 model, its columns shared out to the waves:
-// units come to them through LDS.  A wave brings eight positions of a unit, in registers
-// while the unit before is worked off.  K's 16-byte words of row r lie at word ^ r mod 16, so that
-// the 16 rows that are read at once lie on different banks; V's rows are read whole.
-template <int D, int NT>
+// units come to them through a ring in LDS, by direct-to-LDS loads; a wave brings eight positions
+// of a unit, four a load, which lie in one block.  K's 16-byte words of row r lie at word ^ r
+// mod 16, so that the 16 rows that are read at once lie on different banks; V's rows are read
+// whole.
+template <int D, int NT, typename S>
 __device__ __forceinline__ void run_shared(const GroupAttnParams& p, const Groups& groups, const Shape& s, const Span& x,
-                                           float* dst, Scratch<D>& scratch) {
+                                           float* dst, S& scratch) {
   using R = Regs<bf16_t, D>;
   constexpr int JN = D / 16, POS = R::POS, TILES = R::TILES, NS = R::NS, ROWB = D * 2;
-  static_assert(ROWB == 256, "sixteen words a row");
+  static_assert(ROWB == 256 && UNIT_BYTES == 2 * POS * ROWB, "sixteen words a row");
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), c = lane & 15, q = lane >> 4;
   Columns<bf16_t, D, NT> cl;
   cl.clear();
   const int skip = wave * 16 * NT;  // of the part's columns
-  const int end = end_of(p, s, x), upto = min(x.upto, units_to(end - s.lo, POS));
+  const int end = end_of(p, s, x), upto = min(x.upto, units_to(s, end, POS)), pos0 = s.lo / POS * POS;
   if (x.first < upto) {
     cl.load(p, groups, s, x, skip);
     const char* head_k = p.plane_k + (int64_t)x.kvh * ROWB;
     const char* head_v = p.plane_v + (int64_t)x.kvh * ROWB;
-    Slots<POS> slots(p, s, s.lo + x.first * POS, end);
-    u32x4 bring[4];
-    uint32_t there, coming, after = 0;
+    Slots<POS> slots(p, s, pos0 + x.first * POS, end);
+    const int bytes = 3 * (int)p.row_bytes + ROWB, row_off = q * (int)p.row_bytes;
+    uint32_t there[RING];  // bits of the units in the ring, oldest first
+    // a unit's loads; past the last the last again, so that waits count the same
+    int fetched = x.first;
     const auto fetch = [&](uint32_t& bits) {
-      const int slot = slots.take(p, bits);
+      if (fetched < upto) {
+        const int slot = slots.take(p, bits);
+        char* ring = scratch.ring[(fetched - x.first) % RING];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int64_t at = __shfl(slot, wave * 8 + i * 4 + q, 64) * p.row_bytes + c * 16;
-        bring[i] = *reinterpret_cast<const u32x4_a4*>(head_k + at);
-        bring[2 + i] = *reinterpret_cast<const u32x4_a4*>(head_v + at);
+        for (int i = 0; i < 2; ++i) {
+          const int row = wave * 8 + i * 4;
+          const int64_t at = (int64_t)__builtin_amdgcn_readlane(slot, row) * p.row_bytes;
+          load_lds(head_k + at, bytes, ring + row * ROWB, row_off + ((c ^ ((row + q) & 15)) * 16), 0);
+          load_lds(head_v + at, bytes, ring + POS * ROWB + row * ROWB, row_off + c * 16, 0);
+        }
       }
+      ++fetched;
     };
-    const auto put = [&](char* ring) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int row = wave * 8 + i * 4 + q;
-        *reinterpret_cast<u32x4*>(ring + row * ROWB + ((c ^ (row & 15)) * 16)) = bring[i];
-        *reinterpret_cast<u32x4*>(ring + POS * ROWB + row * ROWB + c * 16) = bring[2 + i];
-      }
-    };
-    fetch(there);
-    put(scratch.ring[0]);
-    if (x.first + 1 < upto) fetch(coming);
-    meet();
+    for (int i = 0; i < RING - 1; ++i) fetch(there[i]);
 #pragma unroll 1
     for (int unit = x.first; unit < upto; ++unit) {
-      char* ring = scratch.ring[(unit - x.first) & 1];
-      const int pos = s.lo + unit * POS;
-      const bool edge = there != 0xffffffffu || (uint32_t)(pos + POS) > (uint32_t)cl.all;
-      const bool busy = skip < x.cols;
-      f32x4 w[NT][TILES];
-      R u;
-      if (busy) {
+      // this unit's loads have landed, those of the later ones may be on their way
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_sched_barrier(0);
+      if (unit + RING - 1 <= upto) KVR_WAIT_VMCNT(4 * (RING - 2));
+      else KVR_WAIT_VMCNT(0);
+      KVR_WAIT_LGKM0();
+      __builtin_amdgcn_s_barrier();  // ... and the other waves', who are done with the unit before
+      __builtin_amdgcn_sched_barrier(0);
+      asm volatile("" ::: "memory");
+      fetch(there[RING - 1]);
+      char* ring = scratch.ring[(unit - x.first) % RING];
+      const int pos = pos0 + unit * POS;
+      const bool edge = there[0] != 0xffffffffu || (uint32_t)(pos + POS) > (uint32_t)cl.all;
+      if (skip < x.cols) {
+        f32x4 w[NT][TILES];
+        R u;
 #pragma unroll
         for (int i = 0; i < TILES; ++i)
 #pragma unroll
           for (int kk = 0; kk < R::NK; ++kk)
             u.k[i][kk] = *reinterpret_cast<const u32x4*>(ring + (i * 16 + c) * ROWB + (((kk * 4 + q) ^ c) * 16));
         cl.scores(u, w);
-        if (edge) cl.mask(w, pos, there);
+        if (edge) cl.mask(w, pos, there[0]);
         cl.weigh(w);
-      }
-      // the next unit to the other half, the one after it on its way
-      if (unit + 1 < upto) put(scratch.ring[(unit - x.first + 1) & 1]);
-      if (unit + 2 < upto) fetch(after);
-      if (busy) {
 #pragma unroll
         for (int i = 0; i < NS; ++i) u.v[i] = *reinterpret_cast<const u32x4*>(ring + POS * ROWB + at_of(i, q) * ROWB + c * 16);
-        if (edge) cl.mask_values(u, pos, there, ring + POS * ROWB, true);
+        if (edge) cl.mask_values(u, pos, there[0], ring + POS * ROWB, true);
         cl.sums(u, w);
       }
-      there = coming;
-      coming = after;
-      meet();
+#pragma unroll
+      for (int i = 0; i + 1 < RING; ++i) there[i] = there[i + 1];
     }
+    asm volatile("" ::: "memory");
+    KVR_WAIT_VMCNT(0);
+    KVR_WAIT_LGKM0();
+    __builtin_amdgcn_s_barrier();  // the ring is free
+    asm volatile("" ::: "memory");
   }
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
@@ -816,24 +836,27 @@ __global__ __launch_bounds__(GA_NT, occupancy_of(COLS)) void group_attn_kernel(G
   constexpr int POS = Regs<T, D>::POS;
   __shared__ int32_t s_groups[KNOWN];
   __shared__ uint32_t s_sum[3][WAVES];
-  __shared__ int s_begin[4];  // the stretch's first entity, units, prefixes' and other items before it
-  __shared__ __attribute__((aligned(16))) Scratch<D> scratch;
+  __shared__ int s_begin[4];  // the stretch's first entity, costs, prefixes' and other items before it
+  __shared__ __attribute__((aligned(1024))) Scratch<D, (COLS > 32)> scratch;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-  const int kvh = blockIdx.x % p.nkv, w = blockIdx.x / p.nkv;
+  // Workgroups go round the eight chiplets: each takes all kv heads of a stretch, so that its
+  // reads spread over all channels of the memory (a head a chiplet, a slot's rows being 256
+  // bytes of each head: 150 us, not 145, for 64 requests of 2000 - 6000 positions).
+  const int kvh = blockIdx.x / 8 % p.nkv, w = blockIdx.x / (8 * p.nkv) * 8 + blockIdx.x % 8;
   const Groups groups{s_groups};
   if (p.G > 0 && p.G < KNOWN)
     for (int i = t; i <= p.G; i += GA_NT) s_groups[i] = p.group_offsets[i];
   if (t == 0) s_begin[0] = -1;
   __syncthreads();
 
-  // ---- the units and items before each thread's entities ----
+  // ---- the costs and items before each thread's entities ----
   const int E = p.G + p.R, per = (E + GA_NT - 1) / GA_NT;
-  uint32_t mine[3] = {0, 0, 0};  // units, items of prefixes, of requests
+  uint32_t mine[3] = {0, 0, 0};  // costs, items of prefixes, of requests
   for (int i = 0; i < per; ++i) {
     const int e = t * per + i;
     if (e < E) {
       const Shape s = shape_of<COLS, POS>(p, groups, e);
-      mine[0] += s.units();
+      mine[0] += s.all();
       mine[e < p.G ? 1 : 2] += s.tiles;
     }
   }
@@ -873,8 +896,8 @@ __global__ __launch_bounds__(GA_NT, occupancy_of(COLS)) void group_attn_kernel(G
       const int e = t * per + i;
       if (e < E) {
         const Shape s = shape_of<COLS, POS>(p, groups, e);
-        p.entities[e] = Entity{pre[0], s.item, (int)pre[e < p.G ? 1 : 2], s.row, s.tiles ? s.cols : 0, s.group, s.lo, 0};
-        pre[0] += s.units();
+        p.entities[e] = Entity{pre[0], s.item, (int)pre[e < p.G ? 1 : 2], s.row, s.tiles ? s.cols : 0, s.group, s.lo, s.cost};
+        pre[0] += s.all();
         pre[e < p.G ? 1 : 2] += s.tiles;
       }
     }
@@ -886,21 +909,22 @@ __global__ __launch_bounds__(GA_NT, occupancy_of(COLS)) void group_attn_kernel(G
   int items[2] = {__builtin_amdgcn_readfirstlane(s_begin[2]), __builtin_amdgcn_readfirstlane(s_begin[3])};
   Shape s = uniform(shape_of<COLS, POS>(p, groups, e));
   for (uint32_t u = u0; u < u1;) {
-    while (u - base >= s.units() && e + 1 < E) {
-      base += s.units();
+    while (u - base >= s.all() && e + 1 < E) {
+      base += s.all();
       items[e < p.G ? 0 : 1] += s.tiles;
       s = uniform(shape_of<COLS, POS>(p, groups, ++e));
     }
     const uint32_t tile = quotient(u - base, s.item);
-    if (tile >= (uint32_t)s.tiles) break;  // offsets that overlap so far that the units passed 2^32
+    if (tile >= (uint32_t)s.tiles) break;  // offsets that overlap so far that the costs passed 2^32
     const uint32_t from = u - base - tile * s.item, to = min(s.item, from + (u1 - u));
     u += to - from;
-    const int first = max((int)from - START, 0), upto = (int)to - START;
-    if (upto <= 0) continue;  // of the start alone
+    // units whose first is here
+    const int first = (max((int)from - START, 0) + s.cost - 1) / s.cost, upto = (max((int)to - START, 0) + s.cost - 1) / s.cost;
+    if (upto <= first) continue;
     const int kind = e < p.G ? 0 : 1;
     // a request's item that is all here, with no prefix before it, goes straight out
     float* dst = nullptr;
-    if (kind == 0 || s.lo > 0 || from > START || to < s.item) {
+    if (kind == 0 || s.lo > 0 || first > 0 || upto < s.units) {
       const int64_t slot = (int64_t)items[kind] + tile + w;
       if (slot >= p.slots[kind]) break;  // offsets that overlap: more items than rows make
       dst = p.part[kind] + (kvh * p.slots[kind] + slot) * p.part_cols[kind] * ROW<D>;
@@ -908,11 +932,11 @@ __global__ __launch_bounds__(GA_NT, occupancy_of(COLS)) void group_attn_kernel(G
     const Span x{e, (int)tile * COLS, min(COLS, s.cols - (int)tile * COLS), first, upto, kvh};
     if (COLS == 16 || x.cols <= 16) {
       run_split<T, D, 1>(p, groups, s, x, dst, scratch);
-    } else if (COLS == 32 || x.cols <= 32) {
-      if constexpr (COLS >= 32) run_split<T, D, 2>(p, groups, s, x, dst, scratch);
-    } else if constexpr (COLS >= 64) {
+    } else if constexpr (COLS == 32) {
+      run_split<T, D, 2>(p, groups, s, x, dst, scratch);
+    } else if constexpr (COLS > 32) {
       if (COLS == 64 || x.cols <= 64) run_shared<D, 1>(p, groups, s, x, dst, scratch);
-      else if constexpr (COLS == 128) run_shared<D, 2>(p, groups, s, x, dst, scratch);
+      else run_shared<D, COLS / 64>(p, groups, s, x, dst, scratch);
     }
   }
 }
@@ -942,7 +966,7 @@ __global__ __launch_bounds__(GA_NT) void group_merge_kernel(GroupAttnParams p) {
         if (at[k] < 0 || at[k] >= y.cols) continue;
         const int tile = at[k] / COLS;
         const uint32_t begin = y.base + (uint32_t)tile * y.item;
-        const int a = st.holder(begin + START), z = st.holder(begin + y.item - 1);
+        const int a = st.holder(begin + START), z = st.holder(begin + y.item - y.cost);
         const int64_t slot = (int64_t)y.first + tile + a;
         if (slot < 0 || slot + (z - a) >= p.slots[k]) continue;
         n[k] = z - a + 1;
@@ -992,14 +1016,16 @@ struct Sizes {
   int g;
 };
 
-// Columns of an item: the fewest that the average of what shares it fills.  More than 32 go
-// through LDS, which takes bf16 and rows on boundaries of 16 bytes.
-int cols_of(const kv_model_desc& d, const Sizes& z, bool aligned) {
+// Columns of an item: the fewest that the average of what shares it fills.  More than 16 go
+// through LDS in bf16, by loads that take rows on boundaries of 16 bytes, four to a block.
+int cols_of(const kv_model_desc& d, const Sizes& z, bool fours) {
   const int64_t cols = z.G > 0 ? (z.rows * z.g + z.G - 1) / z.G : z.g * std::min(z.max_query, z.rows);
-  if (d.dtype != KV_BF16 || !aligned) return cols > 16 ? 32 : 16;
-  return cols > 64 ? 128 : cols > 32 ? 64 : cols > 16 ? 32 : 16;
+  if (d.dtype == KV_BF16 && !fours) return 16;
+  if (d.dtype != KV_BF16) return cols > 16 && d.head_dim < 128 ? 32 : 16;
+  return cols > 64 ? 128 : cols > 16 ? 64 : 16;
 }
-int most_workers(int nkv, int cols) { return std::max(1, CUS * occupancy_of(cols) / nkv); }
+// Workgroups of a kv head, a multiple of eight.
+int most_workers(int nkv, int cols) { return std::max(8, CUS * occupancy_of(cols) / nkv / 8 * 8); }
 
 // The workspace: the plan, the entities, the sums of prefixes and those of requests.  Their
 // numbers grow with every size of a call, whichever kernel it takes.
@@ -1025,7 +1051,7 @@ GroupLayout layout_of(const kv_model_desc& d, const Sizes& z, int cols) {
 
 bool takes(const Sizes& z) {
   if (z.R > MOST_ROWS || z.rows > MOST_ROWS || z.G > MOST_ROWS || z.max_len > INT32_MAX) return false;
-  return (z.R + z.G + z.rows * z.g / 8) * (z.max_len / 16 + 16) <= INT32_MAX;
+  return (z.R + z.G + z.rows * z.g / 8) * (z.max_len / 8 + 16) <= INT32_MAX;
 }
 
 template <typename T, int D, int COLS>
@@ -1036,11 +1062,13 @@ void launch_cols(const GroupAttnParams& p, hipStream_t s) {
 }
 template <typename T, int D>
 void launch(int cols, const GroupAttnParams& p, hipStream_t s) {
-  if (cols == 16) launch_cols<T, D, 16>(p, s);
-  else if (cols == 32) launch_cols<T, D, 32>(p, s);
-  else if constexpr (sizeof(T) == 2) {
+  if (cols == 16) {
+    launch_cols<T, D, 16>(p, s);
+  } else if constexpr (sizeof(T) == 2) {
     if (cols == 64) launch_cols<T, D, 64>(p, s);
     else launch_cols<T, D, 128>(p, s);
+  } else if constexpr (D < 128) {
+    launch_cols<T, D, 32>(p, s);
   }
 }
 
@@ -1097,7 +1125,7 @@ kv_status kv_group_attention(kv_arena_t arena, int32_t layer, const void* q, int
   const int g = d.num_q_heads / d.num_kv_heads;
   const Sizes z{R, rows, num_groups, max_query, max_len, g};
   if (!takes(z)) return kvr_err::set(KV_EINVAL, "max_len or the work of one call above 2^31: split the query rows");
-  const int cols = cols_of(d, z, (uintptr_t)arena->base % 16 == 0);
+  const int cols = cols_of(d, z, (uintptr_t)arena->base % 16 == 0 && arena->block_size % 4 == 0);
   const GroupLayout L = layout_of(d, z, cols);
   if (L.total > ws_bytes)
     return kvr_err::set(KV_ENOMEM, "workspace of %llu bytes < %llu needed", (unsigned long long)ws_bytes,
