@@ -539,24 +539,34 @@ struct Columns {
   }
 };
 
-// The arena's slots of positions pos .., unit after unit: 128 blocks' table entries in a wave's
-// lanes, the second 64 on their way while the first are used.
+// The arena's slots of positions pos .., unit after unit: a window of 256 blocks' table
+// entries in a wave's lanes.  (They are waited for where they are loaded, which waits for the
+// units on their way too: seldom, with four a lane.)
 template <int POS>
 struct Slots {
+  static constexpr int WIN = 4;
   const int32_t* entries;
-  int first, mine, more;  // block of lane 0's entry; the lane's own, and the one 64 further
-  int blk, off, next;     // of the next unit's first position
+  int first, a, b, c, d;  // block of lane 0's first entry; the lane's own, 64 apart
+  int held;               // of those four
+  int blk, off, next;   // of the next unit's first position
   int lo, hi;
   __device__ __forceinline__ Slots(const GroupAttnParams& p, const Shape& s, int pos, int end)
       : entries(p.tables + (int64_t)s.table * p.max_blocks), blk(pos / p.block_size), off(pos - blk * p.block_size),
         next(pos), lo(s.lo), hi(end) {
-    first = blk;
-    mine = entry(p, first);
-    more = entry(p, first + 64);
+    fill(p);
   }
-  __device__ __forceinline__ int entry(const GroupAttnParams& p, int block) const {
-    const uint32_t b = (uint32_t)block + (threadIdx.x & 63);
-    return b < (uint32_t)p.max_blocks ? entries[b] : -1;
+  __device__ __forceinline__ void fill(const GroupAttnParams& p) {
+    const auto entry = [&](int i) {
+      const uint32_t x = (uint32_t)blk + 64 * i + (threadIdx.x & 63);
+      return x < (uint32_t)p.max_blocks ? entries[x] : -1;
+    };
+    first = blk;
+    held = WIN;
+    a = entry(0);
+    b = entry(1);
+    c = entry(2);
+    d = entry(3);
+    asm volatile("" : "+v"(a), "+v"(b), "+v"(c), "+v"(d));
   }
   // blocks to the right of `blk` that position off + n of it lies in
   __device__ __forceinline__ int blocks(const GroupAttnParams& p, int n) const {
@@ -568,13 +578,17 @@ struct Slots {
   __device__ __forceinline__ int take(const GroupAttnParams& p, uint32_t& there) {
     if (blk - first >= 64) {
       first += 64;
-      mine = more;
-      more = entry(p, first + 64);
+      a = b;
+      b = c;
+      c = d;
+      --held;
     }
+    const int last = blk + blocks(p, POS - 1) - first;
+    if (last >= 64 * held) fill(p);
     const int x = threadIdx.x & (POS - 1), n = blocks(p, x), at = blk + n - first;
-    int named = __shfl(mine, at & 63, 64);
-    if (blk + blocks(p, POS - 1) - first >= 64) {
-      const int right = __shfl(more, at & 63, 64);
+    int named = __shfl(a, at & 63, 64);
+    if (last >= 64) {
+      const int right = __shfl(b, at & 63, 64);
       named = at >= 64 ? right : named;
     }
     const bool ok = (uint32_t)named < p.num_blocks;
@@ -597,6 +611,16 @@ struct Scratch {
     float o[WAVES][16][ROW<D>];
     char ring[SHARED ? RING : 1][SHARED ? UNIT_BYTES : 16];
   };
+};
+
+// All that a workgroup has in LDS, as one object: of several the compiler knows which one the
+// direct loads write, and waits for all of them before every read of it.
+template <int D, bool SHARED>
+struct Shared {
+  Scratch<D, SHARED> scratch;
+  int32_t groups[KNOWN];
+  uint32_t sum[3][WAVES];
+  int begin[4];  // the stretch's first entity, costs, prefixes' and other items before it
 };
 
 // The last position, and one more, that a part's columns see.
@@ -834,10 +858,11 @@ constexpr int occupancy_of(int cols) { return 2; }
 template <typename T, int D, int COLS>
 __global__ __launch_bounds__(GA_NT, occupancy_of(COLS)) void group_attn_kernel(GroupAttnParams p) {
   constexpr int POS = Regs<T, D>::POS;
-  __shared__ int32_t s_groups[KNOWN];
-  __shared__ uint32_t s_sum[3][WAVES];
-  __shared__ int s_begin[4];  // the stretch's first entity, costs, prefixes' and other items before it
-  __shared__ __attribute__((aligned(1024))) Scratch<D, (COLS > 32)> scratch;
+  __shared__ __attribute__((aligned(1024))) Shared<D, (COLS > 32)> shared;
+  auto& scratch = shared.scratch;
+  auto& s_groups = shared.groups;
+  auto& s_sum = shared.sum;
+  auto& s_begin = shared.begin;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
   // Workgroups go round the eight chiplets: each takes all kv heads of a stretch, so that its
   // reads spread over all channels of the memory (a head a chiplet, a slot's rows being 256
