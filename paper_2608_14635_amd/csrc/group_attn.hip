@@ -864,10 +864,7 @@ __global__ __launch_bounds__(GA_NT, occupancy_of(COLS)) void group_attn_kernel(G
   auto& s_sum = shared.sum;
   auto& s_begin = shared.begin;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-  // Workgroups go round the eight chiplets: each takes all kv heads of a stretch, so that its
-  // reads spread over all channels of the memory (a head a chiplet, a slot's rows being 256
-  // bytes of each head: 150 us, not 145, for 64 requests of 2000 - 6000 positions).
-  const int kvh = blockIdx.x / 8 % p.nkv, w = blockIdx.x / (8 * p.nkv) * 8 + blockIdx.x % 8;
+  const int w = blockIdx.x / p.nkv, kvh = (blockIdx.x + (w >= p.workers / 2 ? 1 : 0)) % p.nkv;
   const Groups groups{s_groups};
   if (p.G > 0 && p.G < KNOWN)
     for (int i = t; i <= p.G; i += GA_NT) s_groups[i] = p.group_offsets[i];
