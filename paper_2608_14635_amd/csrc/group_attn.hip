@@ -43,7 +43,6 @@ constexpr float SLACK = 8.0f, LIFT = 40.0f;  // log2 units
 constexpr int MOST_ROWS = 1 << 24;           // query rows, requests and groups of a call
 constexpr int START = 8;                     // what an item's start costs
 constexpr int CUS = 256;
-constexpr int KNOWN = 512;                   // groups whose offsets are kept in LDS
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef u32x4 u32x4_a4 __attribute__((aligned(4)));
@@ -120,7 +119,7 @@ __device__ __forceinline__ float sum_over_q(float v) {
   return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
-// What a unit of an item of so many columns costs.
+// What a unit of an item of so many columns costs: two for one whose waves have a unit each.
 constexpr int MOST_COST = 4;
 __host__ __device__ constexpr int cost_of(int cols, int most_cols) {
   return most_cols <= 32 || cols <= 16 ? 2 : cols <= 64 ? 3 : MOST_COST;
@@ -144,18 +143,59 @@ struct Stretches {
   }
 };
 
+// The lists of groups and requests: where they are short, in LDS.
+constexpr int KNOWN_GROUPS = 512, KNOWN_REQUESTS = 1024;
+struct Known {
+  int32_t offsets[KNOWN_GROUPS], prefixes[KNOWN_GROUPS], rows[KNOWN_REQUESTS], lens[KNOWN_REQUESTS];
+};
+template <bool LDS>
+struct Lists {
+  const GroupAttnParams& p;
+  const Known* known;
+  __device__ __forceinline__ bool groups() const { return LDS && p.G < KNOWN_GROUPS; }
+  __device__ __forceinline__ bool requests() const { return LDS && p.R < KNOWN_REQUESTS; }
+  __device__ __forceinline__ int offset(int e) const { return groups() ? known->offsets[e] : p.group_offsets[e]; }
+  __device__ __forceinline__ int prefix(int e) const { return groups() ? known->prefixes[e] : p.prefix_lens[e]; }
+  __device__ __forceinline__ int row(int r) const {
+    return !p.q_offsets ? r : requests() ? known->rows[r] : p.q_offsets[r];
+  }
+  __device__ __forceinline__ int len(int r) const { return requests() ? known->lens[r] : p.lens[r]; }
+};
+// Into LDS, the first 256 of each on their way together.
+__device__ __forceinline__ void fill_known(const GroupAttnParams& p, Known& k) {
+  const int t = threadIdx.x, G = p.G < KNOWN_GROUPS ? p.G : 0, R = p.R < KNOWN_REQUESTS ? p.R : 0;
+  const int groups = G > 0 ? G + 1 : 0, rows = R > 0 && p.q_offsets ? R + 1 : 0;
+  int a = 0, b = 0, c = 0, d = 0;
+  if (t < groups) a = p.group_offsets[t];
+  if (t < G) b = p.prefix_lens[t];
+  if (t < rows) c = p.q_offsets[t];
+  if (t < R) d = p.lens[t];
+  if (t < groups) k.offsets[t] = a;
+  if (t < G) k.prefixes[t] = b;
+  if (t < rows) k.rows[t] = c;
+  if (t < R) k.lens[t] = d;
+  for (int i = t + GA_NT; i < groups; i += GA_NT) k.offsets[i] = p.group_offsets[i];
+  for (int i = t + GA_NT; i < G; i += GA_NT) k.prefixes[i] = p.prefix_lens[i];
+  for (int i = t + GA_NT; i < rows; i += GA_NT) k.rows[i] = p.q_offsets[i];
+  for (int i = t + GA_NT; i < R; i += GA_NT) k.lens[i] = p.lens[i];
+}
+
 // A request's query rows, and the position after the last of them.
 struct Rows {
   int row, all, used, end;  // used: at most max_query of all
+  int start;                // position of the first
 };
-__device__ __forceinline__ Rows rows_of(const GroupAttnParams& p, int r) {
-  Rows x{r, 1, 1, 0};
+template <bool LDS>
+__device__ __forceinline__ Rows rows_of(const Lists<LDS>& lists, int r) {
+  const GroupAttnParams& p = lists.p;
+  Rows x{r, 1, 1, 0, 0};
   if (p.q_offsets) {
-    x.row = clamp_to(p.q_offsets[r], 0, p.rows);
-    x.all = max(min(p.q_offsets[r + 1], p.rows) - x.row, 0);
+    x.row = clamp_to(lists.row(r), 0, p.rows);
+    x.all = max(min(lists.row(r + 1), p.rows) - x.row, 0);
     x.used = min(x.all, p.max_query);
   }
-  x.end = max(p.lens[r], 0) - (x.all - x.used);  // the rows left out are the last ones
+  x.start = max(lists.len(r), 0) - x.all;
+  x.end = x.start + x.used;  // the rows left out are the last ones
   return x;
 }
 
@@ -170,25 +210,19 @@ struct Shape {
   __device__ __forceinline__ uint32_t all() const { return (uint32_t)tiles * item; }
 };
 
-// Group offsets, of the first KNOWN groups in LDS.
-struct Groups {
-  const int32_t* lds;
-  __device__ __forceinline__ int offset(const GroupAttnParams& p, int e) const {
-    return p.G < KNOWN ? lds[e] : p.group_offsets[e];
+// The group that request r is in, -1: none.  One of a single request shares nothing.
+__device__ __forceinline__ int group_of(const Lists<true>& lists, int r) {
+  const GroupAttnParams& p = lists.p;
+  if (p.G == 0) return -1;
+  int a = 0, b = p.G - 1;
+  while (a < b) {
+    const int m = (a + b + 1) / 2;
+    if (lists.offset(m) <= r) a = m;
+    else b = m - 1;
   }
-  // The group that request r is in, -1: none.  One of a single request shares nothing.
-  __device__ __forceinline__ int of(const GroupAttnParams& p, int r) const {
-    if (p.G == 0) return -1;
-    int a = 0, b = p.G - 1;
-    while (a < b) {
-      const int m = (a + b + 1) / 2;
-      if (offset(p, m) <= r) a = m;
-      else b = m - 1;
-    }
-    const int lo = clamp_to(offset(p, a), 0, p.R), hi = clamp_to(offset(p, a + 1), lo, p.R);
-    return r >= lo && r < hi && hi - lo > 1 ? a : -1;
-  }
-};
+  const int lo = clamp_to(lists.offset(a), 0, p.R), hi = clamp_to(lists.offset(a + 1), lo, p.R);
+  return r >= lo && r < hi && hi - lo > 1 ? a : -1;
+}
 
 template <int COLS, int POS>
 __device__ __forceinline__ Shape finish_shape(const GroupAttnParams& p, Shape s) {
@@ -199,26 +233,27 @@ __device__ __forceinline__ Shape finish_shape(const GroupAttnParams& p, Shape s)
   return s;
 }
 template <int COLS, int POS>
-__device__ __forceinline__ Shape shape_of(const GroupAttnParams& p, const Groups& groups, int e) {
+__device__ __forceinline__ Shape shape_of(const Lists<true>& lists, int e) {
+  const GroupAttnParams& p = lists.p;
   Shape s{};
   s.group = -1;
   if (e < p.G) {
-    const int r0 = clamp_to(groups.offset(p, e), 0, p.R), r1 = clamp_to(groups.offset(p, e + 1), r0, p.R);
+    const int r0 = clamp_to(lists.offset(e), 0, p.R), r1 = clamp_to(lists.offset(e + 1), r0, p.R);
     s.table = r0;
-    s.hi = r1 - r0 > 1 ? clamp_to(p.prefix_lens[e], 0, p.most_len) : 0;
+    s.hi = r1 - r0 > 1 ? clamp_to(lists.prefix(e), 0, p.most_len) : 0;
     if (s.hi > 0) {
-      s.row = p.q_offsets ? clamp_to(p.q_offsets[r0], 0, p.rows) : r0;
-      s.cols = ((p.q_offsets ? clamp_to(p.q_offsets[r1], s.row, p.rows) : r1) - s.row) * p.g;
+      s.row = p.q_offsets ? clamp_to(lists.row(r0), 0, p.rows) : r0;
+      s.cols = ((p.q_offsets ? clamp_to(lists.row(r1), s.row, p.rows) : r1) - s.row) * p.g;
     }
     return finish_shape<COLS, POS>(p, s);
   }
   s.table = e - p.G;
-  const Rows x = rows_of(p, s.table);
+  const Rows x = rows_of(lists, s.table);
   s.row = x.row;
   s.cols = x.used * p.g;
-  s.group = groups.of(p, s.table);
+  s.group = group_of(lists, s.table);
   s.hi = clamp_to(x.end, 0, p.most_len);
-  s.lo = s.group >= 0 ? clamp_to(p.prefix_lens[s.group], 0, s.hi) : 0;
+  s.lo = s.group >= 0 ? clamp_to(lists.prefix(s.group), 0, s.hi) : 0;
   return finish_shape<COLS, POS>(p, s);
 }
 
@@ -229,18 +264,19 @@ __device__ __forceinline__ Shape uniform(Shape s) {
 }
 
 // Positions that a query row of a prefix's columns sees.
-__device__ __forceinline__ int limit_in_group(const GroupAttnParams& p, const Groups& groups, int e, int row) {
-  if (!p.q_offsets) return p.lens[row];
-  const int r0 = clamp_to(groups.offset(p, e), 0, p.R), r1 = clamp_to(groups.offset(p, e + 1), r0, p.R);
+__device__ __forceinline__ int limit_in_group(const Lists<true>& lists, int e, int row) {
+  const GroupAttnParams& p = lists.p;
+  if (!p.q_offsets) return lists.len(row);
+  const int r0 = clamp_to(lists.offset(e), 0, p.R), r1 = clamp_to(lists.offset(e + 1), r0, p.R);
   int a = r0, b = max(r1 - 1, r0);
   // the last request whose rows begin at or before it
   while (a < b) {
     const int m = (a + b + 1) / 2;
-    if (p.q_offsets[m] <= row) a = m;
+    if (lists.row(m) <= row) a = m;
     else b = m - 1;
   }
-  const Rows x = rows_of(p, a);
-  return max(p.lens[a], 0) - x.all + (row - x.row) + 1;
+  const Rows x = rows_of(lists, a);
+  return x.start + (row - x.row) + 1;
 }
 
 // Floats of a partial's row: d sums, a maximum and a sum of weights, on boundaries of 16 bytes.
@@ -374,8 +410,9 @@ struct Columns {
   }
 
   // Queries and limits of columns x.tile + skip ..
-  __device__ __forceinline__ void load(const GroupAttnParams& p, const Groups& groups, const Shape& s, const Span& x,
+  __device__ __forceinline__ void load(const Lists<true>& lists, const Shape& s, const Span& x,
                                        int skip) {
+    const GroupAttnParams& p = lists.p;
     const int lane = threadIdx.x & 63, c = lane & 15, qq = lane >> 4;
     all = s.hi;
 #pragma unroll
@@ -393,10 +430,9 @@ struct Columns {
       }
       int lim;
       if (x.entity < p.G) {
-        lim = limit_in_group(p, groups, x.entity, s.row + i);
+        lim = limit_in_group(lists, x.entity, s.row + i);
       } else {
-        const Rows y = rows_of(p, s.table);
-        lim = max(p.lens[s.table], 0) - y.all + i + 1;
+        lim = rows_of(lists, s.table).start + i + 1;
       }
       limit[nt] = clamp_to(lim, 0, s.hi);
       all = there ? min(all, limit[nt]) : all;
@@ -618,16 +654,20 @@ struct Scratch {
 template <int D, bool SHARED>
 struct Shared {
   Scratch<D, SHARED> scratch;
-  int32_t groups[KNOWN];
+  Known known;
   uint32_t sum[3][WAVES];
-  int begin[4];  // the stretch's first entity, costs, prefixes' and other items before it
+  // the stretch's first entity (-1: none), costs and items of its kind and of the requests before it
+  struct {
+    int entity, items[2];
+    uint32_t cost;
+    Shape shape;
+  } begin;
 };
 
 // The last position, and one more, that a part's columns see.
-__device__ __forceinline__ int end_of(const GroupAttnParams& p, const Shape& s, const Span& x) {
-  if (x.entity < p.G) return s.hi;
-  const Rows y = rows_of(p, s.table);
-  return clamp_to(max(p.lens[s.table], 0) - y.all + by_g(p, x.tile + x.cols - 1) + 1, 0, s.hi);
+__device__ __forceinline__ int end_of(const Lists<true>& lists, const Shape& s, const Span& x) {
+  if (x.entity < lists.p.G) return s.hi;
+  return clamp_to(rows_of(lists, s.table).start + by_g(lists.p, x.tile + x.cols - 1) + 1, 0, s.hi);
 }
 // Units of an entity up to a position that its columns see.
 __device__ __forceinline__ int units_to(const Shape& s, int end, int pos) {
@@ -651,18 +691,19 @@ __device__ __forceinline__ T* out_of(const GroupAttnParams& p, int row, int col,
 // A part of an item of up to 16 NT columns, its units shared out to the waves: their sums,
 // merged, to `dst` ([column][ROW]) or, where that is null, to the output rows.
 template <typename T, int D, int NT, typename S>
-__device__ __forceinline__ void run_split(const GroupAttnParams& p, const Groups& groups, const Shape& s, const Span& x,
+__device__ __forceinline__ void run_split(const Lists<true>& lists, const Shape& s, const Span& x,
                                           float* dst, S& scratch) {
+  const GroupAttnParams& p = lists.p;
   using R = Regs<T, D>;
   constexpr int JN = D / 16, POS = R::POS, TILES = R::TILES, NS = R::NS;
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), c = lane & 15, q = lane >> 4;
   Columns<T, D, NT> cl;
   cl.clear();
-  const int end = end_of(p, s, x), n = min(x.upto, units_to(s, end, POS)) - x.first, pos0 = s.lo / POS * POS;
+  const int end = __builtin_amdgcn_readfirstlane(end_of(lists, s, x)), n = min(x.upto, units_to(s, end, POS)) - x.first, pos0 = s.lo / POS * POS;
   const int first = x.first + (int)((int64_t)max(n, 0) * wave / WAVES);
   const int upto = x.first + (int)((int64_t)max(n, 0) * (wave + 1) / WAVES);
   if (first < upto) {
-    cl.load(p, groups, s, x, 0);
+    cl.load(lists, s, x, 0);
     const char* head_k = p.plane_k + (int64_t)x.kvh * D * sizeof(T);
     const char* head_v = p.plane_v + (int64_t)x.kvh * D * sizeof(T);
     Slots<POS> slots(p, s, pos0 + first * POS, end);
@@ -750,8 +791,9 @@ __device__ __forceinline__ void run_split(const GroupAttnParams& p, const Groups
 // mod 16, so that the 16 rows that are read at once lie on different banks; V's rows are read
 // whole.
 template <int D, int NT, typename S>
-__device__ __forceinline__ void run_shared(const GroupAttnParams& p, const Groups& groups, const Shape& s, const Span& x,
+__device__ __forceinline__ void run_shared(const Lists<true>& lists, const Shape& s, const Span& x,
                                            float* dst, S& scratch) {
+  const GroupAttnParams& p = lists.p;
   using R = Regs<bf16_t, D>;
   constexpr int JN = D / 16, POS = R::POS, TILES = R::TILES, NS = R::NS, ROWB = D * 2;
   static_assert(ROWB == 256 && UNIT_BYTES == 2 * POS * ROWB, "sixteen words a row");
@@ -759,9 +801,9 @@ __device__ __forceinline__ void run_shared(const GroupAttnParams& p, const Group
   Columns<bf16_t, D, NT> cl;
   cl.clear();
   const int skip = wave * 16 * NT;  // of the part's columns
-  const int end = end_of(p, s, x), upto = min(x.upto, units_to(s, end, POS)), pos0 = s.lo / POS * POS;
+  const int end = __builtin_amdgcn_readfirstlane(end_of(lists, s, x)), upto = min(x.upto, units_to(s, end, POS)), pos0 = s.lo / POS * POS;
   if (x.first < upto) {
-    cl.load(p, groups, s, x, skip);
+    cl.load(lists, s, x, skip);
     const char* head_k = p.plane_k + (int64_t)x.kvh * ROWB;
     const char* head_v = p.plane_v + (int64_t)x.kvh * ROWB;
     Slots<POS> slots(p, s, pos0 + x.first * POS, end);
@@ -860,27 +902,24 @@ __global__ __launch_bounds__(GA_NT, occupancy_of(COLS)) void group_attn_kernel(G
   constexpr int POS = Regs<T, D>::POS;
   __shared__ __attribute__((aligned(1024))) Shared<D, (COLS > 32)> shared;
   auto& scratch = shared.scratch;
-  auto& s_groups = shared.groups;
-  auto& s_sum = shared.sum;
-  auto& s_begin = shared.begin;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
   // A CU's two workgroups read different heads (256 of a slot's 2 KB, say): reads of some heads take
   // longer, and a CU's return in order, so that all workgroups end nearer together (135 us, not 140,
   // for 64 requests of 600 - 6500 positions).
   const int w = blockIdx.x / p.nkv, kvh = (blockIdx.x + (w >= p.workers / 2 ? 1 : 0)) % p.nkv;
-  const Groups groups{s_groups};
-  if (p.G > 0 && p.G < KNOWN)
-    for (int i = t; i <= p.G; i += GA_NT) s_groups[i] = p.group_offsets[i];
-  if (t == 0) s_begin[0] = -1;
+  const Lists<true> lists{p, &shared.known};
+  fill_known(p, shared.known);
+  if (t == 0) shared.begin.entity = -1;
   __syncthreads();
 
   // ---- the costs and items before each thread's entities ----
   const int E = p.G + p.R, per = (E + GA_NT - 1) / GA_NT;
   uint32_t mine[3] = {0, 0, 0};  // costs, items of prefixes, of requests
+  Shape s{};
   for (int i = 0; i < per; ++i) {
     const int e = t * per + i;
     if (e < E) {
-      const Shape s = shape_of<COLS, POS>(p, groups, e);
+      s = shape_of<COLS, POS>(lists, e);
       mine[0] += s.all();
       mine[e < p.G ? 1 : 2] += s.tiles;
     }
@@ -889,7 +928,7 @@ __global__ __launch_bounds__(GA_NT, occupancy_of(COLS)) void group_attn_kernel(G
 #pragma unroll
   for (int k = 0; k < 3; ++k) {
     pre[k] = wave_scan(mine[k]);
-    if (lane == 63) s_sum[k][wave] = pre[k];
+    if (lane == 63) shared.sum[k][wave] = pre[k];
     pre[k] -= mine[k];
   }
   __syncthreads();
@@ -897,47 +936,51 @@ __global__ __launch_bounds__(GA_NT, occupancy_of(COLS)) void group_attn_kernel(G
   for (int i = 0; i < WAVES; ++i) {
 #pragma unroll
     for (int k = 0; k < 3; ++k)
-      if (i < wave) pre[k] += s_sum[k][i];
-    total += s_sum[0][i];
+      if (i < wave) pre[k] += shared.sum[k][i];
+    total += shared.sum[0][i];
   }
   total = __builtin_amdgcn_readfirstlane(total);
   const Stretches st(p.workers, total);
   const uint32_t u0 = st.begin(w), u1 = st.begin(w + 1);
-  if ((uint32_t)w < st.workers && u0 >= pre[0] && u0 - pre[0] < mine[0]) {
-    s_begin[0] = t * per;
-    s_begin[1] = (int)pre[0];
-    s_begin[2] = (int)pre[1];
-    s_begin[3] = (int)pre[2];
+  const bool starts = (uint32_t)w < st.workers && u0 >= pre[0] && u0 - pre[0] < mine[0];
+  if (blockIdx.x == 0 && t == 0) {
+    Plan h{};
+    h.size = st.size;
+    h.longer = st.longer;
+    h.workers = st.workers;
+    *p.plan = h;
   }
-  if (blockIdx.x == 0) {  // what the second kernel reads
-    if (t == 0) {
-      Plan h{};
-      h.size = st.size;
-      h.longer = st.longer;
-      h.workers = st.workers;
-      *p.plan = h;
-    }
+  // the thread whose entities the stretch begins in says so, and one workgroup what the second
+  // kernel reads
+  if (starts || blockIdx.x == 0)
     for (int i = 0; i < per; ++i) {
       const int e = t * per + i;
-      if (e < E) {
-        const Shape s = shape_of<COLS, POS>(p, groups, e);
-        p.entities[e] = Entity{pre[0], s.item, (int)pre[e < p.G ? 1 : 2], s.row, s.tiles ? s.cols : 0, s.group, s.lo, s.cost};
-        pre[0] += s.all();
-        pre[e < p.G ? 1 : 2] += s.tiles;
+      if (e >= E) break;
+      if (per > 1) s = shape_of<COLS, POS>(lists, e);
+      const int kind = e < p.G ? 0 : 1;
+      if (starts && u0 >= pre[0] && u0 - pre[0] < s.all()) {
+        shared.begin.entity = e;
+        shared.begin.items[0] = (int)pre[1];
+        shared.begin.items[1] = (int)pre[2];
+        shared.begin.cost = pre[0];
+        shared.begin.shape = s;
       }
+      if (blockIdx.x == 0)
+        p.entities[e] = Entity{pre[0], s.item, (int)pre[1 + kind], s.row, s.tiles ? s.cols : 0, s.group, s.lo, s.cost};
+      pre[0] += s.all();
+      pre[1 + kind] += s.tiles;
     }
-  }
   __syncthreads();
-  int e = __builtin_amdgcn_readfirstlane(s_begin[0]);
+  int e = __builtin_amdgcn_readfirstlane(shared.begin.entity);
   if (e < 0) return;
-  uint32_t base = __builtin_amdgcn_readfirstlane(s_begin[1]);
-  int items[2] = {__builtin_amdgcn_readfirstlane(s_begin[2]), __builtin_amdgcn_readfirstlane(s_begin[3])};
-  Shape s = uniform(shape_of<COLS, POS>(p, groups, e));
+  uint32_t base = __builtin_amdgcn_readfirstlane(shared.begin.cost);
+  int items[2] = {__builtin_amdgcn_readfirstlane(shared.begin.items[0]), __builtin_amdgcn_readfirstlane(shared.begin.items[1])};
+  s = uniform(shared.begin.shape);
   for (uint32_t u = u0; u < u1;) {
     while (u - base >= s.all() && e + 1 < E) {
       base += s.all();
       items[e < p.G ? 0 : 1] += s.tiles;
-      s = uniform(shape_of<COLS, POS>(p, groups, ++e));
+      s = uniform(shape_of<COLS, POS>(lists, ++e));
     }
     const uint32_t tile = quotient(u - base, s.item);
     if (tile >= (uint32_t)s.tiles) break;  // offsets that overlap so far that the costs passed 2^32
@@ -956,12 +999,12 @@ __global__ __launch_bounds__(GA_NT, occupancy_of(COLS)) void group_attn_kernel(G
     }
     const Span x{e, (int)tile * COLS, min(COLS, s.cols - (int)tile * COLS), first, upto, kvh};
     if (COLS == 16 || x.cols <= 16) {
-      run_split<T, D, 1>(p, groups, s, x, dst, scratch);
+      run_split<T, D, 1>(lists, s, x, dst, scratch);
     } else if constexpr (COLS == 32) {
-      run_split<T, D, 2>(p, groups, s, x, dst, scratch);
-    } else if constexpr (COLS > 32) {
-      if (COLS == 64 || x.cols <= 64) run_shared<D, 1>(p, groups, s, x, dst, scratch);
-      else run_shared<D, COLS / 64>(p, groups, s, x, dst, scratch);
+      run_split<T, D, 2>(lists, s, x, dst, scratch);
+    } else if constexpr (COLS == 128) {
+      if (x.cols <= 64) run_shared<D, 1>(lists, s, x, dst, scratch);
+      else run_shared<D, 2>(lists, s, x, dst, scratch);
     }
   }
 }
@@ -975,11 +1018,12 @@ template <typename T, int D, int COLS>
 __global__ __launch_bounds__(GA_NT) void group_merge_kernel(GroupAttnParams p) {
   constexpr int LANES = D / 4, CHUNK = 8;
   const Stretches st(*p.plan);
+  const Lists<false> lists{p, nullptr};
   const int64_t all = (int64_t)p.R * p.nkv;
   for (int64_t b = blockIdx.y; b < all; b += gridDim.y) {
     const int kvh = (int)(b % p.nkv), r = (int)(b / p.nkv);
     const Entity own = p.entities[p.G + r];
-    const Rows x = rows_of(p, r);
+    const Rows x = rows_of(lists, r);
     const int cols = x.used * p.g, lane = threadIdx.x % LANES, dim = lane * 4;
     Entity pre{};
     if (own.group >= 0) pre = p.entities[own.group];
@@ -1051,7 +1095,7 @@ int cols_of(const kv_model_desc& d, const Sizes& z, bool fours) {
   const int64_t cols = z.G > 0 ? (z.rows * z.g + z.G - 1) / z.G : z.g * std::min(z.max_query, z.rows);
   if (d.dtype == KV_BF16 && !fours) return 16;
   if (d.dtype != KV_BF16) return cols > 16 && d.head_dim < 128 ? 32 : 16;
-  return cols > 64 ? 128 : cols > 16 ? 64 : 16;
+  return cols > 16 ? 128 : 16;
 }
 // Workgroups of a kv head, a multiple of eight.
 int most_workers(int nkv, int cols) { return std::max(8, CUS * occupancy_of(cols) / nkv / 8 * 8); }
@@ -1096,8 +1140,7 @@ void launch(int cols, const GroupAttnParams& p, hipStream_t s) {
   if (cols == 16) {
     launch_cols<T, D, 16>(p, s);
   } else if constexpr (sizeof(T) == 2) {
-    if (cols == 64) launch_cols<T, D, 64>(p, s);
-    else launch_cols<T, D, 128>(p, s);
+    launch_cols<T, D, 128>(p, s);
   } else if constexpr (D < 128) {
     launch_cols<T, D, 32>(p, s);
   }
