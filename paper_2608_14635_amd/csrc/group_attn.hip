@@ -703,7 +703,6 @@ __device__ __forceinline__ void run_split(const Lists<true>& lists, const Shape&
   const int first = x.first + (int)((int64_t)max(n, 0) * wave / WAVES);
   const int upto = x.first + (int)((int64_t)max(n, 0) * (wave + 1) / WAVES);
   if (first < upto) {
-    cl.load(lists, s, x, 0);
     const char* head_k = p.plane_k + (int64_t)x.kvh * D * sizeof(T);
     const char* head_v = p.plane_v + (int64_t)x.kvh * D * sizeof(T);
     Slots<POS> slots(p, s, pos0 + first * POS, end);
@@ -720,6 +719,7 @@ __device__ __forceinline__ void run_split(const Lists<true>& lists, const Shape&
     };
     load_k();
     load_v();
+    cl.load(lists, s, x, 0);
 #pragma unroll 1
     for (int unit = first; unit < upto; ++unit) {
       const int pos = pos0 + unit * POS;
@@ -803,7 +803,6 @@ __device__ __forceinline__ void run_shared(const Lists<true>& lists, const Shape
   const int skip = wave * 16 * NT;  // of the part's columns
   const int end = __builtin_amdgcn_readfirstlane(end_of(lists, s, x)), upto = min(x.upto, units_to(s, end, POS)), pos0 = s.lo / POS * POS;
   if (x.first < upto) {
-    cl.load(lists, s, x, skip);
     const char* head_k = p.plane_k + (int64_t)x.kvh * ROWB;
     const char* head_v = p.plane_v + (int64_t)x.kvh * ROWB;
     Slots<POS> slots(p, s, pos0 + x.first * POS, end);
@@ -825,8 +824,10 @@ __device__ __forceinline__ void run_shared(const Lists<true>& lists, const Shape
       }
       ++fetched;
     };
+    fetch(there[0]);
+    cl.load(lists, s, x, skip);
 #pragma unroll
-    for (int i = 0; i < RING - 1; ++i) fetch(there[i]);
+    for (int i = 1; i < RING - 1; ++i) fetch(there[i]);
 #pragma unroll 1
     for (int unit = x.first; unit < upto; ++unit) {
       // this unit's loads have landed, those of the later ones may be on their way
