@@ -7,9 +7,15 @@
 // left of 1 - p_t in a sum with its 1 is noise.  The gradient is one factor of the row times
 // e_v, but for the token's entry.
 //
-// A row is cut into chunks; a workgroup reads its chunk once, into registers, and leaves its
-// largest logit and sum.  A wave merges the chunks of a row in a fixed order, in fp64 as all
-// that is done once a row.  A third kernel turns logits into gradients.
+// Many rows, or short ones: a workgroup a row.  Its threads pass over the row once for their
+// largest logits and sums, join them, and pass over it again for the gradient, backwards: what
+// was read last is in the L2 cache yet, the rest in the last-level one, which holds the rows of
+// all workgroups at once.  A row that fits the threads' registers is read once.
+// Few long rows: a row is cut into chunks; a workgroup reads its chunk once, into registers, and
+// leaves its largest logit and sum.  A wave merges the chunks of a row in a fixed order.  A third
+// kernel turns logits into gradients.
+// What is done once a row is done in fp64, by short series: the library's exp, log, log1p and expm1
+// are some hundred instructions each, which a row's only lane would wait for from memory.
 #include <algorithm>
 
 #include "common.h"
@@ -139,35 +145,96 @@ __device__ __forceinline__ double sum_over_wave(double v) {
   return v;
 }
 
+// e^x - 1: x = n ln 2 + r with |r| <= ln 2 / 2, 2^n (e^r - 1) + (2^n - 1), e^r - 1 by its series
+// to r^13 (the next term is below 2^-57 of r).  `one`: e^x instead.
+__device__ __forceinline__ double exp_less(double x, bool one) {
+  const double n = rint(fmin(fmax(x, -800.0), 800.0) * 1.442695040888963407360);
+  const double r = fma(-n, 1.90821492927058770002e-10, fma(-n, 6.93147180369123816490e-01, x));  // ln 2 in two parts
+  double s = 1.0 / 6227020800.0;
+  s = fma(s, r, 1.0 / 479001600.0);
+  s = fma(s, r, 1.0 / 39916800.0);
+  s = fma(s, r, 1.0 / 3628800.0);
+  s = fma(s, r, 1.0 / 362880.0);
+  s = fma(s, r, 1.0 / 40320.0);
+  s = fma(s, r, 1.0 / 5040.0);
+  s = fma(s, r, 1.0 / 720.0);
+  s = fma(s, r, 1.0 / 120.0);
+  s = fma(s, r, 1.0 / 24.0);
+  s = fma(s, r, 1.0 / 6.0);
+  s = fma(s, r, 0.5);
+  s = fma(s * r, r, r);
+  const int k = (int)n;
+  const double y = ldexp(s, k), z = ldexp(1.0, k);
+  const double v = one ? y + z : y + (z - 1.0);
+  return x > 709.0 ? INFINITY : x < -750.0 ? (one ? 0.0 : -1.0) : x != x ? x : v;
+}
+// log(a / b) for 0.5 <= a / b <= 2: 2 atanh(s), s = (a - b) / (a + b), |s| <= 1/3, by its series
+// to s^33 (the next term is below 2^-57 of s).  less: a - b.
+__device__ __forceinline__ double log_ratio(double less, double sum) {
+  const double s = less / sum, z = s * s;
+  double y = 1.0 / 33.0;
+#pragma unroll
+  for (int i = 31; i >= 3; i -= 2) y = fma(y, z, 1.0 / i);
+  return 2.0 * fma(y * z, s, s);
+}
+// log a, a > 0 and finite.
+__device__ __forceinline__ double log_of(double a) {
+  int k;
+  const double m = frexp(a, &k);  // 0.5 .. 1
+  return fma((double)k, 6.93147180559945309417e-01, log_ratio(m - 1.0, m + 1.0));
+}
+
 // What a chunk's t_v leave out, in log2 units: the rounding of its C.
 __device__ __forceinline__ double c_rounding(const PolicyParams& p, float base) {
   const float cm = c_of(base, p.c);
   return by_c(cm) ? (double)base * p.c - cm : 0.0;
 }
 
-// A row's results from its largest logit m, the others' sum `rest` and the token's logit z;
-// rest is relative to m, in exact units.
-__device__ __forceinline__ void finish_row(const PolicyParams& p, int64_t row, int tok, float m, double rest, float z) {
+// 1 - 2^-x of that, |x| <= 2^-5 (C is below 2^20).
+__device__ __forceinline__ double c_rounding_less(const PolicyParams& p, float base) {
+  return -exp_less(-6.93147180559945309417e-01 * c_rounding(p, base), false);
+}
+
+// A row's inputs besides its logits.
+struct RowIn {
+  int tok;
+  float z, old, ref, advantage, weight;
+};
+template <typename T>
+__device__ __forceinline__ RowIn row_in(const PolicyParams& p, int64_t row, int tok) {
+  RowIn r;
+  r.tok = tok;
+  r.old = p.old ? p.old[row] : 0.0f;
+  r.ref = p.ref ? p.ref[row] : 0.0f;
+  r.advantage = p.advantages[row];
+  r.weight = p.weights ? p.weights[row] : 1.0f;
+  r.z = tok >= 0 && tok < p.vocab ? Elem<T>::load(reinterpret_cast<const T*>(p.logits + row * p.stride), tok) : 0.0f;
+  return r;
+}
+
+// A row's results from its largest logit m and the others' sum `rest`, relative to m.
+__device__ __forceinline__ RowGrad finish_row(const PolicyParams& p, int64_t row, const RowIn& r, float m, double rest) {
   const double scale = p.scale, base = base_of(m);
-  const float w = p.weights ? p.weights[row] : 1.0f;
-  const bool in = tok >= 0 && tok < p.vocab;
+  const float w = r.weight;
+  const bool in = r.tok >= 0 && r.tok < p.vocab;
   double lp = 0.0, kl = 0.0, loss = 0.0, slope = 0.0, not_t = 0.0, all = 1.0;
   bool none = true;
   if (in) {
-    const double x = scale * ((double)z - base), mine = exp(x);
+    const double x = scale * ((double)r.z - base), mine = exp_less(x, true);
     all = rest + mine;
     none = all == 0.0;  // every logit is -infinity
-    lp = none ? -INFINITY : rest < mine ? -log1p(rest / mine) : x - log(all);
+    lp = none ? -INFINITY : rest < mine ? -log_ratio(rest, mine + all) : x - log_of(all);
+    if (all != all) lp = all;
     not_t = none ? 1.0 : rest / all;
   }
   if (in && w != 0.0f) {
-    const double a = p.advantages[row];
-    const double rho = p.old ? exp(lp - p.old[row]) : lp != lp ? lp : 1.0;
+    const double a = r.advantage;
+    const double rho = p.old ? exp_less(lp - r.old, true) : lp != lp ? lp : 1.0;
     const double plain = rho * a, cut = fmin(fmax(rho, p.low), p.high) * a;
     const bool kept = !(plain > cut);
     double fall = 0.0;
     if (p.ref) {
-      const double d = p.ref[row] - lp, e = expm1(d);
+      const double d = r.ref - lp, e = exp_less(d, false);
       kl = e == INFINITY ? e : e - d;
       if (p.kl_coef != 0.0f) fall = p.kl_coef * e;
     }
@@ -178,14 +245,21 @@ __device__ __forceinline__ void finish_row(const PolicyParams& p, int64_t row, i
   if (p.logprobs) p.logprobs[row] = (float)lp;
   if (p.kls) p.kls[row] = (float)kl;
   if (p.total) p.row_loss[row] = loss;
-  if (p.grad) {
-    RowGrad g;
-    g.base = (float)base;
-    g.mul = none ? 0.0f : (float)(-slope / all * exp2(-c_rounding(p, g.base)));
-    g.at_tok = (float)(slope * not_t);
-    g.tok = in && w != 0.0f ? tok : -1;
-    p.row_grad[row] = g;
-  }
+  RowGrad g;
+  g.base = (float)base;
+  g.mul = none ? 0.0f : (float)(-slope / all * (1.0 - c_rounding_less(p, g.base)));
+  g.at_tok = (float)(slope * not_t);
+  g.tok = in && w != 0.0f ? r.tok : -1;
+  return g;
+}
+
+// A sum relative to its largest logit m, relative to `most` and without the rounding of its C.
+// The exponent is taken in fp64, what fp32 leaves of it as a factor.
+__device__ __forceinline__ float joined(const PolicyParams& p, float m, float l, float most) {
+  const double x = ((double)base_of(m) - base_of(most)) * ((double)p.c + p.c_rest) - c_rounding(p, base_of(m));
+  const float hi = (float)x, lo = (float)(x - hi);
+  const float f = __builtin_amdgcn_exp2f(hi);
+  return l == 0.0f || f == 0.0f ? (l != l ? l : 0.0f) : l * fmaf(f, lo * LN2, f);
 }
 
 // A wave a row.
@@ -194,40 +268,42 @@ __global__ __launch_bounds__(PL_NT) void policy_row_kernel(PolicyParams p) {
   const int lane = threadIdx.x & 63;
   const int64_t row = (int64_t)blockIdx.x * (PL_NT / 64) + (threadIdx.x >> 6);
   if (row >= p.rows) return;
-  const int tok = p.tokens[row];
-  const float z = tok >= 0 && tok < p.vocab ? Elem<T>::load(reinterpret_cast<const T*>(p.logits + row * p.stride), tok)
-                                            : 0.0f;
+  const RowIn in = row_in<T>(p, row, p.tokens[row]);
   const float2* stats = p.stats + row * p.chunks;
   float m = -INFINITY;
   for (int i = lane; i < p.chunks; i += 64) m = fmaxf(m, stats[i].x);
   m = max_over_wave(m);
-  double rest = 0.0;
+  float sum = 0.0f;
   for (int i = lane; i < p.chunks; i += 64) {
     const float2 q = stats[i];
-    const double b = base_of(q.x), x = (b - base_of(m)) * ((double)p.c + p.c_rest);
-    rest += q.y == 0.0f ? 0.0 : q.y * exp2(x - c_rounding(p, q.x));
+    sum += joined(p, q.x, q.y, m);
   }
-  rest = sum_over_wave(rest);
-  if (lane == 0) finish_row(p, row, tok, m, rest, z);
+  const double rest = sum_over_wave(sum);
+  if (lane == 0) {
+    const RowGrad g = finish_row(p, row, in, m, rest);
+    if (p.grad) p.row_grad[row] = g;
+  }
 }
 
-// The rows' losses, a workgroup's threads in turn.
+// The rows' losses, the threads of NT in turn.
+template <int NT>
 __device__ __forceinline__ void put_total(const PolicyParams& p) {
-  __shared__ double s_sum[PL_NT / 64];
+  __shared__ double s_sum[NT / 64];
   double v = 0.0;
 #pragma unroll 4
-  for (int64_t i = threadIdx.x; i < p.rows; i += PL_NT) v += p.row_loss[i];
+  for (int64_t i = threadIdx.x; i < p.rows; i += NT) v += p.row_loss[i];
   v = sum_over_wave(v);
   if ((threadIdx.x & 63) == 0) s_sum[threadIdx.x >> 6] = v;
   __syncthreads();
   if (threadIdx.x == 0) {
     v = s_sum[0];
 #pragma unroll
-    for (int i = 1; i < PL_NT / 64; ++i) v += s_sum[i];
+    for (int i = 1; i < NT / 64; ++i) v += s_sum[i];
     *p.total = (float)v;
   }
 }
-__global__ __launch_bounds__(PL_NT) void policy_total_kernel(PolicyParams p) { put_total(p); }
+constexpr int TOTAL_NT = 512;
+__global__ __launch_bounds__(TOTAL_NT) void policy_total_kernel(PolicyParams p) { put_total<TOTAL_NT>(p); }
 
 __device__ __forceinline__ void put_entry(float* p, float v) { *p = v; }
 __device__ __forceinline__ void put_entry(bf16_t* p, float v) { *p = f2bf(v); }
@@ -266,18 +342,173 @@ __global__ __launch_bounds__(PL_NT) void policy_grad_kernel(PolicyParams p) {
         if (at + j < p.vocab) put_entry(out + at + j, y[j]);
     }
   }
-  if (p.total && blockIdx.x == 0) put_total(p);
+  if (p.total && blockIdx.x == 0) put_total<PL_NT>(p);
+}
+
+// Gradients of a piece's entries `at` .. of a row that is not left out; the token's own entry is
+// put afterwards.
+template <typename T>
+__device__ __forceinline__ void put_grad(const PolicyParams& p, const RowGrad& g, float cm, bool by, const Piece<T>& v,
+                                         T* out, int at) {
+  constexpr int VEC = Piece<T>::N;
+  float y[VEC];
+  if (by) {
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) y[j] = g.mul * __builtin_amdgcn_exp2f(fmaf(v.value(j), p.c, -cm));
+  } else {
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) y[j] = g.mul * __builtin_amdgcn_exp2f((v.value(j) - g.base) * p.c);
+  }
+  if (at + VEC <= p.vocab) {
+    Piece<T> w;
+    w.put(y);
+    w.store(out + at);
+  } else {
+#pragma unroll
+    for (int j = 0; j < VEC; ++j)
+      if (at + j < p.vocab) put_entry(out + at + j, y[j]);
+  }
+}
+
+// A workgroup of NT threads a row, U pieces of a thread at a time.  HELD: all of the row's.
+template <typename T, int NT, int U, bool HELD>
+__global__ __launch_bounds__(NT) void policy_whole_kernel(PolicyParams p) {
+  constexpr int VEC = Piece<T>::N, WAVES = NT / 64, STEP = NT * VEC, TURN = U * STEP;
+  __shared__ float s_most[WAVES], s_sum[WAVES];
+  __shared__ RowGrad s_grad;
+  const int t = threadIdx.x;
+  const int64_t row = blockIdx.x;
+  const T* z = reinterpret_cast<const T*>(p.logits + row * p.stride);
+  const int tok = p.tokens[row];
+  const int turns = HELD ? 1 : (p.vocab + TURN - 1) / TURN;
+  Piece<T> v[U];
+  const auto load = [&](int begin) {
+    if (begin + TURN <= p.vocab) {
+#pragma unroll
+      for (int i = 0; i < U; ++i) v[i].load(z + (begin + i * STEP) + (uint32_t)(t * VEC));
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int at = begin + i * STEP + t * VEC;
+      v[i] = Piece<T>{};
+      if (at + VEC <= p.vocab) {
+        v[i].load(z + at);
+      } else {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) v[i].set(j, at + j < p.vocab ? Elem<T>::load(z, at + j) : -INFINITY);
+      }
+    }
+  };
+  RowIn in;
+  if (t == 0) in = row_in<T>(p, row, tok);
+  float m = -INFINITY, l = 0.0f;
+#pragma unroll 1
+  for (int turn = 0; turn < turns; ++turn) {
+    const int begin = turn * TURN;
+    load(begin);
+    float most = m;
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) most = fmaxf(most, v[i].value(j));
+    const float cm = c_of(base_of(most), p.c);
+    if (most > m) {
+      const float was = c_of(base_of(m), p.c);
+      const float x = by_c(cm) && by_c(was) ? was - cm : (m - most) * p.c;
+      l = l == 0.0f ? 0.0f : l * __builtin_amdgcn_exp2f(x);
+      m = most;
+    }
+    const int at = tok - begin;  // the token's entry stays out of the sum
+    if (at >= 0 && at < TURN) {
+#pragma unroll
+      for (int i = 0; i < U; ++i)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j)
+          if (at == i * STEP + t * VEC + j) v[i].set(j, -INFINITY);
+    }
+    if (by_c(cm)) {
+#pragma unroll
+      for (int i = 0; i < U; ++i)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) l += __builtin_amdgcn_exp2f(fmaf(v[i].value(j), p.c, -cm));
+    } else {
+      const float base = base_of(m);
+#pragma unroll
+      for (int i = 0; i < U; ++i)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) l += __builtin_amdgcn_exp2f((v[i].value(j) - base) * p.c);
+    }
+  }
+  // ---- the threads' sums, then the waves' ----
+  const float wave_most = max_over_wave(m);
+  const float wave_sum = sum_over_wave(joined(p, m, l, wave_most));
+  if ((t & 63) == 0) {
+    s_most[t >> 6] = wave_most;
+    s_sum[t >> 6] = wave_sum;
+  }
+  __syncthreads();
+  if (t < 64) {
+    const int i = min(t, WAVES - 1);
+    const float most = max_over_wave(s_most[i]);
+    // a wave's sum has no rounded C in it
+    const double x = ((double)base_of(s_most[i]) - base_of(most)) * ((double)p.c + p.c_rest);
+    double sum = t < WAVES && s_sum[i] != 0.0f ? s_sum[i] * exp_less(x * 6.93147180559945309417e-01, true) : 0.0;
+#pragma unroll
+    for (int o = WAVES / 2; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+    if (t == 0) s_grad = finish_row(p, row, in, most, sum);
+  }
+  if (!p.grad) return;
+  __syncthreads();
+  // ---- the gradient ----
+  const RowGrad g = s_grad;
+  T* out = reinterpret_cast<T*>(p.grad + row * p.grad_stride);
+  if (g.tok < 0) {
+    Piece<T> zero{};
+    for (int at = t * VEC; at < p.vocab; at += STEP) {
+      if (at + VEC <= p.vocab) {
+        zero.store(out + at);
+      } else {
+        for (int j = at; j < p.vocab; ++j) put_entry(out + j, 0.0f);
+      }
+    }
+    return;
+  }
+  const float cm = c_of(g.base, p.c);
+  const bool by = by_c(cm);
+#pragma unroll 1
+  for (int turn = turns - 1; turn >= 0; --turn) {
+    const int begin = turn * TURN;
+    if (!HELD) load(begin);
+#pragma unroll
+    for (int i = 0; i < U; ++i) put_grad(p, g, cm, by, v[i], out, begin + i * STEP + t * VEC);
+  }
+  if (g.tok % STEP / VEC == t) put_entry(out + g.tok, g.at_tok);  // after the thread's own store there
 }
 
 int chunks_of(int vocab) { return (vocab + PL_CHUNK - 1) / PL_CHUNK; }
 
+// Whether a call's rows are taken whole: they fit a workgroup's registers, or there are enough of
+// them.
+constexpr int WHOLE_ROWS = 160;
+template <typename T, int NT, int U, bool HELD>
+void launch_whole(const PolicyParams& p, hipStream_t s) {
+  hipLaunchKernelGGL((policy_whole_kernel<T, NT, U, HELD>), dim3((unsigned)p.rows), dim3(NT), 0, s, p);
+  if (p.total) hipLaunchKernelGGL(policy_total_kernel, dim3(1), dim3(TOTAL_NT), 0, s, p);
+}
 template <typename T>
 void launch(const PolicyParams& p, hipStream_t s) {
+  constexpr int VEC = Piece<T>::N, SMALL = 32 / VEC, U = 8;
+  if (p.vocab <= 256 * 32) return launch_whole<T, 256, SMALL, true>(p, s);
+  if (p.rows >= WHOLE_ROWS) {
+    if (p.vocab <= 1024 * VEC * U) return launch_whole<T, 1024, U, true>(p, s);
+    return launch_whole<T, 1024, U, false>(p, s);
+  }
   const dim3 grid((unsigned)(p.rows * p.chunks)), nt(PL_NT);
   hipLaunchKernelGGL((policy_chunk_kernel<T>), grid, nt, 0, s, p);
   hipLaunchKernelGGL((policy_row_kernel<T>), dim3((unsigned)((p.rows + PL_NT / 64 - 1) / (PL_NT / 64))), nt, 0, s, p);
   if (p.grad) hipLaunchKernelGGL((policy_grad_kernel<T>), grid, nt, 0, s, p);
-  else if (p.total) hipLaunchKernelGGL(policy_total_kernel, dim3(1), nt, 0, s, p);
+  else if (p.total) hipLaunchKernelGGL(policy_total_kernel, dim3(1), dim3(TOTAL_NT), 0, s, p);
 }
 
 }  // namespace
@@ -364,7 +595,7 @@ kv_status kv_policy_loss(const void* logits, int32_t dtype, int64_t rows, int32_
   p.row_loss = reinterpret_cast<double*>(p.row_grad + rows);
   p.stats = reinterpret_cast<float2*>(p.row_loss + rows);
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  if (rows == 0) hipLaunchKernelGGL(policy_total_kernel, dim3(1), dim3(PL_NT), 0, s, p);
+  if (rows == 0) hipLaunchKernelGGL(policy_total_kernel, dim3(1), dim3(TOTAL_NT), 0, s, p);
   else if (dtype == KV_BF16) launch<bf16_t>(p, s);
   else launch<float>(p, s);
   return launched();
