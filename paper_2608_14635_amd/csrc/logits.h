@@ -27,6 +27,10 @@ template <> struct Piece<float> {
   __device__ __forceinline__ float value(int j) const { return w[j]; }
   __device__ __forceinline__ void put(const float* v) { w = f32x4{v[0], v[1], v[2], v[3]}; }
   __device__ __forceinline__ void store(float* p) const { *reinterpret_cast<f32x4_a4*>(p) = w; }
+  // past the caches: nothing reads it soon
+  __device__ __forceinline__ void store_past(float* p) const {
+    __builtin_nontemporal_store(w, reinterpret_cast<f32x4_a4*>(p));
+  }
 };
 template <> struct Piece<bf16_t> {
   static constexpr int N = 8;
@@ -45,6 +49,9 @@ template <> struct Piece<bf16_t> {
       w[j] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)v[2 * j], (__bf16)v[2 * j + 1]});
   }
   __device__ __forceinline__ void store(bf16_t* p) const { *reinterpret_cast<u32x4_a2*>(p) = w; }
+  __device__ __forceinline__ void store_past(bf16_t* p) const {
+    __builtin_nontemporal_store(w, reinterpret_cast<u32x4_a2*>(p));
+  }
 };
 
 // f over the wave's lanes, in every lane: neighbours, pairs, fours and eights of a row of

@@ -7,11 +7,10 @@
 // left of 1 - p_t in a sum with its 1 is noise.  The gradient is one factor of the row times
 // e_v, but for the token's entry.
 //
-// Many rows, or short ones: a workgroup a row.  Its threads pass over the row once for their
-// largest logits and sums, join them, and pass over it again for the gradient, backwards: what
-// was read last is in the L2 cache yet, the rest in the last-level one, which holds the rows of
-// all workgroups at once.  A row that fits the threads' registers is read once.
-// Few long rows: a row is cut into chunks; a workgroup reads its chunk once, into registers, and
+// Many rows, or short ones: a workgroup a row, which it holds in its registers, as much of it as
+// fits: its threads take their largest logits and sums from there, join them, and then the
+// gradients.
+// Few long rows, and losses alone: a row is cut into chunks; a workgroup reads its chunk once, into registers, and
 // leaves its largest logit and sum.  A wave merges the chunks of a row in a fixed order.  A third
 // kernel turns logits into gradients.
 // What is done once a row is done in fp64, by short series: the library's exp, log, log1p and expm1
@@ -145,24 +144,29 @@ __device__ __forceinline__ double sum_over_wave(double v) {
   return v;
 }
 
+// The series' coefficients.  In memory, and read where they are used: as numbers of the code a loop
+// over rows keeps all of them in registers that its pieces need.
+__constant__ double EXP_SERIES[12] = {1.0 / 6227020800.0, 1.0 / 479001600.0, 1.0 / 39916800.0, 1.0 / 3628800.0,
+                                      1.0 / 362880.0,     1.0 / 40320.0,     1.0 / 5040.0,     1.0 / 720.0,
+                                      1.0 / 120.0,        1.0 / 24.0,        1.0 / 6.0,        0.5};
+__constant__ double ATANH_SERIES[16] = {1.0 / 33.0, 1.0 / 31.0, 1.0 / 29.0, 1.0 / 27.0, 1.0 / 25.0, 1.0 / 23.0,
+                                        1.0 / 21.0, 1.0 / 19.0, 1.0 / 17.0, 1.0 / 15.0, 1.0 / 13.0, 1.0 / 11.0,
+                                        1.0 / 9.0,  1.0 / 7.0,  1.0 / 5.0,  1.0 / 3.0};
+template <int N>
+__device__ __forceinline__ double series(const double* c, double x) {
+  asm volatile("" : "+s"(c));
+  double s = c[0];
+#pragma unroll
+  for (int i = 1; i < N; ++i) s = fma(s, x, c[i]);
+  return s;
+}
+
 // e^x - 1: x = n ln 2 + r with |r| <= ln 2 / 2, 2^n (e^r - 1) + (2^n - 1), e^r - 1 by its series
 // to r^13 (the next term is below 2^-57 of r).  `one`: e^x instead.
 __device__ __forceinline__ double exp_less(double x, bool one) {
   const double n = rint(fmin(fmax(x, -800.0), 800.0) * 1.442695040888963407360);
   const double r = fma(-n, 1.90821492927058770002e-10, fma(-n, 6.93147180369123816490e-01, x));  // ln 2 in two parts
-  double s = 1.0 / 6227020800.0;
-  s = fma(s, r, 1.0 / 479001600.0);
-  s = fma(s, r, 1.0 / 39916800.0);
-  s = fma(s, r, 1.0 / 3628800.0);
-  s = fma(s, r, 1.0 / 362880.0);
-  s = fma(s, r, 1.0 / 40320.0);
-  s = fma(s, r, 1.0 / 5040.0);
-  s = fma(s, r, 1.0 / 720.0);
-  s = fma(s, r, 1.0 / 120.0);
-  s = fma(s, r, 1.0 / 24.0);
-  s = fma(s, r, 1.0 / 6.0);
-  s = fma(s, r, 0.5);
-  s = fma(s * r, r, r);
+  const double s = fma(series<12>(EXP_SERIES, r) * r, r, r);
   const int k = (int)n;
   const double y = ldexp(s, k), z = ldexp(1.0, k);
   const double v = one ? y + z : y + (z - 1.0);
@@ -172,10 +176,7 @@ __device__ __forceinline__ double exp_less(double x, bool one) {
 // to s^33 (the next term is below 2^-57 of s).  less: a - b.
 __device__ __forceinline__ double log_ratio(double less, double sum) {
   const double s = less / sum, z = s * s;
-  double y = 1.0 / 33.0;
-#pragma unroll
-  for (int i = 31; i >= 3; i -= 2) y = fma(y, z, 1.0 / i);
-  return 2.0 * fma(y * z, s, s);
+  return 2.0 * fma(series<16>(ATANH_SERIES, z) * z, s, s);
 }
 // log a, a > 0 and finite.
 __device__ __forceinline__ double log_of(double a) {
@@ -345,170 +346,285 @@ __global__ __launch_bounds__(PL_NT) void policy_grad_kernel(PolicyParams p) {
   if (p.total && blockIdx.x == 0) put_total<PL_NT>(p);
 }
 
-// Gradients of a piece's entries `at` .. of a row that is not left out; the token's own entry is
-// put afterwards.
+// A thread's piece of entries `at` ..: where it crosses the row's end, entries from further left
+// that others hold too.  First entry of what it holds.
+template <typename T>
+__device__ __forceinline__ int load_piece(const T* z, int at, int vocab, Piece<T>& v) {
+  const int from = min(at, vocab - Piece<T>::N);
+  v.load(z + from);
+  return from;
+}
+// Keeps the compiler from holding the pieces' values of an earlier use, four times their registers.
+template <typename T>
+__device__ __forceinline__ void anew(Piece<T>& v) {
+  asm volatile("" : "+v"(v.w));
+}
+
+// A number that the compiler takes for another one than before, so that nothing made of it is kept
+// from piece to piece, in registers that the pieces need.
+__device__ __forceinline__ int number_anew(int n) {
+  n = __builtin_amdgcn_readfirstlane(n);
+  asm volatile("" : "+s"(n));
+  return n;
+}
+__device__ __forceinline__ int thread_anew() {
+  int t = threadIdx.x;
+  asm volatile("" : "+v"(t));
+  return t;
+}
+
+// A thread's largest logit and sum of the entries it has seen.
+struct Seen {
+  float m = -INFINITY, l = 0.0f;
+};
+// U more pieces, the i-th at i STEP + t VEC of the `left` entries that the row has from there on.
+// The first FULL of them are whole, those past the row's end not looked at.
+template <typename T, int NT, int U, int FULL>
+__device__ __forceinline__ void see(const PolicyParams& p, Piece<T> (&v)[U], int left, int tok, Seen& s) {
+  constexpr int VEC = Piece<T>::N, STEP = NT * VEC;
+  const int t = thread_anew();
+  left = number_anew(left);
+  // of a piece that crosses the row's end the first `skip` entries are others'
+  const auto skip_of = [&](int i) { return max(i * STEP + t * VEC - (left - VEC), 0); };
+  float most = s.m;
+#pragma unroll
+  for (int i = 0; i < U; ++i) {
+    if (i >= FULL && i * STEP >= left) continue;
+    if (i < FULL || (i + 1) * STEP <= left) {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) most = fmaxf(most, v[i].value(j));
+    } else {
+      const int skip = skip_of(i);
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) most = fmaxf(most, j >= skip ? v[i].value(j) : -INFINITY);
+    }
+  }
+  const float base = base_of(most), cm = c_of(base, p.c);
+  if (most > s.m) {
+    const float was = c_of(base_of(s.m), p.c);
+    const float x = by_c(cm) && by_c(was) ? was - cm : (s.m - most) * p.c;
+    s.l = s.l == 0.0f ? 0.0f : s.l * __builtin_amdgcn_exp2f(x);
+    s.m = most;
+  }
+  // the token's entry (of the pieces from the first on, negative: none) stays out of the sum
+  const bool by = __all(by_c(cm));
+  float l = 0.0f;
+  left = number_anew(left);
+  tok = number_anew(tok);
+#pragma unroll
+  for (int i = 0; i < U; ++i) anew(v[i]);
+#pragma unroll
+  for (int i = 0; i < U; ++i) {
+    if (i >= FULL && i * STEP >= left) continue;
+    if ((i < FULL || (i + 1) * STEP <= left) && (uint32_t)(tok - i * STEP) >= (uint32_t)STEP && by) {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) l += __builtin_amdgcn_exp2f(fmaf(v[i].value(j), p.c, -cm));
+    } else {
+      const int skip = skip_of(i), own = tok - i * STEP - t * VEC + skip;
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        const float z = v[i].value(j);
+        const float e = __builtin_amdgcn_exp2f(by_c(cm) ? fmaf(z, p.c, -cm) : (z - base) * p.c);
+        l += j >= skip && !(tok >= 0 && j == own) ? e : 0.0f;
+      }
+    }
+  }
+  s.l += l;
+#pragma unroll
+  for (int i = 0; i < U; ++i) anew(v[i]);
+}
+
+// Gradients of a thread's piece of a row that is not left out; the token's own entry is put
+// afterwards.
 template <typename T>
 __device__ __forceinline__ void put_grad(const PolicyParams& p, const RowGrad& g, float cm, bool by, const Piece<T>& v,
                                          T* out, int at) {
   constexpr int VEC = Piece<T>::N;
+  Piece<T> x = v;
+  anew(x);
   float y[VEC];
-  if (by) {
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) y[j] = g.mul * __builtin_amdgcn_exp2f(fmaf(v.value(j), p.c, -cm));
-  } else {
-#pragma unroll
-    for (int j = 0; j < VEC; ++j) y[j] = g.mul * __builtin_amdgcn_exp2f((v.value(j) - g.base) * p.c);
-  }
+  for (int j = 0; j < VEC; ++j)
+    y[j] = g.mul * __builtin_amdgcn_exp2f(by ? fmaf(x.value(j), p.c, -cm) : (x.value(j) - g.base) * p.c);
   if (at + VEC <= p.vocab) {
-    Piece<T> w;
-    w.put(y);
-    w.store(out + at);
+    x.put(y);
+    x.store_past(out + at);
   } else {
+    const int from = p.vocab - VEC;
 #pragma unroll
     for (int j = 0; j < VEC; ++j)
-      if (at + j < p.vocab) put_entry(out + at + j, y[j]);
+      if (from + j >= at) put_entry(out + from + j, y[j]);
   }
 }
 
-// A workgroup of NT threads a row, U pieces of a thread at a time.  HELD: all of the row's.
-template <typename T, int NT, int U, bool HELD>
-__global__ __launch_bounds__(NT) void policy_whole_kernel(PolicyParams p) {
-  constexpr int VEC = Piece<T>::N, WAVES = NT / 64, STEP = NT * VEC, TURN = U * STEP;
-  __shared__ float s_most[WAVES], s_sum[WAVES];
-  __shared__ RowGrad s_grad;
+// The threads' sums of a row, joined: what its gradient takes, in every thread.
+template <int NT>
+struct JoinScratch {
+  float most[NT / 64], sum[NT / 64];
+  RowGrad grad;
+};
+template <int NT>
+__device__ __forceinline__ RowGrad join_row(const PolicyParams& p, int64_t row, const RowIn& in, const Seen& s,
+                                            JoinScratch<NT>& scratch) {
+  constexpr int WAVES = NT / 64;
   const int t = threadIdx.x;
-  const int64_t row = blockIdx.x;
-  const T* z = reinterpret_cast<const T*>(p.logits + row * p.stride);
-  const int tok = p.tokens[row];
-  const int turns = HELD ? 1 : (p.vocab + TURN - 1) / TURN;
-  Piece<T> v[U];
-  const auto load = [&](int begin) {
-    if (begin + TURN <= p.vocab) {
-#pragma unroll
-      for (int i = 0; i < U; ++i) v[i].load(z + (begin + i * STEP) + (uint32_t)(t * VEC));
-      return;
-    }
-#pragma unroll
-    for (int i = 0; i < U; ++i) {
-      const int at = begin + i * STEP + t * VEC;
-      v[i] = Piece<T>{};
-      if (at + VEC <= p.vocab) {
-        v[i].load(z + at);
-      } else {
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) v[i].set(j, at + j < p.vocab ? Elem<T>::load(z, at + j) : -INFINITY);
-      }
-    }
-  };
-  RowIn in;
-  if (t == 0) in = row_in<T>(p, row, tok);
-  float m = -INFINITY, l = 0.0f;
-#pragma unroll 1
-  for (int turn = 0; turn < turns; ++turn) {
-    const int begin = turn * TURN;
-    load(begin);
-    float most = m;
-#pragma unroll
-    for (int i = 0; i < U; ++i)
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) most = fmaxf(most, v[i].value(j));
-    const float cm = c_of(base_of(most), p.c);
-    if (most > m) {
-      const float was = c_of(base_of(m), p.c);
-      const float x = by_c(cm) && by_c(was) ? was - cm : (m - most) * p.c;
-      l = l == 0.0f ? 0.0f : l * __builtin_amdgcn_exp2f(x);
-      m = most;
-    }
-    const int at = tok - begin;  // the token's entry stays out of the sum
-    if (at >= 0 && at < TURN) {
-#pragma unroll
-      for (int i = 0; i < U; ++i)
-#pragma unroll
-        for (int j = 0; j < VEC; ++j)
-          if (at == i * STEP + t * VEC + j) v[i].set(j, -INFINITY);
-    }
-    if (by_c(cm)) {
-#pragma unroll
-      for (int i = 0; i < U; ++i)
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) l += __builtin_amdgcn_exp2f(fmaf(v[i].value(j), p.c, -cm));
-    } else {
-      const float base = base_of(m);
-#pragma unroll
-      for (int i = 0; i < U; ++i)
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) l += __builtin_amdgcn_exp2f((v[i].value(j) - base) * p.c);
-    }
-  }
-  // ---- the threads' sums, then the waves' ----
-  const float wave_most = max_over_wave(m);
-  const float wave_sum = sum_over_wave(joined(p, m, l, wave_most));
+  const float wave_most = max_over_wave(s.m);
+  const float wave_sum = sum_over_wave(joined(p, s.m, s.l, wave_most));
   if ((t & 63) == 0) {
-    s_most[t >> 6] = wave_most;
-    s_sum[t >> 6] = wave_sum;
+    scratch.most[t >> 6] = wave_most;
+    scratch.sum[t >> 6] = wave_sum;
   }
   __syncthreads();
   if (t < 64) {
     const int i = min(t, WAVES - 1);
-    const float most = max_over_wave(s_most[i]);
+    const float most = max_over_wave(scratch.most[i]);
     // a wave's sum has no rounded C in it
-    const double x = ((double)base_of(s_most[i]) - base_of(most)) * ((double)p.c + p.c_rest);
-    double sum = t < WAVES && s_sum[i] != 0.0f ? s_sum[i] * exp_less(x * 6.93147180559945309417e-01, true) : 0.0;
+    const double x = ((double)base_of(scratch.most[i]) - base_of(most)) * ((double)p.c + p.c_rest);
+    double sum = t < WAVES && scratch.sum[i] != 0.0f ? scratch.sum[i] * exp_less(x * 6.93147180559945309417e-01, true) : 0.0;
 #pragma unroll
     for (int o = WAVES / 2; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
-    if (t == 0) s_grad = finish_row(p, row, in, most, sum);
+    if (t == 0) scratch.grad = finish_row(p, row, in, most, sum);
   }
-  if (!p.grad) return;
   __syncthreads();
-  // ---- the gradient ----
-  const RowGrad g = s_grad;
-  T* out = reinterpret_cast<T*>(p.grad + row * p.grad_stride);
-  if (g.tok < 0) {
-    Piece<T> zero{};
-    for (int at = t * VEC; at < p.vocab; at += STEP) {
-      if (at + VEC <= p.vocab) {
-        zero.store(out + at);
-      } else {
-        for (int j = at; j < p.vocab; ++j) put_entry(out + j, 0.0f);
-      }
-    }
-    return;
+  return scratch.grad;
+}
+
+// A row of zeros.
+template <typename T, int NT>
+__device__ __forceinline__ void put_zeros(const PolicyParams& p, T* out) {
+  constexpr int VEC = Piece<T>::N;
+  const Piece<T> zero{};
+#pragma unroll 1
+  for (int at = threadIdx.x * VEC; at < p.vocab; at += NT * VEC) {
+    if (at + VEC <= p.vocab) zero.store_past(out + at);
+    else
+      for (int j = at; j < p.vocab; ++j) put_entry(out + j, 0.0f);
   }
+}
+
+// Short rows, of at most NT 32 entries: a workgroup a row, in its registers.
+template <typename T, int NT>
+__global__ __launch_bounds__(NT) void policy_short_kernel(PolicyParams p) {
+  constexpr int VEC = Piece<T>::N, U = 32 / VEC, STEP = NT * VEC;
+  __shared__ JoinScratch<NT> scratch;
+  const int t = threadIdx.x;
+  const int64_t row = blockIdx.x;
+  const T* z = reinterpret_cast<const T*>(p.logits + row * p.stride);
+  const int tok = p.tokens[row];
+  Piece<T> v[U];
+#pragma unroll
+  for (int i = 0; i < U; ++i) {
+    const int at = i * STEP + t * VEC;
+    if (i * STEP >= p.vocab) continue;
+    if (p.vocab >= VEC) {
+      load_piece(z, at, p.vocab, v[i]);
+    } else {  // in the place that entries from further left would have
+      v[i] = Piece<T>{};
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) v[i].set(j, p.vocab - VEC + j >= 0 ? Elem<T>::load(z, p.vocab - VEC + j) : -INFINITY);
+    }
+  }
+  const RowIn in = row_in<T>(p, row, tok);
+  Seen s;
+  see<T, NT, U, 0>(p, v, p.vocab, tok, s);
+  const RowGrad g = join_row<NT>(p, row, in, s, scratch);
+  if (!p.grad) return;
+  T* out = reinterpret_cast<T*>(p.grad + row * p.grad_stride);
+  if (g.tok < 0) return put_zeros<T, NT>(p, out);
   const float cm = c_of(g.base, p.c);
   const bool by = by_c(cm);
-#pragma unroll 1
-  for (int turn = turns - 1; turn >= 0; --turn) {
-    const int begin = turn * TURN;
-    if (!HELD) load(begin);
 #pragma unroll
-    for (int i = 0; i < U; ++i) put_grad(p, g, cm, by, v[i], out, begin + i * STEP + t * VEC);
-  }
+  for (int i = 0; i < U; ++i)
+    if (i * STEP < p.vocab) put_grad(p, g, cm, by, v[i], out, i * STEP + t * VEC);
   if (g.tok % STEP / VEC == t) put_entry(out + g.tok, g.at_tok);  // after the thread's own store there
+}
+
+// Long rows with their gradient: a workgroup of 1024 threads to a row, H pieces of a thread in its
+// registers, of which the last four may lie past the row's end, and what is further right read
+// twice.  As pieces go out, those of the workgroup's next row come in.
+template <typename T, int H>
+__global__ __launch_bounds__(1024, 4) void policy_rows_kernel(PolicyParams p) {
+  constexpr int NT = 1024, VEC = Piece<T>::N, STEP = NT * VEC, U = 4, TURN = U * STEP, FULL = H - 4;
+  __shared__ JoinScratch<NT> scratch;
+  const auto row_of = [&](int64_t row) { return reinterpret_cast<const T*>(p.logits + row * p.stride); };
+  Piece<T> v[H];
+  int64_t row = blockIdx.x;
+#pragma unroll
+  for (int i = 0; i < H; ++i) load_piece(row_of(row), i * STEP + (int)threadIdx.x * VEC, p.vocab, v[i]);
+#pragma unroll 1
+  for (; row < p.rows; row += gridDim.x) {
+    const int tok = p.tokens[row];
+    const RowIn in = row_in<T>(p, row, tok);
+    const T* z = row_of(row);
+    Seen s;
+    see<T, NT, H, FULL>(p, v, p.vocab, tok, s);
+#pragma unroll 1
+    for (int begin = H * STEP; begin < p.vocab; begin += TURN) {
+      Piece<T> w[U];
+      const int t = thread_anew();
+#pragma unroll
+      for (int i = 0; i < U; ++i) load_piece(z, begin + i * STEP + t * VEC, p.vocab, w[i]);
+      see<T, NT, U, 0>(p, w, p.vocab - begin, tok >= begin ? tok - begin : -1, s);
+    }
+    const RowGrad g = join_row<NT>(p, row, in, s, scratch);
+    T* out = reinterpret_cast<T*>(p.grad + row * p.grad_stride);
+    const float cm = c_of(g.base, p.c);
+    const bool by = by_c(cm), more = row + gridDim.x < p.rows, kept = g.tok >= 0;
+    const T* next = row_of(more ? row + gridDim.x : row);
+    if (!kept) put_zeros<T, NT>(p, out);
+    const int t = thread_anew(), vocab = number_anew(p.vocab);
+#pragma unroll
+    for (int i = 0; i < H; ++i) {
+      if (kept && (i < FULL || i * STEP < vocab)) put_grad(p, g, cm, by, v[i], out, i * STEP + t * VEC);
+      // after the last row one piece again and again, which is in the cache
+      load_piece(next, more ? i * STEP + t * VEC : t * VEC, vocab, v[i]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if (!kept) continue;
+#pragma unroll 1
+    for (int begin = H * STEP; begin < p.vocab; begin += TURN) {
+      Piece<T> w[U];
+      const int t = thread_anew();
+#pragma unroll
+      for (int i = 0; i < U; ++i) load_piece(z, begin + i * STEP + t * VEC, p.vocab, w[i]);
+#pragma unroll
+      for (int i = 0; i < U; ++i)
+        if (begin + i * STEP < p.vocab) put_grad(p, g, cm, by, w[i], out, begin + i * STEP + t * VEC);
+    }
+    if (g.tok % STEP / VEC == (int)threadIdx.x) put_entry(out + g.tok, g.at_tok);  // after the thread's own store there
+  }
 }
 
 int chunks_of(int vocab) { return (vocab + PL_CHUNK - 1) / PL_CHUNK; }
 
-// Whether a call's rows are taken whole: they fit a workgroup's registers, or there are enough of
-// them.
-constexpr int WHOLE_ROWS = 160;
-template <typename T, int NT, int U, bool HELD>
-void launch_whole(const PolicyParams& p, hipStream_t s) {
-  hipLaunchKernelGGL((policy_whole_kernel<T, NT, U, HELD>), dim3((unsigned)p.rows), dim3(NT), 0, s, p);
-  if (p.total) hipLaunchKernelGGL(policy_total_kernel, dim3(1), dim3(TOTAL_NT), 0, s, p);
-}
+// Rows that a workgroup each is given to, where their gradient is wanted.
+constexpr int WHOLE_ROWS = 160, CUS = 256;
 template <typename T>
 void launch(const PolicyParams& p, hipStream_t s) {
-  constexpr int VEC = Piece<T>::N, SMALL = 32 / VEC, U = 8;
-  if (p.vocab <= 256 * 32) return launch_whole<T, 256, SMALL, true>(p, s);
-  if (p.rows >= WHOLE_ROWS) {
-    if (p.vocab <= 1024 * VEC * U) return launch_whole<T, 1024, U, true>(p, s);
-    return launch_whole<T, 1024, U, false>(p, s);
+  constexpr int VEC = Piece<T>::N, MOST = VEC == 8 ? 19 : 20;  // that the registers take without spilling
+  const dim3 nt(PL_NT);
+  bool total = p.total;
+  if (p.vocab <= PL_NT * 32) {
+    hipLaunchKernelGGL((policy_short_kernel<T, PL_NT>), dim3((unsigned)p.rows), nt, 0, s, p);
+  } else if (p.grad && p.rows >= WHOLE_ROWS) {
+    const dim3 grid((unsigned)std::min<int64_t>(p.rows, CUS));
+    const int pieces = (p.vocab + 1024 * VEC - 1) / (1024 * VEC);
+    const auto go = [&](auto h) { hipLaunchKernelGGL((policy_rows_kernel<T, decltype(h)::value>), grid, dim3(1024), 0, s, p); };
+    if (pieces <= 4) go(std::integral_constant<int, 4>{});
+    else if (pieces <= 8) go(std::integral_constant<int, 8>{});
+    else if (pieces <= 12) go(std::integral_constant<int, 12>{});
+    else if (pieces <= 16) go(std::integral_constant<int, 16>{});
+    else go(std::integral_constant<int, MOST>{});
+  } else {
+    const dim3 grid((unsigned)(p.rows * p.chunks));
+    hipLaunchKernelGGL((policy_chunk_kernel<T>), grid, nt, 0, s, p);
+    hipLaunchKernelGGL((policy_row_kernel<T>), dim3((unsigned)((p.rows + PL_NT / 64 - 1) / (PL_NT / 64))), nt, 0, s, p);
+    if (p.grad) {
+      hipLaunchKernelGGL((policy_grad_kernel<T>), grid, nt, 0, s, p);
+      total = false;
+    }
   }
-  const dim3 grid((unsigned)(p.rows * p.chunks)), nt(PL_NT);
-  hipLaunchKernelGGL((policy_chunk_kernel<T>), grid, nt, 0, s, p);
-  hipLaunchKernelGGL((policy_row_kernel<T>), dim3((unsigned)((p.rows + PL_NT / 64 - 1) / (PL_NT / 64))), nt, 0, s, p);
-  if (p.grad) hipLaunchKernelGGL((policy_grad_kernel<T>), grid, nt, 0, s, p);
-  else if (p.total) hipLaunchKernelGGL(policy_total_kernel, dim3(1), dim3(TOTAL_NT), 0, s, p);
+  if (total) hipLaunchKernelGGL(policy_total_kernel, dim3(1), dim3(TOTAL_NT), 0, s, p);
 }
 
 }  // namespace
