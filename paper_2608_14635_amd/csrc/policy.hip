@@ -443,9 +443,13 @@ __device__ __forceinline__ void put_grad(const PolicyParams& p, const RowGrad& g
   Piece<T> x = v;
   anew(x);
   float y[VEC];
+  if (by) {
 #pragma unroll
-  for (int j = 0; j < VEC; ++j)
-    y[j] = g.mul * __builtin_amdgcn_exp2f(by ? fmaf(x.value(j), p.c, -cm) : (x.value(j) - g.base) * p.c);
+    for (int j = 0; j < VEC; ++j) y[j] = g.mul * __builtin_amdgcn_exp2f(fmaf(x.value(j), p.c, -cm));
+  } else {
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) y[j] = g.mul * __builtin_amdgcn_exp2f((x.value(j) - g.base) * p.c);
+  }
   if (at + VEC <= p.vocab) {
     x.put(y);
     x.store_past(out + at);
@@ -532,7 +536,7 @@ __global__ __launch_bounds__(NT) void policy_short_kernel(PolicyParams p) {
   T* out = reinterpret_cast<T*>(p.grad + row * p.grad_stride);
   if (g.tok < 0) return put_zeros<T, NT>(p, out);
   const float cm = c_of(g.base, p.c);
-  const bool by = by_c(cm);
+  const bool by = __all(by_c(cm));
 #pragma unroll
   for (int i = 0; i < U; ++i)
     if (i * STEP < p.vocab) put_grad(p, g, cm, by, v[i], out, i * STEP + t * VEC);
@@ -549,11 +553,11 @@ __global__ __launch_bounds__(1024, 4) void policy_rows_kernel(PolicyParams p) {
   const auto row_of = [&](int64_t row) { return reinterpret_cast<const T*>(p.logits + row * p.stride); };
   Piece<T> v[H];
   int64_t row = blockIdx.x;
+  int tok = p.tokens[row];
 #pragma unroll
   for (int i = 0; i < H; ++i) load_piece(row_of(row), i * STEP + (int)threadIdx.x * VEC, p.vocab, v[i]);
 #pragma unroll 1
   for (; row < p.rows; row += gridDim.x) {
-    const int tok = p.tokens[row];
     const RowIn in = row_in<T>(p, row, tok);
     const T* z = row_of(row);
     Seen s;
@@ -569,8 +573,9 @@ __global__ __launch_bounds__(1024, 4) void policy_rows_kernel(PolicyParams p) {
     const RowGrad g = join_row<NT>(p, row, in, s, scratch);
     T* out = reinterpret_cast<T*>(p.grad + row * p.grad_stride);
     const float cm = c_of(g.base, p.c);
-    const bool by = by_c(cm), more = row + gridDim.x < p.rows, kept = g.tok >= 0;
+    const bool by = __all(by_c(cm)), more = row + gridDim.x < p.rows, kept = __any(g.tok >= 0);
     const T* next = row_of(more ? row + gridDim.x : row);
+    tok = p.tokens[more ? row + gridDim.x : row];
     if (!kept) put_zeros<T, NT>(p, out);
     const int t = thread_anew(), vocab = number_anew(p.vocab);
 #pragma unroll
