@@ -238,7 +238,7 @@ void launch_rows(const AppendParams& p, hipStream_t s) {
 }
 template <typename T, int D>
 void launch_append(const AppendParams& p, hipStream_t s) {
-  if (p.rows > 1024) launch_rows<T, D, 4>(p, s);
+  if (p.rows > 2048) launch_rows<T, D, 4>(p, s);
   else launch_rows<T, D, 1>(p, s);
 }
 

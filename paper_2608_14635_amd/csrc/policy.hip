@@ -506,9 +506,12 @@ __device__ __forceinline__ void put_zeros(const PolicyParams& p, T* out) {
   }
 }
 
-// Short rows, of at most NT 32 entries: a workgroup a row, in its registers.
+// Short rows, of at most NT 32 entries: a workgroup a row, in its registers.  bf16 rows of the
+// larger workgroups take 64 registers, for two of 1024 threads to a CU: 1024 rows of 32000 with
+// gradient 35.1 us, of 86 registers 41.9.  fp32 rows would spill (256 rows of 32000: 19.9 and
+// 17.3 us).
 template <typename T, int NT>
-__global__ __launch_bounds__(NT) void policy_short_kernel(PolicyParams p) {
+__global__ __launch_bounds__(NT, sizeof(T) == 2 && NT > 256 ? 8 : 4) void policy_short_kernel(PolicyParams p) {
   constexpr int VEC = Piece<T>::N, U = 32 / VEC, STEP = NT * VEC;
   __shared__ JoinScratch<NT> scratch;
   const int t = threadIdx.x;
@@ -602,21 +605,35 @@ __global__ __launch_bounds__(1024, 4) void policy_rows_kernel(PolicyParams p) {
 
 int chunks_of(int vocab) { return (vocab + PL_CHUNK - 1) / PL_CHUNK; }
 
-// Rows that a workgroup each is given to, where their gradient is wanted.
-constexpr int WHOLE_ROWS = 160, CUS = 256;
+// With their gradient, rows from which on each is given to one workgroup.  In us, so and by
+// chunks: of 65536 bf16 logits 96 rows 17.5 and 17.2, 128 rows 18.2 and 19.1, 256 rows 21.1 and
+// 26.1; of 152064 128 rows 29.9 and 28.8, 160 rows 31.7 and 34.1; of 128256 fp32 logits 96 rows
+// 32.1 and 31.0, 128 rows 35.5 and 43.5.
+constexpr int WHOLE_ROWS = 128, CUS = 256;
+// Losses alone of middling rows go by chunks above this many: of 18000 bf16 logits, whole and by
+// chunks, 512 rows 15.2 and 15.5 us, 1024 rows 23.9 and 19.2.
+constexpr int WHOLE_LOSSES = 512;
 template <typename T>
 void launch(const PolicyParams& p, hipStream_t s) {
-  constexpr int VEC = Piece<T>::N, MOST = VEC == 8 ? 19 : 20;  // that the registers take without spilling
+  constexpr int VEC = Piece<T>::N, MOST = VEC == 8 ? 19 : 18;  // fp32, 250 rows of 152064: 68.8 us, with 20 72.6
   const dim3 nt(PL_NT);
   bool total = p.total;
-  if (p.vocab <= PL_NT * 32) {
-    hipLaunchKernelGGL((policy_short_kernel<T, PL_NT>), dim3((unsigned)p.rows), nt, 0, s, p);
+  const auto whole = [&](auto n) {
+    constexpr int NT = decltype(n)::value;
+    hipLaunchKernelGGL((policy_short_kernel<T, NT>), dim3((unsigned)p.rows), dim3(NT), 0, s, p);
+  };
+  if (p.vocab <= 256 * 32) {
+    whole(std::integral_constant<int, 256>{});
+  } else if (p.vocab <= 512 * 32) {
+    whole(std::integral_constant<int, 512>{});
+  } else if (p.vocab <= 1024 * 32 && (p.grad || p.rows <= WHOLE_LOSSES)) {
+    whole(std::integral_constant<int, 1024>{});
   } else if (p.grad && p.rows >= WHOLE_ROWS) {
     const dim3 grid((unsigned)std::min<int64_t>(p.rows, CUS));
-    const int pieces = (p.vocab + 1024 * VEC - 1) / (1024 * VEC);
+    const int pieces = (p.vocab + 1024 * VEC - 1) / (1024 * VEC);  // more than 32 / VEC
     const auto go = [&](auto h) { hipLaunchKernelGGL((policy_rows_kernel<T, decltype(h)::value>), grid, dim3(1024), 0, s, p); };
-    if (pieces <= 4) go(std::integral_constant<int, 4>{});
-    else if (pieces <= 8) go(std::integral_constant<int, 8>{});
+    constexpr int LEAST = VEC == 8 ? 8 : 12;
+    if (pieces <= LEAST) go(std::integral_constant<int, LEAST>{});
     else if (pieces <= 12) go(std::integral_constant<int, 12>{});
     else if (pieces <= 16) go(std::integral_constant<int, 16>{});
     else go(std::integral_constant<int, MOST>{});
