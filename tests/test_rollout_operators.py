@@ -1,0 +1,316 @@
+"""A rollout's step and its loss, as a worker with its own layers runs them: kv_tables_grow,
+kv_append, kv_group_attention, a product with an output matrix, kv_logprobs and
+kv_policy_loss, eagerly and as one captured graph whose lengths and contents change.
+
+Each operator is compared with its formula in 64 bits, taken of what it was given.  With
+u = 2^-24, d the head's dims and half = half a step of the model's type:
+  a stored or turned value of a pair (a, b) with its bias and norm: (d/2 + 6 + 4 + 2) u of
+  |a| + |b| after the norm, the bias's rounding moves the norm by its own share (2 u more),
+  the angle's 2^-48 of at most 2^9 and 2^-46: below (d/2 + 16) u (|a| + |b|); then half;
+  attention: (2 (d + 8) A + 8 + 6 A + 2 (n + 16)) u + 2^-16 of the largest |v| (A the largest
+  sum |q k| / sqrt(d), n positions; 2^-16 for weights as two bf16 numbers), then half;
+  a log probability: (64 + 2 T) u + u |lp| with T = max - min of the scaled logits / ln 2
+  (each exponential's argument and the row's sums);
+  the ratio to the old policy, which was taken of the same logits, and the gradient: the
+  log probability's tolerance once as rho's and e^D's relative error, the gradient's own
+  p_v (64 + 2 T) u twice, then half."""
+import dataclasses
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from paper_2608_14635_amd import harness as Hn  # noqa: E402
+from paper_2608_14635_amd import kvr  # noqa: E402
+from paper_2608_14635_amd import workloads as W  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+CLIP, KL = (0.2, 0.28), 0.05
+
+
+def to64(t):
+    return t.detach().float().cpu().numpy().astype(np.float64)
+
+
+def ptr(t):
+    return t.data_ptr()
+
+
+class Rollout:
+    """Groups of `each` requests over `prefix` common positions; up to `most` new tokens of a
+    request a step."""
+
+    def __init__(self, shape, prefix, each, most, vocab, B=16, seed=0, room=80):
+        self.shape, self.B, self.most, self.V, self.layer = shape, B, most, vocab, 1
+        nq, nkv, d = shape.num_q_heads, shape.num_kv_heads, shape.head_dim
+        self.dt = torch.bfloat16 if shape.dtype == W.BF16 else torch.float32
+        self.g = torch.Generator(device="cuda")
+        self.g.manual_seed(seed)
+        G, R = len(prefix), len(prefix) * each
+        self.R, self.rows = R, R * most
+        self.prefix, self.each = np.array(prefix), each
+        self.lens = np.repeat(self.prefix, each)
+        per = -(-(max(prefix) + room) // B)
+        total = G * per + R * per
+        ids = list(np.random.default_rng(seed).permutation(total))
+        self.tables = np.full((R, per), -1, np.int32)
+        copies = []
+        for r in range(R):
+            first, P = r - r % each, prefix[r // each]
+            for b in range(-(-P // B)):
+                own = r == first or (b + 1) * B > P  # the block in which the prefix ends is each request's
+                self.tables[r, b] = ids.pop() if own else self.tables[first, b]
+                if own and r != first:
+                    copies += [(self.tables[first, b] * B + j, self.tables[r, b] * B + j) for j in range(B)]
+        self.blocks = total
+        self.arena = torch.full((shape.num_layers, 2, total * B, nkv, d), float("nan"), dtype=self.dt, device="cuda")
+        for r in range(R):
+            at = torch.tensor([self.tables[r, j // B] * B + j % B for j in range(self.lens[r])], device="cuda")
+            if r % each == 0:
+                self.arena[self.layer][:, at] = self.rand(2, len(at), nkv, d)
+        if copies:
+            src, dst = torch.tensor(np.array(copies), device="cuda").unbind(1)
+            self.arena[self.layer][:, dst] = self.arena[self.layer][:, src]
+        self.handle = kvr.kv_arena_bind(ptr(self.arena), self.arena.numel() * self.arena.element_size(), shape, B, total)
+        dev = lambda a, t=torch.int32: torch.tensor(np.asarray(a), dtype=t, device="cuda")  # noqa: E731
+        self.d_tables, self.free = dev(self.tables), dev(ids)
+        self.held, self.d_lens = dev(self.lens), dev(self.lens)
+        self.groups, self.d_prefix = dev(np.arange(G + 1) * each), dev(prefix)
+        n = self.rows
+        self.off, self.slots = dev(np.zeros(R + 1)), dev(np.zeros(n), torch.int64)
+        self.positions, self.counts = dev(np.zeros(n)), dev(np.zeros(4))
+        w = (nq + 2 * nkv) * d
+        self.x, self.q = self.rand(n, w), torch.zeros(n, nq * d, dtype=self.dt, device="cuda")
+        self.weights = {}
+        if shape.qk_norm:
+            self.weights.update({k: 1 + 0.1 * self.rand(d) for k in ("q_norm", "k_norm")})
+        if shape.qkv_bias:
+            self.weights.update({k: self.rand((nq if k == "bq" else nkv) * d) for k in ("bq", "bk", "bv")})
+        self.out = torch.zeros(n, nq * d, dtype=self.dt, device="cuda")
+        self.head = self.rand(nq * d, vocab) * (2 / (nq * d) ** 0.5)
+        self.logits = torch.zeros(n, vocab, dtype=self.dt, device="cuda")
+        f = lambda: torch.zeros(n, device="cuda")  # noqa: E731
+        self.tokens, self.noise, self.advantages = dev(np.zeros(n)), torch.zeros(2, n, device="cuda"), f()
+        self.sampled, self.old, self.ref, self.losses, self.lp, self.kls = f(), f(), f(), f(), f(), f()
+        self.total, self.grad = torch.zeros(1, device="cuda"), torch.zeros_like(self.logits)
+        self.max_len = int(self.lens.max()) + room
+        ws = (kvr.kv_group_attention_workspace_bytes(shape, R, n, G, most, self.max_len),
+              kvr.kv_logprobs_workspace_bytes(n, vocab, 0), kvr.kv_policy_loss_workspace_bytes(n, vocab))
+        assert min(ws) > 0
+        self.ws = torch.full((max(ws),), 255, dtype=torch.uint8, device="cuda")  # one for the three, in turn
+
+    def rand(self, *n):
+        return torch.randn(*n, generator=self.g, device="cuda").to(self.dt)
+
+    def feed(self, new):
+        """The next step's inputs: new[r] tokens of request r."""
+        self.held.copy_(self.d_lens)
+        self.lens = self.lens + new
+        self.d_lens.copy_(torch.tensor(self.lens, dtype=torch.int32))
+        rows = int(np.sum(new))
+        self.x.copy_(self.rand(*self.x.shape))
+        pick = lambda *s: torch.randint(0, 5, s, generator=self.g, device="cuda")  # noqa: E731
+        steps = torch.tensor([-0.5, -0.1, 0.0, 0.1, 0.5], device="cuda")  # none near a clip bound
+        self.noise.copy_(steps[pick(2, self.rows)])
+        self.advantages.copy_(torch.randn(self.rows, generator=self.g, device="cuda"))
+        self.tokens.copy_(torch.randint(0, self.V, (self.rows,), generator=self.g, device="cuda", dtype=torch.int32))
+        self.tokens[rows:] = -1
+
+    def step(self):
+        s, n, st = self.shape, self.rows, Hn.stream_ptr()
+        nq, nkv, d = s.num_q_heads, s.num_kv_heads, s.head_dim
+        e, w = self.x.element_size(), self.x.stride(0)
+        kvr.kv_tables_grow(ptr(self.held), ptr(self.d_lens), self.R, self.B, ptr(self.free), len(self.free),
+                           ptr(self.d_tables), self.tables.shape[1], n, ptr(self.off), ptr(self.slots),
+                           ptr(self.positions), ptr(self.counts), stream=st)
+        kvr.kv_append(self.handle, self.layer, {k: ptr(t) for k, t in self.weights.items()}, ptr(self.x), w,
+                      ptr(self.x) + nq * d * e, w, ptr(self.x) + (nq + nkv) * d * e, w, ptr(self.positions),
+                      ptr(self.slots), n, ptr(self.q), nq * d, st)
+        kvr.kv_group_attention(self.handle, self.layer, ptr(self.q), nq * d, ptr(self.off), n, ptr(self.d_lens),
+                               ptr(self.d_tables), self.R, self.tables.shape[1], ptr(self.groups), ptr(self.d_prefix),
+                               len(self.prefix), self.most, self.max_len, ptr(self.out), nq * d, ptr(self.ws),
+                               len(self.ws), st)
+        torch.matmul(self.out, self.head, out=self.logits)
+        kind = kvr.KV_F32 if self.dt == torch.float32 else kvr.KV_BF16
+        kvr.kv_logprobs(ptr(self.logits), kind, n, self.V, self.V, 1.0, ptr(self.tokens), 0, ptr(self.sampled), 0, 0, 0,
+                        ptr(self.ws), len(self.ws), stream=st)
+        torch.add(self.sampled, self.noise[0], out=self.old)
+        torch.add(self.sampled, self.noise[1], out=self.ref)
+        kvr.kv_policy_loss(ptr(self.logits), kind, n, self.V, self.V, 1.0, ptr(self.tokens), ptr(self.old), ptr(self.ref),
+                           ptr(self.advantages), 0, *CLIP, KL, ptr(self.total), ptr(self.losses), ptr(self.lp),
+                           ptr(self.kls), ptr(self.grad), self.V, ptr(self.ws), len(self.ws), stream=st)
+
+    def results(self):
+        return [t.clone() for t in (self.off, self.slots, self.positions, self.counts, self.d_tables, self.q, self.out,
+                                    self.logits, self.sampled, self.total, self.losses, self.lp, self.kls, self.grad,
+                                    self.arena)]
+
+    def check(self, new, before):
+        """`before`: the arena before the step."""
+        s, B = self.shape, self.B
+        nq, nkv, d = s.num_q_heads, s.num_kv_heads, s.head_dim
+        half = torch.finfo(self.dt).eps / 2
+        rows = int(np.sum(new))
+        request = np.repeat(np.arange(self.R), new)
+        position = np.concatenate([np.arange(n - m, n) for n, m in zip(self.lens, new)]).astype(int)
+        tables = self.d_tables.cpu().numpy()
+        assert self.counts.tolist()[1:] == [0, rows, 0]
+        assert self.positions.tolist() == list(position) + [-1] * (self.rows - rows)
+        slots = tables[request, position // B].astype(np.int64) * B + position % B
+        assert self.slots.tolist() == list(slots) + [-1] * (self.rows - rows) and len(set(slots)) == rows
+        # the rows stored and turned; the rest of the arena as it was
+        n = nq + 2 * nkv
+        x = to64(self.x)[:rows].reshape(rows, n, d)
+        w = {k: to64(t) for k, t in self.weights.items()}
+        if s.qkv_bias:
+            x = x + np.concatenate([w["bq"], w["bk"], w["bv"]]).reshape(n, d)
+        qk = x[:, :nq + nkv]
+        if s.qk_norm:
+            qk = qk / np.sqrt((qk ** 2).mean(-1, keepdims=True) + s.rms_eps)
+            qk = qk * np.concatenate([np.tile(w["q_norm"], (nq, 1)), np.tile(w["k_norm"], (nkv, 1))])
+        angle = position[:, None, None] * s.rope_theta ** (-2.0 * np.arange(d // 2) / d)
+        a, b = qk[..., :d // 2], qk[..., d // 2:]
+        turned = np.concatenate([a * np.cos(angle) - b * np.sin(angle), b * np.cos(angle) + a * np.sin(angle)], -1)
+        size = np.tile(np.abs(a) + np.abs(b), 2)
+        tol = (d / 2 + 16) * U * size + half * np.abs(turned) + 1e-37
+        v = x[:, nq + nkv:]
+        v_tol = 2 * U * np.abs(x[:, nq + nkv:]) + half * np.abs(v) + 1e-37
+        if s.qkv_bias:
+            tol, v_tol = tol + 2 * U * (size + 8), v_tol + 2 * U * 8
+        bits = torch.int16 if self.dt == torch.bfloat16 else torch.int32
+        kept = torch.ones(self.arena.shape[:3], dtype=torch.bool, device="cuda")
+        kept[self.layer][:, torch.tensor(slots, device="cuda")] = False
+        assert torch.equal(self.arena.view(bits)[kept], before.view(bits)[kept])
+        plane = to64(self.arena[self.layer])
+        q = to64(self.q)[:rows].reshape(rows, nq, d)
+        assert (np.abs(q - turned[:, :nq]) <= tol[:, :nq]).all()
+        assert (np.abs(plane[0, slots] - turned[:, nq:]) <= tol[:, nq:]).all()
+        assert (np.abs(plane[1, slots] - v) <= v_tol).all()
+        # attention, of the stored rows
+        out = to64(self.out).reshape(self.rows, nq, d)
+        for i in range(rows):
+            r, j = request[i], np.arange(position[i] + 1)
+            at = np.where(j < self.prefix[r // self.each], tables[r - r % self.each, j // B], tables[r, j // B])
+            at = at.astype(np.int64) * B + j % B
+            k, v = (np.repeat(plane[c, at], nq // nkv, 1) for c in (0, 1))
+            score = np.einsum("hd,jhd->hj", q[i], k) / d ** 0.5
+            A = (np.einsum("hd,jhd->hj", np.abs(q[i]), np.abs(k)) / d ** 0.5).max()
+            p = np.exp(score - score.max(1, keepdims=True))
+            want = np.einsum("hj,jhd->hd", p / p.sum(1, keepdims=True), v)
+            off = ((2 * (d + 8) * A + 8 + 6 * A + 2 * (len(j) + 16)) * U + 2.0 ** -16) * np.abs(v).max()
+            assert (np.abs(out[i] - want) <= off + half * np.abs(want) + 1e-37).all(), i
+        # the loss, of the logits
+        z, t = to64(self.logits)[:rows], self.tokens.cpu().numpy()[:rows]
+        m = z.max(1, keepdims=True)
+        e = np.exp(z - m)
+        lse = np.log(e.sum(1))
+        own = np.arange(rows)
+        lp = z[own, t] - m[:, 0] - lse
+        R = (64 + 2 * (m[:, 0] - z.min(1)) / np.log(2)) * U
+        lp_tol = R + U * np.abs(lp)
+        sampled, got, old, ref = (to64(y)[:rows] for y in (self.sampled, self.lp, self.old, self.ref))
+        assert (np.abs(sampled - lp) <= lp_tol).all() and (np.abs(got - lp) <= lp_tol).all()
+        adv = to64(self.advantages)[:rows]
+        rho, D = np.exp(lp - old), ref - lp
+        plain, cut = rho * adv, np.clip(rho, 1 - CLIP[0], 1 + CLIP[1]) * adv
+        assert (np.abs(np.log(rho / (1 - CLIP[0]))) > 1e-2).all() and (np.abs(np.log(rho / (1 + CLIP[1]))) > 1e-2).all()
+        kept = plain <= cut
+        kl = np.expm1(D) - D
+        loss = KL * kl - np.where(kept, plain, cut)
+        slope = -np.where(kept, plain, 0) - KL * np.expm1(D)
+        bend = np.abs(plain) + KL * np.exp(D)
+        loss_tol = 2 * bend * lp_tol + 2 * U * (np.abs(plain) + np.abs(cut) + KL * kl) + 1e-37
+        assert (np.abs(to64(self.losses)[:rows] - loss) <= loss_tol).all()
+        assert (np.abs(to64(self.kls)[:rows] - kl) <= 2 * np.exp(np.abs(D)) * lp_tol + U * kl + 1e-37).all()
+        assert abs(float(self.total) - loss.sum()) <= loss_tol.sum() + U * abs(loss.sum())
+        shape = -e / e.sum(1, keepdims=True)
+        shape[own, t] = -np.expm1(lp)
+        want = slope[:, None] * shape
+        # the token's 1 - p, where p is close to 1: rest over all, as exact as rest is
+        off = np.abs(want) * (2 * R + 8 * U + half)[:, None] + np.abs(shape) * (2 * bend * lp_tol)[:, None] + 1e-36
+        off[own, t] += np.abs(slope) * 2.0 ** -50
+        grad = to64(self.grad)
+        assert (np.abs(grad[:rows] - want) <= off).all()
+        assert not grad[rows:].any() and not to64(self.losses)[rows:].any()
+
+
+CASES = {
+    "bf16": (dataclasses.replace(W.TINY_BF16, num_layers=2), (67, 5, 150), 4, 3, 1000),
+    "bf16_norm_bias": (dataclasses.replace(W.TINY_BF16, num_layers=2, qk_norm=True, qkv_bias=True), (33, 16), 5, 1, 9001),
+    "fp32_norm": (dataclasses.replace(W.TINY_F32, num_layers=2, qk_norm=True), (40, 81), 3, 4, 777),
+    "fp32_many": (dataclasses.replace(W.TINY_F32, num_layers=2, qkv_bias=True), (18,) * 6, 8, 2, 40000),
+}
+
+
+def steps_of(roll, seed):
+    """Tokens of each request, step by step: all, some, none of a group, all again."""
+    rng = np.random.default_rng(seed)
+    for i in range(4):
+        new = np.full(roll.R, roll.most) if i in (0, 3) else rng.integers(0, roll.most + 1, roll.R)
+        if i == 2:
+            new[:roll.each] = 0
+        yield new
+
+
+@pytest.mark.parametrize("name", list(CASES))
+def test_steps_of_a_rollout(name):
+    roll = Rollout(*CASES[name], seed=len(name))
+    for new in steps_of(roll, 3):
+        roll.free = roll.free.roll(-int(roll.counts[0]))  # blocks taken so far go to the back
+        before = roll.arena.clone()
+        roll.feed(new)
+        roll.step()
+        torch.cuda.synchronize()
+        roll.check(new, before)
+
+
+@pytest.mark.parametrize("name", list(CASES))
+def test_a_captured_step_follows_the_rollout(name):
+    """One graph of the whole step, replayed as the contexts grow, against eager calls."""
+    eager, graphed = (Rollout(*CASES[name], seed=7) for _ in range(2))
+    stream = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    first = True
+    for new in steps_of(eager, 5):
+        for x in (eager, graphed):
+            taken = int(x.counts[0])
+            x.free.copy_(x.free.roll(-taken))
+            x.feed(new)
+        if first:  # the library product picks its kernel before the capture
+            with torch.cuda.stream(stream):
+                torch.matmul(graphed.out, graphed.head, out=graphed.logits)
+            torch.cuda.synchronize()
+            with torch.cuda.graph(graph, stream=stream):
+                graphed.step()
+            first = False
+        before = graphed.arena.clone()
+        graph.replay()
+        eager.step()
+        torch.cuda.synchronize()
+        graphed.check(new, before)
+        for a, b in zip(graphed.results(), eager.results()):
+            assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
+def test_two_rollouts_at_once():
+    """Each on a stream and with a workspace of its own, against one after the other."""
+    pair = [Rollout(*CASES["bf16"], seed=1), Rollout(*CASES["fp32_norm"], seed=2)]
+    alone = [Rollout(*CASES["bf16"], seed=1), Rollout(*CASES["fp32_norm"], seed=2)]
+    streams = [torch.cuda.Stream() for _ in pair]
+    for i in range(3):
+        for x in pair + alone:
+            x.free = x.free.roll(-int(x.counts[0]))
+            x.feed(np.full(x.R, 1 + i % x.most))
+        torch.cuda.synchronize()
+        for _ in range(3):  # the same step again writes the same
+            for x, s in zip(pair, streams):
+                with torch.cuda.stream(s):
+                    x.step()
+        for x in alone:
+            x.step()
+        torch.cuda.synchronize()
+        for x, y in zip(pair, alone):
+            for a, b in zip(x.results(), y.results()):
+                assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
