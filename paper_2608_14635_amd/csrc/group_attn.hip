@@ -54,7 +54,7 @@ struct Entity {
   int first, row, cols, group, lo, cost;
 };
 struct Plan {
-  uint32_t size, longer, workers, pad[5];
+  uint32_t more, half, size, longer, workers, pad[3];
 };
 
 struct GroupAttnParams {
@@ -125,21 +125,33 @@ __host__ __device__ constexpr int cost_of(int cols, int most_cols) {
   return most_cols <= 32 || cols <= 16 ? 2 : cols <= 64 ? 3 : MOST_COST;
 }
 
-// All costs in `workers` stretches, the first `longer` of them one longer.  A unit is the
-// worker's that has the first of its cost; none has less than a unit's, so that of an item that
-// several hold each one between the first and the last holds a unit.
+// All costs in stretches: of the first `half` workers `more` each, then the first `longer` of
+// size + 1, then of `size`.  A unit is the worker's that has the first of its cost; none has less
+// than a unit's, so that of an item that several hold each one between the first and the last holds
+// a unit.  Where all are there and have much to do, the first half, on each CU the older of its two
+// workgroups, which is served first, takes 1 + 1/SKEW of the average, the rest as much less (64
+// requests of 1000 - 6000 positions in eight groups: 130 us, evenly 134, with 1/16 132).
+constexpr uint32_t SKEW = 8, SKEWED = 32;
 struct Stretches {
-  uint32_t size, longer, workers;
+  uint32_t more, half, size, longer, workers;
   __device__ __forceinline__ Stretches(uint32_t most, uint32_t total) {
     workers = max(1u, min(most, total / MOST_COST));
-    size = quotient(total, workers);
-    longer = total - size * workers;
+    const uint32_t even = quotient(total, workers);
+    half = workers == most && even >= SKEWED ? workers / 2 : 0;
+    more = even + even / SKEW;
+    const uint32_t rest = total - half * more;
+    size = quotient(rest, workers - half);
+    longer = rest - size * (workers - half);
   }
-  __device__ __forceinline__ explicit Stretches(const Plan& p) : size(p.size), longer(p.longer), workers(p.workers) {}
-  __device__ __forceinline__ uint32_t begin(uint32_t w) const { return w * size + min(w, longer); }
+  __device__ __forceinline__ explicit Stretches(const Plan& p)
+      : more(p.more), half(p.half), size(p.size), longer(p.longer), workers(p.workers) {}
+  __device__ __forceinline__ uint32_t begin(uint32_t w) const {
+    return w < half ? w * more : half * more + (w - half) * size + min(w - half, longer);
+  }
   __device__ __forceinline__ int holder(uint32_t u) const {  // whose u is
-    const uint32_t head = longer * (size + 1);
-    return (int)(u < head ? quotient(u, size + 1) : longer + quotient(u - head, size));
+    if (u < half * more) return (int)quotient(u, more);
+    const uint32_t v = u - half * more, head = longer * (size + 1);
+    return (int)(half + (v < head ? quotient(v, size + 1) : longer + quotient(v - head, size)));
   }
 };
 
@@ -638,6 +650,63 @@ struct Slots {
   }
 };
 
+// The same where four positions on a boundary of four lie in one block, for a wave that brings the
+// fours `four` and four + 1 of every unit: 64 units ahead, a lane each, so that a unit's are read
+// from a lane.  (By the window of entries above it takes 590 of a unit's 3600 cycles, 94 us, not
+// 88, for 48 requests of 24000 shared and 200 - 2000 own positions.)
+template <int POS>
+struct Fours {
+  const int32_t* entries;
+  int lo, hi, four;
+  int first;           // position of lane 0's unit
+  int slot_a, slot_b;  // of the two fours, 0 where the table names none
+  uint32_t bits;       // positions that are there
+  __device__ __forceinline__ Fours(const GroupAttnParams& p, const Shape& s, int pos, int end, int wave)
+      : entries(p.tables + (int64_t)s.table * p.max_blocks), lo(s.lo), hi(end), four(2 * wave) {
+    fill(p, pos);
+  }
+  __device__ __forceinline__ void fill(const GroupAttnParams& p, int pos) {
+    constexpr int N = POS / 4;
+    first = pos;
+    const uint32_t mine = (uint32_t)pos + (threadIdx.x & 63) * POS;
+    int named[N];
+    uint32_t blk = mine / (uint32_t)p.block_size, off = mine - blk * p.block_size, my_off[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      my_off[i] = off;
+      named[i] = blk < (uint32_t)p.max_blocks && mine + 4 * i < (uint32_t)hi ? entries[blk] : -1;
+      off += 4;
+      if (off >= (uint32_t)p.block_size) {
+        off = 0;
+        ++blk;
+      }
+    }
+    bits = 0;
+    slot_a = slot_b = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const bool ok = (uint32_t)named[i] < p.num_blocks;
+      const int slot = ok ? named[i] * p.block_size + (int)my_off[i] : 0;
+      slot_a = i == four ? slot : slot_a;
+      slot_b = i == four + 1 ? slot : slot_b;
+      bits |= ok ? 15u << 4 * i : 0u;
+    }
+    const int from = lo - (int)mine, to = hi - (int)mine;  // of the unit's positions
+    bits &= from <= 0 ? 0xffffffffu : from >= POS ? 0u : 0xffffffffu << from;
+    bits &= to >= POS ? 0xffffffffu : to <= 0 ? 0u : ~(0xffffffffu << to);
+    asm volatile("" : "+v"(slot_a), "+v"(slot_b), "+v"(bits));  // waited for here
+  }
+  // Of the unit that begins at position pos: the fours' slots, the positions that are there.
+  __device__ __forceinline__ void take(const GroupAttnParams& p, int pos, int (&slot)[2], uint32_t& there) {
+    static_assert(POS == 32, "a bit a position");
+    if (pos - first >= 64 * POS) fill(p, pos);
+    const int at = (pos - first) / POS;
+    slot[0] = __builtin_amdgcn_readlane(slot_a, at);
+    slot[1] = __builtin_amdgcn_readlane(slot_b, at);
+    there = __builtin_amdgcn_readlane(bits, at);
+  }
+};
+
 // Sums of the waves, a tile of 16 columns at a time (a wave's part is room for a unit's values
 // too), and units of bf16 K and V on their way and in use.
 constexpr int RING = 4, UNIT_BYTES = 2 * 32 * 256;
@@ -805,19 +874,20 @@ __device__ __forceinline__ void run_shared(const Lists<true>& lists, const Shape
   if (x.first < upto) {
     const char* head_k = p.plane_k + (int64_t)x.kvh * ROWB;
     const char* head_v = p.plane_v + (int64_t)x.kvh * ROWB;
-    Slots<POS> slots(p, s, pos0 + x.first * POS, end);
+    Fours<POS> fours(p, s, pos0 + x.first * POS, end, wave);
     const int bytes = 3 * (int)p.row_bytes + ROWB, row_off = q * (int)p.row_bytes;
     uint32_t there[RING];  // bits of the units in the ring, oldest first
     // a unit's loads; past the last the last again, so that waits count the same
     int fetched = x.first;
     const auto fetch = [&](uint32_t& bits) {
       if (fetched < upto) {
-        const int slot = slots.take(p, bits);
+        int slot[2];
+        fours.take(p, pos0 + fetched * POS, slot, bits);
         char* ring = scratch.ring[(fetched - x.first) % RING];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           const int row = wave * 8 + i * 4;
-          const int64_t at = (int64_t)__builtin_amdgcn_readlane(slot, row) * p.row_bytes;
+          const int64_t at = slot[i] * p.row_bytes;
           load_lds(head_k + at, bytes, ring + row * ROWB, row_off + ((c ^ ((row + q) & 15)) * 16), 0);
           load_lds(head_v + at, bytes, ring + POS * ROWB + row * ROWB, row_off + c * 16, 0);
         }
@@ -946,6 +1016,8 @@ __global__ __launch_bounds__(GA_NT, occupancy_of(COLS)) void group_attn_kernel(G
   const bool starts = (uint32_t)w < st.workers && u0 >= pre[0] && u0 - pre[0] < mine[0];
   if (blockIdx.x == 0 && t == 0) {
     Plan h{};
+    h.more = st.more;
+    h.half = st.half;
     h.size = st.size;
     h.longer = st.longer;
     h.workers = st.workers;

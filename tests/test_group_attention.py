@@ -355,6 +355,51 @@ def test_groups_that_share_nothing_change_nothing():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("each,B", [(9, 16), (40, 24)])
+def test_a_long_prefix_of_many_heads(each, B):
+    """Heads so many that a workgroup's stretch of the prefix is longer than the positions it looks
+    up at once (2048), column tiles of 18 and 80 columns; in 64 bits on the device."""
+    g, nkv, d, P = 2, 64, 128, 19001
+    shape = dataclasses.replace(W.TINY_BF16, num_layers=1, num_q_heads=g * nkv, num_kv_heads=nkv)
+    lens = [P + 1 + 3 * r for r in range(each)]
+    blocks = -(-P // B) + each * (-(-lens[-1] // B) - P // B) + 1
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(each)
+    arena = torch.randn(2, blocks * B, nkv, d, generator=gen, device="cuda", dtype=torch.bfloat16)
+    h = kvr.kv_arena_bind(arena.data_ptr(), arena.numel() * 2, shape, B, blocks)
+    tables = np.full((each, -(-lens[-1] // B)), -1, np.int32)
+    ids = iter(np.random.default_rng(each).permutation(blocks))
+    tables[:, :P // B] = [next(ids) for _ in range(P // B)]
+    for r, n in enumerate(lens):
+        for b in range(P // B, -(-n // B)):
+            tables[r, b] = next(ids)
+    dev = lambda a: torch.tensor(np.asarray(a), dtype=torch.int32, device="cuda")  # noqa: E731
+    q = torch.randn(each, g * nkv * d, generator=gen, device="cuda", dtype=torch.bfloat16)
+    out = torch.full_like(q, KEPT)
+    n = kvr.kv_group_attention_workspace_bytes(shape, each, each, 1, 1, lens[-1])
+    ws = torch.full((n,), 255, dtype=torch.uint8, device="cuda")
+    args = dev(lens), dev(tables), dev([0, each]), dev([P])
+    kvr.kv_group_attention(h, 0, q.data_ptr(), q.stride(0), 0, each, args[0].data_ptr(), args[1].data_ptr(), each,
+                           tables.shape[1], args[2].data_ptr(), args[3].data_ptr(), 1, 1, lens[-1], out.data_ptr(),
+                           out.stride(0), ws.data_ptr(), n, Hn.stream_ptr())
+    torch.cuda.synchronize()
+    for r in (0, 7, each - 1):
+        j = np.arange(lens[r])
+        at = np.where(j < P, tables[0, j // B], tables[r, j // B]).astype(np.int64) * B + j % B
+        at = torch.tensor(at, device="cuda")
+        for head in range(0, nkv, 9):
+            k, v = (arena[c, at, head].double() for c in (0, 1))
+            x = q[r].view(g * nkv, d)[head * g:(head + 1) * g].double()
+            score = x @ k.t().contiguous() / d ** 0.5
+            want = torch.softmax(score, 1) @ v
+            A = float((x.abs() @ k.abs().t().contiguous()).max()) / d ** 0.5
+            off = ((2 * (d + 8) * A + 8 + 6 * A + 2 * (lens[r] + 16)) * U + 2.0 ** -16) * float(v.abs().max())
+            got = out[r].view(g * nkv, d)[head * g:(head + 1) * g].double()
+            assert ((got - want).abs() <= off + 2.0 ** -8 * want.abs() + 1e-37).all(), (r, head)
+    kvr.kv_arena_release(h)
+
+
+@pytest.mark.gpu
 def test_slots_past_four_gib():
     shape = dataclasses.replace(heads("bf16", 4), num_layers=1)
     blocks = (5 << 30) // (2 * 2 * 128 * 16)  # a plane of 5 GiB
