@@ -759,9 +759,9 @@ __device__ __forceinline__ T* out_of(const GroupAttnParams& p, int row, int col,
 
 // A part of an item of up to 16 NT columns, its units shared out to the waves: their sums,
 // merged, to `dst` ([column][ROW]) or, where that is null, to the output rows.
-template <typename T, int D, int NT, typename S>
+template <typename T, int D, int NT, typename S, typename SlotsOf>
 __device__ __forceinline__ void run_split(const Lists<true>& lists, const Shape& s, const Span& x,
-                                          float* dst, S& scratch) {
+                                          float* dst, S& scratch, SlotsOf slots_of) {
   const GroupAttnParams& p = lists.p;
   using R = Regs<T, D>;
   constexpr int JN = D / 16, POS = R::POS, TILES = R::TILES, NS = R::NS;
@@ -774,7 +774,7 @@ __device__ __forceinline__ void run_split(const Lists<true>& lists, const Shape&
   if (first < upto) {
     const char* head_k = p.plane_k + (int64_t)x.kvh * D * sizeof(T);
     const char* head_v = p.plane_v + (int64_t)x.kvh * D * sizeof(T);
-    Slots<POS> slots(p, s, pos0 + first * POS, end);
+    auto slots = slots_of(pos0 + first * POS, end);
     R u;
     uint32_t there, coming;
     int slot = slots.take(p, there);
@@ -1071,15 +1071,82 @@ __global__ __launch_bounds__(GA_NT, occupancy_of(COLS)) void group_attn_kernel(G
       dst = p.part[kind] + (kvh * p.slots[kind] + slot) * p.part_cols[kind] * ROW<D>;
     }
     const Span x{e, (int)tile * COLS, min(COLS, s.cols - (int)tile * COLS), first, upto, kvh};
+    const auto slots_of = [&](int pos, int end) { return Slots<POS>(p, s, pos, end); };
     if (COLS == 16 || x.cols <= 16) {
-      run_split<T, D, 1>(lists, s, x, dst, scratch);
+      run_split<T, D, 1>(lists, s, x, dst, scratch, slots_of);
     } else if constexpr (COLS == 32) {
-      run_split<T, D, 2>(lists, s, x, dst, scratch);
+      run_split<T, D, 2>(lists, s, x, dst, scratch, slots_of);
     } else if constexpr (COLS == 128) {
       if (x.cols <= 64) run_shared<D, 1>(lists, s, x, dst, scratch);
       else run_shared<D, 2>(lists, s, x, dst, scratch);
     }
   }
+}
+
+// Short calls: a workgroup to 16 columns of a request and kv head, all positions there, whose sums
+// go straight out; a prefix is read by every request, through the first one's table, and there is
+// no second kernel.
+constexpr int SHORT_UNITS = 32;
+// The slots of a wave's units, a quarter of those at most, looked up together.
+template <int POS>
+struct ShortSlots {
+  static constexpr int N = SHORT_UNITS / WAVES * POS / 64;
+  int slot[N], first, next;  // of positions first + 64 i + lane, -1 where none is
+  __device__ __forceinline__ ShortSlots(const GroupAttnParams& p, const int32_t* head, const int32_t* own, int prefix,
+                                        int pos, int end)
+      : first(pos), next(pos) {
+    int named[N], blk[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int at = pos + 64 * i + (threadIdx.x & 63);
+      blk[i] = at / p.block_size;
+      named[i] = at < end && blk[i] < p.max_blocks ? (at < prefix ? head : own)[blk[i]] : -1;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int at = pos + 64 * i + (threadIdx.x & 63);
+      slot[i] = (uint32_t)named[i] < p.num_blocks ? named[i] * p.block_size + (at - blk[i] * p.block_size) : -1;
+      asm volatile("" : "+v"(slot[i]));
+    }
+  }
+  __device__ __forceinline__ int take(const GroupAttnParams&, uint32_t& there) {
+    const int at = next - first, x = threadIdx.x & (POS - 1);
+    int from = slot[0];
+#pragma unroll
+    for (int i = 1; i < N; ++i) from = at >= 64 * i ? slot[i] : from;
+    const int mine = __shfl(from, (at & 63) + x, 64);
+    there = (uint32_t)(__ballot(mine >= 0) & ((1ull << POS) - 1));
+    next += POS;
+    return max(mine, 0);
+  }
+};
+template <typename T, int D>
+__global__ __launch_bounds__(GA_NT, 2) void group_short_kernel(GroupAttnParams p) {
+  constexpr int POS = Regs<T, D>::POS;
+  static_assert(SHORT_UNITS / WAVES * POS % 64 == 0 && 64 % POS == 0, "whole units of a wave in its lanes");
+  __shared__ struct {
+    Scratch<D, false> scratch;
+    Known known;
+  } shared;
+  const Lists<true> lists{p, &shared.known};
+  fill_known(p, shared.known);
+  __syncthreads();
+  const int r = blockIdx.z, kvh = blockIdx.y, tile = blockIdx.x * 16;
+  const Rows rows = rows_of(lists, r);
+  Shape s{};
+  s.row = rows.row;
+  s.cols = rows.used * p.g;
+  s.table = r;
+  s.group = group_of(lists, r);
+  s.hi = clamp_to(rows.end, 0, p.most_len);
+  s = uniform(s);
+  if (tile >= s.cols) return;
+  const int prefix = s.group >= 0 ? lists.prefix(s.group) : 0;
+  const int head = s.group >= 0 ? clamp_to(lists.offset(s.group), 0, p.R) : r;
+  const int32_t *own = p.tables + (int64_t)r * p.max_blocks, *first = p.tables + (int64_t)head * p.max_blocks;
+  const Span x{p.G + r, tile, min(16, s.cols - tile), 0, SHORT_UNITS, kvh};
+  run_split<T, D, 1>(lists, s, x, nullptr, shared.scratch,
+                     [&](int pos, int end) { return ShortSlots<POS>(p, first, own, prefix, pos, end); });
 }
 
 // Columns whose sums lie in several places: D / 4 lanes a column, a workgroup the next few
@@ -1200,6 +1267,17 @@ bool takes(const Sizes& z) {
   return (z.R + z.G + z.rows * z.g / 8) * (z.max_len / 8 + 16) <= INT32_MAX;
 }
 
+// Whether a call is short, by the units that its bounds let an item have and by its items.  In us of
+// a call, so and by the other two kernels, 32 q and 8 kv heads in bf16, prefix + own positions: 440
+// + 60 of 4 requests (32 items) 10.3 and 14.3, of 64 (512) 16.7 and 25.8, of 256 (2048) 62.9
+// and 63.0, of 512 122 and 113; 60 + 440 of 256 80 and 118; 900 + 100 of 4 requests 14.7 and
+// 15.3, of 64 26.5 and 28.5, of 128 (1024) 47 and 38.
+int64_t short_tiles(const GroupAttnParams& p) { return ((int64_t)p.g * std::min(p.max_query, p.rows) + 15) / 16; }
+bool is_short(const GroupAttnParams& p, int pos) {
+  const int units = (int)(((int64_t)p.most_len + pos - 1) / pos);
+  return units <= SHORT_UNITS && p.R * (int64_t)p.nkv * short_tiles(p) <= (units <= SHORT_UNITS / 2 ? 2048 : 512);
+}
+
 template <typename T, int D, int COLS>
 void launch_cols(const GroupAttnParams& p, hipStream_t s) {
   hipLaunchKernelGGL((group_attn_kernel<T, D, COLS>), dim3((unsigned)(p.workers * p.nkv)), dim3(GA_NT), 0, s, p);
@@ -1210,7 +1288,10 @@ void launch_cols(const GroupAttnParams& p, hipStream_t s) {
 }
 template <typename T, int D>
 void launch(int cols, const GroupAttnParams& p, hipStream_t s) {
-  if (cols == 16) {
+  if (is_short(p, Regs<T, D>::POS)) {
+    hipLaunchKernelGGL((group_short_kernel<T, D>), dim3((unsigned)short_tiles(p), (unsigned)p.nkv, (unsigned)p.R),
+                       dim3(GA_NT), 0, s, p);
+  } else if (cols == 16) {
     launch_cols<T, D, 16>(p, s);
   } else if constexpr (sizeof(T) == 2) {
     launch_cols<T, D, 128>(p, s);

@@ -176,10 +176,19 @@ class Batch:
         kvr.kv_arena_release(self.handle)
 
 
-def run_and_check(b):
+def run_and_check(b, once=False):
+    """As it is and, unless `once`, with bounds that no short call has."""
     b.run()
     torch.cuda.synchronize()
     b.check()
+    if not once:
+        wider = max(0, -(-1200 // b.B) - b.tables.shape[1])
+        b.tables = np.pad(b.tables, ((0, 0), (0, wider)), constant_values=-1)
+        b.bind(b.max_query, max(b.max_len, 1100))
+        b.out.fill_(KEPT)
+        b.run()
+        torch.cuda.synchronize()
+        b.check()
     b.release()
 
 
@@ -244,20 +253,21 @@ def test_a_prompts_piece(name, g):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("long", [False, True])
 @pytest.mark.parametrize("name", ["bf16", "f32_64"])
-def test_blocks_that_are_not_there(name):
+def test_blocks_that_are_not_there(name, long):
     """Table entries outside the arena, tables narrower than the lengths, a request
     of which nothing is left, lengths above max_len and below zero, prefixes of any number."""
-    b = Batch(heads(name, 4), [100, 64, 33, 200, 50, 10, 90, 80], [1, 3, 2, 1, 1, 2, 1, 2], sizes=[2, 3, 1, 2],
+    b = Batch(heads(name, 4), [100, 64, 33, 1400 if long else 200, 50, 10, 90, 80], [1, 3, 2, 1, 1, 2, 1, 2], sizes=[2, 3, 1, 2],
               prefix=[30, 33, 5, 60], B=16, seed=5)
     b.tables[0, [0, 3]] = -1
     b.tables[1, 2] = b.blocks
     b.tables[2, :3] = [-5, 1 << 30, -(1 << 31)]
-    b.tables = np.ascontiguousarray(b.tables[:, :9])  # request 3 has 13 blocks
+    b.tables = np.ascontiguousarray(b.tables[:, :80 if long else 9])  # request 3 has 88 or 13 blocks
     b.lens[5] = -3
     b.prefix[2], b.prefix[3] = -7, 2 ** 31 - 1
-    b.bind(max_len=64)
-    run_and_check(b)
+    b.bind(max_len=1200 if long else 64)
+    run_and_check(b, once=True)
 
 
 @pytest.mark.gpu
@@ -397,6 +407,15 @@ def test_a_long_prefix_of_many_heads(each, B):
             got = out[r].view(g * nkv, d)[head * g:(head + 1) * g].double()
             assert ((got - want).abs() <= off + 2.0 ** -8 * want.abs() + 1e-37).all(), (r, head)
     kvr.kv_arena_release(h)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name,g", [("bf16", 4), ("bf16", 1), ("f32_32", 4), ("f32_64", 3), ("f32_128", 2)])
+@pytest.mark.parametrize("most", [255, 256, 257, 511, 512, 513, 1023, 1024, 1025])
+def test_lengths_about_a_short_calls(name, g, most):
+    """Lengths up to, at and past those that a workgroup takes at once, of prefixes and behind them."""
+    lens = [most, most - 1, 1, most // 2, most, 64]
+    run_and_check(Batch(heads(name, g), lens, [2, 1, 1, 3, 1, 5], sizes=[2, 3], prefix=[most - 3, 40], before=0, B=24, seed=g), once=True)
 
 
 @pytest.mark.gpu
