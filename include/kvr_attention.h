@@ -5,10 +5,11 @@
  * their requests' block tables name the same blocks for a common prefix, as
  * kv_rebuild_from (kvr_reuse.h) fills them.  kv_group_attention attends over the arena
  * through such tables and reads a group's common positions once for all its requests,
- * not once for each (but in calls so short that reading is not what they wait for).  kv_append (kvr_append.h) stores the rows it reads.  Without groups
- * it is attention over the arena, one or several query rows a request.  Same conventions
- * as kvr.h (status codes, host/device pointers, void* streams, host-side validation
- * before any device work, thread-compatible: calls that only read one arena may overlap).
+ * not once for each (but in calls so short that reading is not what they wait for).
+ * kv_append (kvr_append.h) stores the rows it reads.  Without groups it is attention over
+ * the arena, one or several query rows a request.  Same conventions as kvr.h (status codes,
+ * host/device pointers, void* streams, host-side validation before any device work,
+ * thread-compatible: calls that only read one arena may overlap).
  */
 #ifndef KVR_ATTENTION_H
 #define KVR_ATTENTION_H

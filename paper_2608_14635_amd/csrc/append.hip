@@ -10,6 +10,10 @@
 // of at most an eighth of a turn are their series to y^13 and y^14 (the next terms are
 // below 2^-45), rounded to fp32 at the end.  t's own rounding is 2^-52 of it: 2^-34 of a turn
 // at positions of a million.
+//
+// Every value is read once and written once, so long calls go at a copy's rate: 8191 rows of 40 q
+// and 8 kv heads, 235 MB, in 48.9 us, 4.8 TB/s.  Short ones wait for their loads, one after
+// the other: 64 rows of 32 + 16 heads 5.1 us, 23 rows of 12 + 4 heads 3.8.
 #include <algorithm>
 
 #include "common.h"
@@ -238,6 +242,9 @@ void launch_rows(const AppendParams& p, hipStream_t s) {
 }
 template <typename T, int D>
 void launch_append(const AppendParams& p, hipStream_t s) {
+  // rows of a workgroup, by the calls' us with one and with four: 1024 rows of 64 q and 8 kv heads of
+  // 128 in bf16 11.0 and 16.4, 2048 18.4 and 19.7, 4096 43.9 and 40.2; of 32 + 8 heads 8.3 and
+  // 10.0, 11.9 and 11.6, 25.8 and 22.1; of 8 + 2 heads 7.0 and 6.9, 8.1 and 7.2, 12.7 and 8.7
   if (p.rows > 2048) launch_rows<T, D, 4>(p, s);
   else launch_rows<T, D, 1>(p, s);
 }

@@ -3,11 +3,21 @@
 // Query rows that share a kv head are columns: column i g + h is row i of q head h of the
 // group of heads.  There are two kinds of entities: a group of requests, whose rows all see
 // the group's prefix, and a request, whose rows see what follows it.  An entity's columns in
-// tiles of 16 NT make items, the work of an item comes in units of positions.  Every
-// workgroup takes an equal stretch of the units of all items, entity after entity, whatever
-// the lengths (they are known on the device alone); its four waves share out each item's part
-// of it and merge their sums in LDS.  A second kernel joins what is there of a column: the
-// workgroups' sums over its group's prefix and over its own positions.
+// tiles (of 16, or 128 in bf16 and 32 in fp32) make items, the work of an item comes in units of
+// positions.  Every workgroup takes an equal stretch of the units of all items, entity after
+// entity, whatever the lengths (they are known on the device alone); a unit counts by the
+// columns of its item, an item's start as eight costs more.  Up to 16 (32) columns the four waves
+// share out an item's units and merge their sums in LDS; of more they share out the columns, and
+// units come to all of them through LDS, read once.  A second kernel joins what is there of a
+// column: the workgroups' sums over its group's prefix and over its own positions.  Short calls
+// have a workgroup to an item and no second kernel.
+//
+// Bound by memory with few columns: 64 requests of 1004 - 5980 positions in eight groups, 8 kv
+// heads, 667 MB in 130 us (5.1 TB/s; a read reaches 6.0) + 5.8.  With many (48 requests on one
+// prefix of 24011, 240 columns, 297 MB in 84 - 91 + 9) a workgroup's unit of 32 positions and 128
+// columns takes 3500 cycles: 770 of matrix instructions, 1250 of others, the rest are waits for
+// each other with two waves a SIMD.  Calls of some 20 us by what follows one another: plan 3,
+// first unit 6, the last merges 3, the second kernel 4 to 7.
 //
 // A unit in a wave's registers, lane (q, c) = (lane / 16, lane % 16):
 //   S^T = K Q^T, 16 positions a tile: the lane gets the scores of positions 4q .. 4q+3 for
@@ -42,7 +52,7 @@ constexpr int GA_NT = 256, WAVES = GA_NT / 64;
 constexpr float SLACK = 8.0f, LIFT = 40.0f;  // log2 units
 constexpr int MOST_ROWS = 1 << 24;           // query rows, requests and groups of a call
 constexpr int START = 8;                     // what an item's start costs
-constexpr int CUS = 256;
+constexpr int CUS = 256, A_CU = 2;           // workgroups of a CU, by their registers and LDS
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef u32x4 u32x4_a4 __attribute__((aligned(4)));
@@ -119,7 +129,9 @@ __device__ __forceinline__ float sum_over_q(float v) {
   return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
-// What a unit of an item of so many columns costs: two for one whose waves have a unit each.
+// What a unit of an item of so many columns costs: two for one whose waves have a unit each.  (Four
+// and six of the wider: 98 us, not 94, for 48 requests on one prefix; five and eight 106; four and
+// five 93, but 39.5, not 36.6, where columns are up to 64.)
 constexpr int MOST_COST = 4;
 __host__ __device__ constexpr int cost_of(int cols, int most_cols) {
   return most_cols <= 32 || cols <= 16 ? 2 : cols <= 64 ? 3 : MOST_COST;
@@ -965,11 +977,8 @@ __device__ __forceinline__ void run_shared(const Lists<true>& lists, const Shape
   }
 }
 
-// Workgroups of a CU by their registers.
-constexpr int occupancy_of(int cols) { return 2; }
-
 template <typename T, int D, int COLS>
-__global__ __launch_bounds__(GA_NT, occupancy_of(COLS)) void group_attn_kernel(GroupAttnParams p) {
+__global__ __launch_bounds__(GA_NT, A_CU) void group_attn_kernel(GroupAttnParams p) {
   constexpr int POS = Regs<T, D>::POS;
   __shared__ __attribute__((aligned(1024))) Shared<D, (COLS > 32)> shared;
   auto& scratch = shared.scratch;
@@ -1121,7 +1130,7 @@ struct ShortSlots {
   }
 };
 template <typename T, int D>
-__global__ __launch_bounds__(GA_NT, 2) void group_short_kernel(GroupAttnParams p) {
+__global__ __launch_bounds__(GA_NT, A_CU) void group_short_kernel(GroupAttnParams p) {
   constexpr int POS = Regs<T, D>::POS;
   static_assert(SHORT_UNITS / WAVES * POS % 64 == 0 && 64 % POS == 0, "whole units of a wave in its lanes");
   __shared__ struct {
@@ -1230,7 +1239,8 @@ struct Sizes {
 };
 
 // Columns of an item: the fewest that the average of what shares it fills.  More than 16 go
-// through LDS in bf16, by loads that take rows on boundaries of 16 bytes, four to a block.
+// through LDS in bf16, by loads that take rows on boundaries of 16 bytes, four to a block (128 at
+// most: a wave's two tiles, with their sums, fill its registers; 64 gain nothing for what they fit).
 int cols_of(const kv_model_desc& d, const Sizes& z, bool fours) {
   const int64_t cols = z.G > 0 ? (z.rows * z.g + z.G - 1) / z.G : z.g * std::min(z.max_query, z.rows);
   if (d.dtype == KV_BF16 && !fours) return 16;
@@ -1238,7 +1248,7 @@ int cols_of(const kv_model_desc& d, const Sizes& z, bool fours) {
   return cols > 16 ? 128 : 16;
 }
 // Workgroups of a kv head, a multiple of eight.
-int most_workers(int nkv, int cols) { return std::max(8, CUS * occupancy_of(cols) / nkv / 8 * 8); }
+int most_workers(int nkv) { return std::max(8, CUS * A_CU / nkv / 8 * 8); }
 
 // The workspace: the plan, the entities, the sums of prefixes and those of requests.  Their
 // numbers grow with every size of a call, whichever kernel it takes.
@@ -1248,7 +1258,7 @@ struct GroupLayout {
   int64_t slots[2];
 };
 GroupLayout layout_of(const kv_model_desc& d, const Sizes& z, int cols) {
-  const int64_t columns = z.rows * z.g, row = d.head_dim + 4, most = most_workers(d.num_kv_heads, 16);
+  const int64_t columns = z.rows * z.g, row = d.head_dim + 4, most = most_workers(d.num_kv_heads);
   const int64_t entity[2] = {z.G, z.R}, widest[2] = {std::min<int64_t>(128, columns), std::min<int64_t>(128, z.g * std::min(z.max_query, z.rows))};
   GroupLayout L;
   L.entities = 256;
@@ -1257,7 +1267,7 @@ GroupLayout layout_of(const kv_model_desc& d, const Sizes& z, int cols) {
     const int64_t floats = k == 0 && z.G == 0 ? 0 : d.num_kv_heads * (columns + (entity[k] + most) * widest[k]) * row;
     (k == 0 ? L.part[1] : L.total) = L.part[k] + (uint64_t)round_up(4 * floats, 256);
     L.part_cols[k] = (int)std::min<int64_t>(cols, widest[k]);
-    L.slots[k] = floats ? columns / cols + entity[k] + most_workers(d.num_kv_heads, cols) : 0;
+    L.slots[k] = floats ? columns / cols + entity[k] + most_workers(d.num_kv_heads) : 0;
   }
   return L;
 }
@@ -1387,7 +1397,7 @@ kv_status kv_group_attention(kv_arena_t arena, int32_t layer, const void* q, int
   p.g_inv = g == 1 ? 0 : (uint32_t)(((1ull << 32) + g - 1) / g);
   p.max_query = max_query;
   p.most_len = (int)std::min<int64_t>({max_len, (int64_t)max_blocks * arena->block_size, INT32_MAX});
-  p.workers = most_workers(d.num_kv_heads, cols);
+  p.workers = most_workers(d.num_kv_heads);
   char* ws = static_cast<char*>(workspace);
   p.plan = reinterpret_cast<Plan*>(ws);
   p.entities = reinterpret_cast<Entity*>(ws + L.entities);

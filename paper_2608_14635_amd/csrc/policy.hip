@@ -7,14 +7,19 @@
 // left of 1 - p_t in a sum with its 1 is noise.  The gradient is one factor of the row times
 // e_v, but for the token's entry.
 //
-// Many rows, or short ones: a workgroup a row, which it holds in its registers, as much of it as
-// fits: its threads take their largest logits and sums from there, join them, and then the
-// gradients.
-// Few long rows, and losses alone: a row is cut into chunks; a workgroup reads its chunk once, into registers, and
-// leaves its largest logit and sum.  A wave merges the chunks of a row in a fixed order.  A third
-// kernel turns logits into gradients.
+// Rows that fit the registers of a workgroup, and many longer ones whose gradient is wanted: a
+// workgroup a row, which it holds there, as much of it as fits.  Its threads take their largest
+// logits and sums, join them, and turn what they hold into gradients: the logits are read once.
+// Few long rows, and losses alone: a row is cut into chunks; a workgroup reads its chunk once, into
+// registers, and leaves its largest logit and sum.  A wave merges the chunks of a row in a fixed
+// order.  A third kernel turns logits into gradients.
 // What is done once a row is done in fp64, by short series: the library's exp, log, log1p and expm1
 // are some hundred instructions each, which a row's only lane would wait for from memory.
+//
+// Bound by memory where there is much of it: 1024 rows of 151936 bf16 logits with gradient, 622 MB, in
+// 149 us (4.2 TB/s; a copy reaches 4.7), 250 rows of 152064 fp32 ones 304 MB in 69 (4.4), losses
+// of 384 rows of 128256 bf16 logits 98.5 MB in 22.6 (4.4) + 6.2 + 3.8.  By waiting where there is
+// little: 171 rows of 1024 in 5.7 + 1.6.
 #include <algorithm>
 
 #include "common.h"
@@ -548,7 +553,9 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && NT > 256 ? 8 : 4) void policy
 
 // Long rows with their gradient: a workgroup of 1024 threads to a row, H pieces of a thread in its
 // registers, of which the last four may lie past the row's end, and what is further right read
-// twice.  As pieces go out, those of the workgroup's next row come in.
+// twice.  As pieces go out, those of the workgroup's next row come in.  Of 38 us a row of 151936
+// bf16 logits, sums take 13, the join 10 (it waits for the slowest of 16 waves), gradients 15.
+// Read twice, whole, by 256 to 1024 threads: 162 to 182 us, not 149, for 1024 such rows.
 template <typename T, int H>
 __global__ __launch_bounds__(1024, 4) void policy_rows_kernel(PolicyParams p) {
   constexpr int NT = 1024, VEC = Piece<T>::N, STEP = NT * VEC, U = 4, TURN = U * STEP, FULL = H - 4;
