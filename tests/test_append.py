@@ -172,8 +172,8 @@ def test_rows(name, variant, rows):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("name,rows", [("bf16", 1025), ("bf16", 4097), ("f32_64", 1027), ("f32_16", 1500),
-                                       ("f32_128", 2050)])
+@pytest.mark.parametrize("name,rows", [("bf16", 1025), ("bf16", 2048), ("bf16", 4097), ("f32_64", 2051), ("f32_16", 2500),
+                                       ("f32_32", 2049), ("f32_128", 2050)])
 def test_many_rows(name, rows):
     run_and_check(Rows(shape_of(name, name != "f32_16", True), rows, seed=rows))
 
@@ -189,7 +189,7 @@ def test_positions(name, far):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("name", ["bf16", "f32_32"])
-@pytest.mark.parametrize("rows", [40, 1100])
+@pytest.mark.parametrize("rows", [40, 1100, 2101])
 def test_rows_that_are_passed_over(name, rows):
     """Negative positions; slots of -1, behind the arena, of 2^62 and of the least number."""
     r = Rows(shape_of(name, qk_norm=True, qkv_bias=True), rows, seed=3)
@@ -212,7 +212,7 @@ def test_k_and_v_alone(name):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("rows", [9, 1200])
+@pytest.mark.parametrize("rows", [9, 1200, 2050])
 def test_over_the_queries(rows):
     r = Rows(shape_of("bf16", True), rows, seed=5)
     r.run()

@@ -253,6 +253,13 @@ def test_a_prompts_piece(name, g):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("name", ["bf16", "f32_64"])
+def test_a_whole_prompt(name):
+    """A thousand query rows over as many positions and more, and one row beside them."""
+    run_and_check(Batch(heads(name, 1), [1300, 900], [1000, 1], sizes=[2], prefix=[250], seed=3))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("long", [False, True])
 @pytest.mark.parametrize("name", ["bf16", "f32_64"])
 def test_blocks_that_are_not_there(name, long):

@@ -107,7 +107,9 @@ class Batch:
                 slope = w[i] * (-(plain if kept else 0.0) - fall)
                 bend = w[i] * (abs(plain if kept else 0.0) + beta * np.exp(D))
                 second = np.exp(min(D, 80.0)) * (rest * R) ** 2
-                out["losses"][i], tol["losses"][i] = loss, w[i] * beta * second + abs(slope) * rest * R + 2 * U * w[i] * (abs(plain if kept else cut) + beta * kl)
+                # a term with coefficient 0 is not in the loss, nor is its rounding (0 times an infinite kl is NaN)
+                far = beta * kl if beta else 0.0
+                out["losses"][i], tol["losses"][i] = loss, w[i] * beta * second + abs(slope) * rest * R + 2 * U * w[i] * (abs(plain if kept else cut) + far)
                 out["kls"][i], tol["kls"][i] = kl, abs(np.expm1(D)) * rest * R + U * kl + second
                 shape = -p
                 shape[t[i]] = rest
@@ -138,7 +140,7 @@ class Batch:
             assert not bad.any(), (k, int(bad.sum()), v[bad][:4], w[bad][:4], tol[bad][:4])
 
 
-SIZES = [(1, 1), (3, 2), (5, 7), (70, 301), (4, 8192), (3, 8193), (2, 20001), (3, 131073)]
+SIZES = [(1, 1), (3, 2), (5, 7), (70, 301), (4, 8192), (3, 8193), (2, 20001), (5, 32769), (3, 131073), (1, 1 << 21)]
 
 
 @pytest.mark.gpu
@@ -175,11 +177,12 @@ def test_many_rows(dtype, vocab):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,vocab", [(65, 9001), (7, 40001), (131, 33001)])
 @pytest.mark.parametrize("what", [dict(kl=0.0, ref=False), dict(old=False), dict(weights=False), dict(kl=0.0),
                                   dict(clip=(0.0, 0.0)), dict(clip=(1.0, math.inf)),
                                   dict(old=False, ref=False, weights=False, kl=0.0)])
-def test_what_may_be_left_out(dtype, what):
-    b = Batch(65, 9001, dtype, seed=5, **what)
+def test_what_may_be_left_out(dtype, what, rows, vocab):
+    b = Batch(rows, vocab, dtype, seed=5, **what)
     if what.get("clip") == (0.0, 0.0):
         b.old += 0.01  # off the bounds that ratios of 1 are on
     b.run()
@@ -192,7 +195,7 @@ def test_what_may_be_left_out(dtype, what):
 def test_forward_alone(dtype):
     """The same results without a gradient, by the same tolerances (rows are summed in another
     order), and nothing written to it."""
-    for rows, vocab in ((300, 10007), (5, 40000), (400, 900)):
+    for rows, vocab in ((300, 10007), (5, 40000), (400, 900), (512, 17003), (513, 17003)):
         b = Batch(rows, vocab, dtype, pad=1, seed=6)
         b.run(grad=False)
         torch.cuda.synchronize()
@@ -219,11 +222,11 @@ def test_over_the_logits(dtype, rows, vocab):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("vocab", [700, 17000])
-def test_tokens_next_to_certain(dtype, vocab):
+@pytest.mark.parametrize("rows,vocab", [(40, 700), (40, 17000), (40, 50000), (140, 50000)])
+def test_tokens_next_to_certain(dtype, rows, vocab):
     """Log probabilities of -1e-3 to -1e-20, to parts of themselves."""
-    b = Batch(40, vocab, dtype, seed=8, std=1.0)
-    b.z[torch.arange(40, device="cuda"), b.tokens.long()] = torch.linspace(8, 60, 40, device="cuda").to(b.dt)
+    b = Batch(rows, vocab, dtype, seed=8, std=1.0)
+    b.z[torch.arange(rows, device="cuda"), b.tokens.long()] = torch.linspace(8, 60, rows, device="cuda").to(b.dt)
     b.old.fill_(-0.1)
     b.ref.fill_(-0.05)
     want = b.reference()
@@ -235,12 +238,12 @@ def test_tokens_next_to_certain(dtype, vocab):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("vocab", [64, 9000])
-def test_masked_and_left_out(dtype, vocab):
+@pytest.mark.parametrize("rows,vocab", [(12, 64), (12, 9000), (12, 33000), (140, 33000)])
+def test_masked_and_left_out(dtype, rows, vocab):
     """Masked logits, rows of nothing else, weights of 0 over NaN, tokens that are none."""
-    b = Batch(12, vocab, dtype, seed=9, kl=0.0)
+    b = Batch(rows, vocab, dtype, seed=9, kl=0.0)
     tok, inf, nan = b.tokens.long(), math.inf, math.nan
-    keep = b.z[torch.arange(12), tok].clone()
+    keep = b.z[torch.arange(rows), tok].clone()
     b.z[0, ::2] = -inf
     b.z[1, :] = -inf
     b.z[2, :] = -inf                                  # the token's alone
@@ -275,8 +278,9 @@ def test_masked_and_left_out(dtype, vocab):
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype,std,scale", [("f32", 1e30, 1e-30), ("f32", 5e37, 4e-38), ("bf16", 1e37, 1e-37),
                                              ("f32", 3000.0, 1.0), ("f32", 1e-3, 2000.0)])
-def test_logits_of_any_size(dtype, std, scale):
-    b = Batch(20, 3000, dtype, seed=10, std=std, scale=scale)
+@pytest.mark.parametrize("rows,vocab", [(20, 3000), (20, 33000), (129, 33000)])
+def test_logits_of_any_size(dtype, std, scale, rows, vocab):
+    b = Batch(rows, vocab, dtype, seed=10, std=std, scale=scale)
     lp = torch.log_softmax(b.z.double() * scale, -1)
     b.tokens[:10] = lp[:10].argmax(-1).int()
     mine = lp.gather(1, b.tokens.long()[:, None])[:, 0]
@@ -327,12 +331,13 @@ def test_gradient_against_differences():
 
 @pytest.mark.gpu
 def test_graphs_follow_their_arrays_and_share_a_workspace():
-    a, b = Batch(33, 20000, seed=12), Batch(9, 500, "bf16", seed=13)
-    ws = torch.full((max(a.ws_bytes, b.ws_bytes),), 255, dtype=torch.uint8, device="cuda")
+    batches = (Batch(33, 20000, seed=12), Batch(9, 500, "bf16", seed=13), Batch(131, 33001, "bf16", seed=15),
+               Batch(5, 40000, seed=16))
+    ws = torch.full((max(x.ws_bytes for x in batches),), 255, dtype=torch.uint8, device="cuda")
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     graphs = []
-    for x in (a, b):
+    for x in batches:
         with torch.cuda.stream(side):
             x.run(ws=ws)
         torch.cuda.synchronize()
@@ -341,7 +346,7 @@ def test_graphs_follow_their_arrays_and_share_a_workspace():
             x.run(ws=ws)
         graphs.append(g)
     for step in range(3):
-        for x, g in zip((a, b), graphs):
+        for x, g in zip(batches, graphs):
             x.z.copy_(torch.randn(x.z.shape, device="cuda") * 2)
             x.tokens.copy_(torch.randint(-1, x.vocab, (x.rows,), device="cuda"))
             # rows may land near a bound: replay and eager are compared bit for bit
@@ -357,8 +362,9 @@ def test_graphs_follow_their_arrays_and_share_a_workspace():
 
 
 @pytest.mark.gpu
-def test_two_streams_at_once():
-    b = Batch(200, 30000, "bf16", seed=14)
+@pytest.mark.parametrize("rows,vocab", [(200, 30000), (300, 40000), (50, 40000)])
+def test_two_streams_at_once(rows, vocab):
+    b = Batch(rows, vocab, "bf16", seed=14)
     b.run()
     torch.cuda.synchronize()
     want, wsum = b.g.clone(), b.total.clone()

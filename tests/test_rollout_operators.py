@@ -239,6 +239,7 @@ class Rollout:
 CASES = {
     "bf16": (dataclasses.replace(W.TINY_BF16, num_layers=2), (67, 5, 150), 4, 3, 1000),
     "bf16_norm_bias": (dataclasses.replace(W.TINY_BF16, num_layers=2, qk_norm=True, qkv_bias=True), (33, 16), 5, 1, 9001),
+    "bf16_long": (dataclasses.replace(W.TINY_BF16, num_layers=2, qk_norm=True), (1100, 2111), 6, 2, 40000),
     "fp32_norm": (dataclasses.replace(W.TINY_F32, num_layers=2, qk_norm=True), (40, 81), 3, 4, 777),
     "fp32_many": (dataclasses.replace(W.TINY_F32, num_layers=2, qkv_bias=True), (18,) * 6, 8, 2, 40000),
 }
