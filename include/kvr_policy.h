@@ -54,8 +54,8 @@ uint64_t kv_policy_loss_workspace_bytes(int64_t rows, int32_t vocab);
  * -infinity (a masked token) has probability and gradient 0; a NaN or +infinity makes its
  * row's results NaN, and the total with them.  Elsewhere infinite inputs go the formula's
  * way.  1 - p_t and log p_t are taken from the other tokens' sum, so that they are
- * exact to a few parts of 2^24 for all but certain tokens too.  Sums are fp32 within a few
- * thousand entries and joined in fp64; grad is rounded once; results do not depend on timing.
+ * exact to a few parts of 2^24 for all but certain tokens too.  Sums are fp32 within a wave
+ * or 8192 entries and joined in fp64; grad is rounded once; results do not depend on timing.
  * The arrays on the device are read when the call runs there, so a captured call follows
  * their contents.
  *   KV_EINVAL  null arrays, rows or vocab out of range, a stride < vocab, an unknown dtype, a

@@ -17,7 +17,7 @@
 // are some hundred instructions each, which a row's only lane would wait for from memory.
 //
 // Bound by memory where there is much of it: 1024 rows of 151936 bf16 logits with gradient, 622 MB, in
-// 149 us (4.2 TB/s; a copy reaches 4.7), 250 rows of 152064 fp32 ones 304 MB in 69 (4.4), losses
+// 154 us (4.0 TB/s; a copy reaches 4.7), 250 rows of 152064 fp32 ones 304 MB in 69 (4.4), losses
 // of 384 rows of 128256 bf16 logits 98.5 MB in 22.6 (4.4) + 6.2 + 3.8.  By waiting where there is
 // little: 171 rows of 1024 in 5.7 + 1.6.
 #include <algorithm>
@@ -378,9 +378,12 @@ __device__ __forceinline__ int thread_anew() {
   return t;
 }
 
-// A thread's largest logit and sum of the entries it has seen.
+// A thread's largest logit and sum of the entries it has seen: fp32 over a piece, then over the
+// pieces of a call of see(): equal entries, added one by one, round one way (that took 151 us,
+// not 154, for 1024 rows of 151936 bf16 logits).
 struct Seen {
-  float m = -INFINITY, l = 0.0f;
+  float m = -INFINITY;
+  double l = 0.0;
 };
 // U more pieces, the i-th at i STEP + t VEC of the `left` entries that the row has from there on.
 // The first FULL of them are whole, those past the row's end not looked at.
@@ -408,7 +411,7 @@ __device__ __forceinline__ void see(const PolicyParams& p, Piece<T> (&v)[U], int
   if (most > s.m) {
     const float was = c_of(base_of(s.m), p.c);
     const float x = by_c(cm) && by_c(was) ? was - cm : (s.m - most) * p.c;
-    s.l = s.l == 0.0f ? 0.0f : s.l * __builtin_amdgcn_exp2f(x);
+    s.l = s.l == 0.0 ? 0.0 : s.l * __builtin_amdgcn_exp2f(x);
     s.m = most;
   }
   // the token's entry (of the pieces from the first on, negative: none) stays out of the sum
@@ -422,16 +425,20 @@ __device__ __forceinline__ void see(const PolicyParams& p, Piece<T> (&v)[U], int
   for (int i = 0; i < U; ++i) {
     if (i >= FULL && i * STEP >= left) continue;
     if ((i < FULL || (i + 1) * STEP <= left) && (uint32_t)(tok - i * STEP) >= (uint32_t)STEP && by) {
+      float sum = __builtin_amdgcn_exp2f(fmaf(v[i].value(0), p.c, -cm));
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) l += __builtin_amdgcn_exp2f(fmaf(v[i].value(j), p.c, -cm));
+      for (int j = 1; j < VEC; ++j) sum += __builtin_amdgcn_exp2f(fmaf(v[i].value(j), p.c, -cm));
+      l += sum;
     } else {
+      float sum = 0.0f;
       const int skip = skip_of(i), own = tok - i * STEP - t * VEC + skip;
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
         const float z = v[i].value(j);
         const float e = __builtin_amdgcn_exp2f(by_c(cm) ? fmaf(z, p.c, -cm) : (z - base) * p.c);
-        l += j >= skip && !(tok >= 0 && j == own) ? e : 0.0f;
+        sum += j >= skip && !(tok >= 0 && j == own) ? e : 0.0f;
       }
+      l += sum;
     }
   }
   s.l += l;
@@ -478,7 +485,7 @@ __device__ __forceinline__ RowGrad join_row(const PolicyParams& p, int64_t row, 
   constexpr int WAVES = NT / 64;
   const int t = threadIdx.x;
   const float wave_most = max_over_wave(s.m);
-  const float wave_sum = sum_over_wave(joined(p, s.m, s.l, wave_most));
+  const float wave_sum = sum_over_wave(joined(p, s.m, (float)s.l, wave_most));
   if ((t & 63) == 0) {
     scratch.most[t >> 6] = wave_most;
     scratch.sum[t >> 6] = wave_sum;
@@ -555,7 +562,7 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && NT > 256 ? 8 : 4) void policy
 // registers, of which the last four may lie past the row's end, and what is further right read
 // twice.  As pieces go out, those of the workgroup's next row come in.  Of 38 us a row of 151936
 // bf16 logits, sums take 13, the join 10 (it waits for the slowest of 16 waves), gradients 15.
-// Read twice, whole, by 256 to 1024 threads: 162 to 182 us, not 149, for 1024 such rows.
+// Read twice, whole, by 256 to 1024 threads: 162 to 182 us, not 154, for 1024 such rows.
 template <typename T, int H>
 __global__ __launch_bounds__(1024, 4) void policy_rows_kernel(PolicyParams p) {
   constexpr int NT = 1024, VEC = Piece<T>::N, STEP = NT * VEC, U = 4, TURN = U * STEP, FULL = H - 4;
@@ -622,7 +629,7 @@ constexpr int WHOLE_ROWS = 128, CUS = 256;
 constexpr int WHOLE_LOSSES = 512;
 template <typename T>
 void launch(const PolicyParams& p, hipStream_t s) {
-  constexpr int VEC = Piece<T>::N, MOST = VEC == 8 ? 19 : 18;  // fp32, 250 rows of 152064: 68.8 us, with 20 72.6
+  constexpr int VEC = Piece<T>::N, MOST = VEC == 8 ? 19 : 18;  // fp32, 250 rows of 152064: 68.8 us, with 20 72.6; bf16 with 18 2 us more
   const dim3 nt(PL_NT);
   bool total = p.total;
   const auto whole = [&](auto n) {

@@ -276,6 +276,22 @@ def test_masked_and_left_out(dtype, rows, vocab):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,vocab", [(5, 4000), (5, 30011), (5, 40003), (130, 151936), (130, 500003)])
+def test_equal_logits(dtype, rows, vocab):
+    """Rows of one value, a third of them with a few larger ones: sums of equal terms, whose roundings
+    all go one way."""
+    b = Batch(rows, vocab, dtype, seed=17)
+    b.z[:] = torch.linspace(-3, 3, rows, device="cuda")[:, None].to(b.dt)
+    b.z[::3, ::1000] += 1.0 / 3.0
+    lp = torch.log_softmax(b.z.double(), -1).gather(1, b.tokens.long()[:, None])[:, 0]
+    b.old, b.ref = (lp + 0.1).float(), (lp - 0.2).float()
+    b.run()
+    torch.cuda.synchronize()
+    b.check()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype,std,scale", [("f32", 1e30, 1e-30), ("f32", 5e37, 4e-38), ("bf16", 1e37, 1e-37),
                                              ("f32", 3000.0, 1.0), ("f32", 1e-3, 2000.0)])
 @pytest.mark.parametrize("rows,vocab", [(20, 3000), (20, 33000), (129, 33000)])
