@@ -284,7 +284,8 @@ __device__ __forceinline__ Shape shape_of(const Lists<true>& lists, int e) {
 // The same in every lane, and known to be.
 __device__ __forceinline__ Shape uniform(Shape s) {
   const auto u = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
-  return Shape{u(s.row), u(s.cols), u(s.lo), u(s.hi), u(s.table), u(s.group), u(s.tiles), u(s.units), u(s.cost), (uint32_t)u((int)s.item)};
+  return Shape{u(s.row),   u(s.cols),  u(s.lo),    u(s.hi),   u(s.table),
+               u(s.group), u(s.tiles), u(s.units), u(s.cost), (uint32_t)u((int)s.item)};
 }
 
 // Positions that a query row of a prefix's columns sees.
@@ -780,7 +781,8 @@ __device__ __forceinline__ void run_split(const Lists<true>& lists, const Shape&
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), c = lane & 15, q = lane >> 4;
   Columns<T, D, NT> cl;
   cl.clear();
-  const int end = __builtin_amdgcn_readfirstlane(end_of(lists, s, x)), n = min(x.upto, units_to(s, end, POS)) - x.first, pos0 = s.lo / POS * POS;
+  const int end = __builtin_amdgcn_readfirstlane(end_of(lists, s, x));
+  const int n = min(x.upto, units_to(s, end, POS)) - x.first, pos0 = s.lo / POS * POS;
   const int first = x.first + (int)((int64_t)max(n, 0) * wave / WAVES);
   const int upto = x.first + (int)((int64_t)max(n, 0) * (wave + 1) / WAVES);
   if (first < upto) {
@@ -882,7 +884,8 @@ __device__ __forceinline__ void run_shared(const Lists<true>& lists, const Shape
   Columns<bf16_t, D, NT> cl;
   cl.clear();
   const int skip = wave * 16 * NT;  // of the part's columns
-  const int end = __builtin_amdgcn_readfirstlane(end_of(lists, s, x)), upto = min(x.upto, units_to(s, end, POS)), pos0 = s.lo / POS * POS;
+  const int end = __builtin_amdgcn_readfirstlane(end_of(lists, s, x));
+  const int upto = min(x.upto, units_to(s, end, POS)), pos0 = s.lo / POS * POS;
   if (x.first < upto) {
     const char* head_k = p.plane_k + (int64_t)x.kvh * ROWB;
     const char* head_v = p.plane_v + (int64_t)x.kvh * ROWB;
@@ -937,7 +940,8 @@ __device__ __forceinline__ void run_shared(const Lists<true>& lists, const Shape
         if (edge) cl.mask(w, pos, there[0]);
         cl.weigh(w);
 #pragma unroll
-        for (int i = 0; i < NS; ++i) u.v[i] = *reinterpret_cast<const u32x4*>(ring + POS * ROWB + at_of(i, q) * ROWB + c * 16);
+        for (int i = 0; i < NS; ++i)
+          u.v[i] = *reinterpret_cast<const u32x4*>(ring + POS * ROWB + at_of(i, q) * ROWB + c * 16);
         if (edge) cl.mask_values(u, pos, there[0], ring + POS * ROWB, true);
         cl.sums(u, w);
       }
@@ -1056,7 +1060,8 @@ __global__ __launch_bounds__(GA_NT, A_CU) void group_attn_kernel(GroupAttnParams
   int e = __builtin_amdgcn_readfirstlane(shared.begin.entity);
   if (e < 0) return;
   uint32_t base = __builtin_amdgcn_readfirstlane(shared.begin.cost);
-  int items[2] = {__builtin_amdgcn_readfirstlane(shared.begin.items[0]), __builtin_amdgcn_readfirstlane(shared.begin.items[1])};
+  int items[2] = {__builtin_amdgcn_readfirstlane(shared.begin.items[0]),
+                  __builtin_amdgcn_readfirstlane(shared.begin.items[1])};
   s = uniform(shared.begin.shape);
   for (uint32_t u = u0; u < u1;) {
     while (u - base >= s.all() && e + 1 < E) {
@@ -1069,7 +1074,8 @@ __global__ __launch_bounds__(GA_NT, A_CU) void group_attn_kernel(GroupAttnParams
     const uint32_t from = u - base - tile * s.item, to = min(s.item, from + (u1 - u));
     u += to - from;
     // units whose first is here
-    const int first = (max((int)from - START, 0) + s.cost - 1) / s.cost, upto = (max((int)to - START, 0) + s.cost - 1) / s.cost;
+    const int first = (max((int)from - START, 0) + s.cost - 1) / s.cost;
+    const int upto = (max((int)to - START, 0) + s.cost - 1) / s.cost;
     if (upto <= first) continue;
     const int kind = e < p.G ? 0 : 1;
     // a request's item that is all here, with no prefix before it, goes straight out
@@ -1259,7 +1265,8 @@ struct GroupLayout {
 };
 GroupLayout layout_of(const kv_model_desc& d, const Sizes& z, int cols) {
   const int64_t columns = z.rows * z.g, row = d.head_dim + 4, most = most_workers(d.num_kv_heads);
-  const int64_t entity[2] = {z.G, z.R}, widest[2] = {std::min<int64_t>(128, columns), std::min<int64_t>(128, z.g * std::min(z.max_query, z.rows))};
+  const int64_t entity[2] = {z.G, z.R}, widest[2] = {std::min<int64_t>(128, columns),
+                                                     std::min<int64_t>(128, z.g * std::min(z.max_query, z.rows))};
   GroupLayout L;
   L.entities = 256;
   L.part[0] = L.entities + (uint64_t)round_up((z.G + z.R) * (int64_t)sizeof(Entity), 256);

@@ -629,7 +629,8 @@ constexpr int WHOLE_ROWS = 128, CUS = 256;
 constexpr int WHOLE_LOSSES = 512;
 template <typename T>
 void launch(const PolicyParams& p, hipStream_t s) {
-  constexpr int VEC = Piece<T>::N, MOST = VEC == 8 ? 19 : 18;  // fp32, 250 rows of 152064: 68.8 us, with 20 72.6; bf16 with 18 2 us more
+  // 250 rows of 152064 fp32 logits: 18 pieces held 68.8 us, 20 72.6; bf16 rows of 18 pieces 2 us more
+  constexpr int VEC = Piece<T>::N, MOST = VEC == 8 ? 19 : 18;
   const dim3 nt(PL_NT);
   bool total = p.total;
   const auto whole = [&](auto n) {
@@ -645,7 +646,9 @@ void launch(const PolicyParams& p, hipStream_t s) {
   } else if (p.grad && p.rows >= WHOLE_ROWS) {
     const dim3 grid((unsigned)std::min<int64_t>(p.rows, CUS));
     const int pieces = (p.vocab + 1024 * VEC - 1) / (1024 * VEC);  // more than 32 / VEC
-    const auto go = [&](auto h) { hipLaunchKernelGGL((policy_rows_kernel<T, decltype(h)::value>), grid, dim3(1024), 0, s, p); };
+    const auto go = [&](auto h) {
+      hipLaunchKernelGGL((policy_rows_kernel<T, decltype(h)::value>), grid, dim3(1024), 0, s, p);
+    };
     constexpr int LEAST = VEC == 8 ? 8 : 12;
     if (pieces <= LEAST) go(std::integral_constant<int, LEAST>{});
     else if (pieces <= 12) go(std::integral_constant<int, 12>{});
