@@ -10,7 +10,8 @@
 // Rows that fit the registers of a workgroup, and many longer ones whose gradient is wanted: a
 // workgroup a row, which it holds there, as much of it as fits.  Its threads take their largest
 // logits and sums, join them, and turn what they hold into gradients: the logits are read once.
-// Few long rows, and losses alone: a row is cut into chunks; a workgroup reads its chunk once, into
+// Losses alone of a row to a CU: the same, without holding it.
+// Few long rows, and losses of many: a row is cut into chunks; a workgroup reads its chunk once, into
 // registers, and leaves its largest logit and sum.  A wave merges the chunks of a row in a fixed
 // order.  A third kernel turns logits into gradients.
 // What is done once a row is done in fp64, by short series: the library's exp, log, log1p and expm1
@@ -558,6 +559,37 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && NT > 256 ? 8 : 4) void policy
   if (g.tok % STEP / VEC == t) put_entry(out + g.tok, g.at_tok);  // after the thread's own store there
 }
 
+// Losses of long rows alone: a workgroup a row, which its threads go through with the next four
+// pieces on their way.
+template <typename T>
+__global__ __launch_bounds__(512, 4) void policy_losses_kernel(PolicyParams p) {
+  constexpr int NT = 512, VEC = Piece<T>::N, STEP = NT * VEC, U = 4, TURN = U * STEP;
+  __shared__ JoinScratch<NT> scratch;
+  const int64_t row = blockIdx.x;
+  const T* z = reinterpret_cast<const T*>(p.logits + row * p.stride);
+  const int tok = p.tokens[row];
+  Piece<T> v[U], w[U];
+  const auto load = [&](int begin, Piece<T>(&x)[U]) {
+    const int t = thread_anew();
+#pragma unroll
+    for (int i = 0; i < U; ++i) load_piece(z, min(begin, p.vocab) + i * STEP + t * VEC, p.vocab, x[i]);
+  };
+  const auto look = [&](int begin, Piece<T>(&x)[U], Seen& s) {
+    see<T, NT, U, 0>(p, x, p.vocab - begin, tok >= begin ? tok - begin : -1, s);
+  };
+  load(0, v);
+  const RowIn in = row_in<T>(p, row, tok);
+  Seen s;
+#pragma unroll 1
+  for (int begin = 0; begin < p.vocab; begin += 2 * TURN) {
+    load(begin + TURN, w);
+    look(begin, v, s);
+    load(begin + 2 * TURN, v);
+    if (begin + TURN < p.vocab) look(begin + TURN, w, s);
+  }
+  join_row<NT>(p, row, in, s, scratch);
+}
+
 // Long rows with their gradient: a workgroup of 1024 threads to a row, H pieces of a thread in its
 // registers, of which the last four may lie past the row's end, and what is further right read
 // twice.  As pieces go out, those of the workgroup's next row come in.  Of 38 us a row of 151936
@@ -627,6 +659,10 @@ constexpr int WHOLE_ROWS = 128, CUS = 256;
 // Losses alone of middling rows go by chunks above this many: of 18000 bf16 logits, whole and by
 // chunks, 512 rows 15.2 and 15.5 us, 1024 rows 23.9 and 19.2.
 constexpr int WHOLE_LOSSES = 512;
+// Losses of longer rows: a row to a CU, so and by chunks, of 65536 bf16 logits 16 rows 12.1 and 13.8,
+// 256 rows 13.5 and 18.4; of 128256 64 rows 17.5 and 15.4, 128 rows 17.8 and 17.4, 256 rows 18.6 and
+// 22.3, but 384, of which a CU has two, 34.4 and 30.8; of 152064 fp32 logits 128 rows 23.0 and 22.0,
+// 192 rows 28.0 and 30.0.
 template <typename T>
 void launch(const PolicyParams& p, hipStream_t s) {
   // 250 rows of 152064 fp32 logits: 18 pieces held 68.8 us, 20 72.6; bf16 rows of 18 pieces 2 us more
@@ -643,6 +679,8 @@ void launch(const PolicyParams& p, hipStream_t s) {
     whole(std::integral_constant<int, 512>{});
   } else if (p.vocab <= 1024 * 32 && (p.grad || p.rows <= WHOLE_LOSSES)) {
     whole(std::integral_constant<int, 1024>{});
+  } else if (!p.grad && p.rows <= CUS && (p.vocab <= 65536 || p.rows >= WHOLE_ROWS)) {
+    hipLaunchKernelGGL((policy_losses_kernel<T>), dim3((unsigned)p.rows), dim3(512), 0, s, p);
   } else if (p.grad && p.rows >= WHOLE_ROWS) {
     const dim3 grid((unsigned)std::min<int64_t>(p.rows, CUS));
     const int pieces = (p.vocab + 1024 * VEC - 1) / (1024 * VEC);  // more than 32 / VEC

@@ -195,7 +195,8 @@ def test_what_may_be_left_out(dtype, what, rows, vocab):
 def test_forward_alone(dtype):
     """The same results without a gradient, by the same tolerances (rows are summed in another
     order), and nothing written to it."""
-    for rows, vocab in ((300, 10007), (5, 40000), (400, 900), (512, 17003), (513, 17003)):
+    for rows, vocab in ((300, 10007), (5, 40000), (400, 900), (512, 17003), (513, 17003), (3, 32769), (256, 65536),
+                        (130, 70001), (200, 200003), (257, 40000)):
         b = Batch(rows, vocab, dtype, pad=1, seed=6)
         b.run(grad=False)
         torch.cuda.synchronize()
@@ -234,6 +235,11 @@ def test_tokens_next_to_certain(dtype, rows, vocab):
     b.run()
     torch.cuda.synchronize()
     b.check(want=want)
+    for t in (b.total, b.losses, b.logprobs, b.kls):
+        t.fill_(KEPT)
+    b.run(grad=False)
+    torch.cuda.synchronize()
+    b.check(grad=False, want=want)
 
 
 @pytest.mark.gpu
@@ -273,6 +279,11 @@ def test_masked_and_left_out(dtype, rows, vocab):
     g = to64(b.g)[:, :vocab]
     assert not g[[1, 7, 8, 9, 10, 11]].any()
     assert not g[0, torch.isinf(b.z[0]).cpu().numpy()].any()
+    for t in (b.total, b.losses, b.logprobs, b.kls):
+        t.fill_(KEPT)
+    b.run(grad=False)
+    torch.cuda.synchronize()
+    b.check(grad=False, want=want)
 
 
 @pytest.mark.gpu
@@ -288,7 +299,13 @@ def test_equal_logits(dtype, rows, vocab):
     b.old, b.ref = (lp + 0.1).float(), (lp - 0.2).float()
     b.run()
     torch.cuda.synchronize()
-    b.check()
+    want = b.reference()
+    b.check(want=want)
+    for t in (b.total, b.losses, b.logprobs, b.kls):
+        t.fill_(KEPT)
+    b.run(grad=False)
+    torch.cuda.synchronize()
+    b.check(grad=False, want=want)
 
 
 @pytest.mark.gpu
