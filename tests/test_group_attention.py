@@ -327,11 +327,13 @@ def test_values_next_to_the_largest(name):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("name,g", [("bf16", 2), ("bf16", 5), ("f32_64", 16)])
-def test_more_rows_than_max_query(name, g):
+@pytest.mark.parametrize("wide", [0, 100])
+def test_more_rows_than_max_query(name, g, wide):
     """Rows past max_query are left out; those before them keep their positions."""
     counts = [5, 9, 2, 7]
     b = Batch(heads(name, g), [40, 9, 70, 44], counts, sizes=[4], prefix=[8], seed=12)
-    b.bind(max_query=4)
+    b.tables = np.pad(b.tables, ((0, 0), (0, wide)), constant_values=-1)
+    b.bind(max_query=4, max_len=1100 if wide else None)
     b.run()
     torch.cuda.synchronize()
     want, tol = b.reference()
@@ -344,13 +346,18 @@ def test_more_rows_than_max_query(name, g):
 
 
 @pytest.mark.gpu
-def test_the_prefix_is_the_first_requests():
-    """What other requests' tables say of shared positions is not read."""
-    b = Batch(heads("bf16", 4), [100, 90, 80], sizes=[3], prefix=[64], seed=13)
+@pytest.mark.parametrize("name", ["bf16", "f32_64"])
+@pytest.mark.parametrize("wide", [0, 100])
+def test_the_prefix_is_the_first_requests(name, wide):
+    """What other requests' tables say of shared positions is not read, in a short call and, by its
+    bounds (`wide` entries more in the tables), another."""
+    b = Batch(heads(name, 4), [100, 90, 80], sizes=[3], prefix=[64], seed=13)
+    b.tables = np.pad(b.tables, ((0, 0), (0, wide)), constant_values=-1)
+    b.bind(max_len=1100 if wide else None)
     b.run()
     want = b.out.clone()
     b.tables[1:, :4] = -1
-    b.bind()
+    b.bind(max_len=1100 if wide else None)
     b.out.fill_(KEPT)
     b.run()
     torch.cuda.synchronize()
@@ -513,9 +520,14 @@ def test_two_streams_at_once():
 
 
 @pytest.mark.gpu
-def test_output_over_the_queries():
+@pytest.mark.parametrize("name", ["bf16", "f32_64"])
+@pytest.mark.parametrize("sizes", [[], [3]])
+@pytest.mark.parametrize("wide", [0, 100])
+def test_output_over_the_queries(name, sizes, wide):
     """out may be q itself."""
-    b = Batch(heads("bf16", 5), [70, 500, 63], [4, 2, 1], sizes=[3], prefix=[60], seed=11)
+    b = Batch(heads(name, 5), [70, 500, 63, 90], [4, 2, 1, 30], sizes=sizes, prefix=[60] * len(sizes), seed=11)
+    b.tables = np.pad(b.tables, ((0, 0), (0, wide)), constant_values=-1)
+    b.bind(max_len=1100 if wide else None)
     b.run()
     want = b.out[:, :b.q.shape[1]].clone()
     b.out = b.q
