@@ -22,8 +22,11 @@
 // A unit in a wave's registers, lane (q, c) = (lane / 16, lane % 16):
 //   S^T = K Q^T, 16 positions a tile: the lane gets the scores of positions 4q .. 4q+3 for
 //   column c.
-//   Online softmax per column, exp2 domain, rescaled only where the maximum rose by more
-//   than 2^SLACK.
+//   Online softmax per column, rescaled only where the maximum rose by more than 2^SLACK.
+//   Weights are 2^((s - m) log2 e / sqrt d) with m a score as it came: the difference of near
+//   scores is exact, however large they are.  (A multiple of m, rounded, as the base of one
+//   multiply-add: from scores of 2^33 on its rounding moves the largest weight out of what
+//   fp32 holds.)
 //   O^T = V^T P^T: the lane's weights are the B operand as they are; for the A operand it
 //   holds dims c d/16 .. of its own positions 4q .., which in bf16 it pairs into that
 //   operand's order.  It gets d/4 neighbouring dims of column c: sums, maxima and weights of
@@ -34,9 +37,8 @@
 //   v_mfma_f32_16x16x4_f32) nothing is rounded.
 //   A weight may be 2^SLACK and 2^31 of them add up, so the sums of large V could pass the
 //   largest fp32 number where their quotient, which lies between the V's, does not: all
-//   weights, and their sum, are taken 2^-LIFT as large.  In bf16 the maxima are LIFT too high
-//   for it (exponents are then rounded to 2^-19, below the 2^-17 above), in fp32 weights are
-//   multiplied.
+//   weights, and their sum, are taken 2^-LIFT as large.  In bf16 exponents are LIFT less for it
+//   (and then rounded to 2^-19, below the 2^-17 above), in fp32 weights are multiplied.
 #include <algorithm>
 #include <type_traits>
 
@@ -50,6 +52,9 @@ namespace {
 
 constexpr int GA_NT = 256, WAVES = GA_NT / 64;
 constexpr float SLACK = 8.0f, LIFT = 40.0f;  // log2 units
+// log2 e / sqrt d
+template <int D>
+constexpr float LOG2_SCALE = 1.4426950408889634 / (D == 128 ? 11.313708498984760390 : D == 64 ? 8.0 : 5.6568542494923801952);
 constexpr int MOST_ROWS = 1 << 24;           // query rows, requests and groups of a call
 constexpr int START = 8;                     // what an item's start costs
 constexpr int CUS = 256, A_CU = 2;           // workgroups of a CU, by their registers and LDS
@@ -422,7 +427,7 @@ struct Columns {
   int limit[NT];         // positions that column c sees
   int all;               // that every column does
   f32x4 o[NT][JN];       // [j][r]: dim q d/4 + r d/16 + j of column c
-  float top[NT], l[NT];  // what weights are relative to; the lane's own weights' sum
+  float top[NT], l[NT];  // the score that weights are relative to; the lane's own weights' sum
 
   __device__ __forceinline__ void clear() {
 #pragma unroll
@@ -502,17 +507,16 @@ struct Columns {
 
   // Scores become weights.
   __device__ __forceinline__ void weigh(f32x4 (&sc)[NT][TILES]) {
-    const float scale_log2 = 1.4426950408889634f / sqrtf((float)D);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       float most = sc[nt][0][0];
 #pragma unroll
       for (int i = 1; i < NS; ++i) most = fmaxf(most, sc[nt][i / 4][i % 4]);
-      constexpr float lift = sizeof(T) == 2 ? LIFT : 0.0f;
-      const float rise = max_over_q(most) * scale_log2 + lift;
-      if (__any(rise > top[nt] + SLACK)) {
-        const float now = rise > top[nt] + SLACK ? rise : top[nt];
-        const float f = now == top[nt] ? 1.0f : __builtin_amdgcn_exp2f(top[nt] - now);
+      const float rise = max_over_q(most);
+      const bool higher = (rise - top[nt]) * LOG2_SCALE<D> > SLACK;
+      if (__any(higher)) {
+        const float now = higher ? rise : top[nt];
+        const float f = now == top[nt] ? 1.0f : __builtin_amdgcn_exp2f((top[nt] - now) * LOG2_SCALE<D>);
         top[nt] = now;
         l[nt] *= f;
 #pragma unroll
@@ -521,8 +525,10 @@ struct Columns {
       const float base = top[nt] == -INFINITY ? 0.0f : top[nt];
 #pragma unroll
       for (int i = 0; i < NS; ++i) {
-        float e = __builtin_amdgcn_exp2f(fmaf(sc[nt][i / 4][i % 4], scale_log2, -base));
-        if constexpr (sizeof(T) == 4) e *= 0x1p-40f;
+        const float x = sc[nt][i / 4][i % 4] - base;
+        float e;
+        if constexpr (sizeof(T) == 2) e = __builtin_amdgcn_exp2f(fmaf(x, LOG2_SCALE<D>, -LIFT));
+        else e = __builtin_amdgcn_exp2f(x * LOG2_SCALE<D>) * 0x1p-40f;
         sc[nt][i / 4][i % 4] = e;
         l[nt] += e;
       }
@@ -846,7 +852,7 @@ __device__ __forceinline__ void run_split(const Lists<true>& lists, const Shape&
       for (int j = 0; j < JN; ++j) v[j] = 0.0f;
 #pragma unroll
       for (int i = 0; i < WAVES; ++i) {
-        const float f = __builtin_amdgcn_exp2f(scratch.o[i][col][D] - base);
+        const float f = __builtin_amdgcn_exp2f((scratch.o[i][col][D] - base) * LOG2_SCALE<D>);
         sum = fmaf(scratch.o[i][col][D + 1], f, sum);
 #pragma unroll
         for (int j = 0; j < JN; ++j) v[j] = fmaf(scratch.o[i][col][dim + j], f, v[j]);
@@ -1219,7 +1225,7 @@ __global__ __launch_bounds__(GA_NT) void group_merge_kernel(GroupAttnParams p) {
 #pragma unroll
         for (int i = 0; i < CHUNK; ++i) now = fmaxf(now, ml[i].x);
         const float base = now == -INFINITY ? 0.0f : now;
-        const float was = __builtin_amdgcn_exp2f(top - base);
+        const float was = __builtin_amdgcn_exp2f((top - base) * LOG2_SCALE<D>);
         top = now;
         l *= was;
 #pragma unroll
@@ -1227,7 +1233,7 @@ __global__ __launch_bounds__(GA_NT) void group_merge_kernel(GroupAttnParams p) {
 #pragma unroll
         for (int i = 0; i < CHUNK; ++i)
           if (i0 + i < total) {
-            const float f = __builtin_amdgcn_exp2f(ml[i].x - base);
+            const float f = __builtin_amdgcn_exp2f((ml[i].x - base) * LOG2_SCALE<D>);
             l = fmaf(ml[i].y, f, l);
 #pragma unroll
             for (int d = 0; d < 4; ++d) o[d] = fmaf(v[i][d], f, o[d]);

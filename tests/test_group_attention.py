@@ -315,6 +315,59 @@ def test_scores_of_any_size(name):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("name,counts", [("bf16", None), ("bf16", [9, 5, 1, 12]), ("f32_32", None), ("f32_64", [9, 5, 1, 12]),
+                                         ("f32_128", None)])
+@pytest.mark.parametrize("high,value", [(20, 0), (28, 0), (33, 0), (34, 0), (34, 127), (34, -60), (35, 0), (36, 0), (60, 0),
+                                        (120, 0)])
+def test_large_scores(name, counts, high, value):
+    """Scores of about 2^high and values of about 2^value.  Queries and keys have two dims that are
+    not zero, whose products and sum are fp32 numbers: a score is exact.  Many positions of each
+    sixth share their large product, and differ by what the other adds, few by 2^(high - 20).
+    An exponent's argument, at most 150 where its weight does not vanish, has the roundings of
+    the scale and of two products."""
+    b = Batch(heads(name, 5), [500, 300, 250, 30], counts, sizes=[3], prefix=[200], seed=high)
+    dt, shape = torch_dtype(b.shape), b.shape
+    g = torch.Generator(device="cuda")
+    g.manual_seed(high)
+    of = lambda n, *size: torch.randint(0, n, size, generator=g, device="cuda")  # noqa: E731
+    q = torch.zeros(b.rows, shape.num_q_heads, shape.head_dim, device="cuda")
+    q[..., 7] = (1 + of(128, b.rows, shape.num_q_heads) / 128.0) * 2.0 ** (high // 2)
+    q[1::2, :, 7] *= -1
+    q[..., 9] = 1
+    b.q.copy_(q.flatten(1))
+    keys, values = b.arena[b.layer]
+    new = torch.zeros_like(keys, dtype=torch.float32)
+    steps = torch.tensor([-1.0, -0.75, -127 / 128, 127 / 128, 0.25, 1.0], device="cuda")
+    new[..., 7] = steps[of(6, len(keys), 1)] * 2.0 ** (high - high // 2)
+    new[..., 9] = of(4, len(keys), 1) * 2.0 ** (high - 20)
+    keys.copy_(torch.where(keys.isnan(), torch.nan, new.to(dt)))
+    values.mul_(2.0 ** (value - 4 if value > 0 else value))  # of std 1.3, none above 2^4
+    for copy in (1, 2):  # the prefix's last block is each request's own copy
+        for plane in (keys, values):
+            plane[torch.tensor(b.slots[copy][192:200])] = plane[torch.tensor(b.slots[0][192:200])]
+    q, keys, values = to64(b.q).reshape(q.shape), to64(keys), to64(values)
+    each, half = shape.num_q_heads // shape.num_kv_heads, torch.finfo(dt).eps / 2
+    for wide in (0, 100):  # in a short call, and by its bounds in another
+        b.tables = np.pad(b.tables, ((0, 0), (0, wide)), constant_values=-1)
+        b.bind(b.max_query, max(b.max_len, 12 * wide))
+        b.out.fill_(KEPT)
+        b.run()
+        torch.cuda.synchronize()
+        got = to64(b.out[:, :b.q.shape[1]]).reshape(q.shape)
+        for r, n in enumerate(b.lens):
+            for i in range(b.counts[r]):
+                seen, row = b.slots[r][:n - b.counts[r] + i + 1], b.off[r] + i
+                for h in range(shape.num_q_heads):
+                    x, v = keys[seen, h // each] @ q[row, h], values[seen, h // each]
+                    p = np.exp((x - x.max()) / np.sqrt(shape.head_dim))
+                    want = (p[:, None] * v).sum(0) / p.sum()
+                    rel = (8 + 4 * 150 + 2 * (len(x) + 16)) * U + (2.0 ** -16 if dt == torch.bfloat16 else 0.0)
+                    off = rel * np.abs(v).max() + half * np.abs(want) + 1e-37
+                    assert (np.abs(got[row, h] - want) <= off).all(), (wide, r, i, h, got[row, h, :3], want[:3])
+    b.release()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("name", ["bf16", "f32_64"])
 def test_values_next_to_the_largest(name):
     """Sums of values next to the largest number stay finite, in a prefix and behind it."""
