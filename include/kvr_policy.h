@@ -50,10 +50,14 @@ uint64_t kv_policy_loss_workspace_bytes(int64_t rows, int32_t vocab);
  *   workspace    device scratch, on a boundary of 16 bytes; calls in flight at once
  *                need one each
  * A row with weight 0 has loss and kl 0 and a gradient of zeros, whatever its logits,
- * advantage and log probabilities are; one left out has logprob 0 besides.  A logit of
- * -infinity (a masked token) has probability and gradient 0; a NaN or +infinity makes its
- * row's results NaN, and the total with them.  Elsewhere infinite inputs go the formula's
- * way.  1 - p_t and log p_t are taken from the other tokens' sum, so that they are
+ * advantage and log probabilities are; one left out has logprob 0 besides.  An entry of
+ * probability 0 has gradient 0, also where e^D or rho and the row's slope with it are
+ * infinite (past 2^1023): a masked token, its logit -infinity or so far below the largest
+ * that fp64 holds no e^(x_v - x_max), and every entry beside a token of probability 1.  The
+ * row's own token, where that is masked, is not meant: 1 - p_t is 1 there, lp = -infinity
+ * makes rho 0 (1 without old_logprobs) and D infinite, and loss, kl and the token's entry
+ * are the formula's.  A NaN or +infinity makes its row's results NaN, and the total with
+ * them.  Elsewhere infinite inputs go the formula's way.  1 - p_t and log p_t are taken from the other tokens' sum, so that they are
  * exact to a few parts of 2^24 for all but certain tokens too.  Sums are fp32 within a wave
  * or 8192 entries and joined in fp64; grad is rounded once; results do not depend on timing.
  * The arrays on the device are read when the call runs there, so a captured call follows

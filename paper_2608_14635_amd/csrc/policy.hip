@@ -37,10 +37,11 @@ constexpr int PL_CHUNK = PL_NT * PL_ITEMS;
 constexpr int PL_MAX_VOCAB = 256 * PL_CHUNK;
 constexpr int64_t PL_MOST_CHUNKS = (1 << 24) - 1;  // of a call: a grid holds 2^32 - 1 threads
 
-// What the gradient of a row takes: for v != tok, mul 2^t_v with t_v relative to base; at_tok.
+// What the gradient of a row takes: for v != tok, mul 2^(t_v + more) with t_v relative to base; at_tok.
 struct RowGrad {
   float base, mul, at_tok;
-  int tok;  // -1: a row of zeros, whatever its logits
+  float more;  // 0, but where mul would be large
+  int tok;     // -1: a row of zeros, whatever its logits
 };
 
 struct PolicyParams {
@@ -59,11 +60,6 @@ struct PolicyParams {
   RowGrad* row_grad;  // [rows]
   double* row_loss;   // [rows]
 };
-
-// t of a logit relative to a base whose C is cm.
-__device__ __forceinline__ float t_of(const PolicyParams& p, float z, float base, float cm, bool by) {
-  return by ? fmaf(z, p.c, -cm) : (z - base) * p.c;
-}
 
 // A thread's VECS pieces of the row's entries begin + i STEP + t VEC ..; entries past the row's
 // end are -infinity.  A piece that crosses the end is loaded entry by entry.
@@ -219,6 +215,10 @@ __device__ __forceinline__ RowIn row_in(const PolicyParams& p, int64_t row, int 
   return r;
 }
 
+// Factors above this stay apart from their power of two: a factor near fp32's largest, or past it,
+// times a 2^t that is 0 in fp32 may be any number.  (Of those up to here such products are below
+// 2^-122.)
+constexpr double MOST_MUL = 16.0;
 // A row's results from its largest logit m and the others' sum `rest`, relative to m.
 __device__ __forceinline__ RowGrad finish_row(const PolicyParams& p, int64_t row, const RowIn& r, float m, double rest) {
   const double scale = p.scale, base = base_of(m);
@@ -254,10 +254,39 @@ __device__ __forceinline__ RowGrad finish_row(const PolicyParams& p, int64_t row
   if (p.total) p.row_loss[row] = loss;
   RowGrad g;
   g.base = (float)base;
-  g.mul = none ? 0.0f : (float)(-slope / all * (1.0 - c_rounding_less(p, g.base)));
-  g.at_tok = (float)(slope * not_t);
+  const double factor = none ? 0.0 : -slope / all;
+  g.more = 0.0f;
+  if (fabs(factor) > MOST_MUL) {
+    const bool finite = fabs(factor) < INFINITY;
+    const int k = finite ? ilogb(factor) : 1;
+    g.more = (float)k;
+    g.mul = (float)(finite ? ldexp(factor, -k) : factor);
+  } else {
+    g.mul = (float)(factor * (1.0 - c_rounding_less(p, g.base)));
+  }
+  // what has no probability has no gradient, also where the slope is infinite
+  g.at_tok = not_t == 0.0 && slope == slope ? 0.0f : (float)(slope * not_t);
   g.tok = in && w != 0.0f ? r.tok : -1;
   return g;
+}
+
+// Whether a row's gradients take their exponents by its C, which its factor then allows for.
+__device__ __forceinline__ bool plain_grads(const RowGrad& g, float cm) { return by_c(cm) && g.more == 0.0f; }
+// Gradients of a piece's entries but for the token's.
+template <typename T>
+__device__ __forceinline__ void grads_of(const PolicyParams& p, const RowGrad& g, float cm, bool plain, const Piece<T>& x,
+                                         float (&y)[Piece<T>::N]) {
+  if (plain) {
+#pragma unroll
+    for (int j = 0; j < Piece<T>::N; ++j) y[j] = g.mul * __builtin_amdgcn_exp2f(fmaf(x.value(j), p.c, -cm));
+  } else {
+#pragma unroll
+    for (int j = 0; j < Piece<T>::N; ++j) {
+      const float t = scaled_difference(x.value(j), g.base, p.c, -g.more);
+      // by an infinite slope: of probabilities that fp64 holds
+      y[j] = fabsf(g.mul) == INFINITY ? t < -1074.0f ? 0.0f : g.mul : g.mul * __builtin_amdgcn_exp2f(t);
+    }
+  }
 }
 
 // A sum relative to its largest logit m, relative to `most` and without the rounding of its C.
@@ -328,14 +357,14 @@ __global__ __launch_bounds__(PL_NT) void policy_grad_kernel(PolicyParams p) {
   Piece<T> v[VECS];
   load_pieces(z, begin, p.vocab, v);
   const float cm = c_of(g.base, p.c);
-  const bool by = by_c(cm);
+  const bool plain = __all(plain_grads(g, cm));
 #pragma unroll
   for (int i = 0; i < VECS; ++i) {
     const int at = begin + i * STEP + t * VEC;
     float y[VEC];
+    grads_of(p, g, cm, plain, v[i], y);
 #pragma unroll
     for (int j = 0; j < VEC; ++j) {
-      y[j] = g.mul * __builtin_amdgcn_exp2f(t_of(p, v[i].value(j), g.base, cm, by));
       if (at + j == g.tok) y[j] = g.at_tok;
       if (g.tok < 0) y[j] = 0.0f;
     }
@@ -450,19 +479,13 @@ __device__ __forceinline__ void see(const PolicyParams& p, Piece<T> (&v)[U], int
 // Gradients of a thread's piece of a row that is not left out; the token's own entry is put
 // afterwards.
 template <typename T>
-__device__ __forceinline__ void put_grad(const PolicyParams& p, const RowGrad& g, float cm, bool by, const Piece<T>& v,
+__device__ __forceinline__ void put_grad(const PolicyParams& p, const RowGrad& g, float cm, bool plain, const Piece<T>& v,
                                          T* out, int at) {
   constexpr int VEC = Piece<T>::N;
   Piece<T> x = v;
   anew(x);
   float y[VEC];
-  if (by) {
-#pragma unroll
-    for (int j = 0; j < VEC; ++j) y[j] = g.mul * __builtin_amdgcn_exp2f(fmaf(x.value(j), p.c, -cm));
-  } else {
-#pragma unroll
-    for (int j = 0; j < VEC; ++j) y[j] = g.mul * __builtin_amdgcn_exp2f((x.value(j) - g.base) * p.c);
-  }
+  grads_of(p, g, cm, plain, x, y);
   if (at + VEC <= p.vocab) {
     x.put(y);
     x.store_past(out + at);
@@ -552,10 +575,10 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && NT > 256 ? 8 : 4) void policy
   T* out = reinterpret_cast<T*>(p.grad + row * p.grad_stride);
   if (g.tok < 0) return put_zeros<T, NT>(p, out);
   const float cm = c_of(g.base, p.c);
-  const bool by = __all(by_c(cm));
+  const bool plain = __all(plain_grads(g, cm));
 #pragma unroll
   for (int i = 0; i < U; ++i)
-    if (i * STEP < p.vocab) put_grad(p, g, cm, by, v[i], out, i * STEP + t * VEC);
+    if (i * STEP < p.vocab) put_grad(p, g, cm, plain, v[i], out, i * STEP + t * VEC);
   if (g.tok % STEP / VEC == t) put_entry(out + g.tok, g.at_tok);  // after the thread's own store there
 }
 
@@ -622,14 +645,14 @@ __global__ __launch_bounds__(1024, 4) void policy_rows_kernel(PolicyParams p) {
     const RowGrad g = join_row<NT>(p, row, in, s, scratch);
     T* out = reinterpret_cast<T*>(p.grad + row * p.grad_stride);
     const float cm = c_of(g.base, p.c);
-    const bool by = __all(by_c(cm)), more = row + gridDim.x < p.rows, kept = __any(g.tok >= 0);
+    const bool plain = __all(plain_grads(g, cm)), more = row + gridDim.x < p.rows, kept = __any(g.tok >= 0);
     const T* next = row_of(more ? row + gridDim.x : row);
     tok = p.tokens[more ? row + gridDim.x : row];
     if (!kept) put_zeros<T, NT>(p, out);
     const int t = thread_anew(), vocab = number_anew(p.vocab);
 #pragma unroll
     for (int i = 0; i < H; ++i) {
-      if (kept && (i < FULL || i * STEP < vocab)) put_grad(p, g, cm, by, v[i], out, i * STEP + t * VEC);
+      if (kept && (i < FULL || i * STEP < vocab)) put_grad(p, g, cm, plain, v[i], out, i * STEP + t * VEC);
       // after the last row one piece again and again, which is in the cache
       load_piece(next, more ? i * STEP + t * VEC : t * VEC, vocab, v[i]);
       __builtin_amdgcn_sched_barrier(0);
@@ -643,7 +666,7 @@ __global__ __launch_bounds__(1024, 4) void policy_rows_kernel(PolicyParams p) {
       for (int i = 0; i < U; ++i) load_piece(z, begin + i * STEP + t * VEC, p.vocab, w[i]);
 #pragma unroll
       for (int i = 0; i < U; ++i)
-        if (begin + i * STEP < p.vocab) put_grad(p, g, cm, by, w[i], out, begin + i * STEP + t * VEC);
+        if (begin + i * STEP < p.vocab) put_grad(p, g, cm, plain, w[i], out, begin + i * STEP + t * VEC);
     }
     if (g.tok % STEP / VEC == (int)threadIdx.x) put_entry(out + g.tok, g.at_tok);  // after the thread's own store there
   }
@@ -784,9 +807,9 @@ kv_status kv_policy_loss(const void* logits, int32_t dtype, int64_t rows, int32_
   p.losses = losses;
   p.logprobs = logprobs;
   p.kls = kls;
-  p.row_grad = static_cast<RowGrad*>(workspace);
-  p.row_loss = reinterpret_cast<double*>(p.row_grad + rows);
+  p.row_loss = static_cast<double*>(workspace);
   p.stats = reinterpret_cast<float2*>(p.row_loss + rows);
+  p.row_grad = reinterpret_cast<RowGrad*>(p.stats + rows * p.chunks);
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   if (rows == 0) hipLaunchKernelGGL(policy_total_kernel, dim3(1), dim3(TOTAL_NT), 0, s, p);
   else if (dtype == KV_BF16) launch<bf16_t>(p, s);

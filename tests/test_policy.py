@@ -288,6 +288,51 @@ def test_masked_and_left_out(dtype, rows, vocab):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,vocab", [(12, 64), (12, 9000), (12, 33000), (140, 33000), (140, 170001)])
+def test_steep_rows(dtype, rows, vocab):
+    """Slopes that pass the largest number, by far policies and far references, over probabilities
+    that make numbers of them again; masked logits and those of the least number beside them, at
+    the row's token too.  An entry of probability 0 has gradient 0.  An entry's exponent has the
+    roundings of its difference, of the scale and of the sum: 3 u of its size."""
+    b = Batch(rows, vocab, dtype, pad=1, seed=21, kl=0.05)
+    low, inf = torch.finfo(b.dt).min, math.inf
+    at = [2, vocab // 2, vocab - 3]
+    for i, (mine, others) in enumerate([(-64, -50), (-104, -100), (-304, -300), (-inf, -80), (0, -90), (0, -250), (0, -300),
+                                        (low, -90), (0, -inf)]):
+        b.z[i, at] = others
+        b.z[i, [5, vocab - 9]], b.z[i, [6, vocab // 3]] = -inf, low
+        if i == 8:
+            b.z[i] = -inf
+        b.tokens[i] = [0, vocab - 1, vocab // 4][i % 3]
+        b.z[i, int(b.tokens[i])] = mine
+    lp = torch.log_softmax(b.z[:9].double(), -1).gather(1, b.tokens[:9].long()[:, None])[:, 0]
+    b.old[:9], b.ref[:9] = (lp + 0.1).float(), -2.0
+    b.old[3], b.old[4], b.old[5], b.old[6], b.old[8] = -1.0, lp[4] - 100, lp[5] - 300, lp[6] - 300, -800.0
+    b.advantages[[4, 5, 8]], b.advantages[6] = -1.5, 2.0
+    b.run()
+    torch.cuda.synchronize()
+    want = b.reference()
+    x = to64(b.z) - to64(b.z).max(-1, keepdims=True)
+    with np.errstate(all="ignore"):
+        for k, (v, tol) in want.items():
+            tol = np.where(np.isfinite(tol), tol, 0.0)
+            if k == "grad":
+                none = np.exp(x[:9]) == 0
+                none[8] = True  # its token's probability is 1
+                none[np.arange(8), b.tokens[:8].cpu().numpy()] = False
+                v[:9][none] = 0
+                tol += 3 * U * np.abs(v) * np.minimum(np.abs(x), 1000) / math.log(2)
+            # a rounding to the nearest is infinite from half a step above the largest number on
+            eps = torch.finfo(b.dt if k == "grad" else torch.float32).eps
+            want[k] = (np.where(np.abs(v) >= 2.0 ** 128 * (1 - eps / 4), np.sign(v) * inf, v), tol)
+    assert np.isinf(want["losses"][0][[1, 2, 3, 4, 5, 7, 8]]).all() and np.isfinite(want["losses"][0][[0, 6]]).all()
+    g = np.abs(want["grad"][0][:, at[0]])
+    assert 0.01 < g[1] < 1 and 0.01 < g[2] < 1 and 1e12 < g[5] < 1e22 and np.isinf(g[[3, 7]]).all()
+    b.check(want=want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("rows,vocab", [(5, 4000), (5, 30011), (5, 40003), (130, 151936), (130, 500003)])
 def test_equal_logits(dtype, rows, vocab):
     """Rows of one value, a third of them with a few larger ones: sums of equal terms, whose roundings
