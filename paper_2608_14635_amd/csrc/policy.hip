@@ -439,8 +439,9 @@ __device__ __forceinline__ void see(const PolicyParams& p, Piece<T> (&v)[U], int
   }
   const float base = base_of(most), cm = c_of(base, p.c);
   if (most > s.m) {
-    const float was = c_of(base_of(s.m), p.c);
-    const float x = by_c(cm) && by_c(was) ? was - cm : (s.m - most) * p.c;
+    // by the two C; where not both count, by the logits and the rounding of the one that does
+    const float was = c_of(base_of(s.m), p.c), off = by_c(was) ? -fmaf(base_of(s.m), p.c, -was) : fmaf(base, p.c, -cm);
+    const float x = by_c(cm) == by_c(was) ? by_c(cm) ? was - cm : (s.m - most) * p.c : fmaf(s.m - most, p.c, off);
     s.l = s.l == 0.0 ? 0.0 : s.l * __builtin_amdgcn_exp2f(x);
     s.m = most;
   }

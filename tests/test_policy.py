@@ -380,6 +380,32 @@ def test_logits_of_any_size(dtype, std, scale, rows, vocab):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rows,vocab,grad", [(6, 40000, False), (130, 90001, False), (130, 90001, True), (6, 90001, True),
+                                             (6, 30011, True), (6, 9001, True)])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_logits_of_two_bases(rows, vocab, grad, sign):
+    """Logits in steps of 1/16 about 2^20 ln 2, where their multiples change from numbers that may be
+    rounded to ones that may not: a row's first entries below its later ones, ones above them,
+    all of one height, and steps at odd places.  Differences of logits are exact."""
+    b = Batch(rows, vocab, seed=31, pad=1)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(vocab)
+    steps = torch.randint(-9, 3, b.z.shape, generator=g, device="cuda")  # 726817.5 is 2^20 ln 2 + 0.11
+    at = torch.arange(vocab, device="cuda")
+    steps[0::6] += 6 * (at >= min(8192, vocab // 2))
+    steps[1::6] += 6 * (at < vocab // 2)
+    steps[2::6] += 4 * (at // 4096)
+    steps[4::6] = steps[4::6].clamp(max=-3) + 6 * (at >= 73728)  # past what a long row's registers hold
+    steps[5::6] += 6 * (at % 7919 > 7000)
+    b.z[:] = sign * 726817.5 + steps / 16.0
+    lp = torch.log_softmax(b.z.double(), -1).gather(1, b.tokens.long()[:, None])[:, 0]
+    b.old, b.ref = (lp + 0.1).float(), (lp - 0.2).float()
+    b.run(grad=grad)
+    torch.cuda.synchronize()
+    b.check(grad=grad)
+
+
+@pytest.mark.gpu
 def test_gradient_against_differences():
     """Central differences with step h of the losses that the forward pass returns: off by
     h^2/6 of the third derivative, at most 2 (rho |A| + kl_coef (e^D + 1)), and by the losses' own
