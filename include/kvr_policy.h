@@ -57,9 +57,12 @@ uint64_t kv_policy_loss_workspace_bytes(int64_t rows, int32_t vocab);
  * row's own token, where that is masked, is not meant: 1 - p_t is 1 there, lp = -infinity
  * makes rho 0 (1 without old_logprobs) and D infinite, and loss, kl and the token's entry
  * are the formula's.  A NaN or +infinity makes its row's results NaN, and the total with
- * them.  Elsewhere infinite inputs go the formula's way.  1 - p_t and log p_t are taken from the other tokens' sum, so that they are
- * exact to a few parts of 2^24 for all but certain tokens too.  Sums are fp32 within a wave
- * or 8192 entries and joined in fp64; grad is rounded once; results do not depend on timing.
+ * them.  Elsewhere infinite inputs go the formula's way.  1 - p_t and log p_t are taken
+ * from the other tokens' sum, so that for all but certain tokens too they are off by at most
+ * (50 + 2 T) 2^-24 of themselves, T the largest log2 e (max x - x_v) that counts, below 150
+ * (a few 2^-24 in ordinary rows).  Sums are fp32 over a thread's entries at once or 8192
+ * neighbouring ones and joined in fp64, entries below 2^-126 of the largest left out; grad is
+ * rounded once; results do not depend on timing.
  * The arrays on the device are read when the call runs there, so a captured call follows
  * their contents.
  *   KV_EINVAL  null arrays, rows or vocab out of range, a stride < vocab, an unknown dtype, a

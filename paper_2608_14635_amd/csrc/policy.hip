@@ -140,7 +140,9 @@ __global__ __launch_bounds__(PL_NT) void policy_chunk_kernel(PolicyParams p) {
   }
 }
 
-__device__ __forceinline__ double sum_over_wave(double v) {
+// In fp64, for what is done once a row or a wave of it: a row's threads joined so and in fp32 by
+// lane moves took the same 152.4 - 153.6 us (1024 rows of 151936 bf16 logits).
+__device__ __forceinline__ double sum64_over_wave(double v) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
   return v;
@@ -314,7 +316,7 @@ __global__ __launch_bounds__(PL_NT) void policy_row_kernel(PolicyParams p) {
     const float2 q = stats[i];
     sum += joined(p, q.x, q.y, m);
   }
-  const double rest = sum_over_wave(sum);
+  const double rest = sum64_over_wave(sum);
   if (lane == 0) {
     const RowGrad g = finish_row(p, row, in, m, rest);
     if (p.grad) p.row_grad[row] = g;
@@ -328,7 +330,7 @@ __device__ __forceinline__ void put_total(const PolicyParams& p) {
   double v = 0.0;
 #pragma unroll 4
   for (int64_t i = threadIdx.x; i < p.rows; i += NT) v += p.row_loss[i];
-  v = sum_over_wave(v);
+  v = sum64_over_wave(v);
   if ((threadIdx.x & 63) == 0) s_sum[threadIdx.x >> 6] = v;
   __syncthreads();
   if (threadIdx.x == 0) {
@@ -510,7 +512,7 @@ __device__ __forceinline__ RowGrad join_row(const PolicyParams& p, int64_t row, 
   constexpr int WAVES = NT / 64;
   const int t = threadIdx.x;
   const float wave_most = max_over_wave(s.m);
-  const float wave_sum = sum_over_wave(joined(p, s.m, (float)s.l, wave_most));
+  const float wave_sum = (float)sum64_over_wave(joined(p, s.m, (float)s.l, wave_most));
   if ((t & 63) == 0) {
     scratch.most[t >> 6] = wave_most;
     scratch.sum[t >> 6] = wave_sum;
