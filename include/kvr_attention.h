@@ -68,13 +68,14 @@ uint64_t kv_group_attention_workspace_bytes(const kv_model_desc* desc, int32_t n
  * not finite makes NaN or an infinity of its dim in them.
  * Requests may share blocks, not query rows: q_offsets and group_offsets do not decrease.
  * Nothing but the requests' rows of out is written; q and out may be the same memory only as
- * the same rows.  Results do not depend on timing.  The arrays on the device are read when
- * the call runs there, so a captured call follows their contents.
+ * the same rows, with the same stride.  Results do not depend on timing.  The arrays on the
+ * device are read when the call runs there, so a captured call follows their contents.
  *   KV_EINVAL  null arrays, a layer outside the model, negative sizes, rows, num_requests
  *              or num_groups above 2^24, a stride below nq * d, a pointer or stride not on its
- *              boundary (4 bytes), more than 16 q heads per kv head, head_dim % 32 != 0, an
- *              arena of 2^31 slots or more, rows != num_requests without q_offsets,
- *              max_query or max_len < 1, more work than 2^31 units
+ *              boundary (4 bytes), several rows of out over q with another stride, more
+ *              than 16 q heads per kv head, head_dim % 32 != 0, an arena of 2^31 slots or
+ *              more, rows != num_requests without q_offsets, max_query or max_len < 1, more
+ *              work than 2^31 units
  *   KV_ENOMEM  workspace smaller than kv_group_attention_workspace_bytes
  *   KV_ESTATE  unknown handle
  *   KV_EDEVICE device not selectable, or a device error */

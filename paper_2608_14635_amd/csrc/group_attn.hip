@@ -1367,6 +1367,8 @@ kv_status kv_group_attention(kv_arena_t arena, int32_t layer, const void* q, int
   if (q_stride < row || out_stride < row || q_stride > most_stride || out_stride > most_stride)
     return kvr_err::set(KV_EINVAL, "a stride is below the row's %lld elements, or beyond the addresses there are",
                         (long long)row);
+  if (q == out && rows > 1 && q_stride != out_stride)
+    return kvr_err::set(KV_EINVAL, "out over q needs the same stride");
   if (((uintptr_t)q | (uintptr_t)out | (uintptr_t)(q_stride * e) | (uintptr_t)(out_stride * e) | (uintptr_t)q_offsets |
        (uintptr_t)lens | (uintptr_t)tables | (uintptr_t)group_offsets | (uintptr_t)prefix_lens |
        (uintptr_t)arena->base) % 4 != 0)

@@ -590,6 +590,25 @@ def test_output_over_the_queries(name, sizes, wide):
     b.release()
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("wide", [0, 100])
+def test_output_over_the_queries_takes_their_stride(wide):
+    """Rows at another stride would lie over other requests' queries."""
+    b = Batch(heads("bf16", 5), [70, 500, 63, 90], seed=11)
+    b.tables = np.pad(b.tables, ((0, 0), (0, wide)), constant_values=-1)
+    b.bind(max_len=1100 if wide else None)
+    before, q = b.q.clone(), b.q
+    w = q.shape[1]
+    for out_stride in (w, q.stride(0) - 2):
+        b.out = torch.as_strided(q, q.shape, (out_stride, 1))
+        with pytest.raises(kvr.KvError) as e:
+            b.run()
+        assert e.value.status == kvr.KV_EINVAL
+    torch.cuda.synchronize()
+    assert torch.equal(b.q, before)
+    b.release()
+
+
 # ---- sizes and refusals -----------------------------------------------------
 def test_workspace_bytes():
     s, f = W.LLAMA8B, kvr.kv_group_attention_workspace_bytes
