@@ -432,6 +432,28 @@ def test_groups_that_share_nothing_change_nothing():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("name,g,counts,same", [("bf16", 4, None, True), ("bf16", 16, None, True), ("f32_64", 3, None, True),
+                                                ("f32_128", 8, None, True), ("bf16", 5, [4, 4, 4, 4], True),
+                                                ("bf16", 5, [9, 1, 1, 1], False), ("f32_64", 5, [9, 1, 1, 1], False)])
+@pytest.mark.parametrize("long", [False, True])
+def test_groups_of_one_request_share_nothing(name, g, counts, same, long):
+    """Whatever their prefixes: by the bits of the call without groups where an item has as many
+    columns in both, by its tolerance elsewhere."""
+    lens = [100, 2500 if long else 500, 33, 64]
+    b = Batch(heads(name, g), lens, counts, sizes=[1] * 4, prefix=[50, 300, 33, 1000], seed=15)
+    b.run(groups=False)
+    torch.cuda.synchronize()
+    b.check()
+    want = b.out.clone()
+    b.out.fill_(KEPT)
+    b.run()
+    torch.cuda.synchronize()
+    b.check()
+    assert not same or torch.equal(b.out, want)
+    b.release()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("each,B", [(9, 16), (40, 24)])
 def test_a_long_prefix_of_many_heads(each, B):
     """Heads so many that a workgroup's stretch of the prefix is longer than the positions it looks
