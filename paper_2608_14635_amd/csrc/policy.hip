@@ -691,8 +691,7 @@ constexpr int WHOLE_LOSSES = 512;
 // 192 rows 28.0 and 30.0.
 template <typename T>
 void launch(const PolicyParams& p, hipStream_t s) {
-  // 250 rows of 152064 fp32 logits: 18 pieces held 68.8 us, 20 72.6; bf16 rows of 18 pieces 2 us more
-  constexpr int VEC = Piece<T>::N, MOST = VEC == 8 ? 19 : 18;
+  constexpr int VEC = Piece<T>::N;
   const dim3 nt(PL_NT);
   bool total = p.total;
   const auto whole = [&](auto n) {
@@ -713,11 +712,13 @@ void launch(const PolicyParams& p, hipStream_t s) {
     const auto go = [&](auto h) {
       hipLaunchKernelGGL((policy_rows_kernel<T, decltype(h)::value>), grid, dim3(1024), 0, s, p);
     };
+    // 16 at most, which fill a thread's 128 registers: with 16, 17, 19 and 20 held (those spill) 1024
+    // rows of 151936 bf16 logits take 151, 154, 154 and 159 us, of 200000 194, 196, 204 and 210; 250
+    // rows of 152064 fp32 ones with 16, 18 and 20 67.4, 68.3 and 70.8
     constexpr int LEAST = VEC == 8 ? 8 : 12;
     if (pieces <= LEAST) go(std::integral_constant<int, LEAST>{});
     else if (pieces <= 12) go(std::integral_constant<int, 12>{});
-    else if (pieces <= 16) go(std::integral_constant<int, 16>{});
-    else go(std::integral_constant<int, MOST>{});
+    else go(std::integral_constant<int, 16>{});
   } else {
     const dim3 grid((unsigned)(p.rows * p.chunks));
     hipLaunchKernelGGL((policy_chunk_kernel<T>), grid, nt, 0, s, p);
