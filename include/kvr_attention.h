@@ -4,8 +4,12 @@
  * A trainer samples several answers to one prompt, and agents share a system prompt:
  * their requests' block tables name the same blocks for a common prefix, as
  * kv_rebuild_from (kvr_reuse.h) fills them.  kv_group_attention attends over the arena
- * through such tables and reads a group's common positions once for all its requests,
- * not once for each (but in calls so short that reading is not what they wait for).
+ * through such tables and reads a group's common positions once for many of its requests,
+ * not once for each: for up to 128 pairs of a query row and a q head of one kv head in bf16, 32
+ * in fp32 (16 with head_dim 128).  It is 16 in bf16 too where the arena does not start on a
+ * boundary of 16 bytes or block_size is no multiple of 4, and in both types where the call's
+ * groups have 16 such pairs or fewer on the average.  Calls so short that reading is not what
+ * they wait for read them for each request.
  * kv_append (kvr_append.h) stores the rows it reads.  Without groups it is attention over
  * the arena, one or several query rows a request.  Same conventions as kvr.h (status codes,
  * host/device pointers, void* streams, host-side validation before any device work,
@@ -57,15 +61,16 @@ uint64_t kv_group_attention_workspace_bytes(const kv_model_desc* desc, int32_t n
  *   out          device [rows][nq][d], model dtype, rows out_stride elements apart
  *   workspace    device scratch, on a boundary of 16 bytes; calls in flight at once
  *                need one each
- * Row i attends positions 0 .. its own: out = sum_j p_j v_j, p the softmax of
- * q . k_j / sqrt(d), q head h reading kv head h / (nq/nkv).  Scores, softmax and sums
- * are fp32, the output is rounded once; values next to the largest number do not overflow
- * on the way (below 2^-86 they may count as 0).  Positions in a block whose table entry is
- * outside the arena, and those past max_len or max_blocks_per_req, are left out; a row that
- * is left with no position, or with none whose score is above -infinity, is zero.  What
- * lies at positions that a row does not see changes nothing in it; a key that is not finite
- * makes NaN of the rows that see it (or, with a score of -infinity, nothing), a value that is
- * not finite makes NaN or an infinity of its dim in them.
+ * Row i attends positions 0 .. its own: out = sum_j p_j v_j, p the softmax of q . k_j / sqrt(d),
+ * q head h reading kv head h / (nq/nkv).  Scores, softmax and sums are fp32 (in bf16 models a
+ * weight enters the product with V as two bf16 numbers, which with its exponent's rounding are
+ * off by 2^-16 of it), the output is rounded once; values next to the largest number do not
+ * overflow on the way (below 2^-86 they may count as 0).  Positions in a block whose table entry
+ * is outside the arena, and those past max_len or max_blocks_per_req, are left out; a row that
+ * is left with no position, or with none whose score is above -infinity, is zero.  What lies at
+ * positions that a row does not see changes nothing in it; a key that is not finite makes NaN of
+ * the rows that see it (or, with a score of -infinity, nothing), a value that is not finite
+ * makes NaN or an infinity of its dim in them.
  * Requests may share blocks, not query rows: q_offsets and group_offsets do not decrease.
  * Nothing but the requests' rows of out is written; q and out may be the same memory only as
  * the same rows, with the same stride.  Results do not depend on timing.  The arrays on the

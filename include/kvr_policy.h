@@ -60,9 +60,9 @@ uint64_t kv_policy_loss_workspace_bytes(int64_t rows, int32_t vocab);
  * them.  Elsewhere infinite inputs go the formula's way.  1 - p_t and log p_t are taken
  * from the other tokens' sum, so that for all but certain tokens too they are off by at most
  * (50 + 2 T) 2^-24 of themselves, T the largest log2 e (max x - x_v) that counts, below 150
- * (a few 2^-24 in ordinary rows).  Sums are fp32 over a thread's entries at once or 8192
- * neighbouring ones and joined in fp64, entries below 2^-126 of the largest left out; grad is
- * rounded once; results do not depend on timing.
+ * (a few 2^-24 in ordinary rows).  Sums are fp32 over what a thread takes at once, or over
+ * 8192 neighbouring entries and up to four such parts, and joined in fp64; entries below 2^-126
+ * of the largest are left out.  grad is rounded once; results do not depend on timing.
  * The arrays on the device are read when the call runs there, so a captured call follows
  * their contents.
  *   KV_EINVAL  null arrays, rows or vocab out of range, a stride < vocab, an unknown dtype, a

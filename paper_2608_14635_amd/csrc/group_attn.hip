@@ -14,8 +14,8 @@
 //
 // Bound by memory with few columns: 64 requests of 1004 - 5980 positions in eight groups, 8 kv
 // heads, 667 MB in 130 us (5.1 TB/s; a read reaches 6.0) + 5.8.  With many (48 requests on one
-// prefix of 24011, 240 columns, 297 MB in 84 - 91 + 9) a workgroup's unit of 32 positions and 128
-// columns takes 3500 cycles: 770 of matrix instructions, 1250 of others, the rest are waits for
+// prefix of 24011, 240 columns, 297 MB in 83 - 95 + 9) a workgroup's unit of 32 positions and 128
+// columns takes 3500 cycles: 770 of matrix instructions, some 1300 of others, the rest are waits for
 // each other with two waves a SIMD.  Calls of some 20 us by what follows one another: plan 3,
 // first unit 6, the last merges 3, the second kernel 4 to 7.
 //
@@ -898,7 +898,7 @@ __device__ __forceinline__ void run_shared(const Lists<true>& lists, const Shape
     Fours<POS> fours(p, s, pos0 + x.first * POS, end, wave);
     const int bytes = 3 * (int)p.row_bytes + ROWB, row_off = q * (int)p.row_bytes;
     uint32_t there[RING];  // bits of the units in the ring, oldest first
-    // a unit's loads; past the last the last again, so that waits count the same
+    // a unit's loads; nothing past the last, so that the waits of the last RING - 2 units are for all
     int fetched = x.first;
     const auto fetch = [&](uint32_t& bits) {
       if (fetched < upto) {
@@ -1250,9 +1250,11 @@ struct Sizes {
   int g;
 };
 
-// Columns of an item: the fewest that the average of what shares it fills.  More than 16 go
-// through LDS in bf16, by loads that take rows on boundaries of 16 bytes, four to a block (128 at
-// most: a wave's two tiles, with their sums, fill its registers; 64 gain nothing for what they fit).
+// Columns of an item: the fewest that the average of what shares it fills (the groups' own sizes
+// are known on the device alone; a large group among many small ones gets their narrow items).  More
+// than 16 go through LDS in bf16, by loads that take rows on boundaries of 16 bytes, four to a block
+// (128 at most: a wave's two tiles, with their sums, fill its registers; 64 gain nothing for what
+// they fit).  Other arenas and block sizes have 16, and a prefix's reads up to eight times over.
 int cols_of(const kv_model_desc& d, const Sizes& z, bool fours) {
   const int64_t cols = z.G > 0 ? (z.rows * z.g + z.G - 1) / z.G : z.g * std::min(z.max_query, z.rows);
   if (d.dtype == KV_BF16 && !fours) return 16;

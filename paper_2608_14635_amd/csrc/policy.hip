@@ -18,7 +18,7 @@
 // are some hundred instructions each, which a row's only lane would wait for from memory.
 //
 // Bound by memory where there is much of it: 1024 rows of 151936 bf16 logits with gradient, 622 MB, in
-// 154 us (4.0 TB/s; a copy reaches 4.7), 250 rows of 152064 fp32 ones 304 MB in 69 (4.4), losses
+// 149 us (4.2 TB/s; a copy reaches 4.7), 250 rows of 152064 fp32 ones 304 MB in 68 (4.5), losses
 // of 384 rows of 128256 bf16 logits 98.5 MB in 22.6 (4.4) + 6.2 + 3.8.  By waiting where there is
 // little: 171 rows of 1024 in 5.7 + 1.6.
 #include <algorithm>
@@ -166,10 +166,12 @@ __device__ __forceinline__ double series(const double* c, double x) {
 }
 
 // e^x - 1: x = n ln 2 + r with |r| <= ln 2 / 2, 2^n (e^r - 1) + (2^n - 1), e^r - 1 by its series
-// to r^13 (the next term is below 2^-57 of r).  `one`: e^x instead.
+// to r^13 (the next term is below 2^-57 of r).  `one`: e^x instead.  n ln 2 is taken off by Cody and
+// Waite's two steps: the first part of ln 2 is its first 32 bits, whose product with n is exact (the
+// split that the public fdlibm has too).
 __device__ __forceinline__ double exp_less(double x, bool one) {
   const double n = rint(fmin(fmax(x, -800.0), 800.0) * 1.442695040888963407360);
-  const double r = fma(-n, 1.90821492927058770002e-10, fma(-n, 6.93147180369123816490e-01, x));  // ln 2 in two parts
+  const double r = fma(-n, 1.90821492927058770002e-10, fma(-n, 6.93147180369123816490e-01, x));
   const double s = fma(series<12>(EXP_SERIES, r) * r, r, r);
   const int k = (int)n;
   const double y = ldexp(s, k), z = ldexp(1.0, k);
@@ -619,7 +621,8 @@ __global__ __launch_bounds__(512, 4) void policy_losses_kernel(PolicyParams p) {
 // Long rows with their gradient: a workgroup of 1024 threads to a row, H pieces of a thread in its
 // registers, of which the last four may lie past the row's end, and what is further right read
 // twice.  As pieces go out, those of the workgroup's next row come in.  Of 38 us a row of 151936
-// bf16 logits, sums take 13, the join 10 (it waits for the slowest of 16 waves), gradients 15.
+// bf16 logits (19 pieces held), sums took 13, the join 10 (it waits for the slowest of 16 waves),
+// gradients 15.
 // Read twice, whole, by 256 to 1024 threads: 162 to 182 us, not 154, for 1024 such rows.
 template <typename T, int H>
 __global__ __launch_bounds__(1024, 4) void policy_rows_kernel(PolicyParams p) {
@@ -679,7 +682,7 @@ int chunks_of(int vocab) { return (vocab + PL_CHUNK - 1) / PL_CHUNK; }
 
 // With their gradient, rows from which on each is given to one workgroup.  In us, so and by
 // chunks: of 65536 bf16 logits 96 rows 17.5 and 17.2, 128 rows 18.2 and 19.1, 256 rows 21.1 and
-// 26.1; of 152064 128 rows 29.9 and 28.8, 160 rows 31.7 and 34.1; of 128256 fp32 logits 96 rows
+// 26.1; of 152064 128 rows 28.6 and 28.8, 160 rows 31.7 and 34.1; of 128256 fp32 logits 96 rows
 // 32.1 and 31.0, 128 rows 35.5 and 43.5.
 constexpr int WHOLE_ROWS = 128, CUS = 256;
 // Losses alone of middling rows go by chunks above this many: of 18000 bf16 logits, whole and by
